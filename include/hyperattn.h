@@ -71,7 +71,8 @@ typedef enum hyperattn_status {
 
 typedef enum hyperattn_dtype {
   HYPERATTN_BF16 = 0,
-  HYPERATTN_FP32 = 1
+  HYPERATTN_FP32 = 1,
+  HYPERATTN_FP16 = 2                 /* the serving entry points only (cache and packed prompts) */
 } hyperattn_dtype;
 
 /* Optional device buffers that receive the intermediate results of the integer stages
@@ -314,6 +315,107 @@ int hyperattn_sortlsh_noalloc(const void* x, int n, int d, int hash_bits, uint64
 int hyperattn_alpha(const void* q, const void* k, int B, int H, int n, int n_k, int d, float softmax_scale,
                     int causal, int skip_cols, float* alpha, void* workspace, size_t workspace_bytes, void* stream);
 int hyperattn_alpha_workspace_bytes(int B, int H, int n, int n_k, size_t* bytes);
+
+/* ---- Serving: packed prompts and a paged 4-bit cache ---------------------------------------------
+ * What a program that generates text needs beside the attention of long prompts: exact attention over packed
+ * prompts of different lengths (layers or prompts that are not approximated), a place for the keys and values of
+ * long contexts, the attention of the next token over it, and the bookkeeping of its pages.  Heads may be
+ * grouped: q_heads is a multiple of kv_heads, query head h reads key head h / (q_heads / kv_heads).  d in {64, 128}.
+ * dtype is HYPERATTN_BF16 or HYPERATTN_FP16 (queries, keys, values), out_dtype the same or HYPERATTN_FP32.  Lengths,
+ * offsets, tables and slots are device arrays of int32, read by the kernels: no entry point looks at them on the host,
+ * synchronises or allocates, so every call can be captured in a graph.  Calls without rows return at once.
+ *
+ * The cache: pages of page_tokens tokens (a multiple of 16, at most 1024), uint8 [num_pages, kv_heads,
+ * page_tokens / 16, 20 d].  A block of 20 d bytes holds K and V of 16 tokens of one head.  Every row of d numbers is
+ * cut into groups of 32: with lo, hi the group's smallest and largest, scale s = fp16((hi - lo) / 15), minimum
+ * m = fp16(lo), code c = round-to-even((x - m) * (1 / s)) cut to 0..15 (0 where s = 0), all in fp32; the number that is
+ * held is m + s c.  A group with a number that is not finite, or whose s or m is not a finite fp16, is held as NaN.  Bytes
+ * of a block, t = token in the block, x = coordinate, o = x / 8 % 4, w = x / 32, lane = t % 8 * 4 + o:
+ *   K codes   word (4 bytes) at d = 128: (t / 8) * 512 + lane * 16 + w * 4; d = 64: lane * 16 + t / 8 * 8 + w * 4;
+ *             coordinate e = x % 8 is the nibble (e % 2) * 4 + e / 2 of that word
+ *   V codes   from byte 8 d: with u = x / 16, byte (u / 4) * 512 + (x % 8 * 4 + t % 8 / 2) * 16 + u % 4 * 4
+ *             + t % 2 * 2 + t / 8, low nibble for x % 16 < 8, high nibble otherwise
+ *   K scales  from byte 16 d: fp16 s at (t / 2 * (d / 32) + w) * 8 + t % 2 * 2, fp16 m 4 bytes further
+ *   V scales  from byte 18 d, alike.
+ * (One 16-byte load of a thread is then its share of an operand of the tensor cores, for K and for V.)  A slot is
+ * page * page_tokens + position in the page; num_pages * page_tokens < 2^31.  A block table is int32
+ * [requests, table_width]; entries that are no page (-1) hold no tokens: they are not written, not attended to, and
+ * read as zeros. */
+typedef struct hyperattn_cache {
+  void* pages;             /* device, 16-byte aligned */
+  int num_pages, page_tokens, kv_heads, d;
+} hyperattn_cache;
+
+/* One scheduling step of the cache's pages.  Request r has lengths[r] tokens in the cache and brings new_tokens[r] more
+ * (0: none; negative: the request has ended).  The free pages are a stack, free_pages[0 .. n_free - 1].  The pages of ended
+ * requests are put on it, in order of request and position; then requests are served in order: request r needs as many
+ * pages as its new tokens reach beyond those it has, and is admitted if it needs none, or if its table row has room and
+ * its pages and those of all earlier requests (that have room) are on the stack.  Pages are taken from the top.
+ * The tokens of all requests follow each other in a packed batch of `rows` rows (what is beyond it is cut off, rows
+ * beyond the last token get -1).  Outputs (they must not alias the inputs):
+ *   slots, positions  [rows]          slot and position in the request; -1 for tokens that are not admitted
+ *   cu_new            [requests + 1]  first row of each request's new tokens
+ *   lengths_out       [requests]      tokens after the step (0: ended; unchanged: not admitted)
+ *   cu_lengths        [requests + 1]  their running sum
+ *   table_out         [requests, table_width], unused entries -1
+ *   free_out, n_free_out              the stack after the step, [num_free], unused entries -1
+ * requests <= HYPERATTN_PLAN_MAX_REQUESTS; table_width * page_tokens < 2^31. */
+#define HYPERATTN_PLAN_MAX_REQUESTS 4096
+typedef struct hyperattn_plan {
+  const int32_t *lengths, *new_tokens, *table, *free_pages, *n_free;
+  int requests, table_width, num_free, page_tokens, rows;
+  int32_t *slots, *positions, *cu_new, *cu_lengths, *lengths_out, *table_out, *free_out, *n_free_out;
+  void* stream;
+} hyperattn_plan;
+int hyperattn_cache_plan(const hyperattn_plan* p);
+
+/* Puts row i of k and v ([rows, kv_heads, d]; strides in elements, multiples of 8, d contiguous) into slot slots[i]; rows
+ * whose slot is negative or beyond the cache are left out.  Slots of one call must differ. */
+int hyperattn_cache_store(const hyperattn_cache* cache, const void* k, const void* v, int dtype, int rows, long long k_row_stride,
+                          long long k_head_stride, long long v_row_stride, long long v_head_stride, const int32_t* slots, void* stream);
+
+/* K and V of cached tokens as contiguous [rows, kv_heads, d] of dtype (BF16, FP16 or FP32).  Rows cu[r] .. cu[r + 1] - 1 are
+ * tokens first[r], first[r] + 1, ... of request r (first = NULL: from 0 on); rows beyond cu[requests] and tokens whose page
+ * does not exist are zeros. */
+int hyperattn_cache_read(const hyperattn_cache* cache, const int32_t* table, int requests, int table_width, const int32_t* cu,
+                         const int32_t* first, int rows, void* k, void* v, int dtype, void* stream);
+
+/* Attention of one query token a request over its cached tokens 0 .. lengths[r] - 1:
+ *   out[r, h] = sum_j p_j v_j,  p = softmax_j(softmax_scale <q[r, h], k_j>),  lse[r, h] = ln sum_j exp(softmax_scale <q, k_j>).
+ * A request without tokens gets out = 0 and lse = -infinity.  Queries enter the products as fp16 (after a power of two that
+ * brings the largest entry of a head near one), weights and values too, sums are fp32. */
+typedef struct hyperattn_cache_attention_params {
+  hyperattn_cache cache;
+  const void* q;           /* [requests, q_heads, d], strides in elements (multiples of 8) */
+  long long q_row_stride, q_head_stride;
+  void* out;               /* [requests, q_heads, d] contiguous, out_dtype */
+  float* lse;              /* [requests, q_heads] */
+  const int32_t *table, *lengths;
+  int requests, table_width, q_heads, dtype, out_dtype;
+  float softmax_scale;     /* <= 0 selects 1/sqrt(d) */
+  void* workspace;         /* device scratch of hyperattn_cache_attention_workspace_bytes bytes; its contents do not matter */
+  size_t workspace_bytes;
+  void* stream;
+} hyperattn_cache_attention_params;
+int hyperattn_cache_attention(const hyperattn_cache_attention_params* p);
+int hyperattn_cache_attention_workspace_bytes(const hyperattn_cache_attention_params* p, size_t* bytes);
+
+/* Exact attention over packed prompts.  Rows cu_q[r] .. cu_q[r + 1] - 1 of q are request r's queries, rows cu_k[r] ..
+ * cu_k[r + 1] - 1 of k and v its keys.  causal: the last query sees all keys, every earlier one a key less (so a request
+ * with more keys than queries continues a cached prompt; with fewer, the first queries see none).  A query that sees
+ * no key gets out = 0, lse = -infinity; keys that a query does not see have no influence on it, whatever they hold.
+ * Rows beyond cu_q[requests] are not written. */
+typedef struct hyperattn_prompt_params {
+  const void *q, *k, *v;   /* [q_rows, q_heads, d], [k_rows, kv_heads, d]; strides in elements (multiples of 8) */
+  long long q_row_stride, q_head_stride, k_row_stride, k_head_stride, v_row_stride, v_head_stride;
+  void* out;               /* [q_rows, q_heads, d] contiguous, out_dtype */
+  float* lse;              /* [q_rows, q_heads] */
+  const int32_t *cu_q, *cu_k;
+  int requests, q_rows, k_rows, q_heads, kv_heads, d, causal, dtype, out_dtype;
+  float softmax_scale;
+  void* stream;
+} hyperattn_prompt_params;
+int hyperattn_prompt_attention(const hyperattn_prompt_params* p);
 
 /* Frees the private workspaces and profiling events of every device. */
 int hyperattn_release(void);

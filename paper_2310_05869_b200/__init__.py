@@ -16,3 +16,12 @@ from .binding import (  # noqa: F401
     version,
     workspace_bytes,
 )
+from .serving import (  # noqa: F401
+    CachePlan,
+    cache_attention,
+    cache_pages,
+    cache_plan,
+    cache_read,
+    cache_store,
+    prompt_attention,
+)

@@ -20,7 +20,9 @@ EXPORTS = ["hyperattn_forward", "hyperattn_forward_ex", "hyperattn_forward_host"
            "hyperattn_get_projections", "hyperattn_last_device_status", "hyperattn_profile_enable",
            "hyperattn_profile_reset", "hyperattn_profile_read", "hyperattn_release",
            "hyperattn_status_string", "hyperattn_version", "hyperattn_sortlsh_noalloc",
-           "hyperattn_alpha", "hyperattn_alpha_workspace_bytes", "hyperattn_get_node_projections"]
+           "hyperattn_alpha", "hyperattn_alpha_workspace_bytes", "hyperattn_get_node_projections",
+           "hyperattn_cache_plan", "hyperattn_cache_store", "hyperattn_cache_read", "hyperattn_cache_attention",
+           "hyperattn_cache_attention_workspace_bytes", "hyperattn_prompt_attention"]
 
 
 class HyperAttnError(RuntimeError):
