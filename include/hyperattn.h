@@ -406,7 +406,8 @@ int hyperattn_cache_attention_workspace_bytes(const hyperattn_cache_attention_pa
  * no key gets out = 0, lse = -infinity; keys that a query does not see have no influence on it, whatever they hold.
  * Rows beyond cu_q[requests] are not written. */
 typedef struct hyperattn_prompt_params {
-  const void *q, *k, *v;   /* [q_rows, q_heads, d], [k_rows, kv_heads, d]; strides in elements (multiples of 8) */
+  const void *q, *k, *v;   /* [q_rows, q_heads, d], [k_rows, kv_heads, d]; strides in elements (multiples of 8, not 0);
+                              16-byte aligned.  q_heads / kv_heads <= 128 */
   long long q_row_stride, q_head_stride, k_row_stride, k_head_stride, v_row_stride, v_head_stride;
   void* out;               /* [q_rows, q_heads, d] contiguous, out_dtype */
   float* lse;              /* [q_rows, q_heads] */

@@ -536,6 +536,25 @@ int forward_impl(const hyperattn_params& p, int seg0 = 0, const hyperattn_grads*
 }
 
 }  // namespace
+
+// The status word for kernels outside this file: their bounded waits report to it.
+int device_status_word(cudaStream_t st, int** status) {
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess) return HYPERATTN_CUDA_ERROR;
+  try {
+    std::lock_guard<std::mutex> lock(g_mu);
+    DeviceState& ds = g_dev[dev];
+    if (!ds.status) {
+      cudaStreamCaptureStatus cap = cudaStreamCaptureStatusNone;
+      if (cudaStreamIsCapturing(st, &cap) != cudaSuccess) { cudaGetLastError(); cap = cudaStreamCaptureStatusNone; }
+      if (cap != cudaStreamCaptureStatusNone) return HYPERATTN_WORKSPACE_TOO_SMALL;
+      if (cudaMalloc(&ds.status, 256) != cudaSuccess) { ds.status = nullptr; return HYPERATTN_CUDA_ERROR; }
+      if (cudaMemset(ds.status, 0, 256) != cudaSuccess) return HYPERATTN_CUDA_ERROR;
+    }
+    *status = ds.status;
+  } catch (...) { return HYPERATTN_CUDA_ERROR; }
+  return HYPERATTN_OK;
+}
 }  // namespace hyperattn
 
 using namespace hyperattn;

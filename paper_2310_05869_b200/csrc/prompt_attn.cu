@@ -1,6 +1,25 @@
-// Exact attention over packed prompts with grouped heads.
+// Exact attention over packed prompts with grouped heads, on the 5th-generation tensor cores.
+//
+// A work item is a key head and two neighbouring query tiles of a request.  A tile is 128 rows: 128 / G tokens with all G query heads
+// that read the key head, so that the keys of a group are fetched once and a tile of many heads sees few keys in vain.  A
+// CTA walks over the tiles of 128 keys from the last one that is seen down to the first:
+//     S_i = Q_i K^T           tcgen05.mma, operands in 128B-swizzled shared memory (TMA boxes), S_i in TMEM
+//     P_i = exp2(c S_i - m)   softmax warpgroup i, a thread a row; P_i goes over S_i in the inputs' type
+//     O_i += P_i V            tcgen05.mma, P_i read from TMEM
+// The tensor pipe works for one query tile while the other one's weights are made.  The reference m of a row is the maximum of its first
+// tile and moves when it is exceeded by more than 2^8, and then O is multiplied in TMEM; tiles with keys that a row does not see are
+// the first ones, so masks cost the later ones nothing.
+//
+// Values of keys that a row does not see are multiplied with zeros, which is not nothing where they are infinite or NaN.  Those beyond a
+// request's end are zeros in shared memory; those of later tokens show as a result that is not finite, and such a row is done over, key by key
+// over those that it does see.
+//
+// Warp roles (384 threads): 0-3 and 4-7 softmax and results of query tile 0 and 1, 8 issues the products (and allocates TMEM), 9 loads, 10 prepares items.
+// Every wait is bounded: a CTA that gives up raises the device status word, drains its copies, frees its TMEM and returns.
 #include <cstdio>
+#include <type_traits>
 #include "serving.cuh"
+#include "tc_util.cuh"
 
 namespace hyperattn {
 namespace {
@@ -15,15 +34,9 @@ struct PromptArgs {
   float scale_log2;
 };
 
-__device__ __forceinline__ float ex2f(float x) {
-  float y;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-  return y;
-}
-
 // A warp and one query row of one head: a lane has D / 32 coordinates, the keys follow each other.
 template <int D, class T>
-__device__ __forceinline__ void attend_row(const PromptArgs& a, int row, int head, int key0, int keys) {
+__device__ __noinline__ void attend_row(const PromptArgs& a, int row, int head, int key0, int keys) {
   constexpr int E = D / 32;                                // coordinates of a lane
   const int lane = threadIdx.x & 31, kv = head / (a.q_heads / a.kv_heads);
   auto load = [&](const void* base, size_t at, float (&x)[E]) {
@@ -45,12 +58,12 @@ __device__ __forceinline__ void attend_row(const PromptArgs& a, int row, int hea
     for (int w = 16; w; w >>= 1) s += __shfl_xor_sync(0xffffffffu, s, w);
     s *= a.scale_log2;
     if (s > ref) {
-      const float f = ex2f(ref - s);
+      const float f = ex2(ref - s);
       sum *= f; ref = s;
 #pragma unroll
       for (int i = 0; i < E; ++i) o[i] *= f;
     }
-    const float p = ex2f(s - (ref == -INFINITY ? 0.f : ref));
+    const float p = ex2(s - (ref == -INFINITY ? 0.f : ref));
     sum += p;
 #pragma unroll
     for (int i = 0; i < E; ++i) o[i] = fmaf(p, v[i], o[i]);
@@ -67,14 +80,462 @@ __device__ __forceinline__ void attend_row(const PromptArgs& a, int row, int hea
   if (lane == 0) a.lse[at] = sum == 0.f ? -INFINITY : (ref + log2f(sum)) * 0.6931471805599453f;
 }
 
+struct alignas(64) PromptMaps {
+  CUtensorMap q, k, v;
+};
+
+constexpr int kTileRows = 128, kTileKeys = 128;
+constexpr int kThreads = 384;
+constexpr float kMoveAt = 8.f;          // octaves a row's scores may exceed its reference before that moves (fp16 weights end at 2^16)
+
+template <int D>
+struct Cfg {
+  static constexpr uint32_t kSlab = 128 * 128;                         // 64 columns of 128 rows
+  static constexpr uint32_t kTile = (D / 64) * kSlab;
+  static constexpr int kStages = D == 64 ? 10 : 5;                     // tiles of K or V on their way
+  static constexpr uint32_t kOffQ = 0, kOffRing = 2 * kTile, kOffMisc = kOffRing + kStages * kTile;
+  static constexpr uint32_t kSmem = kOffMisc + 1024;
+};
+
+struct Item {
+  int end;                               // no more items
+  int row0;                              // first query row of the pair's first token
+  int tokens[2];                         // tokens of either tile
+  int tiles[2], most;                    // key tiles of either, of the longer one
+  int key0, keys;                        // first key row, keys of the request
+  int last;                              // last key that the pair's first token sees (may be negative)
+  int kv;
+};
+
+// Item `index`, decoded by a converged warp.  Items are ordered by request, in it from the last query on (the longest first), key heads next to each other.
+__device__ __forceinline__ Item item_at(const PromptArgs& a, int index, int tile_tokens) {
+  const int lane = threadIdx.x & 31;
+  Item it = {};
+  it.end = 1;
+  const int block = index / a.kv_heads, pair_tokens = 2 * tile_tokens;
+  it.kv = index - block * a.kv_heads;
+  int before = 0;
+  for (int r0 = 0; r0 < a.requests; r0 += 32) {
+    const int r = r0 + lane;
+    int q0 = 0, nq = 0;
+    if (r < a.requests) {
+      q0 = min(max(a.cu_q[r], 0), a.q_rows);
+      nq = min(max(a.cu_q[r + 1], q0), a.q_rows) - q0;
+    }
+    const int mine = (nq + pair_tokens - 1) / pair_tokens;
+    int sum = mine;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) { const int y = __shfl_up_sync(0xffffffffu, sum, o); if (lane >= o) sum += y; }
+    const unsigned hit = __ballot_sync(0xffffffffu, before + sum > block);
+    if (hit) {
+      const int src = __ffs(hit) - 1;
+      const int first = before + __shfl_sync(0xffffffffu, sum - mine, src), blocks = __shfl_sync(0xffffffffu, mine, src);
+      q0 = __shfl_sync(0xffffffffu, q0, src);
+      nq = __shfl_sync(0xffffffffu, nq, src);
+      const int req = r0 + src, tok = (blocks - 1 - (block - first)) * pair_tokens;
+      const int k0 = min(max(a.cu_k[req], 0), a.k_rows);
+      it.end = 0;
+      it.key0 = k0;
+      it.keys = min(max(a.cu_k[req + 1], k0), a.k_rows) - k0;
+      it.row0 = q0 + tok;
+      it.last = a.causal ? min(it.keys - 1, tok + it.keys - nq) : it.keys - 1;
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const int left = nq - tok - i * tile_tokens;
+        it.tokens[i] = min(max(left, 0), tile_tokens);
+        const int seen = a.causal ? it.last + i * tile_tokens + it.tokens[i] : it.keys;       // keys that the tile's last token sees
+        it.tiles[i] = it.tokens[i] > 0 && seen > 0 ? (min(seen, it.keys) + kTileKeys - 1) / kTileKeys : 0;
+      }
+      it.most = max(it.tiles[0], it.tiles[1]);
+      return it;
+    }
+    before += __shfl_sync(0xffffffffu, sum, 31);
+  }
+  return it;
+}
+
+template <class T> __device__ __forceinline__ constexpr uint32_t type_bits() { return sizeof(T) && std::is_same<T, __nv_bfloat16>::value ? (1u << 7) | (1u << 10) : 0u; }
+
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float d;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+  return d;
+}
+
+// O of a row times alpha, in TMEM (rare).  All lanes together.
+__device__ __noinline__ void rescale_o(uint32_t addr, int cols, float alpha) {
+  uint32_t r[16];
+  for (int c = 0; c < cols; c += 16) {
+    tmem_ld16_issue(addr + c, r);
+    tmem_ld16_wait(r);
+#pragma unroll
+    for (int e = 0; e < 16; ++e) r[e] = __float_as_uint(__uint_as_float(r[e]) * alpha);
+    tmem_st16(addr + c, r);
+  }
+  tmem_wait_st();
+}
+
 template <int D, class T>
-__global__ void __launch_bounds__(256) prompt_rows_kernel(PromptArgs a) {
+__global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__ PromptMaps maps, int group, int tile_tokens, int* status) {
+  using C = Cfg<D>;
+  extern __shared__ __align__(1024) uint8_t smem[];
+  const uint32_t ubase = smem_u32(smem);
+  Item* s_item = reinterpret_cast<Item*>(smem + C::kOffMisc);                    // [2]
+  uint32_t* s_tmem = reinterpret_cast<uint32_t*>(smem + C::kOffMisc + 256);
+  volatile int* s_abort = reinterpret_cast<volatile int*>(smem + C::kOffMisc + 260);
+  const uint32_t bar0 = ubase + C::kOffMisc + 272;
+  auto bar_item = [&](int set) { return bar0 + 8 * set; };                       // an item's description is written
+  auto bar_itemfree = [&](int set) { return bar0 + 16 + 8 * set; };              // everybody is done with it
+  const uint32_t bar_q = bar0 + 32, bar_qfree = bar0 + 40;                       // Q has landed; no product reads it any more
+  auto bar_s = [&](int i) { return bar0 + 48 + 8 * i; };                         // S_i written
+  auto bar_p = [&](int i) { return bar0 + 64 + 8 * i; };                         // P_i written
+  auto bar_o = [&](int i) { return bar0 + 80 + 8 * i; };                         // O_i complete
+  auto bar_ofree = [&](int i) { return bar0 + 96 + 8 * i; };                     // O_i read
+  auto bar_full = [&](int s) { return bar0 + 112 + 8 * s; };
+  auto bar_empty = [&](int s) { return bar0 + 112 + 8 * (C::kStages + s); };
+  const int tid = threadIdx.x, lane = tid & 31;
+  const int warp = __shfl_sync(0xffffffffu, tid >> 5, 0);
+
+  // (a launch in which a wait gave up drains quickly; read before wait_for_stream() on purpose)
+  if (tid == 0) *s_abort = *reinterpret_cast<volatile int*>(status);
+  __syncthreads();
+  if (*s_abort) return;
+  __syncthreads();
+  if (tid == 0) {
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(bar_item(i), 1);
+      mbar_init(bar_itemfree(i), 256 + 2);
+      mbar_init(bar_s(i), 1);
+      mbar_init(bar_p(i), 128);
+      mbar_init(bar_o(i), 1);
+      mbar_init(bar_ofree(i), 128);
+    }
+    mbar_init(bar_q, 1);
+    mbar_init(bar_qfree, 1);
+    for (int s = 0; s < C::kStages; ++s) { mbar_init(bar_full(s), 1); mbar_init(bar_empty(s), 1); }
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == 8) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(s_tmem)) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = __shfl_sync(0xffffffffu, *s_tmem, 0);
   wait_for_stream();
-  const int head = threadIdx.x / 32 + 8 * blockIdx.y, row = blockIdx.x;
-  const int r = upper_bound(a.cu_q + 1, a.requests, row);
-  if (head >= a.q_heads || r >= a.requests) return;
-  const int nq = a.cu_q[r + 1] - a.cu_q[r], nk = a.cu_k[r + 1] - a.cu_k[r];
-  attend_row<D, T>(a, row, head, a.cu_k[r], a.causal ? max(0, nk - (nq - 1 - (row - a.cu_q[r]))) : nk);
+  // TMEM columns: S_0, S_1 (128 each), O_0, O_1
+  auto item_wait = [&](int it, auto site) { return warp_wait<decltype(site)::value>(bar_item(it & 1), (it >> 1) & 1, s_abort, status); };
+
+  if (warp < 8) {
+    // ================= softmax and results of query tile i: a thread a row =============================
+    const int i = warp >> 2, row = tid & 127;
+    const uint32_t lane_addr = tmem + ((uint32_t)((warp & 3) * 32) << 16);
+    const uint32_t scol = lane_addr + kTileKeys * i, ocol = lane_addr + 256 + 128 * i;
+    const int token = row / group, head = row - token * group;
+    int done = 0;                        // key tiles of this query tile so far
+    int items = 0;                       // items in which it had any
+    bool ok = true;
+    for (int it = 0; ok; ++it) {
+      ok = item_wait(it, std::integral_constant<int, 0>{});
+      if (!ok) break;
+      const Item d = s_item[it & 1];
+      if (d.end) break;
+      const int tiles = i ? d.tiles[1] : d.tiles[0], tokens = i ? d.tokens[1] : d.tokens[0];
+      const int tok = i * tile_tokens + token;                                   // in the pair
+      const int limit = a.causal ? min(d.last + tok, d.keys - 1) : d.keys - 1;  // last key that the row sees
+      const int least = a.causal ? min(d.last + i * tile_tokens, d.keys - 1) : d.keys - 1;       // the tile's first token
+      float ref = -INFINITY;
+      uint64_t sum2 = 0;
+      for (int n = 0; n < tiles && ok; ++n) {
+        const int j = tiles - 1 - n;
+        ok = warp_wait<1>(bar_s(i), (done + n) & 1, s_abort, status);
+        if (!ok) break;
+        tc_fence_after();
+        uint32_t r[4][32];
+#pragma unroll
+        for (int c = 0; c < 4; ++c) tmem_ld32_issue(scol + 32 * c, r[c]);
+#pragma unroll
+        for (int c = 0; c < 4; ++c) tmem_ld32_wait(r[c]);
+        if (j * kTileKeys + kTileKeys - 1 > least) {
+          const int rel = limit - j * kTileKeys;
+#pragma unroll
+          for (int c = 0; c < 4; ++c)
+#pragma unroll
+            for (int e = 0; e < 32; ++e)
+              if (32 * c + e > rel) r[c][e] = 0xff800000u;
+        }
+        float m[4];
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          m[c] = max3(__uint_as_float(r[c][0]), __uint_as_float(r[c][1]), __uint_as_float(r[c][2]));
+#pragma unroll
+          for (int e = 3; e < 31; e += 2) m[c] = max3(m[c], __uint_as_float(r[c][e]), __uint_as_float(r[c][e + 1]));
+          m[c] = fmaxf(m[c], __uint_as_float(r[c][31]));
+        }
+        const float top = fmaxf(max3(m[0], m[1], m[2]), m[3]) * a.scale_log2;
+        const bool move = top > ref + kMoveAt;
+        if (__any_sync(0xffffffffu, move)) {
+          // (S of this tile is there, so the products before it are done; the next one on O waits for this P)
+          float alpha = 1.f;
+          if (move) { alpha = ex2(ref - top); ref = top; }
+          sum2 = fmul2(sum2, pack_f2(alpha, alpha));
+          if (n > 0) rescale_o(ocol, D, alpha);
+        }
+        const float off = ref == -INFINITY ? 0.f : -ref;
+        const uint64_t sc2 = pack_f2(a.scale_log2, a.scale_log2), off2 = pack_f2(off, off);
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          uint32_t p[16];
+#pragma unroll
+          for (int e = 0; e < 16; ++e) {
+            const uint64_t x2 = ffma2(pack_u2(r[c][2 * e], r[c][2 * e + 1]), sc2, off2);
+            float x, y;
+            unpack_f2(x2, x, y);
+            x = ex2(x); y = ex2(y);
+            sum2 = fadd2(sum2, pack_f2(x, y));
+            p[e] = from_float2<T>(x, y);
+          }
+          tmem_st16(scol + 16 * c, p);
+        }
+        tmem_wait_st();
+        tc_fence_before();
+        mbar_arrive(bar_p(i));
+      }
+      if (!ok) break;
+      done += tiles;
+      // ---- results ----
+      float s0, s1;
+      unpack_f2(sum2, s0, s1);
+      const float sum = s0 + s1, inv = sum == 0.f ? 0.f : 1.f / sum;
+      const bool mine = token < tokens && token < tile_tokens;
+      const size_t at = (size_t)(d.row0 + tok) * a.q_heads + d.kv * group + head;
+      bool finite = true;
+      if (tiles > 0) {
+        ok = warp_wait<2>(bar_o(i), items & 1, s_abort, status);
+        if (!ok) break;
+        tc_fence_after();
+#pragma unroll
+        for (int c = 0; c < D / 32; ++c) {
+          uint32_t o[32];
+          tmem_ld32_issue(ocol + 32 * c, o);
+          tmem_ld32_wait(o);
+#pragma unroll
+          for (int e = 0; e < 32; ++e) {
+            const float x = __uint_as_float(o[e]) * inv;
+            finite = finite && fabsf(x) < INFINITY;
+            o[e] = __float_as_uint(x);
+          }
+          if (mine) {
+            if (a.out_kind == HYPERATTN_FP32) {
+              float4* to = reinterpret_cast<float4*>(reinterpret_cast<float*>(a.out) + at * D + 32 * c);
+#pragma unroll
+              for (int e = 0; e < 8; ++e)
+                to[e] = make_float4(__uint_as_float(o[4 * e]), __uint_as_float(o[4 * e + 1]), __uint_as_float(o[4 * e + 2]), __uint_as_float(o[4 * e + 3]));
+            } else {
+              uint4* to = reinterpret_cast<uint4*>(reinterpret_cast<T*>(a.out) + at * D + 32 * c);
+#pragma unroll
+              for (int e = 0; e < 4; ++e) {
+                uint32_t w[4];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) w[k] = from_float2<T>(__uint_as_float(o[8 * e + 2 * k]), __uint_as_float(o[8 * e + 2 * k + 1]));
+                to[e] = make_uint4(w[0], w[1], w[2], w[3]);
+              }
+            }
+          }
+        }
+        tc_fence_before();
+        mbar_arrive(bar_ofree(i));
+        ++items;
+        if (mine) a.lse[at] = sum == 0.f ? -INFINITY : (ref + log2f(sum)) * 0.6931471805599453f;
+      } else if (mine) {
+        a.lse[at] = -INFINITY;
+        const int bytes = D * (a.out_kind == HYPERATTN_FP32 ? 4 : 2);
+        for (int e = 0; e < bytes; e += 16) *reinterpret_cast<uint4*>(reinterpret_cast<char*>(a.out) + at * bytes + e) = make_uint4(0, 0, 0, 0);
+      }
+      // rows that are not finite: over again, over the keys that they see
+      for (unsigned bad = __ballot_sync(0xffffffffu, mine && tiles > 0 && !finite); bad; bad &= bad - 1) {
+        const int src = __ffs(bad) - 1;
+        const int t = __shfl_sync(0xffffffffu, tok, src), h = __shfl_sync(0xffffffffu, head, src), last = __shfl_sync(0xffffffffu, limit, src);
+        __syncwarp();
+        attend_row<D, T>(a, d.row0 + t, d.kv * group + h, d.key0, last + 1);
+      }
+      mbar_arrive(bar_itemfree(it & 1));
+    }
+  } else if (warp == 8) {
+    // ================= products ============================================================================
+    const bool el = elect_one();
+    constexpr uint32_t idesc_s = (1u << 4) | type_bits<T>() | ((kTileKeys >> 3) << 17) | ((128u >> 4) << 24);
+    constexpr uint32_t idesc_o = (1u << 4) | type_bits<T>() | (1u << 16) | ((uint32_t)(D >> 3) << 17) | ((128u >> 4) << 24);
+    constexpr uint32_t desc_hi = (1024u >> 4) | (1u << 14) | (2u << 29);
+    const uint32_t dq_lo = ((ubase + C::kOffQ) >> 4) | (1u << 16);
+    const uint32_t dk_lo = ((ubase + C::kOffRing) >> 4) | (1u << 16);
+    const uint32_t dv_lo = ((ubase + C::kOffRing) >> 4) | ((C::kSlab >> 4) << 16);
+    int ring = 0;                        // tiles of K and V before this item
+    int done[2] = {0, 0}, items[2] = {0, 0}, qitems = 0;
+    bool ok = true;
+    for (int it = 0; ok; ++it) {
+      ok = item_wait(it, std::integral_constant<int, 3>{});
+      if (!ok) break;
+      const Item& d = s_item[it & 1];
+      auto uni = [&](int x) { return __shfl_sync(0xffffffffu, x, 0); };
+      const bool end = uni(d.end) != 0;
+      const int most = uni(d.most), tiles[2] = {uni(d.tiles[0]), uni(d.tiles[1])};
+      __syncwarp();
+      if (el) mbar_arrive(bar_itemfree(it & 1));
+      if (end) break;
+      if (most == 0) continue;
+      ok = warp_wait<4>(bar_q, qitems & 1, s_abort, status);
+      ++qitems;
+      if (!ok) break;
+      auto stage_of = [&](int j, int v) { return ring + 2 * (most - 1 - j) + v; };
+      auto wait_tile = [&](int g) {
+        if (ok) ok = warp_wait<5>(bar_full(g % C::kStages), (g / C::kStages) & 1, s_abort, status);
+      };
+      auto scores = [&](int i, int j) {
+        const uint32_t k_lo = dk_lo + (uint32_t)(stage_of(j, 0) % C::kStages) * (C::kTile >> 4), q_lo = dq_lo + i * (C::kTile >> 4);
+        if (el) {
+#pragma unroll
+          for (int ks = 0; ks < D / 16; ++ks) {
+            const uint32_t step = ((ks >> 2) * C::kSlab + (ks & 3) * 32) >> 4;
+            mma_ss2(tmem + kTileKeys * i, q_lo + step, k_lo + step, desc_hi, idesc_s, ks > 0);
+          }
+          umma_commit(bar_s(i));
+        }
+      };
+      // scores of the first key tile
+      wait_tile(stage_of(most - 1, 0));
+      if (!ok) break;
+      tc_fence_after();
+      for (int i = 0; i < 2; ++i)
+        if (tiles[i] == most) scores(i, most - 1);
+      if (el) {
+        umma_commit(bar_empty(stage_of(most - 1, 0) % C::kStages));
+        if (most == 1) umma_commit(bar_qfree);
+      }
+      for (int j = most - 1; j >= 0 && ok; --j) {
+        wait_tile(stage_of(j, 1));
+        if (j > 0) wait_tile(stage_of(j - 1, 0));
+        const uint32_t v_lo = dv_lo + (uint32_t)(stage_of(j, 1) % C::kStages) * (C::kTile >> 4);
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          if (ok && j < tiles[i]) {
+            if (j == tiles[i] - 1 && items[i] > 0) ok = warp_wait<6>(bar_ofree(i), (items[i] - 1) & 1, s_abort, status);
+            if (ok) ok = warp_wait<7>(bar_p(i), (done[i] + tiles[i] - 1 - j) & 1, s_abort, status);
+            if (ok) {
+              tc_fence_after();
+              if (el) {
+#pragma unroll
+                for (int kk = 0; kk < kTileKeys / 16; ++kk)
+                  mma_ts2(tmem + 256 + 128 * i, tmem + kTileKeys * i + kk * 8, v_lo + kk * (2048 >> 4), desc_hi, idesc_o, kk > 0 || j < tiles[i] - 1);
+                if (j == 0) umma_commit(bar_o(i));
+              }
+            }
+          }
+          if (ok && i == 1 && el) umma_commit(bar_empty(stage_of(j, 1) % C::kStages));
+          if (ok && j > 0 && j - 1 < tiles[i]) scores(i, j - 1);
+        }
+        if (ok && j > 0 && el) {
+          umma_commit(bar_empty(stage_of(j - 1, 0) % C::kStages));
+          if (j == 1) umma_commit(bar_qfree);
+        }
+      }
+      ring += 2 * most;
+      for (int i = 0; i < 2; ++i) { done[i] += tiles[i]; items[i] += tiles[i] > 0; }
+    }
+    __syncwarp();
+  } else if (warp == 9) {
+    // ================= loads ===============================================================================
+    bool ok = true;
+    int ring = 0, qitems = 0, armed = 0;           // armed: tiles that have been asked for
+    for (int it = 0; ok; ++it) {
+      ok = item_wait(it, std::integral_constant<int, 8>{});
+      if (!ok) break;
+      const Item d = s_item[it & 1];
+      __syncwarp();
+      if (lane == 0) mbar_arrive(bar_itemfree(it & 1));
+      if (d.end) break;
+      if (d.most == 0) continue;
+      if (qitems > 0) ok = warp_wait<9>(bar_qfree, (qitems - 1) & 1, s_abort, status);
+      if (!ok) break;
+      if (lane == 0) {
+        const uint32_t bytes = (uint32_t)(tile_tokens * group) * 128u * (D / 64);
+        mbar_expect_tx(bar_q, d.tokens[1] > 0 ? 2 * bytes : bytes);
+        for (int i = 0; i < (d.tokens[1] > 0 ? 2 : 1); ++i)
+#pragma unroll
+          for (int sl = 0; sl < D / 64; ++sl)
+            tma_heads_tile(ubase + C::kOffQ + i * C::kTile + sl * C::kSlab, &maps.q, sl * 64, d.kv * group, d.row0 + i * tile_tokens, bar_q);
+        mbar_arrive(bar_q);
+      }
+      ++qitems;
+      for (int n = 0; n < 2 * d.most && ok; ++n) {
+        const int g = ring + n, s = g % C::kStages, j = d.most - 1 - (n >> 1);
+        if (g >= C::kStages) ok = warp_wait<10>(bar_empty(s), (g / C::kStages - 1) & 1, s_abort, status);
+        if (!ok) break;
+        const uint32_t dst = ubase + C::kOffRing + s * C::kTile;
+        const int have = d.keys - j * kTileKeys;                         // keys of the tile that exist
+        if ((n & 1) && have < kTileKeys) {
+          // values beyond the request's end: zeros, whatever lies there
+          const T* src = reinterpret_cast<const T*>(a.v) + (size_t)(d.key0 + j * kTileKeys) * a.v_row + (size_t)d.kv * a.v_head;
+          for (int e = lane; e < kTileKeys * (D / 8); e += 32) {
+            const int key = e / (D / 8), c = e % (D / 8);
+            cp_async16_or_zero(dst + tile_off<128>(key, c), src + (size_t)(key < have ? key : 0) * a.v_row + c * 8, key < have);
+          }
+          cp_async_commit();
+          cp_async_wait_all();
+          fence_async_smem();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(bar_full(s));
+        } else if (lane == 0) {
+          mbar_expect_tx(bar_full(s), C::kTile);
+#pragma unroll
+          for (int sl = 0; sl < D / 64; ++sl)
+            tma_heads_tile(dst + sl * C::kSlab, (n & 1) ? &maps.v : &maps.k, sl * 64, d.kv, d.key0 + j * kTileKeys, bar_full(s));
+          mbar_arrive(bar_full(s));
+        }
+        armed = g + 1;
+        __syncwarp();
+      }
+      ring += 2 * d.most;
+    }
+    // nothing may be on its way into shared memory when the CTA ends
+    for (int s = 0; s < C::kStages && s < armed; ++s) mbar_drain(bar_full(s), ((armed - 1 - s) / C::kStages) & 1);
+    if (qitems > 0) mbar_drain(bar_q, (qitems - 1) & 1);
+  } else if (warp == 10) {
+    // ================= items ===============================================================================
+    bool ok = true;
+    for (int it = 0; ok; ++it) {
+      // rounds of the grid in alternating direction: a CTA that had a long item of one round has a short one of the next
+      const int index = it * gridDim.x + ((it & 1) ? gridDim.x - 1 - blockIdx.x : blockIdx.x);
+      const Item d = item_at(a, index, tile_tokens);
+      if (it >= 2) ok = warp_wait<11>(bar_itemfree(it & 1), ((it >> 1) - 1) & 1, s_abort, status);
+      if (!ok) break;
+      if (lane == 0) {
+        s_item[it & 1] = d;
+        mbar_arrive(bar_item(it & 1));
+      }
+      __syncwarp();
+      if (d.end) break;
+    }
+  }
+
+  // ---- teardown ----
+  tc_fence_before();
+  __syncthreads();
+  if (warp == 8) {
+    tc_fence_after();
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
+  }
+}
+
+template <int D, class T>
+cudaError_t run_prompt(const PromptArgs& a, const PromptMaps& maps, int group, int tile_tokens, int* status, cudaStream_t st) {
+  int sms = 0;
+  cudaError_t e = sm_count(&sms);
+  if (e == cudaSuccess) e = allow_smem<prompt_kernel<D, T>>(Cfg<D>::kSmem);
+  if (e != cudaSuccess) return e;
+  const long long items = ((long long)a.q_rows / (2 * tile_tokens) + a.requests) * a.kv_heads;       // at most
+  return launch(prompt_kernel<D, T>, dim3((unsigned)(items < sms ? items : sms)), dim3(kThreads), Cfg<D>::kSmem, st, a, maps, group, tile_tokens, status);
 }
 
 }  // namespace
@@ -88,7 +549,7 @@ extern "C" int hyperattn_prompt_attention(const hyperattn_prompt_params* p) {
   if (p->out_dtype != p->dtype && p->out_dtype != HYPERATTN_FP32) return HYPERATTN_INVALID_ARGUMENT;
   if ((p->d != 64 && p->d != 128) || p->q_heads % p->kv_heads || p->q_heads / p->kv_heads > 128) return HYPERATTN_UNSUPPORTED_SHAPE;
   for (long long s : {p->q_row_stride, p->q_head_stride, p->k_row_stride, p->k_head_stride, p->v_row_stride, p->v_head_stride})
-    if (bad_stride(s)) return HYPERATTN_UNSUPPORTED_SHAPE;
+    if (bad_stride(s) || s == 0) return HYPERATTN_UNSUPPORTED_SHAPE;
   if (p->requests == 0 || p->q_rows == 0) return HYPERATTN_OK;
   if (!p->q || (p->k_rows && (!p->k || !p->v)) || !p->out || !p->lse || !p->cu_q || !p->cu_k) return HYPERATTN_INVALID_ARGUMENT;
   if (misaligned(p->q) || misaligned(p->k) || misaligned(p->v) || misaligned(p->out)) return HYPERATTN_MISALIGNED;
@@ -100,16 +561,25 @@ extern "C" int hyperattn_prompt_attention(const hyperattn_prompt_params* p) {
   a.requests = p->requests; a.q_rows = p->q_rows; a.k_rows = p->k_rows; a.q_heads = p->q_heads; a.kv_heads = p->kv_heads;
   a.causal = p->causal != 0; a.out_kind = p->out_dtype;
   a.scale_log2 = (p->softmax_scale > 0.f ? p->softmax_scale : 1.f / sqrtf((float)p->d)) * 1.4426950408889634f;
-  const dim3 grid((unsigned)p->q_rows, (unsigned)((p->q_heads + 7) / 8));
-  if (grid.y > 65535) return HYPERATTN_UNSUPPORTED_SHAPE;
-  const cudaStream_t st = reinterpret_cast<cudaStream_t>(p->stream);
-  auto go = [&](auto kernel) {
-    const cudaError_t e = launch(kernel, grid, dim3(256), 0, st, a);
-    if (e == cudaSuccess) return (int)HYPERATTN_OK;
-    std::fprintf(stderr, "hyperattn: prompt attention failed: %s\n", cudaGetErrorString(e));
-    return (int)HYPERATTN_CUDA_ERROR;
-  };
+  const int group = p->q_heads / p->kv_heads, tile_tokens = kTileRows / group;
   const bool bf16 = p->dtype == HYPERATTN_BF16;
-  if (p->d == 64) return bf16 ? go(prompt_rows_kernel<64, __nv_bfloat16>) : go(prompt_rows_kernel<64, __half>);
-  return bf16 ? go(prompt_rows_kernel<128, __nv_bfloat16>) : go(prompt_rows_kernel<128, __half>);
+  PromptMaps maps;
+  // (the stride of an axis of one entry does not matter, but has to be one; without keys the maps of K and V are not used)
+  auto map = [&](CUtensorMap* m, const void* base, int rows, long long row, int heads, long long head, int box_rows, int box_heads) {
+    return encode_heads_map(m, base, bf16, rows, rows > 1 ? row : (long long)heads * p->d, heads, heads > 1 ? head : p->d, p->d, box_rows, box_heads);
+  };
+  const bool keys = p->k_rows > 0;
+  if (!map(&maps.q, p->q, p->q_rows, p->q_row_stride, p->q_heads, p->q_head_stride, tile_tokens, group) ||
+      !map(&maps.k, keys ? p->k : p->q, keys ? p->k_rows : 1, p->k_row_stride, p->kv_heads, keys ? p->k_head_stride : p->d, kTileKeys, 1) ||
+      !map(&maps.v, keys ? p->v : p->q, keys ? p->k_rows : 1, p->v_row_stride, p->kv_heads, keys ? p->v_head_stride : p->d, kTileKeys, 1))
+    return HYPERATTN_UNSUPPORTED_SHAPE;
+  const cudaStream_t st = reinterpret_cast<cudaStream_t>(p->stream);
+  int* status = nullptr;
+  if (int rc = device_status_word(st, &status)) return rc;
+  cudaError_t e;
+  if (p->d == 64) e = bf16 ? run_prompt<64, __nv_bfloat16>(a, maps, group, tile_tokens, status, st) : run_prompt<64, __half>(a, maps, group, tile_tokens, status, st);
+  else e = bf16 ? run_prompt<128, __nv_bfloat16>(a, maps, group, tile_tokens, status, st) : run_prompt<128, __half>(a, maps, group, tile_tokens, status, st);
+  if (e == cudaSuccess) return HYPERATTN_OK;
+  std::fprintf(stderr, "hyperattn: prompt attention failed: %s\n", cudaGetErrorString(e));
+  return HYPERATTN_CUDA_ERROR;
 }

@@ -10,6 +10,9 @@ namespace hyperattn {
 bool encode_rows_map(CUtensorMap* m, const void* base, size_t rows, int d, int box_rows);
 // [rows x d] fp32 accumulator, row-major; one box = 32 columns x 32 rows, 128-byte swizzle (attn_tc.cu)
 bool encode_acc_map(CUtensorMap* m, const void* base, size_t rows, int d);
+// [rows x heads x d] of bf16 or fp16 with strides in elements; one box = 64 columns x box_heads heads x box_rows rows, 128-byte swizzle (attn_tc.cu)
+bool encode_heads_map(CUtensorMap* m, const void* base, bool bf16, long long rows, long long row_stride, int heads, long long head_stride, int d, int box_rows,
+                      int box_heads);
 
 namespace {
 
@@ -230,6 +233,11 @@ __device__ __forceinline__ void fence_async_smem() { asm volatile("fence.proxy.a
 __device__ __forceinline__ void tma_tile(uint32_t dst, const CUtensorMap* map, int x, int y, uint32_t bar) {
   asm volatile("cp.async.bulk.tensor.2d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
                ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(bar) : "memory");
+}
+// One box of a map of heads: 64 columns from column x on, heads from h on, rows from y on.
+__device__ __forceinline__ void tma_heads_tile(uint32_t dst, const CUtensorMap* map, int x, int h, int y, uint32_t bar) {
+  asm volatile("cp.async.bulk.tensor.3d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
+               ::"r"(dst), "l"(map), "r"(x), "r"(h), "r"(y), "r"(bar) : "memory");
 }
 // One box from shared memory (128-byte swizzle) added to global memory, as a bulk group of its own.
 __device__ __forceinline__ void tma_add_tile(const CUtensorMap* map, int x, int y, uint32_t src) {

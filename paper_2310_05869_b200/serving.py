@@ -79,7 +79,7 @@ def _ints(device, **tensors):
 def _rows(x):
     """x [rows, heads, d] with strides that the kernels take: d contiguous, the others and the address in steps of 16 bytes."""
     s = x.stride()
-    if s[2] != 1 or s[0] % 8 or s[1] % 8 or s[0] < 0 or s[1] < 0 or x.data_ptr() % 16:
+    if s[2] != 1 or s[0] % 8 or s[1] % 8 or s[0] <= 0 or s[1] <= 0 or x.data_ptr() % 16:
         return x.clone(memory_format=torch.contiguous_format)
     return x
 
