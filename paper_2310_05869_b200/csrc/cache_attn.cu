@@ -8,9 +8,16 @@
 //   O^T += V^T P^T   V = min + scale * code in fp16 (exact codes, one rounding); its 32-bit words hold four tokens of two coordinates,
 //               so that masking yields operands with pairs of tokens, and P^T is what the lanes have after S.
 // fp16 and not bf16 for the weights and values: a product is then off by 2^-11 and not 2^-8, which is what the output's type can show; V fits by
-// its format, a head's query after a power of two.
+// its format, a head's query after a power of two.  For fp16 results, which show 2^-11, the weights' rounding errors go through the products too.
+//
+// The blocks of all (request, key head, up to 16 heads) segments are one sequence, cut into equal parts, one for every warp that the
+// GPU holds, whatever the lengths are.  A warp streams its blocks through a ring of its own in shared memory (bulk copies, no other
+// warp to wait for).  A segment that lies in one part is finished there; pieces of others go to the workspace - one piece for a
+// CTA that is inside a segment as a whole - and a second launch puts them together, in order, so that results do not depend on timing.
 #include <cstdio>
+#include <type_traits>
 #include "serving.cuh"
+#include "tc_util.cuh"
 
 namespace hyperattn {
 namespace {
@@ -25,7 +32,11 @@ struct CacheAttnArgs {
   float* lse;
   const int32_t *table, *lengths;
   int requests, width, q_heads, out_kind;      // out_kind: hyperattn_dtype
+  int chunks;                                  // of query heads of a key head
   float scale_log2;
+  int* starts;                                 // [requests + 1] blocks before each request; [requests + 1]: blocks of a warp's part
+  float* part;                                 // pieces: [slots][heads of a chunk][d + 2] (outputs, reference, sum)
+  int part_heads;                              // heads of a chunk
 };
 
 __device__ __forceinline__ void mma_f16(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
@@ -33,11 +44,6 @@ __device__ __forceinline__ void mma_f16(float (&c)[4], uint32_t a0, uint32_t a1,
       "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};\n"
       : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
       : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
-}
-__device__ __forceinline__ float ex2f(float x) {
-  float y;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-  return y;
 }
 // nibbles 1 and 5 of a word (bits 4..7 of either half) as 64 + code in fp16
 __device__ __forceinline__ uint32_t codes_at_4(uint32_t w) { return (w & 0x00f000f0u) | 0x54005400u; }
@@ -112,7 +118,7 @@ __device__ __forceinline__ void move_reference(Heads<D, NT>& h, float (&top)[NT]
     m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 1));
     m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 2));
     float alpha = 1.f;
-    if (m > h.ref[t] + kMoveAt) { alpha = ex2f(h.ref[t] - m); h.ref[t] = m; }      // (from -infinity: 0)
+    if (m > h.ref[t] + kMoveAt) { alpha = ex2(h.ref[t] - m); h.ref[t] = m; }      // (from -infinity: 0)
     h.sum[t] *= alpha;
     const float a0 = __shfl_sync(0xffffffffu, alpha, 8 * c), a1 = __shfl_sync(0xffffffffu, alpha, 8 * c + 4);
 #pragma unroll
@@ -123,8 +129,8 @@ __device__ __forceinline__ void move_reference(Heads<D, NT>& h, float (&top)[NT]
   }
 }
 
-// One block of 16 tokens at `block`, the first `valid` of which exist.
-template <int D, int NT>
+// One block of 16 tokens at `block`, the first `valid` of which exist.  FINE: what rounding the weights to fp16 has lost is added.
+template <int D, int NT, bool FINE>
 __device__ __forceinline__ void attend_block(Heads<D, NT>& h, const uint8_t* block, int valid) {
   constexpr int G = D / kGroup;
   const int lane = threadIdx.x & 31, c = lane & 3;
@@ -178,16 +184,21 @@ __device__ __forceinline__ void attend_block(Heads<D, NT>& h, const uint8_t* blo
     move = move || top[t] > h.ref[t] + kMoveAt;
   }
   if (__any_sync(0xffffffffu, move)) move_reference<D, NT>(h, top);
-  uint32_t p[NT][2];
+  uint32_t p[NT][2], rest[NT][2];
 #pragma unroll
   for (int t = 0; t < NT; ++t) {
     const float ref = h.ref[t] == -INFINITY ? 0.f : h.ref[t];
     float e[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) e[i] = ex2f(x[t][i] - ref);
+    for (int i = 0; i < 4; ++i) e[i] = ex2(x[t][i] - ref);
     h.sum[t] += (e[0] + e[1]) + (e[2] + e[3]);
     p[t][0] = from_float2<__half>(e[0], e[1]);
     p[t][1] = from_float2<__half>(e[2], e[3]);
+    if constexpr (FINE) {
+      const float2 a = to_float2<__half>(p[t][0]), b = to_float2<__half>(p[t][1]);
+      rest[t][0] = from_float2<__half>(e[0] - a.x, e[1] - a.y);
+      rest[t][1] = from_float2<__half>(e[2] - b.x, e[3] - b.y);
+    }
   }
   // ---- values ----
   uint32_t sv[2][2 * G];                                 // (scale pair, minimum pair) of tokens (2 c, 2 c + 1), (8 + 2 c, 9 + 2 c)
@@ -217,7 +228,10 @@ __device__ __forceinline__ void attend_block(Heads<D, NT>& h, const uint8_t* blo
       auto value = [&](uint32_t bits, int half) { return u32(__hfma2(__hadd2(h2(codes_at_4(bits)), minus64), h2(sv[half][2 * w]), h2(sv[half][2 * w + 1]))); };
       const uint32_t a0 = value(vw[j] << 4, 0), a1 = value(vw[j], 0), a2 = value(vw[j] >> 4, 1), a3 = value(vw[j] >> 8, 1);
 #pragma unroll
-      for (int t = 0; t < NT; ++t) mma_f16(h.o[t][u], a0, a1, a2, a3, p[t][0], p[t][1]);
+      for (int t = 0; t < NT; ++t) {
+        mma_f16(h.o[t][u], a0, a1, a2, a3, p[t][0], p[t][1]);
+        if constexpr (FINE) mma_f16(h.o[t][u], a0, a1, a2, a3, rest[t][0], rest[t][1]);
+      }
     }
   }
 }
@@ -229,52 +243,305 @@ __device__ __forceinline__ void put(void* out, int kind, size_t at, float x) {
 }
 
 constexpr int kWarps = 4;
+constexpr int kLeastPart = 2;           // blocks of a warp's part at least
+constexpr int kMaxRequests = 4096;      // running sums in shared memory
+
+template <int D>
+struct Ring {
+  static constexpr int kStages = D == 128 ? 4 : 8;                       // blocks on their way, a warp
+  static constexpr int kWarpBytes = kStages * Block<D>::kBytes;          // (>= 16 x D floats: a warp's outputs, when the parts are put together)
+  static constexpr int kOffBar = kWarps * kWarpBytes, kOffMisc = kOffBar + kWarps * kStages * 8, kOffStarts = kOffMisc + 1280;
+  static constexpr int bytes(int requests) { return kOffStarts + (requests + 1) * 4; }
+};
+// CTAs that an SM holds: by registers (two tiles of heads need 168 a thread), and by shared memory
+template <int D, int NT> constexpr int ctas_by_registers() { return NT == 1 ? 4 : 3; }
+template <int D> int ctas_by_memory(int requests) { return 227 * 1024 / (Ring<D>::bytes(requests) + 1024); }
+
+__device__ __forceinline__ void bulk_copy(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
+  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
+}
+__device__ __forceinline__ int blocks_of(const CacheAttnArgs& a, int r) {
+  return (min(max(a.lengths[r], 0), a.width * a.cache.page) + kBlockTokens - 1) / kBlockTokens;
+}
+// where the pieces of a segment lie: see combine
+__device__ __forceinline__ float* piece_at(const CacheAttnArgs& a, long long slot, int head, int d) { return a.part + (slot * a.part_heads + head) * (d + 2); }
 
 template <int D, int NT, class T>
-__global__ void __launch_bounds__(32 * kWarps) cache_attn_kernel(CacheAttnArgs a, int chunks) {
-  __shared__ float s_o[kWarps][8 * NT][D];
-  __shared__ float s_ref[kWarps][8 * NT], s_sum[kWarps][8 * NT];
+__global__ void __launch_bounds__(32 * kWarps, (ctas_by_registers<D, NT>())) cache_attn_kernel(const __grid_constant__ CacheAttnArgs a, int* status) {
+  using R = Ring<D>;
+  constexpr bool FINE = std::is_same<T, __half>::value;
+  extern __shared__ __align__(128) uint8_t smem[];
+  int* s_starts = reinterpret_cast<int*>(smem + R::kOffStarts);          // [requests + 1] blocks (of one segment each) before a request
+  int* s_sums = reinterpret_cast<int*>(smem + R::kOffMisc);              // [kWarps]
+  volatile int* s_abort = reinterpret_cast<volatile int*>(smem + R::kOffMisc + 64);
+  float* s_stat = reinterpret_cast<float*>(smem + R::kOffMisc + 128);    // [kWarps][16][2] references, sums
+  const int tid = threadIdx.x, lane = tid & 31, c = lane & 3;
+  const int warp = __shfl_sync(0xffffffffu, tid >> 5, 0);
+  const uint32_t ring = smem_u32(smem) + warp * R::kWarpBytes, bars = smem_u32(smem) + R::kOffBar + warp * R::kStages * 8;
+  if (tid == 0) *s_abort = 0;
+  if (lane == 0) {
+    for (int st = 0; st < R::kStages; ++st) mbar_init(bars + 8 * st, 1);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
   wait_for_stream();
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, c = lane & 3;
-  const int r = blockIdx.x, kv = blockIdx.y / chunks, chunk = blockIdx.y % chunks;
-  const int per_kv = a.q_heads / a.cache.heads, first = kv * per_kv + chunk * 8 * NT, heads = min(per_kv - chunk * 8 * NT, 8 * NT);
-  Heads<D, NT> h;
-  load_heads<D, NT, T>(h, a, r, first, heads);
-  const int len = min(max(a.lengths[r], 0), a.width * a.cache.page), subs = a.cache.page / kBlockTokens;
-  for (int b = warp; b * kBlockTokens < len; b += kWarps) {
-    const int page = a.table[(size_t)r * a.width + b / subs];
-    if (page < 0 || page >= a.cache.num_pages) continue;
-    attend_block<D, NT>(h, block_at<D>(a.cache, page, kv, b % subs), min(len - b * kBlockTokens, kBlockTokens));
-  }
-  // ---- the warps' parts together ----
+  // ---- running sum of the requests' blocks ----
+  const int per = (a.requests + 32 * kWarps - 1) / (32 * kWarps), r0 = min(a.requests, tid * per), r1 = min(a.requests, r0 + per);
+  int mine = 0;
+  for (int r = r0; r < r1; ++r) mine += blocks_of(a, r);
+  int run = mine;
 #pragma unroll
-  for (int t = 0; t < NT; ++t) {
-    float sum = h.sum[t];
-    sum += __shfl_xor_sync(0xffffffffu, sum, 1);
-    sum += __shfl_xor_sync(0xffffffffu, sum, 2);
-    if (c == 0) { s_ref[warp][lane / 4 + 8 * t] = h.ref[t]; s_sum[warp][lane / 4 + 8 * t] = sum; }
-#pragma unroll
-    for (int m = 0; m < D / 16; ++m)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) s_o[warp][8 * t + 2 * c + (i & 1)][16 * m + lane / 4 + 8 * (i >> 1)] = h.o[t][m][i];
-  }
+  for (int o = 1; o < 32; o <<= 1) { const int y = __shfl_up_sync(0xffffffffu, run, o); if (lane >= o) run += y; }
+  if (lane == 31) s_sums[warp] = run;
   __syncthreads();
-  for (int i = threadIdx.x; i < heads * D; i += 32 * kWarps) {
-    const int head = i / D, x = i - head * D;
-    float ref = -INFINITY;
-#pragma unroll
-    for (int w = 0; w < kWarps; ++w) ref = fmaxf(ref, s_ref[w][head]);
-    float sum = 0.f, o = 0.f;
-#pragma unroll
-    for (int w = 0; w < kWarps; ++w) {
-      const float f = s_ref[w][head] == -INFINITY ? (s_sum[w][head] == 0.f ? 0.f : 1.f) : ex2f(s_ref[w][head] - ref);   // (a sum without a reference: NaN)
-      sum += f * s_sum[w][head];
-      o += f * s_o[w][head][x];
-    }
-    const size_t row = (size_t)r * a.q_heads + first + head;
-    put(a.out, a.out_kind, row * D + x, sum == 0.f ? 0.f : o / sum);
-    if (x == 0) a.lse[row] = sum == 0.f ? -INFINITY : (ref + log2f(sum)) * 0.6931471805599453f;
+  run -= mine;
+  for (int w = 0; w < warp; ++w) run += s_sums[w];
+  for (int r = r0; r < r1; ++r) { s_starts[r] = run; run += blocks_of(a, r); }
+  if (tid == 32 * kWarps - 1) s_starts[a.requests] = run;
+  __syncthreads();
+  const int segs = a.cache.heads * a.chunks;                             // of a request
+  const long long total = (long long)s_starts[a.requests] * segs, warps = (long long)gridDim.x * kWarps;
+  const int part = (int)max((long long)kLeastPart, (total + warps - 1) / warps);
+  if (blockIdx.x == 0) {
+    for (int r = tid; r <= a.requests; r += 32 * kWarps) a.starts[r] = s_starts[r];
+    if (tid == 0) a.starts[a.requests + 1] = part;
   }
+  const long long cta_first = (long long)blockIdx.x * kWarps * part, cta_end = min(cta_first + (long long)kWarps * part, total);
+  const long long first = min(cta_first + (long long)warp * part, total), end = min(first + part, total);
+  const int count = (int)(end - first);                                  // blocks of this warp
+  const int subs = a.cache.page / kBlockTokens, per_kv = a.q_heads / a.cache.heads;
+
+  // A lane knows one of 32 blocks of the part: its segment (of all requests'), how many tokens there are from it on, and which block of the cache it
+  // is (-1: none).
+  struct Known { int seg, left, at; };
+  auto know = [&](int i) {
+    Known k = {0, 0, -1};
+    if (i >= count) return k;
+    const long long n = first + i;
+    int lo = 0, hi = a.requests;                                         // the last request whose blocks start there or before
+    const int t = (int)(n / segs);
+    while (hi - lo > 1) { const int mid = (lo + hi) >> 1; if (s_starts[mid] <= t) lo = mid; else hi = mid; }
+    const int blocks = s_starts[lo + 1] - s_starts[lo];
+    const int rest = (int)(n - (long long)s_starts[lo] * segs);
+    const int seg = rest / blocks, b = rest - seg * blocks;
+    k.seg = lo * segs + seg;
+    k.left = min(a.lengths[lo], a.width * a.cache.page) - b * kBlockTokens;
+    const int page = a.table[(size_t)lo * a.width + b / subs];
+    if (page >= 0 && page < a.cache.num_pages) k.at = (page * a.cache.heads + seg / a.chunks) * subs + b % subs;
+    return k;
+  };
+  int asked = 0;                                                         // blocks whose copies have been asked for
+  auto ask = [&](const Known& k, int from) {                              // the next one, known by lane `from`
+    const int at = __shfl_sync(0xffffffffu, k.at, from);
+    if (lane == 0) {
+      const int st = asked % R::kStages;
+      if (at >= 0) {
+        mbar_expect_tx(bars + 8 * st, Block<D>::kBytes);
+        bulk_copy(ring + st * Block<D>::kBytes, a.cache.pages + (size_t)at * Block<D>::kBytes, Block<D>::kBytes, bars + 8 * st);
+      }
+      mbar_arrive(bars + 8 * st);
+    }
+    ++asked;
+  };
+  Known now = know(lane), next = now;
+  while (asked < R::kStages && asked < count) ask(now, asked);
+  bool ok = true;
+  Heads<D, NT> h;
+  int segment = -1, request = 0, seg = 0;                                // segment = request * segs + seg
+  // the segment's results, or a piece of them: O in the lanes' fragments, sums of all lanes
+  auto flush = [&](float* to) {                                            // to: null for final results
+    const int chunk = seg % a.chunks, kv = seg / a.chunks, first_head = kv * per_kv + chunk * 8 * NT, heads = min(per_kv - chunk * 8 * NT, 8 * NT);
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+      float sum = h.sum[t];
+      sum += __shfl_xor_sync(0xffffffffu, sum, 1);
+      sum += __shfl_xor_sync(0xffffffffu, sum, 2);
+      const int head = lane / 4 + 8 * t;
+      if (c == 0 && head < heads) {
+        if (to) { to[head * (D + 2) + D] = h.ref[t]; to[head * (D + 2) + D + 1] = sum; }
+        else a.lse[(size_t)request * a.q_heads + first_head + head] = sum == 0.f ? -INFINITY : (h.ref[t] + log2f(sum)) * 0.6931471805599453f;
+      }
+      const float inv = to ? 1.f : sum == 0.f ? 0.f : 1.f / sum;
+      const float inv0 = __shfl_sync(0xffffffffu, inv, 8 * c), inv1 = __shfl_sync(0xffffffffu, inv, 8 * c + 4);
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const int hd = 8 * t + 2 * c + i;
+        if (hd < heads) {
+#pragma unroll
+          for (int m = 0; m < D / 16; ++m)
+#pragma unroll
+            for (int up = 0; up < 2; ++up) {
+              const int x = 16 * m + lane / 4 + 8 * up;
+              const float v = h.o[t][m][i + 2 * up];
+              if (to) to[hd * (D + 2) + x] = v;
+              else put(a.out, a.out_kind, ((size_t)request * a.q_heads + first_head + hd) * D + x, v * (i ? inv1 : inv0));
+            }
+        }
+      }
+    }
+  };
+  bool together = false;                                                 // the whole CTA works for one segment
+  for (int n = 0; n < count && ok; ++n) {
+    const int at = n & 31;
+    if (at == 0) {
+      if (n > 0) now = next;
+      next = know(n + 32 + lane);
+    }
+    const int sg = __shfl_sync(0xffffffffu, now.seg, at), left = __shfl_sync(0xffffffffu, now.left, at);
+    const bool there = __shfl_sync(0xffffffffu, now.at, at) >= 0;
+    if (sg != segment) {
+      segment = sg;
+      request = segment / segs; seg = segment - request * segs;
+      const int kv = seg / a.chunks, chunk = seg - kv * a.chunks;
+      load_heads<D, NT, T>(h, a, request, kv * per_kv + chunk * 8 * NT, min(per_kv - chunk * 8 * NT, 8 * NT));
+    }
+    const int st = n % R::kStages;
+    ok = warp_wait<12>(bars + 8 * st, (uint32_t)(n / R::kStages) & 1, s_abort, status);
+    if (!ok) break;
+    if (there) attend_block<D, NT, FINE>(h, smem + warp * R::kWarpBytes + st * Block<D>::kBytes, min(left, kBlockTokens));
+    __syncwarp();
+    if (asked < count) { if (at + R::kStages < 32) ask(now, at + R::kStages); else ask(next, at + R::kStages - 32); }
+    if (left <= kBlockTokens || n + 1 == count) {                          // the segment's last block, or the part's
+      const long long blocks = s_starts[request + 1] - s_starts[request], seg_first = (long long)s_starts[request] * segs + seg * blocks, seg_end = seg_first + blocks;
+      if (seg_first >= first && seg_end <= end) flush(nullptr);
+      else {
+        together = seg_first <= cta_first && seg_end >= cta_end;
+        if (!together) flush(piece_at(a, 2 * ((long long)blockIdx.x * kWarps + warp) + (seg_first < first ? 0 : 1), 0, D));
+      }
+    }
+  }
+  if (!ok)                                                               // nothing may be on its way into shared memory when the CTA ends
+    for (int st = 0; st < R::kStages && st < asked; ++st) mbar_drain(bars + 8 * st, (uint32_t)((asked - 1 - st) / R::kStages) & 1);
+  // ---- a CTA inside one segment: one piece ----
+  if (__syncthreads_or(together)) {
+    float* s_o = reinterpret_cast<float*>(smem + warp * R::kWarpBytes);  // [8 NT][D] of this warp
+    if (together) {
+#pragma unroll
+      for (int t = 0; t < NT; ++t) {
+        float sum = h.sum[t];
+        sum += __shfl_xor_sync(0xffffffffu, sum, 1);
+        sum += __shfl_xor_sync(0xffffffffu, sum, 2);
+        if (c == 0) { s_stat[(warp * 16 + lane / 4 + 8 * t) * 2] = h.ref[t]; s_stat[(warp * 16 + lane / 4 + 8 * t) * 2 + 1] = sum; }
+#pragma unroll
+        for (int m = 0; m < D / 16; ++m)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) s_o[(8 * t + 2 * c + (i & 1)) * D + 16 * m + lane / 4 + 8 * (i >> 1)] = h.o[t][m][i];
+      }
+    }
+    __syncthreads();
+    const int used = (int)((cta_end - cta_first + part - 1) / part);     // warps that have a part
+    const int heads = min(per_kv - (seg % a.chunks) * 8 * NT, 8 * NT);
+    if (warp < used) {
+      for (int i = warp * 32 + lane; i < heads * D; i += used * 32) {
+        const int head = i / D, x = i - head * D;
+        float ref = -INFINITY;
+        for (int w = 0; w < used; ++w) ref = fmaxf(ref, s_stat[(w * 16 + head) * 2]);
+        float sum = 0.f, o = 0.f;
+        for (int w = 0; w < used; ++w) {
+          const float rw = s_stat[(w * 16 + head) * 2], sw = s_stat[(w * 16 + head) * 2 + 1];
+          const float f = rw == -INFINITY ? (sw == 0.f ? 0.f : 1.f) : ex2(rw - ref);          // (a sum without a reference: NaN)
+          sum += f * sw;
+          o += f * reinterpret_cast<const float*>(smem + w * R::kWarpBytes)[i];
+        }
+        float* to = piece_at(a, 2 * (long long)blockIdx.x * kWarps, head, D);
+        to[x] = o;
+        if (x == 0) { to[D] = ref; to[D + 1] = sum; }
+      }
+    }
+  }
+}
+
+// Puts the pieces of segments together that lie in several parts; requests without tokens get their zeros.
+constexpr int kJoinThreads = 128;
+
+template <int D>
+__global__ void __launch_bounds__(kJoinThreads) join_kernel(const __grid_constant__ CacheAttnArgs a, int heads_per_cta) {
+  constexpr int LANES = D / 4, ROWS = kJoinThreads / LANES;               // a thread: four coordinates of every ROWS-th piece
+  __shared__ float4 s_o[ROWS][LANES];
+  __shared__ float s_ref[ROWS], s_sum[ROWS];
+  wait_for_stream();
+  const int segs = a.cache.heads * a.chunks, per_kv = a.q_heads / a.cache.heads;
+  const int r = blockIdx.x / segs, seg = blockIdx.x - r * segs, kv = seg / a.chunks, chunk = seg - kv * a.chunks;
+  const int first_head = kv * per_kv + chunk * a.part_heads, heads = min(per_kv - chunk * a.part_heads, a.part_heads);
+  const long long part = a.starts[a.requests + 1], blocks = a.starts[r + 1] - a.starts[r];
+  const long long begin = (long long)a.starts[r] * segs + seg * blocks, end = begin + blocks, cta_part = part * kWarps, total = (long long)a.starts[a.requests] * segs;
+  const int lane = threadIdx.x % LANES, row = threadIdx.x / LANES;
+  const int h0 = blockIdx.y * heads_per_cta, h1 = min(h0 + heads_per_cta, heads);
+  if (blocks == 0) {
+    for (int i = threadIdx.x; i < (h1 - h0) * D; i += kJoinThreads) put(a.out, a.out_kind, ((size_t)r * a.q_heads + first_head + h0) * D + i, 0.f);
+    for (int i = h0 + threadIdx.x; i < h1; i += kJoinThreads) a.lse[(size_t)r * a.q_heads + first_head + i] = -INFINITY;
+    return;
+  }
+  const long long w0 = begin / part, w1 = (end - 1) / part;               // warps that have a part of it
+  if (w0 == w1) return;                                                   // finished there
+  // Its pieces in order: those of the first CTA's warps (or its one), one of every CTA inside, those of the last CTA's warps (or its one)
+  const long long c0 = w0 / kWarps, c1 = w1 / kWarps;
+  auto whole = [&](long long cta) { return cta * cta_part >= begin && min((cta + 1) * cta_part, total) <= end; };
+  const int n0 = whole(c0) ? 1 : (int)(min(w1, c0 * kWarps + kWarps - 1) - w0 + 1);
+  const int n1 = c1 == c0 ? 0 : whole(c1) ? 1 : (int)(w1 - c1 * kWarps + 1);
+  const int inside = c1 > c0 ? (int)(c1 - c0 - 1) : 0, count = n0 + inside + n1;
+  auto slot_of = [&](int i) {
+    long long w;
+    if (i < n0) { if (whole(c0)) return 2 * c0 * kWarps; w = w0 + i; }
+    else if (i < n0 + inside) return 2 * (c0 + 1 + i - n0) * kWarps;
+    else { if (whole(c1)) return 2 * c1 * kWarps; w = c1 * kWarps + (i - n0 - inside); }
+    return 2 * w + (begin < w * part ? 0 : 1);
+  };
+  for (int head = h0; head < h1; ++head) {
+    float ref = -INFINITY, sum = 0.f;
+    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int i = row; i < count; i += ROWS) {
+      const float* from = piece_at(a, slot_of(i), head, D);
+      const float rw = from[D], sw = from[D + 1];
+      const float2 lo = *reinterpret_cast<const float2*>(from + 4 * lane), hi = *reinterpret_cast<const float2*>(from + 4 * lane + 2);
+      const float m = fmaxf(ref, rw);
+      const float f = rw == -INFINITY ? (sw == 0.f ? 0.f : 1.f) : ex2(rw - m), g = ref == -INFINITY ? (sum == 0.f ? 0.f : 1.f) : ex2(ref - m);
+      ref = m;
+      sum = sum * g + sw * f;
+      o = make_float4(o.x * g + lo.x * f, o.y * g + lo.y * f, o.z * g + hi.x * f, o.w * g + hi.y * f);
+    }
+    s_o[row][lane] = o;
+    if (lane == 0) { s_ref[row] = ref; s_sum[row] = sum; }
+    __syncthreads();
+    if (row == 0) {
+      float m = ref;
+#pragma unroll
+      for (int i = 1; i < ROWS; ++i) m = fmaxf(m, s_ref[i]);
+      sum = 0.f;
+      o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+      for (int i = 0; i < ROWS; ++i) {
+        const float f = s_ref[i] == -INFINITY ? (s_sum[i] == 0.f ? 0.f : 1.f) : ex2(s_ref[i] - m);
+        sum += f * s_sum[i];
+        o = make_float4(o.x + f * s_o[i][lane].x, o.y + f * s_o[i][lane].y, o.z + f * s_o[i][lane].z, o.w + f * s_o[i][lane].w);
+      }
+      const float inv = sum == 0.f ? 0.f : 1.f / sum;
+      const size_t at = (size_t)r * a.q_heads + first_head + head;
+      const float v[4] = {o.x * inv, o.y * inv, o.z * inv, o.w * inv};
+#pragma unroll
+      for (int i = 0; i < 4; ++i) put(a.out, a.out_kind, at * D + 4 * lane + i, v[i]);
+      if (lane == 0) a.lse[at] = sum == 0.f ? -INFINITY : (m + log2f(sum)) * 0.6931471805599453f;
+    }
+    __syncthreads();
+  }
+}
+
+// What a call's launches look like: heads of a chunk, CTAs, bytes of the workspace (which follow from the call's arguments alone)
+struct Shape { bool two; int chunks, part_heads, ctas; size_t starts, bytes; };
+Shape shape_of(const hyperattn_cache_attention_params& p) {
+  Shape s;
+  const int per_kv = p.q_heads / p.cache.kv_heads;
+  s.two = per_kv > 8;
+  s.chunks = (per_kv + (s.two ? 15 : 7)) / (s.two ? 16 : 8);
+  s.part_heads = s.two ? 16 : 8;
+  if (s.part_heads > per_kv) s.part_heads = per_kv;
+  const long long blocks = (long long)p.requests * p.cache.kv_heads * s.chunks * (((long long)p.table_width * p.cache.page_tokens + kBlockTokens - 1) / kBlockTokens);
+  const long long ctas = (blocks + kWarps * kLeastPart - 1) / (kWarps * kLeastPart);
+  const int memory = p.cache.d == 64 ? ctas_by_memory<64>(p.requests) : ctas_by_memory<128>(p.requests), registers = s.two ? ctas_by_registers<128, 2>() : ctas_by_registers<128, 1>();
+  const int most = kSms * (memory < registers ? memory : registers);
+  s.ctas = (int)(ctas < most ? ctas : most);
+  s.starts = ((size_t)(p.requests + 2) * 4 + 255) / 256 * 256;
+  s.bytes = s.starts + (size_t)s.ctas * kWarps * 2 * s.part_heads * (p.cache.d + 2) * 4;
+  return s;
 }
 
 }  // namespace
@@ -282,46 +549,68 @@ __global__ void __launch_bounds__(32 * kWarps) cache_attn_kernel(CacheAttnArgs a
 
 using namespace hyperattn;
 
-extern "C" int hyperattn_cache_attention_workspace_bytes(const hyperattn_cache_attention_params* p, size_t* bytes) {
-  if (!p || !bytes) return HYPERATTN_INVALID_ARGUMENT;
-  *bytes = 0;
-  return HYPERATTN_OK;
-}
-
-extern "C" int hyperattn_cache_attention(const hyperattn_cache_attention_params* p) {
+namespace {
+int check(const hyperattn_cache_attention_params* p) {
   int rc;
   if (!p || p->requests < 0 || p->table_width <= 0 || p->q_heads <= 0) return HYPERATTN_INVALID_ARGUMENT;
   if (bad_cache(p->cache, &rc)) return rc;
   if (p->dtype != HYPERATTN_BF16 && p->dtype != HYPERATTN_FP16) return p->dtype == HYPERATTN_FP32 ? HYPERATTN_UNSUPPORTED_SHAPE : HYPERATTN_INVALID_ARGUMENT;
   if (p->out_dtype != p->dtype && p->out_dtype != HYPERATTN_FP32) return HYPERATTN_INVALID_ARGUMENT;
-  if (p->q_heads % p->cache.kv_heads || bad_stride(p->q_row_stride) || bad_stride(p->q_head_stride)) return HYPERATTN_UNSUPPORTED_SHAPE;
-  if ((long long)p->table_width * p->cache.page_tokens > 0x7fffffffLL) return HYPERATTN_UNSUPPORTED_SHAPE;
+  if (p->q_heads % p->cache.kv_heads || bad_stride(p->q_row_stride) || bad_stride(p->q_head_stride) || p->requests > kMaxRequests) return HYPERATTN_UNSUPPORTED_SHAPE;
+  if ((long long)p->table_width * p->cache.page_tokens > 0x7fffffffLL || (long long)p->requests * p->table_width * (p->cache.page_tokens / kBlockTokens) > 0x7fffffffLL ||
+      (long long)p->requests * p->q_heads > 0x7fffffffLL || (long long)p->cache.num_pages * (p->cache.page_tokens / kBlockTokens) * p->cache.kv_heads > 0x7fffffffLL)
+    return HYPERATTN_UNSUPPORTED_SHAPE;
+  return HYPERATTN_OK;
+}
+}  // namespace
+
+extern "C" int hyperattn_cache_attention_workspace_bytes(const hyperattn_cache_attention_params* p, size_t* bytes) {
+  if (!bytes) return HYPERATTN_INVALID_ARGUMENT;
+  if (int rc = check(p)) return rc;
+  *bytes = p->requests ? shape_of(*p).bytes : 0;
+  return HYPERATTN_OK;
+}
+
+extern "C" int hyperattn_cache_attention(const hyperattn_cache_attention_params* p) {
+  if (int rc = check(p)) return rc;
   if (p->requests == 0) return HYPERATTN_OK;
-  if (!p->q || !p->out || !p->lse || !p->table || !p->lengths) return HYPERATTN_INVALID_ARGUMENT;
-  if (misaligned(p->q) || misaligned(p->out)) return HYPERATTN_MISALIGNED;
+  if (!p->q || !p->out || !p->lse || !p->table || !p->lengths || !p->workspace) return HYPERATTN_INVALID_ARGUMENT;
+  if (misaligned(p->q) || misaligned(p->out) || misaligned(p->workspace)) return HYPERATTN_MISALIGNED;
+  const Shape s = shape_of(*p);
+  if (p->workspace_bytes < s.bytes) return HYPERATTN_WORKSPACE_TOO_SMALL;
   CacheAttnArgs a;
   a.cache = {reinterpret_cast<uint8_t*>(p->cache.pages), p->cache.num_pages, p->cache.page_tokens, p->cache.kv_heads};
   a.q = p->q; a.q_row = p->q_row_stride; a.q_head = p->q_head_stride;
   a.out = p->out; a.lse = p->lse; a.table = p->table; a.lengths = p->lengths;
-  a.requests = p->requests; a.width = p->table_width; a.q_heads = p->q_heads; a.out_kind = p->out_dtype;
-  const int d = p->cache.d, per_kv = p->q_heads / p->cache.kv_heads;
+  a.requests = p->requests; a.width = p->table_width; a.q_heads = p->q_heads; a.out_kind = p->out_dtype; a.chunks = s.chunks;
+  const int d = p->cache.d;
   a.scale_log2 = (p->softmax_scale > 0.f ? p->softmax_scale : 1.f / sqrtf((float)d)) * 1.4426950408889634f;
-  const bool two = per_kv > 8;
-  const int chunks = (per_kv + (two ? 15 : 7)) / (two ? 16 : 8);
-  const dim3 grid((unsigned)p->requests, (unsigned)(p->cache.kv_heads * chunks));
-  if (grid.y > 65535) return HYPERATTN_UNSUPPORTED_SHAPE;
+  a.starts = reinterpret_cast<int*>(p->workspace);
+  a.part = reinterpret_cast<float*>(reinterpret_cast<char*>(p->workspace) + s.starts);
+  a.part_heads = s.part_heads;
   const cudaStream_t st = reinterpret_cast<cudaStream_t>(p->stream);
-  auto go = [&](auto kernel) {
-    const cudaError_t e = launch(kernel, grid, dim3(32 * kWarps), 0, st, a, chunks);
+  int* status = nullptr;
+  if (int rc = device_status_word(st, &status)) return rc;
+  const int segments = p->requests * p->cache.kv_heads * s.chunks;
+  auto go = [&](auto dim, auto kernel) {
+    constexpr int D = decltype(dim)::value;
+    cudaError_t e = launch(kernel, dim3((unsigned)s.ctas), dim3(32 * kWarps), Ring<D>::bytes(p->requests), st, a, status);
+    // few segments: a CTA for a head or some
+    int split = (4 * kSms + segments - 1) / segments;
+    if (split > s.part_heads) split = s.part_heads;
+    const int heads = (s.part_heads + split - 1) / split;
+    if (e == cudaSuccess) e = launch(join_kernel<D>, dim3((unsigned)segments, (unsigned)((s.part_heads + heads - 1) / heads)), dim3(kJoinThreads), 0, st, a, heads);
     if (e == cudaSuccess) return (int)HYPERATTN_OK;
     std::fprintf(stderr, "hyperattn: cache attention failed: %s\n", cudaGetErrorString(e));
     return (int)HYPERATTN_CUDA_ERROR;
   };
-  const bool bf16 = p->dtype == HYPERATTN_BF16;
-  if (d == 64) {
-    if (two) return bf16 ? go(cache_attn_kernel<64, 2, __nv_bfloat16>) : go(cache_attn_kernel<64, 2, __half>);
-    return bf16 ? go(cache_attn_kernel<64, 1, __nv_bfloat16>) : go(cache_attn_kernel<64, 1, __half>);
-  }
-  if (two) return bf16 ? go(cache_attn_kernel<128, 2, __nv_bfloat16>) : go(cache_attn_kernel<128, 2, __half>);
-  return bf16 ? go(cache_attn_kernel<128, 1, __nv_bfloat16>) : go(cache_attn_kernel<128, 1, __half>);
+  auto build = [&](auto dim, auto tiles, auto type) {
+    constexpr int D = decltype(dim)::value, NT = decltype(tiles)::value;
+    using T = decltype(type);
+    if (allow_smem<cache_attn_kernel<D, NT, T>>(Ring<D>::bytes(kMaxRequests)) != cudaSuccess) return (int)HYPERATTN_CUDA_ERROR;
+    return go(dim, cache_attn_kernel<D, NT, T>);
+  };
+  auto of_type = [&](auto dim, auto tiles) { return p->dtype == HYPERATTN_BF16 ? build(dim, tiles, __nv_bfloat16()) : build(dim, tiles, __half()); };
+  auto of_tiles = [&](auto dim) { return s.two ? of_type(dim, std::integral_constant<int, 2>{}) : of_type(dim, std::integral_constant<int, 1>{}); };
+  return d == 64 ? of_tiles(std::integral_constant<int, 64>{}) : of_tiles(std::integral_constant<int, 128>{});
 }
