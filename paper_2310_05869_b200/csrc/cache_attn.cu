@@ -2,8 +2,7 @@
 //
 // A warp takes a block of 16 tokens of one key head and up to 16 query heads that read it, on the warp-level tensor cores
 // (mma.sync m16n8k16, fp16 operands, fp32 sums):
-//   S = Q K^T   the codes of K become 64 + c in fp16 by one logical operation for two of them; the sums start at -64 sum(q), so that
-//               sum(q c) is left, and a group's scale and minimum enter in fp32:  s = sum_g scale_g sum(q c) + min_g sum_g(q)
+//   S = Q K^T   with the codes of K as fp16 numbers (see codes_of), exact sums of a group, s = sum_g scale_g sum(q c) + min_g sum_g(q) in fp32
 //   p = exp2(s c - ref), the reference of a head moves when it is exceeded by more than 2^8
 //   O^T += V^T P^T   V = min + scale * code in fp16 (exact codes, one rounding); its 32-bit words hold four tokens of two coordinates,
 //               so that masking yields operands with pairs of tokens, and P^T is what the lanes have after S.
@@ -39,23 +38,39 @@ struct CacheAttnArgs {
   int part_heads;                              // heads of a chunk
 };
 
+// c += A B, or d = A B (no registers to be cleared)
 __device__ __forceinline__ void mma_f16(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
   asm volatile(
       "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};\n"
       : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
       : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
-// nibbles 1 and 5 of a word (bits 4..7 of either half) as 64 + code in fp16
-__device__ __forceinline__ uint32_t codes_at_4(uint32_t w) { return (w & 0x00f000f0u) | 0x54005400u; }
+__device__ __forceinline__ void mma_f16_first(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+  asm volatile(
+      "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};\n"
+      : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.f));
+}
 __device__ __forceinline__ __half2 h2(uint32_t v) { return *reinterpret_cast<__half2*>(&v); }
 __device__ __forceinline__ uint32_t u32(__half2 v) { return *reinterpret_cast<uint32_t*>(&v); }
+// The codes of a word (8 of them, k at bit 4 k) as fp16 pairs (k, k + 4), k = 0..3: even ones as they are, odd ones 64 too large.  A code with the exponent
+// of 2^6 above its bits 4..7 is 64 + c; both codes of a byte with that of 2^10 are 1024 + low + 16 high, from which 16 (64 + high) is taken.  (Two logical
+// operations and half a shift for two pairs: those run at half the rate of the fused multiply-adds and are what a block has most of.)
+__device__ __forceinline__ void codes_of(uint32_t w, uint32_t (&k)[4]) {
+  const __half2 minus16 = __half2half2(__ushort_as_half(0xcc00));
+  const uint32_t up = w >> 8;
+  k[1] = (w & 0x00f000f0u) | 0x54005400u;
+  k[3] = (up & 0x00f000f0u) | 0x54005400u;
+  k[0] = u32(__hfma2(h2(k[1]), minus16, h2((w & 0x00ff00ffu) | 0x64006400u)));
+  k[2] = u32(__hfma2(h2(k[3]), minus16, h2((up & 0x00ff00ffu) | 0x64006400u)));
+}
 
 // What a warp keeps of the heads it works for: NT = 1: up to 8 of them (a lane's head: lane / 4), NT = 2: up to 16 (and lane / 4 + 8)
 template <int D, int NT>
 struct Heads {
   static constexpr int kGroups = D / kGroup;
   uint32_t q[NT][kGroups][4];           // fp16 pairs: coordinates 32 w + 8 c + 0..7
-  float qsum[NT][kGroups];              // sums of the group's entries
+  uint32_t fix[NT][2];                  // operands of the product that adds what belongs to minima and to codes that are 64 too large, see load_heads
   float scale[NT];                      // to the base-2 scores
   float ref[NT], sum[NT];               // sum: of this lane's tokens
   float o[NT][D / 16][4];               // O^T: coordinates lane / 4 (+ 8) of every 16, heads 2 c, 2 c + 1 (+ 8)
@@ -85,21 +100,39 @@ __device__ __forceinline__ void load_heads(Heads<D, NT>& h, const CacheAttnArgs&
     e = top == 0.f || !(top < INFINITY) ? 0 : min(max(e, -126), 126);
     const float down = __uint_as_float((uint32_t)(127 - e) << 23), up = __uint_as_float((uint32_t)(127 + e) << 23);
     h.scale[t] = up * a.scale_log2;
+    // Scores want sum_g min_g sum(q) - 64 scale_g sum(q at odd codes).  That is one product more over 16 "coordinates" of a token: the minima of the groups,
+    // again, their scales, again, with the sums (as two fp16 numbers, high and low part) as the query's entries.  A lane has groups 2 (c % 2), + 1 (d = 64:
+    // 0, 1), the high parts for c < 2 (d = 64: c = 0), the low ones otherwise (c = 1; none).
+    constexpr int G = Heads<D, NT>::kGroups;
+    float all[G], odd[G];
 #pragma unroll
-    for (int w = 0; w < Heads<D, NT>::kGroups; ++w) {
+    for (int w = 0; w < G; ++w) {
       const uint32_t v[4] = {raw[w].x, raw[w].y, raw[w].z, raw[w].w};
-      float sum = 0.f;
+      all[w] = odd[w] = 0.f;
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const float2 f = to_float2<T>(v[i]);
         h.q[t][w][i] = from_float2<__half>(f.x * down, f.y * down);
         const float2 r = to_float2<__half>(h.q[t][w][i]);
-        sum += r.x + r.y;
+        all[w] += r.x + r.y;
+        if (i & 1) odd[w] += r.x + r.y;
       }
-      sum += __shfl_xor_sync(0xffffffffu, sum, 1);
-      sum += __shfl_xor_sync(0xffffffffu, sum, 2);
-      h.qsum[t][w] = sum;
+#pragma unroll
+      for (int o = 1; o < 4; o <<= 1) {
+        all[w] += __shfl_xor_sync(0xffffffffu, all[w], o);
+        odd[w] += __shfl_xor_sync(0xffffffffu, odd[w], o);
+      }
+      odd[w] *= -64.f;
     }
+    const bool second = G == 4 && (c & 1), low = G == 4 ? c >= 2 : c == 1, none = G == 2 && c >= 2;
+    auto operand = [&](const float (&x)[G]) {
+      const float x0 = second ? x[G - 2] : x[0], x1 = second ? x[G - 1] : x[1];
+      const uint32_t high = from_float2<__half>(x0, x1);
+      const float2 f = to_float2<__half>(high);
+      return none ? 0u : low ? from_float2<__half>(x0 - f.x, x1 - f.y) : high;
+    };
+    h.fix[t][0] = operand(all);
+    h.fix[t][1] = operand(odd);
     h.ref[t] = -INFINITY; h.sum[t] = 0.f;
 #pragma unroll
     for (int m = 0; m < D / 16; ++m)
@@ -138,7 +171,7 @@ __device__ __forceinline__ void attend_block(Heads<D, NT>& h, const uint8_t* blo
   float x[NT][4];                                        // tokens 2 c, 2 c + 1, 8 + 2 c, 9 + 2 c
 #pragma unroll
   for (int half = 0; half < 2; ++half) {
-    uint32_t kw[G], sc[2 * G];
+    uint32_t kw[G], sc[G];                               // codes of token lane / 4; scales of tokens 2 c, 2 c + 1
     if constexpr (D == 128) {
       const uint4 v = *reinterpret_cast<const uint4*>(block + half * 512 + lane * 16);
       kw[0] = v.x; kw[1] = v.y; kw[2] = v.z; kw[3] = v.w;
@@ -149,31 +182,41 @@ __device__ __forceinline__ void attend_block(Heads<D, NT>& h, const uint8_t* blo
 #pragma unroll
     for (int i = 0; i < G / 2; ++i) {
       const uint4 v = *reinterpret_cast<const uint4*>(block + Block<D>::kScaleK + (half * 4 + c) * G * 8 + i * 16);
-      sc[4 * i] = v.x; sc[4 * i + 1] = v.y; sc[4 * i + 2] = v.z; sc[4 * i + 3] = v.w;
+      sc[2 * i] = v.x; sc[2 * i + 1] = v.z;
     }
-    float s[NT][2];
+    // minima and scales of token lane / 4, two groups
+    const uint4 f = *reinterpret_cast<const uint4*>(block + Block<D>::kScaleK + ((half * 4 + lane / 8) * G + (G == 4 ? 2 * (c & 1) : 0)) * 8);
+    const uint32_t pick = lane & 4 ? 0x7632u : 0x5410u;
+    float fix[4];
+    mma_f16_first(fix, h.fix[0][0], NT == 2 ? h.fix[NT - 1][0] : 0u, h.fix[0][1], NT == 2 ? h.fix[NT - 1][1] : 0u, __byte_perm(f.y, f.w, pick), __byte_perm(f.x, f.z, pick));
+    uint64_t s2[NT];
 #pragma unroll
-    for (int t = 0; t < NT; ++t) s[t][0] = s[t][1] = 0.f;
+    for (int t = 0; t < NT; ++t) s2[t] = pack_f2(fix[2 * t], fix[2 * t + 1]);
 #pragma unroll
     for (int w = 0; w < G; ++w) {
-      const uint32_t b0 = codes_at_4(kw[w] << 4), b1 = codes_at_4(kw[w]), b2 = codes_at_4(kw[w] >> 4), b3 = codes_at_4(kw[w] >> 8);
+      uint32_t k[4];
+      codes_of(kw[w], k);
       float acc[4];
-      acc[0] = acc[1] = -64.f * h.qsum[0][w];
-      acc[2] = acc[3] = NT == 2 ? -64.f * h.qsum[NT - 1][w] : 0.f;
-      mma_f16(acc, h.q[0][w][0], NT == 2 ? h.q[NT - 1][w][0] : 0u, h.q[0][w][1], NT == 2 ? h.q[NT - 1][w][1] : 0u, b0, b1);
-      mma_f16(acc, h.q[0][w][2], NT == 2 ? h.q[NT - 1][w][2] : 0u, h.q[0][w][3], NT == 2 ? h.q[NT - 1][w][3] : 0u, b2, b3);
-      const float2 fs = to_float2<__half>(sc[2 * w]), fm = to_float2<__half>(sc[2 * w + 1]);
+      mma_f16_first(acc, h.q[0][w][0], NT == 2 ? h.q[NT - 1][w][0] : 0u, h.q[0][w][1], NT == 2 ? h.q[NT - 1][w][1] : 0u, k[0], k[1]);
+      mma_f16(acc, h.q[0][w][2], NT == 2 ? h.q[NT - 1][w][2] : 0u, h.q[0][w][3], NT == 2 ? h.q[NT - 1][w][3] : 0u, k[2], k[3]);
+      const float2 fs = to_float2<__half>(sc[w]);
 #pragma unroll
-      for (int t = 0; t < NT; ++t) {
-        s[t][0] = fmaf(acc[2 * t], fs.x, fmaf(h.qsum[t][w], fm.x, s[t][0]));
-        s[t][1] = fmaf(acc[2 * t + 1], fs.y, fmaf(h.qsum[t][w], fm.y, s[t][1]));
-      }
+      for (int t = 0; t < NT; ++t) s2[t] = ffma2(pack_f2(acc[2 * t], acc[2 * t + 1]), pack_f2(fs.x, fs.y), s2[t]);
     }
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
-      x[t][2 * half] = half * 8 + 2 * c < valid ? s[t][0] * h.scale[t] : -INFINITY;
-      x[t][2 * half + 1] = half * 8 + 2 * c + 1 < valid ? s[t][1] * h.scale[t] : -INFINITY;
+      float s0, s1;
+      unpack_f2(s2[t], s0, s1);
+      x[t][2 * half] = s0 * h.scale[t];
+      x[t][2 * half + 1] = s1 * h.scale[t];
     }
+  }
+  if (valid < kBlockTokens) {
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if ((i >> 1) * 8 + 2 * c + (i & 1) >= valid) x[t][i] = -INFINITY;
   }
   // ---- weights ----
   float top[NT];
@@ -225,8 +268,10 @@ __device__ __forceinline__ void attend_block(Heads<D, NT>& h, const uint8_t* blo
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       const int u = 4 * i + j, w = u / 2;
-      auto value = [&](uint32_t bits, int half) { return u32(__hfma2(__hadd2(h2(codes_at_4(bits)), minus64), h2(sv[half][2 * w]), h2(sv[half][2 * w + 1]))); };
-      const uint32_t a0 = value(vw[j] << 4, 0), a1 = value(vw[j], 0), a2 = value(vw[j] >> 4, 1), a3 = value(vw[j] >> 8, 1);
+      uint32_t k[4];
+      codes_of(vw[j], k);
+      auto value = [&](__half2 code, int half) { return u32(__hfma2(code, h2(sv[half][2 * w]), h2(sv[half][2 * w + 1]))); };
+      const uint32_t a0 = value(h2(k[0]), 0), a1 = value(__hadd2(h2(k[1]), minus64), 0), a2 = value(h2(k[2]), 1), a3 = value(__hadd2(h2(k[3]), minus64), 1);
 #pragma unroll
       for (int t = 0; t < NT; ++t) {
         mma_f16(h.o[t][u], a0, a1, a2, a3, p[t][0], p[t][1]);
