@@ -2,10 +2,10 @@
 //
 // A warp takes a block of 16 tokens of one key head and up to 16 query heads that read it, on the warp-level tensor cores
 // (mma.sync m16n8k16, fp16 operands, fp32 sums):
-//   S = Q K^T   with the codes of K as fp16 numbers (see codes_of), exact sums of a group, s = sum_g scale_g sum(q c) + min_g sum_g(q) in fp32
+//   S^T = K Q^T with the codes of K as fp16 numbers (see codes_of), exact sums of a group, s = sum_g scale_g sum(q c) + min_g sum_g(q) in fp32
 //   p = exp2(s c - ref), the reference of a head moves when it is exceeded by more than 2^8
 //   O^T += V^T P^T   V = min + scale * code in fp16 (exact codes, one rounding); its 32-bit words hold four tokens of two coordinates,
-//               so that masking yields operands with pairs of tokens, and P^T is what the lanes have after S.
+//               so that masking yields operands with pairs of tokens; P^T is turned once (movmatrix).
 // fp16 and not bf16 for the weights and values: a product is then off by 2^-11 and not 2^-8, which is what the output's type can show; V fits by
 // its format, a head's query after a power of two.  For fp16 results, which show 2^-11, the weights' rounding errors go through the products too.
 //
@@ -33,7 +33,7 @@ struct CacheAttnArgs {
   int requests, width, q_heads, out_kind;      // out_kind: hyperattn_dtype
   int chunks;                                  // of query heads of a key head
   float scale_log2;
-  int* starts;                                 // [requests + 1] blocks before each request; [requests + 1]: blocks of a warp's part
+  int* starts;                                 // [requests + 1] units before each request; [requests + 1]: units of a warp's part
   float* part;                                 // pieces: [slots][heads of a chunk][d + 2] (outputs, reference, sum)
   int part_heads;                              // heads of a chunk
 };
@@ -65,27 +65,29 @@ __device__ __forceinline__ void codes_of(uint32_t w, uint32_t (&k)[4]) {
   k[2] = u32(__hfma2(h2(k[3]), minus16, h2((up & 0x00ff00ffu) | 0x64006400u)));
 }
 
-// What a warp keeps of the heads it works for: NT = 1: up to 8 of them (a lane's head: lane / 4), NT = 2: up to 16 (and lane / 4 + 8)
+// What a warp keeps of the heads it works for: NT tiles of up to 8 of them.  As an operand a lane has head lane / 4, in results heads 2 c, 2 c + 1.
+constexpr float kNoReference = 3.0e38f;
 template <int D, int NT>
 struct Heads {
   static constexpr int kGroups = D / kGroup;
   uint32_t q[NT][kGroups][4];           // fp16 pairs: coordinates 32 w + 8 c + 0..7
   uint32_t fix[NT][2];                  // operands of the product that adds what belongs to minima and to codes that are 64 too large, see load_heads
-  float scale[NT];                      // to the base-2 scores
-  float ref[NT], sum[NT];               // sum: of this lane's tokens
-  float o[NT][D / 16][4];               // O^T: coordinates lane / 4 (+ 8) of every 16, heads 2 c, 2 c + 1 (+ 8)
+  float scale[NT][2];                   // to the base-2 scores
+  float minus[NT][2], sum[NT][2];       // minus the reference (kNoReference: none yet); sum of this lane's tokens
+  float o[NT][D / 16][4];               // O^T: coordinates lane / 4 (+ 8) of every 16
 };
 
 template <int D, int NT, class T>
 __device__ __forceinline__ void load_heads(Heads<D, NT>& h, const CacheAttnArgs& a, int request, int first_head, int heads) {
+  constexpr int G = Heads<D, NT>::kGroups;
   const int lane = threadIdx.x & 31, c = lane & 3;
 #pragma unroll
   for (int t = 0; t < NT; ++t) {
     const int head = lane / 4 + 8 * t;
     float top = 0.f;
-    uint4 raw[Heads<D, NT>::kGroups];
+    uint4 raw[G];
 #pragma unroll
-    for (int w = 0; w < Heads<D, NT>::kGroups; ++w) {
+    for (int w = 0; w < G; ++w) {
       raw[w] = make_uint4(0, 0, 0, 0);
       if (head < heads)
         raw[w] = *reinterpret_cast<const uint4*>(reinterpret_cast<const T*>(a.q) + request * a.q_row + (first_head + head) * a.q_head + 32 * w + 8 * c);
@@ -98,12 +100,10 @@ __device__ __forceinline__ void load_heads(Heads<D, NT>& h, const CacheAttnArgs&
     // 2^-e, e the exponent of the largest entry (0 and what is not finite: as it is)
     int e = (int)(__float_as_uint(top) >> 23) - 127;
     e = top == 0.f || !(top < INFINITY) ? 0 : min(max(e, -126), 126);
-    const float down = __uint_as_float((uint32_t)(127 - e) << 23), up = __uint_as_float((uint32_t)(127 + e) << 23);
-    h.scale[t] = up * a.scale_log2;
+    const float down = __uint_as_float((uint32_t)(127 - e) << 23), scale = __uint_as_float((uint32_t)(127 + e) << 23) * a.scale_log2;
     // Scores want sum_g min_g sum(q) - 64 scale_g sum(q at odd codes).  That is one product more over 16 "coordinates" of a token: the minima of the groups,
     // again, their scales, again, with the sums (as two fp16 numbers, high and low part) as the query's entries.  A lane has groups 2 (c % 2), + 1 (d = 64:
     // 0, 1), the high parts for c < 2 (d = 64: c = 0), the low ones otherwise (c = 1; none).
-    constexpr int G = Heads<D, NT>::kGroups;
     float all[G], odd[G];
 #pragma unroll
     for (int w = 0; w < G; ++w) {
@@ -133,32 +133,16 @@ __device__ __forceinline__ void load_heads(Heads<D, NT>& h, const CacheAttnArgs&
     };
     h.fix[t][0] = operand(all);
     h.fix[t][1] = operand(odd);
-    h.ref[t] = -INFINITY; h.sum[t] = 0.f;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      h.scale[t][i] = __shfl_sync(0xffffffffu, scale, 8 * c + 4 * i);
+      h.minus[t][i] = kNoReference;
+      h.sum[t][i] = 0.f;
+    }
 #pragma unroll
     for (int m = 0; m < D / 16; ++m)
 #pragma unroll
       for (int i = 0; i < 4; ++i) h.o[t][m][i] = 0.f;
-  }
-}
-
-// The references move to the scores' maximum where they are exceeded; sums and outputs follow.  top: the lane's largest score of its head.
-template <int D, int NT>
-__device__ __forceinline__ void move_reference(Heads<D, NT>& h, float (&top)[NT]) {
-  const int lane = threadIdx.x & 31, c = lane & 3;
-#pragma unroll
-  for (int t = 0; t < NT; ++t) {
-    float m = top[t];
-    m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 1));
-    m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 2));
-    float alpha = 1.f;
-    if (m > h.ref[t] + kMoveAt) { alpha = ex2(h.ref[t] - m); h.ref[t] = m; }      // (from -infinity: 0)
-    h.sum[t] *= alpha;
-    const float a0 = __shfl_sync(0xffffffffu, alpha, 8 * c), a1 = __shfl_sync(0xffffffffu, alpha, 8 * c + 4);
-#pragma unroll
-    for (int m16 = 0; m16 < D / 16; ++m16) {
-      h.o[t][m16][0] *= a0; h.o[t][m16][1] *= a1;
-      h.o[t][m16][2] *= a0; h.o[t][m16][3] *= a1;
-    }
   }
 }
 
@@ -167,48 +151,49 @@ template <int D, int NT, bool FINE>
 __device__ __forceinline__ void attend_block(Heads<D, NT>& h, const uint8_t* block, int valid) {
   constexpr int G = D / kGroup;
   const int lane = threadIdx.x & 31, c = lane & 3;
-  // ---- scores ----
-  float x[NT][4];                                        // tokens 2 c, 2 c + 1, 8 + 2 c, 9 + 2 c
+  // ---- scores: S^T of tokens lane / 4 (+ 8) and heads 2 c, 2 c + 1 ----
+  uint32_t kw[2][G], sc[2][G / 2], mn[2];                // codes, scales of group pairs, minima of the lane's pair (see load_heads)
+  if constexpr (D == 128) {
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+      const uint4 v = *reinterpret_cast<const uint4*>(block + half * 512 + lane * 16);
+      kw[half][0] = v.x; kw[half][1] = v.y; kw[half][2] = v.z; kw[half][3] = v.w;
+    }
+  } else {
+    const uint4 v = *reinterpret_cast<const uint4*>(block + lane * 16);
+    kw[0][0] = v.x; kw[0][1] = v.y; kw[1][0] = v.z; kw[1][1] = v.w;
+  }
+  const uint32_t pick = lane & 4 ? 0x7632u : 0x5410u;    // of two halves with tokens (2 i, 2 i + 1): the lane's token
 #pragma unroll
   for (int half = 0; half < 2; ++half) {
-    uint32_t kw[G], sc[G];                               // codes of token lane / 4; scales of tokens 2 c, 2 c + 1
-    if constexpr (D == 128) {
-      const uint4 v = *reinterpret_cast<const uint4*>(block + half * 512 + lane * 16);
-      kw[0] = v.x; kw[1] = v.y; kw[2] = v.z; kw[3] = v.w;
-    } else {
-      const uint2 v = *reinterpret_cast<const uint2*>(block + lane * 16 + half * 8);
-      kw[0] = v.x; kw[1] = v.y;
+    const uint8_t* at = block + Block<D>::kScaleK + (half * 4 + lane / 8) * G * 8;
+    const uint4 v = *reinterpret_cast<const uint4*>(at);
+    sc[half][0] = __byte_perm(v.x, v.z, pick);
+    if constexpr (G == 2) mn[half] = __byte_perm(v.y, v.w, pick);
+    else {
+      const uint4 u = *reinterpret_cast<const uint4*>(at + 16);
+      sc[half][G / 2 - 1] = __byte_perm(u.x, u.z, pick);
+      mn[half] = __byte_perm(c & 1 ? u.y : v.y, c & 1 ? u.w : v.w, pick);
     }
+  }
+  float s[NT][4];
 #pragma unroll
-    for (int i = 0; i < G / 2; ++i) {
-      const uint4 v = *reinterpret_cast<const uint4*>(block + Block<D>::kScaleK + (half * 4 + c) * G * 8 + i * 16);
-      sc[2 * i] = v.x; sc[2 * i + 1] = v.z;
-    }
-    // minima and scales of token lane / 4, two groups
-    const uint4 f = *reinterpret_cast<const uint4*>(block + Block<D>::kScaleK + ((half * 4 + lane / 8) * G + (G == 4 ? 2 * (c & 1) : 0)) * 8);
-    const uint32_t pick = lane & 4 ? 0x7632u : 0x5410u;
-    float fix[4];
-    mma_f16_first(fix, h.fix[0][0], NT == 2 ? h.fix[NT - 1][0] : 0u, h.fix[0][1], NT == 2 ? h.fix[NT - 1][1] : 0u, __byte_perm(f.y, f.w, pick), __byte_perm(f.x, f.z, pick));
-    uint64_t s2[NT];
+  for (int t = 0; t < NT; ++t)
+    mma_f16_first(s[t], mn[0], mn[1], G == 4 && (c & 1) ? sc[0][G / 2 - 1] : sc[0][0], G == 4 && (c & 1) ? sc[1][G / 2 - 1] : sc[1][0], h.fix[t][0], h.fix[t][1]);
 #pragma unroll
-    for (int t = 0; t < NT; ++t) s2[t] = pack_f2(fix[2 * t], fix[2 * t + 1]);
-#pragma unroll
-    for (int w = 0; w < G; ++w) {
-      uint32_t k[4];
-      codes_of(kw[w], k);
-      float acc[4];
-      mma_f16_first(acc, h.q[0][w][0], NT == 2 ? h.q[NT - 1][w][0] : 0u, h.q[0][w][1], NT == 2 ? h.q[NT - 1][w][1] : 0u, k[0], k[1]);
-      mma_f16(acc, h.q[0][w][2], NT == 2 ? h.q[NT - 1][w][2] : 0u, h.q[0][w][3], NT == 2 ? h.q[NT - 1][w][3] : 0u, k[2], k[3]);
-      const float2 fs = to_float2<__half>(sc[w]);
-#pragma unroll
-      for (int t = 0; t < NT; ++t) s2[t] = ffma2(pack_f2(acc[2 * t], acc[2 * t + 1]), pack_f2(fs.x, fs.y), s2[t]);
-    }
+  for (int w = 0; w < G; ++w) {
+    uint32_t k0[4], k1[4];
+    codes_of(kw[0][w], k0);
+    codes_of(kw[1][w], k1);
+    const float2 f0 = to_float2<__half>(sc[0][w / 2]), f1 = to_float2<__half>(sc[1][w / 2]);
+    const float a0 = w & 1 ? f0.y : f0.x, a1 = w & 1 ? f1.y : f1.x;
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
-      float s0, s1;
-      unpack_f2(s2[t], s0, s1);
-      x[t][2 * half] = s0 * h.scale[t];
-      x[t][2 * half + 1] = s1 * h.scale[t];
+      float acc[4];
+      mma_f16_first(acc, k0[0], k1[0], k0[1], k1[1], h.q[t][w][0], h.q[t][w][1]);
+      mma_f16(acc, k0[2], k1[2], k0[3], k1[3], h.q[t][w][2], h.q[t][w][3]);
+      s[t][0] = fmaf(acc[0], a0, s[t][0]); s[t][1] = fmaf(acc[1], a0, s[t][1]);
+      s[t][2] = fmaf(acc[2], a1, s[t][2]); s[t][3] = fmaf(acc[3], a1, s[t][3]);
     }
   }
   if (valid < kBlockTokens) {
@@ -216,31 +201,58 @@ __device__ __forceinline__ void attend_block(Heads<D, NT>& h, const uint8_t* blo
     for (int t = 0; t < NT; ++t)
 #pragma unroll
       for (int i = 0; i < 4; ++i)
-        if ((i >> 1) * 8 + 2 * c + (i & 1) >= valid) x[t][i] = -INFINITY;
+        if (lane / 4 + 8 * (i >> 1) >= valid) s[t][i] = -INFINITY;
   }
   // ---- weights ----
-  float top[NT];
-  bool move = false;
+  float y[NT][4], most = -INFINITY;
 #pragma unroll
-  for (int t = 0; t < NT; ++t) {
-    top[t] = fmaxf(fmaxf(x[t][0], x[t][1]), fmaxf(x[t][2], x[t][3]));
-    move = move || top[t] > h.ref[t] + kMoveAt;
+  for (int t = 0; t < NT; ++t)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      y[t][i] = fmaf(s[t][i], h.scale[t][i & 1], h.minus[t][i & 1]);
+      most = fmaxf(most, y[t][i]);
+    }
+  if (__any_sync(0xffffffffu, most > kMoveAt)) {
+    // the references move to the scores' maximum where they are exceeded; sums and outputs follow
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        float m = fmaxf(s[t][i], s[t][i + 2]) * h.scale[t][i];
+#pragma unroll
+        for (int o = 4; o < 32; o <<= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+        if (m + h.minus[t][i] > kMoveAt) {
+          const float alpha = h.minus[t][i] == kNoReference ? 0.f : ex2(-h.minus[t][i] - m);
+          h.minus[t][i] = -m;
+          h.sum[t][i] *= alpha;
+#pragma unroll
+          for (int u = 0; u < D / 16; ++u) { h.o[t][u][i] *= alpha; h.o[t][u][i + 2] *= alpha; }
+        }
+        y[t][i] = fmaf(s[t][i], h.scale[t][i], h.minus[t][i]);
+        y[t][i + 2] = fmaf(s[t][i + 2], h.scale[t][i], h.minus[t][i]);
+      }
   }
-  if (__any_sync(0xffffffffu, move)) move_reference<D, NT>(h, top);
-  uint32_t p[NT][2], rest[NT][2];
+  uint32_t p[NT][2], rest[NT][2];                        // P^T as an operand: head lane / 4, tokens 2 c, 2 c + 1 and 8 + 2 c, 9 + 2 c
+  auto turn = [](uint32_t v) {
+    uint32_t r;
+    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
+    return r;
+  };
 #pragma unroll
   for (int t = 0; t < NT; ++t) {
-    const float ref = h.ref[t] == -INFINITY ? 0.f : h.ref[t];
     float e[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) e[i] = ex2(x[t][i] - ref);
-    h.sum[t] += (e[0] + e[1]) + (e[2] + e[3]);
-    p[t][0] = from_float2<__half>(e[0], e[1]);
-    p[t][1] = from_float2<__half>(e[2], e[3]);
-    if constexpr (FINE) {
-      const float2 a = to_float2<__half>(p[t][0]), b = to_float2<__half>(p[t][1]);
-      rest[t][0] = from_float2<__half>(e[0] - a.x, e[1] - a.y);
-      rest[t][1] = from_float2<__half>(e[2] - b.x, e[3] - b.y);
+    for (int i = 0; i < 4; ++i) e[i] = ex2(y[t][i]);
+    h.sum[t][0] += e[0] + e[2];
+    h.sum[t][1] += e[1] + e[3];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const uint32_t both = from_float2<__half>(e[2 * i], e[2 * i + 1]);
+      p[t][i] = turn(both);
+      if constexpr (FINE) {
+        const float2 f = to_float2<__half>(both);
+        rest[t][i] = turn(from_float2<__half>(e[2 * i] - f.x, e[2 * i + 1] - f.y));
+      }
     }
   }
   // ---- values ----
@@ -288,14 +300,16 @@ __device__ __forceinline__ void put(void* out, int kind, size_t at, float x) {
 }
 
 constexpr int kWarps = 4;
-constexpr int kLeastPart = 2;           // blocks of a warp's part at least
 constexpr int kMaxRequests = 4096;      // running sums in shared memory
 
+// A unit of work and of the ring: 32 (d = 128) or 64 tokens of a segment, 5 KB.
 template <int D>
 struct Ring {
-  static constexpr int kStages = D == 128 ? 4 : 8;                       // blocks on their way, a warp
-  static constexpr int kWarpBytes = kStages * Block<D>::kBytes;          // (>= 16 x D floats: a warp's outputs, when the parts are put together)
-  static constexpr int kOffBar = kWarps * kWarpBytes, kOffMisc = kOffBar + kWarps * kStages * 8, kOffStarts = kOffMisc + 1280;
+  static constexpr int kUnit = D == 128 ? 2 : 4;                         // blocks
+  static constexpr int kUnitBytes = kUnit * Block<D>::kBytes, kUnitTokens = kUnit * kBlockTokens;
+  static constexpr int kStages = 2;                                      // units on their way, a warp
+  static constexpr int kWarpBytes = kStages * kUnitBytes;                // (>= 16 x D floats: a warp's outputs, when the parts are put together)
+  static constexpr int kOffBar = kWarps * kWarpBytes, kOffMisc = kOffBar + kWarps * kStages * 8, kOffStarts = kOffMisc + 768;
   static constexpr int bytes(int requests) { return kOffStarts + (requests + 1) * 4; }
 };
 // CTAs that an SM holds: by registers (two tiles of heads need 168 a thread), and by shared memory
@@ -305,8 +319,8 @@ template <int D> int ctas_by_memory(int requests) { return 227 * 1024 / (Ring<D>
 __device__ __forceinline__ void bulk_copy(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
   asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
 }
-__device__ __forceinline__ int blocks_of(const CacheAttnArgs& a, int r) {
-  return (min(max(a.lengths[r], 0), a.width * a.cache.page) + kBlockTokens - 1) / kBlockTokens;
+template <int D> __device__ __forceinline__ int units_of(const CacheAttnArgs& a, int r) {
+  return (min(max(a.lengths[r], 0), a.width * a.cache.page) + Ring<D>::kUnitTokens - 1) / Ring<D>::kUnitTokens;
 }
 // where the pieces of a segment lie: see combine
 __device__ __forceinline__ float* piece_at(const CacheAttnArgs& a, long long slot, int head, int d) { return a.part + (slot * a.part_heads + head) * (d + 2); }
@@ -316,7 +330,7 @@ __global__ void __launch_bounds__(32 * kWarps, (ctas_by_registers<D, NT>())) cac
   using R = Ring<D>;
   constexpr bool FINE = std::is_same<T, __half>::value;
   extern __shared__ __align__(128) uint8_t smem[];
-  int* s_starts = reinterpret_cast<int*>(smem + R::kOffStarts);          // [requests + 1] blocks (of one segment each) before a request
+  int* s_starts = reinterpret_cast<int*>(smem + R::kOffStarts);          // [requests + 1] units (of one segment each) before a request
   int* s_sums = reinterpret_cast<int*>(smem + R::kOffMisc);              // [kWarps]
   volatile int* s_abort = reinterpret_cast<volatile int*>(smem + R::kOffMisc + 64);
   float* s_stat = reinterpret_cast<float*>(smem + R::kOffMisc + 128);    // [kWarps][16][2] references, sums
@@ -329,10 +343,10 @@ __global__ void __launch_bounds__(32 * kWarps, (ctas_by_registers<D, NT>())) cac
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   wait_for_stream();
-  // ---- running sum of the requests' blocks ----
+  // ---- running sum of the requests' units ----
   const int per = (a.requests + 32 * kWarps - 1) / (32 * kWarps), r0 = min(a.requests, tid * per), r1 = min(a.requests, r0 + per);
   int mine = 0;
-  for (int r = r0; r < r1; ++r) mine += blocks_of(a, r);
+  for (int r = r0; r < r1; ++r) mine += units_of<D>(a, r);
   int run = mine;
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) { const int y = __shfl_up_sync(0xffffffffu, run, o); if (lane >= o) run += y; }
@@ -340,99 +354,98 @@ __global__ void __launch_bounds__(32 * kWarps, (ctas_by_registers<D, NT>())) cac
   __syncthreads();
   run -= mine;
   for (int w = 0; w < warp; ++w) run += s_sums[w];
-  for (int r = r0; r < r1; ++r) { s_starts[r] = run; run += blocks_of(a, r); }
+  for (int r = r0; r < r1; ++r) { s_starts[r] = run; run += units_of<D>(a, r); }
   if (tid == 32 * kWarps - 1) s_starts[a.requests] = run;
   __syncthreads();
   const int segs = a.cache.heads * a.chunks;                             // of a request
   const long long total = (long long)s_starts[a.requests] * segs, warps = (long long)gridDim.x * kWarps;
-  const int part = (int)max((long long)kLeastPart, (total + warps - 1) / warps);
+  const int part = (int)max(1ll, (total + warps - 1) / warps);
   if (blockIdx.x == 0) {
     for (int r = tid; r <= a.requests; r += 32 * kWarps) a.starts[r] = s_starts[r];
     if (tid == 0) a.starts[a.requests + 1] = part;
   }
   const long long cta_first = (long long)blockIdx.x * kWarps * part, cta_end = min(cta_first + (long long)kWarps * part, total);
   const long long first = min(cta_first + (long long)warp * part, total), end = min(first + part, total);
-  const int count = (int)(end - first);                                  // blocks of this warp
+  const int count = (int)(end - first);                                  // units of this warp
   const int subs = a.cache.page / kBlockTokens, per_kv = a.q_heads / a.cache.heads;
 
-  // A lane knows one of 32 blocks of the part: its segment (of all requests'), how many tokens there are from it on, and which block of the cache it
-  // is (-1: none).
+  // A lane knows one block of the next 32 / kUnit units: its segment (of all requests'), how many tokens there are from its unit on, and which block of
+  // the cache it is (-1: none).
+  constexpr int U = R::kUnit, kBatch = 32 / U;
   struct Known { int seg, left, at; };
-  auto know = [&](int i) {
+  auto know = [&](int unit) {                                            // units unit .. unit + kBatch - 1
     Known k = {0, 0, -1};
+    const int i = unit + lane / U;
     if (i >= count) return k;
     const long long n = first + i;
-    int lo = 0, hi = a.requests;                                         // the last request whose blocks start there or before
+    int lo = 0, hi = a.requests;                                         // the last request whose units start there or before
     const int t = (int)(n / segs);
     while (hi - lo > 1) { const int mid = (lo + hi) >> 1; if (s_starts[mid] <= t) lo = mid; else hi = mid; }
-    const int blocks = s_starts[lo + 1] - s_starts[lo];
+    const int units = s_starts[lo + 1] - s_starts[lo];
     const int rest = (int)(n - (long long)s_starts[lo] * segs);
-    const int seg = rest / blocks, b = rest - seg * blocks;
+    const int seg = rest / units, b = (rest - seg * units) * U + lane % U;
     k.seg = lo * segs + seg;
-    k.left = min(a.lengths[lo], a.width * a.cache.page) - b * kBlockTokens;
-    const int page = a.table[(size_t)lo * a.width + b / subs];
-    if (page >= 0 && page < a.cache.num_pages) k.at = (page * a.cache.heads + seg / a.chunks) * subs + b % subs;
+    k.left = min(a.lengths[lo], a.width * a.cache.page) - (b - lane % U) * kBlockTokens;
+    if ((lane % U) * kBlockTokens < k.left) {
+      const int page = a.table[(size_t)lo * a.width + b / subs];
+      if (page >= 0 && page < a.cache.num_pages) k.at = (page * a.cache.heads + seg / a.chunks) * subs + b % subs;
+    }
     return k;
   };
-  int asked = 0;                                                         // blocks whose copies have been asked for
-  auto ask = [&](const Known& k, int from) {                              // the next one, known by lane `from`
-    const int at = __shfl_sync(0xffffffffu, k.at, from);
-    if (lane == 0) {
-      const int st = asked % R::kStages;
-      if (at >= 0) {
-        mbar_expect_tx(bars + 8 * st, Block<D>::kBytes);
-        bulk_copy(ring + st * Block<D>::kBytes, a.cache.pages + (size_t)at * Block<D>::kBytes, Block<D>::kBytes, bars + 8 * st);
-      }
-      mbar_arrive(bars + 8 * st);
-    }
+  int asked = 0;                                                         // units whose copies have been asked for
+  auto ask = [&](const Known& k, int from) {                              // the next one, known by lanes U from, ...
+    const int st = asked % R::kStages;
+    const bool mine = lane / U == from && k.at >= 0;
+    const unsigned all = __ballot_sync(0xffffffffu, mine);
+    if (lane == 0) asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bars + 8 * st), "r"(__popc(all) * Block<D>::kBytes) : "memory");
+    if (mine) bulk_copy(ring + st * R::kUnitBytes + (lane % U) * Block<D>::kBytes, a.cache.pages + (size_t)k.at * Block<D>::kBytes, Block<D>::kBytes, bars + 8 * st);
     ++asked;
   };
-  Known now = know(lane), next = now;
+  Known now = know(0), next = now;
   while (asked < R::kStages && asked < count) ask(now, asked);
   bool ok = true;
   Heads<D, NT> h;
   int segment = -1, request = 0, seg = 0;                                // segment = request * segs + seg
-  // the segment's results, or a piece of them: O in the lanes' fragments, sums of all lanes
+  // the segment's results, or a piece of them
   auto flush = [&](float* to) {                                            // to: null for final results
     const int chunk = seg % a.chunks, kv = seg / a.chunks, first_head = kv * per_kv + chunk * 8 * NT, heads = min(per_kv - chunk * 8 * NT, 8 * NT);
 #pragma unroll
-    for (int t = 0; t < NT; ++t) {
-      float sum = h.sum[t];
-      sum += __shfl_xor_sync(0xffffffffu, sum, 1);
-      sum += __shfl_xor_sync(0xffffffffu, sum, 2);
-      const int head = lane / 4 + 8 * t;
-      if (c == 0 && head < heads) {
-        if (to) { to[head * (D + 2) + D] = h.ref[t]; to[head * (D + 2) + D + 1] = sum; }
-        else a.lse[(size_t)request * a.q_heads + first_head + head] = sum == 0.f ? -INFINITY : (h.ref[t] + log2f(sum)) * 0.6931471805599453f;
-      }
-      const float inv = to ? 1.f : sum == 0.f ? 0.f : 1.f / sum;
-      const float inv0 = __shfl_sync(0xffffffffu, inv, 8 * c), inv1 = __shfl_sync(0xffffffffu, inv, 8 * c + 4);
+    for (int t = 0; t < NT; ++t)
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
-        const int hd = 8 * t + 2 * c + i;
-        if (hd < heads) {
+        float sum = h.sum[t][i];
+#pragma unroll
+        for (int o = 4; o < 32; o <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+        const float ref = h.minus[t][i] == kNoReference ? -INFINITY : -h.minus[t][i];
+        const int head = 8 * t + 2 * c + i;
+        if (head < heads) {
+          const size_t row = (size_t)request * a.q_heads + first_head + head;
+          if (lane < 4) {
+            if (to) { to[head * (D + 2) + D] = ref; to[head * (D + 2) + D + 1] = sum; }
+            else a.lse[row] = sum == 0.f ? -INFINITY : (ref + log2f(sum)) * 0.6931471805599453f;
+          }
+          const float inv = sum == 0.f ? 0.f : 1.f / sum;
 #pragma unroll
           for (int m = 0; m < D / 16; ++m)
 #pragma unroll
             for (int up = 0; up < 2; ++up) {
               const int x = 16 * m + lane / 4 + 8 * up;
               const float v = h.o[t][m][i + 2 * up];
-              if (to) to[hd * (D + 2) + x] = v;
-              else put(a.out, a.out_kind, ((size_t)request * a.q_heads + first_head + hd) * D + x, v * (i ? inv1 : inv0));
+              if (to) to[head * (D + 2) + x] = v;
+              else put(a.out, a.out_kind, row * D + x, v * inv);
             }
         }
       }
-    }
   };
   bool together = false;                                                 // the whole CTA works for one segment
-  for (int n = 0; n < count && ok; ++n) {
-    const int at = n & 31;
+  for (int n = 0; n < count; ++n) {
+    const int at = n % kBatch;
     if (at == 0) {
       if (n > 0) now = next;
-      next = know(n + 32 + lane);
+      next = know(n + kBatch);
     }
-    const int sg = __shfl_sync(0xffffffffu, now.seg, at), left = __shfl_sync(0xffffffffu, now.left, at);
-    const bool there = __shfl_sync(0xffffffffu, now.at, at) >= 0;
+    const int sg = __shfl_sync(0xffffffffu, now.seg, at * U), left = __shfl_sync(0xffffffffu, now.left, at * U);
+    const unsigned there = __ballot_sync(0xffffffffu, now.at >= 0) >> (at * U);
     if (sg != segment) {
       segment = sg;
       request = segment / segs; seg = segment - request * segs;
@@ -442,11 +455,13 @@ __global__ void __launch_bounds__(32 * kWarps, (ctas_by_registers<D, NT>())) cac
     const int st = n % R::kStages;
     ok = warp_wait<12>(bars + 8 * st, (uint32_t)(n / R::kStages) & 1, s_abort, status);
     if (!ok) break;
-    if (there) attend_block<D, NT, FINE>(h, smem + warp * R::kWarpBytes + st * Block<D>::kBytes, min(left, kBlockTokens));
+#pragma unroll 1
+    for (int b = 0; b < U; ++b)
+      if ((there >> b) & 1) attend_block<D, NT, FINE>(h, smem + warp * R::kWarpBytes + st * R::kUnitBytes + b * Block<D>::kBytes, left - b * kBlockTokens);
     __syncwarp();
-    if (asked < count) { if (at + R::kStages < 32) ask(now, at + R::kStages); else ask(next, at + R::kStages - 32); }
-    if (left <= kBlockTokens || n + 1 == count) {                          // the segment's last block, or the part's
-      const long long blocks = s_starts[request + 1] - s_starts[request], seg_first = (long long)s_starts[request] * segs + seg * blocks, seg_end = seg_first + blocks;
+    if (asked < count) { if (at + R::kStages < kBatch) ask(now, at + R::kStages); else ask(next, at + R::kStages - kBatch); }
+    if (left <= R::kUnitTokens || n + 1 == count) {                        // the segment's last unit, or the part's
+      const long long units = s_starts[request + 1] - s_starts[request], seg_first = (long long)s_starts[request] * segs + seg * units, seg_end = seg_first + units;
       if (seg_first >= first && seg_end <= end) flush(nullptr);
       else {
         together = seg_first <= cta_first && seg_end >= cta_end;
@@ -461,16 +476,19 @@ __global__ void __launch_bounds__(32 * kWarps, (ctas_by_registers<D, NT>())) cac
     float* s_o = reinterpret_cast<float*>(smem + warp * R::kWarpBytes);  // [8 NT][D] of this warp
     if (together) {
 #pragma unroll
-      for (int t = 0; t < NT; ++t) {
-        float sum = h.sum[t];
-        sum += __shfl_xor_sync(0xffffffffu, sum, 1);
-        sum += __shfl_xor_sync(0xffffffffu, sum, 2);
-        if (c == 0) { s_stat[(warp * 16 + lane / 4 + 8 * t) * 2] = h.ref[t]; s_stat[(warp * 16 + lane / 4 + 8 * t) * 2 + 1] = sum; }
+      for (int t = 0; t < NT; ++t)
 #pragma unroll
-        for (int m = 0; m < D / 16; ++m)
+        for (int i = 0; i < 2; ++i) {
+          const int head = 8 * t + 2 * c + i;
+          float sum = h.sum[t][i];
 #pragma unroll
-          for (int i = 0; i < 4; ++i) s_o[(8 * t + 2 * c + (i & 1)) * D + 16 * m + lane / 4 + 8 * (i >> 1)] = h.o[t][m][i];
-      }
+          for (int o = 4; o < 32; o <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+          if (lane < 4) { s_stat[(warp * 16 + head) * 2] = h.minus[t][i] == kNoReference ? -INFINITY : -h.minus[t][i]; s_stat[(warp * 16 + head) * 2 + 1] = sum; }
+#pragma unroll
+          for (int m = 0; m < D / 16; ++m)
+#pragma unroll
+            for (int up = 0; up < 2; ++up) s_o[head * D + 16 * m + lane / 4 + 8 * up] = h.o[t][m][i + 2 * up];
+        }
     }
     __syncthreads();
     const int used = (int)((cta_end - cta_first + part - 1) / part);     // warps that have a part
@@ -507,11 +525,11 @@ __global__ void __launch_bounds__(kJoinThreads) join_kernel(const __grid_constan
   const int segs = a.cache.heads * a.chunks, per_kv = a.q_heads / a.cache.heads;
   const int r = blockIdx.x / segs, seg = blockIdx.x - r * segs, kv = seg / a.chunks, chunk = seg - kv * a.chunks;
   const int first_head = kv * per_kv + chunk * a.part_heads, heads = min(per_kv - chunk * a.part_heads, a.part_heads);
-  const long long part = a.starts[a.requests + 1], blocks = a.starts[r + 1] - a.starts[r];
-  const long long begin = (long long)a.starts[r] * segs + seg * blocks, end = begin + blocks, cta_part = part * kWarps, total = (long long)a.starts[a.requests] * segs;
+  const long long part = a.starts[a.requests + 1], units = a.starts[r + 1] - a.starts[r];
+  const long long begin = (long long)a.starts[r] * segs + seg * units, end = begin + units, cta_part = part * kWarps, total = (long long)a.starts[a.requests] * segs;
   const int lane = threadIdx.x % LANES, row = threadIdx.x / LANES;
   const int h0 = blockIdx.y * heads_per_cta, h1 = min(h0 + heads_per_cta, heads);
-  if (blocks == 0) {
+  if (units == 0) {
     for (int i = threadIdx.x; i < (h1 - h0) * D; i += kJoinThreads) put(a.out, a.out_kind, ((size_t)r * a.q_heads + first_head + h0) * D + i, 0.f);
     for (int i = h0 + threadIdx.x; i < h1; i += kJoinThreads) a.lse[(size_t)r * a.q_heads + first_head + i] = -INFINITY;
     return;
@@ -579,8 +597,9 @@ Shape shape_of(const hyperattn_cache_attention_params& p) {
   s.chunks = (per_kv + (s.two ? 15 : 7)) / (s.two ? 16 : 8);
   s.part_heads = s.two ? 16 : 8;
   if (s.part_heads > per_kv) s.part_heads = per_kv;
-  const long long blocks = (long long)p.requests * p.cache.kv_heads * s.chunks * (((long long)p.table_width * p.cache.page_tokens + kBlockTokens - 1) / kBlockTokens);
-  const long long ctas = (blocks + kWarps * kLeastPart - 1) / (kWarps * kLeastPart);
+  const int unit = p.cache.d == 64 ? Ring<64>::kUnitTokens : Ring<128>::kUnitTokens;
+  const long long units = (long long)p.requests * p.cache.kv_heads * s.chunks * (((long long)p.table_width * p.cache.page_tokens + unit - 1) / unit);
+  const long long ctas = (units + kWarps - 1) / kWarps;
   const int memory = p.cache.d == 64 ? ctas_by_memory<64>(p.requests) : ctas_by_memory<128>(p.requests), registers = s.two ? ctas_by_registers<128, 2>() : ctas_by_registers<128, 1>();
   const int most = kSms * (memory < registers ? memory : registers);
   s.ctas = (int)(ctas < most ? ctas : most);
