@@ -40,14 +40,12 @@ struct CacheAttnArgs {
 
 // c += A B, or d = A B (no registers to be cleared)
 __device__ __forceinline__ void mma_f16(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
-  asm volatile(
-      "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};\n"
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};\n"
       : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
       : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 __device__ __forceinline__ void mma_f16_first(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
-  asm volatile(
-      "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};\n"
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};\n"
       : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
       : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.f));
 }
@@ -56,13 +54,23 @@ __device__ __forceinline__ uint32_t u32(__half2 v) { return *reinterpret_cast<ui
 // The codes of a word (8 of them, k at bit 4 k) as fp16 pairs (k, k + 4), k = 0..3: even ones as they are, odd ones 64 too large.  A code with the exponent
 // of 2^6 above its bits 4..7 is 64 + c; both codes of a byte with that of 2^10 are 1024 + low + 16 high, from which 16 (64 + high) is taken.  (Two logical
 // operations and half a shift for two pairs: those run at half the rate of the fused multiply-adds and are what a block has most of.)
-__device__ __forceinline__ void codes_of(uint32_t w, uint32_t (&k)[4]) {
-  const __half2 minus16 = __half2half2(__ushort_as_half(0xcc00));
+struct Constants { uint32_t e6, e10, minus16, minus64; };       // fp16 pairs: 2^6, 2^10, -16, -64
+__device__ __forceinline__ Constants constants() {                // (opaque, so that they stay in registers instead of being made again at every use)
+  Constants k;
+  asm volatile("mov.b32 %0, 0x54005400;\n\tmov.b32 %1, 0x64006400;\n\tmov.b32 %2, 0xcc00cc00;\n\tmov.b32 %3, 0xd400d400;" : "=r"(k.e6), "=r"(k.e10), "=r"(k.minus16), "=r"(k.minus64));
+  return k;
+}
+template <uint32_t MASK> __device__ __forceinline__ uint32_t and_or(uint32_t w, uint32_t bits) {   // (one operation; written with & and | it became two)
+  uint32_t r;
+  asm("lop3.b32 %0, %1, %2, %3, 0xea;" : "=r"(r) : "r"(w), "n"(MASK), "r"(bits));
+  return r;
+}
+__device__ __forceinline__ void codes_of(uint32_t w, const Constants& n, uint32_t (&k)[4]) {
   const uint32_t up = w >> 8;
-  k[1] = (w & 0x00f000f0u) | 0x54005400u;
-  k[3] = (up & 0x00f000f0u) | 0x54005400u;
-  k[0] = u32(__hfma2(h2(k[1]), minus16, h2((w & 0x00ff00ffu) | 0x64006400u)));
-  k[2] = u32(__hfma2(h2(k[3]), minus16, h2((up & 0x00ff00ffu) | 0x64006400u)));
+  k[1] = and_or<0x00f000f0u>(w, n.e6);
+  k[3] = and_or<0x00f000f0u>(up, n.e6);
+  k[0] = u32(__hfma2(h2(k[1]), h2(n.minus16), h2(and_or<0x00ff00ffu>(w, n.e10))));
+  k[2] = u32(__hfma2(h2(k[3]), h2(n.minus16), h2(and_or<0x00ff00ffu>(up, n.e10))));
 }
 
 // What a warp keeps of the heads it works for: NT tiles of up to 8 of them.  As an operand a lane has head lane / 4, in results heads 2 c, 2 c + 1.
@@ -148,7 +156,7 @@ __device__ __forceinline__ void load_heads(Heads<D, NT>& h, const CacheAttnArgs&
 
 // One block of 16 tokens at `block`, the first `valid` of which exist.  FINE: what rounding the weights to fp16 has lost is added.
 template <int D, int NT, bool FINE>
-__device__ __forceinline__ void attend_block(Heads<D, NT>& h, const uint8_t* block, int valid) {
+__device__ __forceinline__ void attend_block(Heads<D, NT>& h, const Constants& num, const uint8_t* block, int valid) {
   constexpr int G = D / kGroup;
   const int lane = threadIdx.x & 31, c = lane & 3;
   // ---- scores: S^T of tokens lane / 4 (+ 8) and heads 2 c, 2 c + 1 ----
@@ -183,8 +191,8 @@ __device__ __forceinline__ void attend_block(Heads<D, NT>& h, const uint8_t* blo
 #pragma unroll
   for (int w = 0; w < G; ++w) {
     uint32_t k0[4], k1[4];
-    codes_of(kw[0][w], k0);
-    codes_of(kw[1][w], k1);
+    codes_of(kw[0][w], num, k0);
+    codes_of(kw[1][w], num, k1);
     const float2 f0 = to_float2<__half>(sc[0][w / 2]), f1 = to_float2<__half>(sc[1][w / 2]);
     const float a0 = w & 1 ? f0.y : f0.x, a1 = w & 1 ? f1.y : f1.x;
 #pragma unroll
@@ -235,7 +243,7 @@ __device__ __forceinline__ void attend_block(Heads<D, NT>& h, const uint8_t* blo
   uint32_t p[NT][2], rest[NT][2];                        // P^T as an operand: head lane / 4, tokens 2 c, 2 c + 1 and 8 + 2 c, 9 + 2 c
   auto turn = [](uint32_t v) {
     uint32_t r;
-    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
+    asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
     return r;
   };
 #pragma unroll
@@ -272,7 +280,6 @@ __device__ __forceinline__ void attend_block(Heads<D, NT>& h, const uint8_t* blo
       for (int i = 0; i < 2 * G; ++i) sv[half][i] &= keep;
     }
   }
-  const __half2 minus64 = __half2half2(__ushort_as_half(0xd400));
 #pragma unroll
   for (int i = 0; i < D / 64; ++i) {
     const uint4 v = *reinterpret_cast<const uint4*>(block + Block<D>::kV + i * 512 + lane * 16);
@@ -281,9 +288,9 @@ __device__ __forceinline__ void attend_block(Heads<D, NT>& h, const uint8_t* blo
     for (int j = 0; j < 4; ++j) {
       const int u = 4 * i + j, w = u / 2;
       uint32_t k[4];
-      codes_of(vw[j], k);
+      codes_of(vw[j], num, k);
       auto value = [&](__half2 code, int half) { return u32(__hfma2(code, h2(sv[half][2 * w]), h2(sv[half][2 * w + 1]))); };
-      const uint32_t a0 = value(h2(k[0]), 0), a1 = value(__hadd2(h2(k[1]), minus64), 0), a2 = value(h2(k[2]), 1), a3 = value(__hadd2(h2(k[3]), minus64), 1);
+      const uint32_t a0 = value(h2(k[0]), 0), a1 = value(__hadd2(h2(k[1]), h2(num.minus64)), 0), a2 = value(h2(k[2]), 1), a3 = value(__hadd2(h2(k[3]), h2(num.minus64)), 1);
 #pragma unroll
       for (int t = 0; t < NT; ++t) {
         mma_f16(h.o[t][u], a0, a1, a2, a3, p[t][0], p[t][1]);
@@ -358,15 +365,14 @@ __global__ void __launch_bounds__(32 * kWarps, (ctas_by_registers<D, NT>())) cac
   if (tid == 32 * kWarps - 1) s_starts[a.requests] = run;
   __syncthreads();
   const int segs = a.cache.heads * a.chunks;                             // of a request
-  const long long total = (long long)s_starts[a.requests] * segs, warps = (long long)gridDim.x * kWarps;
-  const int part = (int)max(1ll, (total + warps - 1) / warps);
+  const int total = s_starts[a.requests] * segs, warps = gridDim.x * kWarps, part = max(1, (total + warps - 1) / warps);
   if (blockIdx.x == 0) {
     for (int r = tid; r <= a.requests; r += 32 * kWarps) a.starts[r] = s_starts[r];
     if (tid == 0) a.starts[a.requests + 1] = part;
   }
-  const long long cta_first = (long long)blockIdx.x * kWarps * part, cta_end = min(cta_first + (long long)kWarps * part, total);
-  const long long first = min(cta_first + (long long)warp * part, total), end = min(first + part, total);
-  const int count = (int)(end - first);                                  // units of this warp
+  const int cta_first = (int)min((long long)blockIdx.x * kWarps * part, (long long)total), cta_end = (int)min((long long)cta_first + kWarps * part, (long long)total);
+  const int first = (int)min((long long)cta_first + warp * part, (long long)total), end = min(first + min(part, total - first), total);
+  const int count = end - first;                                  // units of this warp
   const int subs = a.cache.page / kBlockTokens, per_kv = a.q_heads / a.cache.heads;
 
   // A lane knows one block of the next 32 / kUnit units: its segment (of all requests'), how many tokens there are from its unit on, and which block of
@@ -377,12 +383,12 @@ __global__ void __launch_bounds__(32 * kWarps, (ctas_by_registers<D, NT>())) cac
     Known k = {0, 0, -1};
     const int i = unit + lane / U;
     if (i >= count) return k;
-    const long long n = first + i;
+    const int n = first + i;
     int lo = 0, hi = a.requests;                                         // the last request whose units start there or before
-    const int t = (int)(n / segs);
+    const int t = n / segs;
     while (hi - lo > 1) { const int mid = (lo + hi) >> 1; if (s_starts[mid] <= t) lo = mid; else hi = mid; }
     const int units = s_starts[lo + 1] - s_starts[lo];
-    const int rest = (int)(n - (long long)s_starts[lo] * segs);
+    const int rest = n - s_starts[lo] * segs;
     const int seg = rest / units, b = (rest - seg * units) * U + lane % U;
     k.seg = lo * segs + seg;
     k.left = min(a.lengths[lo], a.width * a.cache.page) - (b - lane % U) * kBlockTokens;
@@ -395,15 +401,26 @@ __global__ void __launch_bounds__(32 * kWarps, (ctas_by_registers<D, NT>())) cac
   int asked = 0;                                                         // units whose copies have been asked for
   auto ask = [&](const Known& k, int from) {                              // the next one, known by lanes U from, ...
     const int st = asked % R::kStages;
-    const bool mine = lane / U == from && k.at >= 0;
-    const unsigned all = __ballot_sync(0xffffffffu, mine);
-    if (lane == 0) asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bars + 8 * st), "r"(__popc(all) * Block<D>::kBytes) : "memory");
-    if (mine) bulk_copy(ring + st * R::kUnitBytes + (lane % U) * Block<D>::kBytes, a.cache.pages + (size_t)k.at * Block<D>::kBytes, Block<D>::kBytes, bars + 8 * st);
+    const uint32_t dst = ring + st * R::kUnitBytes, bar = bars + 8 * st;
+    if (subs % U == 0) {                                                 // a unit never leaves its page: one copy
+      const int at = __shfl_sync(0xffffffffu, k.at, U * from), left = __shfl_sync(0xffffffffu, k.left, U * from);
+      if (lane == 0) {
+        const uint32_t bytes = at < 0 ? 0 : (min(left, R::kUnitTokens) + kBlockTokens - 1) / kBlockTokens * Block<D>::kBytes;
+        asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
+        if (bytes) bulk_copy(dst, a.cache.pages + (size_t)at * Block<D>::kBytes, bytes, bar);
+      }
+    } else {
+      const bool mine = lane / U == from && k.at >= 0;
+      const unsigned all = __ballot_sync(0xffffffffu, mine);
+      if (lane == 0) asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(__popc(all) * Block<D>::kBytes) : "memory");
+      if (mine) bulk_copy(dst + (lane % U) * Block<D>::kBytes, a.cache.pages + (size_t)k.at * Block<D>::kBytes, Block<D>::kBytes, bar);
+    }
     ++asked;
   };
   Known now = know(0), next = now;
   while (asked < R::kStages && asked < count) ask(now, asked);
   bool ok = true;
+  const Constants num = constants();
   Heads<D, NT> h;
   int segment = -1, request = 0, seg = 0;                                // segment = request * segs + seg
   // the segment's results, or a piece of them
@@ -457,11 +474,11 @@ __global__ void __launch_bounds__(32 * kWarps, (ctas_by_registers<D, NT>())) cac
     if (!ok) break;
 #pragma unroll 1
     for (int b = 0; b < U; ++b)
-      if ((there >> b) & 1) attend_block<D, NT, FINE>(h, smem + warp * R::kWarpBytes + st * R::kUnitBytes + b * Block<D>::kBytes, left - b * kBlockTokens);
+      if ((there >> b) & 1) attend_block<D, NT, FINE>(h, num, smem + warp * R::kWarpBytes + st * R::kUnitBytes + b * Block<D>::kBytes, left - b * kBlockTokens);
     __syncwarp();
     if (asked < count) { if (at + R::kStages < kBatch) ask(now, at + R::kStages); else ask(next, at + R::kStages - kBatch); }
     if (left <= R::kUnitTokens || n + 1 == count) {                        // the segment's last unit, or the part's
-      const long long units = s_starts[request + 1] - s_starts[request], seg_first = (long long)s_starts[request] * segs + seg * units, seg_end = seg_first + units;
+      const int units = s_starts[request + 1] - s_starts[request], seg_first = s_starts[request] * segs + seg * units, seg_end = seg_first + units;
       if (seg_first >= first && seg_end <= end) flush(nullptr);
       else {
         together = seg_first <= cta_first && seg_end >= cta_end;
@@ -621,7 +638,7 @@ int check(const hyperattn_cache_attention_params* p) {
   if (p->dtype != HYPERATTN_BF16 && p->dtype != HYPERATTN_FP16) return p->dtype == HYPERATTN_FP32 ? HYPERATTN_UNSUPPORTED_SHAPE : HYPERATTN_INVALID_ARGUMENT;
   if (p->out_dtype != p->dtype && p->out_dtype != HYPERATTN_FP32) return HYPERATTN_INVALID_ARGUMENT;
   if (p->q_heads % p->cache.kv_heads || bad_stride(p->q_row_stride) || bad_stride(p->q_head_stride) || p->requests > kMaxRequests) return HYPERATTN_UNSUPPORTED_SHAPE;
-  if ((long long)p->table_width * p->cache.page_tokens > 0x7fffffffLL || (long long)p->requests * p->table_width * (p->cache.page_tokens / kBlockTokens) > 0x7fffffffLL ||
+  if ((long long)p->table_width * p->cache.page_tokens > 0x7fffffffLL || (long long)p->requests * p->q_heads * ((long long)p->table_width * p->cache.page_tokens / 32 + 1) > 0x7fffffffLL ||
       (long long)p->requests * p->q_heads > 0x7fffffffLL || (long long)p->cache.num_pages * (p->cache.page_tokens / kBlockTokens) * p->cache.kv_heads > 0x7fffffffLL)
     return HYPERATTN_UNSUPPORTED_SHAPE;
   return HYPERATTN_OK;
