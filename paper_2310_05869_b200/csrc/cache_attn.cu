@@ -2,17 +2,18 @@
 //
 // A warp takes a block of 16 tokens of one key head and up to 16 query heads that read it, on the warp-level tensor cores
 // (mma.sync m16n8k16, fp16 operands, fp32 sums):
-//   S^T = K Q^T with the codes of K as fp16 numbers (see codes_of), exact sums of a group, s = sum_g scale_g sum(q c) + min_g sum_g(q) in fp32
-//   p = exp2(s c - ref), the reference of a head moves when it is exceeded by more than 2^8
-//   O^T += V^T P^T   V = min + scale * code in fp16 (exact codes, one rounding); its 32-bit words hold four tokens of two coordinates,
-//               so that masking yields operands with pairs of tokens; P^T is turned once (movmatrix).
-// fp16 and not bf16 for the weights and values: a product is then off by 2^-11 and not 2^-8, which is what the output's type can show; V fits by
-// its format, a head's query after a power of two.  For fp16 results, which show 2^-11, the weights' rounding errors go through the products too.
+//   S^T = K Q^T with the codes of K as fp16 numbers (see codes_of), exact sums of a group:  s = sum_g scale_g sum(q c) + min_g sum_g(q)  in fp32
+//   p = exp2(s c - ref), the reference of a head moves when it is exceeded by more than 2^2; P^T is turned once (movmatrix)
+//   O^T += V^T P^T  likewise: V = min + scale * code, so the codes meet the weights times the group's scales, the minima the weights.  V's 32-bit words
+//               hold four tokens of two coordinates, so that masking yields operands with pairs of tokens.
+// fp16 and not bf16 for the weights: they are then off by 2^-11 and not 2^-8, which bf16 results do not show; for fp16 results what the rounding has lost goes
+// through the products too.  What rounding a weight times a scale has lost always does: scale * code and minimum are both larger than the value they add up to.
+// (Weights times scales below 2^-14 lose places: values of a size of 10^-4, whose scales are as coarse.)
 //
-// The blocks of all (request, key head, up to 16 heads) segments are one sequence, cut into equal parts, one for every warp that the
-// GPU holds, whatever the lengths are.  A warp streams its blocks through a ring of its own in shared memory (bulk copies, no other
-// warp to wait for).  A segment that lies in one part is finished there; pieces of others go to the workspace - one piece for a
-// CTA that is inside a segment as a whole - and a second launch puts them together, in order, so that results do not depend on timing.
+// A segment is a request, a key head and up to 8 or 16 of its query heads.  The tokens of all segments are one sequence of units of 5 KB, cut into equal
+// parts, one for every warp that the GPU holds, whatever the lengths are.  A warp streams its units through a ring of its own in shared memory (bulk
+// copies, no other warp to wait for).  A segment that lies in one part is finished there; pieces of others go to the workspace - one piece for
+// a CTA that is inside a segment as a whole - and a second launch puts them together, in order, so that results do not depend on timing.
 #include <cstdio>
 #include <type_traits>
 #include "serving.cuh"
@@ -21,7 +22,7 @@
 namespace hyperattn {
 namespace {
 
-constexpr float kMoveAt = 8.f;          // octaves the scores of a head may exceed its reference before that moves
+constexpr float kMoveAt = 2.f;          // octaves the scores of a head may exceed its reference before that moves: 2^2 times the largest scale is an fp16 number
 
 struct CacheAttnArgs {
   CacheView cache;
@@ -38,7 +39,7 @@ struct CacheAttnArgs {
   int part_heads;                              // heads of a chunk
 };
 
-// c += A B, or d = A B (no registers to be cleared)
+// c += A B, or d = A B (no registers to be cleared), the latter over 8 too
 __device__ __forceinline__ void mma_f16(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
   asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};\n"
       : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
@@ -49,28 +50,23 @@ __device__ __forceinline__ void mma_f16_first(float (&d)[4], uint32_t a0, uint32
       : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
       : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.f));
 }
+__device__ __forceinline__ void mma_f16_first8(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t b0) {
+  asm("mma.sync.aligned.m16n8k8.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5}, {%6}, {%7,%7,%7,%7};\n"
+      : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+      : "r"(a0), "r"(a1), "r"(b0), "f"(0.f));
+}
 __device__ __forceinline__ __half2 h2(uint32_t v) { return *reinterpret_cast<__half2*>(&v); }
 __device__ __forceinline__ uint32_t u32(__half2 v) { return *reinterpret_cast<uint32_t*>(&v); }
-// The codes of a word (8 of them, k at bit 4 k) as fp16 pairs (k, k + 4), k = 0..3: even ones as they are, odd ones 64 too large.  A code with the exponent
-// of 2^6 above its bits 4..7 is 64 + c; both codes of a byte with that of 2^10 are 1024 + low + 16 high, from which 16 (64 + high) is taken.  (Two logical
-// operations and half a shift for two pairs: those run at half the rate of the fused multiply-adds and are what a block has most of.)
-struct Constants { uint32_t e6, e10, minus16, minus64; };       // fp16 pairs: 2^6, 2^10, -16, -64
-__device__ __forceinline__ Constants constants() {                // (opaque, so that they stay in registers instead of being made again at every use)
-  Constants k;
-  asm volatile("mov.b32 %0, 0x54005400;\n\tmov.b32 %1, 0x64006400;\n\tmov.b32 %2, 0xcc00cc00;\n\tmov.b32 %3, 0xd400d400;" : "=r"(k.e6), "=r"(k.e10), "=r"(k.minus16), "=r"(k.minus64));
-  return k;
-}
-template <uint32_t MASK> __device__ __forceinline__ uint32_t and_or(uint32_t w, uint32_t bits) {   // (one operation; written with & and | it became two)
-  uint32_t r;
-  asm("lop3.b32 %0, %1, %2, %3, 0xea;" : "=r"(r) : "r"(w), "n"(MASK), "r"(bits));
-  return r;
-}
-__device__ __forceinline__ void codes_of(uint32_t w, const Constants& n, uint32_t (&k)[4]) {
+// The codes of a word (8 of them, k at bit 4 k) as fp16 pairs (k, k + 4), k = 0..3.  A code in the lowest bits of an fp16 number is that number:
+// c 2^-24 at bits 0..3 and c 2^-20 at bits 4..7, subnormal and exact, and products take them as any others.  So five logical operations are all that
+// eight codes cost; the powers of two are made up for in the queries (even k) and in results.
+constexpr float kTwo20 = 1048576.f, kTwo24 = 16777216.f;
+__device__ __forceinline__ void codes_of(uint32_t w, uint32_t (&k)[4]) {
   const uint32_t up = w >> 8;
-  k[1] = and_or<0x00f000f0u>(w, n.e6);
-  k[3] = and_or<0x00f000f0u>(up, n.e6);
-  k[0] = u32(__hfma2(h2(k[1]), h2(n.minus16), h2(and_or<0x00ff00ffu>(w, n.e10))));
-  k[2] = u32(__hfma2(h2(k[3]), h2(n.minus16), h2(and_or<0x00ff00ffu>(up, n.e10))));
+  k[0] = w & 0x000f000fu;
+  k[1] = w & 0x00f000f0u;
+  k[2] = up & 0x000f000fu;
+  k[3] = up & 0x00f000f0u;
 }
 
 // What a warp keeps of the heads it works for: NT tiles of up to 8 of them.  As an operand a lane has head lane / 4, in results heads 2 c, 2 c + 1.
@@ -78,11 +74,12 @@ constexpr float kNoReference = 3.0e38f;
 template <int D, int NT>
 struct Heads {
   static constexpr int kGroups = D / kGroup;
-  uint32_t q[NT][kGroups][4];           // fp16 pairs: coordinates 32 w + 8 c + 0..7
-  uint32_t fix[NT][2];                  // operands of the product that adds what belongs to minima and to codes that are 64 too large, see load_heads
+  uint32_t q[NT][kGroups][4];           // fp16 pairs: coordinates 32 w + 8 c + 0..7, 0, 1, 4, 5 of them times 16
+  uint32_t sums[NT];                    // operand of the product with the minima, see load_heads
   float scale[NT][2];                   // to the base-2 scores
   float minus[NT][2], sum[NT][2];       // minus the reference (kNoReference: none yet); sum of this lane's tokens
-  float o[NT][D / 16][4];               // O^T: coordinates lane / 4 (+ 8) of every 16
+  float o[NT][D / 16][4];               // O^T without the minima: coordinates lane / 4 (times 2^-24) and lane / 4 + 8 (times 2^-20) of every 16
+  float om[NT][4];                      // sum of weights times minima of group lane / 4
 };
 
 template <int D, int NT, class T>
@@ -109,38 +106,32 @@ __device__ __forceinline__ void load_heads(Heads<D, NT>& h, const CacheAttnArgs&
     int e = (int)(__float_as_uint(top) >> 23) - 127;
     e = top == 0.f || !(top < INFINITY) ? 0 : min(max(e, -126), 126);
     const float down = __uint_as_float((uint32_t)(127 - e) << 23), scale = __uint_as_float((uint32_t)(127 + e) << 23) * a.scale_log2;
-    // Scores want sum_g min_g sum(q) - 64 scale_g sum(q at odd codes).  That is one product more over 16 "coordinates" of a token: the minima of the groups,
-    // again, their scales, again, with the sums (as two fp16 numbers, high and low part) as the query's entries.  A lane has groups 2 (c % 2), + 1 (d = 64:
-    // 0, 1), the high parts for c < 2 (d = 64: c = 0), the low ones otherwise (c = 1; none).
-    float all[G], odd[G];
+    // Scores want sum_g min_g sum(q): one product more, over 8 "coordinates" of a token, the minima of the groups and again, with the sums (as two fp16
+    // numbers, high and low part) as the query's entries.  A lane has groups 2 (c % 2), + 1 (d = 64: 0, 1), the high parts for c < 2 (d = 64: c = 0), the
+    // low ones otherwise (c = 1; none).
+    float all[G];
 #pragma unroll
     for (int w = 0; w < G; ++w) {
       const uint32_t v[4] = {raw[w].x, raw[w].y, raw[w].z, raw[w].w};
-      all[w] = odd[w] = 0.f;
+      all[w] = 0.f;
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const float2 f = to_float2<T>(v[i]);
-        h.q[t][w][i] = from_float2<__half>(f.x * down, f.y * down);
-        const float2 r = to_float2<__half>(h.q[t][w][i]);
+        const uint32_t entry = from_float2<__half>(f.x * down, f.y * down);
+        const float2 r = to_float2<__half>(entry);
         all[w] += r.x + r.y;
-        if (i & 1) odd[w] += r.x + r.y;
+        h.q[t][w][i] = i & 1 ? entry : from_float2<__half>(r.x * 16.f, r.y * 16.f);
       }
 #pragma unroll
-      for (int o = 1; o < 4; o <<= 1) {
-        all[w] += __shfl_xor_sync(0xffffffffu, all[w], o);
-        odd[w] += __shfl_xor_sync(0xffffffffu, odd[w], o);
-      }
-      odd[w] *= -64.f;
+      for (int o = 1; o < 4; o <<= 1) all[w] += __shfl_xor_sync(0xffffffffu, all[w], o);
     }
     const bool second = G == 4 && (c & 1), low = G == 4 ? c >= 2 : c == 1, none = G == 2 && c >= 2;
-    auto operand = [&](const float (&x)[G]) {
-      const float x0 = second ? x[G - 2] : x[0], x1 = second ? x[G - 1] : x[1];
-      const uint32_t high = from_float2<__half>(x0, x1);
-      const float2 f = to_float2<__half>(high);
-      return none ? 0u : low ? from_float2<__half>(x0 - f.x, x1 - f.y) : high;
-    };
-    h.fix[t][0] = operand(all);
-    h.fix[t][1] = operand(odd);
+    const float x0 = second ? all[G - 2] : all[0], x1 = second ? all[G - 1] : all[1];
+    const uint32_t high = from_float2<__half>(x0, x1);
+    const float2 hf = to_float2<__half>(high);
+    h.sums[t] = none ? 0u : low ? from_float2<__half>(x0 - hf.x, x1 - hf.y) : high;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) h.om[t][i] = 0.f;
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
       h.scale[t][i] = __shfl_sync(0xffffffffu, scale, 8 * c + 4 * i);
@@ -154,12 +145,11 @@ __device__ __forceinline__ void load_heads(Heads<D, NT>& h, const CacheAttnArgs&
   }
 }
 
-// One block of 16 tokens at `block`, the first `valid` of which exist.  FINE: what rounding the weights to fp16 has lost is added.
-template <int D, int NT, bool FINE>
-__device__ __forceinline__ void attend_block(Heads<D, NT>& h, const Constants& num, const uint8_t* block, int valid) {
+// Scores of one block of 16 tokens at `block`, the first `valid` of which exist: S^T of tokens lane / 4 (+ 8) and heads 2 c, 2 c + 1.
+template <int D, int NT>
+__device__ __forceinline__ void scores_of(const Heads<D, NT>& h, const uint8_t* block, int valid, float (&s)[NT][4]) {
   constexpr int G = D / kGroup;
   const int lane = threadIdx.x & 31, c = lane & 3;
-  // ---- scores: S^T of tokens lane / 4 (+ 8) and heads 2 c, 2 c + 1 ----
   uint32_t kw[2][G], sc[2][G / 2], mn[2];                // codes, scales of group pairs, minima of the lane's pair (see load_heads)
   if constexpr (D == 128) {
 #pragma unroll
@@ -184,15 +174,11 @@ __device__ __forceinline__ void attend_block(Heads<D, NT>& h, const Constants& n
       mn[half] = __byte_perm(c & 1 ? u.y : v.y, c & 1 ? u.w : v.w, pick);
     }
   }
-  float s[NT][4];
-#pragma unroll
-  for (int t = 0; t < NT; ++t)
-    mma_f16_first(s[t], mn[0], mn[1], G == 4 && (c & 1) ? sc[0][G / 2 - 1] : sc[0][0], G == 4 && (c & 1) ? sc[1][G / 2 - 1] : sc[1][0], h.fix[t][0], h.fix[t][1]);
 #pragma unroll
   for (int w = 0; w < G; ++w) {
     uint32_t k0[4], k1[4];
-    codes_of(kw[0][w], num, k0);
-    codes_of(kw[1][w], num, k1);
+    codes_of(kw[0][w], k0);
+    codes_of(kw[1][w], k1);
     const float2 f0 = to_float2<__half>(sc[0][w / 2]), f1 = to_float2<__half>(sc[1][w / 2]);
     const float a0 = w & 1 ? f0.y : f0.x, a1 = w & 1 ? f1.y : f1.x;
 #pragma unroll
@@ -200,9 +186,16 @@ __device__ __forceinline__ void attend_block(Heads<D, NT>& h, const Constants& n
       float acc[4];
       mma_f16_first(acc, k0[0], k1[0], k0[1], k1[1], h.q[t][w][0], h.q[t][w][1]);
       mma_f16(acc, k0[2], k1[2], k0[3], k1[3], h.q[t][w][2], h.q[t][w][3]);
-      s[t][0] = fmaf(acc[0], a0, s[t][0]); s[t][1] = fmaf(acc[1], a0, s[t][1]);
-      s[t][2] = fmaf(acc[2], a1, s[t][2]); s[t][3] = fmaf(acc[3], a1, s[t][3]);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) s[t][i] = w ? fmaf(acc[i], i < 2 ? a0 : a1, s[t][i]) : acc[i] * (i < 2 ? a0 : a1);
     }
+  }
+#pragma unroll
+  for (int t = 0; t < NT; ++t) {
+    float m[4];
+    mma_f16_first8(m, mn[0], mn[1], h.sums[t]);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) s[t][i] = fmaf(s[t][i], kTwo20, m[i]);
   }
   if (valid < kBlockTokens) {
 #pragma unroll
@@ -211,22 +204,93 @@ __device__ __forceinline__ void attend_block(Heads<D, NT>& h, const Constants& n
       for (int i = 0; i < 4; ++i)
         if (lane / 4 + 8 * (i >> 1) >= valid) s[t][i] = -INFINITY;
   }
-  // ---- weights ----
-  float y[NT][4], most = -INFINITY;
+}
+
+// O^T += V^T P^T of one block, P^T (and what rounding it to fp16 has lost) as operands: the codes with the weights times the scales, the minima with the weights.
+template <int D, int NT, bool FINE>
+__device__ __forceinline__ void add_values(Heads<D, NT>& h, const uint8_t* block, int valid, const uint32_t (&p)[NT][2], const uint32_t (&rest)[NT][2]) {
+  constexpr int G = D / kGroup;
+  const int lane = threadIdx.x & 31, c = lane & 3;
+  uint32_t sv[2][G], mv[2];                              // scales of tokens (2 c, 2 c + 1), (8 + 2 c, 9 + 2 c); minima of those of group lane / 4
 #pragma unroll
-  for (int t = 0; t < NT; ++t)
+  for (int half = 0; half < 2; ++half) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      y[t][i] = fmaf(s[t][i], h.scale[t][i & 1], h.minus[t][i & 1]);
-      most = fmaxf(most, y[t][i]);
+    for (int i = 0; i < G / 2; ++i) {
+      const uint4 v = *reinterpret_cast<const uint4*>(block + Block<D>::kScaleV + (half * 4 + c) * G * 8 + i * 16);
+      sv[half][2 * i] = v.x; sv[half][2 * i + 1] = v.z;
     }
+    mv[half] = *reinterpret_cast<const uint32_t*>(block + Block<D>::kScaleV + ((half * 4 + c) * G + lane / 4 % G) * 8 + 4);
+  }
+  if (valid < kBlockTokens) {                            // whatever the rest of the block holds: zeros
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+      const uint32_t keep = (half * 8 + 2 * c < valid ? 0xffffu : 0u) | (half * 8 + 2 * c + 1 < valid ? 0xffff0000u : 0u);
+#pragma unroll
+      for (int i = 0; i < G; ++i) sv[half][i] &= keep;
+      mv[half] &= keep;
+    }
+  }
+#pragma unroll
+  for (int t = 0; t < NT; ++t) {
+    mma_f16(h.om[t], mv[0], 0u, mv[1], 0u, p[t][0], p[t][1]);
+    if constexpr (FINE) mma_f16(h.om[t], mv[0], 0u, mv[1], 0u, rest[t][0], rest[t][1]);
+  }
+  uint32_t ps[NT][2], pr[NT][2];                         // weights times scales of a group, and what rounding them has lost
+#pragma unroll
+  for (int i = 0; i < D / 64; ++i) {
+    const uint4 v = *reinterpret_cast<const uint4*>(block + Block<D>::kV + i * 512 + lane * 16);
+    const uint32_t vw[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int u = 4 * i + j, w = u / 2;
+      if (j % 2 == 0) {
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+          for (int half = 0; half < 2; ++half) {
+            const __half2 sc = h2(sv[half][w]), prod = __hmul2(h2(p[t][half]), sc);
+            ps[t][half] = u32(prod);
+            const __half2 lost = __hfma2(h2(p[t][half]), sc, __hneg2(prod));
+            pr[t][half] = u32(FINE ? __hfma2(h2(rest[t][half]), sc, lost) : lost);
+          }
+      }
+      uint32_t k[4];
+      codes_of(vw[j], k);
+#pragma unroll
+      for (int t = 0; t < NT; ++t) {
+        mma_f16(h.o[t][u], k[0], k[1], k[2], k[3], ps[t][0], ps[t][1]);
+        mma_f16(h.o[t][u], k[0], k[1], k[2], k[3], pr[t][0], pr[t][1]);
+      }
+    }
+  }
+}
+
+// NB blocks that follow each other, `valid[b]` tokens of each (0: nothing there).  FINE: what rounding the weights to fp16 has lost is added.
+// (Two blocks at a time: one block is a chain of products, exponentials and products again that four warps a scheduler do not hide.)
+template <int D, int NT, int NB, bool FINE>
+__device__ __forceinline__ void attend_blocks(Heads<D, NT>& h, const uint8_t* block, const int (&valid)[NB]) {
+  float s[NB][NT][4], y[NB][NT][4], most = -INFINITY;
+#pragma unroll
+  for (int b = 0; b < NB; ++b) scores_of<D, NT>(h, block + b * Block<D>::kBytes, valid[b], s[b]);
+#pragma unroll
+  for (int b = 0; b < NB; ++b)
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        y[b][t][i] = fmaf(s[b][t][i], h.scale[t][i & 1], h.minus[t][i & 1]);
+        most = fmaxf(most, y[b][t][i]);
+      }
   if (__any_sync(0xffffffffu, most > kMoveAt)) {
     // the references move to the scores' maximum where they are exceeded; sums and outputs follow
 #pragma unroll
     for (int t = 0; t < NT; ++t)
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
-        float m = fmaxf(s[t][i], s[t][i + 2]) * h.scale[t][i];
+        float m = -INFINITY;
+#pragma unroll
+        for (int b = 0; b < NB; ++b) m = fmaxf(m, fmaxf(s[b][t][i], s[b][t][i + 2]));
+        m *= h.scale[t][i];
 #pragma unroll
         for (int o = 4; o < 32; o <<= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
         if (m + h.minus[t][i] > kMoveAt) {
@@ -235,69 +299,42 @@ __device__ __forceinline__ void attend_block(Heads<D, NT>& h, const Constants& n
           h.sum[t][i] *= alpha;
 #pragma unroll
           for (int u = 0; u < D / 16; ++u) { h.o[t][u][i] *= alpha; h.o[t][u][i + 2] *= alpha; }
+          h.om[t][i] *= alpha;
         }
-        y[t][i] = fmaf(s[t][i], h.scale[t][i], h.minus[t][i]);
-        y[t][i + 2] = fmaf(s[t][i + 2], h.scale[t][i], h.minus[t][i]);
+#pragma unroll
+        for (int b = 0; b < NB; ++b) {
+          y[b][t][i] = fmaf(s[b][t][i], h.scale[t][i], h.minus[t][i]);
+          y[b][t][i + 2] = fmaf(s[b][t][i + 2], h.scale[t][i], h.minus[t][i]);
+        }
       }
   }
-  uint32_t p[NT][2], rest[NT][2];                        // P^T as an operand: head lane / 4, tokens 2 c, 2 c + 1 and 8 + 2 c, 9 + 2 c
+  uint32_t p[NB][NT][2], rest[NB][NT][2];                // P^T as an operand: head lane / 4, tokens 2 c, 2 c + 1 and 8 + 2 c, 9 + 2 c
   auto turn = [](uint32_t v) {
     uint32_t r;
     asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
     return r;
   };
 #pragma unroll
-  for (int t = 0; t < NT; ++t) {
-    float e[4];
+  for (int b = 0; b < NB; ++b)
 #pragma unroll
-    for (int i = 0; i < 4; ++i) e[i] = ex2(y[t][i]);
-    h.sum[t][0] += e[0] + e[2];
-    h.sum[t][1] += e[1] + e[3];
+    for (int t = 0; t < NT; ++t) {
+      float e[4];
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const uint32_t both = from_float2<__half>(e[2 * i], e[2 * i + 1]);
-      p[t][i] = turn(both);
-      if constexpr (FINE) {
-        const float2 f = to_float2<__half>(both);
-        rest[t][i] = turn(from_float2<__half>(e[2 * i] - f.x, e[2 * i + 1] - f.y));
+      for (int i = 0; i < 4; ++i) e[i] = ex2(y[b][t][i]);
+      h.sum[t][0] += e[0] + e[2];
+      h.sum[t][1] += e[1] + e[3];
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const uint32_t both = from_float2<__half>(e[2 * i], e[2 * i + 1]);
+        p[b][t][i] = turn(both);
+        if constexpr (FINE) {
+          const float2 f = to_float2<__half>(both);
+          rest[b][t][i] = turn(from_float2<__half>(e[2 * i] - f.x, e[2 * i + 1] - f.y));
+        }
       }
     }
-  }
-  // ---- values ----
-  uint32_t sv[2][2 * G];                                 // (scale pair, minimum pair) of tokens (2 c, 2 c + 1), (8 + 2 c, 9 + 2 c)
 #pragma unroll
-  for (int half = 0; half < 2; ++half)
-#pragma unroll
-    for (int i = 0; i < G / 2; ++i) {
-      const uint4 v = *reinterpret_cast<const uint4*>(block + Block<D>::kScaleV + (half * 4 + c) * G * 8 + i * 16);
-      sv[half][4 * i] = v.x; sv[half][4 * i + 1] = v.y; sv[half][4 * i + 2] = v.z; sv[half][4 * i + 3] = v.w;
-    }
-  if (valid < kBlockTokens) {                            // whatever the rest of the block holds: zeros
-#pragma unroll
-    for (int half = 0; half < 2; ++half) {
-      const uint32_t keep = (half * 8 + 2 * c < valid ? 0xffffu : 0u) | (half * 8 + 2 * c + 1 < valid ? 0xffff0000u : 0u);
-#pragma unroll
-      for (int i = 0; i < 2 * G; ++i) sv[half][i] &= keep;
-    }
-  }
-#pragma unroll
-  for (int i = 0; i < D / 64; ++i) {
-    const uint4 v = *reinterpret_cast<const uint4*>(block + Block<D>::kV + i * 512 + lane * 16);
-    const uint32_t vw[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const int u = 4 * i + j, w = u / 2;
-      uint32_t k[4];
-      codes_of(vw[j], num, k);
-      auto value = [&](__half2 code, int half) { return u32(__hfma2(code, h2(sv[half][2 * w]), h2(sv[half][2 * w + 1]))); };
-      const uint32_t a0 = value(h2(k[0]), 0), a1 = value(__hadd2(h2(k[1]), h2(num.minus64)), 0), a2 = value(h2(k[2]), 1), a3 = value(__hadd2(h2(k[3]), h2(num.minus64)), 1);
-#pragma unroll
-      for (int t = 0; t < NT; ++t) {
-        mma_f16(h.o[t][u], a0, a1, a2, a3, p[t][0], p[t][1]);
-        if constexpr (FINE) mma_f16(h.o[t][u], a0, a1, a2, a3, rest[t][0], rest[t][1]);
-      }
-    }
-  }
+  for (int b = 0; b < NB; ++b) add_values<D, NT, FINE>(h, block + b * Block<D>::kBytes, valid[b], p[b], rest[b]);
 }
 
 __device__ __forceinline__ void put(void* out, int kind, size_t at, float x) {
@@ -306,7 +343,9 @@ __device__ __forceinline__ void put(void* out, int kind, size_t at, float x) {
   else reinterpret_cast<float*>(out)[at] = x;
 }
 
+// warps of a CTA, and CTAs that an SM holds by registers (two tiles of heads need 168 a thread)
 constexpr int kWarps = 4;
+constexpr int ctas_by_registers(int tiles) { return tiles == 1 ? 4 : 3; }
 constexpr int kMaxRequests = 4096;      // running sums in shared memory
 
 // A unit of work and of the ring: 32 (d = 128) or 64 tokens of a segment, 5 KB.
@@ -316,11 +355,8 @@ struct Ring {
   static constexpr int kUnitBytes = kUnit * Block<D>::kBytes, kUnitTokens = kUnit * kBlockTokens;
   static constexpr int kStages = 2;                                      // units on their way, a warp
   static constexpr int kWarpBytes = kStages * kUnitBytes;                // (>= 16 x D floats: a warp's outputs, when the parts are put together)
-  static constexpr int kOffBar = kWarps * kWarpBytes, kOffMisc = kOffBar + kWarps * kStages * 8, kOffStarts = kOffMisc + 768;
-  static constexpr int bytes(int requests) { return kOffStarts + (requests + 1) * 4; }
+  static constexpr int bytes(int requests) { return kWarps * (kWarpBytes + kStages * 8 + 4 + 16 * 12) + 16 + (requests + 1) * 4; }
 };
-// CTAs that an SM holds: by registers (two tiles of heads need 168 a thread), and by shared memory
-template <int D, int NT> constexpr int ctas_by_registers() { return NT == 1 ? 4 : 3; }
 template <int D> int ctas_by_memory(int requests) { return 227 * 1024 / (Ring<D>::bytes(requests) + 1024); }
 
 __device__ __forceinline__ void bulk_copy(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
@@ -333,17 +369,19 @@ template <int D> __device__ __forceinline__ int units_of(const CacheAttnArgs& a,
 __device__ __forceinline__ float* piece_at(const CacheAttnArgs& a, long long slot, int head, int d) { return a.part + (slot * a.part_heads + head) * (d + 2); }
 
 template <int D, int NT, class T>
-__global__ void __launch_bounds__(32 * kWarps, (ctas_by_registers<D, NT>())) cache_attn_kernel(const __grid_constant__ CacheAttnArgs a, int* status) {
+__global__ void __launch_bounds__(32 * kWarps, ctas_by_registers(NT)) cache_attn_kernel(const __grid_constant__ CacheAttnArgs a, int* status) {
   using R = Ring<D>;
   constexpr bool FINE = std::is_same<T, __half>::value;
   extern __shared__ __align__(128) uint8_t smem[];
-  int* s_starts = reinterpret_cast<int*>(smem + R::kOffStarts);          // [requests + 1] units (of one segment each) before a request
-  int* s_sums = reinterpret_cast<int*>(smem + R::kOffMisc);              // [kWarps]
-  volatile int* s_abort = reinterpret_cast<volatile int*>(smem + R::kOffMisc + 64);
-  float* s_stat = reinterpret_cast<float*>(smem + R::kOffMisc + 128);    // [kWarps][16][2] references, sums
+  uint8_t* misc = smem + kWarps * R::kWarpBytes + kWarps * R::kStages * 8;
+  volatile int* s_abort = reinterpret_cast<volatile int*>(misc);
+  int* s_sums = reinterpret_cast<int*>(misc + 16);                       // [kWarps]
+  float* s_stat = reinterpret_cast<float*>(s_sums + kWarps);             // [kWarps][16][2] references, sums
+  float* s_factor = s_stat + kWarps * 32;                                // [kWarps][16]
+  int* s_starts = reinterpret_cast<int*>(s_factor + kWarps * 16);        // [requests + 1] units (of one segment each) before a request
   const int tid = threadIdx.x, lane = tid & 31, c = lane & 3;
   const int warp = __shfl_sync(0xffffffffu, tid >> 5, 0);
-  const uint32_t ring = smem_u32(smem) + warp * R::kWarpBytes, bars = smem_u32(smem) + R::kOffBar + warp * R::kStages * 8;
+  const uint32_t ring = smem_u32(smem) + warp * R::kWarpBytes, bars = smem_u32(smem) + kWarps * R::kWarpBytes + warp * R::kStages * 8;
   if (tid == 0) *s_abort = 0;
   if (lane == 0) {
     for (int st = 0; st < R::kStages; ++st) mbar_init(bars + 8 * st, 1);
@@ -371,8 +409,8 @@ __global__ void __launch_bounds__(32 * kWarps, (ctas_by_registers<D, NT>())) cac
     if (tid == 0) a.starts[a.requests + 1] = part;
   }
   const int cta_first = (int)min((long long)blockIdx.x * kWarps * part, (long long)total), cta_end = (int)min((long long)cta_first + kWarps * part, (long long)total);
-  const int first = (int)min((long long)cta_first + warp * part, (long long)total), end = min(first + min(part, total - first), total);
-  const int count = end - first;                                  // units of this warp
+  const int first = (int)min((long long)cta_first + warp * part, (long long)total), end = (int)min((long long)first + part, (long long)total);
+  const int count = end - first;                                         // units of this warp
   const int subs = a.cache.page / kBlockTokens, per_kv = a.q_heads / a.cache.heads;
 
   // A lane knows one block of the next 32 / kUnit units: its segment (of all requests'), how many tokens there are from its unit on, and which block of
@@ -420,7 +458,6 @@ __global__ void __launch_bounds__(32 * kWarps, (ctas_by_registers<D, NT>())) cac
   Known now = know(0), next = now;
   while (asked < R::kStages && asked < count) ask(now, asked);
   bool ok = true;
-  const Constants num = constants();
   Heads<D, NT> h;
   int segment = -1, request = 0, seg = 0;                                // segment = request * segs + seg
   // the segment's results, or a piece of them
@@ -434,6 +471,9 @@ __global__ void __launch_bounds__(32 * kWarps, (ctas_by_registers<D, NT>())) cac
 #pragma unroll
         for (int o = 4; o < 32; o <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
         const float ref = h.minus[t][i] == kNoReference ? -INFINITY : -h.minus[t][i];
+        float om[D / kGroup];
+#pragma unroll
+        for (int w = 0; w < D / kGroup; ++w) om[w] = __shfl_sync(0xffffffffu, h.om[t][i], 4 * w + c);
         const int head = 8 * t + 2 * c + i;
         if (head < heads) {
           const size_t row = (size_t)request * a.q_heads + first_head + head;
@@ -447,7 +487,7 @@ __global__ void __launch_bounds__(32 * kWarps, (ctas_by_registers<D, NT>())) cac
 #pragma unroll
             for (int up = 0; up < 2; ++up) {
               const int x = 16 * m + lane / 4 + 8 * up;
-              const float v = h.o[t][m][i + 2 * up];
+              const float v = fmaf(h.o[t][m][i + 2 * up], up ? kTwo20 : kTwo24, om[m / 2]);
               if (to) to[head * (D + 2) + x] = v;
               else put(a.out, a.out_kind, row * D + x, v * inv);
             }
@@ -473,8 +513,13 @@ __global__ void __launch_bounds__(32 * kWarps, (ctas_by_registers<D, NT>())) cac
     ok = warp_wait<12>(bars + 8 * st, (uint32_t)(n / R::kStages) & 1, s_abort, status);
     if (!ok) break;
 #pragma unroll 1
-    for (int b = 0; b < U; ++b)
-      if ((there >> b) & 1) attend_block<D, NT, FINE>(h, num, smem + warp * R::kWarpBytes + st * R::kUnitBytes + b * Block<D>::kBytes, left - b * kBlockTokens);
+    for (int b = 0; b < U; b += 2) {
+      // (a block that is not there: whatever its place holds, no token of it)
+      int valid[2];
+#pragma unroll
+      for (int i = 0; i < 2; ++i) valid[i] = (there >> (b + i)) & 1 ? left - (b + i) * kBlockTokens : 0;
+      if (valid[0] | valid[1]) attend_blocks<D, NT, 2, FINE>(h, smem + warp * R::kWarpBytes + st * R::kUnitBytes + b * Block<D>::kBytes, valid);
+    }
     __syncwarp();
     if (asked < count) { if (at + R::kStages < kBatch) ask(now, at + R::kStages); else ask(next, at + R::kStages - kBatch); }
     if (left <= R::kUnitTokens || n + 1 == count) {                        // the segment's last unit, or the part's
@@ -504,28 +549,34 @@ __global__ void __launch_bounds__(32 * kWarps, (ctas_by_registers<D, NT>())) cac
 #pragma unroll
           for (int m = 0; m < D / 16; ++m)
 #pragma unroll
-            for (int up = 0; up < 2; ++up) s_o[head * D + 16 * m + lane / 4 + 8 * up] = h.o[t][m][i + 2 * up];
+            for (int up = 0; up < 2; ++up) s_o[head * D + 16 * m + lane / 4 + 8 * up] = fmaf(h.o[t][m][i + 2 * up], up ? kTwo20 : kTwo24, __shfl_sync(0xffffffffu, h.om[t][i], 4 * (m / 2) + c));
         }
     }
     __syncthreads();
-    const int used = (int)((cta_end - cta_first + part - 1) / part);     // warps that have a part
-    const int heads = min(per_kv - (seg % a.chunks) * 8 * NT, 8 * NT);
-    if (warp < used) {
-      for (int i = warp * 32 + lane; i < heads * D; i += used * 32) {
-        const int head = i / D, x = i - head * D;
-        float ref = -INFINITY;
-        for (int w = 0; w < used; ++w) ref = fmaxf(ref, s_stat[(w * 16 + head) * 2]);
-        float sum = 0.f, o = 0.f;
-        for (int w = 0; w < used; ++w) {
-          const float rw = s_stat[(w * 16 + head) * 2], sw = s_stat[(w * 16 + head) * 2 + 1];
-          const float f = rw == -INFINITY ? (sw == 0.f ? 0.f : 1.f) : ex2(rw - ref);          // (a sum without a reference: NaN)
-          sum += f * sw;
-          o += f * reinterpret_cast<const float*>(smem + w * R::kWarpBytes)[i];
-        }
-        float* to = piece_at(a, 2 * (long long)blockIdx.x * kWarps, head, D);
-        to[x] = o;
-        if (x == 0) { to[D] = ref; to[D + 1] = sum; }
+    const int used = (cta_end - cta_first + part - 1) / part;            // warps that have a part: all of them are together
+    float* piece = piece_at(a, 2ll * blockIdx.x * kWarps, 0, D);
+    if (tid < 8 * NT) {
+      float ref = -INFINITY, sum = 0.f;
+      for (int w = 0; w < used; ++w) ref = fmaxf(ref, s_stat[(w * 16 + tid) * 2]);
+      for (int w = 0; w < used; ++w) {
+        const float rw = s_stat[(w * 16 + tid) * 2], sw = s_stat[(w * 16 + tid) * 2 + 1];
+        const float f = rw == -INFINITY ? (sw == 0.f ? 0.f : 1.f) : ex2(rw - ref);            // (a sum without a reference: NaN)
+        s_factor[w * 16 + tid] = f;
+        sum += f * sw;
       }
+      if (tid < a.part_heads) { piece[tid * (D + 2) + D] = ref; piece[tid * (D + 2) + D + 1] = sum; }
+    }
+    __syncthreads();
+    for (int i = tid; i < a.part_heads * (D / 4); i += 32 * kWarps) {    // (of a chunk with fewer heads the others are not read)
+      const int head = i / (D / 4), x = i - head * (D / 4);
+      float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+      for (int w = 0; w < used; ++w) {
+        const float f = s_factor[w * 16 + head];
+        const float4 v = reinterpret_cast<const float4*>(smem + w * R::kWarpBytes)[i];
+        o = make_float4(o.x + f * v.x, o.y + f * v.y, o.z + f * v.z, o.w + f * v.w);
+      }
+      float2* to = reinterpret_cast<float2*>(piece + head * (D + 2) + 4 * x);
+      to[0] = make_float2(o.x, o.y); to[1] = make_float2(o.z, o.w);
     }
   }
 }
@@ -542,8 +593,8 @@ __global__ void __launch_bounds__(kJoinThreads) join_kernel(const __grid_constan
   const int segs = a.cache.heads * a.chunks, per_kv = a.q_heads / a.cache.heads;
   const int r = blockIdx.x / segs, seg = blockIdx.x - r * segs, kv = seg / a.chunks, chunk = seg - kv * a.chunks;
   const int first_head = kv * per_kv + chunk * a.part_heads, heads = min(per_kv - chunk * a.part_heads, a.part_heads);
-  const long long part = a.starts[a.requests + 1], units = a.starts[r + 1] - a.starts[r];
-  const long long begin = (long long)a.starts[r] * segs + seg * units, end = begin + units, cta_part = part * kWarps, total = (long long)a.starts[a.requests] * segs;
+  const int part = a.starts[a.requests + 1], before = a.starts[r], units = a.starts[r + 1] - before, total = a.starts[a.requests] * segs;
+  const int begin = before * segs + seg * units, end = begin + units;
   const int lane = threadIdx.x % LANES, row = threadIdx.x / LANES;
   const int h0 = blockIdx.y * heads_per_cta, h1 = min(h0 + heads_per_cta, heads);
   if (units == 0) {
@@ -551,20 +602,21 @@ __global__ void __launch_bounds__(kJoinThreads) join_kernel(const __grid_constan
     for (int i = h0 + threadIdx.x; i < h1; i += kJoinThreads) a.lse[(size_t)r * a.q_heads + first_head + i] = -INFINITY;
     return;
   }
-  const long long w0 = begin / part, w1 = (end - 1) / part;               // warps that have a part of it
+  const int w0 = begin / part, w1 = (end - 1) / part;                     // warps that have a part of it
   if (w0 == w1) return;                                                   // finished there
   // Its pieces in order: those of the first CTA's warps (or its one), one of every CTA inside, those of the last CTA's warps (or its one)
-  const long long c0 = w0 / kWarps, c1 = w1 / kWarps;
-  auto whole = [&](long long cta) { return cta * cta_part >= begin && min((cta + 1) * cta_part, total) <= end; };
-  const int n0 = whole(c0) ? 1 : (int)(min(w1, c0 * kWarps + kWarps - 1) - w0 + 1);
-  const int n1 = c1 == c0 ? 0 : whole(c1) ? 1 : (int)(w1 - c1 * kWarps + 1);
-  const int inside = c1 > c0 ? (int)(c1 - c0 - 1) : 0, count = n0 + inside + n1;
+  const int c0 = w0 / kWarps, c1 = w1 / kWarps;
+  auto whole = [&](int cta) { return (long long)cta * kWarps * part >= begin && min((long long)(cta + 1) * kWarps * part, (long long)total) <= end; };
+  const bool whole0 = whole(c0), whole1 = whole(c1);
+  const int n0 = whole0 ? 1 : min(w1, c0 * kWarps + kWarps - 1) - w0 + 1;
+  const int n1 = c1 == c0 ? 0 : whole1 ? 1 : w1 - c1 * kWarps + 1;
+  const int inside = c1 > c0 ? c1 - c0 - 1 : 0, count = n0 + inside + n1;
   auto slot_of = [&](int i) {
-    long long w;
-    if (i < n0) { if (whole(c0)) return 2 * c0 * kWarps; w = w0 + i; }
-    else if (i < n0 + inside) return 2 * (c0 + 1 + i - n0) * kWarps;
-    else { if (whole(c1)) return 2 * c1 * kWarps; w = c1 * kWarps + (i - n0 - inside); }
-    return 2 * w + (begin < w * part ? 0 : 1);
+    int w;
+    if (i < n0) { if (whole0) return 2ll * c0 * kWarps; w = w0 + i; }
+    else if (i < n0 + inside) return 2ll * (c0 + 1 + i - n0) * kWarps;
+    else { if (whole1) return 2ll * c1 * kWarps; w = c1 * kWarps + (i - n0 - inside); }
+    return 2ll * w + (begin < (long long)w * part ? 0 : 1);
   };
   for (int head = h0; head < h1; ++head) {
     float ref = -INFINITY, sum = 0.f;
@@ -609,19 +661,19 @@ __global__ void __launch_bounds__(kJoinThreads) join_kernel(const __grid_constan
 struct Shape { bool two; int chunks, part_heads, ctas; size_t starts, bytes; };
 Shape shape_of(const hyperattn_cache_attention_params& p) {
   Shape s;
-  const int per_kv = p.q_heads / p.cache.kv_heads;
+  const int per_kv = p.q_heads / p.cache.kv_heads, d = p.cache.d;
   s.two = per_kv > 8;
   s.chunks = (per_kv + (s.two ? 15 : 7)) / (s.two ? 16 : 8);
   s.part_heads = s.two ? 16 : 8;
   if (s.part_heads > per_kv) s.part_heads = per_kv;
-  const int unit = p.cache.d == 64 ? Ring<64>::kUnitTokens : Ring<128>::kUnitTokens;
+  const int unit = d == 64 ? Ring<64>::kUnitTokens : Ring<128>::kUnitTokens;
   const long long units = (long long)p.requests * p.cache.kv_heads * s.chunks * (((long long)p.table_width * p.cache.page_tokens + unit - 1) / unit);
   const long long ctas = (units + kWarps - 1) / kWarps;
-  const int memory = p.cache.d == 64 ? ctas_by_memory<64>(p.requests) : ctas_by_memory<128>(p.requests), registers = s.two ? ctas_by_registers<128, 2>() : ctas_by_registers<128, 1>();
+  const int memory = d == 64 ? ctas_by_memory<64>(p.requests) : ctas_by_memory<128>(p.requests), registers = ctas_by_registers(s.two ? 2 : 1);
   const int most = kSms * (memory < registers ? memory : registers);
   s.ctas = (int)(ctas < most ? ctas : most);
   s.starts = ((size_t)(p.requests + 2) * 4 + 255) / 256 * 256;
-  s.bytes = s.starts + (size_t)s.ctas * kWarps * 2 * s.part_heads * (p.cache.d + 2) * 4;
+  s.bytes = s.starts + (size_t)s.ctas * kWarps * 2 * s.part_heads * (d + 2) * 4;
   return s;
 }
 
