@@ -355,7 +355,7 @@ struct Ring {
   static constexpr int kUnitBytes = kUnit * Block<D>::kBytes, kUnitTokens = kUnit * kBlockTokens;
   static constexpr int kStages = 2;                                      // units on their way, a warp
   static constexpr int kWarpBytes = kStages * kUnitBytes;                // (>= 16 x D floats: a warp's outputs, when the parts are put together)
-  static constexpr int bytes(int requests) { return kWarps * (kWarpBytes + kStages * 8 + 4 + 16 * 12) + 16 + (requests + 1) * 4; }
+  static constexpr int bytes(int requests) { return kWarps * (kWarpBytes + 1280 + kStages * 8 + 4 + 16 * 12) + 16 + (requests + 1) * 4; }
 };
 template <int D> int ctas_by_memory(int requests) { return 227 * 1024 / (Ring<D>::bytes(requests) + 1024); }
 
@@ -373,7 +373,7 @@ __global__ void __launch_bounds__(32 * kWarps, ctas_by_registers(NT)) cache_attn
   using R = Ring<D>;
   constexpr bool FINE = std::is_same<T, __half>::value;
   extern __shared__ __align__(128) uint8_t smem[];
-  uint8_t* misc = smem + kWarps * R::kWarpBytes + kWarps * R::kStages * 8;
+  uint8_t* misc = smem + kWarps * (R::kWarpBytes + 1280 + R::kStages * 8);
   volatile int* s_abort = reinterpret_cast<volatile int*>(misc);
   int* s_sums = reinterpret_cast<int*>(misc + 16);                       // [kWarps]
   float* s_stat = reinterpret_cast<float*>(s_sums + kWarps);             // [kWarps][16][2] references, sums
@@ -381,7 +381,7 @@ __global__ void __launch_bounds__(32 * kWarps, ctas_by_registers(NT)) cache_attn
   int* s_starts = reinterpret_cast<int*>(s_factor + kWarps * 16);        // [requests + 1] units (of one segment each) before a request
   const int tid = threadIdx.x, lane = tid & 31, c = lane & 3;
   const int warp = __shfl_sync(0xffffffffu, tid >> 5, 0);
-  const uint32_t ring = smem_u32(smem) + warp * R::kWarpBytes, bars = smem_u32(smem) + kWarps * R::kWarpBytes + warp * R::kStages * 8;
+  const uint32_t ring = smem_u32(smem) + warp * R::kWarpBytes, bars = smem_u32(smem) + kWarps * (R::kWarpBytes + 1280) + warp * R::kStages * 8;
   if (tid == 0) *s_abort = 0;
   if (lane == 0) {
     for (int st = 0; st < R::kStages; ++st) mbar_init(bars + 8 * st, 1);
@@ -413,50 +413,55 @@ __global__ void __launch_bounds__(32 * kWarps, ctas_by_registers(NT)) cache_attn
   const int count = end - first;                                         // units of this warp
   const int subs = a.cache.page / kBlockTokens, per_kv = a.q_heads / a.cache.heads;
 
-  // A lane knows one block of the next 32 / kUnit units: its segment (of all requests'), how many tokens there are from its unit on, and which block of
-  // the cache it is (-1: none).
+  // What is known of the blocks of the next 32 / kUnit units, a lane a block, in shared memory (a batch while another is used): first, by look(), where to
+  // look - {segment of all requests', block in it, page, length} and the block's place in its page, page and length on their way - and then, by know(),
+  // what is there: {segment, tokens from the unit on, block of the cache, bytes of the copy to ask for | blocks of the unit that exist << 16}.  A unit that
+  // cannot leave its page is one copy, its first block's.
   constexpr int U = R::kUnit, kBatch = 32 / U;
-  struct Known { int seg, left, at; };
-  auto know = [&](int unit) {                                            // units unit .. unit + kBatch - 1
-    Known k = {0, 0, -1};
-    const int i = unit + lane / U;
-    if (i >= count) return k;
+  const bool whole = subs % U == 0;
+  const int shift = subs & (subs - 1) ? -1 : 31 - __clz(subs);           // blocks of a page: a power of two?
+  int4* s_known = reinterpret_cast<int4*>(smem + kWarps * R::kWarpBytes) + warp * 64;                       // [2][32]
+  int* s_place = reinterpret_cast<int*>(smem + kWarps * (R::kWarpBytes + 1024)) + warp * 64;                // [2][32]
+  auto look = [&](int unit) {                                            // units unit .. unit + kBatch - 1
+    const int slot = (unit / kBatch & 1) * 32 + lane, i = min(unit + lane / U, count - 1);
     const int n = first + i;
     int lo = 0, hi = a.requests;                                         // the last request whose units start there or before
     const int t = n / segs;
     while (hi - lo > 1) { const int mid = (lo + hi) >> 1; if (s_starts[mid] <= t) lo = mid; else hi = mid; }
     const int units = s_starts[lo + 1] - s_starts[lo];
-    const int rest = n - s_starts[lo] * segs;
-    const int seg = rest / units, b = (rest - seg * units) * U + lane % U;
-    k.seg = lo * segs + seg;
-    k.left = min(a.lengths[lo], a.width * a.cache.page) - (b - lane % U) * kBlockTokens;
-    if ((lane % U) * kBlockTokens < k.left) {
-      const int page = a.table[(size_t)lo * a.width + b / subs];
-      if (page >= 0 && page < a.cache.num_pages) k.at = (page * a.cache.heads + seg / a.chunks) * subs + b % subs;
-    }
-    return k;
+    const int rest = n - s_starts[lo] * segs, seg = rest / units, b = (rest - seg * units) * U + lane % U;
+    const int column = shift >= 0 ? b >> shift : b / subs;
+    *reinterpret_cast<int2*>(&s_known[slot]) = make_int2(lo * segs + seg, b);
+    s_place[slot] = (a.chunks == 1 ? seg : seg / a.chunks) * subs + b - column * subs;
+    const uint32_t to = smem_u32(&s_known[slot]);
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 4;\n\tcp.async.ca.shared.global [%2], [%3], 4;" ::"r"(to + 8), "l"(a.table + (size_t)lo * a.width + min(column, a.width - 1)), "r"(to + 12),
+                 "l"(a.lengths + lo) : "memory");
+  };
+  auto know = [&](int unit) {
+    asm volatile("cp.async.wait_all;" ::: "memory");
+    __syncwarp();
+    const int slot = (unit / kBatch & 1) * 32 + lane, in_unit = lane % U;
+    const int4 k = s_known[slot];
+    const int left = min(k.w, a.width * a.cache.page) - (k.y - in_unit) * kBlockTokens;
+    const bool there = in_unit * kBlockTokens < left && k.z >= 0 && k.z < a.cache.num_pages;
+    const unsigned all = __ballot_sync(0xffffffffu, there) >> (lane - in_unit) & ((1u << U) - 1);
+    const int bytes = whole ? (in_unit == 0 ? __popc(all) : 0) : there;
+    s_known[slot] = make_int4(k.x, left, k.z * a.cache.heads * subs + s_place[slot], bytes * Block<D>::kBytes | all << 16);
+    __syncwarp();
   };
   int asked = 0;                                                         // units whose copies have been asked for
-  auto ask = [&](const Known& k, int from) {                              // the next one, known by lanes U from, ...
-    const int st = asked % R::kStages;
-    const uint32_t dst = ring + st * R::kUnitBytes, bar = bars + 8 * st;
-    if (subs % U == 0) {                                                 // a unit never leaves its page: one copy
-      const int at = __shfl_sync(0xffffffffu, k.at, U * from), left = __shfl_sync(0xffffffffu, k.left, U * from);
-      if (lane == 0) {
-        const uint32_t bytes = at < 0 ? 0 : (min(left, R::kUnitTokens) + kBlockTokens - 1) / kBlockTokens * Block<D>::kBytes;
-        asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
-        if (bytes) bulk_copy(dst, a.cache.pages + (size_t)at * Block<D>::kBytes, bytes, bar);
-      }
-    } else {
-      const bool mine = lane / U == from && k.at >= 0;
-      const unsigned all = __ballot_sync(0xffffffffu, mine);
-      if (lane == 0) asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(__popc(all) * Block<D>::kBytes) : "memory");
-      if (mine) bulk_copy(dst + (lane % U) * Block<D>::kBytes, a.cache.pages + (size_t)k.at * Block<D>::kBytes, Block<D>::kBytes, bar);
+  auto ask = [&] {
+    if (lane < U) {
+      const int st = asked % R::kStages;
+      const uint32_t bar = bars + 8 * st;
+      const int4 k = s_known[asked % (2 * kBatch) * U + lane];
+      if (lane == 0) asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(__popc(k.w >> 16) * Block<D>::kBytes) : "memory");
+      if (k.w & 0xffff) bulk_copy(ring + st * R::kUnitBytes + lane * Block<D>::kBytes, a.cache.pages + (size_t)k.z * Block<D>::kBytes, k.w & 0xffff, bar);
     }
     ++asked;
   };
-  Known now = know(0), next = now;
-  while (asked < R::kStages && asked < count) ask(now, asked);
+  if (count > 0) { look(0); know(0); }
+  while (asked < R::kStages && asked < count) ask();
   bool ok = true;
   Heads<D, NT> h;
   int segment = -1, request = 0, seg = 0;                                // segment = request * segs + seg
@@ -496,13 +501,10 @@ __global__ void __launch_bounds__(32 * kWarps, ctas_by_registers(NT)) cache_attn
   };
   bool together = false;                                                 // the whole CTA works for one segment
   for (int n = 0; n < count; ++n) {
-    const int at = n % kBatch;
-    if (at == 0) {
-      if (n > 0) now = next;
-      next = know(n + kBatch);
-    }
-    const int sg = __shfl_sync(0xffffffffu, now.seg, at * U), left = __shfl_sync(0xffffffffu, now.left, at * U);
-    const unsigned there = __ballot_sync(0xffffffffu, now.at >= 0) >> (at * U);
+    if (n % kBatch == 0 && n + kBatch < count) look(n + kBatch);
+    if (n % kBatch == kBatch / 2 && n + kBatch / 2 < count) know(n + kBatch / 2);
+    const int4 unit = s_known[n % (2 * kBatch) * U];
+    const int sg = unit.x, left = unit.y, there = unit.w >> 16;
     if (sg != segment) {
       segment = sg;
       request = segment / segs; seg = segment - request * segs;
@@ -521,7 +523,7 @@ __global__ void __launch_bounds__(32 * kWarps, ctas_by_registers(NT)) cache_attn
       if (valid[0] | valid[1]) attend_blocks<D, NT, 2, FINE>(h, smem + warp * R::kWarpBytes + st * R::kUnitBytes + b * Block<D>::kBytes, valid);
     }
     __syncwarp();
-    if (asked < count) { if (at + R::kStages < kBatch) ask(now, at + R::kStages); else ask(next, at + R::kStages - kBatch); }
+    if (asked < count) ask();
     if (left <= R::kUnitTokens || n + 1 == count) {                        // the segment's last unit, or the part's
       const int units = s_starts[request + 1] - s_starts[request], seg_first = s_starts[request] * segs + seg * units, seg_end = seg_first + units;
       if (seg_first >= first && seg_end <= end) flush(nullptr);
