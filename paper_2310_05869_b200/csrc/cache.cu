@@ -1,6 +1,7 @@
 // The paged 4-bit cache: pages (plan), storing, reading.
 #include <cstdio>
 #include "serving.cuh"
+#include "tc_util.cuh"
 
 namespace hyperattn {
 namespace {
@@ -136,52 +137,11 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(hyperattn_plan p) {
 }
 
 // ---- store -----------------------------------------------------------------------------------------------------------------
-// A row of d numbers is d / 8 lanes with 8 numbers each, a group of 32 the numbers of four neighbouring lanes.
-template <class T>
-struct Packed8 {                        // 8 numbers as loaded
-  uint4 v;
-  __device__ __forceinline__ void floats(float (&x)[8]) const {
-    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) { const float2 f = to_float2<T>(w[i]); x[2 * i] = f.x; x[2 * i + 1] = f.y; }
-  }
-};
-
-// codes of the lane's 8 numbers, 4 bits each from bit 0 on; scale and minimum (fp16) of its group
-template <class T>
-__device__ __forceinline__ uint32_t quantise8(const Packed8<T>& in, __half& s, __half& m) {
-  float x[8];
-  in.floats(x);
-  float lo = x[0], hi = x[0];
-  bool finite = true;
-#pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    lo = fminf(lo, x[i]); hi = fmaxf(hi, x[i]);
-    finite = finite && fabsf(x[i]) < INFINITY;          // (false for NaN)
-  }
-#pragma unroll
-  for (int o = 1; o < 4; o <<= 1) {
-    lo = fminf(lo, __shfl_xor_sync(0xffffffffu, lo, o));
-    hi = fmaxf(hi, __shfl_xor_sync(0xffffffffu, hi, o));
-  }
-  const unsigned all = __ballot_sync(0xffffffffu, finite);
-  const unsigned mine = 0xfu << (threadIdx.x & 28);
-  s = __float2half_rn((hi - lo) / 15.f);
-  m = __float2half_rn(lo);
-  if ((all & mine) != mine || __hisinf(s) || __hisinf(m)) {
-    s = m = __ushort_as_half(0x7fff);
-    return 0;
-  }
-  const float fs = __half2float(s), fm = __half2float(m);
-  const float r = fs == 0.f ? 0.f : 1.f / fs;
-  uint32_t codes = 0;
-#pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const float c = fminf(fmaxf(rintf((x[i] - fm) * r), 0.f), 15.f);
-    codes |= (uint32_t)c << (4 * i);
-  }
-  return codes;
-}
+// A CTA takes the runs that begin among its rows: rows that follow each other into consecutive slots of one block (so a run is at most a block, and
+// for prompts nearly always is one).  A warp makes a run's part of a block in shared memory, first K, then V - a row of d numbers is d / 8 lanes with 8
+// numbers each, a group of 32 the numbers of four neighbouring lanes - and writes a whole block with 16-byte stores, a part of one by the pieces that its
+// tokens own.
+constexpr int kStoreRows = 64, kStoreWarps = 8;
 
 struct StoreArgs {
   CacheView cache;
@@ -191,110 +151,291 @@ struct StoreArgs {
   const int32_t* slots;
 };
 
-// A warp takes K and V of one (row, head) at d = 128, of two at d = 64.
+template <class T> struct Pair;          // two numbers of a 16-bit type
+template <> struct Pair<__half> { using type = __half2; };
+template <> struct Pair<__nv_bfloat16> { using type = __nv_bfloat162; };
+template <class T> __device__ __forceinline__ uint32_t min2(uint32_t a, uint32_t b) {      // (NaN if one of two is)
+  using P = typename Pair<T>::type;
+  P r = __hmin2_nan(*reinterpret_cast<P*>(&a), *reinterpret_cast<P*>(&b));
+  return *reinterpret_cast<uint32_t*>(&r);
+}
+template <class T> __device__ __forceinline__ uint32_t max2(uint32_t a, uint32_t b) {
+  using P = typename Pair<T>::type;
+  P r = __hmax2_nan(*reinterpret_cast<P*>(&a), *reinterpret_cast<P*>(&b));
+  return *reinterpret_cast<uint32_t*>(&r);
+}
+
+// The codes of the lane's 8 numbers, in the lowest bytes of c; scale and minimum (fp16) of its group.
+template <class T>
+__device__ __forceinline__ void quantise8(const uint4& in, uint32_t (&c)[8], __half& s, __half& m) {
+  // smallest and minus largest number as a pair
+  const uint32_t low = min2<T>(min2<T>(in.x, in.y), min2<T>(in.z, in.w)), high = max2<T>(max2<T>(in.x, in.y), max2<T>(in.z, in.w)) ^ 0x80008000u;
+  uint32_t both = min2<T>(__byte_perm(low, high, 0x5410), __byte_perm(low, high, 0x7632));
+  both = min2<T>(both, __shfl_xor_sync(0xffffffffu, both, 1));
+  both = min2<T>(both, __shfl_xor_sync(0xffffffffu, both, 2));
+  const float2 f = to_float2<T>(both);
+  s = __float2half_rn((-f.y - f.x) / 15.f);
+  m = __float2half_rn(f.x);
+  float fs = __half2float(s), fm = __half2float(m);
+  if (!(fabsf(fs) < INFINITY) || !(fabsf(fm) < INFINITY)) {            // (a number that is not finite shows in one of the two)
+    s = m = __ushort_as_half(0x7fff);
+    fs = fm = 0.f;
+  }
+  const float r = fs == 0.f ? 0.f : 1.f / fs;
+  const uint64_t minus = pack_f2(-fm, -fm), times = pack_f2(r, r);
+  const uint32_t w[4] = {in.x, in.y, in.z, in.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const float2 x = to_float2<T>(w[i]);
+    float t0, t1;
+    unpack_f2(fmul2(fadd2(pack_f2(x.x, x.y), minus), times), t0, t1);
+    // 1.5 * 2^23 + t is rounded to the nearest integer, ties to even, and has it in its lowest bits
+    c[2 * i] = __float_as_uint(fminf(fmaxf(t0, 0.f), 15.f) + 12582912.f);
+    c[2 * i + 1] = __float_as_uint(fminf(fmaxf(t1, 0.f), 15.f) + 12582912.f);
+  }
+}
+__device__ __forceinline__ uint32_t low_bytes(uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+  return __byte_perm(__byte_perm(a, b, 0x0040), __byte_perm(c, d, 0x0040), 0x5410);
+}
+
 template <int D, class T>
-__global__ void __launch_bounds__(256) store_kernel(StoreArgs a) {
+__global__ void __launch_bounds__(32 * kStoreWarps) store_kernel(const __grid_constant__ StoreArgs a) {
+  using B = Block<D>;
+  constexpr int LANES = D / 8, PER = 32 / LANES, STEPS = kBlockTokens / PER, kWindow = kStoreRows + kBlockTokens;     // PER: rows at a time
+  __shared__ int s_slot[kWindow + 1], s_run[kStoreRows];
+  __shared__ unsigned s_begin[kStoreRows / 32];
+  __shared__ __align__(16) uint8_t s_block[kStoreWarps][B::kBytes];
   wait_for_stream();
-  constexpr int LANES = D / 8;                          // lanes of a row
-  const int lane = threadIdx.x & 31;
-  const long long item = (long long)blockIdx.x * (256 / (2 * LANES)) + threadIdx.x / (2 * LANES);
-  const bool is_v = (lane / LANES) & 1;
-  const int o = lane % LANES;                           // octet of the row
-  const long long row = item / a.cache.heads;
-  const int head = (int)(item - row * a.cache.heads);
-  const int slot = row < a.rows ? a.slots[row] : -1;
-  const int page = slot < 0 ? -1 : slot / a.cache.page;
-  const bool there = page >= 0 && page < a.cache.num_pages;
-  Packed8<T> in = {make_uint4(0, 0, 0, 0)};
-  if (there) {
-    const T* src = is_v ? reinterpret_cast<const T*>(a.v) + row * a.v_row + head * a.v_head : reinterpret_cast<const T*>(a.k) + row * a.k_row + head * a.k_head;
-    in.v = *reinterpret_cast<const uint4*>(src + o * 8);
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const long long w0 = (long long)blockIdx.x * kStoreRows;
+  // slots of the row before, of the CTA's rows, and of those that a run may reach into
+  for (int i = tid; i <= kWindow; i += 32 * kStoreWarps) {
+    const long long row = w0 + i - 1;
+    const int slot = row >= 0 && row < a.rows ? a.slots[row] : -1;
+    s_slot[i] = slot >= 0 && slot / a.cache.page < a.cache.num_pages ? slot : -1;
   }
-  __half s, m;
-  const uint32_t codes = quantise8(in, s, m);
-  const uint32_t other = __shfl_xor_sync(0xffffffffu, codes, 1);
-  if (!there) return;
-  const int in_page = slot - page * a.cache.page, t = in_page % kBlockTokens;
-  uint8_t* block = block_at<D>(a.cache, page, head, in_page / kBlockTokens);
-  if (!is_v) {
-    uint32_t word = 0;
+  __syncthreads();
+  auto follows = [&](int i) { return s_slot[i] >= 0 && s_slot[i - 1] >= 0 && s_slot[i] == s_slot[i - 1] + 1 && s_slot[i] % kBlockTokens != 0; };
+  // the runs in order (all CTAs of a window have to number them alike)
+  static_assert(kStoreRows == 64, "two warps look");
+  const bool begins = tid < kStoreRows && s_slot[tid + 1] >= 0 && !follows(tid + 1);
+  const unsigned flags = __ballot_sync(0xffffffffu, begins);
+  if (tid < kStoreRows && lane == 0) s_begin[warp] = flags;
+  __syncthreads();
+  if (begins) s_run[__popc(flags & ((1u << lane) - 1u)) + (warp ? __popc(s_begin[0]) : 0)] = tid + 1;
+  __syncthreads();
+  const int items = (__popc(s_begin[0]) + __popc(s_begin[1])) * a.cache.heads;
+  uint8_t* block = s_block[warp];
+  const int o = lane % LANES, sub = lane / LANES;
+  for (int item = blockIdx.y * kStoreWarps + warp; item < items; item += kStoreWarps * gridDim.y) {
+    const int run = item / a.cache.heads, head = item - run * a.cache.heads, at = s_run[run];
+    int n = 1;
+    while (n < kBlockTokens && at + n <= kWindow && follows(at + n)) ++n;
+    const int slot = s_slot[at], page = slot / a.cache.page, in_page = slot - page * a.cache.page, t0 = in_page % kBlockTokens;
+    const long long row0 = w0 + at - 1 - t0;                               // (the row of the block's token 0)
+    const T *ks = reinterpret_cast<const T*>(a.k) + head * a.k_head + o * 8, *vs = reinterpret_cast<const T*>(a.v) + head * a.v_head + o * 8;
+    auto mine = [&](int t) { return t >= t0 && t < t0 + n; };
+    // K: tokens sub, sub + PER, ...; V: a lane takes the four tokens of a word one after the other
+    auto k_token = [&](int i) { return i * PER + sub; };
+    auto v_token = [&](int i) { return 2 * (sub * (STEPS / 4) + i / 4) + i % 4 / 2 + (i & 1) * 8; };
+    uint4 in[STEPS];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) word |= ((codes >> (4 * e)) & 15u) << (4 * ((e % 2) * 4 + e / 2));
-    const int ln = (t % 8) * 4 + o % 4;
-    const int at = (D == 128 ? (t / 8) * 512 + ln * 16 : ln * 16 + (t / 8) * 8) + (o / 4) * 4;
-    *reinterpret_cast<uint32_t*>(block + at) = word;
-  } else {
-    // the octets of a byte are neighbours: the even lane writes coordinates 0..3 of both, the odd one 4..7
-    const uint32_t low = (o & 1) ? other : codes, high = (o & 1) ? codes : other;
-    const int u = o / 2;
-    uint8_t* at = block + Block<D>::kV + (u / 4) * 512 + (t % 8 / 2) * 16 + (u % 4) * 4 + (t % 2) * 2 + t / 8;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int r = (o & 1) * 4 + i;
-      at[r * 64] = (uint8_t)(((low >> (4 * r)) & 15u) | (((high >> (4 * r)) & 15u) << 4));
+    for (int i = 0; i < STEPS; ++i) {
+      const int t = k_token(i);
+      in[i] = mine(t) ? *reinterpret_cast<const uint4*>(ks + (row0 + t) * a.k_row) : make_uint4(0, 0, 0, 0);
     }
-  }
-  if (o % 4 == 0) {
-    __half* at = reinterpret_cast<__half*>(block + (is_v ? Block<D>::kScaleV : Block<D>::kScaleK) + ((t / 2) * Block<D>::kGroups + o / 4) * 8 + (t % 2) * 2);
-    at[0] = s;
-    at[2] = m;
+    auto scales = [&](int at0, int t, __half s, __half m) {
+      if (o % 4 == 0) {
+        __half* to = reinterpret_cast<__half*>(block + at0 + ((t / 2) * B::kGroups + o / 4) * 8 + (t % 2) * 2);
+        to[0] = s;
+        to[2] = m;
+      }
+    };
+#pragma unroll
+    for (int i = 0; i < STEPS; ++i) {
+      const int t = k_token(i);
+      uint32_t c[8];
+      __half s, m;
+      if (__any_sync(0xffffffffu, mine(t))) {
+        quantise8<T>(in[i], c, s, m);
+        // nibble e of the codes is (e % 2) * 4 + e / 2 of the word
+        const uint32_t word = low_bytes(c[0], c[4], c[1], c[5]) + 16 * low_bytes(c[2], c[6], c[3], c[7]);
+        const int ln = (t % 8) * 4 + o % 4;
+        *reinterpret_cast<uint32_t*>(block + (D == 128 ? (t / 8) * 512 + ln * 16 : ln * 16 + (t / 8) * 8) + (o / 4) * 4) = word;
+        scales(B::kScaleK, t, s, m);
+      }
+      const int tv = v_token(i);
+      in[i] = mine(tv) ? *reinterpret_cast<const uint4*>(vs + (row0 + tv) * a.v_row) : make_uint4(0, 0, 0, 0);
+    }
+#pragma unroll
+    for (int i4 = 0; i4 < STEPS; i4 += 4) {
+      uint32_t w[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int t = v_token(i4 + i);
+        w[i] = 0;
+        if (__any_sync(0xffffffffu, mine(t))) {
+          uint32_t c[8];
+          __half s, m;
+          quantise8<T>(in[i4 + i], c, s, m);
+          // the octets of a byte are neighbours: the even lane makes coordinates 0..3 of both, the odd one 4..7
+          const uint32_t first = low_bytes(c[0], c[1], c[2], c[3]), second = low_bytes(c[4], c[5], c[6], c[7]);
+          const uint32_t other = __shfl_xor_sync(0xffffffffu, o & 1 ? first : second, 1);
+          w[i] = o & 1 ? other + 16 * second : first + 16 * other;
+          scales(B::kScaleV, t, s, m);
+        }
+      }
+      // four tokens of four coordinates, the other way round
+      const uint32_t x0 = __byte_perm(w[0], w[1], 0x5140), x1 = __byte_perm(w[2], w[3], 0x5140), x2 = __byte_perm(w[0], w[1], 0x7362), x3 = __byte_perm(w[2], w[3], 0x7362);
+      const int u = o / 2, quad = sub * (STEPS / 4) + i4 / 4;
+      uint32_t* to = reinterpret_cast<uint32_t*>(block + B::kV + (u / 4) * 512 + ((o & 1) * 16 + quad) * 16 + (u % 4) * 4);
+      to[0] = __byte_perm(x0, x1, 0x5410); to[16] = __byte_perm(x0, x1, 0x7632); to[32] = __byte_perm(x2, x3, 0x5410); to[48] = __byte_perm(x2, x3, 0x7632);
+    }
+    __syncwarp();
+    uint8_t* out = block_at<D>(a.cache, page, head, in_page / kBlockTokens);
+    if (n == kBlockTokens) {
+#pragma unroll
+      for (int i = 0; i < B::kBytes; i += 512) {
+        const int x = i + lane * 16;
+        if (x < B::kBytes) *reinterpret_cast<uint4*>(out + x) = *reinterpret_cast<const uint4*>(block + x);
+      }
+    } else {
+      // K: D / 2 bytes a token, in pieces of 8 bytes
+      for (int i = lane; i < D; i += 32) {
+        const int t = D == 128 ? i / 64 * 8 + i % 64 / 8 : i / 8 + (i & 1) * 8;
+        if (mine(t)) *reinterpret_cast<uint2*>(out + i * 8) = *reinterpret_cast<const uint2*>(block + i * 8);
+      }
+      // V: a word has tokens 2 c, 8 + 2 c, 2 c + 1, 9 + 2 c in its bytes
+      for (int i = lane; i < 2 * D; i += 32) {
+        const int c = i / 4 % 4;
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+          if (mine(2 * c + k / 2 + (k & 1) * 8)) out[B::kV + i * 4 + k] = block[B::kV + i * 4 + k];
+      }
+      // scales and minima: (2 i, 2 i + 1) of a group, twice
+      for (int i = lane; i < 2 * D; i += 32) {
+        const int t = i / 4 / B::kGroups % 8 * 2 + (i & 1);
+        if (mine(t)) reinterpret_cast<__half*>(out + B::kScaleK)[i] = reinterpret_cast<const __half*>(block + B::kScaleK)[i];
+      }
+    }
+    __syncwarp();
   }
 }
 
 // ---- read ------------------------------------------------------------------------------------------------------------------
+// A CTA takes some rows of the result, a warp a block of 16 tokens of one head at a time: 16-byte loads of codes and scales; V's words, which hold four
+// tokens of two coordinates, are turned by movmatrix so that a lane has neighbouring coordinates of a token, as it has for K.  Rows leave through shared memory.
 struct ReadArgs {
   CacheView cache;
   const int32_t *table, *cu, *first;
   int requests, width, rows;
   void *k, *v;
 };
-
-template <class T> __device__ __forceinline__ void put8(T* to, const float (&x)[8]) {
-  *reinterpret_cast<uint4*>(to) = make_uint4(from_float2<T>(x[0], x[1]), from_float2<T>(x[2], x[3]), from_float2<T>(x[4], x[5]), from_float2<T>(x[6], x[7]));
-}
-template <> __device__ __forceinline__ void put8<float>(float* to, const float (&x)[8]) {
-  reinterpret_cast<float4*>(to)[0] = make_float4(x[0], x[1], x[2], x[3]);
-  reinterpret_cast<float4*>(to)[1] = make_float4(x[4], x[5], x[6], x[7]);
-}
+constexpr int kReadRows = 64, kReadWarps = 4;
 
 template <int D, class T>
-__global__ void __launch_bounds__(256) read_kernel(ReadArgs a) {
+__global__ void __launch_bounds__(32 * kReadWarps) read_kernel(const __grid_constant__ ReadArgs a) {
+  using B = Block<D>;
+  constexpr int G = B::kGroups, kPitch = D * (int)sizeof(T) + 16;        // bytes of a row in shared memory
+  __shared__ __align__(16) uint8_t s_rows[kReadWarps][kBlockTokens * kPitch];
   wait_for_stream();
-  constexpr int LANES = D / 8;
-  const int lane = threadIdx.x & 31;
-  const long long item = (long long)blockIdx.x * (256 / (2 * LANES)) + threadIdx.x / (2 * LANES);
-  const bool is_v = (lane / LANES) & 1;
-  const int o = lane % LANES;
-  const long long row = item / a.cache.heads;
-  const int head = (int)(item - row * a.cache.heads);
-  if (row >= a.rows) return;
-  const int r = upper_bound(a.cu + 1, a.requests, (int)row);
-  float x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-  int page = -1, token = 0;
-  if (r < a.requests) {
-    token = (int)row - a.cu[r] + (a.first ? a.first[r] : 0);
-    const int c = token / a.cache.page;
-    if (token >= 0 && c < a.width) page = a.table[(size_t)r * a.width + c];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, c = lane & 3;
+  uint8_t* rows = s_rows[warp];
+  // The CTA's rows as pieces: rows of one request in one block, numbered in order (several CTAs share the rows of few)
+  __shared__ int s_request[kReadRows], s_token[kReadRows], s_piece[kReadRows + 1];
+  __shared__ unsigned s_begin[kReadRows / 32];
+  static_assert(kReadRows == 64 && kReadWarps >= 2, "two warps look");
+  const int tid = threadIdx.x, w0 = blockIdx.x * kReadRows, in_window = min(kReadRows, a.rows - w0), subs = a.cache.page / kBlockTokens;
+  if (tid < kReadRows) {
+    const int row = w0 + tid, r = upper_bound(a.cu + 1, a.requests, row);
+    s_request[tid] = r;
+    s_token[tid] = r < a.requests ? (a.first ? a.first[r] : 0) + row - a.cu[r] : tid;               // (beyond the requests: blocks of 16 rows)
   }
-  if (page >= 0 && page < a.cache.num_pages) {
-    const int in_page = token % a.cache.page, t = in_page % kBlockTokens;
-    const uint8_t* block = block_at<D>(a.cache, page, head, in_page / kBlockTokens);
-    const __half* sc = reinterpret_cast<const __half*>(block + (is_v ? Block<D>::kScaleV : Block<D>::kScaleK) + ((t / 2) * Block<D>::kGroups + o / 4) * 8 + (t % 2) * 2);
-    const float s = __half2float(sc[0]), m = __half2float(sc[2]);
-    if (!is_v) {
-      const int ln = (t % 8) * 4 + o % 4;
-      const int at = (D == 128 ? (t / 8) * 512 + ln * 16 : ln * 16 + (t / 8) * 8) + (o / 4) * 4;
-      const uint32_t word = *reinterpret_cast<const uint32_t*>(block + at);
+  __syncthreads();
+  const bool begins = tid < in_window && (tid == 0 || s_request[tid] != s_request[tid - 1] || (s_token[tid] & 15) == 0);
+  const unsigned flags = __ballot_sync(0xffffffffu, begins);
+  if (tid < kReadRows && lane == 0) s_begin[warp] = flags;
+  __syncthreads();
+  const int pieces = __popc(s_begin[0]) + __popc(s_begin[1]);
+  if (begins) s_piece[__popc(flags & ((1u << lane) - 1u)) + (warp ? __popc(s_begin[0]) : 0)] = tid;
+  if (tid == 0) s_piece[pieces] = in_window;
+  __syncthreads();
+  for (int i = blockIdx.y * kReadWarps + warp; i < pieces * a.cache.heads; i += kReadWarps * gridDim.y) {
+    const int piece = i / a.cache.heads, head = i - piece * a.cache.heads, from = s_piece[piece], r = s_request[from], token = s_token[from], b = token >> 4;
+    int page = -1;
+    if (r < a.requests && b >= 0 && b / subs < a.width) page = a.table[(size_t)r * a.width + b / subs];
+    const bool there = page >= 0 && page < a.cache.num_pages;
+    const int t_first = token & 15, t_end = t_first + s_piece[piece + 1] - from;                    // tokens of the block that are asked for
+    const long long row0 = (long long)w0 + from - t_first;               // (the result's row of the block's token 0)
+    auto flush = [&](void* out) {
+      __syncwarp();
+      constexpr int CHUNKS = D * (int)sizeof(T) / 16;
+      for (int e = lane; e < kBlockTokens * CHUNKS; e += 32) {
+        const int t = e / CHUNKS, x = e - t * CHUNKS;
+        if (t >= t_first && t < t_end)
+          reinterpret_cast<uint4*>(reinterpret_cast<T*>(out) + ((row0 + t) * a.cache.heads + head) * D)[x] = there ? *reinterpret_cast<const uint4*>(rows + t * kPitch + x * 16) : make_uint4(0, 0, 0, 0);
+      }
+      __syncwarp();
+    };
+    auto put2 = [&](int t, int x, float f0, float f1) {                   // coordinates x, x + 1
+      if constexpr (sizeof(T) == 4) *reinterpret_cast<float2*>(rows + t * kPitch + x * 4) = make_float2(f0, f1);
+      else *reinterpret_cast<uint32_t*>(rows + t * kPitch + x * 2) = from_float2<T>(f0, f1);
+    };
+    if (!there) { flush(a.k); flush(a.v); continue; }
+    const uint8_t* block = block_at<D>(a.cache, page, head, b % subs);
+    uint32_t kw[2][G], vw[D / 16];
+    if constexpr (D == 128) {
 #pragma unroll
-      for (int e = 0; e < 8; ++e) x[e] = fmaf(s, (float)((word >> (4 * ((e % 2) * 4 + e / 2))) & 15u), m);
+      for (int half = 0; half < 2; ++half) {
+        const uint4 v = *reinterpret_cast<const uint4*>(block + half * 512 + lane * 16);
+        kw[half][0] = v.x; kw[half][1] = v.y; kw[half][2] = v.z; kw[half][3] = v.w;
+      }
     } else {
-      const int u = o / 2;
-      const uint8_t* at = block + Block<D>::kV + (u / 4) * 512 + (t % 8 / 2) * 16 + (u % 4) * 4 + (t % 2) * 2 + t / 8;
-#pragma unroll
-      for (int i = 0; i < 8; ++i) x[i] = fmaf(s, (float)((at[i * 64] >> (4 * (o & 1))) & 15u), m);
+      const uint4 v = *reinterpret_cast<const uint4*>(block + lane * 16);
+      kw[0][0] = v.x; kw[0][1] = v.y; kw[1][0] = v.z; kw[1][1] = v.w;
     }
+#pragma unroll
+    for (int i4 = 0; i4 < D / 64; ++i4) {
+      const uint4 v = *reinterpret_cast<const uint4*>(block + B::kV + i4 * 512 + lane * 16);
+      vw[4 * i4] = v.x; vw[4 * i4 + 1] = v.y; vw[4 * i4 + 2] = v.z; vw[4 * i4 + 3] = v.w;
+    }
+    uint32_t sk[2][2 * G], sv[2][2 * G];                                 // (scales, minima) of the token pair of token lane / 4 (+ 8), by group
+#pragma unroll
+    for (int half = 0; half < 2; ++half)
+#pragma unroll
+      for (int i4 = 0; i4 < G / 2; ++i4) {
+        const int at = (half * 4 + lane / 8) * G * 8 + i4 * 16;
+        const uint4 x = *reinterpret_cast<const uint4*>(block + B::kScaleK + at), y = *reinterpret_cast<const uint4*>(block + B::kScaleV + at);
+        sk[half][4 * i4] = x.x; sk[half][4 * i4 + 1] = x.y; sk[half][4 * i4 + 2] = x.z; sk[half][4 * i4 + 3] = x.w;
+        sv[half][4 * i4] = y.x; sv[half][4 * i4 + 1] = y.y; sv[half][4 * i4 + 2] = y.z; sv[half][4 * i4 + 3] = y.w;
+      }
+    const int odd = (lane >> 2) & 1;                                     // the lane's token is the pair's second
+    auto half_of = [&](uint32_t two) { return __half2float(__ushort_as_half((unsigned short)(odd ? two >> 16 : two))); };
+#pragma unroll
+    for (int half = 0; half < 2; ++half)
+#pragma unroll
+      for (int w = 0; w < G; ++w) {
+        const float s = half_of(sk[half][2 * w]), m = half_of(sk[half][2 * w + 1]);
+#pragma unroll
+        for (int e = 0; e < 4; ++e)                                      // coordinates 2 e, 2 e + 1 of the octet: nibbles e and e + 4
+          put2(lane / 4 + 8 * half, 32 * w + 8 * c + 2 * e, fmaf(s, (float)((kw[half][w] >> (4 * e)) & 15u), m), fmaf(s, (float)((kw[half][w] >> (4 * e + 16)) & 15u), m));
+      }
+    flush(a.k);
+#pragma unroll
+    for (int u = 0; u < D / 16; ++u) {
+      const int w = u / 2;
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {                                      // nibbles q and q + 4: tokens 2 c, 2 c + 1 (+ 8 for q >= 2) of coordinate 16 u + lane / 4 (+ 8 for odd q)
+        uint32_t codes = (vw[u] >> (4 * q)) & 0x000f000fu;
+        asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(codes) : "r"(codes));
+        // now coordinates 2 c, 2 c + 1 of token lane / 4
+        const int half = q / 2;
+        const float s = half_of(sv[half][2 * w]), m = half_of(sv[half][2 * w + 1]);
+        put2(lane / 4 + 8 * half, 16 * u + 8 * (q & 1) + 2 * c, fmaf(s, (float)(codes & 0xffffu), m), fmaf(s, (float)(codes >> 16), m));
+      }
+    }
+    flush(a.v);
   }
-  put8<T>(reinterpret_cast<T*>(is_v ? a.v : a.k) + (row * a.cache.heads + head) * D + o * 8, x);
 }
 
 CacheView view_of(const hyperattn_cache& c) { return {reinterpret_cast<uint8_t*>(c.pages), c.num_pages, c.page_tokens, c.kv_heads}; }
@@ -338,11 +479,12 @@ extern "C" int hyperattn_cache_store(const hyperattn_cache* cache, const void* k
   if (bad_stride(k_row_stride) || bad_stride(k_head_stride) || bad_stride(v_row_stride) || bad_stride(v_head_stride)) return HYPERATTN_UNSUPPORTED_SHAPE;
   if (misaligned(k) || misaligned(v)) return HYPERATTN_MISALIGNED;
   const StoreArgs a = {view_of(*cache), k, v, k_row_stride, k_head_stride, v_row_stride, v_head_stride, rows, slots};
-  const int per = 256 / (cache->d / 4);
-  const long long grid = ((long long)rows * cache->kv_heads + per - 1) / per;
-  if (grid > 0x7fffffffLL) return HYPERATTN_UNSUPPORTED_SHAPE;
   const cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
-  auto go = [&](auto kernel) { return status_of(launch(kernel, dim3((unsigned)grid), dim3(256), 0, st, a), "store"); };
+  // few rows: their heads over several CTAs
+  const int windows = (rows + kStoreRows - 1) / kStoreRows, most = (kStoreRows * cache->kv_heads + kStoreWarps - 1) / kStoreWarps;
+  int split = (2 * kSms + windows - 1) / windows;
+  if (split > most) split = most;
+  auto go = [&](auto kernel) { return status_of(launch(kernel, dim3((unsigned)windows, (unsigned)split), dim3(32 * kStoreWarps), 0, st, a), "store"); };
   if (cache->d == 64) return dtype == HYPERATTN_BF16 ? go(store_kernel<64, __nv_bfloat16>) : go(store_kernel<64, __half>);
   return dtype == HYPERATTN_BF16 ? go(store_kernel<128, __nv_bfloat16>) : go(store_kernel<128, __half>);
 }
@@ -356,12 +498,13 @@ extern "C" int hyperattn_cache_read(const hyperattn_cache* cache, const int32_t*
   if (rows == 0) return HYPERATTN_OK;
   if ((requests && !table) || !cu || !k || !v) return HYPERATTN_INVALID_ARGUMENT;
   if (misaligned(k) || misaligned(v)) return HYPERATTN_MISALIGNED;
+  // few rows: their blocks over several CTAs
+  const int windows = (rows + kReadRows - 1) / kReadRows, most = (kReadRows * cache->kv_heads + kReadWarps - 1) / kReadWarps;
+  int split = (8 * kSms + windows - 1) / windows;
+  if (split > most) split = most;
   const ReadArgs a = {view_of(*cache), table, cu, first, requests, table_width, rows, k, v};
-  const int per = 256 / (cache->d / 4);
-  const long long grid = ((long long)rows * cache->kv_heads + per - 1) / per;
-  if (grid > 0x7fffffffLL) return HYPERATTN_UNSUPPORTED_SHAPE;
   const cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
-  auto go = [&](auto kernel) { return status_of(launch(kernel, dim3((unsigned)grid), dim3(256), 0, st, a), "read"); };
+  auto go = [&](auto kernel) { return status_of(launch(kernel, dim3((unsigned)windows, (unsigned)split), dim3(32 * kReadWarps), 0, st, a), "read"); };
   if (cache->d == 64)
     return dtype == HYPERATTN_BF16 ? go(read_kernel<64, __nv_bfloat16>) : dtype == HYPERATTN_FP16 ? go(read_kernel<64, __half>) : go(read_kernel<64, float>);
   return dtype == HYPERATTN_BF16 ? go(read_kernel<128, __nv_bfloat16>) : dtype == HYPERATTN_FP16 ? go(read_kernel<128, __half>) : go(read_kernel<128, float>);
