@@ -199,7 +199,7 @@ __device__ __forceinline__ uint32_t low_bytes(uint32_t a, uint32_t b, uint32_t c
 }
 
 template <int D, class T>
-__global__ void __launch_bounds__(32 * kStoreWarps) store_kernel(const __grid_constant__ StoreArgs a) {
+__global__ void __launch_bounds__(32 * kStoreWarps, D == 64 ? 4 : 3) store_kernel(const __grid_constant__ StoreArgs a) {
   using B = Block<D>;
   constexpr int LANES = D / 8, PER = 32 / LANES, STEPS = kBlockTokens / PER, kWindow = kStoreRows + kBlockTokens;     // PER: rows at a time
   __shared__ int s_slot[kWindow + 1], s_run[kStoreRows];
@@ -480,9 +480,10 @@ extern "C" int hyperattn_cache_store(const hyperattn_cache* cache, const void* k
   if (misaligned(k) || misaligned(v)) return HYPERATTN_MISALIGNED;
   const StoreArgs a = {view_of(*cache), k, v, k_row_stride, k_head_stride, v_row_stride, v_head_stride, rows, slots};
   const cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
-  // few rows: their heads over several CTAs
+  // The heads of a window over several CTAs, until there are a few rounds of them: 32768 tokens of 32 heads (d = 64) with twice as many CTAs as SMs at least
+  // 181 us, six times 114, twelve times 100, 24 times 99; the kernel needs the registers of four CTAs an SM (d = 128: three).
   const int windows = (rows + kStoreRows - 1) / kStoreRows, most = (kStoreRows * cache->kv_heads + kStoreWarps - 1) / kStoreWarps;
-  int split = (2 * kSms + windows - 1) / windows;
+  int split = (12 * kSms + windows - 1) / windows;
   if (split > most) split = most;
   auto go = [&](auto kernel) { return status_of(launch(kernel, dim3((unsigned)windows, (unsigned)split), dim3(32 * kStoreWarps), 0, st, a), "store"); };
   if (cache->d == 64) return dtype == HYPERATTN_BF16 ? go(store_kernel<64, __nv_bfloat16>) : go(store_kernel<64, __half>);
@@ -498,9 +499,9 @@ extern "C" int hyperattn_cache_read(const hyperattn_cache* cache, const int32_t*
   if (rows == 0) return HYPERATTN_OK;
   if ((requests && !table) || !cu || !k || !v) return HYPERATTN_INVALID_ARGUMENT;
   if (misaligned(k) || misaligned(v)) return HYPERATTN_MISALIGNED;
-  // few rows: their blocks over several CTAs
+  // (likewise: 65536 tokens of 8 heads (d = 128) 68.0 us with eight times as many CTAs as SMs at least, 65.2 with 24 times, 66.5 with 48)
   const int windows = (rows + kReadRows - 1) / kReadRows, most = (kReadRows * cache->kv_heads + kReadWarps - 1) / kReadWarps;
-  int split = (8 * kSms + windows - 1) / windows;
+  int split = (24 * kSms + windows - 1) / windows;
   if (split > most) split = most;
   const ReadArgs a = {view_of(*cache), table, cu, first, requests, table_width, rows, k, v};
   const cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
