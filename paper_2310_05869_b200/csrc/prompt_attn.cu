@@ -95,6 +95,10 @@ struct Cfg {
   static constexpr int kStages = D == 64 ? 10 : 5;                     // tiles of K or V on their way
   static constexpr uint32_t kOffQ = 0, kOffRing = 2 * kTile, kOffMisc = kOffRing + kStages * kTile;
   static constexpr uint32_t kSmem = kOffMisc + 1024;
+  // TMEM columns: S_0, S_1 (128 each), O_0, O_1; at d = 64 there is room for P_i beside S_i, so that the next scores do not wait for this tile's weights
+  static constexpr bool kOwnP = D == 64;
+  static constexpr uint32_t kColO = kOwnP ? 384 : 256, kStepO = kOwnP ? 64 : 128;
+  __host__ __device__ static constexpr uint32_t col_p(int i) { return kOwnP ? 256 + 64 * i : 128 * i; }
 };
 
 struct Item {
@@ -112,6 +116,7 @@ __device__ __forceinline__ Item item_at(const PromptArgs& a, int index, int tile
   const int lane = threadIdx.x & 31;
   Item it = {};
   it.end = 1;
+  if (index < 0) return it;
   const int block = index / a.kv_heads, pair_tokens = 2 * tile_tokens;
   it.kv = index - block * a.kv_heads;
   int before = 0;
@@ -183,16 +188,19 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const __grid_consta
   Item* s_item = reinterpret_cast<Item*>(smem + C::kOffMisc);                    // [2]
   uint32_t* s_tmem = reinterpret_cast<uint32_t*>(smem + C::kOffMisc + 256);
   volatile int* s_abort = reinterpret_cast<volatile int*>(smem + C::kOffMisc + 260);
-  const uint32_t bar0 = ubase + C::kOffMisc + 272;
+  const uint32_t next0 = ubase + C::kOffMisc + 272, bar0 = next0 + 16;           // answer of next_index
   auto bar_item = [&](int set) { return bar0 + 8 * set; };                       // an item's description is written
   auto bar_itemfree = [&](int set) { return bar0 + 16 + 8 * set; };              // everybody is done with it
   const uint32_t bar_q = bar0 + 32, bar_qfree = bar0 + 40;                       // Q has landed; no product reads it any more
   auto bar_s = [&](int i) { return bar0 + 48 + 8 * i; };                         // S_i written
-  auto bar_p = [&](int i) { return bar0 + 64 + 8 * i; };                         // P_i written
-  auto bar_o = [&](int i) { return bar0 + 80 + 8 * i; };                         // O_i complete
-  auto bar_ofree = [&](int i) { return bar0 + 96 + 8 * i; };                     // O_i read
-  auto bar_full = [&](int s) { return bar0 + 112 + 8 * s; };
-  auto bar_empty = [&](int s) { return bar0 + 112 + 8 * (C::kStages + s); };
+  auto bar_p = [&](int i, int half) { return bar0 + 64 + 16 * i + 8 * half; };   // P_i written, keys 0..63 and 64..127
+  auto bar_o = [&](int i) { return bar0 + 96 + 8 * i; };                         // O_i complete
+  auto bar_ofree = [&](int i) { return bar0 + 112 + 8 * i; };                    // O_i read
+  auto bar_sfree = [&](int i) { return bar0 + 128 + 8 * i; };                    // (P beside S) S_i read
+  auto bar_pfree = [&](int i) { return bar0 + 144 + 8 * i; };                    // (P beside S) P_i multiplied
+  const uint32_t bar_loaded = bar0 + 160, bar_next = bar0 + 168;                 // all loads of an item have been asked for; an answer has come
+  auto bar_full = [&](int s) { return bar0 + 176 + 8 * s; };
+  auto bar_empty = [&](int s) { return bar0 + 176 + 8 * (C::kStages + s); };
   const int tid = threadIdx.x, lane = tid & 31;
   const int warp = __shfl_sync(0xffffffffu, tid >> 5, 0);
 
@@ -206,12 +214,17 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const __grid_consta
       mbar_init(bar_item(i), 1);
       mbar_init(bar_itemfree(i), 256 + 2);
       mbar_init(bar_s(i), 1);
-      mbar_init(bar_p(i), 128);
+      mbar_init(bar_p(i, 0), 128);
+      mbar_init(bar_p(i, 1), 128);
       mbar_init(bar_o(i), 1);
       mbar_init(bar_ofree(i), 128);
+      mbar_init(bar_sfree(i), 128);
+      mbar_init(bar_pfree(i), 1);
     }
     mbar_init(bar_q, 1);
     mbar_init(bar_qfree, 1);
+    mbar_init(bar_loaded, 1);
+    mbar_init(bar_next, 1);
     for (int s = 0; s < C::kStages; ++s) { mbar_init(bar_full(s), 1); mbar_init(bar_empty(s), 1); }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
@@ -224,14 +237,28 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const __grid_consta
   tc_fence_after();
   const uint32_t tmem = __shfl_sync(0xffffffffu, *s_tmem, 0);
   wait_for_stream();
-  // TMEM columns: S_0, S_1 (128 each), O_0, O_1
+  // the number of a CTA that has not been launched and will not be, or -1 if there is none left
+  auto next_index = [&](int& asked, int& index) {
+    if (lane == 0)
+      asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%1], 16;\n\t"
+                   "clusterlaunchcontrol.try_cancel.async.shared::cta.mbarrier::complete_tx::bytes.b128 [%0], [%1];" ::"r"(next0), "r"(bar_next) : "memory");
+    const bool ok = warp_wait<16>(bar_next, asked & 1, s_abort, status);
+    ++asked;
+    uint32_t x = 0, got = 0;
+    asm volatile("{\n\t.reg .pred p;\n\t.reg .b128 r;\n\tld.shared.b128 r, [%2];\n\tclusterlaunchcontrol.query_cancel.is_canceled.pred.b128 p, r;\n\tselp.u32 %1, 1, 0, p;\n\t"
+                 "mov.u32 %0, 0;\n\t@p clusterlaunchcontrol.query_cancel.get_first_ctaid::x.b32.b128 %0, r;\n\t}" : "=r"(x), "=r"(got) : "r"(next0) : "memory");
+    fence_async_smem();                                                    // (the next answer comes by the async proxy)
+    __syncwarp();
+    index = got ? (int)x : -1;
+    return ok;
+  };
   auto item_wait = [&](int it, auto site) { return warp_wait<decltype(site)::value>(bar_item(it & 1), (it >> 1) & 1, s_abort, status); };
 
   if (warp < 8) {
     // ================= softmax and results of query tile i: a thread a row =============================
     const int i = warp >> 2, row = tid & 127;
     const uint32_t lane_addr = tmem + ((uint32_t)((warp & 3) * 32) << 16);
-    const uint32_t scol = lane_addr + kTileKeys * i, ocol = lane_addr + 256 + 128 * i;
+    const uint32_t scol = lane_addr + kTileKeys * i, pcol = lane_addr + C::col_p(i), ocol = lane_addr + C::kColO + C::kStepO * i;
     const int token = row / group, head = row - token * group;
     int done = 0;                        // key tiles of this query tile so far
     int items = 0;                       // items in which it had any
@@ -257,6 +284,10 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const __grid_consta
         for (int c = 0; c < 4; ++c) tmem_ld32_issue(scol + 32 * c, r[c]);
 #pragma unroll
         for (int c = 0; c < 4; ++c) tmem_ld32_wait(r[c]);
+        if constexpr (C::kOwnP) {
+          tc_fence_before();
+          mbar_arrive(bar_sfree(i));
+        }
         if (j * kTileKeys + kTileKeys - 1 > least) {
           const int rel = limit - j * kTileKeys;
 #pragma unroll
@@ -275,8 +306,15 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const __grid_consta
         }
         const float top = fmaxf(max3(m[0], m[1], m[2]), m[3]) * a.scale_log2;
         const bool move = top > ref + kMoveAt;
+        if constexpr (C::kOwnP) {
+          if (done + n > 0) {                                              // the weights before these have been multiplied
+            ok = warp_wait<13>(bar_pfree(i), (done + n - 1) & 1, s_abort, status);
+            if (!ok) break;
+            tc_fence_after();
+          }
+        }
         if (__any_sync(0xffffffffu, move)) {
-          // (S of this tile is there, so the products before it are done; the next one on O waits for this P)
+          // (the products before this tile's are done - without P beside S because its scores came after them; the next one on O waits for this P)
           float alpha = 1.f;
           if (move) { alpha = ex2(ref - top); ref = top; }
           sum2 = fmul2(sum2, pack_f2(alpha, alpha));
@@ -296,11 +334,13 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const __grid_consta
             sum2 = fadd2(sum2, pack_f2(x, y));
             p[e] = from_float2<T>(x, y);
           }
-          tmem_st16(scol + 16 * c, p);
+          tmem_st16(pcol + 16 * c, p);
+          if (c & 1) {
+            tmem_wait_st();
+            tc_fence_before();
+            mbar_arrive(bar_p(i, c >> 1));
+          }
         }
-        tmem_wait_st();
-        tc_fence_before();
-        mbar_arrive(bar_p(i));
       }
       if (!ok) break;
       done += tiles;
@@ -413,31 +453,64 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const __grid_consta
         umma_commit(bar_empty(stage_of(most - 1, 0) % C::kStages));
         if (most == 1) umma_commit(bar_qfree);
       }
-      for (int j = most - 1; j >= 0 && ok; --j) {
-        wait_tile(stage_of(j, 1));
-        if (j > 0) wait_tile(stage_of(j - 1, 0));
+      // O_i += P_i V of key tile j, in two steps as the weights come
+      auto outputs = [&](int i, int j) {
         const uint32_t v_lo = dv_lo + (uint32_t)(stage_of(j, 1) % C::kStages) * (C::kTile >> 4);
+        if (j == tiles[i] - 1 && items[i] > 0) ok = warp_wait<6>(bar_ofree(i), (items[i] - 1) & 1, s_abort, status);
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          if (ok && j < tiles[i]) {
-            if (j == tiles[i] - 1 && items[i] > 0) ok = warp_wait<6>(bar_ofree(i), (items[i] - 1) & 1, s_abort, status);
-            if (ok) ok = warp_wait<7>(bar_p(i), (done[i] + tiles[i] - 1 - j) & 1, s_abort, status);
-            if (ok) {
-              tc_fence_after();
-              if (el) {
+        for (int half = 0; half < 2; ++half) {
+          if (ok) ok = warp_wait<7>(bar_p(i, half), (done[i] + tiles[i] - 1 - j) & 1, s_abort, status);
+          if (!ok) return;
+          tc_fence_after();
+          if (el) {
 #pragma unroll
-                for (int kk = 0; kk < kTileKeys / 16; ++kk)
-                  mma_ts2(tmem + 256 + 128 * i, tmem + kTileKeys * i + kk * 8, v_lo + kk * (2048 >> 4), desc_hi, idesc_o, kk > 0 || j < tiles[i] - 1);
-                if (j == 0) umma_commit(bar_o(i));
-              }
+            for (int k4 = 0; k4 < kTileKeys / 32; ++k4) {
+              const int kk = half * (kTileKeys / 32) + k4;
+              mma_ts2(tmem + C::kColO + C::kStepO * i, tmem + C::col_p(i) + kk * 8, v_lo + kk * (2048 >> 4), desc_hi, idesc_o, kk > 0 || j < tiles[i] - 1);
             }
           }
-          if (ok && i == 1 && el) umma_commit(bar_empty(stage_of(j, 1) % C::kStages));
-          if (ok && j > 0 && j - 1 < tiles[i]) scores(i, j - 1);
         }
-        if (ok && j > 0 && el) {
-          umma_commit(bar_empty(stage_of(j - 1, 0) % C::kStages));
-          if (j == 1) umma_commit(bar_qfree);
+        if (el) {
+          if (C::kOwnP) umma_commit(bar_pfree(i));
+          if (j == 0) umma_commit(bar_o(i));
+        }
+      };
+      for (int j = most - 1; j >= 0 && ok; --j) {
+        if constexpr (C::kOwnP) {
+          // the next scores as soon as these have been read, then the products with V
+          if (j > 0) {
+            wait_tile(stage_of(j - 1, 0));
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+              if (ok && j - 1 < tiles[i]) {
+                if (j < tiles[i]) ok = warp_wait<14>(bar_sfree(i), (done[i] + tiles[i] - 1 - j) & 1, s_abort, status);
+                if (!ok) break;
+                tc_fence_after();
+                scores(i, j - 1);
+              }
+            if (ok && el) {
+              umma_commit(bar_empty(stage_of(j - 1, 0) % C::kStages));
+              if (j == 1) umma_commit(bar_qfree);
+            }
+          }
+          if (ok) wait_tile(stage_of(j, 1));
+#pragma unroll
+          for (int i = 0; i < 2; ++i)
+            if (ok && j < tiles[i]) outputs(i, j);
+          if (ok && el) umma_commit(bar_empty(stage_of(j, 1) % C::kStages));
+        } else {
+          wait_tile(stage_of(j, 1));
+          if (j > 0) wait_tile(stage_of(j - 1, 0));
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            if (ok && j < tiles[i]) outputs(i, j);
+            if (ok && i == 1 && el) umma_commit(bar_empty(stage_of(j, 1) % C::kStages));
+            if (ok && j > 0 && j - 1 < tiles[i]) scores(i, j - 1);
+          }
+          if (ok && j > 0 && el) {
+            umma_commit(bar_empty(stage_of(j - 1, 0) % C::kStages));
+            if (j == 1) umma_commit(bar_qfree);
+          }
         }
       }
       ring += 2 * most;
@@ -455,7 +528,10 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const __grid_consta
       __syncwarp();
       if (lane == 0) mbar_arrive(bar_itemfree(it & 1));
       if (d.end) break;
-      if (d.most == 0) continue;
+      if (d.most == 0) {
+        if (lane == 0) mbar_arrive(bar_loaded);
+        continue;
+      }
       if (qitems > 0) ok = warp_wait<9>(bar_qfree, (qitems - 1) & 1, s_abort, status);
       if (!ok) break;
       if (lane == 0) {
@@ -496,6 +572,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const __grid_consta
         armed = g + 1;
         __syncwarp();
       }
+      if (lane == 0) mbar_arrive(bar_loaded);
       ring += 2 * d.most;
     }
     // nothing may be on its way into shared memory when the CTA ends
@@ -503,12 +580,17 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const __grid_consta
     if (qitems > 0) mbar_drain(bar_q, (qitems - 1) & 1);
   } else if (warp == 10) {
     // ================= items ===============================================================================
+    // The grid has a CTA for every item that there can be.  A CTA that is done with its own takes the place of one that has not been launched (cluster launch
+    // control), so that whoever is free takes the next item, in order; it asks when its loads of the present one are on their way, not earlier.
     bool ok = true;
+    int asked = 0, index = blockIdx.x;
     for (int it = 0; ok; ++it) {
-      // rounds of the grid in alternating direction: a CTA that had a long item of one round has a short one of the next
-      const int index = it * gridDim.x + ((it & 1) ? gridDim.x - 1 - blockIdx.x : blockIdx.x);
-      const Item d = item_at(a, index, tile_tokens);
-      if (it >= 2) ok = warp_wait<11>(bar_itemfree(it & 1), ((it >> 1) - 1) & 1, s_abort, status);
+      Item d = item_at(a, index, tile_tokens);
+      while (d.end && it > 0 && index >= 0 && ok) {                        // (numbers that are no item come last, and are taken out of the way)
+        ok = next_index(asked, index);
+        if (ok && index >= 0) d = item_at(a, index, tile_tokens);
+      }
+      if (ok && it >= 2) ok = warp_wait<11>(bar_itemfree(it & 1), ((it >> 1) - 1) & 1, s_abort, status);
       if (!ok) break;
       if (lane == 0) {
         s_item[it & 1] = d;
@@ -516,7 +598,10 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const __grid_consta
       }
       __syncwarp();
       if (d.end) break;
+      ok = warp_wait<15>(bar_loaded, it & 1, s_abort, status);
+      if (ok) ok = next_index(asked, index);
     }
+    if (asked > 0) mbar_drain(bar_next, (asked - 1) & 1);
   }
 
   // ---- teardown ----
@@ -530,12 +615,11 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const __grid_consta
 
 template <int D, class T>
 cudaError_t run_prompt(const PromptArgs& a, const PromptMaps& maps, int group, int tile_tokens, int* status, cudaStream_t st) {
-  int sms = 0;
-  cudaError_t e = sm_count(&sms);
-  if (e == cudaSuccess) e = allow_smem<prompt_kernel<D, T>>(Cfg<D>::kSmem);
+  cudaError_t e = allow_smem<prompt_kernel<D, T>>(Cfg<D>::kSmem);
   if (e != cudaSuccess) return e;
   const long long items = ((long long)a.q_rows / (2 * tile_tokens) + a.requests) * a.kv_heads;       // at most
-  return launch(prompt_kernel<D, T>, dim3((unsigned)(items < sms ? items : sms)), dim3(kThreads), Cfg<D>::kSmem, st, a, maps, group, tile_tokens, status);
+  if (items > 0x7fffffffLL) return cudaErrorInvalidValue;
+  return launch(prompt_kernel<D, T>, dim3((unsigned)items), dim3(kThreads), Cfg<D>::kSmem, st, a, maps, group, tile_tokens, status);
 }
 
 }  // namespace
