@@ -4,10 +4,10 @@
 // that read the key head, so that the keys of a group are fetched once and a tile of many heads sees few keys in vain.  A
 // CTA walks over the tiles of 128 keys from the last one that is seen down to the first:
 //     S_i = Q_i K^T           tcgen05.mma, operands in 128B-swizzled shared memory (TMA boxes), S_i in TMEM
-//     P_i = exp2(c S_i - m)   softmax warpgroup i, a thread a row; P_i goes over S_i in the inputs' type
+//     P_i = exp2(c S_i - m)   softmax warpgroup i, a thread a row; P_i in TMEM, in the inputs' type
 //     O_i += P_i V            tcgen05.mma, P_i read from TMEM
 // The tensor pipe works for one query tile while the other one's weights are made.  The reference m of a row is the maximum of its first
-// tile and moves when it is exceeded by more than 2^8, and then O is multiplied in TMEM; tiles with keys that a row does not see are
+// tile; it moves when a tile's weights sum to more than 2^15, and then O is multiplied in TMEM.  Tiles with keys that a row does not see are
 // the first ones, so masks cost the later ones nothing.
 //
 // Values of keys that a row does not see are multiplied with zeros, which is not nothing where they are infinite or NaN.  Those beyond a
@@ -86,7 +86,7 @@ struct alignas(64) PromptMaps {
 
 constexpr int kTileRows = 128, kTileKeys = 128;
 constexpr int kThreads = 384;
-constexpr float kMoveAt = 8.f;          // octaves a row's scores may exceed its reference before that moves (fp16 weights end at 2^16)
+constexpr float kSumLimit = 32768.f;    // a tile whose weights sum to more has its reference moved (fp16 weights end at 2^16)
 
 template <int D>
 struct Cfg {
@@ -98,6 +98,7 @@ struct Cfg {
   // TMEM columns: S_0, S_1 (128 each), O_0, O_1; at d = 64 there is room for P_i beside S_i, so that the next scores do not wait for this tile's weights
   static constexpr bool kOwnP = D == 64;
   static constexpr uint32_t kColO = kOwnP ? 384 : 256, kStepO = kOwnP ? 64 : 128;
+  static constexpr int kArithmetic = 8;                                // every so many-th pair of exponentials is made by arithmetic
   __host__ __device__ static constexpr uint32_t col_p(int i) { return kOwnP ? 256 + 64 * i : 128 * i; }
 };
 
@@ -161,10 +162,30 @@ __device__ __forceinline__ Item item_at(const PromptArgs& a, int index, int tile
 
 template <class T> __device__ __forceinline__ constexpr uint32_t type_bits() { return sizeof(T) && std::is_same<T, __nv_bfloat16>::value ? (1u << 7) | (1u << 10) : 0u; }
 
+// (NaN if one of them is)
 __device__ __forceinline__ float max3(float a, float b, float c) {
   float d;
-  asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+  asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
   return d;
+}
+
+// 2^x of two numbers in -infinity .. 2^10 by arithmetic: x = n + f with n the nearest integer, 2^f by a polynomial of degree 4 (its coefficients a least-maximum
+// fit of the relative error over -1/2 .. 1/2: 2.7e-6), n added to the exponent.  Below 2^-125 it is that.  The exponential unit makes 16 a clock and SM,
+// which is what a tile of scores takes longest for; so some of them are made here.
+__device__ __forceinline__ uint64_t exp2_pair(uint64_t x2) {
+  float x, y;
+  unpack_f2(x2, x, y);
+  x2 = pack_f2(max3(x, -125.f, -125.f), max3(y, -125.f, -125.f));                       // (NaN stays, and becomes a huge number or NaN)
+  const uint64_t t = fadd2(x2, pack_f2(12582912.f, 12582912.f));                      // 1.5 * 2^23 + n
+  const uint64_t f = ffma2(fadd2(t, pack_f2(-12582912.f, -12582912.f)), pack_f2(-1.f, -1.f), x2);
+  uint64_t p = ffma2(f, pack_f2(0.009570102207362652f, 0.009570102207362652f), pack_f2(0.05591786280274391f, 0.05591786280274391f));
+  p = ffma2(f, p, pack_f2(0.240247443318367f, 0.240247443318367f));
+  p = ffma2(f, p, pack_f2(0.6931217908859253f, 0.6931217908859253f));
+  p = ffma2(f, p, pack_f2(0.9999992847442627f, 0.9999992847442627f));
+  float p0, p1, t0, t1;
+  unpack_f2(p, p0, p1);
+  unpack_f2(t, t0, t1);
+  return pack_u2(__float_as_uint(p0) + (__float_as_uint(t0) << 23), __float_as_uint(p1) + (__float_as_uint(t1) << 23));
 }
 
 // O of a row times alpha, in TMEM (rare).  All lanes together.
@@ -193,7 +214,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const __grid_consta
   auto bar_itemfree = [&](int set) { return bar0 + 16 + 8 * set; };              // everybody is done with it
   const uint32_t bar_q = bar0 + 32, bar_qfree = bar0 + 40;                       // Q has landed; no product reads it any more
   auto bar_s = [&](int i) { return bar0 + 48 + 8 * i; };                         // S_i written
-  auto bar_p = [&](int i, int half) { return bar0 + 64 + 16 * i + 8 * half; };   // P_i written, keys 0..63 and 64..127
+  auto bar_p = [&](int i) { return bar0 + 64 + 8 * i; };                         // P_i written
   auto bar_o = [&](int i) { return bar0 + 96 + 8 * i; };                         // O_i complete
   auto bar_ofree = [&](int i) { return bar0 + 112 + 8 * i; };                    // O_i read
   auto bar_sfree = [&](int i) { return bar0 + 128 + 8 * i; };                    // (P beside S) S_i read
@@ -214,8 +235,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const __grid_consta
       mbar_init(bar_item(i), 1);
       mbar_init(bar_itemfree(i), 256 + 2);
       mbar_init(bar_s(i), 1);
-      mbar_init(bar_p(i, 0), 128);
-      mbar_init(bar_p(i, 1), 128);
+      mbar_init(bar_p(i), 128);
       mbar_init(bar_o(i), 1);
       mbar_init(bar_ofree(i), 128);
       mbar_init(bar_sfree(i), 128);
@@ -273,6 +293,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const __grid_consta
       const int limit = a.causal ? min(d.last + tok, d.keys - 1) : d.keys - 1;  // last key that the row sees
       const int least = a.causal ? min(d.last + i * tile_tokens, d.keys - 1) : d.keys - 1;       // the tile's first token
       float ref = -INFINITY;
+      bool finite = true;
       uint64_t sum2 = 0;
       for (int n = 0; n < tiles && ok; ++n) {
         const int j = tiles - 1 - n;
@@ -296,16 +317,6 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const __grid_consta
             for (int e = 0; e < 32; ++e)
               if (32 * c + e > rel) r[c][e] = 0xff800000u;
         }
-        float m[4];
-#pragma unroll
-        for (int c = 0; c < 4; ++c) {
-          m[c] = max3(__uint_as_float(r[c][0]), __uint_as_float(r[c][1]), __uint_as_float(r[c][2]));
-#pragma unroll
-          for (int e = 3; e < 31; e += 2) m[c] = max3(m[c], __uint_as_float(r[c][e]), __uint_as_float(r[c][e + 1]));
-          m[c] = fmaxf(m[c], __uint_as_float(r[c][31]));
-        }
-        const float top = fmaxf(max3(m[0], m[1], m[2]), m[3]) * a.scale_log2;
-        const bool move = top > ref + kMoveAt;
         if constexpr (C::kOwnP) {
           if (done + n > 0) {                                              // the weights before these have been multiplied
             ok = warp_wait<13>(bar_pfree(i), (done + n - 1) & 1, s_abort, status);
@@ -313,44 +324,73 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const __grid_consta
             tc_fence_after();
           }
         }
-        if (__any_sync(0xffffffffu, move)) {
+        // The maximum is not taken of every tile: weights are made against the reference that the row has, and only where their sum shows that one of them may be
+        // too large (or a score is not a number), or there is no reference yet, the maximum is taken, the reference moved to it, and the weights are made again.
+        auto move_reference = [&] {
+          float m[4];
+#pragma unroll
+          for (int c = 0; c < 4; ++c) {
+            m[c] = max3(__uint_as_float(r[c][0]), __uint_as_float(r[c][1]), __uint_as_float(r[c][2]));
+#pragma unroll
+            for (int e = 3; e < 31; e += 2) m[c] = max3(m[c], __uint_as_float(r[c][e]), __uint_as_float(r[c][e + 1]));
+            m[c] = max3(m[c], __uint_as_float(r[c][31]), __uint_as_float(r[c][31]));
+          }
+          const float top = max3(max3(m[0], m[1], m[2]), m[3], m[3]) * a.scale_log2;
+          finite = finite && top < INFINITY;                               // (false for NaN)
+          const bool move = top > ref;
+          if (!__any_sync(0xffffffffu, move)) return;
           // (the products before this tile's are done - without P beside S because its scores came after them; the next one on O waits for this P)
           float alpha = 1.f;
           if (move) { alpha = ex2(ref - top); ref = top; }
           sum2 = fmul2(sum2, pack_f2(alpha, alpha));
           if (n > 0) rescale_o(ocol, D, alpha);
-        }
-        const float off = ref == -INFINITY ? 0.f : -ref;
-        const uint64_t sc2 = pack_f2(a.scale_log2, a.scale_log2), off2 = pack_f2(off, off);
+        };
+        if (__any_sync(0xffffffffu, ref == -INFINITY)) move_reference();
+        const uint64_t sc2 = pack_f2(a.scale_log2, a.scale_log2);
+        for (int attempt = 0;; ++attempt) {
+          const float off = ref == -INFINITY ? 0.f : -ref;
+          const uint64_t off2 = pack_f2(off, off);
+          uint64_t tile2 = 0;
 #pragma unroll
-        for (int c = 0; c < 4; ++c) {
-          uint32_t p[16];
+          for (int c = 0; c < 4; ++c) {
+            uint32_t p[16];
 #pragma unroll
-          for (int e = 0; e < 16; ++e) {
-            const uint64_t x2 = ffma2(pack_u2(r[c][2 * e], r[c][2 * e + 1]), sc2, off2);
-            float x, y;
-            unpack_f2(x2, x, y);
-            x = ex2(x); y = ex2(y);
-            sum2 = fadd2(sum2, pack_f2(x, y));
-            p[e] = from_float2<T>(x, y);
+            for (int e = 0; e < 16; ++e) {
+              const uint64_t x2 = ffma2(pack_u2(r[c][2 * e], r[c][2 * e + 1]), sc2, off2);
+              uint64_t w2;
+              if (e % C::kArithmetic == C::kArithmetic - 1) w2 = exp2_pair(x2);
+              else {
+                float x, y;
+                unpack_f2(x2, x, y);
+                w2 = pack_f2(ex2(x), ex2(y));
+              }
+              tile2 = fadd2(tile2, w2);
+              float x, y;
+              unpack_f2(w2, x, y);
+              p[e] = from_float2<T>(x, y);
+            }
+            tmem_st16(pcol + 16 * c, p);
           }
-          tmem_st16(pcol + 16 * c, p);
-          if (c & 1) {
-            tmem_wait_st();
-            tc_fence_before();
-            mbar_arrive(bar_p(i, c >> 1));
+          float t0, t1;
+          unpack_f2(tile2, t0, t1);
+          if (attempt > 0 || !__any_sync(0xffffffffu, !(t0 + t1 <= kSumLimit))) {
+            sum2 = fadd2(sum2, tile2);
+            break;
           }
+          move_reference();
         }
+        tmem_wait_st();
+        tc_fence_before();
+        mbar_arrive(bar_p(i));
       }
       if (!ok) break;
       done += tiles;
       // ---- results ----
       float s0, s1;
       unpack_f2(sum2, s0, s1);
-      const float sum = s0 + s1, inv = sum == 0.f ? 0.f : 1.f / sum;
+      const float sum = s0 + s1, inv = ref == -INFINITY ? 0.f : 1.f / sum;        // (no reference: nothing was seen, or only -infinity)
       const bool mine = token < tokens && token < tile_tokens;
       const size_t at = (size_t)(d.row0 + tok) * a.q_heads + d.kv * group + head;
-      bool finite = true;
       if (tiles > 0) {
         ok = warp_wait<2>(bar_o(i), items & 1, s_abort, status);
         if (!ok) break;
@@ -387,7 +427,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const __grid_consta
         tc_fence_before();
         mbar_arrive(bar_ofree(i));
         ++items;
-        if (mine) a.lse[at] = sum == 0.f ? -INFINITY : (ref + log2f(sum)) * 0.6931471805599453f;
+        if (mine) a.lse[at] = ref == -INFINITY ? -INFINITY : (ref + log2f(sum)) * 0.6931471805599453f;
       } else if (mine) {
         a.lse[at] = -INFINITY;
         const int bytes = D * (a.out_kind == HYPERATTN_FP32 ? 4 : 2);
@@ -453,22 +493,17 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const __grid_consta
         umma_commit(bar_empty(stage_of(most - 1, 0) % C::kStages));
         if (most == 1) umma_commit(bar_qfree);
       }
-      // O_i += P_i V of key tile j, in two steps as the weights come
+      // O_i += P_i V of key tile j
       auto outputs = [&](int i, int j) {
         const uint32_t v_lo = dv_lo + (uint32_t)(stage_of(j, 1) % C::kStages) * (C::kTile >> 4);
         if (j == tiles[i] - 1 && items[i] > 0) ok = warp_wait<6>(bar_ofree(i), (items[i] - 1) & 1, s_abort, status);
+        if (ok) ok = warp_wait<7>(bar_p(i), (done[i] + tiles[i] - 1 - j) & 1, s_abort, status);
+        if (!ok) return;
+        tc_fence_after();
+        if (el) {
 #pragma unroll
-        for (int half = 0; half < 2; ++half) {
-          if (ok) ok = warp_wait<7>(bar_p(i, half), (done[i] + tiles[i] - 1 - j) & 1, s_abort, status);
-          if (!ok) return;
-          tc_fence_after();
-          if (el) {
-#pragma unroll
-            for (int k4 = 0; k4 < kTileKeys / 32; ++k4) {
-              const int kk = half * (kTileKeys / 32) + k4;
-              mma_ts2(tmem + C::kColO + C::kStepO * i, tmem + C::col_p(i) + kk * 8, v_lo + kk * (2048 >> 4), desc_hi, idesc_o, kk > 0 || j < tiles[i] - 1);
-            }
-          }
+          for (int kk = 0; kk < kTileKeys / 16; ++kk)
+            mma_ts2(tmem + C::kColO + C::kStepO * i, tmem + C::col_p(i) + kk * 8, v_lo + kk * (2048 >> 4), desc_hi, idesc_o, kk > 0 || j < tiles[i] - 1);
         }
         if (el) {
           if (C::kOwnP) umma_commit(bar_pfree(i));
