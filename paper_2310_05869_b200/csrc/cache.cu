@@ -8,35 +8,36 @@ namespace {
 
 // ---- plan ------------------------------------------------------------------------------------------------------------------
 // Everything follows from three running sums over the requests (new tokens, pages needed, pages released), which every CTA makes for
-// itself in shared memory - reading a few KB again costs less than a launch to make them first - and then takes its share of the tables,
-// the stack and the rows.
-constexpr int kPlanThreads = 512;
+// itself in shared memory - reading a few KB again costs less than a launch to make them first.  Then it does one thing: some CTAs
+// write the tables, some the rows, some the stack, one the requests' new state, so that their latencies do not add up.
+constexpr int kPlanThreads = 512, kPlanWarps = kPlanThreads / 32, kPlanColumns = 512;      // kPlanColumns: table entries of a warp at a time
 
-struct PlanShared {      // [R] each, running sums inclusive
-  int *add, *need, *rel, *info;      // info: pages the request has, | 1 << 30: admitted, | 1 << 31: ended
-};
+struct PlanParts { int tables, rows, stack; };           // CTAs for each
 
-__global__ void __launch_bounds__(kPlanThreads) plan_kernel(hyperattn_plan p) {
+__global__ void __launch_bounds__(kPlanThreads) plan_kernel(const __grid_constant__ hyperattn_plan p, PlanParts parts) {
   extern __shared__ int smem[];
-  __shared__ int s_warp[3][kPlanThreads / 32];
+  __shared__ int s_warp[3][kPlanWarps], s_given;
   wait_for_stream();
   const int R = p.requests, W = p.table_width, P = p.page_tokens, F = p.num_free;
-  int *s_add = smem, *s_need = smem + R, *s_rel = smem + 2 * R, *s_have = smem + 3 * R;
+  // running sums (inclusive); pages that a request has, 1 << 29: there is room for it, 1 << 30: it has ended; its length
+  int *s_add = smem, *s_need = smem + R, *s_rel = smem + 2 * R, *s_have = smem + 3 * R, *s_len = smem + 4 * R;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int n_free = min(max(p.n_free[0], 0), F);
+  if (tid == 0) s_given = 0;
 
   // a thread takes consecutive requests
   const int per = (R + kPlanThreads - 1) / kPlanThreads, r0 = min(R, tid * per), r1 = min(R, r0 + per);
   int sum[3] = {0, 0, 0};
   for (int r = r0; r < r1; ++r) {
     const int len = max(p.lengths[r], 0), add = p.new_tokens[r];
-    const int have = min((len + P - 1) / P, W);
+    const int have = min((int)(((long long)len + P - 1) / P), W);
     const long long pages = ((long long)len + max(add, 0) + P - 1) / P;
     const bool ended = add < 0, fits = !ended && pages <= W;
     const int need = fits ? max((int)pages - have, 0) : 0;
     sum[0] += max(add, 0); sum[1] += need; sum[2] += ended ? have : 0;
     s_add[r] = sum[0]; s_need[r] = sum[1]; s_rel[r] = sum[2];
     s_have[r] = have | (fits ? 1 << 29 : 0) | (ended ? 1 << 30 : 0);
+    s_len[r] = len;
   }
   int base[3];
 #pragma unroll
@@ -68,72 +69,84 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(hyperattn_plan p) {
   };
   auto fresh = [&](int r, int k) { return stack(total - 1 - (before(s_need, r) + k)); };      // request r's k-th new page
 
-  const int threads = gridDim.x * kPlanThreads, gid = blockIdx.x * kPlanThreads + tid;
-  // block tables: a thread writes four entries of a row, or one where rows do not start on 16 bytes
-  const bool quads = W % 4 == 0 && ((reinterpret_cast<uintptr_t>(p.table) | reinterpret_cast<uintptr_t>(p.table_out)) & 15) == 0;
-  const int step = quads ? 4 : 1, row_units = W / step;
-  for (long long u = gid; u < (long long)R * row_units; u += threads) {
-    const int r = (int)(u / row_units), c = (int)(u - (long long)r * row_units) * step;
-    const int have = have_of(r), keep = ended(r) ? 0 : have, end = admitted(r) ? have + need_of(r) : keep;
-    const size_t at = (size_t)r * W + c;
-    if (quads) {
-      int4 v = make_int4(-1, -1, -1, -1);
-      if (c < keep) v = *reinterpret_cast<const int4*>(p.table + at);
-      int* e = reinterpret_cast<int*>(&v);
+  int cta = blockIdx.x;
+  if (cta < parts.tables) {
+    // block tables: a warp takes pieces of rows
+    const int pieces = (W + kPlanColumns - 1) / kPlanColumns;
+    for (int u = cta * kPlanWarps + warp; u < R * pieces; u += parts.tables * kPlanWarps) {
+      const int r = u / pieces, c0 = (u - r * pieces) * kPlanColumns;
+      const int have = have_of(r), keep = ended(r) ? 0 : have, end = admitted(r) ? have + need_of(r) : keep;
+      const int32_t* from = p.table + (size_t)r * W;
+      int32_t* to = p.table_out + (size_t)r * W;
+      int v[kPlanColumns / 32];
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
-        if (c + i >= keep) e[i] = c + i < end ? fresh(r, c + i - have) : -1;
-      *reinterpret_cast<int4*>(p.table_out + at) = v;
-    } else {
-      p.table_out[at] = c < keep ? p.table[at] : c < end ? fresh(r, c - have) : -1;
+      for (int i = 0; i < kPlanColumns / 32; ++i) { const int c = c0 + 32 * i + lane; v[i] = c < keep ? from[c] : -1; }
+#pragma unroll
+      for (int i = 0; i < kPlanColumns / 32; ++i) {
+        const int c = c0 + 32 * i + lane;
+        if (c >= keep && c < end) v[i] = fresh(r, c - have);
+        if (c < W) to[c] = v[i];
+      }
     }
+    return;
   }
-  // rows of the packed batch
-  for (int i = gid; i < p.rows; i += threads) {
-    const int r = upper_bound(s_add, R, i);
-    int slot = -1, pos = -1;
-    if (r < R && admitted(r)) {
-      pos = max(p.lengths[r], 0) + i - before(s_add, r);
-      const int c = pos / P, have = have_of(r);
-      const int page = c < have ? p.table[(size_t)r * W + c] : fresh(r, c - have);
-      if (page >= 0) slot = page * P + (pos - c * P);
+  cta -= parts.tables;
+  if (cta < parts.rows) {
+    // rows of the packed batch
+    for (int i = cta * kPlanThreads + tid; i < p.rows; i += parts.rows * kPlanThreads) {
+      const int r = upper_bound(s_add, R, i);
+      int slot = -1, pos = -1;
+      if (r < R && admitted(r)) {
+        pos = s_len[r] + i - before(s_add, r);
+        const int c = pos / P, have = have_of(r);
+        const int page = c < have ? p.table[(size_t)r * W + c] : fresh(r, c - have);
+        if (page >= 0) slot = page * P + (pos - c * P);
+      }
+      p.slots[i] = slot;
+      p.positions[i] = pos;
     }
-    p.slots[i] = slot;
-    p.positions[i] = pos;
+    return;
   }
+  cta -= parts.rows;
   // pages that are taken: those of the admitted requests, which are the first ones that need any
-  __shared__ int s_given, s_long[kPlanThreads / 32];
-  if (tid == 0) s_given = 0;
-  __syncthreads();
   int given = 0;
   for (int r = r0; r < r1; ++r)
     if (admitted(r) && need_of(r) > 0) given = s_need[r];
   if (given) atomicMax(&s_given, given);
   __syncthreads();
   const int left = min(total - s_given, F);
-  for (int i = gid; i < F; i += threads) p.free_out[i] = i < left ? stack(i) : -1;
-  if (blockIdx.x == 0) {
-    int len_sum = 0;
-    for (int r = r0; r < r1; ++r) {
-      const int len = max(p.lengths[r], 0);
-      const int out = ended(r) ? 0 : admitted(r) ? len + s_add[r] - before(s_add, r) : len;
-      p.lengths_out[r] = out;
-      p.cu_new[r + 1] = s_add[r];
-      len_sum += out;
+  if (cta < parts.stack) {
+    const bool quads = ((reinterpret_cast<uintptr_t>(p.free_pages) | reinterpret_cast<uintptr_t>(p.free_out)) & 15) == 0;
+    for (int i = 4 * (cta * kPlanThreads + tid); i < F; i += 4 * parts.stack * kPlanThreads) {
+      if (quads && i + 4 <= F && (i >= left || i + 4 <= min(left, n_free))) {
+        *reinterpret_cast<int4*>(p.free_out + i) = i >= left ? make_int4(-1, -1, -1, -1) : *reinterpret_cast<const int4*>(p.free_pages + i);
+      } else {
+        for (int k = i; k < min(i + 4, F); ++k) p.free_out[k] = k < left ? stack(k) : -1;
+      }
     }
-    int x = len_sum;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) { const int y = __shfl_up_sync(0xffffffffu, x, o); if (lane >= o) x += y; }
-    if (lane == 31) s_long[warp] = x;
-    __syncthreads();
-    int run = x - len_sum;
-    for (int w = 0; w < warp; ++w) run += s_long[w];
-    for (int r = r0; r < r1; ++r) {
-      run += p.lengths_out[r];                          // (written by this thread)
-      p.cu_lengths[r + 1] = run;
-    }
-    if (tid == 0) { p.cu_new[0] = 0; p.cu_lengths[0] = 0; p.n_free_out[0] = left; }
+    return;
   }
+  // the requests' state
+  int len_sum = 0;
+  auto length_after = [&](int r) { return ended(r) ? 0 : admitted(r) ? s_len[r] + s_add[r] - before(s_add, r) : s_len[r]; };
+  for (int r = r0; r < r1; ++r) {
+    const int out = length_after(r);
+    p.lengths_out[r] = out;
+    p.cu_new[r + 1] = s_add[r];
+    len_sum += out;
+  }
+  int x = len_sum;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) { const int y = __shfl_up_sync(0xffffffffu, x, o); if (lane >= o) x += y; }
+  if (lane == 31) s_warp[0][warp] = x;
+  __syncthreads();
+  int run = x - len_sum;
+  for (int w = 0; w < warp; ++w) run += s_warp[0][w];
+  for (int r = r0; r < r1; ++r) {
+    run += length_after(r);
+    p.cu_lengths[r + 1] = run;
+  }
+  if (tid == 0) { p.cu_new[0] = 0; p.cu_lengths[0] = 0; p.n_free_out[0] = left; }
 }
 
 // ---- store -----------------------------------------------------------------------------------------------------------------
@@ -458,14 +471,13 @@ extern "C" int hyperattn_cache_plan(const hyperattn_plan* p) {
       !p->cu_new || !p->cu_lengths || !p->lengths_out || !p->table_out || !p->n_free_out)
     return HYPERATTN_INVALID_ARGUMENT;
   if (p->lengths_out == p->lengths || p->table_out == p->table || (p->num_free && p->free_out == p->free_pages) || p->n_free_out == p->n_free) return HYPERATTN_MISALIGNED;
-  const int smem = 4 * p->requests * (int)sizeof(int);
+  const int smem = 5 * p->requests * (int)sizeof(int);
   if (smem > 40 * 1024)
-    if (int rc = status_of(allow_smem<plan_kernel>(4 * HYPERATTN_PLAN_MAX_REQUESTS * (int)sizeof(int)), "plan: shared memory")) return rc;
-  const long long work = (long long)p->requests * p->table_width / 4 + p->rows + p->num_free / 4;
-  long long grid = (work + 2 * kPlanThreads - 1) / (2 * kPlanThreads);
-  if (grid > 2 * kSms) grid = 2 * kSms;
-  if (grid < 1) grid = 1;
-  return status_of(launch(plan_kernel, dim3((unsigned)grid), dim3(kPlanThreads), smem, reinterpret_cast<cudaStream_t>(p->stream), *p), "plan");
+    if (int rc = status_of(allow_smem<plan_kernel>(5 * HYPERATTN_PLAN_MAX_REQUESTS * (int)sizeof(int)), "plan: shared memory")) return rc;
+  auto ctas = [](long long work, int per, int most) { return (int)(work <= 0 ? 0 : (work + per - 1) / per < most ? (work + per - 1) / per : most); };
+  const PlanParts parts = {ctas((long long)p->requests * ((p->table_width + kPlanColumns - 1) / kPlanColumns), kPlanWarps, 2 * kSms), ctas(p->rows, kPlanThreads, kSms / 2),
+                           ctas(p->num_free, 8 * kPlanThreads, kSms)};
+  return status_of(launch(plan_kernel, dim3((unsigned)(parts.tables + parts.rows + parts.stack + 1)), dim3(kPlanThreads), smem, reinterpret_cast<cudaStream_t>(p->stream), *p, parts), "plan");
 }
 
 extern "C" int hyperattn_cache_store(const hyperattn_cache* cache, const void* k, const void* v, int dtype, int rows, long long k_row_stride,

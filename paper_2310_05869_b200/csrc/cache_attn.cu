@@ -79,7 +79,7 @@ struct Heads {
   float scale[NT][2];                   // to the base-2 scores
   float minus[NT][2], sum[NT][2];       // minus the reference (kNoReference: none yet); sum of this lane's tokens
   float o[NT][D / 16][4];               // O^T without the minima: coordinates lane / 4 (times 2^-24) and lane / 4 + 8 (times 2^-20) of every 16
-  float om[NT][4];                      // sum of weights times minima of group lane / 4
+  float om[NT][2];                      // sum of weights times minima of group lane / 4
 };
 
 template <int D, int NT, class T>
@@ -131,7 +131,7 @@ __device__ __forceinline__ void load_heads(Heads<D, NT>& h, const CacheAttnArgs&
     const float2 hf = to_float2<__half>(high);
     h.sums[t] = none ? 0u : low ? from_float2<__half>(x0 - hf.x, x1 - hf.y) : high;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) h.om[t][i] = 0.f;
+    for (int i = 0; i < 2; ++i) h.om[t][i] = 0.f;
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
       h.scale[t][i] = __shfl_sync(0xffffffffu, scale, 8 * c + 4 * i);
@@ -206,61 +206,86 @@ __device__ __forceinline__ void scores_of(const Heads<D, NT>& h, const uint8_t* 
   }
 }
 
-// O^T += V^T P^T of one block, P^T (and what rounding it to fp16 has lost) as operands: the codes with the weights times the scales, the minima with the weights.
-template <int D, int NT, bool FINE>
-__device__ __forceinline__ void add_values(Heads<D, NT>& h, const uint8_t* block, int valid, const uint32_t (&p)[NT][2], const uint32_t (&rest)[NT][2]) {
+// O^T += V^T P^T of NB blocks, P^T (and what rounding it to fp16 has lost) as operands: the codes with the weights times the scales, the minima with the weights.
+// The products of the blocks are summed from zero and then added to O: the tensor cores' sums are cut, not rounded, and both parts of O are many times
+// as large as what they add up to in a long context (131072 tokens in one chain of products a warp: results off by 0.7 %; like this 0.03 %).
+template <int D, int NT, int NB, bool FINE>
+__device__ __forceinline__ void add_values(Heads<D, NT>& h, const uint8_t* block, const int (&valid)[NB], const uint32_t (&p)[NB][NT][2], const uint32_t (&rest)[NB][NT][2]) {
   constexpr int G = D / kGroup;
   const int lane = threadIdx.x & 31, c = lane & 3;
-  uint32_t sv[2][G], mv[2];                              // scales of tokens (2 c, 2 c + 1), (8 + 2 c, 9 + 2 c); minima of those of group lane / 4
+  uint32_t sv[NB][2][G], mv[NB][2];                      // scales of tokens (2 c, 2 c + 1), (8 + 2 c, 9 + 2 c); minima of those of group lane / 4
 #pragma unroll
-  for (int half = 0; half < 2; ++half) {
-#pragma unroll
-    for (int i = 0; i < G / 2; ++i) {
-      const uint4 v = *reinterpret_cast<const uint4*>(block + Block<D>::kScaleV + (half * 4 + c) * G * 8 + i * 16);
-      sv[half][2 * i] = v.x; sv[half][2 * i + 1] = v.z;
-    }
-    mv[half] = *reinterpret_cast<const uint32_t*>(block + Block<D>::kScaleV + ((half * 4 + c) * G + lane / 4 % G) * 8 + 4);
-  }
-  if (valid < kBlockTokens) {                            // whatever the rest of the block holds: zeros
+  for (int b = 0; b < NB; ++b) {
+    const uint8_t* scales = block + b * Block<D>::kBytes + Block<D>::kScaleV;
 #pragma unroll
     for (int half = 0; half < 2; ++half) {
-      const uint32_t keep = (half * 8 + 2 * c < valid ? 0xffffu : 0u) | (half * 8 + 2 * c + 1 < valid ? 0xffff0000u : 0u);
 #pragma unroll
-      for (int i = 0; i < G; ++i) sv[half][i] &= keep;
-      mv[half] &= keep;
+      for (int i = 0; i < G / 2; ++i) {
+        const uint4 v = *reinterpret_cast<const uint4*>(scales + (half * 4 + c) * G * 8 + i * 16);
+        sv[b][half][2 * i] = v.x; sv[b][half][2 * i + 1] = v.z;
+      }
+      mv[b][half] = *reinterpret_cast<const uint32_t*>(scales + ((half * 4 + c) * G + lane / 4 % G) * 8 + 4);
+    }
+    if (valid[b] < kBlockTokens) {                       // whatever the rest of the block holds: zeros
+#pragma unroll
+      for (int half = 0; half < 2; ++half) {
+        const uint32_t keep = (half * 8 + 2 * c < valid[b] ? 0xffffu : 0u) | (half * 8 + 2 * c + 1 < valid[b] ? 0xffff0000u : 0u);
+#pragma unroll
+        for (int i = 0; i < G; ++i) sv[b][half][i] &= keep;
+        mv[b][half] &= keep;
+      }
     }
   }
+  auto add = [](float (&to)[4], const float (&x)[4]) {
+#pragma unroll
+    for (int i = 0; i < 4; i += 2) unpack_f2(fadd2(pack_f2(to[i], to[i + 1]), pack_f2(x[i], x[i + 1])), to[i], to[i + 1]);
+  };
 #pragma unroll
   for (int t = 0; t < NT; ++t) {
-    mma_f16(h.om[t], mv[0], 0u, mv[1], 0u, p[t][0], p[t][1]);
-    if constexpr (FINE) mma_f16(h.om[t], mv[0], 0u, mv[1], 0u, rest[t][0], rest[t][1]);
+    float m[4];
+#pragma unroll
+    for (int b = 0; b < NB; ++b) {
+      if (b == 0) mma_f16_first(m, mv[b][0], 0u, mv[b][1], 0u, p[b][t][0], p[b][t][1]);
+      else mma_f16(m, mv[b][0], 0u, mv[b][1], 0u, p[b][t][0], p[b][t][1]);
+      if constexpr (FINE) mma_f16(m, mv[b][0], 0u, mv[b][1], 0u, rest[b][t][0], rest[b][t][1]);
+    }
+    unpack_f2(fadd2(pack_f2(h.om[t][0], h.om[t][1]), pack_f2(m[0], m[1])), h.om[t][0], h.om[t][1]);
   }
-  uint32_t ps[NT][2], pr[NT][2];                         // weights times scales of a group, and what rounding them has lost
+  uint32_t ps[NB][NT][2], pr[NB][NT][2];                 // weights times scales of a group, and what rounding them has lost
 #pragma unroll
   for (int i = 0; i < D / 64; ++i) {
-    const uint4 v = *reinterpret_cast<const uint4*>(block + Block<D>::kV + i * 512 + lane * 16);
-    const uint32_t vw[4] = {v.x, v.y, v.z, v.w};
+    uint32_t vw[NB][4];
+#pragma unroll
+    for (int b = 0; b < NB; ++b) {
+      const uint4 v = *reinterpret_cast<const uint4*>(block + b * Block<D>::kBytes + Block<D>::kV + i * 512 + lane * 16);
+      vw[b][0] = v.x; vw[b][1] = v.y; vw[b][2] = v.z; vw[b][3] = v.w;
+    }
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       const int u = 4 * i + j, w = u / 2;
-      if (j % 2 == 0) {
+      float x[NT][4];
 #pragma unroll
-        for (int t = 0; t < NT; ++t)
+      for (int b = 0; b < NB; ++b) {
+        uint32_t k[4];
+        codes_of(vw[b][j], k);
 #pragma unroll
-          for (int half = 0; half < 2; ++half) {
-            const __half2 sc = h2(sv[half][w]), prod = __hmul2(h2(p[t][half]), sc);
-            ps[t][half] = u32(prod);
-            const __half2 lost = __hfma2(h2(p[t][half]), sc, __hneg2(prod));
-            pr[t][half] = u32(FINE ? __hfma2(h2(rest[t][half]), sc, lost) : lost);
+        for (int t = 0; t < NT; ++t) {
+          if (j % 2 == 0) {
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+              const __half2 sc = h2(sv[b][half][w]), prod = __hmul2(h2(p[b][t][half]), sc);
+              ps[b][t][half] = u32(prod);
+              const __half2 lost = __hfma2(h2(p[b][t][half]), sc, __hneg2(prod));
+              pr[b][t][half] = u32(FINE ? __hfma2(h2(rest[b][t][half]), sc, lost) : lost);
+            }
           }
+          if (b == 0) mma_f16_first(x[t], k[0], k[1], k[2], k[3], ps[b][t][0], ps[b][t][1]);
+          else mma_f16(x[t], k[0], k[1], k[2], k[3], ps[b][t][0], ps[b][t][1]);
+          mma_f16(x[t], k[0], k[1], k[2], k[3], pr[b][t][0], pr[b][t][1]);
+        }
       }
-      uint32_t k[4];
-      codes_of(vw[j], k);
 #pragma unroll
-      for (int t = 0; t < NT; ++t) {
-        mma_f16(h.o[t][u], k[0], k[1], k[2], k[3], ps[t][0], ps[t][1]);
-        mma_f16(h.o[t][u], k[0], k[1], k[2], k[3], pr[t][0], pr[t][1]);
-      }
+      for (int t = 0; t < NT; ++t) add(h.o[t][u], x[t]);
     }
   }
 }
@@ -333,8 +358,7 @@ __device__ __forceinline__ void attend_blocks(Heads<D, NT>& h, const uint8_t* bl
         }
       }
     }
-#pragma unroll
-  for (int b = 0; b < NB; ++b) add_values<D, NT, FINE>(h, block + b * Block<D>::kBytes, valid[b], p[b], rest[b]);
+  add_values<D, NT, NB, FINE>(h, block, valid, p, rest);
 }
 
 __device__ __forceinline__ void put(void* out, int kind, size_t at, float x) {

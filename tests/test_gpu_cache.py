@@ -235,6 +235,26 @@ def test_cache_attention_long_contexts_and_few_requests():
         _check(q, lens, K, V, out.cpu().numpy(), lse.cpu().numpy())
 
 
+@pytest.mark.parametrize("d,dtype", [(64, "fp16"), (128, "bf16")])
+def test_cache_attention_of_a_long_context_relative_to_its_result(d, dtype):
+    """A result over 100000 tokens is a few hundred times smaller than what it is summed from (scales times codes, and minima): errors are held to
+    the result.  Weights rounded to fp16 (bf16 queries) are 2^-11 each, independent of each other; everything else has to stay below that."""
+    gen = torch.Generator("cuda").manual_seed(3)
+    T, H, page = 100_003, 2, 64
+    pages = -(-T // page)
+    cache = ha.cache_pages(pages, H, d, page)
+    k, v = (torch.randn(T, H, d, generator=gen, device="cuda").to(DT[dtype]) for _ in range(2))
+    q = torch.randn(1, 2 * H, d, generator=gen, device="cuda").to(DT[dtype])
+    ha.cache_store(cache, k, v, torch.arange(T, dtype=torch.int32, device="cuda"))
+    table = torch.arange(pages, dtype=torch.int32, device="cuda")[None]
+    K, V = (x.double() for x in ha.cache_read(cache, table, ints([0, T]), T, dtype=torch.float32))
+    out, _ = ha.cache_attention(q, cache, table, ints([T]), out_dtype=torch.float32)
+    for h in range(2 * H):
+        p = torch.softmax(K[:, h // 2] @ q[0, h].double() / d ** 0.5, 0)
+        want = p @ V[:, h // 2]
+        assert (out[0, h] - want).norm() <= 2.0 ** -11 * want.norm(), (h, float((out[0, h] - want).norm() / want.norm()))
+
+
 def test_cache_attention_many_short_requests():
     rng = np.random.default_rng(8)
     lens = rng.integers(0, 90, 777).tolist()
