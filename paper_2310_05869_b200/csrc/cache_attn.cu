@@ -415,7 +415,7 @@ __global__ void __launch_bounds__(32 * kWarps, ctas_by_registers(NT)) cache_attn
   // ---- running sum of the requests' units ----
   const int per = (a.requests + 32 * kWarps - 1) / (32 * kWarps), r0 = min(a.requests, tid * per), r1 = min(a.requests, r0 + per);
   int mine = 0;
-  for (int r = r0; r < r1; ++r) mine += units_of<D>(a, r);
+  for (int r = r0; r < r1; ++r) { s_starts[r] = mine; mine += units_of<D>(a, r); }
   int run = mine;
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) { const int y = __shfl_up_sync(0xffffffffu, run, o); if (lane >= o) run += y; }
@@ -423,8 +423,8 @@ __global__ void __launch_bounds__(32 * kWarps, ctas_by_registers(NT)) cache_attn
   __syncthreads();
   run -= mine;
   for (int w = 0; w < warp; ++w) run += s_sums[w];
-  for (int r = r0; r < r1; ++r) { s_starts[r] = run; run += units_of<D>(a, r); }
-  if (tid == 32 * kWarps - 1) s_starts[a.requests] = run;
+  for (int r = r0; r < r1; ++r) s_starts[r] += run;
+  if (tid == 32 * kWarps - 1) s_starts[a.requests] = run + mine;
   __syncthreads();
   const int segs = a.cache.heads * a.chunks;                             // of a request
   const int total = s_starts[a.requests] * segs, warps = gridDim.x * kWarps, part = max(1, (total + warps - 1) / warps);
@@ -484,11 +484,22 @@ __global__ void __launch_bounds__(32 * kWarps, ctas_by_registers(NT)) cache_attn
     }
     ++asked;
   };
-  if (count > 0) { look(0); know(0); }
-  while (asked < R::kStages && asked < count) ask();
   bool ok = true;
   Heads<D, NT> h;
   int segment = -1, request = 0, seg = 0;                                // segment = request * segs + seg
+  auto take_segment = [&](int sg) {
+    segment = sg;
+    request = segment / segs; seg = segment - request * segs;
+    const int kv = seg / a.chunks, chunk = seg - kv * a.chunks;
+    load_heads<D, NT, T>(h, a, request, kv * per_kv + chunk * 8 * NT, min(per_kv - chunk * 8 * NT, 8 * NT));
+  };
+  if (count > 0) {
+    look(0);
+    __syncwarp();
+    take_segment(s_known[0].x);                                          // (beside the table's and the lengths' loads)
+    know(0);
+  }
+  while (asked < R::kStages && asked < count) ask();
   // the segment's results, or a piece of them
   auto flush = [&](float* to) {                                            // to: null for final results
     const int chunk = seg % a.chunks, kv = seg / a.chunks, first_head = kv * per_kv + chunk * 8 * NT, heads = min(per_kv - chunk * 8 * NT, 8 * NT);
@@ -529,12 +540,7 @@ __global__ void __launch_bounds__(32 * kWarps, ctas_by_registers(NT)) cache_attn
     if (n % kBatch == kBatch / 2 && n + kBatch / 2 < count) know(n + kBatch / 2);
     const int4 unit = s_known[n % (2 * kBatch) * U];
     const int sg = unit.x, left = unit.y, there = unit.w >> 16;
-    if (sg != segment) {
-      segment = sg;
-      request = segment / segs; seg = segment - request * segs;
-      const int kv = seg / a.chunks, chunk = seg - kv * a.chunks;
-      load_heads<D, NT, T>(h, a, request, kv * per_kv + chunk * 8 * NT, min(per_kv - chunk * 8 * NT, 8 * NT));
-    }
+    if (sg != segment) take_segment(sg);
     const int st = n % R::kStages;
     ok = warp_wait<12>(bars + 8 * st, (uint32_t)(n / R::kStages) & 1, s_abort, status);
     if (!ok) break;
