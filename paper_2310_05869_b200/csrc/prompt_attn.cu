@@ -16,6 +16,7 @@
 //
 // Warp roles (384 threads): 0-3 and 4-7 softmax and results of query tile 0 and 1, 8 issues the products (and allocates TMEM), 9 loads, 10 prepares items.
 // Every wait is bounded: a CTA that gives up raises the device status word, drains its copies, frees its TMEM and returns.
+#include <climits>
 #include <cstdio>
 #include <type_traits>
 #include "serving.cuh"
@@ -112,7 +113,8 @@ struct Item {
   int kv;
 };
 
-// Item `index`, decoded by a converged warp.  Items are ordered by request, in it from the last query on (the longest first), key heads next to each other.
+// Item `index`, decoded by a converged warp.  Items are ordered by request - of every 32 requests the one with most keys first - and in it from the last
+// query on, so that the longest come first and little is left over at the end; key heads are next to each other.
 __device__ __forceinline__ Item item_at(const PromptArgs& a, int index, int tile_tokens) {
   const int lane = threadIdx.x & 31;
   Item it = {};
@@ -122,8 +124,20 @@ __device__ __forceinline__ Item item_at(const PromptArgs& a, int index, int tile
   it.kv = index - block * a.kv_heads;
   int before = 0;
   for (int r0 = 0; r0 < a.requests; r0 += 32) {
-    const int r = r0 + lane;
+    int r = r0 + lane;
     int q0 = 0, nq = 0;
+    if (a.requests > 1) {
+      const int keys = r < a.requests ? a.cu_k[r + 1] - a.cu_k[r] : INT_MIN;
+      int rank = 0, from = 0;
+#pragma unroll
+      for (int k = 0; k < 32; ++k) {
+        const int other = __shfl_sync(0xffffffffu, keys, k);
+        rank += other > keys || (other == keys && k < lane);
+      }
+#pragma unroll
+      for (int k = 0; k < 32; ++k) from = __shfl_sync(0xffffffffu, rank, k) == lane ? k : from;
+      r = r0 + from;
+    }
     if (r < a.requests) {
       q0 = min(max(a.cu_q[r], 0), a.q_rows);
       nq = min(max(a.cu_q[r + 1], q0), a.q_rows) - q0;
@@ -138,7 +152,7 @@ __device__ __forceinline__ Item item_at(const PromptArgs& a, int index, int tile
       const int first = before + __shfl_sync(0xffffffffu, sum - mine, src), blocks = __shfl_sync(0xffffffffu, mine, src);
       q0 = __shfl_sync(0xffffffffu, q0, src);
       nq = __shfl_sync(0xffffffffu, nq, src);
-      const int req = r0 + src, tok = (blocks - 1 - (block - first)) * pair_tokens;
+      const int req = __shfl_sync(0xffffffffu, r, src), tok = (blocks - 1 - (block - first)) * pair_tokens;
       const int k0 = min(max(a.cu_k[req], 0), a.k_rows);
       it.end = 0;
       it.key0 = k0;
