@@ -323,7 +323,10 @@ int hyperattn_alpha_workspace_bytes(int B, int H, int n, int n_k, size_t* bytes)
  * grouped: q_heads is a multiple of kv_heads, query head h reads key head h / (q_heads / kv_heads).  d in {64, 128}.
  * dtype is HYPERATTN_BF16 or HYPERATTN_FP16 (queries, keys, values), out_dtype the same or HYPERATTN_FP32.  Lengths,
  * offsets, tables and slots are device arrays of int32, read by the kernels: no entry point looks at them on the host,
- * synchronises or allocates, so every call can be captured in a graph.  Calls without rows return at once.
+ * synchronises or allocates, so every call can be captured in a graph (the two attentions after one call outside a capture, or
+ * any other call of the library: the first one on a device makes the status word, HYPERATTN_WORKSPACE_TOO_SMALL in a capture).
+ * Their waits on the device are bounded like those of hyperattn_forward: hyperattn_last_device_status.  Calls without rows
+ * return at once.
  *
  * The cache: pages of page_tokens tokens (a multiple of 16, at most 1024), uint8 [num_pages, kv_heads,
  * page_tokens / 16, 20 d].  A block of 20 d bytes holds K and V of 16 tokens of one head.  Every row of d numbers is

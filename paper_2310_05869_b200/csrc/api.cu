@@ -23,7 +23,7 @@ cudaError_t launch_backward(const AttnArgs& a, const void* out, int out_fp32, co
 
 namespace {
 
-constexpr int kVersion = 2;
+constexpr int kVersion = 3;
 constexpr size_t kAlign = 256;
 
 size_t align_up(size_t x) { return (x + kAlign - 1) / kAlign * kAlign; }

@@ -1,6 +1,7 @@
 """Binding of the serving entry points: exact attention over packed prompts, and a paged cache that holds keys and values in
 4 bits, with its scheduling.  Argument marshalling only, like `binding.py`; lengths, tables and slots are int32 CUDA tensors
-that only the kernels read, so nothing here waits for the GPU.
+that only the kernels read, so nothing here waits for the GPU.  `stream`: the handle of a stream to enqueue on instead of torch's current one
+(which the caller orders with it).
 
 A cache is a uint8 tensor [pages, kv_heads, page_tokens / 16, 20 d] (`cache_pages` makes one; include/hyperattn.h has the order of
 its bytes).  A decode step of a server:
@@ -92,6 +93,14 @@ def _stream(index, stream):
     return torch._C._cuda_getCurrentRawStream(index) if stream is None else stream
 
 
+def _used(stream, device, *tensors):
+    """Tensors that a call on a stream of the caller's uses and this module has made or may let go: the allocator waits for that stream."""
+    if stream is not None:
+        other = torch.cuda.ExternalStream(stream, device=device)
+        for t in tensors:
+            t.record_stream(other)
+
+
 def _new(shape, dtype, device):
     """torch.empty of one to three axes (which takes longer to find out that the strides are these)."""
     if len(shape) == 3:
@@ -173,6 +182,7 @@ def cache_plan(lengths, new, table, free, n_free, page_tokens, rows, stream=None
         lengths.data_ptr(), new.data_ptr(), table.data_ptr(), free.data_ptr(), n_free.data_ptr(), R, W, F, page_tokens, rows,
         at, at + 4 * rows, at + 8 * rows, at + 4 * (2 * rows + R + 1), at + 4 * (2 * rows + 2 * R + 2), table_out.data_ptr(),
         free_out.data_ptr(), at + 4 * (2 * rows + 3 * R + 2), _stream(index, stream)))
+    _used(stream, small.device, small, table_out, free_out)
     slots, positions, cu_new, cu_len, lengths_out, n_free_out = torch.unsafe_split_with_sizes(small, (rows, rows, R + 1, R + 1, R, 1))
     return CachePlan(slots, positions, cu_new, cu_len, lengths_out, table_out, free_out, n_free_out)
 
@@ -190,6 +200,7 @@ def cache_store(cache, k, v, slots, stream=None):
     v, v_row, v_head = _rows(v)
     _call("hyperattn_cache_store", index, _cache_bytes(*c), k.data_ptr(), v.data_ptr(), _code(k.dtype, "k"), k.shape[0], k_row, k_head, v_row, v_head,
           slots.data_ptr(), _stream(index, stream))
+    _used(stream, cache.device, k, v)
 
 
 def cache_read(cache, table, cu, rows, first=None, dtype=torch.bfloat16, stream=None):
@@ -209,6 +220,7 @@ def cache_read(cache, table, cu, rows, first=None, dtype=torch.bfloat16, stream=
     v = torch.empty_like(k)
     _call("hyperattn_cache_read", index, _cache_bytes(*c), table.data_ptr(), R, W, cu.data_ptr(), None if first is None else first.data_ptr(), rows,
           k.data_ptr(), v.data_ptr(), _code(dtype, "the result"), _stream(index, stream))
+    _used(stream, cache.device, k, v)
     return k, v
 
 
@@ -247,6 +259,7 @@ def cache_attention(q, cache, table, lengths, scale=0.0, out_dtype=None, stream=
     _call("hyperattn_cache_attention", index, _attention_bytes(
         *c, q.data_ptr(), row, head, out.data_ptr(), lse.data_ptr(), table.data_ptr(), lengths.data_ptr(), R, W, H, dtype, out_code, scale,
         work.data_ptr(), size, _stream(index, stream)))
+    _used(stream, device, q, out, lse, work)
     return out, lse
 
 
@@ -279,4 +292,5 @@ def prompt_attention(q, k, v, cu_q, cu_k=None, causal=True, scale=0.0, out_dtype
     _call("hyperattn_prompt_attention", index, _prompt_bytes(
         q.data_ptr(), k.data_ptr(), v.data_ptr(), q_row, q_head, k_row, k_head, v_row, v_head, out.data_ptr(), lse.data_ptr(), cu_q.data_ptr(),
         cu_k.data_ptr(), cu_q.shape[0] - 1, T, k_rows, H, kv_heads, d, 1 if causal else 0, dtype, out_code, scale, _stream(index, stream)))
+    _used(stream, device, q, k, v, out, lse)
     return out, lse

@@ -332,6 +332,9 @@ def test_strided_queries_another_stream_and_a_graph():
         got = ha.cache_attention(q, cache, t, n)
     torch.cuda.current_stream().wait_stream(side)
     assert all(torch.equal(a, b) for a, b in zip(want, got))
+    got = ha.cache_attention(q, cache, t, n, stream=side.cuda_stream)
+    side.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(want, got))
     # a captured decode step: lengths change between replays
     lengths, new = ints([100, 31, 0, 514]), ints([1, 1, 1, 1])
     free, n_free = ints([cache.shape[0] - 1]), ints([1])

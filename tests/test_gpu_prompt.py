@@ -156,6 +156,25 @@ def test_what_a_query_does_not_see_has_no_influence(d, G):
         assert not torch.isfinite(out[60:100, :G]).any()
 
 
+def test_no_keys_at_all():
+    q, k, v = inputs(8, [5, 130], [0, 0], 4, 2, 128, "bf16")
+    out, lse = ha.prompt_attention(q, k, v, offsets([5, 130]), offsets([0, 0]))
+    assert not out.any() and torch.isinf(lse).all() and (lse < 0).all()
+    out, lse = ha.prompt_attention(q[:0], k, v, offsets([0, 0]), offsets([0, 0]))
+    assert out.shape == (0, 4, 128) and lse.shape == (0, 4)
+
+
+def test_offsets_that_do_not_fit_the_tensors():
+    """Offsets beyond the rows that there are, or that go back, read and write nothing outside."""
+    q, k, v = inputs(9, [40], [40], 2, 2, 64, "bf16")
+    guard = [x.clone() for x in (q, k, v)]
+    for cu_q, cu_k in (([0, 90], [0, 40]), ([0, 40], [0, 500]), ([-7, 40], [-9, 40]), ([0, 30, 10, 40], [0, 20, 5, 40])):
+        out, lse = ha.prompt_attention(q, k, v, ints(cu_q), ints(cu_k))
+        assert out.shape == q.shape
+    assert all(torch.equal(a, b) for a, b in zip(guard, (q, k, v)))
+    assert ha.last_device_status() == 0
+
+
 def test_rows_beyond_the_last_request_are_not_written():
     q, k, v = inputs(7, [70], [70], 2, 1, 64, "bf16")
     v[50:] = float("nan")
@@ -185,6 +204,10 @@ def test_views_streams_and_a_graph():
     torch.cuda.current_stream().wait_stream(side)
     assert all(torch.equal(x, y) for x, y in zip(want, got))
     cu = offsets(n)
+    side.wait_stream(torch.cuda.current_stream())
+    got = ha.prompt_attention(q, k, v, cu, stream=side.cuda_stream)
+    side.synchronize()
+    assert all(torch.equal(x, y) for x, y in zip(want, got))
     ha.prompt_attention(q, k, v, cu)
     graph = torch.cuda.CUDAGraph()
     torch.cuda.synchronize()
