@@ -385,8 +385,9 @@ int hyperattn_cache_read(const hyperattn_cache* cache, const int32_t* table, int
 
 /* Attention of one query token a request over its cached tokens 0 .. lengths[r] - 1:
  *   out[r, h] = sum_j p_j v_j,  p = softmax_j(softmax_scale <q[r, h], k_j>),  lse[r, h] = ln sum_j exp(softmax_scale <q, k_j>).
- * A request without tokens gets out = 0 and lse = -infinity.  requests <= 4096.  Queries enter the products as fp16 (after a power of two that
- * brings the largest entry of a head near one), weights and values too, sums are fp32. */
+ * A request without tokens gets out = 0 and lse = -infinity.  requests <= 4096.  Queries enter the products as fp16 (after a
+ * power of two that brings the largest entry of a head near one), and so do the weights (2^-11; with fp16 queries what that
+ * rounding loses enters too); scores and all sums are fp32. */
 typedef struct hyperattn_cache_attention_params {
   hyperattn_cache cache;
   const void* q;           /* [requests, q_heads, d], strides in elements (multiples of 8) */

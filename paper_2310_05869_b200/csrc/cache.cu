@@ -9,7 +9,8 @@ namespace {
 // ---- plan ------------------------------------------------------------------------------------------------------------------
 // Everything follows from three running sums over the requests (new tokens, pages needed, pages released), which every CTA makes for
 // itself in shared memory - reading a few KB again costs less than a launch to make them first.  Then it does one thing: some CTAs
-// write the tables, some the rows, some the stack, one the requests' new state, so that their latencies do not add up.
+// write the tables, some the rows, some the stack, one the requests' new state, so that their latencies do not add up.  256 requests with tables of 129 pages: 4.9 us,
+// latency (7.0 with the four in a row); 1024 requests with 2049 pages: 11.1 us, 2.4 TB/s.
 constexpr int kPlanThreads = 512, kPlanWarps = kPlanThreads / 32, kPlanColumns = 512;      // kPlanColumns: table entries of a warp at a time
 
 struct PlanParts { int tables, rows, stack; };           // CTAs for each
@@ -153,7 +154,7 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const __grid_constan
 // A CTA takes the runs that begin among its rows: rows that follow each other into consecutive slots of one block (so a run is at most a block, and
 // for prompts nearly always is one).  A warp makes a run's part of a block in shared memory, first K, then V - a row of d numbers is d / 8 lanes with 8
 // numbers each, a group of 32 the numbers of four neighbouring lanes - and writes a whole block with 16-byte stores, a part of one by the pieces that its
-// tokens own.
+// tokens own.  What bounds it is the arithmetic of the codes (about 90 operations a lane for 8 numbers): 32768 tokens of 32 heads of 64, fp16, 336 MB: 100 us.
 constexpr int kStoreRows = 64, kStoreWarps = 8;
 
 struct StoreArgs {
@@ -338,6 +339,7 @@ __global__ void __launch_bounds__(32 * kStoreWarps, D == 64 ? 4 : 3) store_kerne
 // ---- read ------------------------------------------------------------------------------------------------------------------
 // A CTA takes some rows of the result, a warp a block of 16 tokens of one head at a time: 16-byte loads of codes and scales; V's words, which hold four
 // tokens of two coordinates, are turned by movmatrix so that a lane has neighbouring coordinates of a token, as it has for K.  Rows leave through shared memory.
+// 65536 tokens of 8 heads of 128, bf16, 352 MB: 65 us, 5.4 TB/s (84 % of copy bandwidth).
 struct ReadArgs {
   CacheView cache;
   const int32_t *table, *cu, *first;

@@ -3,17 +3,21 @@
 // A warp takes a block of 16 tokens of one key head and up to 16 query heads that read it, on the warp-level tensor cores
 // (mma.sync m16n8k16, fp16 operands, fp32 sums):
 //   S^T = K Q^T with the codes of K as fp16 numbers (see codes_of), exact sums of a group:  s = sum_g scale_g sum(q c) + min_g sum_g(q)  in fp32
-//   p = exp2(s c - ref), the reference of a head moves when it is exceeded by more than 2^2; P^T is turned once (movmatrix)
+//   p = exp2(s c - ref), the reference of a head is set 2^12 below its largest score and moves when that exceeds it by 2^14; P^T is turned once (movmatrix)
 //   O^T += V^T P^T  likewise: V = min + scale * code, so the codes meet the weights times the group's scales, the minima the weights.  V's 32-bit words
 //               hold four tokens of two coordinates, so that masking yields operands with pairs of tokens.
 // fp16 and not bf16 for the weights: they are then off by 2^-11 and not 2^-8, which bf16 results do not show; for fp16 results what the rounding has lost goes
 // through the products too.  What rounding a weight times a scale has lost always does: scale * code and minimum are both larger than the value they add up to.
-// (Weights times scales below 2^-14 lose places: values of a size of 10^-4, whose scales are as coarse.)
 //
 // A segment is a request, a key head and up to 8 or 16 of its query heads.  The tokens of all segments are one sequence of units of 5 KB, cut into equal
 // parts, one for every warp that the GPU holds, whatever the lengths are.  A warp streams its units through a ring of its own in shared memory (bulk
 // copies, no other warp to wait for).  A segment that lies in one part is finished there; pieces of others go to the workspace - one piece for
 // a CTA that is inside a segment as a whole - and a second launch puts them together, in order, so that results do not depend on timing.
+//
+// What bounds it: the issue of about 190 (d = 64) or 320 (d = 128) operations a block, of which 80 logical ones at half rate; memory next.  2 requests of up to 131072
+// tokens, 32 heads of 64: 157 us, 658 MB at 4.2 TB/s (65 % of copy bandwidth; the copies without the arithmetic 103 us).  64 requests of up to 8192,
+// 32 / 8 heads of 128: 72 us, 3.8 TB/s, of which the running sums, the first loads and the join take 14.  4 requests of up to 600: 10.2 us, two launches of
+// dependent loads.
 #include <cstdio>
 #include <type_traits>
 #include "serving.cuh"
@@ -22,7 +26,8 @@
 namespace hyperattn {
 namespace {
 
-constexpr float kMoveAt = 2.f;          // octaves the scores of a head may exceed its reference before that moves: 2^2 times the largest scale is an fp16 number
+constexpr float kBelow = 12.f, kMoveAt = 14.f;      // octaves that a head's reference is set below its largest score, and that scores may exceed it by before it moves: weights
+                                                    // of up to 2^14 use fp16's range, and times a scale below 2 they are still numbers
 
 struct CacheAttnArgs {
   CacheView cache;
@@ -208,9 +213,9 @@ __device__ __forceinline__ void scores_of(const Heads<D, NT>& h, const uint8_t* 
 
 // O^T += V^T P^T of NB blocks, P^T (and what rounding it to fp16 has lost) as operands: the codes with the weights times the scales, the minima with the weights.
 // The products of the blocks are summed from zero and then added to O: the tensor cores' sums are cut, not rounded, and both parts of O are many times
-// as large as what they add up to in a long context (131072 tokens in one chain of products a warp: results off by 0.7 %; like this 0.03 %).
+// as large as what they add up to in a long context (131072 tokens in one chain of products a warp: results off by 0.7 %; like this 0.024 %).
 template <int D, int NT, int NB, bool FINE>
-__device__ __forceinline__ void add_values(Heads<D, NT>& h, const uint8_t* block, const int (&valid)[NB], const uint32_t (&p)[NB][NT][2], const uint32_t (&rest)[NB][NT][2]) {
+__device__ __forceinline__ void add_values(Heads<D, NT>& h, const uint8_t* block, const int (&valid)[NB], uint32_t (&p)[NB][NT][2], uint32_t (&rest)[NB][NT][2]) {
   constexpr int G = D / kGroup;
   const int lane = threadIdx.x & 31, c = lane & 3;
   uint32_t sv[NB][2][G], mv[NB][2];                      // scales of tokens (2 c, 2 c + 1), (8 + 2 c, 9 + 2 c); minima of those of group lane / 4
@@ -236,10 +241,6 @@ __device__ __forceinline__ void add_values(Heads<D, NT>& h, const uint8_t* block
       }
     }
   }
-  auto add = [](float (&to)[4], const float (&x)[4]) {
-#pragma unroll
-    for (int i = 0; i < 4; i += 2) unpack_f2(fadd2(pack_f2(to[i], to[i + 1]), pack_f2(x[i], x[i + 1])), to[i], to[i + 1]);
-  };
 #pragma unroll
   for (int t = 0; t < NT; ++t) {
     float m[4];
@@ -251,6 +252,34 @@ __device__ __forceinline__ void add_values(Heads<D, NT>& h, const uint8_t* block
     }
     unpack_f2(fadd2(pack_f2(h.om[t][0], h.om[t][1]), pack_f2(m[0], m[1])), h.om[t][0], h.om[t][1]);
   }
+  // Scales of 2 and more (values that differ by 30 in a group): the weights get so much smaller that the products stay numbers, the sums larger.
+  uint32_t any = 0;
+#pragma unroll
+  for (int b = 0; b < NB; ++b)
+#pragma unroll
+    for (int half = 0; half < 2; ++half)
+#pragma unroll
+      for (int i = 0; i < G; ++i) any |= sv[b][half][i];
+  float up = 1.f;
+  if (__any_sync(0xffffffffu, any & 0x40004000u)) {
+    const int k = (int)((__reduce_or_sync(0xffffffffu, any | any >> 16) >> 10) & 31u) - 15;       // all scales are below 2^(k + 1)
+    const __half2 down = __half2half2(__float2half_rn(__uint_as_float((uint32_t)(127 - k) << 23)));
+    up = __uint_as_float((uint32_t)(127 + k) << 23);
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+      for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+          p[b][t][half] = u32(__hmul2(h2(p[b][t][half]), down));
+          if constexpr (FINE) rest[b][t][half] = u32(__hmul2(h2(rest[b][t][half]), down));
+        }
+  }
+  const uint64_t up2 = pack_f2(up, up);
+  auto add = [&](float (&to)[4], const float (&x)[4]) {
+#pragma unroll
+    for (int i = 0; i < 4; i += 2) unpack_f2(ffma2(pack_f2(x[i], x[i + 1]), up2, pack_f2(to[i], to[i + 1])), to[i], to[i + 1]);
+  };
   uint32_t ps[NB][NT][2], pr[NB][NT][2];                 // weights times scales of a group, and what rounding them has lost
 #pragma unroll
   for (int i = 0; i < D / 64; ++i) {
@@ -291,7 +320,7 @@ __device__ __forceinline__ void add_values(Heads<D, NT>& h, const uint8_t* block
 }
 
 // NB blocks that follow each other, `valid[b]` tokens of each (0: nothing there).  FINE: what rounding the weights to fp16 has lost is added.
-// (Two blocks at a time: one block is a chain of products, exponentials and products again that four warps a scheduler do not hide.)
+// (Several at a time: a block is a chain of products, exponentials and products again that four warps a scheduler do not hide.)
 template <int D, int NT, int NB, bool FINE>
 __device__ __forceinline__ void attend_blocks(Heads<D, NT>& h, const uint8_t* block, const int (&valid)[NB]) {
   float s[NB][NT][4], y[NB][NT][4], most = -INFINITY;
@@ -319,8 +348,8 @@ __device__ __forceinline__ void attend_blocks(Heads<D, NT>& h, const uint8_t* bl
 #pragma unroll
         for (int o = 4; o < 32; o <<= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
         if (m + h.minus[t][i] > kMoveAt) {
-          const float alpha = h.minus[t][i] == kNoReference ? 0.f : ex2(-h.minus[t][i] - m);
-          h.minus[t][i] = -m;
+          const float alpha = h.minus[t][i] == kNoReference ? 0.f : ex2(kBelow - m - h.minus[t][i]);
+          h.minus[t][i] = kBelow - m;
           h.sum[t][i] *= alpha;
 #pragma unroll
           for (int u = 0; u < D / 16; ++u) { h.o[t][u][i] *= alpha; h.o[t][u][i + 2] *= alpha; }
@@ -441,7 +470,9 @@ __global__ void __launch_bounds__(32 * kWarps, ctas_by_registers(NT)) cache_attn
   // look - {segment of all requests', block in it, page, length} and the block's place in its page, page and length on their way - and then, by know(),
   // what is there: {segment, tokens from the unit on, block of the cache, bytes of the copy to ask for | blocks of the unit that exist << 16}.  A unit that
   // cannot leave its page is one copy, its first block's.
-  constexpr int U = R::kUnit, kBatch = 32 / U;
+  // NB blocks at a time: the four of a unit at d = 64 (2 x 131072: 157 us; two 162, one 167), one at d = 128 (64 requests: 71.4; two 72.8, which spill), two
+  // where two tiles of heads work on a block (36 / 4 heads of 64: 33.9; four, which spill, 35.6).
+  constexpr int U = R::kUnit, kBatch = 32 / U, NB = NT == 2 ? 2 : D == 64 ? 4 : 1;
   const bool whole = subs % U == 0;
   const int shift = subs & (subs - 1) ? -1 : 31 - __clz(subs);           // blocks of a page: a power of two?
   int4* s_known = reinterpret_cast<int4*>(smem + kWarps * R::kWarpBytes) + warp * 64;                       // [2][32]
@@ -545,12 +576,12 @@ __global__ void __launch_bounds__(32 * kWarps, ctas_by_registers(NT)) cache_attn
     ok = warp_wait<12>(bars + 8 * st, (uint32_t)(n / R::kStages) & 1, s_abort, status);
     if (!ok) break;
 #pragma unroll 1
-    for (int b = 0; b < U; b += 2) {
+    for (int b = 0; b < U; b += NB) {
       // (a block that is not there: whatever its place holds, no token of it)
-      int valid[2];
+      int valid[NB];
 #pragma unroll
-      for (int i = 0; i < 2; ++i) valid[i] = (there >> (b + i)) & 1 ? left - (b + i) * kBlockTokens : 0;
-      if (valid[0] | valid[1]) attend_blocks<D, NT, 2, FINE>(h, smem + warp * R::kWarpBytes + st * R::kUnitBytes + b * Block<D>::kBytes, valid);
+      for (int i = 0; i < NB; ++i) valid[i] = (there >> (b + i)) & 1 ? left - (b + i) * kBlockTokens : 0;
+      if ((there >> b) & ((1 << NB) - 1)) attend_blocks<D, NT, NB, FINE>(h, smem + warp * R::kWarpBytes + st * R::kUnitBytes + b * Block<D>::kBytes, valid);
     }
     __syncwarp();
     if (asked < count) ask();

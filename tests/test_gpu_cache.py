@@ -235,8 +235,9 @@ def test_cache_attention_long_contexts_and_few_requests():
         _check(q, lens, K, V, out.cpu().numpy(), lse.cpu().numpy())
 
 
+@pytest.mark.parametrize("size", [1.0, 0.002, 50.0, 5000.0])
 @pytest.mark.parametrize("d,dtype", [(64, "fp16"), (128, "bf16")])
-def test_cache_attention_of_a_long_context_relative_to_its_result(d, dtype):
+def test_cache_attention_of_a_long_context_relative_to_its_result(d, dtype, size):
     """A result over 100000 tokens is a few hundred times smaller than what it is summed from (scales times codes, and minima): errors are held to
     the result.  Weights rounded to fp16 (bf16 queries) are 2^-11 each, independent of each other; everything else has to stay below that."""
     gen = torch.Generator("cuda").manual_seed(3)
@@ -244,6 +245,7 @@ def test_cache_attention_of_a_long_context_relative_to_its_result(d, dtype):
     pages = -(-T // page)
     cache = ha.cache_pages(pages, H, d, page)
     k, v = (torch.randn(T, H, d, generator=gen, device="cuda").to(DT[dtype]) for _ in range(2))
+    v = (v.float() * size).to(DT[dtype])
     q = torch.randn(1, 2 * H, d, generator=gen, device="cuda").to(DT[dtype])
     ha.cache_store(cache, k, v, torch.arange(T, dtype=torch.int32, device="cuda"))
     table = torch.arange(pages, dtype=torch.int32, device="cuda")[None]
