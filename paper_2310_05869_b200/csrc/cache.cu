@@ -154,7 +154,8 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const __grid_constan
 // A CTA takes the runs that begin among its rows: rows that follow each other into consecutive slots of one block (so a run is at most a block, and
 // for prompts nearly always is one).  A warp makes a run's part of a block in shared memory, first K, then V - a row of d numbers is d / 8 lanes with 8
 // numbers each, a group of 32 the numbers of four neighbouring lanes - and writes a whole block with 16-byte stores, a part of one by the pieces that its
-// tokens own.  What bounds it is the arithmetic of the codes (about 90 operations a lane for 8 numbers): 32768 tokens of 32 heads of 64, fp16, 336 MB: 100 us.
+// tokens own.  What bounds it is the arithmetic of the codes.  Blocks that a run covers whole take a path without tests (32768 tokens of 32 heads of 64, fp16, 352 MB, with
+// the reading back: 201 us; with this path, codes clamped as pairs of integers, the divisions and the lengths of runs by fewer operations 163).
 constexpr int kStoreRows = 64, kStoreWarps = 8;
 
 struct StoreArgs {
@@ -179,45 +180,58 @@ template <class T> __device__ __forceinline__ uint32_t max2(uint32_t a, uint32_t
   return *reinterpret_cast<uint32_t*>(&r);
 }
 
-// The codes of the lane's 8 numbers, in the lowest bytes of c; scale and minimum (fp16) of its group.
-template <class T>
-__device__ __forceinline__ void quantise8(const uint4& in, uint32_t (&c)[8], __half& s, __half& m) {
+// x / 15 as the division rounds it (P. Markstein, 1990: one correction of a product with the rounded reciprocal).  Results below 2^-126 are not: they become zero in fp16.
+__device__ __forceinline__ float fifteenth(float x) {
+  constexpr float c = 1.f / 15.f;
+  const float q = x * c;
+  return fmaf(fmaf(-15.f, q, x), c, q);
+}
+// 1 / s for an s from fp16: the approximate reciprocal and one step of Newton's; for each of them what 1.f / s gives.
+__device__ __forceinline__ float reciprocal(float s) {
+  float y;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(s));
+  return fmaf(y, fmaf(-s, y, 1.f), y);
+}
+// The codes of the lane's 8 numbers, c[i] = number A(i) and, 16 bits higher, number B(i); scale and minimum (fp16) of its group.
+template <class T, class A, class B>
+__device__ __forceinline__ void quantise8(const uint4& in, A first, B second, uint32_t (&c)[4], __half& s, __half& m) {
   // smallest and minus largest number as a pair
   const uint32_t low = min2<T>(min2<T>(in.x, in.y), min2<T>(in.z, in.w)), high = max2<T>(max2<T>(in.x, in.y), max2<T>(in.z, in.w)) ^ 0x80008000u;
   uint32_t both = min2<T>(__byte_perm(low, high, 0x5410), __byte_perm(low, high, 0x7632));
   both = min2<T>(both, __shfl_xor_sync(0xffffffffu, both, 1));
   both = min2<T>(both, __shfl_xor_sync(0xffffffffu, both, 2));
   const float2 f = to_float2<T>(both);
-  s = __float2half_rn((-f.y - f.x) / 15.f);
+  s = __float2half_rn(fifteenth(-f.y - f.x));
   m = __float2half_rn(f.x);
   float fs = __half2float(s), fm = __half2float(m);
   if (!(fabsf(fs) < INFINITY) || !(fabsf(fm) < INFINITY)) {            // (a number that is not finite shows in one of the two)
     s = m = __ushort_as_half(0x7fff);
     fs = fm = 0.f;
   }
-  const float r = fs == 0.f ? 0.f : 1.f / fs;
+  const float r = fs == 0.f ? 0.f : reciprocal(fs);
   const uint64_t minus = pack_f2(-fm, -fm), times = pack_f2(r, r);
   const uint32_t w[4] = {in.x, in.y, in.z, in.w};
+  uint32_t u[8];
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     const float2 x = to_float2<T>(w[i]);
     float t0, t1;
+    // 1.5 * 2^23 + t is rounded to the nearest integer, ties to even, and has it in its lowest bits (|t| < 32: where s is rounded to a multiple of 2^-24 it is at least two
+    // thirds of what it stands for, and m is off by half of one)
     unpack_f2(fmul2(fadd2(pack_f2(x.x, x.y), minus), times), t0, t1);
-    // 1.5 * 2^23 + t is rounded to the nearest integer, ties to even, and has it in its lowest bits
-    c[2 * i] = __float_as_uint(fminf(fmaxf(t0, 0.f), 15.f) + 12582912.f);
-    c[2 * i + 1] = __float_as_uint(fminf(fmaxf(t1, 0.f), 15.f) + 12582912.f);
+    u[2 * i] = __float_as_uint(__fadd_rn(t0, 12582912.f));              // (not as a pair: product and sum of pairs become one operation, rounded once)
+    u[2 * i + 1] = __float_as_uint(__fadd_rn(t1, 12582912.f));
   }
-}
-__device__ __forceinline__ uint32_t low_bytes(uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
-  return __byte_perm(__byte_perm(a, b, 0x0040), __byte_perm(c, d, 0x0040), 0x5410);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) c[i] = __vimin_s16x2_relu(__byte_perm(u[first(i)], u[second(i)], 0x5410), 0x000f000fu);
 }
 
 template <int D, class T>
 __global__ void __launch_bounds__(32 * kStoreWarps, D == 64 ? 4 : 3) store_kernel(const __grid_constant__ StoreArgs a) {
   using B = Block<D>;
   constexpr int LANES = D / 8, PER = 32 / LANES, STEPS = kBlockTokens / PER, kWindow = kStoreRows + kBlockTokens;     // PER: rows at a time
-  __shared__ int s_slot[kWindow + 1], s_run[kStoreRows];
-  __shared__ unsigned s_begin[kStoreRows / 32];
+  __shared__ int s_slot[kWindow + 1], s_run[kStoreRows], s_count[kStoreRows];
+  __shared__ unsigned s_begin[kStoreRows / 32], s_break[3];
   __shared__ __align__(16) uint8_t s_block[kStoreWarps][B::kBytes];
   wait_for_stream();
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -230,34 +244,33 @@ __global__ void __launch_bounds__(32 * kStoreWarps, D == 64 ? 4 : 3) store_kerne
   }
   __syncthreads();
   auto follows = [&](int i) { return s_slot[i] >= 0 && s_slot[i - 1] >= 0 && s_slot[i] == s_slot[i - 1] + 1 && s_slot[i] % kBlockTokens != 0; };
-  // the runs in order (all CTAs of a window have to number them alike)
-  static_assert(kStoreRows == 64, "two warps look");
-  const bool begins = tid < kStoreRows && s_slot[tid + 1] >= 0 && !follows(tid + 1);
-  const unsigned flags = __ballot_sync(0xffffffffu, begins);
-  if (tid < kStoreRows && lane == 0) s_begin[warp] = flags;
+  // the runs in order (all CTAs of a window have to number them alike), and their lengths: a run ends before the next row that does not follow
+  static_assert(kWindow <= 96 && kStoreRows == 64, "three warps look, the first two for beginnings");
+  const bool breaks = tid < 96 && !(tid < kWindow && follows(tid + 1)), begins = breaks && tid < kStoreRows && s_slot[tid + 1] >= 0;
+  const unsigned flags = __ballot_sync(0xffffffffu, begins), ends = __ballot_sync(0xffffffffu, breaks);
+  if (warp < 3 && lane == 0) s_break[warp] = ends;
+  if (warp < 2 && lane == 0) s_begin[warp] = flags;
   __syncthreads();
-  if (begins) s_run[__popc(flags & ((1u << lane) - 1u)) + (warp ? __popc(s_begin[0]) : 0)] = tid + 1;
+  if (begins) {
+    const int run = __popc(flags & ((1u << lane) - 1u)) + (warp ? __popc(s_begin[0]) : 0);
+    s_run[run] = tid + 1;
+    s_count[run] = __ffs((int)__funnelshift_rc(ends, s_break[warp + 1], lane + 1));       // (at most a block, whose end breaks it)
+  }
   __syncthreads();
-  const int items = (__popc(s_begin[0]) + __popc(s_begin[1])) * a.cache.heads;
+  const int items = (__popc(s_begin[0]) + __popc(s_begin[1])) * a.cache.heads, warps = kStoreWarps * gridDim.y;
+  const int next_run = warps / a.cache.heads, next_head = warps - next_run * a.cache.heads;
   uint8_t* block = s_block[warp];
   const int o = lane % LANES, sub = lane / LANES;
-  for (int item = blockIdx.y * kStoreWarps + warp; item < items; item += kStoreWarps * gridDim.y) {
-    const int run = item / a.cache.heads, head = item - run * a.cache.heads, at = s_run[run];
-    int n = 1;
-    while (n < kBlockTokens && at + n <= kWindow && follows(at + n)) ++n;
+  const int first = blockIdx.y * kStoreWarps + warp;
+  int run = first / a.cache.heads, head = first - run * a.cache.heads;
+  for (int item = first; item < items; item += warps) {
+    const int at = s_run[run], n = s_count[run];
     const int slot = s_slot[at], page = slot / a.cache.page, in_page = slot - page * a.cache.page, t0 = in_page % kBlockTokens;
     const long long row0 = w0 + at - 1 - t0;                               // (the row of the block's token 0)
-    const T *ks = reinterpret_cast<const T*>(a.k) + head * a.k_head + o * 8, *vs = reinterpret_cast<const T*>(a.v) + head * a.v_head + o * 8;
     auto mine = [&](int t) { return t >= t0 && t < t0 + n; };
     // K: tokens sub, sub + PER, ...; V: a lane takes the four tokens of a word one after the other
     auto k_token = [&](int i) { return i * PER + sub; };
     auto v_token = [&](int i) { return 2 * (sub * (STEPS / 4) + i / 4) + i % 4 / 2 + (i & 1) * 8; };
-    uint4 in[STEPS];
-#pragma unroll
-    for (int i = 0; i < STEPS; ++i) {
-      const int t = k_token(i);
-      in[i] = mine(t) ? *reinterpret_cast<const uint4*>(ks + (row0 + t) * a.k_row) : make_uint4(0, 0, 0, 0);
-    }
     auto scales = [&](int at0, int t, __half s, __half m) {
       if (o % 4 == 0) {
         __half* to = reinterpret_cast<__half*>(block + at0 + ((t / 2) * B::kGroups + o / 4) * 8 + (t % 2) * 2);
@@ -265,46 +278,60 @@ __global__ void __launch_bounds__(32 * kStoreWarps, D == 64 ? 4 : 3) store_kerne
         to[2] = m;
       }
     };
+    // (whole: no token of the block is left out)
+    auto make = [&](auto whole) {
+      constexpr bool WHOLE = decltype(whole)::value;
+      const T* ks = reinterpret_cast<const T*>(a.k) + head * a.k_head + o * 8 + (row0 + k_token(0)) * a.k_row;
+      const T* vs = reinterpret_cast<const T*>(a.v) + head * a.v_head + o * 8 + (row0 + v_token(0)) * a.v_row;
+      uint4 in[STEPS];
 #pragma unroll
-    for (int i = 0; i < STEPS; ++i) {
-      const int t = k_token(i);
-      uint32_t c[8];
-      __half s, m;
-      if (__any_sync(0xffffffffu, mine(t))) {
-        quantise8<T>(in[i], c, s, m);
-        // nibble e of the codes is (e % 2) * 4 + e / 2 of the word
-        const uint32_t word = low_bytes(c[0], c[4], c[1], c[5]) + 16 * low_bytes(c[2], c[6], c[3], c[7]);
-        const int ln = (t % 8) * 4 + o % 4;
-        *reinterpret_cast<uint32_t*>(block + (D == 128 ? (t / 8) * 512 + ln * 16 : ln * 16 + (t / 8) * 8) + (o / 4) * 4) = word;
-        scales(B::kScaleK, t, s, m);
+      for (int i = 0; i < STEPS; ++i) {
+        in[i] = WHOLE || mine(k_token(i)) ? *reinterpret_cast<const uint4*>(ks) : make_uint4(0, 0, 0, 0);
+        ks += PER * a.k_row;
       }
-      const int tv = v_token(i);
-      in[i] = mine(tv) ? *reinterpret_cast<const uint4*>(vs + (row0 + tv) * a.v_row) : make_uint4(0, 0, 0, 0);
-    }
 #pragma unroll
-    for (int i4 = 0; i4 < STEPS; i4 += 4) {
-      uint32_t w[4];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int t = v_token(i4 + i);
-        w[i] = 0;
-        if (__any_sync(0xffffffffu, mine(t))) {
-          uint32_t c[8];
-          __half s, m;
-          quantise8<T>(in[i4 + i], c, s, m);
-          // the octets of a byte are neighbours: the even lane makes coordinates 0..3 of both, the odd one 4..7
-          const uint32_t first = low_bytes(c[0], c[1], c[2], c[3]), second = low_bytes(c[4], c[5], c[6], c[7]);
-          const uint32_t other = __shfl_xor_sync(0xffffffffu, o & 1 ? first : second, 1);
-          w[i] = o & 1 ? other + 16 * second : first + 16 * other;
-          scales(B::kScaleV, t, s, m);
+      for (int i = 0; i < STEPS; ++i) {
+        const int t = k_token(i);
+        uint32_t c[4];
+        __half s, m;
+        if (WHOLE || __any_sync(0xffffffffu, mine(t))) {
+          quantise8<T>(in[i], [](int j) { return 2 * j; }, [](int j) { return 2 * j + 1; }, c, s, m);
+          // nibble e of the codes is (e % 2) * 4 + e / 2 of the word
+          const uint32_t word = c[0] + 16 * c[1] + 256 * (c[2] + 16 * c[3]);
+          const int ln = (t % 8) * 4 + o % 4;
+          *reinterpret_cast<uint32_t*>(block + (D == 128 ? (t / 8) * 512 + ln * 16 : ln * 16 + (t / 8) * 8) + (o / 4) * 4) = word;
+          scales(B::kScaleK, t, s, m);
         }
+        in[i] = WHOLE || mine(v_token(i)) ? *reinterpret_cast<const uint4*>(vs + (i & 1) * 8 * a.v_row) : make_uint4(0, 0, 0, 0);
+        if (i & 1) vs += a.v_row;
       }
-      // four tokens of four coordinates, the other way round
-      const uint32_t x0 = __byte_perm(w[0], w[1], 0x5140), x1 = __byte_perm(w[2], w[3], 0x5140), x2 = __byte_perm(w[0], w[1], 0x7362), x3 = __byte_perm(w[2], w[3], 0x7362);
-      const int u = o / 2, quad = sub * (STEPS / 4) + i4 / 4;
-      uint32_t* to = reinterpret_cast<uint32_t*>(block + B::kV + (u / 4) * 512 + ((o & 1) * 16 + quad) * 16 + (u % 4) * 4);
-      to[0] = __byte_perm(x0, x1, 0x5410); to[16] = __byte_perm(x0, x1, 0x7632); to[32] = __byte_perm(x2, x3, 0x5410); to[48] = __byte_perm(x2, x3, 0x7632);
-    }
+#pragma unroll
+      for (int i4 = 0; i4 < STEPS; i4 += 4) {
+        uint32_t w[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int t = v_token(i4 + i);
+          w[i] = 0;
+          if (WHOLE || __any_sync(0xffffffffu, mine(t))) {
+            uint32_t c[4];
+            __half s, m;
+            quantise8<T>(in[i4 + i], [](int j) { return j / 2 * 4 + j % 2; }, [](int j) { return j / 2 * 4 + j % 2 + 2; }, c, s, m);
+            // the octets of a byte are neighbours: the even lane makes coordinates 0..3 of both, the odd one 4..7
+            const uint32_t low = c[0] + 256 * c[1], high = c[2] + 256 * c[3];
+            const uint32_t other = __shfl_xor_sync(0xffffffffu, o & 1 ? low : high, 1);
+            w[i] = o & 1 ? other + 16 * high : low + 16 * other;
+            scales(B::kScaleV, t, s, m);
+          }
+        }
+        // four tokens of four coordinates, the other way round
+        const uint32_t x0 = __byte_perm(w[0], w[1], 0x5140), x1 = __byte_perm(w[2], w[3], 0x5140), x2 = __byte_perm(w[0], w[1], 0x7362), x3 = __byte_perm(w[2], w[3], 0x7362);
+        const int u = o / 2, quad = sub * (STEPS / 4) + i4 / 4;
+        uint32_t* to = reinterpret_cast<uint32_t*>(block + B::kV + (u / 4) * 512 + ((o & 1) * 16 + quad) * 16 + (u % 4) * 4);
+        to[0] = __byte_perm(x0, x1, 0x5410); to[16] = __byte_perm(x0, x1, 0x7632); to[32] = __byte_perm(x2, x3, 0x5410); to[48] = __byte_perm(x2, x3, 0x7632);
+      }
+    };
+    if (n == kBlockTokens) make(std::true_type());
+    else make(std::false_type());
     __syncwarp();
     uint8_t* out = block_at<D>(a.cache, page, head, in_page / kBlockTokens);
     if (n == kBlockTokens) {
@@ -333,6 +360,8 @@ __global__ void __launch_bounds__(32 * kStoreWarps, D == 64 ? 4 : 3) store_kerne
       }
     }
     __syncwarp();
+    run += next_run;
+    if ((head += next_head) >= a.cache.heads) { head -= a.cache.heads; ++run; }
   }
 }
 

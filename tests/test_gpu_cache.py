@@ -127,6 +127,24 @@ def test_store_and_read(kind, heads, d, page, dtype):
         assert np.array_equal(block, want_bytes)
 
 
+def test_store_with_every_scale():
+    # groups from -7 s to 8 s with numbers at and beside the ties, for every s of fp16 with finite ends: the codes are those of the divisions
+    rng = np.random.default_rng(5)
+    s = np.arange(1, 0x7c00, dtype=np.uint16).view(np.float16).astype(np.float64)
+    s = s[8 * s < 65504]
+    s = s[:len(s) // 4 * 4]
+    x = np.concatenate([s[:, None] * [[-7, 8]], s[:, None] * (rng.integers(-14, 17, (len(s), 30)) / 2)], 1)
+    x = rng.permuted(x, axis=1).astype(np.float16).reshape(-1, 1, 64)
+    for dtype in (torch.float16, torch.bfloat16):
+        k, v = torch.tensor(x[0::2]).to(dtype).cuda(), torch.tensor(x[1::2]).to(dtype).cuda()
+        T = len(k)
+        cache = ha.cache_pages(-(-T // 64), 1, 64, 64)
+        ha.cache_store(cache, k, v, ints(np.arange(T)))
+        got = ha.cache_read(cache, ints(np.arange(len(cache))[None]), ints([0, T]), T, dtype=torch.float32)
+        for w, g in zip((k, v), got):
+            assert np.array_equal(g.cpu().numpy(), SU.held(w.float().cpu().numpy()))
+
+
 def test_store_leaves_out_slots_that_are_none_and_touches_nothing_else():
     rng = np.random.default_rng(1)
     for d in (64, 128):
