@@ -155,7 +155,8 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const __grid_constan
 // for prompts nearly always is one).  A warp makes a run's part of a block in shared memory, first K, then V - a row of d numbers is d / 8 lanes with 8
 // numbers each, a group of 32 the numbers of four neighbouring lanes - and writes a whole block with 16-byte stores, a part of one by the pieces that its
 // tokens own.  What bounds it is the arithmetic of the codes.  Blocks that a run covers whole take a path without tests (32768 tokens of 32 heads of 64, fp16, 352 MB, with
-// the reading back: 201 us; with this path, codes clamped as pairs of integers, the divisions and the lengths of runs by fewer operations 163).
+// the reading back: 201 us; with this path, codes clamped as pairs of integers, the divisions and the lengths of runs by fewer operations 163;
+// K rows of the next item asked for beside V 153, where those in registers made it slower, 175, and V's as well no faster, 154).
 constexpr int kStoreRows = 64, kStoreWarps = 8;
 
 struct StoreArgs {
@@ -263,6 +264,20 @@ __global__ void __launch_bounds__(32 * kStoreWarps, D == 64 ? 4 : 3) store_kerne
   const int o = lane % LANES, sub = lane / LANES;
   const int first = blockIdx.y * kStoreWarps + warp;
   int run = first / a.cache.heads, head = first - run * a.cache.heads;
+  // The K rows of an item come while the item before is at its V, each lane's into places that it alone reads (zeros for rows that are not the run's).
+  extern __shared__ __align__(16) uint8_t s_next[];
+  uint8_t* const next = s_next + (warp * STEPS * 32 + lane) * 16;
+  auto ask_k = [&](int r, int h) {
+    const int at = s_run[r], t0 = s_slot[at] % kBlockTokens, t1 = t0 + s_count[r];               // (a page is whole blocks)
+    const T* from = reinterpret_cast<const T*>(a.k) + h * a.k_head + o * 8 + (w0 + at - 1 - t0 + sub) * a.k_row;
+#pragma unroll
+    for (int i = 0; i < STEPS; ++i, from += PER * a.k_row) {
+      const int t = i * PER + sub;
+      const bool in = t >= t0 && t < t1;
+      asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(smem_u32(next + i * 512)), "l"(in ? from : reinterpret_cast<const T*>(a.k)), "r"(in ? 16 : 0) : "memory");
+    }
+  };
+  if (first < items) ask_k(run, head);
   for (int item = first; item < items; item += warps) {
     const int at = s_run[run], n = s_count[run];
     const int slot = s_slot[at], page = slot / a.cache.page, in_page = slot - page * a.cache.page, t0 = in_page % kBlockTokens;
@@ -278,24 +293,21 @@ __global__ void __launch_bounds__(32 * kStoreWarps, D == 64 ? 4 : 3) store_kerne
         to[2] = m;
       }
     };
+    int then_run = run + next_run, then_head = head + next_head;
+    if (then_head >= a.cache.heads) { then_head -= a.cache.heads; ++then_run; }
     // (whole: no token of the block is left out)
     auto make = [&](auto whole) {
       constexpr bool WHOLE = decltype(whole)::value;
-      const T* ks = reinterpret_cast<const T*>(a.k) + head * a.k_head + o * 8 + (row0 + k_token(0)) * a.k_row;
       const T* vs = reinterpret_cast<const T*>(a.v) + head * a.v_head + o * 8 + (row0 + v_token(0)) * a.v_row;
       uint4 in[STEPS];
-#pragma unroll
-      for (int i = 0; i < STEPS; ++i) {
-        in[i] = WHOLE || mine(k_token(i)) ? *reinterpret_cast<const uint4*>(ks) : make_uint4(0, 0, 0, 0);
-        ks += PER * a.k_row;
-      }
+      asm volatile("cp.async.wait_all;" ::: "memory");
 #pragma unroll
       for (int i = 0; i < STEPS; ++i) {
         const int t = k_token(i);
         uint32_t c[4];
         __half s, m;
         if (WHOLE || __any_sync(0xffffffffu, mine(t))) {
-          quantise8<T>(in[i], [](int j) { return 2 * j; }, [](int j) { return 2 * j + 1; }, c, s, m);
+          quantise8<T>(*reinterpret_cast<const uint4*>(next + i * 512), [](int j) { return 2 * j; }, [](int j) { return 2 * j + 1; }, c, s, m);
           // nibble e of the codes is (e % 2) * 4 + e / 2 of the word
           const uint32_t word = c[0] + 16 * c[1] + 256 * (c[2] + 16 * c[3]);
           const int ln = (t % 8) * 4 + o % 4;
@@ -305,6 +317,7 @@ __global__ void __launch_bounds__(32 * kStoreWarps, D == 64 ? 4 : 3) store_kerne
         in[i] = WHOLE || mine(v_token(i)) ? *reinterpret_cast<const uint4*>(vs + (i & 1) * 8 * a.v_row) : make_uint4(0, 0, 0, 0);
         if (i & 1) vs += a.v_row;
       }
+      if (item + warps < items) ask_k(then_run, then_head);
 #pragma unroll
       for (int i4 = 0; i4 < STEPS; i4 += 4) {
         uint32_t w[4];
@@ -360,8 +373,8 @@ __global__ void __launch_bounds__(32 * kStoreWarps, D == 64 ? 4 : 3) store_kerne
       }
     }
     __syncwarp();
-    run += next_run;
-    if ((head += next_head) >= a.cache.heads) { head -= a.cache.heads; ++run; }
+    run = then_run;
+    head = then_head;
   }
 }
 
@@ -524,13 +537,19 @@ extern "C" int hyperattn_cache_store(const hyperattn_cache* cache, const void* k
   const StoreArgs a = {view_of(*cache), k, v, k_row_stride, k_head_stride, v_row_stride, v_head_stride, rows, slots};
   const cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
   // The heads of a window over several CTAs, until there are a few rounds of them: 32768 tokens of 32 heads (d = 64) with twice as many CTAs as SMs at least
-  // 181 us, six times 114, twelve times 100, 24 times 99; the kernel needs the registers of four CTAs an SM (d = 128: three).
+  // twice as long, eight and twelve times 153 us with the reading back, 24 times 156; the kernel needs the registers of four CTAs an SM (d = 128: three; d = 64 with five: 160).
   const int windows = (rows + kStoreRows - 1) / kStoreRows, most = (kStoreRows * cache->kv_heads + kStoreWarps - 1) / kStoreWarps;
   int split = (12 * kSms + windows - 1) / windows;
   if (split > most) split = most;
-  auto go = [&](auto kernel) { return status_of(launch(kernel, dim3((unsigned)windows, (unsigned)split), dim3(32 * kStoreWarps), 0, st, a), "store"); };
-  if (cache->d == 64) return dtype == HYPERATTN_BF16 ? go(store_kernel<64, __nv_bfloat16>) : go(store_kernel<64, __half>);
-  return dtype == HYPERATTN_BF16 ? go(store_kernel<128, __nv_bfloat16>) : go(store_kernel<128, __half>);
+  const int smem = kStoreWarps * kBlockTokens * cache->d * 2;
+  auto go = [&](auto dim, auto type) {
+    constexpr auto kernel = store_kernel<decltype(dim)::value, decltype(type)>;
+    cudaError_t e = allow_smem<kernel>(smem);
+    if (e == cudaSuccess) e = launch(kernel, dim3((unsigned)windows, (unsigned)split), dim3(32 * kStoreWarps), smem, st, a);
+    return status_of(e, "store");
+  };
+  auto of_type = [&](auto dim) { return dtype == HYPERATTN_BF16 ? go(dim, __nv_bfloat16()) : go(dim, __half()); };
+  return cache->d == 64 ? of_type(std::integral_constant<int, 64>()) : of_type(std::integral_constant<int, 128>());
 }
 
 extern "C" int hyperattn_cache_read(const hyperattn_cache* cache, const int32_t* table, int requests, int table_width, const int32_t* cu,
