@@ -15,8 +15,8 @@
 // a CTA that is inside a segment as a whole - and a second launch puts them together, in order, so that results do not depend on timing.
 //
 // What bounds it: the issue of about 190 (d = 64) or 320 (d = 128) operations a block, of which 80 logical ones at half rate; memory next.  2 requests of up to 131072
-// tokens, 32 heads of 64: 157 us, 658 MB at 4.2 TB/s (65 % of copy bandwidth; the copies without the arithmetic 103 us).  64 requests of up to 8192,
-// 32 / 8 heads of 128: 72 us, 3.8 TB/s, of which the running sums, the first loads and the join take 14.  4 requests of up to 600: 10.2 us, two launches of
+// tokens, 32 heads of 64: 150 us, 658 MB at 4.4 TB/s (68 % of copy bandwidth; the copies without the arithmetic 103 us).  64 requests of up to 8192,
+// 32 / 8 heads of 128: 66 us, 4.1 TB/s, of which the running sums, the first loads and the join take 14.  4 requests of up to 600: 10.2 us, two launches of
 // dependent loads.
 #include <cstdio>
 #include <type_traits>
@@ -87,13 +87,13 @@ struct Heads {
   float om[NT][2];                      // sum of weights times minima of group lane / 4
 };
 
-template <int D, int NT, class T>
+template <int D, int NT, bool PAIR, class T>
 __device__ __forceinline__ void load_heads(Heads<D, NT>& h, const CacheAttnArgs& a, int request, int first_head, int heads) {
   constexpr int G = Heads<D, NT>::kGroups;
   const int lane = threadIdx.x & 31, c = lane & 3;
 #pragma unroll
   for (int t = 0; t < NT; ++t) {
-    const int head = lane / 4 + 8 * t;
+    const int head = PAIR ? lane / 4 % 4 : lane / 4 + 8 * t;
     float top = 0.f;
     uint4 raw[G];
 #pragma unroll
@@ -214,10 +214,13 @@ __device__ __forceinline__ void scores_of(const Heads<D, NT>& h, const uint8_t* 
 // O^T += V^T P^T of NB blocks, P^T (and what rounding it to fp16 has lost) as operands: the codes with the weights times the scales, the minima with the weights.
 // The products of the blocks are summed from zero and then added to O: the tensor cores' sums are cut, not rounded, and both parts of O are many times
 // as large as what they add up to in a long context (131072 tokens in one chain of products a warp: results off by 0.7 %; like this 0.024 %).
-template <int D, int NT, int NB, bool FINE>
+// PAIR: up to four heads, twice.  Columns 4 .. 7 of the operand P^T have what the rounding of columns 0 .. 3 has lost, in the same product; the two are added at the
+// segment's end.  (2 x 131072 tokens, 32 / 32 heads of 64: 156 -> 150 us; 64 requests, 32 / 8 of 128: 71 -> 67.)
+template <int D, int NT, bool PAIR, int NB, bool FINE>
 __device__ __forceinline__ void add_values(Heads<D, NT>& h, const uint8_t* block, const int (&valid)[NB], uint32_t (&p)[NB][NT][2], uint32_t (&rest)[NB][NT][2]) {
   constexpr int G = D / kGroup;
   const int lane = threadIdx.x & 31, c = lane & 3;
+  const bool upper = lane >= 16;                         // (the lane's column of P^T is one of 4 .. 7)
   uint32_t sv[NB][2][G], mv[NB][2];                      // scales of tokens (2 c, 2 c + 1), (8 + 2 c, 9 + 2 c); minima of those of group lane / 4
 #pragma unroll
   for (int b = 0; b < NB; ++b) {
@@ -246,6 +249,12 @@ __device__ __forceinline__ void add_values(Heads<D, NT>& h, const uint8_t* block
     float m[4];
 #pragma unroll
     for (int b = 0; b < NB; ++b) {
+      if constexpr (PAIR) {
+        const uint32_t w0 = upper ? (FINE ? rest[b][t][0] : 0u) : p[b][t][0], w1 = upper ? (FINE ? rest[b][t][1] : 0u) : p[b][t][1];
+        if (b == 0) mma_f16_first(m, mv[b][0], 0u, mv[b][1], 0u, w0, w1);
+        else mma_f16(m, mv[b][0], 0u, mv[b][1], 0u, w0, w1);
+        continue;
+      }
       if (b == 0) mma_f16_first(m, mv[b][0], 0u, mv[b][1], 0u, p[b][t][0], p[b][t][1]);
       else mma_f16(m, mv[b][0], 0u, mv[b][1], 0u, p[b][t][0], p[b][t][1]);
       if constexpr (FINE) mma_f16(m, mv[b][0], 0u, mv[b][1], 0u, rest[b][t][0], rest[b][t][1]);
@@ -275,6 +284,18 @@ __device__ __forceinline__ void add_values(Heads<D, NT>& h, const uint8_t* block
           if constexpr (FINE) rest[b][t][half] = u32(__hmul2(h2(rest[b][t][half]), down));
         }
   }
+  uint32_t minus[NB][NT][2];                             // PAIR: minus the weights in columns 4 .. 7, so that p s + (minus s) is the product there rounded off, elsewhere the product
+  if constexpr (PAIR) {
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+      for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+          minus[b][t][half] = upper ? p[b][t][half] ^ 0x80008000u : 0u;
+          if constexpr (FINE) rest[b][t][half] = upper ? rest[b][t][half] : 0u;
+        }
+  }
   const uint64_t up2 = pack_f2(up, up);
   auto add = [&](float (&to)[4], const float (&x)[4]) {
 #pragma unroll
@@ -302,15 +323,18 @@ __device__ __forceinline__ void add_values(Heads<D, NT>& h, const uint8_t* block
           if (j % 2 == 0) {
 #pragma unroll
             for (int half = 0; half < 2; ++half) {
-              const __half2 sc = h2(sv[b][half][w]), prod = __hmul2(h2(p[b][t][half]), sc);
+              const __half2 sc = h2(sv[b][half][w]), prod = PAIR ? __hneg2(__hmul2(h2(minus[b][t][half]), sc)) : __hmul2(h2(p[b][t][half]), sc);
               ps[b][t][half] = u32(prod);
               const __half2 lost = __hfma2(h2(p[b][t][half]), sc, __hneg2(prod));
               pr[b][t][half] = u32(FINE ? __hfma2(h2(rest[b][t][half]), sc, lost) : lost);
             }
           }
-          if (b == 0) mma_f16_first(x[t], k[0], k[1], k[2], k[3], ps[b][t][0], ps[b][t][1]);
-          else mma_f16(x[t], k[0], k[1], k[2], k[3], ps[b][t][0], ps[b][t][1]);
-          mma_f16(x[t], k[0], k[1], k[2], k[3], pr[b][t][0], pr[b][t][1]);
+          if constexpr (!PAIR) {
+            if (b == 0) mma_f16_first(x[t], k[0], k[1], k[2], k[3], ps[b][t][0], ps[b][t][1]);
+            else mma_f16(x[t], k[0], k[1], k[2], k[3], ps[b][t][0], ps[b][t][1]);
+          }
+          if (PAIR && b == 0) mma_f16_first(x[t], k[0], k[1], k[2], k[3], pr[b][t][0], pr[b][t][1]);
+          else mma_f16(x[t], k[0], k[1], k[2], k[3], pr[b][t][0], pr[b][t][1]);
         }
       }
 #pragma unroll
@@ -321,7 +345,7 @@ __device__ __forceinline__ void add_values(Heads<D, NT>& h, const uint8_t* block
 
 // NB blocks that follow each other, `valid[b]` tokens of each (0: nothing there).  FINE: what rounding the weights to fp16 has lost is added.
 // (Several at a time: a block is a chain of products, exponentials and products again that four warps a scheduler do not hide.)
-template <int D, int NT, int NB, bool FINE>
+template <int D, int NT, bool PAIR, int NB, bool FINE>
 __device__ __forceinline__ void attend_blocks(Heads<D, NT>& h, const uint8_t* block, const int (&valid)[NB]) {
   float s[NB][NT][4], y[NB][NT][4], most = -INFINITY;
 #pragma unroll
@@ -387,7 +411,7 @@ __device__ __forceinline__ void attend_blocks(Heads<D, NT>& h, const uint8_t* bl
         }
       }
     }
-  add_values<D, NT, NB, FINE>(h, block, valid, p, rest);
+  add_values<D, NT, PAIR, NB, FINE>(h, block, valid, p, rest);
 }
 
 __device__ __forceinline__ void put(void* out, int kind, size_t at, float x) {
@@ -421,7 +445,7 @@ template <int D> __device__ __forceinline__ int units_of(const CacheAttnArgs& a,
 // where the pieces of a segment lie: see combine
 __device__ __forceinline__ float* piece_at(const CacheAttnArgs& a, long long slot, int head, int d) { return a.part + (slot * a.part_heads + head) * (d + 2); }
 
-template <int D, int NT, class T>
+template <int D, int NT, bool PAIR, class T>
 __global__ void __launch_bounds__(32 * kWarps, ctas_by_registers(NT)) cache_attn_kernel(const __grid_constant__ CacheAttnArgs a, int* status) {
   using R = Ring<D>;
   constexpr bool FINE = std::is_same<T, __half>::value;
@@ -470,9 +494,10 @@ __global__ void __launch_bounds__(32 * kWarps, ctas_by_registers(NT)) cache_attn
   // look - {segment of all requests', block in it, page, length} and the block's place in its page, page and length on their way - and then, by know(),
   // what is there: {segment, tokens from the unit on, block of the cache, bytes of the copy to ask for | blocks of the unit that exist << 16}.  A unit that
   // cannot leave its page is one copy, its first block's.
-  // NB blocks at a time: the four of a unit at d = 64 (2 x 131072: 157 us; two 162, one 167), one at d = 128 (64 requests: 71.4; two 72.8, which spill), two
-  // where two tiles of heads work on a block (36 / 4 heads of 64: 33.9; four, which spill, 35.6).
-  constexpr int U = R::kUnit, kBatch = 32 / U, NB = NT == 2 ? 2 : D == 64 ? 4 : 1;
+  // NB blocks at a time.  One tile of heads, fp16: four at d = 64 (2 x 131072 tokens, 32 / 32 heads: 150 us; two 153, one 160), two at d = 128 (16 x 32768, 8 / 8: 75; one 77).
+  // bf16, whose blocks are less work: half of that (64, 32 / 8: 39, with four, which spill, 41; 128, 64 requests: 66, two 68).  Two tiles: two (36 / 4 heads of 64: 33.9,
+  // four, which spill, 35.6; 32 / 2 of 128: 34.7, one 35.8).
+  constexpr int U = R::kUnit, kBatch = 32 / U, NB = NT == 2 ? 2 : (D == 64 ? 2 : 1) * (FINE ? 2 : 1);
   const bool whole = subs % U == 0;
   const int shift = subs & (subs - 1) ? -1 : 31 - __clz(subs);           // blocks of a page: a power of two?
   int4* s_known = reinterpret_cast<int4*>(smem + kWarps * R::kWarpBytes) + warp * 64;                       // [2][32]
@@ -522,7 +547,7 @@ __global__ void __launch_bounds__(32 * kWarps, ctas_by_registers(NT)) cache_attn
     segment = sg;
     request = segment / segs; seg = segment - request * segs;
     const int kv = seg / a.chunks, chunk = seg - kv * a.chunks;
-    load_heads<D, NT, T>(h, a, request, kv * per_kv + chunk * 8 * NT, min(per_kv - chunk * 8 * NT, 8 * NT));
+    load_heads<D, NT, PAIR, T>(h, a, request, kv * per_kv + chunk * 8 * NT, min(per_kv - chunk * 8 * NT, 8 * NT));
   };
   if (count > 0) {
     look(0);
@@ -581,11 +606,19 @@ __global__ void __launch_bounds__(32 * kWarps, ctas_by_registers(NT)) cache_attn
       int valid[NB];
 #pragma unroll
       for (int i = 0; i < NB; ++i) valid[i] = (there >> (b + i)) & 1 ? left - (b + i) * kBlockTokens : 0;
-      if ((there >> b) & ((1 << NB) - 1)) attend_blocks<D, NT, NB, FINE>(h, smem + warp * R::kWarpBytes + st * R::kUnitBytes + b * Block<D>::kBytes, valid);
+      if ((there >> b) & ((1 << NB) - 1)) attend_blocks<D, NT, PAIR, NB, FINE>(h, smem + warp * R::kWarpBytes + st * R::kUnitBytes + b * Block<D>::kBytes, valid);
     }
     __syncwarp();
     if (asked < count) ask();
     if (left <= R::kUnitTokens || n + 1 == count) {                        // the segment's last unit, or the part's
+      if constexpr (PAIR) {                                                // what columns 4 .. 7 have belongs to heads 0 .. 3
+#pragma unroll
+        for (int u = 0; u < D / 16; ++u)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) h.o[0][u][i] += __shfl_xor_sync(0xffffffffu, h.o[0][u][i], 2);
+#pragma unroll
+        for (int i = 0; i < 2; ++i) h.om[0][i] += __shfl_xor_sync(0xffffffffu, h.om[0][i], 2);
+      }
       const int units = s_starts[request + 1] - s_starts[request], seg_first = s_starts[request] * segs + seg * units, seg_end = seg_first + units;
       if (seg_first >= first && seg_end <= end) flush(nullptr);
       else {
@@ -801,12 +834,14 @@ extern "C" int hyperattn_cache_attention(const hyperattn_cache_attention_params*
     return (int)HYPERATTN_CUDA_ERROR;
   };
   auto build = [&](auto dim, auto tiles, auto type) {
-    constexpr int D = decltype(dim)::value, NT = decltype(tiles)::value;
+    constexpr int D = decltype(dim)::value, NT = decltype(tiles)::value > 1 ? 2 : 1;
+    constexpr bool PAIR = decltype(tiles)::value == 0;
     using T = decltype(type);
-    if (allow_smem<cache_attn_kernel<D, NT, T>>(Ring<D>::bytes(kMaxRequests)) != cudaSuccess) return (int)HYPERATTN_CUDA_ERROR;
-    return go(dim, cache_attn_kernel<D, NT, T>);
+    if (allow_smem<cache_attn_kernel<D, NT, PAIR, T>>(Ring<D>::bytes(kMaxRequests)) != cudaSuccess) return (int)HYPERATTN_CUDA_ERROR;
+    return go(dim, cache_attn_kernel<D, NT, PAIR, T>);
   };
   auto of_type = [&](auto dim, auto tiles) { return p->dtype == HYPERATTN_BF16 ? build(dim, tiles, __nv_bfloat16()) : build(dim, tiles, __half()); };
-  auto of_tiles = [&](auto dim) { return s.two ? of_type(dim, std::integral_constant<int, 2>{}) : of_type(dim, std::integral_constant<int, 1>{}); };
+  // (four heads or fewer: both halves of a tile, see add_values)
+  auto of_tiles = [&](auto dim) { return s.part_heads <= 4 ? of_type(dim, std::integral_constant<int, 0>{}) : s.two ? of_type(dim, std::integral_constant<int, 2>{}) : of_type(dim, std::integral_constant<int, 1>{}); };
   return d == 64 ? of_tiles(std::integral_constant<int, 64>{}) : of_tiles(std::integral_constant<int, 128>{});
 }
