@@ -95,10 +95,9 @@ def _stream(index, stream):
 
 def _used(stream, device, *tensors):
     """Tensors that a call on a stream of the caller's uses and this module has made or may let go: the allocator waits for that stream."""
-    if stream is not None:
-        other = torch.cuda.ExternalStream(stream, device=device)
-        for t in tensors:
-            t.record_stream(other)
+    other = torch.cuda.ExternalStream(stream, device=device)
+    for t in tensors:
+        t.record_stream(other)
 
 
 def _new(shape, dtype, device):
@@ -174,16 +173,18 @@ def cache_plan(lengths, new, table, free, n_free, page_tokens, rows, stream=None
         none = lengths.new_full((2, rows), -1)
         zero = lengths.new_zeros((2, 1))
         return CachePlan(none[0], none[1], zero[0], zero[1], lengths.clone(), table.clone(), free.clone(), n_free.clone())
-    # one allocation for the small results
-    small = _new((2 * rows + 3 * R + 3,), torch.int32, lengths.device)
-    table_out, free_out = torch.empty_like(table), torch.empty_like(free)
-    at = small.data_ptr()
+    # one allocation for all but the table, the stack first (its address stays in steps of 16 bytes)
+    flat = _new((F + 2 * rows + 3 * R + 3,), torch.int32, lengths.device)
+    table_out = torch.empty_like(table)
+    stack = flat.data_ptr()
+    at = stack + 4 * F
     _call("hyperattn_cache_plan", index, _plan_bytes(
         lengths.data_ptr(), new.data_ptr(), table.data_ptr(), free.data_ptr(), n_free.data_ptr(), R, W, F, page_tokens, rows,
         at, at + 4 * rows, at + 8 * rows, at + 4 * (2 * rows + R + 1), at + 4 * (2 * rows + 2 * R + 2), table_out.data_ptr(),
-        free_out.data_ptr(), at + 4 * (2 * rows + 3 * R + 2), _stream(index, stream)))
-    _used(stream, small.device, small, table_out, free_out)
-    slots, positions, cu_new, cu_len, lengths_out, n_free_out = torch.unsafe_split_with_sizes(small, (rows, rows, R + 1, R + 1, R, 1))
+        stack, at + 4 * (2 * rows + 3 * R + 2), _stream(index, stream)))
+    if stream is not None:
+        _used(stream, flat.device, flat, table_out)
+    free_out, slots, positions, cu_new, cu_len, lengths_out, n_free_out = torch.unsafe_split_with_sizes(flat, (F, rows, rows, R + 1, R + 1, R, 1))
     return CachePlan(slots, positions, cu_new, cu_len, lengths_out, table_out, free_out, n_free_out)
 
 
@@ -200,7 +201,8 @@ def cache_store(cache, k, v, slots, stream=None):
     v, v_row, v_head = _rows(v)
     _call("hyperattn_cache_store", index, _cache_bytes(*c), k.data_ptr(), v.data_ptr(), _code(k.dtype, "k"), k.shape[0], k_row, k_head, v_row, v_head,
           slots.data_ptr(), _stream(index, stream))
-    _used(stream, cache.device, k, v)
+    if stream is not None:
+        _used(stream, cache.device, k, v)
 
 
 def cache_read(cache, table, cu, rows, first=None, dtype=torch.bfloat16, stream=None):
@@ -220,7 +222,8 @@ def cache_read(cache, table, cu, rows, first=None, dtype=torch.bfloat16, stream=
     v = torch.empty_like(k)
     _call("hyperattn_cache_read", index, _cache_bytes(*c), table.data_ptr(), R, W, cu.data_ptr(), None if first is None else first.data_ptr(), rows,
           k.data_ptr(), v.data_ptr(), _code(dtype, "the result"), _stream(index, stream))
-    _used(stream, cache.device, k, v)
+    if stream is not None:
+        _used(stream, cache.device, k, v)
     return k, v
 
 
@@ -259,7 +262,8 @@ def cache_attention(q, cache, table, lengths, scale=0.0, out_dtype=None, stream=
     _call("hyperattn_cache_attention", index, _attention_bytes(
         *c, q.data_ptr(), row, head, out.data_ptr(), lse.data_ptr(), table.data_ptr(), lengths.data_ptr(), R, W, H, dtype, out_code, scale,
         work.data_ptr(), size, _stream(index, stream)))
-    _used(stream, device, q, out, lse, work)
+    if stream is not None:
+        _used(stream, device, q, out, lse, work)
     return out, lse
 
 
@@ -292,5 +296,6 @@ def prompt_attention(q, k, v, cu_q, cu_k=None, causal=True, scale=0.0, out_dtype
     _call("hyperattn_prompt_attention", index, _prompt_bytes(
         q.data_ptr(), k.data_ptr(), v.data_ptr(), q_row, q_head, k_row, k_head, v_row, v_head, out.data_ptr(), lse.data_ptr(), cu_q.data_ptr(),
         cu_k.data_ptr(), cu_q.shape[0] - 1, T, k_rows, H, kv_heads, d, 1 if causal else 0, dtype, out_code, scale, _stream(index, stream)))
-    _used(stream, device, q, k, v, out, lse)
+    if stream is not None:
+        _used(stream, device, q, k, v, out, lse)
     return out, lse
