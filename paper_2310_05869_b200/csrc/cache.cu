@@ -156,7 +156,8 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const __grid_constan
 // numbers each, a group of 32 the numbers of four neighbouring lanes - and writes a whole block with 16-byte stores, a part of one by the pieces that its
 // tokens own.  What bounds it is the arithmetic of the codes.  Blocks that a run covers whole take a path without tests (32768 tokens of 32 heads of 64, fp16, 352 MB, with
 // the reading back: 201 us; with this path, codes clamped as pairs of integers, the divisions and the lengths of runs by fewer operations 163;
-// K rows of the next item asked for beside V 153, where those in registers made it slower, 175, and V's as well no faster, 154).
+// K rows of the next item asked for beside V 153, where those in registers made it slower, 175, and V's as well no faster, 154;
+// scales and minima of four rows by four lanes, each for one, and not by all four for each, 150; all V rows asked for at once spill and are no faster, 149 but d = 128 138 for 137).
 constexpr int kStoreRows = 64, kStoreWarps = 8;
 
 struct StoreArgs {
@@ -193,24 +194,37 @@ __device__ __forceinline__ float reciprocal(float s) {
   asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(s));
   return fmaf(y, fmaf(-s, y, 1.f), y);
 }
-// The codes of the lane's 8 numbers, c[i] = number A(i) and, 16 bits higher, number B(i); scale and minimum (fp16) of its group.
-template <class T, class A, class B>
-__device__ __forceinline__ void quantise8(const uint4& in, A first, B second, uint32_t (&c)[4], __half& s, __half& m) {
-  // smallest and minus largest number as a pair
+// Smallest and minus largest of the lane's 8 numbers, as a pair.
+template <class T>
+__device__ __forceinline__ uint32_t extremes(const uint4& in) {
   const uint32_t low = min2<T>(min2<T>(in.x, in.y), min2<T>(in.z, in.w)), high = max2<T>(max2<T>(in.x, in.y), max2<T>(in.z, in.w)) ^ 0x80008000u;
-  uint32_t both = min2<T>(__byte_perm(low, high, 0x5410), __byte_perm(low, high, 0x7632));
-  both = min2<T>(both, __shfl_xor_sync(0xffffffffu, both, 1));
-  both = min2<T>(both, __shfl_xor_sync(0xffffffffu, both, 2));
-  const float2 f = to_float2<T>(both);
-  s = __float2half_rn(fifteenth(-f.y - f.x));
-  m = __float2half_rn(f.x);
-  float fs = __half2float(s), fm = __half2float(m);
+  return min2<T>(__byte_perm(low, high, 0x5410), __byte_perm(low, high, 0x7632));
+}
+// What a group is held with: scale and minimum (fp16), minus the minimum and one over the scale as its codes take them.
+struct Held { __half s, m; float minus, r; };
+// Of four rows' extremes, each over four neighbouring lanes: lane j of the four gets row j's, and what follows from them.
+template <class T>
+__device__ __forceinline__ Held held_of(const uint32_t (&e)[4]) {
+  const bool b0 = threadIdx.x & 1, b1 = threadIdx.x & 2;
+  const uint32_t x0 = min2<T>(b1 ? e[2] : e[0], __shfl_xor_sync(0xffffffffu, b1 ? e[0] : e[2], 2)), x1 = min2<T>(b1 ? e[3] : e[1], __shfl_xor_sync(0xffffffffu, b1 ? e[1] : e[3], 2));
+  const float2 f = to_float2<T>(min2<T>(b0 ? x1 : x0, __shfl_xor_sync(0xffffffffu, b0 ? x0 : x1, 1)));
+  Held h;
+  h.s = __float2half_rn(fifteenth(-f.y - f.x));
+  h.m = __float2half_rn(f.x);
+  float fs = __half2float(h.s), fm = __half2float(h.m);
   if (!(fabsf(fs) < INFINITY) || !(fabsf(fm) < INFINITY)) {            // (a number that is not finite shows in one of the two)
-    s = m = __ushort_as_half(0x7fff);
+    h.s = h.m = __ushort_as_half(0x7fff);
     fs = fm = 0.f;
   }
-  const float r = fs == 0.f ? 0.f : reciprocal(fs);
-  const uint64_t minus = pack_f2(-fm, -fm), times = pack_f2(r, r);
+  h.r = fs == 0.f ? 0.f : reciprocal(fs);
+  h.minus = -fm;
+  return h;
+}
+// The codes of the lane's 8 numbers, of row j of held_of's four: c[i] = number A(i) and, 16 bits higher, number B(i).
+template <class T, class A, class B>
+__device__ __forceinline__ void codes8(const uint4& in, const Held& h, int j, A first, B second, uint32_t (&c)[4]) {
+  const float m = __shfl_sync(0xffffffffu, h.minus, j, 4), r = __shfl_sync(0xffffffffu, h.r, j, 4);
+  const uint64_t minus = pack_f2(m, m), times = pack_f2(r, r);
   const uint32_t w[4] = {in.x, in.y, in.z, in.w};
   uint32_t u[8];
 #pragma unroll
@@ -287,11 +301,9 @@ __global__ void __launch_bounds__(32 * kStoreWarps, D == 64 ? 4 : 3) store_kerne
     auto k_token = [&](int i) { return i * PER + sub; };
     auto v_token = [&](int i) { return 2 * (sub * (STEPS / 4) + i / 4) + i % 4 / 2 + (i & 1) * 8; };
     auto scales = [&](int at0, int t, __half s, __half m) {
-      if (o % 4 == 0) {
-        __half* to = reinterpret_cast<__half*>(block + at0 + ((t / 2) * B::kGroups + o / 4) * 8 + (t % 2) * 2);
-        to[0] = s;
-        to[2] = m;
-      }
+      __half* to = reinterpret_cast<__half*>(block + at0 + ((t / 2) * B::kGroups + o / 4) * 8 + (t % 2) * 2);
+      to[0] = s;
+      to[2] = m;
     };
     int then_run = run + next_run, then_head = head + next_head;
     if (then_head >= a.cache.heads) { then_head -= a.cache.heads; ++then_run; }
@@ -302,38 +314,47 @@ __global__ void __launch_bounds__(32 * kStoreWarps, D == 64 ? 4 : 3) store_kerne
       uint4 in[STEPS];
       asm volatile("cp.async.wait_all;" ::: "memory");
 #pragma unroll
-      for (int i = 0; i < STEPS; ++i) {
-        const int t = k_token(i);
-        uint32_t c[4];
-        __half s, m;
-        if (WHOLE || __any_sync(0xffffffffu, mine(t))) {
-          quantise8<T>(*reinterpret_cast<const uint4*>(next + i * 512), [](int j) { return 2 * j; }, [](int j) { return 2 * j + 1; }, c, s, m);
-          // nibble e of the codes is (e % 2) * 4 + e / 2 of the word
-          const uint32_t word = c[0] + 16 * c[1] + 256 * (c[2] + 16 * c[3]);
-          const int ln = (t % 8) * 4 + o % 4;
-          *reinterpret_cast<uint32_t*>(block + (D == 128 ? (t / 8) * 512 + ln * 16 : ln * 16 + (t / 8) * 8) + (o / 4) * 4) = word;
-          scales(B::kScaleK, t, s, m);
+      for (int i4 = 0; i4 < STEPS; i4 += 4) {
+        auto row = [&](int i) { return *reinterpret_cast<const uint4*>(next + i * 512); };
+        uint32_t e[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) e[i] = extremes<T>(row(i4 + i));
+        const Held h = held_of<T>(e);
+        scales(B::kScaleK, k_token(i4 + o % 4), h.s, h.m);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const int i = i4 + j, t = k_token(i);
+          if (WHOLE || __any_sync(0xffffffffu, mine(t))) {
+            uint32_t c[4];
+            codes8<T>(row(i), h, j, [](int x) { return 2 * x; }, [](int x) { return 2 * x + 1; }, c);
+            // nibble e of the codes is (e % 2) * 4 + e / 2 of the word
+            const uint32_t word = c[0] + 16 * c[1] + 256 * (c[2] + 16 * c[3]);
+            const int ln = (t % 8) * 4 + o % 4;
+            *reinterpret_cast<uint32_t*>(block + (D == 128 ? (t / 8) * 512 + ln * 16 : ln * 16 + (t / 8) * 8) + (o / 4) * 4) = word;
+          }
+          in[i] = WHOLE || mine(v_token(i)) ? *reinterpret_cast<const uint4*>(vs + (i & 1) * 8 * a.v_row) : make_uint4(0, 0, 0, 0);
+          if (i & 1) vs += a.v_row;
         }
-        in[i] = WHOLE || mine(v_token(i)) ? *reinterpret_cast<const uint4*>(vs + (i & 1) * 8 * a.v_row) : make_uint4(0, 0, 0, 0);
-        if (i & 1) vs += a.v_row;
       }
       if (item + warps < items) ask_k(then_run, then_head);
 #pragma unroll
       for (int i4 = 0; i4 < STEPS; i4 += 4) {
-        uint32_t w[4];
+        uint32_t w[4], e[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) e[i] = extremes<T>(in[i4 + i]);
+        const Held h = held_of<T>(e);
+        scales(B::kScaleV, v_token(i4 + o % 4), h.s, h.m);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           const int t = v_token(i4 + i);
           w[i] = 0;
           if (WHOLE || __any_sync(0xffffffffu, mine(t))) {
             uint32_t c[4];
-            __half s, m;
-            quantise8<T>(in[i4 + i], [](int j) { return j / 2 * 4 + j % 2; }, [](int j) { return j / 2 * 4 + j % 2 + 2; }, c, s, m);
+            codes8<T>(in[i4 + i], h, i, [](int x) { return x / 2 * 4 + x % 2; }, [](int x) { return x / 2 * 4 + x % 2 + 2; }, c);
             // the octets of a byte are neighbours: the even lane makes coordinates 0..3 of both, the odd one 4..7
             const uint32_t low = c[0] + 256 * c[1], high = c[2] + 256 * c[3];
             const uint32_t other = __shfl_xor_sync(0xffffffffu, o & 1 ? low : high, 1);
             w[i] = o & 1 ? other + 16 * high : low + 16 * other;
-            scales(B::kScaleV, t, s, m);
           }
         }
         // four tokens of four coordinates, the other way round
@@ -537,7 +558,7 @@ extern "C" int hyperattn_cache_store(const hyperattn_cache* cache, const void* k
   const StoreArgs a = {view_of(*cache), k, v, k_row_stride, k_head_stride, v_row_stride, v_head_stride, rows, slots};
   const cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
   // The heads of a window over several CTAs, until there are a few rounds of them: 32768 tokens of 32 heads (d = 64) with twice as many CTAs as SMs at least
-  // twice as long, eight and twelve times 153 us with the reading back, 24 times 156; the kernel needs the registers of four CTAs an SM (d = 128: three; d = 64 with five: 160).
+  // twice as long, eight and twelve times 150 us with the reading back, 24 times 153; the kernel needs the registers of four CTAs an SM (d = 128: three; d = 64 with five: 5 % longer).
   const int windows = (rows + kStoreRows - 1) / kStoreRows, most = (kStoreRows * cache->kv_heads + kStoreWarps - 1) / kStoreWarps;
   int split = (12 * kSms + windows - 1) / windows;
   if (split > most) split = most;
