@@ -558,7 +558,8 @@ extern "C" int hyperattn_cache_store(const hyperattn_cache* cache, const void* k
   const StoreArgs a = {view_of(*cache), k, v, k_row_stride, k_head_stride, v_row_stride, v_head_stride, rows, slots};
   const cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
   // The heads of a window over several CTAs, until there are a few rounds of them: 32768 tokens of 32 heads (d = 64) with twice as many CTAs as SMs at least
-  // twice as long, eight and twelve times 150 us with the reading back, 24 times 153; the kernel needs the registers of four CTAs an SM (d = 128: three; d = 64 with five: 5 % longer).
+  // 181 us, six times 114, twelve times 100 (the first form); with the reading back eight and twelve times 153, 24 times 156 (the form before the last).
+  // The kernel needs the registers of four CTAs an SM (d = 128: three); d = 64 with five: 160 for 153.
   const int windows = (rows + kStoreRows - 1) / kStoreRows, most = (kStoreRows * cache->kv_heads + kStoreWarps - 1) / kStoreWarps;
   int split = (12 * kSms + windows - 1) / windows;
   if (split > most) split = most;
