@@ -92,6 +92,7 @@ struct alignas(64) PromptMaps {
 constexpr int kTileRows = 128, kTileKeys = 128;
 constexpr int kThreads = 384;
 constexpr float kSumLimit = 32768.f;    // a tile whose weights sum to more has its reference moved (fp16 weights end at 2^16)
+constexpr float kMostByArithmetic = 120.f;       // and one with a weight beyond 2 to that (which exp2_pair does not make; those up to it show in the sum)
 
 template <int D>
 struct Cfg {
@@ -187,12 +188,14 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
   return d;
 }
 
-// 2^x of two numbers in -infinity .. 2^10 by arithmetic: x = n + f with n the nearest integer, 2^f by a polynomial of degree 4 (its coefficients a least-maximum
-// fit of the relative error over -1/2 .. 1/2: 2.7e-6), n added to the exponent.  Below 2^-125 it is that.  The exponential unit makes 16 a clock and SM,
-// which is what a tile of scores takes longest for; so some of them are made here.
-__device__ __forceinline__ uint64_t exp2_pair(uint64_t x2) {
+// 2^x of two numbers up to 127 by arithmetic: x = n + f with n the nearest integer, 2^f by a polynomial of degree 4 (its coefficients a least-maximum
+// fit of the relative error over -1/2 .. 1/2: 2.7e-6), n added to the exponent.  Below 2^-125 it is that; above 2^127 the exponent does not hold n, so the caller
+// looks at the largest x, which goes to `most` (NaN if one is).  The exponential unit makes 16 a clock and SM, which is what a tile of scores takes longest
+// for; so some of them are made here.
+__device__ __forceinline__ uint64_t exp2_pair(uint64_t x2, float& most) {
   float x, y;
   unpack_f2(x2, x, y);
+  most = max3(most, x, y);
   x2 = pack_f2(max3(x, -125.f, -125.f), max3(y, -125.f, -125.f));                       // (NaN stays, and becomes a huge number or NaN)
   const uint64_t t = fadd2(x2, pack_f2(12582912.f, 12582912.f));                      // 1.5 * 2^23 + n
   const uint64_t f = ffma2(fadd2(t, pack_f2(-12582912.f, -12582912.f)), pack_f2(-1.f, -1.f), x2);
@@ -369,6 +372,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const __grid_consta
           const float off = ref == -INFINITY ? 0.f : -ref;
           const uint64_t off2 = pack_f2(off, off);
           uint64_t tile2 = 0;
+          float most = -INFINITY;
 #pragma unroll
           for (int c = 0; c < 4; ++c) {
             uint32_t p[16];
@@ -376,7 +380,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const __grid_consta
             for (int e = 0; e < 16; ++e) {
               const uint64_t x2 = ffma2(pack_u2(r[c][2 * e], r[c][2 * e + 1]), sc2, off2);
               uint64_t w2;
-              if (e % C::kArithmetic == C::kArithmetic - 1) w2 = exp2_pair(x2);
+              if (e % C::kArithmetic == C::kArithmetic - 1) w2 = exp2_pair(x2, most);
               else {
                 float x, y;
                 unpack_f2(x2, x, y);
@@ -391,7 +395,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const __grid_consta
           }
           float t0, t1;
           unpack_f2(tile2, t0, t1);
-          if (attempt > 0 || !__any_sync(0xffffffffu, !(t0 + t1 <= kSumLimit))) {
+          if (attempt > 0 || !__any_sync(0xffffffffu, !(t0 + t1 <= kSumLimit && most <= kMostByArithmetic))) {
             sum2 = fadd2(sum2, tile2);
             break;
           }
