@@ -189,9 +189,11 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
 }
 
 // 2^x of two numbers up to 127 by arithmetic: x = n + f with n the nearest integer, 2^f by a polynomial of degree 4 (its coefficients a least-maximum
-// fit of the relative error over -1/2 .. 1/2: 2.7e-6), n added to the exponent.  Below 2^-125 it is that; above 2^127 the exponent does not hold n, so the caller
-// looks at the largest x, which goes to `most` (NaN if one is).  The exponential unit makes 16 a clock and SM, which is what a tile of scores takes longest
-// for; so some of them are made here.
+// fit of the relative error over -1/2 .. 1/2: 2.7e-6), n added to the exponent.  Below -125 x counts as that, and what it gives is taken off every result: zero for
+// those, no difference to others.  (ZERO; where results become fp16 it is zero anyway, and sums do not show it.)  Above 2^127 the exponent does not hold n,
+// so the caller looks at the largest x, which goes to `most` (NaN if one is).  The exponential unit makes 16 a clock and SM, which is what a tile of scores
+// takes longest for; so some of them are made here.
+template <bool ZERO>
 __device__ __forceinline__ uint64_t exp2_pair(uint64_t x2, float& most) {
   float x, y;
   unpack_f2(x2, x, y);
@@ -206,7 +208,9 @@ __device__ __forceinline__ uint64_t exp2_pair(uint64_t x2, float& most) {
   float p0, p1, t0, t1;
   unpack_f2(p, p0, p1);
   unpack_f2(t, t0, t1);
-  return pack_u2(__float_as_uint(p0) + (__float_as_uint(t0) << 23), __float_as_uint(p1) + (__float_as_uint(t1) << 23));
+  const uint64_t w = pack_u2(__float_as_uint(p0) + (__float_as_uint(t0) << 23), __float_as_uint(p1) + (__float_as_uint(t1) << 23));
+  constexpr float least = 0.9999992847442627f * 0x1p-125f;
+  return ZERO ? fadd2(w, pack_f2(-least, -least)) : w;
 }
 
 // O of a row times alpha, in TMEM (rare).  All lanes together.
@@ -380,7 +384,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const __grid_consta
             for (int e = 0; e < 16; ++e) {
               const uint64_t x2 = ffma2(pack_u2(r[c][2 * e], r[c][2 * e + 1]), sc2, off2);
               uint64_t w2;
-              if (e % C::kArithmetic == C::kArithmetic - 1) w2 = exp2_pair(x2, most);
+              if (e % C::kArithmetic == C::kArithmetic - 1) w2 = exp2_pair<std::is_same<T, __nv_bfloat16>::value>(x2, most);
               else {
                 float x, y;
                 unpack_f2(x2, x, y);
