@@ -261,7 +261,8 @@ __device__ __forceinline__ void add_values(Heads<D, NT>& h, const uint8_t* block
     }
     unpack_f2(fadd2(pack_f2(h.om[t][0], h.om[t][1]), pack_f2(m[0], m[1])), h.om[t][0], h.om[t][1]);
   }
-  // Scales of 2 and more (values that differ by 30 in a group): the weights get so much smaller that the products stay numbers, the sums larger.
+  // Scales of 2 and more (values that differ by 30 in a group): the weights get so much smaller that the products stay numbers, the sums larger.  What a weight then
+  // loses below fp16's 2^-24 is lost: 2^-25 beside a largest one of 2^(12 - k).
   uint32_t any = 0;
 #pragma unroll
   for (int b = 0; b < NB; ++b)
@@ -271,7 +272,15 @@ __device__ __forceinline__ void add_values(Heads<D, NT>& h, const uint8_t* block
       for (int i = 0; i < G; ++i) any |= sv[b][half][i];
   float up = 1.f;
   if (__any_sync(0xffffffffu, any & 0x40004000u)) {
-    const int k = (int)((__reduce_or_sync(0xffffffffu, any | any >> 16) >> 10) & 31u) - 15;       // all scales are below 2^(k + 1)
+    __half2 most = __half2half2(__ushort_as_half(0));    // the largest scales (of a number and NaN the number: a NaN's group is NaN whatever the others are multiplied with)
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+      for (int half = 0; half < 2; ++half)
+#pragma unroll
+        for (int i = 0; i < G; ++i) most = __hmax2(most, h2(sv[b][half][i]));
+    const uint32_t top = __reduce_max_sync(0xffffffffu, max(u32(most) & 0xffffu, u32(most) >> 16));
+    const int k = max((int)(top >> 10) - 15, 0);         // all scales are below 2^(k + 1)
     const __half2 down = __half2half2(__float2half_rn(__uint_as_float((uint32_t)(127 - k) << 23)));
     up = __uint_as_float((uint32_t)(127 + k) << 23);
 #pragma unroll

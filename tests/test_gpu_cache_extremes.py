@@ -1,0 +1,48 @@
+"""Attention over the 4-bit cache where numbers come near the ends of their types."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2310_05869_b200 as ha
+
+pytestmark = pytest.mark.gpu
+
+DT = {"bf16": torch.bfloat16, "fp16": torch.float16}
+
+
+def ints(x):
+    return torch.tensor(np.asarray(x), dtype=torch.int32, device="cuda")
+
+
+@pytest.mark.parametrize("d,dtype,heads", [(64, "fp16", 1), (64, "bf16", 8), (128, "bf16", 4), (128, "fp16", 16)])
+@pytest.mark.parametrize("size", [8.0, 300.0])
+@pytest.mark.parametrize("nan", [False, True])
+def test_values_of_several_scales_under_small_weights(d, dtype, heads, size, nan):
+    """One token 16.5 octaves above 30 others that are alike and have all the values, in groups whose scales are on either side of powers of two (and with a
+    NaN among them, which its own group alone shows).  Weights are fp16 numbers, 2^-11 off at most where they are not smaller than 2^-14: the largest is
+    2^12 over the power of two in the scales of a block - 2^12 / 2^7 for values of 300 - and the others 2^-16.5 of that, 2^-11.5."""
+    R, T, page = 50, 31, 32                              # (a request is less than what one warp takes: all its tokens meet)
+    gen = torch.Generator("cuda").manual_seed(d + heads)
+    cache = ha.cache_pages(R, 1, d, page)
+    k = torch.zeros(R, T, 1, d, device="cuda")
+    k[:, 7] = 16.5 * np.log(2) / (4 * d ** 0.5)
+    v = size * (1 + torch.randn(R, T, 1, d, generator=gen, device="cuda") * torch.rand(R, T, 1, 1, generator=gen, device="cuda"))
+    v[:, 7] = 0
+    if nan:
+        v[:, 20, 0, 40] = float("nan")
+    k, v = (x.reshape(R * T, 1, d).to(DT[dtype]) for x in (k, v))
+    ha.cache_store(cache, k, v, ints((np.arange(R)[:, None] * page + np.arange(T)).ravel()))
+    table = ints(np.arange(R))[:, None]
+    K, V = (x.view(R, T, d).double() for x in ha.cache_read(cache, table, ints(np.arange(R + 1) * T), R * T, dtype=torch.float32))
+    q = torch.full((R, heads, d), 4.0, device="cuda").to(DT[dtype])
+    out, lse = ha.cache_attention(q, cache, table, ints([T] * R), out_dtype=torch.float32)
+    z = K @ q[0, 0].double() / d ** 0.5
+    want = torch.einsum("rt,rtd->rd", torch.softmax(z, 1), V)[:, None]
+    size_of = torch.einsum("rt,rtd->rd", torch.softmax(z, 1), V.abs())[:, None]
+    bad = torch.zeros(d, dtype=torch.bool, device="cuda")
+    if nan:
+        bad[32:64] = True
+    assert torch.equal(want.isnan(), bad.expand_as(want)) and out[:, :, bad].isnan().all()
+    bound = (2.0 ** -11 + 2.0 ** -15 * float(z.max()) + 1e-5) * size_of
+    assert ((out.double() - want).abs() <= bound)[:, :, ~bad].all(), float(((out.double() - want).abs() / size_of)[:, :, ~bad].max())
+    assert (lse.double() - torch.logsumexp(z, 1)[:, None]).abs().max() <= 1e-4
