@@ -316,6 +316,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const __grid_consta
       const int tiles = i ? d.tiles[1] : d.tiles[0], tokens = i ? d.tokens[1] : d.tokens[0];
       const int tok = i * tile_tokens + token;                                   // in the pair
       const int limit = a.causal ? min(d.last + tok, d.keys - 1) : d.keys - 1;  // last key that the row sees
+      const bool there = token < tokens && token < tile_tokens;                 // (other rows of the tile are other requests', or whatever shared memory held)
       const int least = a.causal ? min(d.last + i * tile_tokens, d.keys - 1) : d.keys - 1;       // the tile's first token
       float ref = -INFINITY;
       bool finite = true;
@@ -350,8 +351,9 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const __grid_consta
           }
         }
         // The maximum is not taken of every tile: weights are made against the reference that the row has, and only where their sum shows that one of them may be
-        // too large (or a score is not a number), or there is no reference yet, the maximum is taken, the reference moved to it, and the weights are made again.
-        auto move_reference = [&] {
+        // too large (or a score is not a number), or there is no reference yet, the maximum is taken, the reference moved to it, and the weights are made again -
+        // in rows that need it: no row's result depends on which others it shares a warp with.
+        auto move_reference = [&](bool need) {
           float m[4];
 #pragma unroll
           for (int c = 0; c < 4; ++c) {
@@ -362,7 +364,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const __grid_consta
           }
           const float top = max3(max3(m[0], m[1], m[2]), m[3], m[3]) * a.scale_log2;
           finite = finite && top < INFINITY;                               // (false for NaN)
-          const bool move = top > ref;
+          const bool move = need && top > ref;
           if (!__any_sync(0xffffffffu, move)) return;
           // (the products before this tile's are done - without P beside S because its scores came after them; the next one on O waits for this P)
           float alpha = 1.f;
@@ -370,7 +372,8 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const __grid_consta
           sum2 = fmul2(sum2, pack_f2(alpha, alpha));
           if (n > 0) rescale_o(ocol, D, alpha);
         };
-        if (__any_sync(0xffffffffu, ref == -INFINITY)) move_reference();
+        const bool first = there && ref == -INFINITY;
+        if (__any_sync(0xffffffffu, first)) move_reference(first);
         const uint64_t sc2 = pack_f2(a.scale_log2, a.scale_log2);
         for (int attempt = 0;; ++attempt) {
           const float off = ref == -INFINITY ? 0.f : -ref;
@@ -399,11 +402,12 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const __grid_consta
           }
           float t0, t1;
           unpack_f2(tile2, t0, t1);
-          if (attempt > 0 || !__any_sync(0xffffffffu, !(t0 + t1 <= kSumLimit && most <= kMostByArithmetic))) {
+          const bool over = there && !(t0 + t1 <= kSumLimit && most <= kMostByArithmetic);
+          if (attempt > 0 || !__any_sync(0xffffffffu, over)) {
             sum2 = fadd2(sum2, tile2);
             break;
           }
-          move_reference();
+          move_reference(over);
         }
         tmem_wait_st();
         tc_fence_before();
@@ -415,7 +419,6 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const __grid_consta
       float s0, s1;
       unpack_f2(sum2, s0, s1);
       const float sum = s0 + s1, inv = ref == -INFINITY ? 0.f : 1.f / sum;        // (no reference: nothing was seen, or only -infinity)
-      const bool mine = token < tokens && token < tile_tokens;
       const size_t at = (size_t)(d.row0 + tok) * a.q_heads + d.kv * group + head;
       if (tiles > 0) {
         ok = warp_wait<2>(bar_o(i), items & 1, s_abort, status);
@@ -432,7 +435,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const __grid_consta
             finite = finite && fabsf(x) < INFINITY;
             o[e] = __float_as_uint(x);
           }
-          if (mine) {
+          if (there) {
             if (a.out_kind == HYPERATTN_FP32) {
               float4* to = reinterpret_cast<float4*>(reinterpret_cast<float*>(a.out) + at * D + 32 * c);
 #pragma unroll
@@ -453,14 +456,14 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const __grid_consta
         tc_fence_before();
         mbar_arrive(bar_ofree(i));
         ++items;
-        if (mine) a.lse[at] = ref == -INFINITY ? -INFINITY : (ref + log2f(sum)) * 0.6931471805599453f;
-      } else if (mine) {
+        if (there) a.lse[at] = ref == -INFINITY ? -INFINITY : (ref + log2f(sum)) * 0.6931471805599453f;
+      } else if (there) {
         a.lse[at] = -INFINITY;
         const int bytes = D * (a.out_kind == HYPERATTN_FP32 ? 4 : 2);
         for (int e = 0; e < bytes; e += 16) *reinterpret_cast<uint4*>(reinterpret_cast<char*>(a.out) + at * bytes + e) = make_uint4(0, 0, 0, 0);
       }
       // rows that are not finite: over again, over the keys that they see
-      for (unsigned bad = __ballot_sync(0xffffffffu, mine && tiles > 0 && !finite); bad; bad &= bad - 1) {
+      for (unsigned bad = __ballot_sync(0xffffffffu, there && tiles > 0 && !finite); bad; bad &= bad - 1) {
         const int src = __ffs(bad) - 1;
         const int t = __shfl_sync(0xffffffffu, tok, src), h = __shfl_sync(0xffffffffu, head, src), last = __shfl_sync(0xffffffffu, limit, src);
         __syncwarp();

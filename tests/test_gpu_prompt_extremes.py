@@ -1,4 +1,4 @@
-"""Exact attention over packed prompts where numbers come near the ends of their types: scores far apart, values that nobody may see."""
+"""Exact attention over packed prompts where numbers come near the ends of their types: scores far apart, values that nobody may see, rows beside others."""
 import numpy as np
 import pytest
 import torch
