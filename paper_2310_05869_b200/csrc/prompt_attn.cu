@@ -10,15 +10,16 @@
 // tile; it moves when a tile's weights sum to more than 2^15, and then O is multiplied in TMEM.  Tiles with keys that a row does not see are
 // the first ones, so masks cost the later ones nothing.
 //
-// Values of keys that a row does not see are multiplied with zeros, which is not nothing where they are infinite or NaN.  Those beyond a
-// request's end are zeros in shared memory; those of later tokens show as a result that is not finite, and such a row is done over, key by key
-// over those that it does see.
+// Values of keys that a row does not see are multiplied with zeros, which is not nothing where they are infinite or NaN.  In the tiles with such keys - of later tokens
+// of the item, and beyond the request's end - infinities and NaN of keys that not all of its rows see are set to zero before they are multiplied, and the rows that do
+// see them get them added at the end.
 //
 // What bounds it: at d = 128 the tensor pipe (68 % of its cycles) at the clock that the power limit leaves; 16384 tokens, 16 / 2 heads: 910 us, 1.2 PFLOP/s.  At d = 64
 // the exponentials: a warp takes 1900 of 2800 clocks a tile for its own, of which the unit works 1790 for the two warps of a scheduler; 6001 tokens behind 5000 cached ones,
 // 32 heads: 213 us, 0.62 PFLOP/s.  13 short prompts of 1021 tokens: 15 us, two items of a CTA one after the other.
 //
-// Warp roles (384 threads): 0-3 and 4-7 softmax and results of query tile 0 and 1, 8 issues the products (and allocates TMEM), 9 loads, 10 prepares items.
+// Warp roles (384 threads): 0-3 and 4-7 softmax and results of query tile 0 and 1, 8 issues the products (and allocates TMEM), 9 loads, 10 prepares items, 11 sees to
+// values that are not finite.
 // Every wait is bounded: a CTA that gives up raises the device status word, drains its copies, frees its TMEM and returns.
 #include <climits>
 #include <cstdio>
@@ -39,50 +40,38 @@ struct PromptArgs {
   float scale_log2;
 };
 
-// A warp and one query row of one head: a lane has D / 32 coordinates, the keys follow each other.
+// A lane's row at out[at]: the values that are not finite of keys key0 + from .. key0 + last (those that the row sees; none for last < from).  All lanes
+// together: a lane looks at D / 32 coordinates of a key, and every row gathers, for each coordinate, whether there was an infinity of either sign (NaN: both).
 template <int D, class T>
-__device__ __noinline__ void attend_row(const PromptArgs& a, int row, int head, int key0, int keys) {
-  constexpr int E = D / 32;                                // coordinates of a lane
-  const int lane = threadIdx.x & 31, kv = head / (a.q_heads / a.kv_heads);
-  auto load = [&](const void* base, size_t at, float (&x)[E]) {
-    const uint32_t* src = reinterpret_cast<const uint32_t*>(reinterpret_cast<const T*>(base) + at) + lane * (E / 2);
+__device__ __noinline__ void add_unfinite(const PromptArgs& a, int kv, int key0, int from, int last, size_t at) {
+  constexpr int E = D / 32;
+  const int lane = threadIdx.x & 31, end = __reduce_max_sync(0xffffffffu, last);
+  const uint32_t* src = reinterpret_cast<const uint32_t*>(reinterpret_cast<const T*>(a.v) + (size_t)(key0 + from) * a.v_row + (size_t)kv * a.v_head) + lane * (E / 2);
+  uint32_t up[E], down[E];
 #pragma unroll
-    for (int i = 0; i < E / 2; ++i) { const float2 f = to_float2<T>(src[i]); x[2 * i] = f.x; x[2 * i + 1] = f.y; }
-  };
-  float q[E], o[E], ref = -INFINITY, sum = 0.f;
-  load(a.q, (size_t)row * a.q_row + (size_t)head * a.q_head, q);
+  for (int e = 0; e < E; ++e) up[e] = down[e] = 0;
+#pragma unroll 4
+  for (int key = from; key <= end; ++key, src += a.v_row / 2) {
 #pragma unroll
-  for (int i = 0; i < E; ++i) o[i] = 0.f;
-  for (int j = 0; j < keys; ++j) {
-    float k[E], v[E], s = 0.f;
-    load(a.k, (size_t)(key0 + j) * a.k_row + (size_t)kv * a.k_head, k);
-    load(a.v, (size_t)(key0 + j) * a.v_row + (size_t)kv * a.v_head, v);
+    for (int i = 0; i < E / 2; ++i) {
+      const float2 f = to_float2<T>(src[i]);
+      const float x[2] = {f.x, f.y};
 #pragma unroll
-    for (int i = 0; i < E; ++i) s = fmaf(q[i], k[i], s);
-#pragma unroll
-    for (int w = 16; w; w >>= 1) s += __shfl_xor_sync(0xffffffffu, s, w);
-    s *= a.scale_log2;
-    if (s > ref) {
-      const float f = ex2(ref - s);
-      sum *= f; ref = s;
-#pragma unroll
-      for (int i = 0; i < E; ++i) o[i] *= f;
+      for (int e = 0; e < 2; ++e) {
+        const unsigned p = __ballot_sync(0xffffffffu, !(x[e] < INFINITY)), m = __ballot_sync(0xffffffffu, !(x[e] > -INFINITY));
+        if (key <= last) { up[2 * i + e] |= p; down[2 * i + e] |= m; }
+      }
     }
-    const float p = ex2(s - (ref == -INFINITY ? 0.f : ref));
-    sum += p;
-#pragma unroll
-    for (int i = 0; i < E; ++i) o[i] = fmaf(p, v[i], o[i]);
   }
-  const size_t at = (size_t)row * a.q_heads + head;
 #pragma unroll
-  for (int i = 0; i < E; ++i) {
-    const float x = sum == 0.f ? 0.f : o[i] / sum;
-    const size_t e = at * D + lane * E + i;
-    if (a.out_kind == HYPERATTN_FP32) reinterpret_cast<float*>(a.out)[e] = x;
-    else if (a.out_kind == HYPERATTN_BF16) reinterpret_cast<__nv_bfloat16*>(a.out)[e] = __float2bfloat16_rn(x);
-    else reinterpret_cast<__half*>(a.out)[e] = __float2half_rn(x);
-  }
-  if (lane == 0) a.lse[at] = sum == 0.f ? -INFINITY : (ref + log2f(sum)) * 0.6931471805599453f;
+  for (int e = 0; e < E; ++e)
+    for (uint32_t any = up[e] | down[e]; any; any &= any - 1) {
+      const int l = __ffs(any) - 1;
+      const float x = (up[e] >> l & 1 ? INFINITY : 0.f) - (down[e] >> l & 1 ? INFINITY : 0.f);
+      const size_t i = at * D + l * E + e;
+      if (a.out_kind == HYPERATTN_FP32) reinterpret_cast<float*>(a.out)[i] += x;
+      else reinterpret_cast<T*>(a.out)[i] = static_cast<T>(static_cast<float>(reinterpret_cast<T*>(a.out)[i]) + x);
+    }
 }
 
 struct alignas(64) PromptMaps {
@@ -116,6 +105,8 @@ struct Item {
   int key0, keys;                        // first key row, keys of the request
   int last;                              // last key that the pair's first token sees (may be negative)
   int kv;
+  __device__ __forceinline__ int partly() const { return max(last + 1, 0); }                          // first key that not all rows see (from `keys` on: none does)
+  __device__ __forceinline__ bool checked(int j) const { return (j + 1) * kTileKeys > partly(); }     // tile j has such keys
 };
 
 // Item `index`, decoded by a converged warp.  Items are ordered by request - of every 32 requests the one with most keys first - and in it from the last
@@ -247,6 +238,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const __grid_consta
   const uint32_t bar_loaded = bar0 + 160, bar_next = bar0 + 168;                 // all loads of an item have been asked for; an answer has come
   auto bar_full = [&](int s) { return bar0 + 176 + 8 * s; };
   auto bar_empty = [&](int s) { return bar0 + 176 + 8 * (C::kStages + s); };
+  auto bar_raw = [&](int s) { return bar0 + 176 + 8 * (2 * C::kStages + s); };   // values have landed that warp 11 checks before they are `full`
   const int tid = threadIdx.x, lane = tid & 31;
   const int warp = __shfl_sync(0xffffffffu, tid >> 5, 0);
 
@@ -258,7 +250,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const __grid_consta
   if (tid == 0) {
     for (int i = 0; i < 2; ++i) {
       mbar_init(bar_item(i), 1);
-      mbar_init(bar_itemfree(i), 256 + 2);
+      mbar_init(bar_itemfree(i), 256 + 3);
       mbar_init(bar_s(i), 1);
       mbar_init(bar_p(i), 128);
       mbar_init(bar_o(i), 1);
@@ -270,7 +262,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const __grid_consta
     mbar_init(bar_qfree, 1);
     mbar_init(bar_loaded, 1);
     mbar_init(bar_next, 1);
-    for (int s = 0; s < C::kStages; ++s) { mbar_init(bar_full(s), 1); mbar_init(bar_empty(s), 1); }
+    for (int s = 0; s < C::kStages; ++s) { mbar_init(bar_full(s), 1); mbar_init(bar_empty(s), 1); mbar_init(bar_raw(s), 1); }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   if (warp == 8) {
@@ -319,7 +311,6 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const __grid_consta
       const bool there = token < tokens && token < tile_tokens;                 // (other rows of the tile are other requests', or whatever shared memory held)
       const int least = a.causal ? min(d.last + i * tile_tokens, d.keys - 1) : d.keys - 1;       // the tile's first token
       float ref = -INFINITY;
-      bool finite = true;
       uint64_t sum2 = 0;
       for (int n = 0; n < tiles && ok; ++n) {
         const int j = tiles - 1 - n;
@@ -363,7 +354,6 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const __grid_consta
             m[c] = max3(m[c], __uint_as_float(r[c][31]), __uint_as_float(r[c][31]));
           }
           const float top = max3(max3(m[0], m[1], m[2]), m[3], m[3]) * a.scale_log2;
-          finite = finite && top < INFINITY;                               // (false for NaN)
           const bool move = need && top > ref;
           if (!__any_sync(0xffffffffu, move)) return;
           // (the products before this tile's are done - without P beside S because its scores came after them; the next one on O waits for this P)
@@ -418,7 +408,8 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const __grid_consta
       // ---- results ----
       float s0, s1;
       unpack_f2(sum2, s0, s1);
-      const float sum = s0 + s1, inv = ref == -INFINITY ? 0.f : 1.f / sum;        // (no reference: nothing was seen, or only -infinity)
+      const float sum = s0 + s1, inv = 1.f / sum;
+      const bool none = ref == -INFINITY && sum == sum;                    // nothing was seen, or only scores of -infinity
       const size_t at = (size_t)(d.row0 + tok) * a.q_heads + d.kv * group + head;
       if (tiles > 0) {
         ok = warp_wait<2>(bar_o(i), items & 1, s_abort, status);
@@ -430,11 +421,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const __grid_consta
           tmem_ld32_issue(ocol + 32 * c, o);
           tmem_ld32_wait(o);
 #pragma unroll
-          for (int e = 0; e < 32; ++e) {
-            const float x = __uint_as_float(o[e]) * inv;
-            finite = finite && fabsf(x) < INFINITY;
-            o[e] = __float_as_uint(x);
-          }
+          for (int e = 0; e < 32; ++e) o[e] = none ? 0u : __float_as_uint(__uint_as_float(o[e]) * inv);
           if (there) {
             if (a.out_kind == HYPERATTN_FP32) {
               float4* to = reinterpret_cast<float4*>(reinterpret_cast<float*>(a.out) + at * D + 32 * c);
@@ -456,18 +443,11 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const __grid_consta
         tc_fence_before();
         mbar_arrive(bar_ofree(i));
         ++items;
-        if (there) a.lse[at] = ref == -INFINITY ? -INFINITY : (ref + log2f(sum)) * 0.6931471805599453f;
+        if (there) a.lse[at] = none ? -INFINITY : (ref + log2f(sum)) * 0.6931471805599453f;
       } else if (there) {
         a.lse[at] = -INFINITY;
         const int bytes = D * (a.out_kind == HYPERATTN_FP32 ? 4 : 2);
         for (int e = 0; e < bytes; e += 16) *reinterpret_cast<uint4*>(reinterpret_cast<char*>(a.out) + at * bytes + e) = make_uint4(0, 0, 0, 0);
-      }
-      // rows that are not finite: over again, over the keys that they see
-      for (unsigned bad = __ballot_sync(0xffffffffu, there && tiles > 0 && !finite); bad; bad &= bad - 1) {
-        const int src = __ffs(bad) - 1;
-        const int t = __shfl_sync(0xffffffffu, tok, src), h = __shfl_sync(0xffffffffu, head, src), last = __shfl_sync(0xffffffffu, limit, src);
-        __syncwarp();
-        attend_row<D, T>(a, d.row0 + t, d.kv * group + h, d.key0, last + 1);
       }
       mbar_arrive(bar_itemfree(it & 1));
     }
@@ -585,6 +565,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const __grid_consta
     // ================= loads ===============================================================================
     bool ok = true;
     int ring = 0, qitems = 0, armed = 0;           // armed: tiles that have been asked for
+    uint32_t raw = 0, turns = 0;                   // by place in the ring: does the last one go through warp 11; parity of the next such one
     for (int it = 0; ok; ++it) {
       ok = item_wait(it, std::integral_constant<int, 8>{});
       if (!ok) break;
@@ -613,34 +594,26 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const __grid_consta
         if (g >= C::kStages) ok = warp_wait<10>(bar_empty(s), (g / C::kStages - 1) & 1, s_abort, status);
         if (!ok) break;
         const uint32_t dst = ubase + C::kOffRing + s * C::kTile;
-        const int have = d.keys - j * kTileKeys;                         // keys of the tile that exist
-        if ((n & 1) && have < kTileKeys) {
-          // values beyond the request's end: zeros, whatever lies there
-          const T* src = reinterpret_cast<const T*>(a.v) + (size_t)(d.key0 + j * kTileKeys) * a.v_row + (size_t)d.kv * a.v_head;
-          for (int e = lane; e < kTileKeys * (D / 8); e += 32) {
-            const int key = e / (D / 8), c = e % (D / 8);
-            cp_async16_or_zero(dst + tile_off<128>(key, c), src + (size_t)(key < have ? key : 0) * a.v_row + c * 8, key < have);
-          }
-          cp_async_commit();
-          cp_async_wait_all();
-          fence_async_smem();
-          __syncwarp();
-          if (lane == 0) mbar_arrive(bar_full(s));
-        } else if (lane == 0) {
-          mbar_expect_tx(bar_full(s), C::kTile);
+        const bool check = (n & 1) && d.checked(j);
+        const uint32_t landed = check ? bar_raw(s) : bar_full(s);
+        if (lane == 0) {
+          mbar_expect_tx(landed, C::kTile);
 #pragma unroll
           for (int sl = 0; sl < D / 64; ++sl)
-            tma_heads_tile(dst + sl * C::kSlab, (n & 1) ? &maps.v : &maps.k, sl * 64, d.kv, d.key0 + j * kTileKeys, bar_full(s));
-          mbar_arrive(bar_full(s));
+            tma_heads_tile(dst + sl * C::kSlab, (n & 1) ? &maps.v : &maps.k, sl * 64, d.kv, d.key0 + j * kTileKeys, landed);
+          mbar_arrive(landed);
         }
         armed = g + 1;
+        raw = check ? raw | 1u << s : raw & ~(1u << s);
+        turns ^= check ? 1u << s : 0u;
         __syncwarp();
       }
       if (lane == 0) mbar_arrive(bar_loaded);
       ring += 2 * d.most;
     }
     // nothing may be on its way into shared memory when the CTA ends
-    for (int s = 0; s < C::kStages && s < armed; ++s) mbar_drain(bar_full(s), ((armed - 1 - s) / C::kStages) & 1);
+    for (int s = 0; s < C::kStages && s < armed; ++s)
+      mbar_drain(raw >> s & 1 ? bar_raw(s) : bar_full(s), raw >> s & 1 ? ~(turns >> s) & 1 : ((armed - 1 - s) / C::kStages) & 1);
     if (qitems > 0) mbar_drain(bar_q, (qitems - 1) & 1);
   } else if (warp == 10) {
     // ================= items ===============================================================================
@@ -666,6 +639,62 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const __grid_consta
       if (ok) ok = next_index(asked, index);
     }
     if (asked > 0) mbar_drain(bar_next, (asked - 1) & 1);
+  } else {
+    // ================= values that are not finite ==========================================================
+    // (looked for while the weights of their tile are made)
+    bool ok = true;
+    int ring = 0;
+    uint32_t turns = 0;                  // by place in the ring: parity of the next tile
+    for (int it = 0; ok; ++it) {
+      ok = item_wait(it, std::integral_constant<int, 17>{});
+      if (!ok) break;
+      const Item d = s_item[it & 1];
+      __syncwarp();
+      if (lane == 0) mbar_arrive(bar_itemfree(it & 1));
+      if (d.end) break;
+      uint32_t add = 0;                  // some of keys that are seen
+      for (int j = d.most - 1; j >= 0 && d.checked(j); --j) {
+        const int s = (ring + 2 * (d.most - 1 - j) + 1) % C::kStages;
+        ok = warp_wait<18>(bar_raw(s), turns >> s & 1, s_abort, status);
+        if (!ok) break;
+        turns ^= 1u << s;
+        const int first = max(d.partly() - j * kTileKeys, 0), chunks = (kTileKeys - first) * 8, real = (d.keys - j * kTileKeys - first) * 8;     // (of 16 bytes, a slab)
+        // an exponent of ones carries into the sign's place
+        constexpr uint32_t kCarry = std::is_same<T, __half>::value ? 0x04000400u : 0x00800080u;
+        auto bad_of = [&](uint32_t x) { return ((x & 0x7fff7fffu) + kCarry) & 0x80008000u; };
+        uint32_t any = 0;
+        for (int sl = 0; sl < D / 64; ++sl) {
+          const uint4* at = reinterpret_cast<const uint4*>(smem + C::kOffRing + s * C::kTile + sl * C::kSlab + first * 128);
+#pragma unroll 8
+          for (int e = lane; e < chunks; e += 32) {
+            const uint4 x = at[e];
+            const uint32_t bad = bad_of(x.x) | bad_of(x.y) | bad_of(x.z) | bad_of(x.w);
+            any |= bad;
+            add |= e < real ? bad : 0u;
+          }
+        }
+        if (__any_sync(0xffffffffu, any)) {
+          for (int sl = 0; sl < D / 64; ++sl) {
+            uint32_t* at = reinterpret_cast<uint32_t*>(smem + C::kOffRing + s * C::kTile + sl * C::kSlab + first * 128);
+            for (int e = lane; e < 4 * chunks; e += 32) at[e] &= ~((bad_of(at[e]) >> 15) * 0xffffu);
+          }
+          fence_async_smem();
+        }
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar_full(s));
+      }
+      ring += 2 * d.most;
+      if (!ok || !__any_sync(0xffffffffu, add)) continue;
+      ok = warp_wait<19>(bar_itemfree(it & 1), (it >> 1) & 1, s_abort, status);                // the results have been written
+      if (!ok) break;
+      for (int r = 0; r < 2 * kTileRows; r += 32) {
+        const int i = r / kTileRows, row = r % kTileRows + lane, token = row / group, tok = i * tile_tokens + token;
+        const size_t at = (size_t)(d.row0 + tok) * a.q_heads + d.kv * group + row - token * group;
+        // (a row without weights stays zero)
+        const bool sees = token < min(i ? d.tokens[1] : d.tokens[0], tile_tokens) && a.lse[at] != -INFINITY;
+        add_unfinite<D, T>(a, d.kv, d.key0, d.partly(), sees ? min(a.causal ? d.last + tok : d.keys - 1, d.keys - 1) : -1, at);
+      }
+    }
   }
 
   // ---- teardown ----

@@ -1,4 +1,4 @@
-"""Exact attention over packed prompts where numbers come near the ends of their types: scores far apart, values that nobody may see, rows beside others."""
+"""Exact attention over packed prompts where numbers come near the ends of their types: scores far apart, values that nobody may see, rows beside others, infinities."""
 import numpy as np
 import pytest
 import torch
@@ -49,6 +49,91 @@ def test_values_of_keys_without_weight_have_no_influence(d, dtype, most):
     v[gone] = most
     out, lse = ha.prompt_attention(q, k, v, offsets([256]), out_dtype=torch.float32)
     assert torch.isfinite(out).all() and torch.equal(out, want) and torch.equal(lse, lse_want)
+
+
+def _seen_unfinite(v, n, causal):
+    """For every row and coordinate of the packed prompts: has it seen +infinity or NaN, -infinity or NaN?"""
+    up, down = ~(v < float("inf")), ~(v > -float("inf"))
+    got, at = [], 0
+    for a in n:
+        for x in (up, down):
+            x = x[at:at + a].int()
+            got.append((x.cumsum(0) > 0) if causal else (x.sum(0, keepdim=True) > 0).expand_as(x))
+        at += a
+    return torch.cat(got[0::2]), torch.cat(got[1::2])
+
+
+def _check_unfinite(v, n, causal, out, lse, clean, lse_clean):
+    group = out.shape[1] // v.shape[1]
+    up, down = (x.repeat_interleave(group, 1) for x in _seen_unfinite(v, n, causal))
+    want = torch.where(up & down, float("nan"), torch.where(up, float("inf"), -float("inf")))
+    bad = up | down
+    assert torch.equal(out[bad].nan_to_num(nan=5.0, posinf=6.0, neginf=7.0), want[bad].nan_to_num(nan=5.0, posinf=6.0, neginf=7.0))
+    assert torch.equal(out[~bad], clean[~bad]) and torch.equal(lse, lse_clean)
+    assert ha.last_device_status() == 0
+
+
+@pytest.mark.parametrize("d,G,dtype", [(64, 1, "bf16"), (64, 4, "fp16"), (128, 1, "fp16"), (128, 16, "bf16")])
+@pytest.mark.parametrize("causal", [True, False])
+def test_infinities_and_nan_reach_exactly_the_rows_that_see_them(d, G, dtype, causal):
+    n = [300, 129, 1, 0, 40, 700]
+    q, k, v = inputs(d + G, n, n, 2 * G, 2, d, dtype)
+    clean, lse_clean = ha.prompt_attention(q, k, v, offsets(n), causal=causal, out_dtype=torch.float32)
+    inf, nan = float("inf"), float("nan")
+    for places in ([(299, 0, 5, nan)], [(0, 1, 0, inf)], [(130, 0, 9, inf), (250, 0, 9, -inf), (251, 1, 33, -inf), (127, 0, 63, nan)],
+                   [(428, 0, 1, -inf), (429, 1, 2, inf), (469, 0, 3, nan), (470, 0, 3, inf)], [(470 + 127 * i, i % 2, 7 * i, (nan, inf, -inf)[i % 3]) for i in range(6)]):
+        v2 = v.clone()
+        for key, head, x, value in places:
+            v2[key, head, x] = value
+        _check_unfinite(v2, n, causal, *ha.prompt_attention(q, k, v2, offsets(n), causal=causal, out_dtype=torch.float32), clean, lse_clean)
+    v2 = v.clone()
+    v2[400:] = inf                                       # all of them, from somewhere on
+    _check_unfinite(v2, n, causal, *ha.prompt_attention(q, k, v2, offsets(n), causal=causal, out_dtype=torch.float32), clean, lse_clean)
+
+
+def test_infinities_in_many_prompts():
+    rng = np.random.default_rng(12)
+    n = rng.integers(0, 500, 150).tolist()
+    q, k, v = inputs(12, n, n, 8, 2, 64, "bf16")
+    clean, lse_clean = ha.prompt_attention(q, k, v, offsets(n), out_dtype=torch.float32)
+    for share in (1e-6, 1e-5, 1e-4):
+        v2 = torch.where(torch.tensor(rng.random(v.shape) < share, device="cuda"), float("inf"), v)
+        _check_unfinite(v2, n, True, *ha.prompt_attention(q, k, v2, offsets(n), out_dtype=torch.float32), clean, lse_clean)
+
+
+def test_a_query_that_only_sees_keys_at_minus_infinity_has_no_result_whatever_their_values():
+    q, k, v = inputs(13, [200], [200], 1, 1, 64, "bf16")
+    q = q.abs() + 0.1
+    k[:150], v[:150] = -float("inf"), float("inf")
+    out, lse = ha.prompt_attention(q, k, v, offsets([200]), out_dtype=torch.float32)
+    assert not out[:150].any() and (lse[:150] == -float("inf")).all()
+
+
+@pytest.mark.parametrize("d,dtype", [(64, "fp16"), (128, "bf16")])
+def test_one_bad_value_does_not_make_a_call_slow(d, dtype):
+    """A value that every row sees, and one in each tile of keys.  (Four times as long as without: what the clock may do, and the rows that see them.)"""
+    n = [6000]
+    q, k, v = inputs(14, n, n, 2, 1, d, dtype)
+    v2 = v.clone()
+    v2[0, 0, 3], v2[100::128, 0, 7] = float("nan"), float("inf")
+    cu = offsets(n)
+    clean, lse_clean = ha.prompt_attention(q, k, v, cu, out_dtype=torch.float32)
+    _check_unfinite(v2, n, True, *ha.prompt_attention(q, k, v2, cu, out_dtype=torch.float32), clean, lse_clean)
+
+    def time(values):
+        took = []
+        for _ in range(6):
+            a, b = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+            a.record()
+            for _ in range(5):
+                ha.prompt_attention(q, k, values, cu)
+            b.record()
+            b.synchronize()
+            took.append(a.elapsed_time(b))
+        return min(took)
+
+    once = time(v)
+    assert time(v2) <= 4 * once, (time(v2), once)
 
 
 @pytest.mark.parametrize("hq,hkv,d,dtype", [(6, 2, 64, "fp16"), (7, 1, 128, "fp16"), (5, 1, 64, "bf16"), (3, 3, 128, "bf16"), (24, 2, 64, "fp16")])
