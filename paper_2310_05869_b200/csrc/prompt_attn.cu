@@ -7,8 +7,9 @@
 //     P_i = exp2(c S_i - m)   softmax warpgroup i, a thread a row; P_i in TMEM, in the inputs' type
 //     O_i += P_i V            tcgen05.mma, P_i read from TMEM
 // The tensor pipe works for one query tile while the other one's weights are made.  The reference m of a row is the maximum of its first
-// tile; it moves when a tile's weights sum to more than 2^15, and then O is multiplied in TMEM.  Tiles with keys that a row does not see are
-// the first ones, so masks cost the later ones nothing.
+// tile (fp16: 2^7 below it, so that weights 2^-21 of the largest are still whole numbers of their type and down to 2^-32 are not nothing); it moves when a
+// tile's weights sum to more than 2^15, and then O is multiplied in TMEM.  Tiles with keys that a row does not see are the first ones, so masks cost the
+// later ones nothing.
 //
 // Values of keys that a row does not see are multiplied with zeros, which is not nothing where they are infinite or NaN.  In the tiles with such keys - of later tokens
 // of the item, and beyond the request's end - infinities and NaN of keys that not all of its rows see are set to zero before they are multiplied, and the rows that do
@@ -344,6 +345,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const __grid_consta
         // The maximum is not taken of every tile: weights are made against the reference that the row has, and only where their sum shows that one of them may be
         // too large (or a score is not a number), or there is no reference yet, the maximum is taken, the reference moved to it, and the weights are made again -
         // in rows that need it: no row's result depends on which others it shares a warp with.
+        constexpr float kBelow = std::is_same<T, __half>::value ? 7.f : 0.f;          // (128 weights of 2^7 are within the limit of a tile's sum)
         auto move_reference = [&](bool need) {
           float m[4];
 #pragma unroll
@@ -353,7 +355,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const __grid_consta
             for (int e = 3; e < 31; e += 2) m[c] = max3(m[c], __uint_as_float(r[c][e]), __uint_as_float(r[c][e + 1]));
             m[c] = max3(m[c], __uint_as_float(r[c][31]), __uint_as_float(r[c][31]));
           }
-          const float top = max3(max3(m[0], m[1], m[2]), m[3], m[3]) * a.scale_log2;
+          const float top = max3(max3(m[0], m[1], m[2]), m[3], m[3]) * a.scale_log2 - kBelow;
           const bool move = need && top > ref;
           if (!__any_sync(0xffffffffu, move)) return;
           // (the products before this tile's are done - without P beside S because its scores came after them; the next one on O waits for this P)

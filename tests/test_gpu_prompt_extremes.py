@@ -4,7 +4,7 @@ import pytest
 import torch
 
 import paper_2310_05869_b200 as ha
-from test_gpu_prompt import DT, check, inputs, offsets
+from test_gpu_prompt import DT, ROUND, check, inputs, offsets
 
 pytestmark = pytest.mark.gpu
 
@@ -49,6 +49,28 @@ def test_values_of_keys_without_weight_have_no_influence(d, dtype, most):
     v[gone] = most
     out, lse = ha.prompt_attention(q, k, v, offsets([256]), out_dtype=torch.float32)
     assert torch.isfinite(out).all() and torch.equal(out, want) and torch.equal(lse, lse_want)
+
+
+@pytest.mark.parametrize("octaves", [15.3, 20.7, 25.2])
+@pytest.mark.parametrize("d", [64, 128])
+def test_fp16_weights_of_a_long_even_rest(d, octaves):
+    """One key far above 32767 others that are alike, which have all the values: the result is the rest's.  A weight is an fp16 number that may be 2^-25 off
+    where it is small, beside a largest one of 2^7: 2^-32 of the values that are summed; otherwise weights and their sum are 2^-12 off."""
+    n = 32768
+    gen = torch.Generator("cuda").manual_seed(d)
+    for place in (n - 1, 5):
+        k = torch.zeros(n, 1, d, device="cuda", dtype=torch.float16)
+        k[place] = octaves * np.log(2) / (4 * d ** 0.5)
+        v = (100 + torch.randn(n, 1, d, generator=gen, device="cuda")).half()
+        v[place] = 0
+        q = torch.full((1, 1, d), 4.0, device="cuda", dtype=torch.float16)
+        out, lse = ha.prompt_attention(q, k, v, offsets([1]), offsets([n]), out_dtype=torch.float32)
+        z = (k[:, 0].double() @ q[0, 0].double()) / d ** 0.5
+        w = torch.softmax(z, 0)
+        want = w @ v[:, 0].double()
+        bound = (2 * ROUND["fp16"] + 2 ** -16 * float(z.max()) + 1e-5) * want + 2.0 ** -32 * (v[:, 0].double().sum(0))
+        assert ((out[0, 0].double() - want).abs() <= bound).all(), (place, float(((out[0, 0].double() - want) / want).abs().max()))
+        assert abs(float(lse[0, 0]) - float(torch.logsumexp(z, 0))) <= 2.0 ** -17 * float(z.max()) + 1e-5
 
 
 def _seen_unfinite(v, n, causal):
