@@ -1,4 +1,4 @@
-"""Exact attention over packed prompts where numbers come near the ends of their types: scores far apart, values that nobody may see, rows beside others, infinities."""
+"""Exact attention over packed prompts where numbers come near the ends of their types: scores far apart, values that nobody may see, rows beside others, infinities, long contexts."""
 import numpy as np
 import pytest
 import torch
@@ -71,6 +71,29 @@ def test_fp16_weights_of_a_long_even_rest(d, octaves):
         bound = (2 * ROUND["fp16"] + 2 ** -16 * float(z.max()) + 1e-5) * want + 2.0 ** -32 * (v[:, 0].double().sum(0))
         assert ((out[0, 0].double() - want).abs() <= bound).all(), (place, float(((out[0, 0].double() - want) / want).abs().max()))
         assert abs(float(lse[0, 0]) - float(torch.logsumexp(z, 0))) <= 2.0 ** -17 * float(z.max()) + 1e-5
+
+
+@pytest.mark.parametrize("mean", [0.0, 1.0])
+@pytest.mark.parametrize("hq,hkv,d,dtype", [(2, 2, 64, "fp16"), (4, 1, 128, "bf16"), (2, 1, 128, "fp16"), (1, 1, 64, "bf16")])
+def test_131072_keys_relative_to_the_result(hq, hkv, d, dtype, mean):
+    """The context of the headline configuration.  A result over so many values is a few hundred times smaller than they are: errors are held to the result.
+    Weights are rounded to the type, independently of each other, and once as a sum; O is one chain of 8 x 1024 products, and the tensor cores cut what
+    they add (up to 2^-23 of O each): 2^-10 together."""
+    n, past = 131072 + 77, 131072 - 123
+    gen = torch.Generator("cuda").manual_seed(d + hq)
+    q = torch.randn(200, hq, d, generator=gen, device="cuda").to(DT[dtype])
+    k, v = (torch.randn(n, hkv, d, generator=gen, device="cuda") for _ in range(2))
+    k, v = k.to(DT[dtype]), (v + mean).to(DT[dtype])
+    out, lse = ha.prompt_attention(q, k, v, offsets([200]), offsets([n]), out_dtype=torch.float32)
+    assert past + 200 == n
+    for i in (0, 1, 63, 128, 199):
+        for h in range(hq):
+            g = h // (hq // hkv)
+            z = k[:past + i + 1, g].double() @ q[i, h].double() / d ** 0.5
+            want = torch.softmax(z, 0) @ v[:past + i + 1, g].double()
+            err = float((out[i, h].double() - want).norm() / want.norm())
+            assert err <= 2 * ROUND[dtype] + 2.0 ** -10, (i, h, err)
+            assert abs(float(lse[i, h]) - float(torch.logsumexp(z, 0))) <= 1e-4
 
 
 def _seen_unfinite(v, n, causal):
