@@ -362,7 +362,8 @@ typedef struct hyperattn_cache {
  *   cu_lengths        [requests + 1]  their running sum
  *   table_out         [requests, table_width], unused entries -1
  *   free_out, n_free_out              the stack after the step, [num_free], unused entries -1
- * requests <= HYPERATTN_PLAN_MAX_REQUESTS; table_width * page_tokens < 2^31. */
+ * requests <= HYPERATTN_PLAN_MAX_REQUESTS; table_width * page_tokens < 2^31, table_width < 2^28, requests * table_width + num_free < 2^31.
+ * Sums of tokens that pass 2^31 - 1 (cu_new, cu_lengths) are given as that. */
 #define HYPERATTN_PLAN_MAX_REQUESTS 4096
 typedef struct hyperattn_plan {
   const int32_t *lengths, *new_tokens, *table, *free_pages, *n_free;

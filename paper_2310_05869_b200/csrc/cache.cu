@@ -15,6 +15,26 @@ constexpr int kPlanThreads = 512, kPlanWarps = kPlanThreads / 32, kPlanColumns =
 
 struct PlanParts { int tables, rows, stack; };           // CTAs for each
 
+// a + b of two numbers that are not negative, 2^31 - 1 at most (what requests bring may be any numbers; sums of pages cannot get there)
+__device__ __forceinline__ int plus(int a, int b) { return (int)min((unsigned)a + (unsigned)b, 0x7fffffffu); }
+// Of the threads' numbers x[q]: the sums of those before this thread's, in their place.  All threads together.
+template <int N>
+__device__ __forceinline__ void sums_before(int (&x)[N], int (*s_warp)[kPlanWarps]) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+#pragma unroll
+  for (int q = 0; q < N; ++q) {
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) { const int y = __shfl_up_sync(0xffffffffu, x[q], o); if (lane >= o) x[q] = plus(x[q], y); }
+    if (lane == 31) s_warp[q][warp] = x[q];
+    x[q] = __shfl_up_sync(0xffffffffu, x[q], 1);
+    if (lane == 0) x[q] = 0;
+  }
+  __syncthreads();
+#pragma unroll
+  for (int q = 0; q < N; ++q)
+    for (int w = 0; w < warp; ++w) x[q] = plus(x[q], s_warp[q][w]);
+}
+
 __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const __grid_constant__ hyperattn_plan p, PlanParts parts) {
   extern __shared__ int smem[];
   __shared__ int s_warp[3][kPlanWarps], s_given;
@@ -35,25 +55,13 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const __grid_constan
     const long long pages = ((long long)len + max(add, 0) + P - 1) / P;
     const bool ended = add < 0, fits = !ended && pages <= W;
     const int need = fits ? max((int)pages - have, 0) : 0;
-    sum[0] += max(add, 0); sum[1] += need; sum[2] += ended ? have : 0;
+    sum[0] = plus(sum[0], max(add, 0)); sum[1] += need; sum[2] += ended ? have : 0;
     s_add[r] = sum[0]; s_need[r] = sum[1]; s_rel[r] = sum[2];
     s_have[r] = have | (fits ? 1 << 29 : 0) | (ended ? 1 << 30 : 0);
     s_len[r] = len;
   }
-  int base[3];
-#pragma unroll
-  for (int q = 0; q < 3; ++q) {
-    int x = sum[q];
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) { const int y = __shfl_up_sync(0xffffffffu, x, o); if (lane >= o) x += y; }
-    if (lane == 31) s_warp[q][warp] = x;
-    base[q] = x - sum[q];
-  }
-  __syncthreads();
-#pragma unroll
-  for (int q = 0; q < 3; ++q)
-    for (int w = 0; w < warp; ++w) base[q] += s_warp[q][w];
-  for (int r = r0; r < r1; ++r) { s_add[r] += base[0]; s_need[r] += base[1]; s_rel[r] += base[2]; }
+  sums_before(sum, s_warp);
+  for (int r = r0; r < r1; ++r) { s_add[r] = plus(s_add[r], sum[0]); s_need[r] += sum[1]; s_rel[r] += sum[2]; }
   __syncthreads();
   const int total = n_free + s_rel[R - 1];             // pages on the stack before any is taken
 
@@ -128,24 +136,18 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const __grid_constan
     return;
   }
   // the requests' state
-  int len_sum = 0;
-  auto length_after = [&](int r) { return ended(r) ? 0 : admitted(r) ? s_len[r] + s_add[r] - before(s_add, r) : s_len[r]; };
+  int run[1] = {0};
+  auto length_after = [&](int r) { return ended(r) ? 0 : admitted(r) ? s_len[r] + p.new_tokens[r] : s_len[r]; };
   for (int r = r0; r < r1; ++r) {
     const int out = length_after(r);
     p.lengths_out[r] = out;
     p.cu_new[r + 1] = s_add[r];
-    len_sum += out;
+    run[0] = plus(run[0], out);
   }
-  int x = len_sum;
-#pragma unroll
-  for (int o = 1; o < 32; o <<= 1) { const int y = __shfl_up_sync(0xffffffffu, x, o); if (lane >= o) x += y; }
-  if (lane == 31) s_warp[0][warp] = x;
-  __syncthreads();
-  int run = x - len_sum;
-  for (int w = 0; w < warp; ++w) run += s_warp[0][w];
+  sums_before(run, s_warp);
   for (int r = r0; r < r1; ++r) {
-    run += length_after(r);
-    p.cu_lengths[r + 1] = run;
+    run[0] = plus(run[0], length_after(r));
+    p.cu_lengths[r + 1] = run[0];
   }
   if (tid == 0) { p.cu_new[0] = 0; p.cu_lengths[0] = 0; p.n_free_out[0] = left; }
 }
@@ -530,7 +532,9 @@ using namespace hyperattn;
 
 extern "C" int hyperattn_cache_plan(const hyperattn_plan* p) {
   if (!p || p->requests < 0 || p->table_width <= 0 || p->num_free < 0 || p->rows < 0 || p->page_tokens <= 0) return HYPERATTN_INVALID_ARGUMENT;
-  if (p->requests > HYPERATTN_PLAN_MAX_REQUESTS || (long long)p->table_width * p->page_tokens > 0x7fffffffLL) return HYPERATTN_UNSUPPORTED_SHAPE;
+  if (p->requests > HYPERATTN_PLAN_MAX_REQUESTS || (long long)p->table_width * p->page_tokens > 0x7fffffffLL || p->table_width >= 1 << 28 ||
+      (long long)p->requests * p->table_width + p->num_free > 0x7fffffffLL)
+    return HYPERATTN_UNSUPPORTED_SHAPE;
   if (p->requests == 0) return HYPERATTN_OK;
   if (!p->lengths || !p->new_tokens || !p->table || (p->num_free && (!p->free_pages || !p->free_out)) || !p->n_free || (p->rows && (!p->slots || !p->positions)) ||
       !p->cu_new || !p->cu_lengths || !p->lengths_out || !p->table_out || !p->n_free_out)

@@ -1,4 +1,4 @@
-"""Attention over the 4-bit cache where numbers come near the ends of their types."""
+"""The paged 4-bit cache where numbers come near the ends of their types."""
 import numpy as np
 import pytest
 import torch
@@ -46,3 +46,22 @@ def test_values_of_several_scales_under_small_weights(d, dtype, heads, size, nan
     bound = (2.0 ** -11 + 2.0 ** -15 * float(z.max()) + 1e-5) * size_of
     assert ((out.double() - want).abs() <= bound)[:, :, ~bad].all(), float(((out.double() - want).abs() / size_of)[:, :, ~bad].max())
     assert (lse.double() - torch.logsumexp(z, 1)[:, None]).abs().max() <= 1e-4
+
+
+def test_a_plan_of_more_new_tokens_than_an_int_counts():
+    """Requests that bring 2^31 - 1 tokens have no room and are not admitted; their tokens count, up to 2^31 - 1, and push the others' out of the batch."""
+    most = 2 ** 31 - 1
+    for R, at in ((6, 0), (600, 500)):                   # (in one thread's share, and far behind others)
+        lens, new, table = np.zeros(R, np.int64), np.zeros(R, np.int64), np.full((R, 4), -1)
+        lens[at:at + 6], new[at:at + 6] = [3, 0, 40, 1, most, most], [5, most, 7, most, 2, -1]
+        table[at, 0], table[at + 2, :3], table[at + 3, 0], table[at + 4], table[at + 5] = 0, [1, 2, 3], 4, [5, 6, 7, 8], [9, 10, 11, 12]
+        free = np.concatenate([np.arange(20, 30), [-1] * 6])
+        got = ha.cache_plan(ints(lens), ints(new), ints(table), ints(free), ints([10]), 16, 12)
+        assert got.slots.cpu().tolist() == [3, 4, 5, 6, 7] + [-1] * 7 and got.positions.cpu().tolist() == [3, 4, 5, 6, 7] + [-1] * 7
+        assert got.cu_new.cpu().tolist()[at:at + 7] == [0, 5] + [most] * 5 and got.cu_new.cpu().tolist()[-1] == most
+        assert got.lengths.cpu().tolist()[at:at + 6] == [8, 0, 47, 1, most, 0]
+        assert got.cu_len.cpu().tolist()[at:at + 7] == [0, 8, 8, 55, 56, most, most]
+        want = table.copy()
+        want[at + 5] = -1
+        assert np.array_equal(got.table.cpu().numpy(), want)          # (47 tokens fit the three pages that there were)
+        assert int(got.n_free) == 14 and got.free.cpu().tolist() == [*range(20, 30), 9, 10, 11, 12, -1, -1]

@@ -116,3 +116,8 @@ def test_the_plain_statements():
     assert not out[0].any() and lse[0] == -np.inf and np.allclose(out[1], [0.5, 0.5, 0, 0]) and np.isclose(lse[1], np.log(2))
     got = SU.plan([3, 20], [1, -1], [[5, -1], [6, 7]], [8, -1, -1], 1, 16, 3)
     assert got["table"] == [[5, -1], [-1, -1]] and got["slots"] == [83, -1, -1] and got["free"] == [8, 6, 7] and got["n_free"] == [3]
+
+
+@pytest.mark.parametrize("kw,code", [(dict(page_tokens=1, table_width=1 << 28), -2), (dict(requests=4096, table_width=1 << 19), -2), (dict(requests=1, table_width=1 << 20, num_free=(1 << 31) - (1 << 20)), -2)])
+def test_plans_whose_pages_do_not_fit_an_int(kw, code):
+    assert S._lib().hyperattn_cache_plan(C.byref(plan(**kw))) == code
