@@ -449,7 +449,8 @@ __device__ __forceinline__ void bulk_copy(uint32_t dst, const void* src, uint32_
   asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
 }
 template <int D> __device__ __forceinline__ int units_of(const CacheAttnArgs& a, int r) {
-  return (min(max(a.lengths[r], 0), a.width * a.cache.page) + Ring<D>::kUnitTokens - 1) / Ring<D>::kUnitTokens;
+  const int tokens = min(max(a.lengths[r], 0), a.width * a.cache.page);        // (up to 2^31 - 1)
+  return tokens / Ring<D>::kUnitTokens + (tokens % Ring<D>::kUnitTokens != 0);
 }
 // where the pieces of a segment lie: see combine
 __device__ __forceinline__ float* piece_at(const CacheAttnArgs& a, long long slot, int head, int d) { return a.part + (slot * a.part_heads + head) * (d + 2); }

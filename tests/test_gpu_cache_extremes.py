@@ -65,3 +65,20 @@ def test_a_plan_of_more_new_tokens_than_an_int_counts():
         want[at + 5] = -1
         assert np.array_equal(got.table.cpu().numpy(), want)          # (47 tokens fit the three pages that there were)
         assert int(got.n_free) == 14 and got.free.cpu().tolist() == [*range(20, 30), 9, 10, 11, 12, -1, -1]
+
+
+def test_attention_of_a_length_that_fills_the_longest_table():
+    """2^31 - 16 tokens, of which 200 exist: the other pages of the table do not."""
+    gen = torch.Generator("cuda").manual_seed(1)
+    for d, dtype in ((64, "fp16"), (128, "bf16")):
+        cache = ha.cache_pages(20, 1, d, 16)
+        k, v = (torch.randn(200, 1, d, generator=gen, device="cuda").to(DT[dtype]) for _ in range(2))
+        ha.cache_store(cache, k, v, ints(np.arange(200)))
+        width = (1 << 27) - 1
+        table = torch.full((1, width), -1, dtype=torch.int32, device="cuda")
+        table[0, :6], table[0, -7:-1] = ints(np.arange(6)), ints(np.arange(6, 12))
+        q = torch.randn(1, 2, d, generator=gen, device="cuda").to(DT[dtype])
+        want = ha.cache_attention(q, cache, ints(np.arange(12))[None], ints([192]), out_dtype=torch.float32)
+        got = ha.cache_attention(q, cache, table, ints([2 ** 31 - 1]), out_dtype=torch.float32)
+        assert (got[0] - want[0]).abs().max() <= 2.0 ** -10 * want[0].abs().max() and (got[1] - want[1]).abs().max() <= 1e-5
+        assert ha.last_device_status() == 0
