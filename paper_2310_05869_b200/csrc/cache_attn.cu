@@ -490,7 +490,7 @@ __global__ void __launch_bounds__(32 * kWarps, ctas_by_registers(NT)) cache_attn
   if (tid == 32 * kWarps - 1) s_starts[a.requests] = run + mine;
   __syncthreads();
   const int segs = a.cache.heads * a.chunks;                             // of a request
-  const int total = s_starts[a.requests] * segs, warps = gridDim.x * kWarps, part = max(1, (total + warps - 1) / warps);
+  const int total = s_starts[a.requests] * segs, warps = gridDim.x * kWarps, part = max(1, total / warps + (total % warps != 0));
   if (blockIdx.x == 0) {
     for (int r = tid; r <= a.requests; r += 32 * kWarps) a.starts[r] = s_starts[r];
     if (tid == 0) a.starts[a.requests + 1] = part;

@@ -82,3 +82,19 @@ def test_attention_of_a_length_that_fills_the_longest_table():
         got = ha.cache_attention(q, cache, table, ints([2 ** 31 - 1]), out_dtype=torch.float32)
         assert (got[0] - want[0]).abs().max() <= 2.0 ** -10 * want[0].abs().max() and (got[1] - want[1]).abs().max() <= 1e-5
         assert ha.last_device_status() == 0
+
+
+def test_attention_of_nearly_as_many_units_as_an_int_counts():
+    """64 heads over nearly 2^30 tokens, of which 70 exist, in the last page of the table."""
+    gen = torch.Generator("cuda").manual_seed(2)
+    d, heads, page, width = 128, 64, 1024, (1 << 20) - 1
+    cache = ha.cache_pages(1, heads, d, page)
+    k, v = (torch.randn(70, heads, d, generator=gen, device="cuda").bfloat16() for _ in range(2))
+    ha.cache_store(cache, k, v, ints(np.arange(70)))
+    table = torch.full((1, width), -1, dtype=torch.int32, device="cuda")
+    table[0, -1] = 0
+    q = torch.randn(1, heads, d, generator=gen, device="cuda").bfloat16()
+    want = ha.cache_attention(q, cache, ints([[0]]), ints([70]), out_dtype=torch.float32)
+    got = ha.cache_attention(q, cache, table, ints([(width - 1) * page + 70]), out_dtype=torch.float32)
+    assert (got[0] - want[0]).abs().max() <= 2.0 ** -10 * want[0].abs().max() and (got[1] - want[1]).abs().max() <= 1e-5
+    assert ha.last_device_status() == 0
