@@ -110,6 +110,35 @@ def _call(fn, what, device, *args):
     _check(rc, what)
 
 
+def _tensors(x):
+    """The CUDA tensors of arguments or results."""
+    if isinstance(x, torch.Tensor):
+        return [x] if x.is_cuda else []
+    if isinstance(x, dict):
+        x = tuple(x.values())
+    return [t for y in x for t in _tensors(y)] if isinstance(x, (tuple, list)) else []
+
+
+def _on_stream(stream, fn, *args, **kw):
+    """fn(...) with the stream of a handle as torch's current one, so that the copies and fills that it enqueues come before its kernels, and the memory that it
+    takes is that stream's; the allocator keeps the arguments for it, and the results for the stream that is current outside."""
+    given = _tensors((args, kw))
+    if not given:
+        return fn(*args, **kw)
+    device = given[0].device
+    here = torch.cuda.current_stream(device)
+    if here.cuda_stream == stream:
+        return fn(*args, **kw)
+    there = torch.cuda.ExternalStream(stream, device=device)
+    with torch.cuda.stream(there):
+        got = fn(*args, **kw)
+    for t in given:
+        t.record_stream(there)
+    for t in _tensors(got):
+        t.record_stream(here)
+    return got
+
+
 def _dtype_code(t: torch.dtype) -> int:
     if t == torch.bfloat16:
         return BF16

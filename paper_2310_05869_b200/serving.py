@@ -1,7 +1,8 @@
 """Binding of the serving entry points: exact attention over packed prompts, and a paged cache that holds keys and values in
 4 bits, with its scheduling.  Argument marshalling only, like `binding.py`; lengths, tables and slots are int32 CUDA tensors
-that only the kernels read, so nothing here waits for the GPU.  `stream`: the handle of a stream to enqueue on instead of torch's current one
-(which the caller orders with it).
+that only the kernels read, so nothing here waits for the GPU.  `stream`: the handle of a stream to do all of the call on instead of torch's current
+one - copies of tensors whose strides do not suit and the memory of results included, as if it were the current one.  The caller orders it with what makes
+the arguments and what uses the results; their memory is kept for both streams.
 
 A cache is a uint8 tensor [pages, kv_heads, page_tokens / 16, 20 d] (`cache_pages` makes one; include/hyperattn.h has the order of
 its bytes).  A decode step of a server:
@@ -19,7 +20,7 @@ from typing import NamedTuple
 
 import torch
 
-from .binding import BF16, FP32, HyperAttnError, _check, lib
+from .binding import BF16, FP32, HyperAttnError, _check, _on_stream, lib
 
 FP16 = 2
 _CODES = {torch.bfloat16: BF16, torch.float16: FP16, torch.float32: FP32}
@@ -89,15 +90,7 @@ def _call(name, index, *args):
         _check(rc, name)
 
 
-def _stream(index, stream):
-    return torch._C._cuda_getCurrentRawStream(index) if stream is None else stream
-
-
-def _used(stream, device, *tensors):
-    """Tensors that a call on a stream of the caller's uses and this module has made or may let go: the allocator waits for that stream."""
-    other = torch.cuda.ExternalStream(stream, device=device)
-    for t in tensors:
-        t.record_stream(other)
+_stream = torch._C._cuda_getCurrentRawStream
 
 
 def _new(shape, dtype, device):
@@ -161,6 +154,8 @@ def cache_plan(lengths, new, table, free, n_free, page_tokens, rows, stream=None
     """One scheduling step: hands pages to the requests' new tokens, takes back those of ended requests (new < 0), and says where
     every token of the packed batch of `rows` rows goes.  lengths, new [requests], table [requests, width], free [any], n_free [1]:
     int32 CUDA tensors, not changed.  Requests whose pages cannot be had keep their length and get no slots.  Returns a CachePlan."""
+    if stream is not None:
+        return _on_stream(stream, cache_plan, lengths, new, table, free, n_free, page_tokens, rows)
     if not lengths.is_cuda:
         raise HyperAttnError("lengths must be a CUDA tensor (there is no CPU path)")
     index = lengths.get_device()
@@ -181,15 +176,15 @@ def cache_plan(lengths, new, table, free, n_free, page_tokens, rows, stream=None
     _call("hyperattn_cache_plan", index, _plan_bytes(
         lengths.data_ptr(), new.data_ptr(), table.data_ptr(), free.data_ptr(), n_free.data_ptr(), R, W, F, page_tokens, rows,
         at, at + 4 * rows, at + 8 * rows, at + 4 * (2 * rows + R + 1), at + 4 * (2 * rows + 2 * R + 2), table_out.data_ptr(),
-        stack, at + 4 * (2 * rows + 3 * R + 2), _stream(index, stream)))
-    if stream is not None:
-        _used(stream, flat.device, flat, table_out)
+        stack, at + 4 * (2 * rows + 3 * R + 2), _stream(index)))
     free_out, slots, positions, cu_new, cu_len, lengths_out, n_free_out = torch.unsafe_split_with_sizes(flat, (F, rows, rows, R + 1, R + 1, R, 1))
     return CachePlan(slots, positions, cu_new, cu_len, lengths_out, table_out, free_out, n_free_out)
 
 
 def cache_store(cache, k, v, slots, stream=None):
     """Puts k, v [rows, kv_heads, d] (bf16 or fp16, any strides) into the cache's slots [rows] (int32; negative: left out)."""
+    if stream is not None:
+        return _on_stream(stream, cache_store, cache, k, v, slots)
     c = _cache_of(cache)
     index = cache.get_device()
     _ints(index, slots)
@@ -200,14 +195,14 @@ def cache_store(cache, k, v, slots, stream=None):
     k, k_row, k_head = _rows(k)
     v, v_row, v_head = _rows(v)
     _call("hyperattn_cache_store", index, _cache_bytes(*c), k.data_ptr(), v.data_ptr(), _code(k.dtype, "k"), k.shape[0], k_row, k_head, v_row, v_head,
-          slots.data_ptr(), _stream(index, stream))
-    if stream is not None:
-        _used(stream, cache.device, k, v)
+          slots.data_ptr(), _stream(index))
 
 
 def cache_read(cache, table, cu, rows, first=None, dtype=torch.bfloat16, stream=None):
     """K and V [rows, kv_heads, d] of cached tokens: rows cu[r] .. cu[r + 1] - 1 are tokens first[r] (default 0), first[r] + 1, ... of
     request r; table [requests, width], cu [requests + 1], first [requests]: int32.  What is not in the cache reads as zeros."""
+    if stream is not None:
+        return _on_stream(stream, cache_read, cache, table, cu, rows, first, dtype)
     c = _cache_of(cache)
     index = cache.get_device()
     _ints(index, table, cu)
@@ -221,9 +216,7 @@ def cache_read(cache, table, cu, rows, first=None, dtype=torch.bfloat16, stream=
     k = _new((rows, c[3], c[4]), dtype, cache.device)
     v = torch.empty_like(k)
     _call("hyperattn_cache_read", index, _cache_bytes(*c), table.data_ptr(), R, W, cu.data_ptr(), None if first is None else first.data_ptr(), rows,
-          k.data_ptr(), v.data_ptr(), _code(dtype, "the result"), _stream(index, stream))
-    if stream is not None:
-        _used(stream, cache.device, k, v)
+          k.data_ptr(), v.data_ptr(), _code(dtype, "the result"), _stream(index))
     return k, v
 
 
@@ -242,6 +235,8 @@ def cache_attention(q, cache, table, lengths, scale=0.0, out_dtype=None, stream=
     """Attention of one query token a request, q [requests, q_heads, d] (bf16 or fp16, any strides), over its cached tokens
     0 .. lengths[r] - 1.  table [requests, width], lengths [requests]: int32.  Returns (out [requests, q_heads, d], lse
     [requests, q_heads]); a request without tokens gets zeros and -inf."""
+    if stream is not None:
+        return _on_stream(stream, cache_attention, q, cache, table, lengths, scale, out_dtype)
     c = _cache_of(cache)
     index = cache.get_device()
     _ints(index, table, lengths)
@@ -261,9 +256,7 @@ def cache_attention(q, cache, table, lengths, scale=0.0, out_dtype=None, stream=
     work = _new((size,), torch.uint8, device)
     _call("hyperattn_cache_attention", index, _attention_bytes(
         *c, q.data_ptr(), row, head, out.data_ptr(), lse.data_ptr(), table.data_ptr(), lengths.data_ptr(), R, W, H, dtype, out_code, scale,
-        work.data_ptr(), size, _stream(index, stream)))
-    if stream is not None:
-        _used(stream, device, q, out, lse, work)
+        work.data_ptr(), size, _stream(index)))
     return out, lse
 
 
@@ -272,6 +265,8 @@ def prompt_attention(q, k, v, cu_q, cu_k=None, causal=True, scale=0.0, out_dtype
     queries are rows cu_q[r] .. cu_q[r + 1] - 1, its keys rows cu_k[r] .. cu_k[r + 1] - 1 (default: those of the queries).  causal: a
     request's last query sees all its keys, every earlier one a key less.  Returns (out [q_rows, q_heads, d], lse [q_rows,
     q_heads]); a query that sees no key gets zeros and -inf, rows beyond cu_q[-1] are not written."""
+    if stream is not None:
+        return _on_stream(stream, prompt_attention, q, k, v, cu_q, cu_k, causal, scale, out_dtype)
     if not q.is_cuda:
         raise HyperAttnError("q, k, v must be CUDA tensors (there is no CPU path)")
     index = q.get_device()
@@ -295,7 +290,5 @@ def prompt_attention(q, k, v, cu_q, cu_k=None, causal=True, scale=0.0, out_dtype
     lse = _new((T, H), torch.float32, device)
     _call("hyperattn_prompt_attention", index, _prompt_bytes(
         q.data_ptr(), k.data_ptr(), v.data_ptr(), q_row, q_head, k_row, k_head, v_row, v_head, out.data_ptr(), lse.data_ptr(), cu_q.data_ptr(),
-        cu_k.data_ptr(), cu_q.shape[0] - 1, T, k_rows, H, kv_heads, d, 1 if causal else 0, dtype, out_code, scale, _stream(index, stream)))
-    if stream is not None:
-        _used(stream, device, q, k, v, out, lse)
+        cu_k.data_ptr(), cu_q.shape[0] - 1, T, k_rows, H, kv_heads, d, 1 if causal else 0, dtype, out_code, scale, _stream(index)))
     return out, lse

@@ -1,0 +1,78 @@
+"""Calls on a stream of the caller's while torch's current one is busy: nothing of theirs may wait for it, or run on it."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2310_05869_b200 as ha
+
+pytestmark = pytest.mark.gpu
+
+
+def ints(x):
+    return torch.tensor(np.asarray(x), dtype=torch.int32, device="cuda")
+
+
+def check(call, after=None):
+    """call(**kw) -> tensors; after(): what the call has changed."""
+    got = call()
+    want = [x.clone() for x in (after() if after else got)]
+    side = torch.cuda.Stream()
+    for x in (after() if after else ()):
+        x.zero_()
+    torch.cuda.synchronize()
+    torch.cuda._sleep(400_000_000)                       # some tenths of a second
+    got = call(stream=side.cuda_stream)
+    with torch.cuda.stream(side):
+        got = [x.clone() for x in (after() if after else got)]
+    side.synchronize()
+    assert not torch.cuda.current_stream().query()       # the current stream has not been waited for
+    torch.cuda.synchronize()
+    assert len(got) == len(want) and all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+# strides that a call has to copy for: an odd address, rows that are all the same one, coordinates that are not next to each other
+def odd(x):
+    wide = torch.zeros(*x.shape[:-1], x.shape[-1] + 1, dtype=x.dtype, device=x.device)
+    wide[..., 1:] = x
+    return wide[..., 1:]
+
+
+COPIES = {"odd": odd, "one row": lambda x: x[:1].expand_as(x), "turned": lambda x: x.transpose(-1, -2).contiguous().transpose(-1, -2)}
+
+
+@pytest.mark.parametrize("kind", list(COPIES))
+@pytest.mark.parametrize("d", [64, 128])
+def test_tensors_that_are_copied(kind, d):
+    make = COPIES[kind]
+    T, H, page = 3000, 4, 64
+    q, k, v = (make(torch.randn(T, H, d, device="cuda").bfloat16()) for _ in range(3))
+    cu = ints([0, 1000, 3000])
+    check(lambda **kw: ha.prompt_attention(q, k, v, cu, **kw))
+    cache = ha.cache_pages(T // page + 1, H, d, page)
+    slots = ints(np.arange(T))
+    check(lambda **kw: ha.cache_store(cache, k, v, slots, **kw), lambda: [cache])
+    table, lengths = ints(np.arange(T // page))[None].repeat(40, 1), ints(np.arange(40) * 60)
+    check(lambda **kw: ha.cache_attention(q[:40], cache, table, lengths, **kw))
+    rows = ints(np.arange(41) * 50)
+    check(lambda **kw: ha.cache_read(cache, table, rows, 2000, **kw))
+
+
+def test_plans_of_some_requests_and_of_none():
+    rng = np.random.default_rng(0)
+    for R in (0, 5):
+        lengths, new, table = ints(rng.integers(0, 40, R)), ints(rng.integers(-1, 9, R)), ints(np.arange(R * 4).reshape(R, 4))
+        free, n_free = ints(np.arange(30, 60)), ints([30])
+        check(lambda **kw: ha.cache_plan(lengths, new, table, free, n_free, 16, 50, **kw))
+
+
+def test_the_default_stream_from_another_one():
+    q, k, v = (torch.randn(500, 2, 64, device="cuda").bfloat16() for _ in range(3))
+    cu = ints([0, 500])
+    want = ha.prompt_attention(q, k, v, cu)
+    torch.cuda.synchronize()
+    with torch.cuda.stream(torch.cuda.Stream()):
+        q = odd(q)
+        torch.cuda.synchronize()
+        got = ha.prompt_attention(q, k, v, cu, stream=torch.cuda.default_stream().cuda_stream)
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(want, got))
