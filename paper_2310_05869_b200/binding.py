@@ -177,7 +177,11 @@ def forward(q, k, v, block, samples, hash_bits, causal=False, n0=0, seed=0, out_
             node_directions=False):
     """HyperAttention forward on CUDA tensors q [B, H, n, d] and k, v [B, H, n_k, d] (bf16 or fp32).
     caps = (cap_scale, kappa) runs the row-sum estimate with the caps of Alg. 2.
+    `stream`: the handle of a stream to do all of the call on, copies of its tensors included, instead of torch's current one; so for the functions below.
     Returns (out, lse) or (out, lse, intermediates) when debug=True."""
+    if stream is not None:
+        return _on_stream(stream, forward, q, k, v, block, samples, hash_bits, causal, n0, seed, out_dtype, scale, workspace, debug,
+                          precise=precise, caps=caps, value_norm_sampling=value_norm_sampling, node_directions=node_directions)
     if not (q.is_cuda and k.is_cuda and v.is_cuda):
         raise HyperAttnError("q, k, v must be CUDA tensors (there is no CPU path)")
     q, k, v = q.contiguous(), k.contiguous(), v.contiguous()
@@ -193,7 +197,7 @@ def forward(q, k, v, block, samples, hash_bits, causal=False, n0=0, seed=0, out_
     ws, ws_bytes = (None, 0) if workspace is None else (workspace.data_ptr(), workspace.numel() * workspace.element_size())
     p = _Params(q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), lse.data_ptr(), B, H, n, d, block, samples, hash_bits,
                 1 if causal else 0, n0, seed, _dtype_code(q.dtype), _dtype_code(out_dtype), scale, ws, ws_bytes, None,
-                _raw_stream(dev) if stream is None else stream, 1 if precise else 0, 0 if n_k == n else n_k, capped, cap_scale, kappa,
+                _raw_stream(dev), 1 if precise else 0, 0 if n_k == n else n_k, capped, cap_scale, kappa,
                 1 if value_norm_sampling else 0, 1 if node_directions else 0)
     inter = None
     if debug:
@@ -225,6 +229,8 @@ def backward(q, k, v, out, lse, dout, block, samples, hash_bits, causal=False, n
              stream=None):
     """Backward pass of `forward` (same shape arguments and seed as the forward call; out and lse are its
     results).  q, k, v, dout: bf16 CUDA tensors [B, H, n, d].  Returns (dq, dk, dv) of grad_dtype (default bf16)."""
+    if stream is not None:
+        return _on_stream(stream, backward, q, k, v, out, lse, dout, block, samples, hash_bits, causal, n0, seed, grad_dtype, scale)
     if not all(t.is_cuda for t in (q, k, v, out, lse, dout)):
         raise HyperAttnError("all tensors must be CUDA tensors (there is no CPU path)")
     q, k, v, out, lse, dout = (t.contiguous() for t in (q, k, v, out, lse, dout))
@@ -234,7 +240,7 @@ def backward(q, k, v, out, lse, dout, block, samples, hash_bits, causal=False, n
     dq, dk, dv = (torch.empty((B, H, n, d), dtype=grad_dtype, device=dev) for _ in range(3))
     p = _Params(q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), lse.data_ptr(), B, H, n, d, block, samples, hash_bits,
                 1 if causal else 0, n0, seed, _dtype_code(q.dtype), _dtype_code(out.dtype), scale, None, 0, None,
-                _raw_stream(dev) if stream is None else stream)
+                _raw_stream(dev))
     g = _Grads(dout.data_ptr(), dq.data_ptr(), dk.data_ptr(), dv.data_ptr(), _dtype_code(grad_dtype))
     _call(lib().hyperattn_backward, "hyperattn_backward", dev, C.byref(p), C.byref(g))
     return dq, dk, dv
@@ -259,6 +265,8 @@ def sortlsh_noalloc(x, hash_bits, seed=0, stream=None):
     inside the library (its scratch is a fixed array in the library image; n is capped at
     NOALLOC_MAX_ROWS).  The three result tensors are allocated here, by the caller.
     Returns (ids uint8[n], perm int32[n], rank int32[n])."""
+    if stream is not None:
+        return _on_stream(stream, sortlsh_noalloc, x, hash_bits, seed)
     if not x.is_cuda or x.dtype != torch.bfloat16 or x.dim() != 2:
         raise HyperAttnError("x must be a 2-D CUDA bf16 tensor")
     x = x.contiguous()
@@ -266,7 +274,7 @@ def sortlsh_noalloc(x, hash_bits, seed=0, stream=None):
     ids = torch.empty(n, dtype=torch.uint8, device=x.device)
     perm = torch.empty(n, dtype=torch.int32, device=x.device)
     rank = torch.empty(n, dtype=torch.int32, device=x.device)
-    s = stream if stream is not None else torch.cuda.current_stream(x.device).cuda_stream
+    s = torch.cuda.current_stream(x.device).cuda_stream
     with torch.cuda.device(x.device):
         _check(lib().hyperattn_sortlsh_noalloc(x.data_ptr(), n, d, hash_bits, seed, ids.data_ptr(), perm.data_ptr(),
                                                rank.data_ptr(), s), "hyperattn_sortlsh_noalloc")
@@ -276,6 +284,8 @@ def sortlsh_noalloc(x, hash_bits, seed=0, stream=None):
 def alpha(q, k, causal=False, skip_cols=0, scale=0.0, stream=None):
     """n times the largest squared column norm of the exact softmax matrix of every (batch, head) (the alpha
     of the paper's Theorem 1): CUDA bf16 tensors q [B, H, n, d], k [B, H, n_k, d] -> float tensor [B, H]."""
+    if stream is not None:
+        return _on_stream(stream, alpha, q, k, causal, skip_cols, scale)
     if not (q.is_cuda and k.is_cuda) or q.dtype != torch.bfloat16 or k.dtype != torch.bfloat16:
         raise HyperAttnError("q and k must be CUDA bf16 tensors")
     q, k = q.contiguous(), k.contiguous()
@@ -285,7 +295,7 @@ def alpha(q, k, causal=False, skip_cols=0, scale=0.0, stream=None):
     _check(lib().hyperattn_alpha_workspace_bytes(B, H, n, n_k, C.byref(nbytes)), "hyperattn_alpha_workspace_bytes")
     ws = torch.empty(int(nbytes.value), dtype=torch.uint8, device=q.device)
     out = torch.empty((B, H), dtype=torch.float32, device=q.device)
-    s = stream if stream is not None else torch.cuda.current_stream(q.device).cuda_stream
+    s = torch.cuda.current_stream(q.device).cuda_stream
     with torch.cuda.device(q.device):
         _check(lib().hyperattn_alpha(q.data_ptr(), k.data_ptr(), B, H, n, 0 if n_k == n else n_k, d, float(scale), int(bool(causal)),
                                      int(skip_cols), out.data_ptr(), ws.data_ptr(), ws.numel(), s), "hyperattn_alpha")

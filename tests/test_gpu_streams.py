@@ -12,8 +12,8 @@ def ints(x):
     return torch.tensor(np.asarray(x), dtype=torch.int32, device="cuda")
 
 
-def check(call, after=None):
-    """call(**kw) -> tensors; after(): what the call has changed."""
+def check(call, after=None, off=0.0):
+    """call(**kw) -> tensors; after(): what the call has changed; off: what two calls may differ by, relative (sums whose order is anybody's)."""
     got = call()
     want = [x.clone() for x in (after() if after else got)]
     side = torch.cuda.Stream()
@@ -27,7 +27,7 @@ def check(call, after=None):
     side.synchronize()
     assert not torch.cuda.current_stream().query()       # the current stream has not been waited for
     torch.cuda.synchronize()
-    assert len(got) == len(want) and all(torch.equal(a, b) for a, b in zip(got, want))
+    assert len(got) == len(want) and all(torch.equal(a, b) if not off else ((a - b).abs() <= off * b.abs()).all() for a, b in zip(got, want))
 
 
 # strides that a call has to copy for: an odd address, rows that are all the same one, coordinates that are not next to each other
@@ -76,3 +76,23 @@ def test_the_default_stream_from_another_one():
         got = ha.prompt_attention(q, k, v, cu, stream=torch.cuda.default_stream().cuda_stream)
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(want, got))
+
+
+def test_the_approximation_its_gradients_and_its_parts():
+    q, k, v, dout = (torch.randn(3000, 1, 2, 64, device="cuda").bfloat16().permute(1, 2, 0, 3) for _ in range(4))       # (copied: rows are not next to each other)
+    check(lambda **kw: ha.forward(q, k, v, 256, 256, 7, causal=True, n0=1024, **kw))
+    check(lambda **kw: tuple(x for x in ha.forward(q, k, v, 256, 256, 7, debug=True, **kw)[:2]))
+    out, lse = ha.forward(q, k, v, 256, 256, 7)
+    x = q[0, 0, :, :]
+    check(lambda **kw: ha.sortlsh_noalloc(x, 7, **kw))
+    check(lambda **kw: (ha.alpha(q, k, **kw),), off=3000 * 2.0 ** -24)          # (a column's sum over the rows, in any order)
+    grads = ha.backward(q, k, v, out, lse, dout, 256, 256, 7)
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    torch.cuda._sleep(400_000_000)
+    got = ha.backward(q, k, v, out, lse, dout, 256, 256, 7, stream=side.cuda_stream)
+    side.synchronize()
+    assert not torch.cuda.current_stream().query()
+    torch.cuda.synchronize()
+    for a, b in zip(got, grads):                         # (sums of the key's gradients come in any order)
+        assert (a.float() - b.float()).abs().max() <= 2.0 ** -7 * b.float().abs().max()
