@@ -226,6 +226,24 @@ struct StageEvents { cudaEvent_t beg, end; int stage; int launches; };
 
 std::mutex g_mu;
 std::map<int, DeviceState> g_dev;
+// Makes the status word of the current device if there is none yet (g_mu is held).  It is zero before anybody gets to know it: cleared on a stream of its own, which
+// is waited for - kernels of any stream may look at it first thing, and the default stream orders nothing for streams that do not block.
+int make_status(DeviceState& ds, bool capturing) {
+  if (ds.status) return HYPERATTN_OK;
+  if (capturing) return HYPERATTN_WORKSPACE_TOO_SMALL;
+  int* word = nullptr;
+  cudaStream_t st = nullptr;
+  bool ok = cudaMalloc(&word, 256) == cudaSuccess && cudaStreamCreateWithFlags(&st, cudaStreamNonBlocking) == cudaSuccess;
+  ok = ok && cudaMemsetAsync(word, 0, 256, st) == cudaSuccess && cudaStreamSynchronize(st) == cudaSuccess;
+  if (st) cudaStreamDestroy(st);
+  if (!ok) {
+    if (word) cudaFree(word);
+    cudaGetLastError();
+    return HYPERATTN_CUDA_ERROR;
+  }
+  ds.status = word;
+  return HYPERATTN_OK;
+}
 bool g_profile = false;
 unsigned g_profile_mask = ~0u;          // stages that are timed while profiling is on
 std::vector<StageEvents> g_events;
@@ -317,11 +335,7 @@ int forward_impl(const hyperattn_params& p, int seg0 = 0, const hyperattn_grads*
   cudaStreamCaptureStatus cap = cudaStreamCaptureStatusNone;
   if (cudaStreamIsCapturing(st, &cap) != cudaSuccess) { cudaGetLastError(); cap = cudaStreamCaptureStatusNone; }
   const bool capturing = cap != cudaStreamCaptureStatusNone;
-  if (!ds.status) {
-    if (capturing) return HYPERATTN_WORKSPACE_TOO_SMALL;
-    if (cudaMalloc(&ds.status, 256) != cudaSuccess) return HYPERATTN_CUDA_ERROR;
-    if (cudaMemset(ds.status, 0, 256) != cudaSuccess) return HYPERATTN_CUDA_ERROR;
-  }
+  if (int rc = make_status(ds, capturing)) return rc;
   char* base = nullptr;
   if (pl.total > (p.workspace ? p.workspace_bytes : capturing ? ds.ws_bytes : pl.total)) {
     choose_chunks(p, g, false);
@@ -548,8 +562,7 @@ int device_status_word(cudaStream_t st, int** status) {
       cudaStreamCaptureStatus cap = cudaStreamCaptureStatusNone;
       if (cudaStreamIsCapturing(st, &cap) != cudaSuccess) { cudaGetLastError(); cap = cudaStreamCaptureStatusNone; }
       if (cap != cudaStreamCaptureStatusNone) return HYPERATTN_WORKSPACE_TOO_SMALL;
-      if (cudaMalloc(&ds.status, 256) != cudaSuccess) { ds.status = nullptr; return HYPERATTN_CUDA_ERROR; }
-      if (cudaMemset(ds.status, 0, 256) != cudaSuccess) return HYPERATTN_CUDA_ERROR;
+      if (int rc = make_status(ds, false)) return rc;
     }
     *status = ds.status;
   } catch (...) { return HYPERATTN_CUDA_ERROR; }
@@ -734,11 +747,12 @@ int hyperattn_last_device_status(void* stream, int* status) {
   *status = 0;
   if (!ds.status) return HYPERATTN_OK;
   int word = 0;
-  if (cudaMemcpy(&word, ds.status, 4, cudaMemcpyDeviceToHost) != cudaSuccess) return HYPERATTN_CUDA_ERROR;
+  const cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
+  if (cudaMemcpyAsync(&word, ds.status, 4, cudaMemcpyDeviceToHost, st) != cudaSuccess || cudaStreamSynchronize(st) != cudaSuccess) return HYPERATTN_CUDA_ERROR;
   if (word) {
     if (getenv("HYPERATTN_DEBUG")) std::fprintf(stderr, "hyperattn: device status word %d (site of the wait that gave up)\n", word);
     *status = HYPERATTN_DEVICE_TIMEOUT;
-    cudaMemset(ds.status, 0, 4);
+    if (cudaMemsetAsync(ds.status, 0, 4, st) != cudaSuccess || cudaStreamSynchronize(st) != cudaSuccess) return HYPERATTN_CUDA_ERROR;       // (calls on any stream find it cleared)
   }
   return HYPERATTN_OK;
 }
