@@ -162,12 +162,16 @@ def cache_plan(lengths, new, table, free, n_free, page_tokens, rows, stream=None
     _ints(index, lengths, new, table, free, n_free)
     if lengths.dim() != 1 or table.dim() != 2 or free.dim() != 1 or n_free.numel() != 1 or new.shape != lengths.shape or table.shape[0] != lengths.shape[0]:
         raise HyperAttnError("lengths and new are [requests], table [requests, width], free [pages], n_free [1]")
+    if rows < 0 or page_tokens <= 0:
+        raise HyperAttnError("rows must not be negative, page_tokens positive")
     R, W = table.shape
     F = free.shape[0]
     if R == 0:
         none = lengths.new_full((2, rows), -1)
         zero = lengths.new_zeros((2, 1))
-        return CachePlan(none[0], none[1], zero[0], zero[1], lengths.clone(), table.clone(), free.clone(), n_free.clone())
+        left = n_free.clamp(0, F).view(1)
+        stack = torch.where(torch.arange(F, dtype=torch.int32, device=free.device) < left, free, -1)
+        return CachePlan(none[0], none[1], zero[0], zero[1], lengths.clone(), table.clone(), stack, left)
     # one allocation for all but the table, the stack first (its address stays in steps of 16 bytes)
     flat = _new((F + 2 * rows + 3 * R + 3,), torch.int32, lengths.device)
     table_out = torch.empty_like(table)

@@ -98,3 +98,16 @@ def test_attention_of_nearly_as_many_units_as_an_int_counts():
     got = ha.cache_attention(q, cache, table, ints([(width - 1) * page + 70]), out_dtype=torch.float32)
     assert (got[0] - want[0]).abs().max() <= 2.0 ** -10 * want[0].abs().max() and (got[1] - want[1]).abs().max() <= 1e-5
     assert ha.last_device_status() == 0
+
+
+def test_a_plan_of_no_requests_says_what_one_of_idle_requests_says():
+    for n_free in (-3, 0, 2, 9):
+        free = ints([5, 6, 7, 8])
+        got = ha.cache_plan(ints([]), ints([]), ints(np.zeros((0, 4))), free, ints([n_free]), 16, 3)
+        want = ha.cache_plan(ints([0]), ints([0]), ints([[-1] * 4]), free, ints([n_free]), 16, 3)
+        for name in ("slots", "positions", "free", "n_free"):
+            assert torch.equal(getattr(got, name), getattr(want, name)), (n_free, name)
+    for rows, page in ((-1, 16), (3, 0)):
+        for R in (0, 2):
+            with pytest.raises(ha.HyperAttnError):
+                ha.cache_plan(ints([0] * R), ints([0] * R), ints(np.zeros((R, 4))), ints([1]), ints([1]), page, rows)
