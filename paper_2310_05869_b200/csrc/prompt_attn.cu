@@ -398,6 +398,8 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const __grid_consta
           unpack_f2(tile2, t0, t1);
           const bool over = there && !(t0 + t1 <= kSumLimit && most <= kMostByArithmetic);
           if (attempt > 0 || !__any_sync(0xffffffffu, over)) {
+            // (over it still: a score is no number, and the arithmetic has made one of it)
+            if (attempt > 0 && !(most <= kMostByArithmetic)) tile2 = pack_f2(NAN, NAN);
             sum2 = fadd2(sum2, tile2);
             break;
           }

@@ -198,3 +198,18 @@ def test_results_depend_on_a_request_alone(hq, hkv, d, dtype, causal):
         alone = ha.prompt_attention(q[at:at + a], k[at:at + a], v[at:at + a], offsets([a]), causal=causal)
         assert torch.equal(out[at:at + a], alone[0]) and torch.equal(lse[at:at + a], alone[1]), a
         at += a
+
+
+@pytest.mark.parametrize("d,dtype", [(64, "bf16"), (128, "bf16"), (64, "fp16"), (128, "fp16")])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+def test_a_score_that_is_no_number_in_every_column(d, dtype, bad):
+    """A request a column of a key tile, the first one walked and the second: every row that sees the key is NaN throughout, its log-sum-exp too; no other row changes."""
+    nq, nk = [9] * 256, [260] * 256
+    q, k, v = inputs(d, nq, nk, 1, 1, d, dtype)
+    clean, lse_clean = ha.prompt_attention(q, k, v, offsets(nq), offsets(nk), out_dtype=torch.float32)
+    k2 = k.view(256, 260, d).clone()
+    k2[torch.arange(256), 4 + torch.arange(256)] = bad                  # (of an infinity and a query of both signs the score is NaN)
+    out, lse = ha.prompt_attention(q, k2.view(-1, 1, d), v, offsets(nq), offsets(nk), out_dtype=torch.float32)
+    sees = (torch.arange(9)[None] + 251 >= 4 + torch.arange(256)[:, None]).reshape(-1).cuda()       # row i sees keys 0 .. 251 + i
+    assert out[sees].isnan().all() and lse[sees].isnan().all()
+    assert torch.equal(out[~sees], clean[~sees]) and torch.equal(lse[~sees], lse_clean[~sees]) and int((~sees).sum()) == 36
