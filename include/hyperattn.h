@@ -326,7 +326,7 @@ int hyperattn_alpha_workspace_bytes(int B, int H, int n, int n_k, size_t* bytes)
  * synchronises or allocates, so every call can be captured in a graph (the two attentions after one call outside a capture, or
  * any other call of the library: the first one on a device makes the status word, HYPERATTN_WORKSPACE_TOO_SMALL in a capture).
  * Their waits on the device are bounded like those of hyperattn_forward: hyperattn_last_device_status.  Calls without rows
- * return at once.
+ * return at once (and write nothing).
  *
  * The cache: pages of page_tokens tokens (a multiple of 16, at most 1024), uint8 [num_pages, kv_heads,
  * page_tokens / 16, 20 d].  A block of 20 d bytes holds K and V of 16 tokens of one head.  Every row of d numbers is
@@ -386,9 +386,10 @@ int hyperattn_cache_read(const hyperattn_cache* cache, const int32_t* table, int
 
 /* Attention of one query token a request over its cached tokens 0 .. lengths[r] - 1:
  *   out[r, h] = sum_j p_j v_j,  p = softmax_j(softmax_scale <q[r, h], k_j>),  lse[r, h] = ln sum_j exp(softmax_scale <q, k_j>).
- * A request without tokens gets out = 0 and lse = -infinity.  requests <= 4096.  Queries enter the products as fp16 (after a
- * power of two that brings the largest entry of a head near one), and so do the weights (2^-11; with fp16 queries what that
- * rounding loses enters too); scores and all sums are fp32. */
+ * A request without tokens gets out = 0 and lse = -infinity.  requests <= 4096; requests * q_heads * (table_width * page_tokens / 32 + 1)
+ * < 2^31.  Queries enter the products as fp16 (after a power of two that brings the largest entry of a head near one), and so do the
+ * weights (2^-11; with fp16 queries what that rounding loses enters too), whatever out_dtype is; beside values whose groups have a scale of
+ * 2^k and more (k >= 1) weights smaller than 2^(k - 26) of the largest are up to 2^(k - 37) of it off.  Scores and all sums are fp32. */
 typedef struct hyperattn_cache_attention_params {
   hyperattn_cache cache;
   const void* q;           /* [requests, q_heads, d], strides in elements (multiples of 8) */
@@ -409,7 +410,10 @@ int hyperattn_cache_attention_workspace_bytes(const hyperattn_cache_attention_pa
  * cu_k[r + 1] - 1 of k and v its keys.  causal: the last query sees all keys, every earlier one a key less (so a request
  * with more keys than queries continues a cached prompt; with fewer, the first queries see none).  A query that sees
  * no key gets out = 0, lse = -infinity; keys that a query does not see have no influence on it, whatever they hold.
- * Rows beyond cu_q[requests] are not written. */
+ * Rows beyond cu_q[requests] are not written.  A result depends on its request alone, bit for bit.
+ * Weights enter the products in the inputs' type, whatever out_dtype is: bf16 weights are up to 2^-8 off, fp16 ones up to 2^-11 (those below 2^-21
+ * of the largest up to 2^-32 of it), independently of each other; the sum of weights and the log-sum-exp take them as they were.  One pair of exponentials in
+ * eight is 2.7e-6 off, the others 2^-22.  Scores are fp32 sums.  out is one chain of products of 16 keys, from each of whose sums up to 2^-23 is cut. */
 typedef struct hyperattn_prompt_params {
   const void *q, *k, *v;   /* [q_rows, q_heads, d], [k_rows, kv_heads, d]; strides in elements (multiples of 8, not 0);
                               16-byte aligned.  q_heads / kv_heads <= 128 */
@@ -423,7 +427,7 @@ typedef struct hyperattn_prompt_params {
 } hyperattn_prompt_params;
 int hyperattn_prompt_attention(const hyperattn_prompt_params* p);
 
-/* Frees the private workspaces and profiling events of every device. */
+/* Frees the private workspaces and profiling events of every device.  Graphs that hold calls of the library must not be replayed afterwards. */
 int hyperattn_release(void);
 
 const char* hyperattn_status_string(int status);

@@ -9,8 +9,8 @@ namespace {
 // ---- plan ------------------------------------------------------------------------------------------------------------------
 // Everything follows from three running sums over the requests (new tokens, pages needed, pages released), which every CTA makes for
 // itself in shared memory - reading a few KB again costs less than a launch to make them first.  Then it does one thing: some CTAs
-// write the tables, some the rows, some the stack, one the requests' new state, so that their latencies do not add up.  256 requests with tables of 129 pages: 4.9 us,
-// latency (7.0 with the four in a row); 1024 requests with 2049 pages: 11.1 us, 2.4 TB/s.
+// write the tables, some the rows, some the stack, one the requests' new state, so that their latencies do not add up.  256 requests with tables of 129 pages: 5.0 us,
+// latency (7.0 with the four in a row); 1024 requests with 2049 pages: 11.6 us, bound by the instructions of the sums (two 64-bit divisions a request, in each of 519 CTAs).
 constexpr int kPlanThreads = 512, kPlanWarps = kPlanThreads / 32, kPlanColumns = 512;      // kPlanColumns: table entries of a warp at a time
 
 struct PlanParts { int tables, rows, stack; };           // CTAs for each

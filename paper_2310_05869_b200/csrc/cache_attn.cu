@@ -14,10 +14,11 @@
 // copies, no other warp to wait for).  A segment that lies in one part is finished there; pieces of others go to the workspace - one piece for
 // a CTA that is inside a segment as a whole - and a second launch puts them together, in order, so that results do not depend on timing.
 //
-// What bounds it: the issue of about 190 (d = 64) or 320 (d = 128) operations a block, of which 80 logical ones at half rate; memory next.  2 requests of up to 131072
-// tokens, 32 heads of 64: 150 us, 658 MB at 4.4 TB/s (68 % of copy bandwidth; the copies without the arithmetic 103 us).  64 requests of up to 8192,
-// 32 / 8 heads of 128: 66 us, 4.1 TB/s, of which the running sums, the first loads and the join take 14.  4 requests of up to 600: 10.2 us, two launches of
-// dependent loads.
+// What bounds it: no unit is full (issue 58 to 63 % of the cycles, the pipe of logical operations 54 to 59 %, DRAM half); four warps a scheduler, which their 128 registers
+// leave room for, do not cover the fixed latencies of their chains of about 190 (d = 64) or 330 (d = 128) operations a block.  2 requests of up to 131072
+// tokens, 32 heads of 64: 149 us, 658 MB at 4.4 TB/s (68 % of copy bandwidth; the copies without the arithmetic 103 us).  64 requests of up to 8192,
+// 32 / 8 heads of 128: 67 us, 4.1 TB/s, of which the running sums, the first loads and the join take 14.  4 requests of up to 600: 10.5 us, two launches of
+// dependent loads.  16 requests of up to 32768, 32 / 2 heads of 128 (two tiles of heads): 55 us for a floor of 13.
 #include <cstdio>
 #include <type_traits>
 #include "serving.cuh"

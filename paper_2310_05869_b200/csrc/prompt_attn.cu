@@ -15,9 +15,13 @@
 // of the item, and beyond the request's end - infinities and NaN of keys that not all of its rows see are set to zero before they are multiplied, and the rows that do
 // see them get them added at the end.
 //
-// What bounds it: at d = 128 the tensor pipe (68 % of its cycles) at the clock that the power limit leaves; 16384 tokens, 16 / 2 heads: 910 us, 1.2 PFLOP/s.  At d = 64
-// the exponentials: a warp takes 1900 of 2800 clocks a tile for its own, of which the unit works 1790 for the two warps of a scheduler; 6001 tokens behind 5000 cached ones,
-// 32 heads: 213 us, 0.62 PFLOP/s.  13 short prompts of 1021 tokens: 15 us, two items of a CTA one after the other.
+// Roundings: weights enter the products in the inputs' type (the tensor cores take both operands in one; a second term would be a second product), which is up to 2^-8 of each
+// in bf16 and 2^-11 in fp16; sums of weights are taken before that, in fp32.  O is one chain of products over all keys, of whose sums the tensor cores cut up to 2^-23 each: within
+// 2^-10 of a result at 131072 keys.
+//
+// What bounds it: at d = 128 the tensor pipe (64 % of its cycles) at the clock that the power limit leaves; 16384 tokens, 16 / 2 heads: 842 us, 1.3 PFLOP/s.  At d = 64 no unit
+// is full (exponentials 57 %, issue 41 %, tensor pipe 32 %): two softmax warps a scheduler, each in one chain of loads, exponentials, stores and hand-overs; 6001
+// tokens behind 5000 cached ones, 32 heads: 222 us, 0.6 PFLOP/s.  13 short prompts of 1021 tokens: 15.6 us, two items of a CTA one after the other.
 //
 // Warp roles (384 threads): 0-3 and 4-7 softmax and results of query tile 0 and 1, 8 issues the products (and allocates TMEM), 9 loads, 10 prepares items, 11 sees to
 // values that are not finite.
