@@ -427,6 +427,84 @@ typedef struct hyperattn_prompt_params {
 } hyperattn_prompt_params;
 int hyperattn_prompt_attention(const hyperattn_prompt_params* p);
 
+/* Attention of several new tokens a request over the cache that holds them too: a part of a prompt, drafted tokens.  Rows cu_q[r] ..
+ * cu_q[r + 1] - 1 of q are request r's queries (cu_q = NULL: row r alone, and rows = requests), its keys and values tokens 0 .. lengths[r] - 1 of
+ * the cache.  causal: the last query sees all of them, every earlier one a token less (so with fewer tokens than queries the first queries see none).
+ * out and lse as in hyperattn_cache_attention; a query that sees no token gets out = 0, lse = -infinity; rows beyond cu_q[requests] are not
+ * written.  A group of K or V whose scale or minimum is not finite counts as NaN: a query that sees it gets NaN (K) or NaN in those 32
+ * coordinates (V), other queries do not notice.  requests <= 4096; rows * q_heads < 2^31. */
+typedef struct hyperattn_chunk_params {
+  hyperattn_cache cache;
+  const void* q;           /* [rows, q_heads, d], strides in elements (multiples of 8) */
+  long long q_row_stride, q_head_stride;
+  void* out;               /* [rows, q_heads, d] contiguous, out_dtype */
+  float* lse;              /* [rows, q_heads] */
+  const int32_t *table, *lengths, *cu_q;
+  int requests, rows, table_width, q_heads, causal, dtype, out_dtype;
+  float softmax_scale;     /* <= 0 selects 1/sqrt(d) */
+  void* workspace;         /* device scratch of hyperattn_cache_chunk_attention_workspace_bytes bytes; its contents do not matter */
+  size_t workspace_bytes;
+  void* stream;
+} hyperattn_chunk_params;
+int hyperattn_cache_chunk_attention(const hyperattn_chunk_params* p);
+int hyperattn_cache_chunk_attention_workspace_bytes(const hyperattn_chunk_params* p, size_t* bytes);
+
+/* Attention weight that every cached token has got so far, for each key head: with q, cu_q, causal as above, n = request r's queries and lse the
+ * log-sum-exps that an attention over the cache gave for them (fp32 [rows, q_heads]),
+ *   weights_out[r, g, t] = decay weights[r, g, t] [t < lengths[r] - n] + sum exp(softmax_scale <q[i, h], k_t> - lse[i, h])
+ * over the request's rows i that see token t and the query heads h that read key head g; 0 for t >= lengths[r].  (Tokens of the rows themselves start
+ * from nothing, whatever their places held.)  weights, weights_out: fp32 [requests, kv_heads, table_width * page_tokens] contiguous,
+ * weights = NULL: nothing so far; they may be the same array.  Tokens in table entries that are no page get no weight. */
+typedef struct hyperattn_weights_params {
+  hyperattn_cache cache;
+  const void* q;
+  long long q_row_stride, q_head_stride;
+  const float *lse, *weights;
+  float* weights_out;
+  const int32_t *table, *lengths, *cu_q;
+  int requests, rows, table_width, q_heads, causal, dtype;
+  float softmax_scale, decay;
+  void* workspace;         /* device scratch of hyperattn_cache_weights_workspace_bytes bytes; its contents do not matter */
+  size_t workspace_bytes;
+  void* stream;
+} hyperattn_weights_params;
+int hyperattn_cache_weights(const hyperattn_weights_params* p);
+int hyperattn_cache_weights_workspace_bytes(const hyperattn_weights_params* p, size_t* bytes);
+
+/* Pages for what stays of requests that have grown too long.  Request r is to be cut to keep[r] tokens if 0 <= keep[r] < lengths[r].  Such requests are
+ * served in order: each needs as many new pages as keep[r] tokens take and is cut if the stack has them for it and all earlier ones.  They are
+ * taken from the top; then the old pages of those that are cut are put on the stack, in order of request and position.  (The new pages are none of
+ * the old ones, which can be read until something is stored into them by a later step's plan.)  Outputs (they must not alias the inputs):
+ *   lengths_out [requests]  keep[r] if request r is cut, else lengths[r]
+ *   table_out   [requests, table_width]: the new pages of a request that is cut, else its old ones; unused entries -1
+ *   free_out, n_free_out    the stack after the step, [num_free], unused entries -1
+ * Limits as for hyperattn_cache_plan. */
+typedef struct hyperattn_evict_plan {
+  const int32_t *lengths, *keep, *table, *free_pages, *n_free;
+  int requests, table_width, num_free, page_tokens;
+  int32_t *lengths_out, *table_out, *free_out, *n_free_out;
+  void* stream;
+} hyperattn_evict_plan;
+int hyperattn_cache_evict_plan(const hyperattn_evict_plan* p);
+
+/* Cuts every request r with to_lengths[r] < lengths[r] to n = to_lengths[r] tokens, for every key head by itself: of its tokens stay the last
+ * min(recent, n), the first min(first, n - those) and, of the others, those with the largest weights (of equal ones the earlier; weights that are negative or
+ * no numbers count as 0).  K and V of those that stay go, in their order and unchanged, to tokens 0 .. n - 1 of the pages of to_table, none of which may be a
+ * page that the call reads (hyperattn_cache_evict_plan makes such a table).  Nothing of other requests moves.
+ *   weights, weights_out  fp32 [requests, kv_heads, table_width * page_tokens]: what every token has, in its new order; 0 beyond the tokens
+ *   kept                  int32, of that shape: the tokens (before) that the new ones are; -1 beyond them, and for requests that are not cut
+ * weights_out must not be weights. */
+typedef struct hyperattn_evict_params {
+  hyperattn_cache cache;
+  const float* weights;
+  float* weights_out;
+  int32_t* kept;
+  const int32_t *table, *lengths, *to_table, *to_lengths;
+  int requests, table_width, recent, first;
+  void* stream;
+} hyperattn_evict_params;
+int hyperattn_cache_evict(const hyperattn_evict_params* p);
+
 /* Frees the private workspaces and profiling events of every device.  Graphs that hold calls of the library must not be replayed afterwards. */
 int hyperattn_release(void);
 

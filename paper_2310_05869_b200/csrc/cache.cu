@@ -11,29 +11,9 @@ namespace {
 // itself in shared memory - reading a few KB again costs less than a launch to make them first.  Then it does one thing: some CTAs
 // write the tables, some the rows, some the stack, one the requests' new state, so that their latencies do not add up.  256 requests with tables of 129 pages: 5.0 us,
 // latency (7.0 with the four in a row); 1024 requests with 2049 pages: 11.6 us, bound by the instructions of the sums (two 64-bit divisions a request, in each of 519 CTAs).
-constexpr int kPlanThreads = 512, kPlanWarps = kPlanThreads / 32, kPlanColumns = 512;      // kPlanColumns: table entries of a warp at a time
+constexpr int kPlanColumns = 512;        // table entries of a warp at a time
 
 struct PlanParts { int tables, rows, stack; };           // CTAs for each
-
-// a + b of two numbers that are not negative, 2^31 - 1 at most (what requests bring may be any numbers; sums of pages cannot get there)
-__device__ __forceinline__ int plus(int a, int b) { return (int)min((unsigned)a + (unsigned)b, 0x7fffffffu); }
-// Of the threads' numbers x[q]: the sums of those before this thread's, in their place.  All threads together.
-template <int N>
-__device__ __forceinline__ void sums_before(int (&x)[N], int (*s_warp)[kPlanWarps]) {
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-#pragma unroll
-  for (int q = 0; q < N; ++q) {
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) { const int y = __shfl_up_sync(0xffffffffu, x[q], o); if (lane >= o) x[q] = plus(x[q], y); }
-    if (lane == 31) s_warp[q][warp] = x[q];
-    x[q] = __shfl_up_sync(0xffffffffu, x[q], 1);
-    if (lane == 0) x[q] = 0;
-  }
-  __syncthreads();
-#pragma unroll
-  for (int q = 0; q < N; ++q)
-    for (int w = 0; w < warp; ++w) x[q] = plus(x[q], s_warp[q][w]);
-}
 
 __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const __grid_constant__ hyperattn_plan p, PlanParts parts) {
   extern __shared__ int smem[];
@@ -516,13 +496,6 @@ __global__ void __launch_bounds__(32 * kReadWarps) read_kernel(const __grid_cons
     }
     flush(a.v);
   }
-}
-
-CacheView view_of(const hyperattn_cache& c) { return {reinterpret_cast<uint8_t*>(c.pages), c.num_pages, c.page_tokens, c.kv_heads}; }
-int status_of(cudaError_t e, const char* what) {
-  if (e == cudaSuccess) return HYPERATTN_OK;
-  std::fprintf(stderr, "hyperattn: %s failed: %s\n", what, cudaGetErrorString(e));
-  return HYPERATTN_CUDA_ERROR;
 }
 
 }  // namespace

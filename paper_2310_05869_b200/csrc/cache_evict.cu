@@ -1,0 +1,357 @@
+// Requests that have grown too long: new pages for what stays (plan), which tokens stay, and moving them.
+#include "serving.cuh"
+#include "tc_util.cuh"
+
+namespace hyperattn {
+namespace {
+
+// ---- plan ------------------------------------------------------------------------------------------------------------------
+// As the cache's plan (cache.cu): every CTA makes the running sums for itself, then some write the tables, some the stack, one the requests' lengths.
+constexpr int kColumns = 512;            // table entries of a warp at a time
+struct EvictParts { int tables, stack; };
+
+__global__ void __launch_bounds__(kPlanThreads) evict_plan_kernel(const __grid_constant__ hyperattn_evict_plan p, EvictParts parts) {
+  extern __shared__ int smem[];
+  __shared__ int s_warp[1][kPlanWarps], s_given;
+  wait_for_stream();
+  const int R = p.requests, W = p.table_width, P = p.page_tokens, F = p.num_free;
+  // running sums (inclusive) of the pages that are asked for and of those that come back; pages that a request has, 1 << 30: it is cut
+  int *s_need = smem, *s_rel = smem + R, *s_have = smem + 2 * R;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int n_free = min(max(p.n_free[0], 0), F);
+  if (tid == 0) s_given = 0;
+  auto pages_of = [&](int tokens) { return (int)(((long long)tokens + P - 1) / P); };
+  const int per = (R + kPlanThreads - 1) / kPlanThreads, r0 = min(R, tid * per), r1 = min(R, r0 + per);
+  int sum[1] = {0};
+  for (int r = r0; r < r1; ++r) {
+    const int len = max(p.lengths[r], 0), keep = p.keep[r];
+    const bool wants = keep >= 0 && keep < len && pages_of(keep) <= W;
+    sum[0] += wants ? pages_of(keep) : 0;
+    s_need[r] = sum[0];
+    s_have[r] = min(pages_of(len), W) | (wants ? 1 << 30 : 0);
+  }
+  sums_before(sum, s_warp);
+  int back[1] = {0}, given = 0;
+  for (int r = r0; r < r1; ++r) {
+    s_need[r] += sum[0];
+    const int need = s_need[r] - (r > r0 ? s_need[r - 1] : sum[0]);
+    if ((s_have[r] >> 30) && need > 0 && s_need[r] > n_free) s_have[r] &= ~(1 << 30);
+    if ((s_have[r] >> 30) && need > 0) given = s_need[r];
+    back[0] += s_have[r] >> 30 ? s_have[r] & 0x3fffffff : 0;
+    s_rel[r] = back[0];
+  }
+  __syncthreads();                                     // (s_warp is used again)
+  if (given) atomicMax(&s_given, given);
+  sums_before(back, s_warp);
+  for (int r = r0; r < r1; ++r) s_rel[r] += back[0];
+  __syncthreads();
+  const int left = n_free - s_given, total = min(left + s_rel[R - 1], F);
+  auto before = [](const int* a, int r) { return r ? a[r - 1] : 0; };
+  auto cut = [&](int r) { return (s_have[r] >> 30 & 1) != 0; };
+
+  int cta = blockIdx.x;
+  if (cta < parts.tables) {
+    const int pieces = (W + kColumns - 1) / kColumns;
+    for (int u = cta * kPlanWarps + warp; u < R * pieces; u += parts.tables * kPlanWarps) {
+      const int r = u / pieces, c0 = (u - r * pieces) * kColumns;
+      const bool moved = cut(r);
+      const int first = before(s_need, r), end = moved ? s_need[r] - first : s_have[r] & 0x3fffffff;
+      const int32_t* from = p.table + (size_t)r * W;
+      int v[kColumns / 32];
+#pragma unroll
+      for (int i = 0; i < kColumns / 32; ++i) {
+        const int c = c0 + 32 * i + lane;
+        v[i] = c >= end ? -1 : moved ? p.free_pages[n_free - 1 - first - c] : from[c];
+      }
+#pragma unroll
+      for (int i = 0; i < kColumns / 32; ++i) {
+        const int c = c0 + 32 * i + lane;
+        if (c < W) p.table_out[(size_t)r * W + c] = v[i];
+      }
+    }
+    return;
+  }
+  cta -= parts.tables;
+  if (cta < parts.stack) {
+    auto stack = [&](int i) {
+      if (i >= total) return -1;
+      if (i < left) return p.free_pages[i];
+      const int r = upper_bound(s_rel, R, i - left);
+      return r < R ? p.table[(size_t)r * W + (i - left - before(s_rel, r))] : -1;
+    };
+    const bool quads = ((reinterpret_cast<uintptr_t>(p.free_pages) | reinterpret_cast<uintptr_t>(p.free_out)) & 15) == 0;
+    for (int i = 4 * (cta * kPlanThreads + tid); i < F; i += 4 * parts.stack * kPlanThreads) {
+      if (quads && i + 4 <= F && (i >= total || i + 4 <= left))
+        *reinterpret_cast<int4*>(p.free_out + i) = i >= total ? make_int4(-1, -1, -1, -1) : *reinterpret_cast<const int4*>(p.free_pages + i);
+      else
+        for (int k = i; k < min(i + 4, F); ++k) p.free_out[k] = stack(k);
+    }
+    return;
+  }
+  for (int r = tid; r < R; r += kPlanThreads) p.lengths_out[r] = cut(r) ? p.keep[r] : max(p.lengths[r], 0);
+  if (tid == 0) p.n_free_out[0] = total;
+}
+
+// ---- which tokens stay -------------------------------------------------------------------------------------------------------
+struct EvictArgs {
+  CacheView cache;
+  const float* weights;
+  float* weights_out;
+  int32_t* kept;
+  const int32_t *table, *lengths, *to_table, *to_lengths;
+  int requests, width, recent, first;
+};
+struct Cut {                             // of a request
+  int len, n;                            // tokens before and after
+  __device__ __forceinline__ bool moved() const { return n < len; }
+};
+__device__ __forceinline__ Cut cut_of(const EvictArgs& a, int r) {
+  Cut c;
+  c.len = min(max(a.lengths[r], 0), a.width * a.cache.page);
+  c.n = min(max(a.to_lengths[r], 0), c.len);
+  return c;
+}
+// the order of weights as that of whole numbers: those that are negative or no numbers count as 0
+__device__ __forceinline__ uint32_t order_of(float w) { return w > 0.f ? __float_as_uint(w) : 0u; }
+
+// A CTA takes a request and key head: the smallest weight that stays is found digit by digit (8 bits at a time, from the top), then the tokens are numbered in order.
+constexpr int kSelectThreads = 1024, kSelectWarps = kSelectThreads / 32;
+
+__global__ void __launch_bounds__(kSelectThreads) select_kernel(const __grid_constant__ EvictArgs a) {
+  __shared__ int s_hist[256], s_digit, s_above;
+  __shared__ uint32_t s_warp[kSelectWarps];
+  wait_for_stream();
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int r = blockIdx.x / a.cache.heads, cap = a.width * a.cache.page;
+  const Cut c = cut_of(a, r);
+  const float* w = a.weights + (size_t)blockIdx.x * cap;
+  float* out = a.weights_out + (size_t)blockIdx.x * cap;
+  int32_t* kept = a.kept + (size_t)blockIdx.x * cap;
+  if (!c.moved()) {
+    for (int t = tid; t < cap; t += kSelectThreads) { out[t] = t < c.len ? w[t] : 0.f; kept[t] = -1; }
+    return;
+  }
+  const int recent = min(a.recent, c.n), first = min(a.first, c.n - recent), begin = first, end = c.len - recent;
+  int want = c.n - recent - first;                     // tokens of [begin, end) that stay
+  uint32_t top = 0;                                    // digits of the smallest one's weight so far
+  if (want > 0) {
+    for (int shift = 24; shift >= 0; shift -= 8) {
+      for (int i = tid; i < 256; i += kSelectThreads) s_hist[i] = 0;
+      __syncthreads();
+      for (int t = begin + tid; t < end; t += kSelectThreads) {
+        const uint32_t x = order_of(w[t]);
+        if (shift == 24 || x >> (shift + 8) == top >> (shift + 8)) atomicAdd(&s_hist[x >> shift & 255], 1);
+      }
+      __syncthreads();
+      if (warp == 0) {
+        // lane l has digits 255 - 8 l downwards
+        int mine = 0;
+        for (int i = 0; i < 8; ++i) mine += s_hist[255 - 8 * lane - i];
+        int sum = mine;
+        for (int o = 1; o < 32; o <<= 1) { const int y = __shfl_up_sync(0xffffffffu, sum, o); if (lane >= o) sum += y; }
+        int above = sum - mine;
+        if (above < want && sum >= want)
+          for (int i = 0; i < 8; ++i) {
+            const int digit = 255 - 8 * lane - i;
+            if (above + s_hist[digit] >= want) { s_digit = digit; s_above = above; break; }
+            above += s_hist[digit];
+          }
+      }
+      __syncthreads();
+      top |= (uint32_t)s_digit << shift;
+      want -= s_above;
+      __syncthreads();
+    }
+  } else top = 0xffffffffu;
+  // `want` of those that weigh `top` stay, the first ones; and all that weigh more
+  int base = 0, equal = 0;                             // tokens that stay, and equal ones, before this round's
+  for (int t0 = 0; t0 < c.len; t0 += 4 * kSelectThreads) {
+    float x[4];
+    uint32_t mine = 0, stays = 0, same = 0;            // counts: those that stay for sure | equal ones << 16
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int t = t0 + 4 * tid + i;
+      x[i] = t < c.len ? w[t] : 0.f;
+      const bool inside = t >= begin && t < end;
+      const bool sure = t < c.len && (!inside || order_of(x[i]) > top), eq = inside && want > 0 && order_of(x[i]) == top;
+      stays |= (uint32_t)sure << i;
+      same |= (uint32_t)eq << i;
+      mine += sure + ((uint32_t)eq << 16);
+    }
+    uint32_t sum = mine;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) { const uint32_t y = __shfl_up_sync(0xffffffffu, sum, o); if (lane >= o) sum += y; }
+    if (lane == 31) s_warp[warp] = sum;
+    __syncthreads();
+    uint32_t all = 0, mybase = 0;
+    for (int k = 0; k < kSelectWarps; ++k) { if (k == warp) mybase = all; all += s_warp[k]; }
+    const uint32_t ahead = mybase + sum - mine;
+    int sure = base + (ahead & 0xffff), eq = equal + (ahead >> 16);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const bool s = stays >> i & 1, e = same >> i & 1;
+      if (s || (e && eq < want)) {
+        const int at = sure + min(eq, want);
+        kept[at] = t0 + 4 * tid + i;
+        out[at] = x[i];
+      }
+      sure += s;
+      eq += e;
+    }
+    base += all & 0xffff;
+    equal += all >> 16;
+    __syncthreads();
+  }
+  for (int t = c.n + tid; t < cap; t += kSelectThreads) { out[t] = 0.f; kept[t] = -1; }
+}
+
+// ---- moving them -------------------------------------------------------------------------------------------------------------
+// A warp makes a block of 16 tokens of the new pages at a time, from the blocks that its tokens are in: K by pieces of a token (16 bytes, d = 64: 8), V by 16-byte loads that
+// hold a token's byte of four words, scales and minima one by one.  The blocks of all requests that are cut are one sequence, in equal parts for the warps.
+constexpr int kMoveWarps = 4, kMostRequests = HYPERATTN_PLAN_MAX_REQUESTS;
+
+template <int D>
+__global__ void __launch_bounds__(32 * kMoveWarps) move_kernel(const __grid_constant__ EvictArgs a) {
+  using B = Block<D>;
+  constexpr int G = B::kGroups;
+  extern __shared__ int s_starts[];                    // [requests + 1] blocks of one head before a request
+  __shared__ int s_sums[kMoveWarps];
+  wait_for_stream();
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int per = (a.requests + 32 * kMoveWarps - 1) / (32 * kMoveWarps), r0 = min(a.requests, tid * per), r1 = min(a.requests, r0 + per);
+  int mine = 0;
+  for (int r = r0; r < r1; ++r) {
+    const Cut c = cut_of(a, r);
+    s_starts[r] = mine;
+    mine += c.moved() ? (c.n + kBlockTokens - 1) / kBlockTokens : 0;
+  }
+  int run = mine;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) { const int y = __shfl_up_sync(0xffffffffu, run, o); if (lane >= o) run += y; }
+  if (lane == 31) s_sums[warp] = run;
+  __syncthreads();
+  run -= mine;
+  for (int w = 0; w < warp; ++w) run += s_sums[w];
+  for (int r = r0; r < r1; ++r) s_starts[r] += run;
+  if (tid == 32 * kMoveWarps - 1) s_starts[a.requests] = run + mine;
+  __syncthreads();
+  const int H = a.cache.heads, subs = a.cache.page / kBlockTokens, cap = a.width * a.cache.page;
+  const long long total = (long long)s_starts[a.requests] * H, warps = (long long)gridDim.x * kMoveWarps;
+  const uint8_t* pages = a.cache.pages;
+  for (long long u = blockIdx.x * kMoveWarps + warp; u < total; u += warps) {
+    int lo = 0, hi = a.requests;                       // the last request whose blocks start there or before
+    while (hi - lo > 1) { const int mid = (lo + hi) >> 1; if ((long long)s_starts[mid] * H <= u) lo = mid; else hi = mid; }
+    const int r = lo, blocks = s_starts[r + 1] - s_starts[r];
+    const int rest = (int)(u - (long long)s_starts[r] * H), head = rest / blocks, b = rest - head * blocks;
+    const int to_page = b / subs < a.width ? a.to_table[(size_t)r * a.width + b / subs] : -1;
+    if (to_page < 0 || to_page >= a.cache.num_pages) continue;
+    uint8_t* to = block_at<D>(a.cache, to_page, head, b % subs);
+    // lane t < 16: where token t comes from (block -1: nowhere, zeros)
+    int src = -1, block = -1;
+    if (lane < kBlockTokens) {
+      const int at = b * kBlockTokens + lane;
+      src = at < cap ? a.kept[((size_t)r * H + head) * cap + at] : -1;
+      if (src >= 0) {
+        const int page = a.table[(size_t)r * a.width + src / a.cache.page];
+        if (page >= 0 && page < a.cache.num_pages) block = (page * H + head) * subs + src % a.cache.page / kBlockTokens;
+      }
+    }
+    src &= kBlockTokens - 1;
+    auto block_of = [&](int t) { return __shfl_sync(0xffffffffu, block, t); };
+    auto token_of = [&](int t) { return __shfl_sync(0xffffffffu, src, t); };
+    auto bytes_at = [&](int blk, int at) { return pages + (size_t)blk * B::kBytes + at; };
+    // K
+    uint4 k[2];
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+      const int blk = block_of(half * 8 + lane / 4), t = token_of(half * 8 + lane / 4), ln = t % 8 * 4 + lane % 4;
+      if constexpr (D == 128) k[half] = blk < 0 ? make_uint4(0, 0, 0, 0) : *reinterpret_cast<const uint4*>(bytes_at(blk, t / 8 * 512 + ln * 16));
+      else {
+        const uint2 x = blk < 0 ? make_uint2(0, 0) : *reinterpret_cast<const uint2*>(bytes_at(blk, ln * 16 + t / 8 * 8));
+        if (half) { k[0].z = x.x; k[0].w = x.y; } else { k[0].x = x.x; k[0].y = x.y; }
+      }
+    }
+    // V: bytes of a word: tokens 2 c, 8 + 2 c, 2 c + 1, 9 + 2 c
+    uint4 v[D / 64];
+#pragma unroll
+    for (int i = 0; i < D / 64; ++i) v[i] = make_uint4(0, 0, 0, 0);
+#pragma unroll
+    for (int p = 0; p < 4; ++p) {
+      const int mine_t = 2 * (lane % 4) + p / 2 + (p & 1) * 8, blk = block_of(mine_t), t = token_of(mine_t), byte = t % 2 * 2 + t / 8;
+#pragma unroll
+      for (int i = 0; i < D / 64; ++i) {
+        const uint4 x = blk < 0 ? make_uint4(0, 0, 0, 0) : *reinterpret_cast<const uint4*>(bytes_at(blk, B::kV + i * 512 + (lane / 4 * 4 + t % 8 / 2) * 16));
+        const uint32_t pick = 0x3210u & ~(0xfu << (4 * p)) | (uint32_t)(4 + byte) << (4 * p);              // byte p from the source
+        v[i].x = __byte_perm(v[i].x, x.x, pick); v[i].y = __byte_perm(v[i].y, x.y, pick);
+        v[i].z = __byte_perm(v[i].z, x.z, pick); v[i].w = __byte_perm(v[i].w, x.w, pick);
+      }
+    }
+    // scales and minima: words of tokens 2 i, 2 i + 1
+    uint32_t sc[2 * D / 64];
+#pragma unroll
+    for (int j = 0; j < 2 * D / 64; ++j) {
+      const int word = j * 32 + lane, tp = word / (2 * G) % 8, at = B::kScaleK + (word / (16 * G)) * 2 * D;         // K's, then V's
+      uint32_t both = 0;
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const int blk = block_of(2 * tp + e), t = token_of(2 * tp + e);
+        const uint32_t x = blk < 0 ? 0u : *reinterpret_cast<const uint16_t*>(bytes_at(blk, at + (t / 2 * 2 * G + word % (2 * G)) * 4 + t % 2 * 2));
+        both |= x << (16 * e);
+      }
+      sc[j] = both;
+    }
+    *reinterpret_cast<uint4*>(to + lane * 16) = k[0];
+    if constexpr (D == 128) *reinterpret_cast<uint4*>(to + 512 + lane * 16) = k[1];
+#pragma unroll
+    for (int i = 0; i < D / 64; ++i) *reinterpret_cast<uint4*>(to + B::kV + i * 512 + lane * 16) = v[i];
+#pragma unroll
+    for (int j = 0; j < 2 * D / 64; ++j) *reinterpret_cast<uint32_t*>(to + B::kScaleK + (j * 32 + lane) * 4) = sc[j];
+  }
+}
+
+}  // namespace
+}  // namespace hyperattn
+
+using namespace hyperattn;
+
+extern "C" int hyperattn_cache_evict_plan(const hyperattn_evict_plan* p) {
+  if (!p || p->requests < 0 || p->table_width <= 0 || p->num_free < 0 || p->page_tokens <= 0) return HYPERATTN_INVALID_ARGUMENT;
+  if (p->requests > HYPERATTN_PLAN_MAX_REQUESTS || (long long)p->table_width * p->page_tokens > 0x7fffffffLL || p->table_width >= 1 << 28 ||
+      (long long)p->requests * p->table_width + p->num_free > 0x7fffffffLL)
+    return HYPERATTN_UNSUPPORTED_SHAPE;
+  if (p->requests == 0) return HYPERATTN_OK;
+  if (!p->lengths || !p->keep || !p->table || (p->num_free && (!p->free_pages || !p->free_out)) || !p->n_free || !p->lengths_out || !p->table_out || !p->n_free_out)
+    return HYPERATTN_INVALID_ARGUMENT;
+  if (p->lengths_out == p->lengths || p->lengths_out == p->keep || p->table_out == p->table || (p->num_free && p->free_out == p->free_pages) || p->n_free_out == p->n_free)
+    return HYPERATTN_MISALIGNED;
+  const int smem = 3 * p->requests * (int)sizeof(int);
+  if (smem > 40 * 1024)
+    if (int rc = status_of(allow_smem<evict_plan_kernel>(3 * HYPERATTN_PLAN_MAX_REQUESTS * (int)sizeof(int)), "evict plan: shared memory")) return rc;
+  auto ctas = [](long long work, int per, int most) { return (int)(work <= 0 ? 0 : (work + per - 1) / per < most ? (work + per - 1) / per : most); };
+  const EvictParts parts = {ctas((long long)p->requests * ((p->table_width + kColumns - 1) / kColumns), kPlanWarps, 2 * kSms), ctas(p->num_free, 8 * kPlanThreads, kSms)};
+  return status_of(launch(evict_plan_kernel, dim3((unsigned)(parts.tables + parts.stack + 1)), dim3(kPlanThreads), smem, reinterpret_cast<cudaStream_t>(p->stream), *p, parts), "evict plan");
+}
+
+extern "C" int hyperattn_cache_evict(const hyperattn_evict_params* p) {
+  int rc;
+  if (!p || p->requests < 0 || p->table_width <= 0 || p->recent < 0 || p->first < 0) return HYPERATTN_INVALID_ARGUMENT;
+  if (bad_cache(p->cache, &rc)) return rc;
+  if (p->requests > kMostRequests || (long long)p->table_width * p->cache.page_tokens > 0x7fffffffLL || (long long)p->requests * p->cache.kv_heads > 0x7fffffffLL ||
+      (long long)p->requests * p->table_width * (p->cache.page_tokens / kBlockTokens) > 0x7fffffffLL ||
+      (long long)p->cache.num_pages * (p->cache.page_tokens / kBlockTokens) * p->cache.kv_heads > 0x7fffffffLL)
+    return HYPERATTN_UNSUPPORTED_SHAPE;
+  if (p->requests == 0) return HYPERATTN_OK;
+  if (!p->weights || !p->weights_out || !p->kept || !p->table || !p->lengths || !p->to_table || !p->to_lengths) return HYPERATTN_INVALID_ARGUMENT;
+  if (misaligned(p->weights) || misaligned(p->weights_out) || misaligned(p->kept) || p->weights == p->weights_out) return HYPERATTN_MISALIGNED;
+  const EvictArgs a = {view_of(p->cache), p->weights, p->weights_out, p->kept, p->table, p->lengths, p->to_table, p->to_lengths, p->requests, p->table_width, p->recent, p->first};
+  const cudaStream_t st = reinterpret_cast<cudaStream_t>(p->stream);
+  cudaError_t e = launch(select_kernel, dim3((unsigned)(p->requests * p->cache.kv_heads)), dim3(kSelectThreads), 0, st, a);
+  if (e == cudaSuccess) {
+    const long long blocks = (long long)p->requests * p->cache.kv_heads * ((long long)p->table_width * p->cache.page_tokens / kBlockTokens);
+    const long long want = (blocks + kMoveWarps - 1) / kMoveWarps;
+    const dim3 grid((unsigned)(want < 12 * kSms ? want : 12 * kSms));
+    const int smem = (p->requests + 1) * (int)sizeof(int);
+    e = p->cache.d == 64 ? launch(move_kernel<64>, grid, dim3(32 * kMoveWarps), smem, st, a) : launch(move_kernel<128>, grid, dim3(32 * kMoveWarps), smem, st, a);
+  }
+  return status_of(e, "evict");
+}

@@ -1,5 +1,6 @@
 // Shared declarations of the serving entry points: packed prompts and the paged 4-bit cache.
 #pragma once
+#include <cstdio>
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include "../../include/hyperattn.h"
@@ -63,6 +64,36 @@ __device__ __forceinline__ int upper_bound(const int* a, int n, int x) {
     if (a[mid] > x) hi = mid; else lo = mid + 1;
   }
   return lo;
+}
+
+// ---- running sums over the requests, which every CTA of the plans makes for itself ---------------------------------------
+constexpr int kPlanThreads = 512, kPlanWarps = kPlanThreads / 32;
+
+// a + b of two numbers that are not negative, 2^31 - 1 at most (what requests bring may be any numbers; sums of pages cannot get there)
+__device__ __forceinline__ int plus(int a, int b) { return (int)min((unsigned)a + (unsigned)b, 0x7fffffffu); }
+// Of the threads' numbers x[q]: the sums of those before this thread's, in their place.  All threads together.
+template <int N>
+__device__ __forceinline__ void sums_before(int (&x)[N], int (*s_warp)[kPlanWarps]) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+#pragma unroll
+  for (int q = 0; q < N; ++q) {
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) { const int y = __shfl_up_sync(0xffffffffu, x[q], o); if (lane >= o) x[q] = plus(x[q], y); }
+    if (lane == 31) s_warp[q][warp] = x[q];
+    x[q] = __shfl_up_sync(0xffffffffu, x[q], 1);
+    if (lane == 0) x[q] = 0;
+  }
+  __syncthreads();
+#pragma unroll
+  for (int q = 0; q < N; ++q)
+    for (int w = 0; w < warp; ++w) x[q] = plus(x[q], s_warp[q][w]);
+}
+
+inline CacheView view_of(const hyperattn_cache& c) { return {reinterpret_cast<uint8_t*>(c.pages), c.num_pages, c.page_tokens, c.kv_heads}; }
+inline int status_of(cudaError_t e, const char* what) {
+  if (e == cudaSuccess) return HYPERATTN_OK;
+  std::fprintf(stderr, "hyperattn: %s failed: %s\n", what, cudaGetErrorString(e));
+  return HYPERATTN_CUDA_ERROR;
 }
 
 }  // namespace

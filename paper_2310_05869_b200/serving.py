@@ -53,6 +53,31 @@ class _Prompt(C.Structure):                            # hyperattn_prompt_params
                 + [("softmax_scale", C.c_float), ("stream", C.c_void_p)])
 
 
+class _Chunk(C.Structure):                             # hyperattn_chunk_params
+    _fields_ = ([("cache", _Cache), ("q", C.c_void_p), ("q_row_stride", C.c_longlong), ("q_head_stride", C.c_longlong)]
+                + [(n, C.c_void_p) for n in ("out", "lse", "table", "lengths", "cu_q")]
+                + [(n, C.c_int) for n in ("requests", "rows", "table_width", "q_heads", "causal", "dtype", "out_dtype")]
+                + [("softmax_scale", C.c_float), ("workspace", C.c_void_p), ("workspace_bytes", C.c_size_t), ("stream", C.c_void_p)])
+
+
+class _Weights(C.Structure):                           # hyperattn_weights_params
+    _fields_ = ([("cache", _Cache), ("q", C.c_void_p), ("q_row_stride", C.c_longlong), ("q_head_stride", C.c_longlong)]
+                + [(n, C.c_void_p) for n in ("lse", "weights", "weights_out", "table", "lengths", "cu_q")]
+                + [(n, C.c_int) for n in ("requests", "rows", "table_width", "q_heads", "causal", "dtype")]
+                + [("softmax_scale", C.c_float), ("decay", C.c_float), ("workspace", C.c_void_p), ("workspace_bytes", C.c_size_t), ("stream", C.c_void_p)])
+
+
+class _EvictPlan(C.Structure):                         # hyperattn_evict_plan
+    _fields_ = ([(n, C.c_void_p) for n in ("lengths", "keep", "table", "free_pages", "n_free")]
+                + [(n, C.c_int) for n in ("requests", "table_width", "num_free", "page_tokens")]
+                + [(n, C.c_void_p) for n in ("lengths_out", "table_out", "free_out", "n_free_out", "stream")])
+
+
+class _Evict(C.Structure):                             # hyperattn_evict_params
+    _fields_ = ([("cache", _Cache)] + [(n, C.c_void_p) for n in ("weights", "weights_out", "kept", "table", "lengths", "to_table", "to_lengths")]
+                + [(n, C.c_int) for n in ("requests", "table_width", "recent", "first")] + [("stream", C.c_void_p)])
+
+
 def _packer(kind):
     """A struct's members as bytes: what a call passes (filling a ctypes object member by member takes several times as long)."""
     def format_of(kind):
@@ -64,6 +89,7 @@ def _packer(kind):
 
 
 _cache_bytes, _plan_bytes, _attention_bytes, _prompt_bytes = (_packer(k) for k in (_Cache, _Plan, _CacheAttention, _Prompt))
+_chunk_bytes, _weights_bytes, _evict_plan_bytes, _evict_bytes = (_packer(k) for k in (_Chunk, _Weights, _EvictPlan, _Evict))
 
 
 @functools.cache
@@ -72,7 +98,10 @@ def _lib():
     i, p, ll = C.c_int, C.c_void_p, C.c_longlong
     for name, args in (("hyperattn_cache_plan", [p]), ("hyperattn_cache_store", [p, p, p, i, i, ll, ll, ll, ll, p, p]),
                        ("hyperattn_cache_read", [p, p, i, i, p, p, i, p, p, i, p]), ("hyperattn_cache_attention", [p]),
-                       ("hyperattn_cache_attention_workspace_bytes", [p, C.POINTER(C.c_size_t)]), ("hyperattn_prompt_attention", [p])):
+                       ("hyperattn_cache_attention_workspace_bytes", [p, C.POINTER(C.c_size_t)]), ("hyperattn_prompt_attention", [p]),
+                       ("hyperattn_cache_chunk_attention", [p]), ("hyperattn_cache_chunk_attention_workspace_bytes", [p, C.POINTER(C.c_size_t)]),
+                       ("hyperattn_cache_weights", [p]), ("hyperattn_cache_weights_workspace_bytes", [p, C.POINTER(C.c_size_t)]),
+                       ("hyperattn_cache_evict_plan", [p]), ("hyperattn_cache_evict", [p])):
         getattr(L, name).restype = i
         getattr(L, name).argtypes = args
     return L
@@ -296,3 +325,157 @@ def prompt_attention(q, k, v, cu_q, cu_k=None, causal=True, scale=0.0, out_dtype
         q.data_ptr(), k.data_ptr(), v.data_ptr(), q_row, q_head, k_row, k_head, v_row, v_head, out.data_ptr(), lse.data_ptr(), cu_q.data_ptr(),
         cu_k.data_ptr(), cu_q.shape[0] - 1, T, k_rows, H, kv_heads, d, 1 if causal else 0, dtype, out_code, scale, _stream(index)))
     return out, lse
+
+
+def _queries(q, cache, table, lengths, cu_q):
+    """What the calls with several queries a request have in common: the cache's members, the device's index, q as the kernels take it and its strides."""
+    c = _cache_of(cache)
+    index = cache.get_device()
+    _ints(index, table, lengths)
+    if cu_q is not None:
+        _ints(index, cu_q)
+    if q.dim() != 3 or table.dim() != 2 or lengths.dim() != 1 or q.get_device() != index or q.shape[2] != c[4] or table.shape[0] != lengths.shape[0]:
+        raise HyperAttnError("q must be [rows, q_heads, d] on the cache's device, table [requests, width], lengths [requests]")
+    R = lengths.shape[0]
+    if q.shape[0] != R if cu_q is None else cu_q.dim() != 1 or cu_q.shape[0] != R + 1:
+        raise HyperAttnError("cu_q must be [requests + 1]; without it there is one row a request")
+    return c, index, *_rows(q)
+
+
+@functools.lru_cache(4096)
+def _chunk_workspace(*shape):
+    """Workspace of hyperattn_cache_chunk_attention: (pages, page_tokens, kv_heads, d, requests, rows, width, q_heads, causal, dtype, out_dtype)."""
+    size = C.c_size_t(0)
+    cache, (R, T, W, H, causal, dtype, out_dtype) = shape[:4], shape[4:]
+    d = cache[3]
+    _check(_lib().hyperattn_cache_chunk_attention_workspace_bytes(_chunk_bytes(
+        16, *cache, 0, d, d, 0, 0, 0, 0, 0, R, T, W, H, causal, dtype, out_dtype, 0.0, 0, 0, 0), C.byref(size)), "hyperattn_cache_chunk_attention_workspace_bytes")
+    return size.value
+
+
+def cache_chunk_attention(q, cache, table, lengths, cu_q=None, causal=True, scale=0.0, out_dtype=None, stream=None):
+    """Attention of several new tokens a request, q [rows, q_heads, d] (bf16 or fp16, any strides), over its cached tokens 0 .. lengths[r] - 1, which
+    are theirs too: request r's queries are rows cu_q[r] .. cu_q[r + 1] - 1 (default: one row a request).  causal: a request's last query sees
+    all its tokens, every earlier one a token less.  table [requests, width], lengths [requests], cu_q [requests + 1]: int32.  Returns (out
+    [rows, q_heads, d], lse [rows, q_heads]); a query that sees no token gets zeros and -inf, rows beyond cu_q[-1] are not written."""
+    if stream is not None:
+        return _on_stream(stream, cache_chunk_attention, q, cache, table, lengths, cu_q, causal, scale, out_dtype)
+    c, index, q, row, head = _queries(q, cache, table, lengths, cu_q)
+    T, H, d = q.shape
+    R, W = table.shape
+    out_dtype = out_dtype or q.dtype
+    dtype, out_code = _code(q.dtype, "q"), _code(out_dtype, "the result")
+    device = q.device
+    out = _new((T, H, d), out_dtype, device)
+    lse = _new((T, H), torch.float32, device)
+    causal = 1 if causal else 0
+    size = _chunk_workspace(*c[1:], R, T, W, H, causal, dtype, out_code)
+    work = _new((size,), torch.uint8, device)
+    _call("hyperattn_cache_chunk_attention", index, _chunk_bytes(
+        *c, q.data_ptr(), row, head, out.data_ptr(), lse.data_ptr(), table.data_ptr(), lengths.data_ptr(), 0 if cu_q is None else cu_q.data_ptr(), R, T, W, H, causal, dtype, out_code,
+        scale, work.data_ptr(), size, _stream(index)))
+    return out, lse
+
+
+@functools.lru_cache(4096)
+def _weights_workspace(*shape):
+    """Workspace of hyperattn_cache_weights: (pages, page_tokens, kv_heads, d, requests, rows, width, q_heads, causal, dtype)."""
+    size = C.c_size_t(0)
+    cache, (R, T, W, H, causal, dtype) = shape[:4], shape[4:]
+    d = cache[3]
+    _check(_lib().hyperattn_cache_weights_workspace_bytes(_weights_bytes(
+        16, *cache, 0, d, d, 0, 0, 0, 0, 0, 0, R, T, W, H, causal, dtype, 0.0, 0.0, 0, 0, 0), C.byref(size)), "hyperattn_cache_weights_workspace_bytes")
+    return size.value
+
+
+def _weights_of(x, name, requests, c, width, index):
+    """The address of accumulated weights, which are fp32 [requests, kv_heads, width * page_tokens]."""
+    if x.dtype is not torch.float32 or x.get_device() != index or tuple(x.shape) != (requests, c[3], width * c[2]) or not x.is_contiguous():
+        raise HyperAttnError(f"{name} must be a contiguous float32 tensor [requests, kv_heads, width * page_tokens] on the cache's device")
+    return x.data_ptr()
+
+
+def cache_weights(q, cache, table, lengths, lse, cu_q=None, weights=None, decay=1.0, causal=True, scale=0.0, out=None, stream=None):
+    """The attention weight that every cached token has got, summed over queries and the query heads of its key head: decay times what it had (weights; None: nothing)
+    plus what these rows give it.  q, cu_q, causal as for cache_chunk_attention, lse [rows, q_heads] (float32) as it or cache_attention returned it.  Tokens of the rows
+    themselves - a request's last ones, as many as it has rows - start from nothing.  Returns fp32 [requests, kv_heads, width * page_tokens], zeros beyond a request's tokens; out: the
+    tensor to write it to (it may be `weights`)."""
+    if stream is not None:
+        return _on_stream(stream, cache_weights, q, cache, table, lengths, lse, cu_q, weights, decay, causal, scale, out)
+    c, index, q, row, head = _queries(q, cache, table, lengths, cu_q)
+    T, H, d = q.shape
+    R, W = table.shape
+    if lse.dtype is not torch.float32 or lse.get_device() != index or tuple(lse.shape) != (T, H):
+        raise HyperAttnError("lse must be a float32 tensor [rows, q_heads] on the cache's device")
+    lse = lse.contiguous()
+    before = 0 if weights is None else _weights_of(weights, "weights", R, c, W, index)
+    if out is None:
+        out = _new((R, c[3], W * c[2]), torch.float32, q.device)
+    to = _weights_of(out, "out", R, c, W, index)
+    dtype, causal = _code(q.dtype, "q"), 1 if causal else 0
+    size = _weights_workspace(*c[1:], R, T, W, H, causal, dtype)
+    work = _new((size,), torch.uint8, q.device)
+    _call("hyperattn_cache_weights", index, _weights_bytes(
+        *c, q.data_ptr(), row, head, lse.data_ptr(), before, to, table.data_ptr(), lengths.data_ptr(), 0 if cu_q is None else cu_q.data_ptr(), R, T, W, H, causal, dtype,
+        scale, decay, work.data_ptr(), size, _stream(index)))
+    return out
+
+
+class EvictPlan(NamedTuple):
+    lengths: torch.Tensor     # [requests] tokens after the cut
+    table: torch.Tensor       # [requests, width] pages that hold them then, -1: none
+    free: torch.Tensor        # the stack of free pages, -1: none
+    n_free: torch.Tensor      # [1] entries on it
+
+
+def cache_evict_plan(lengths, keep, table, free, n_free, page_tokens, stream=None):
+    """New pages for what stays of requests that are to be cut to keep[r] tokens (those with 0 <= keep[r] < lengths[r]), as long as there are free ones, in order; their old pages go
+    on the stack.  lengths, keep [requests], table [requests, width], free [any], n_free [1]: int32 CUDA tensors, not changed.  Once for all layers; then
+    cache_evict for each.  Returns an EvictPlan."""
+    if stream is not None:
+        return _on_stream(stream, cache_evict_plan, lengths, keep, table, free, n_free, page_tokens)
+    if not lengths.is_cuda:
+        raise HyperAttnError("lengths must be a CUDA tensor (there is no CPU path)")
+    index = lengths.get_device()
+    _ints(index, lengths, keep, table, free, n_free)
+    if lengths.dim() != 1 or table.dim() != 2 or free.dim() != 1 or n_free.numel() != 1 or keep.shape != lengths.shape or table.shape[0] != lengths.shape[0]:
+        raise HyperAttnError("lengths and keep are [requests], table [requests, width], free [pages], n_free [1]")
+    if page_tokens <= 0:
+        raise HyperAttnError("page_tokens must be positive")
+    R, W = table.shape
+    F = free.shape[0]
+    if R == 0:
+        left = n_free.clamp(0, F).view(1)
+        stack = torch.where(torch.arange(F, dtype=torch.int32, device=free.device) < left, free, -1)
+        return EvictPlan(lengths.clone(), table.clone(), stack, left)
+    flat = _new((F + R + 1,), torch.int32, lengths.device)                 # (the stack first: its address stays in steps of 16 bytes)
+    table_out = torch.empty_like(table)
+    at = flat.data_ptr()
+    _call("hyperattn_cache_evict_plan", index, _evict_plan_bytes(
+        lengths.data_ptr(), keep.data_ptr(), table.data_ptr(), free.data_ptr(), n_free.data_ptr(), R, W, F, page_tokens, at + 4 * F, table_out.data_ptr(), at, at + 4 * (F + R), _stream(index)))
+    free_out, lengths_out, n_free_out = torch.unsafe_split_with_sizes(flat, (F, R, 1))
+    return EvictPlan(lengths_out, table_out, free_out, n_free_out)
+
+
+def cache_evict(cache, weights, table, lengths, to_table, to_lengths, recent=0, first=0, stream=None):
+    """Cuts every request with to_lengths[r] < lengths[r] to that many tokens, for every key head by itself: the last `recent` and the first `first` ones stay, and those with the
+    largest weights (of equal ones the earlier).  They move, in order, to the pages of to_table (those of cache_evict_plan: none that is read here).  weights: fp32 [requests, kv_heads, width *
+    page_tokens] as cache_weights gives them.  Returns (weights, kept) of that shape: the tokens' weights in their new order, and which tokens they were (int32; -1: none, or the request
+    is not cut)."""
+    if stream is not None:
+        return _on_stream(stream, cache_evict, cache, weights, table, lengths, to_table, to_lengths, recent, first)
+    c = _cache_of(cache)
+    index = cache.get_device()
+    _ints(index, table, lengths, to_table, to_lengths)
+    if table.dim() != 2 or lengths.dim() != 1 or table.shape[0] != lengths.shape[0] or to_table.shape != table.shape or to_lengths.shape != lengths.shape:
+        raise HyperAttnError("table and to_table must be [requests, width], lengths and to_lengths [requests]")
+    if recent < 0 or first < 0:
+        raise HyperAttnError("recent and first must not be negative")
+    R, W = table.shape
+    at = _weights_of(weights, "weights", R, c, W, index)
+    most = W * c[2]                                                        # (more than all there are: all)
+    out = torch.empty_like(weights)
+    kept = _new((R, c[3], most), torch.int32, weights.device)
+    _call("hyperattn_cache_evict", index, _evict_bytes(
+        *c, at, out.data_ptr(), kept.data_ptr(), table.data_ptr(), lengths.data_ptr(), to_table.data_ptr(), to_lengths.data_ptr(), R, W, min(recent, most), min(first, most), _stream(index)))
+    return out, kept
