@@ -104,34 +104,6 @@ __global__ void __launch_bounds__(128) chunk_kernel(const __grid_constant__ Chun
   if (lane == 0) a.lse[at] = sum == 0.f ? -INFINITY : (ref + log2f(sum)) * 0.6931471805599453f;
 }
 
-template <int D, class T>
-__global__ void __launch_bounds__(128) weights_kernel(const __grid_constant__ ChunkArgs a) {
-  wait_for_stream();
-  const int cap = a.width * a.cache.page, lane = threadIdx.x & 31, G = a.q_heads / a.cache.heads;
-  const long long warps = (long long)gridDim.x * 4, total = (long long)a.requests * a.cache.heads * cap;
-  for (long long u = (long long)blockIdx.x * 4 + (threadIdx.x >> 5); u < total; u += warps) {
-    const int t = (int)(u % cap), kv = (int)(u / cap % a.cache.heads), r = (int)(u / cap / a.cache.heads);
-    const Span s = span_of(a, r);
-    float w = 0.f;
-    if (t < s.len) {
-      if (a.weights && t < s.len - s.rows) w = a.decay * a.weights[u];
-      const int page = a.table[(size_t)r * a.width + t / a.cache.page];
-      if (page >= 0 && page < a.cache.num_pages) {
-        float k[D / 32], q[D / 32], sum = 0.f;
-        values_of<D>(block_at<D>(a.cache, page, kv, t % a.cache.page / kBlockTokens), t % kBlockTokens, 0, k);
-        for (int i = a.causal ? max(0, t - (s.len - s.rows)) : 0; i < s.rows; ++i)
-          for (int g = 0; g < G; ++g) {
-            query_of<D, T>(a, s.first + i, kv * G + g, q);
-            const float lse = a.lse_in[(size_t)(s.first + i) * a.q_heads + kv * G + g];
-            sum += lse == -INFINITY ? 0.f : exp2f(fmaf(dot(q, k), a.scale_log2, -lse * 1.4426950408889634f));
-          }
-        w += sum;
-      }
-    }
-    if (lane == 0) a.weights_out[u] = w;
-  }
-}
-
 template <class P>
 int check(const P* p) {
   int rc;
@@ -181,26 +153,4 @@ extern "C" int hyperattn_cache_chunk_attention(const hyperattn_chunk_params* p) 
   const bool bf16 = p->dtype == HYPERATTN_BF16;
   if (p->cache.d == 64) return status_of(bf16 ? launch(chunk_kernel<64, __nv_bfloat16>, grid, block, 0, st, a) : launch(chunk_kernel<64, __half>, grid, block, 0, st, a), "chunk attention");
   return status_of(bf16 ? launch(chunk_kernel<128, __nv_bfloat16>, grid, block, 0, st, a) : launch(chunk_kernel<128, __half>, grid, block, 0, st, a), "chunk attention");
-}
-
-extern "C" int hyperattn_cache_weights_workspace_bytes(const hyperattn_weights_params* p, size_t* bytes) {
-  if (!bytes) return HYPERATTN_INVALID_ARGUMENT;
-  if (int rc = check(p)) return rc;
-  *bytes = 0;
-  return HYPERATTN_OK;
-}
-
-extern "C" int hyperattn_cache_weights(const hyperattn_weights_params* p) {
-  if (int rc = check(p)) return rc;
-  if (!p->cu_q && p->rows != p->requests) return HYPERATTN_INVALID_ARGUMENT;
-  if (p->requests == 0) return HYPERATTN_OK;
-  if ((p->rows && (!p->q || !p->lse)) || !p->weights_out || !p->table || !p->lengths) return HYPERATTN_INVALID_ARGUMENT;
-  if (misaligned(p->q) || misaligned(p->weights) || misaligned(p->weights_out)) return HYPERATTN_MISALIGNED;
-  ChunkArgs a = args_of(*p);
-  a.lse_in = p->lse; a.weights = p->weights; a.weights_out = p->weights_out; a.decay = p->decay;
-  const cudaStream_t st = reinterpret_cast<cudaStream_t>(p->stream);
-  const dim3 grid(16 * kSms), block(128);
-  const bool bf16 = p->dtype == HYPERATTN_BF16;
-  if (p->cache.d == 64) return status_of(bf16 ? launch(weights_kernel<64, __nv_bfloat16>, grid, block, 0, st, a) : launch(weights_kernel<64, __half>, grid, block, 0, st, a), "cache weights");
-  return status_of(bf16 ? launch(weights_kernel<128, __nv_bfloat16>, grid, block, 0, st, a) : launch(weights_kernel<128, __half>, grid, block, 0, st, a), "cache weights");
 }

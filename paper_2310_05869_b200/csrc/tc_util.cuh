@@ -13,6 +13,8 @@ bool encode_acc_map(CUtensorMap* m, const void* base, size_t rows, int d);
 // [rows x heads x d] of bf16 or fp16 with strides in elements; one box = 64 columns x box_heads heads x box_rows rows, 128-byte swizzle (attn_tc.cu)
 bool encode_heads_map(CUtensorMap* m, const void* base, bool bf16, long long rows, long long row_stride, int heads, long long head_stride, int d, int box_rows,
                       int box_heads);
+// [rows x row_words] of 32-bit words, row-major; one box = box_words x box_rows, as they are (attn_tc.cu)
+bool encode_words_map(CUtensorMap* m, const void* base, long long rows, int row_words, int box_words, int box_rows);
 
 namespace {
 
