@@ -1,0 +1,118 @@
+// Few rows a request over the paged 4-bit cache - drafted tokens, single tokens - and the weight that cached tokens get from them: the launches of the warp-level kernels
+// (cache_attn.cuh) with some rows in the place of a key head's query heads.
+#include "cache_attn.cuh"
+#include "cache_rows.cuh"
+#include "cache_tiles.cuh"
+
+namespace hyperattn {
+
+namespace {
+
+// What a call's launches look like: rows of a chunk (0: four, twice in a tile), CTAs, bytes of the workspace
+struct RowsShape { int tiles, per_chunk, ctas; long long slots; size_t starts, bytes; };
+template <int D, Mode MODE>
+RowsShape rows_shape(int requests, int rows, int group, int kv_heads, long long tokens) {
+  RowsShape s;
+  const long long all = (long long)rows * group;
+  // as many rows in a tile as requests have on average: four (and what the rounding of their weights loses beside them), eight, or two tiles of eight
+  s.tiles = MODE == kSomeRows && all <= 4ll * requests ? 0 : all <= 8ll * requests ? 1 : 2;
+  s.per_chunk = s.tiles == 0 ? 4 : 8 * s.tiles;
+  s.slots = chunk_slots(rows, requests, group, s.per_chunk) + 1;
+  constexpr int unit = Ring<D, MODE>::kUnitTokens;
+  const long long units = (MODE == kWeights ? requests : s.slots) * kv_heads * ((tokens + unit - 1) / unit), ctas = (units + kWarps - 1) / kWarps;
+  const int memory = ctas_by_memory<D, MODE>(requests), registers = ctas_by_registers(s.tiles == 2 ? 2 : 1);
+  const int most = kSms * (memory < registers ? memory : registers);
+  s.ctas = (int)(ctas < most ? ctas : most);
+  s.starts = ((size_t)(requests + 2) * 4 + 255) / 256 * 256;
+  s.bytes = MODE == kWeights ? 0 : s.starts + (size_t)s.ctas * kWarps * 2 * s.per_chunk * (D + 2) * 4;
+  return s;
+}
+// units are counted in ints
+template <int D, Mode MODE>
+bool countable(const RowsShape& s, int requests, int kv_heads, long long tokens) {
+  return (MODE == kWeights ? (long long)requests : s.slots) * kv_heads <= 0x7fffffffLL / (tokens / Ring<D, MODE>::kUnitTokens + 2) && s.slots * kv_heads <= 0x7fffffffLL;
+}
+CacheAttnArgs rows_args(const ChunkArgs& c) {
+  CacheAttnArgs a = {};
+  a.cache = c.cache; a.q = c.q; a.q_row = c.q_row; a.q_head = c.q_head; a.table = c.table; a.lengths = c.lengths; a.cu_q = c.cu_q;
+  a.requests = c.requests; a.width = c.width; a.q_heads = c.q_heads; a.rows = c.rows; a.causal = c.causal; a.scale_log2 = c.scale_log2; a.chunks = 1;
+  return a;
+}
+template <class F>
+auto of_dim(int d, F f) { return d == 64 ? f(std::integral_constant<int, 64>{}) : f(std::integral_constant<int, 128>{}); }
+
+}  // namespace
+
+bool few_rows_attention(const hyperattn_chunk_params& p, size_t* bytes) {
+  const int group = p.q_heads / p.cache.kv_heads;
+  const long long tokens = (long long)p.table_width * p.cache.page_tokens;
+  return of_dim(p.cache.d, [&](auto dim) {
+    constexpr int D = decltype(dim)::value;
+    const RowsShape s = rows_shape<D, kSomeRows>(p.requests, p.rows, group, p.cache.kv_heads, tokens);
+    *bytes = s.bytes;
+    return countable<D, kSomeRows>(s, p.requests, p.cache.kv_heads, tokens);
+  });
+}
+
+int launch_few_rows_attention(const hyperattn_chunk_params& p, int* status) {
+  const int group = p.q_heads / p.cache.kv_heads;
+  const cudaStream_t st = reinterpret_cast<cudaStream_t>(p.stream);
+  CacheAttnArgs a = rows_args(chunk_args(p));
+  a.out = p.out; a.lse = p.lse; a.out_kind = p.out_dtype;
+  return of_dim(p.cache.d, [&](auto dim) {
+    constexpr int D = decltype(dim)::value;
+    using R = Ring<D, kSomeRows>;
+    const RowsShape s = rows_shape<D, kSomeRows>(p.requests, p.rows, group, p.cache.kv_heads, (long long)p.table_width * p.cache.page_tokens);
+    a.starts = reinterpret_cast<int*>(p.workspace);
+    a.part = reinterpret_cast<float*>(reinterpret_cast<char*>(p.workspace) + s.starts);
+    a.part_heads = s.per_chunk;
+    auto go = [&](auto tiles, auto type) {
+      constexpr int NT = decltype(tiles)::value > 1 ? 2 : 1;
+      constexpr bool PAIR = decltype(tiles)::value == 0;
+      constexpr auto kernel = cache_attn_kernel<D, NT, PAIR, decltype(type), kSomeRows>;
+      cudaError_t e = allow_smem<kernel>(R::bytes(kMaxRequests));
+      if (e == cudaSuccess) e = launch(kernel, dim3((unsigned)s.ctas), dim3(32 * kWarps), R::bytes(p.requests), st, a, status);
+      const long long segments = s.slots * p.cache.kv_heads;
+      int split = (int)((4 * kSms + segments - 1) / segments);
+      if (split > s.per_chunk) split = s.per_chunk;
+      const int heads = (s.per_chunk + split - 1) / split;
+      if (e == cudaSuccess) e = launch(join_kernel<D, kSomeRows>, dim3((unsigned)segments, (unsigned)((s.per_chunk + heads - 1) / heads)), dim3(kJoinThreads), 0, st, a, heads);
+      return status_of(e, "chunk attention");
+    };
+    auto of_type = [&](auto tiles) { return p.dtype == HYPERATTN_BF16 ? go(tiles, __nv_bfloat16()) : go(tiles, __half()); };
+    return s.tiles == 0 ? of_type(std::integral_constant<int, 0>{}) : s.tiles == 1 ? of_type(std::integral_constant<int, 1>{}) : of_type(std::integral_constant<int, 2>{});
+  });
+}
+
+bool few_rows_weights(const hyperattn_weights_params& p) {
+  const int group = p.q_heads / p.cache.kv_heads;
+  const long long tokens = (long long)p.table_width * p.cache.page_tokens;
+  if ((long long)p.rows * group > 16ll * p.requests) return false;
+  return of_dim(p.cache.d, [&](auto dim) {
+    constexpr int D = decltype(dim)::value;
+    return countable<D, kWeights>(rows_shape<D, kWeights>(p.requests, p.rows, group, p.cache.kv_heads, tokens), p.requests, p.cache.kv_heads, tokens);
+  });
+}
+
+int launch_few_rows_weights(const hyperattn_weights_params& p, int* status) {
+  const cudaStream_t st = reinterpret_cast<cudaStream_t>(p.stream);
+  CacheAttnArgs a = rows_args(chunk_args(p));
+  a.lse_in = p.lse; a.before = p.weights; a.weights = p.weights_out; a.decay = p.decay;
+  return of_dim(p.cache.d, [&](auto dim) {
+    constexpr int D = decltype(dim)::value;
+    using R = Ring<D, kWeights>;
+    const RowsShape s = rows_shape<D, kWeights>(p.requests, p.rows, p.q_heads / p.cache.kv_heads, p.cache.kv_heads, (long long)p.table_width * p.cache.page_tokens);
+    auto go = [&](auto tiles, auto type) {
+      constexpr auto kernel = cache_attn_kernel<D, decltype(tiles)::value, false, decltype(type), kWeights>;
+      cudaError_t e = allow_smem<kernel>(R::bytes(kMaxRequests));
+      if (e == cudaSuccess) e = launch(kernel, dim3((unsigned)s.ctas), dim3(32 * kWarps), R::bytes(p.requests), st, a, status);
+      return status_of(e, "cache weights");
+    };
+    auto of_type = [&](auto tiles) { return p.dtype == HYPERATTN_BF16 ? go(tiles, __nv_bfloat16()) : go(tiles, __half()); };
+    return s.tiles == 1 ? of_type(std::integral_constant<int, 1>{}) : of_type(std::integral_constant<int, 2>{});
+  });
+}
+
+int few_rows_unit(int d) { return d == 64 ? Ring<64, kWeights>::kUnitTokens : Ring<128, kWeights>::kUnitTokens; }
+
+}  // namespace hyperattn

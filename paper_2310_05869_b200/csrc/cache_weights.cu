@@ -8,6 +8,7 @@
 // Warp roles: 0-7 sums (two groups of four, for every other image), 8-15 keys (two groups, for every other tile), 16 products (and TMEM), 17 copies of keys, 18 of images.
 // Every wait is bounded: a CTA that gives up raises the device status word, drains its copies, frees its TMEM and returns.
 #include <type_traits>
+#include "cache_rows.cuh"
 #include "cache_tiles.cuh"
 
 namespace hyperattn {
@@ -367,21 +368,19 @@ __global__ void __launch_bounds__(kWThreads, 1) weights_kernel(const __grid_cons
   }
 }
 
-// zeros beyond the requests' tokens (the last tile's are the kernel's)
-__global__ void __launch_bounds__(256) blank_kernel(const __grid_constant__ WeightArgs p) {
+// zeros beyond the requests' tokens (and beyond those that the kernels take with them, `unit` at a time)
+__global__ void __launch_bounds__(256) blank_kernel(const __grid_constant__ WeightArgs p, int unit) {
   wait_for_stream();
   const ChunkArgs& a = p.c;
   const int cap = a.width * a.cache.page, r = blockIdx.x / a.cache.heads;
   const Span s = span_of(a, r);
-  const int from = (int)min(((long long)s.len + kTileTokens - 1) / kTileTokens * kTileTokens, (long long)cap);
+  const int from = (int)min(((long long)s.len + unit - 1) / unit * unit, (long long)cap);
   float4* to = reinterpret_cast<float4*>(p.out + (size_t)blockIdx.x * cap);                // (a page is a multiple of 16 tokens)
   for (int i = from / 4 + blockIdx.y * 256 + threadIdx.x; i < cap / 4; i += 256 * gridDim.y) to[i] = make_float4(0.f, 0.f, 0.f, 0.f);
 }
 
-// rows of an image: few where requests have few
-int image_rows(const hyperattn_weights_params& p) { return (long long)p.rows * (p.q_heads / p.cache.kv_heads) <= 16ll * p.requests ? 16 : 64; }
-template <int D> size_t image_bytes(int nr) { return nr == 16 ? Image<D, 16>::kBytes : Image<D, 64>::kBytes; }
-long long slots_of(const hyperattn_weights_params& p) { return image_slots(p.rows, p.requests, p.q_heads / p.cache.kv_heads, image_rows(p)) + 1; }
+constexpr int kImageRows = 64;
+long long slots_of(const hyperattn_weights_params& p) { return image_slots(p.rows, p.requests, p.q_heads / p.cache.kv_heads, kImageRows) + 1; }
 
 }  // namespace
 }  // namespace hyperattn
@@ -391,9 +390,10 @@ using namespace hyperattn;
 extern "C" int hyperattn_cache_weights_workspace_bytes(const hyperattn_weights_params* p, size_t* bytes) {
   if (!bytes) return HYPERATTN_INVALID_ARGUMENT;
   if (int rc = check_chunk(p)) return rc;
+  *bytes = 0;
+  if (p->requests == 0 || few_rows_weights(*p)) return HYPERATTN_OK;
   if (slots_of(*p) * p->cache.kv_heads > 0x7fffffffLL) return HYPERATTN_UNSUPPORTED_SHAPE;
-  const int nr = image_rows(*p);
-  *bytes = p->requests ? (size_t)(slots_of(*p) * p->cache.kv_heads) * (p->cache.d == 64 ? image_bytes<64>(nr) : image_bytes<128>(nr)) : 0;
+  *bytes = (size_t)(slots_of(*p) * p->cache.kv_heads) * (p->cache.d == 64 ? Image<64, kImageRows>::kBytes : Image<128, kImageRows>::kBytes);
   return HYPERATTN_OK;
 }
 
@@ -402,35 +402,35 @@ extern "C" int hyperattn_cache_weights(const hyperattn_weights_params* p) {
   if (int rc = hyperattn_cache_weights_workspace_bytes(p, &bytes)) return rc;
   if (!p->cu_q && p->rows != p->requests) return HYPERATTN_INVALID_ARGUMENT;
   if (p->requests == 0) return HYPERATTN_OK;
-  if ((p->rows && (!p->q || !p->lse)) || !p->weights_out || !p->table || !p->lengths || !p->workspace) return HYPERATTN_INVALID_ARGUMENT;
+  if ((p->rows && (!p->q || !p->lse)) || !p->weights_out || !p->table || !p->lengths || (bytes && !p->workspace)) return HYPERATTN_INVALID_ARGUMENT;
   if (misaligned(p->q) || misaligned(p->weights) || misaligned(p->weights_out) || misaligned(p->workspace)) return HYPERATTN_MISALIGNED;
   if (p->workspace_bytes < bytes) return HYPERATTN_WORKSPACE_TOO_SMALL;
   const int subs = p->cache.page_tokens / kBlockTokens, d = p->cache.d;
-  WeightArgs w = {chunk_args(*p), p->weights, p->weights_out, p->decay, subs % 8 == 0 ? 8 : subs & -subs};
+  const WeightArgs w = {chunk_args(*p), p->weights, p->weights_out, p->decay, subs % 8 == 0 ? 8 : subs & -subs};
+  const bool few = few_rows_weights(*p);
   KeyMaps maps;
   const long long blocks = (long long)p->cache.num_pages * p->cache.kv_heads * subs;
-  if (!encode_words_map(&maps.codes, p->cache.pages, blocks, 5 * d, 2 * d, w.run) || !encode_words_map(&maps.scales, p->cache.pages, blocks, 5 * d, d / 2, w.run)) return HYPERATTN_UNSUPPORTED_SHAPE;
+  if (!few && (!encode_words_map(&maps.codes, p->cache.pages, blocks, 5 * d, 2 * d, w.run) || !encode_words_map(&maps.scales, p->cache.pages, blocks, 5 * d, d / 2, w.run))) return HYPERATTN_UNSUPPORTED_SHAPE;
   const cudaStream_t st = reinterpret_cast<cudaStream_t>(p->stream);
   int* status = nullptr;
   if (int rc = device_status_word(st, &status)) return rc;
   int sms = 0;
   cudaError_t e = sm_count(&sms);
-  if (e != cudaSuccess) return status_of(e, "cache weights");
   const int heads = p->requests * p->cache.kv_heads, cap = p->table_width * p->cache.page_tokens;
-  auto go = [&](auto dim, auto nr) {
-    constexpr int D = decltype(dim)::value, NR = decltype(nr)::value;
+  int y = (4 * kSms + heads - 1) / heads;
+  if (y > (cap + 4095) / 4096) y = (cap + 4095) / 4096;
+  if (e == cudaSuccess) e = launch(blank_kernel, dim3((unsigned)heads, (unsigned)y), dim3(256), 0, st, w, few ? few_rows_unit(d) : kTileTokens);
+  if (e != cudaSuccess) return status_of(e, "cache weights");
+  if (few) return launch_few_rows_weights(*p, status);
+  auto go = [&](auto dim) {
+    constexpr int D = decltype(dim)::value, NR = kImageRows;
     using C = WCfg<D, NR>;
     cudaError_t e = allow_smem<weights_kernel<D, NR>>(C::kSmem);
-    int y = (4 * kSms + heads - 1) / heads;
-    if (y > (cap + 4095) / 4096) y = (cap + 4095) / 4096;
-    if (e == cudaSuccess) e = launch(blank_kernel, dim3((unsigned)heads, (unsigned)y), dim3(256), 0, st, w);
     const dim3 slots((unsigned)(slots_of(*p) * p->cache.kv_heads));
-    if (e == cudaSuccess && p->rows)
-      e = p->dtype == HYPERATTN_BF16 ? launch(image_kernel<D, NR, __nv_bfloat16>, slots, dim3(128), 0, st, w.c, p->lse) : launch(image_kernel<D, NR, __half>, slots, dim3(128), 0, st, w.c, p->lse);
+    if (e == cudaSuccess) e = p->dtype == HYPERATTN_BF16 ? launch(image_kernel<D, NR, __nv_bfloat16>, slots, dim3(128), 0, st, w.c, p->lse) : launch(image_kernel<D, NR, __half>, slots, dim3(128), 0, st, w.c, p->lse);
     const long long tiles = (long long)heads * ((cap + kTileTokens - 1) / kTileTokens);
     if (e == cudaSuccess) e = launch(weights_kernel<D, NR>, dim3((unsigned)(tiles < sms ? tiles : sms)), dim3(kWThreads), C::kSmem, st, w, maps, status);
     return status_of(e, "cache weights");
   };
-  auto of_rows = [&](auto dim) { return image_rows(*p) == 16 ? go(dim, std::integral_constant<int, 16>()) : go(dim, std::integral_constant<int, 64>()); };
-  return p->cache.d == 64 ? of_rows(std::integral_constant<int, 64>()) : of_rows(std::integral_constant<int, 128>());
+  return d == 64 ? go(std::integral_constant<int, 64>()) : go(std::integral_constant<int, 128>());
 }

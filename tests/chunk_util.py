@@ -66,11 +66,11 @@ def visible(n, length, causal):
 
 
 def attention(q, k, v, lens, counts, causal=True, scale=None, there=None):
-    """out, lse [T, Hq, (d)], and the bounds' ingredients: sum p |v| and the largest scale sum |q k|.  k, v: rows of all requests, one after the other; there [sum(lens)]: is a token's page one."""
+    """out, lse [T, Hq, (d)], and the bounds' ingredients: sum p |v|, the same with the largest |v| of its group of 32, and the largest scale sum |q k|.  k, v: rows of all requests, one after the other; there [sum(lens)]: is a token's page one."""
     T, Hq, d = q.shape
     H = k.shape[1]
     G = Hq // H
-    out, mass = q.new_zeros(T, Hq, d), q.new_zeros(T, Hq, d)
+    out, mass, coarse = q.new_zeros(T, Hq, d), q.new_zeros(T, Hq, d), q.new_zeros(T, Hq, d)
     lse, size = q.new_full((T, Hq), -math.inf), q.new_zeros(T, Hq)
     q0 = k0 = 0
     for n, m in zip(counts, lens):
@@ -96,27 +96,30 @@ def attention(q, k, v, lens, counts, causal=True, scale=None, there=None):
                 sees_nan = (seen.double() @ nan.double() > 0)[:, None].expand_as(o)
                 out[rows, hs] = torch.where(sees_nan & ~none, math.nan, o)
                 mass[rows, hs] = p @ clean.abs()
+                coarse[rows, hs] = p @ clean.abs().unflatten(-1, (-1, SU.GROUP)).amax(-1, keepdim=True).expand(-1, -1, SU.GROUP).flatten(-2)
                 lse[rows, hs] = (top + total.log()).squeeze(-1)
                 size[rows, hs] = s
         q0 += n
         k0 += m
-    return out, lse, mass, size
+    return out, lse, (mass, coarse), size
 
 
 def check_attention(got, want, dtype, keys, rows):
     """Against the bounds that the header's roundings add up to.  Scores: the products of exact operands are summed in fp32, at most 40 sums that lose 2^-23 of the partial sum (at
     most `size`) each: 2^-17 size.  Weights: that, 2.7e-6 of an exponential, 2^-11 as fp16; values once 2^-11 as fp16; the sum over keys 2^-23 for every 16 of them, and as many again where parts are
-    joined; the result's own type (fp16 numbers below 2^-14 are multiples of 2^-24, so that half a step is 2^-25 there, whatever the size of the result)."""
-    (out, lse), (o, l, mass, size) = got, want
+    joined; the result's own type (fp16 numbers below 2^-14 are multiples of 2^-24, so that half a step is 2^-25 there, whatever the size of the result).  A value is
+    minimum + scale * code, two terms that may each be twice the group's largest value while the value is nearly nothing: with weights times scales as two fp16 numbers (2^-22) and the minima
+    apart, and in what the sums over keys lose, it is those terms that count."""
+    (out, lse), (o, l, (mass, coarse), size) = got, want
     rows = slice(0, rows)
-    out, lse, o, l, mass, size = out[rows].double(), lse[rows].double(), o[rows], l[rows], mass[rows], size[rows]
+    out, lse, o, l, mass, coarse, size = out[rows].double(), lse[rows].double(), o[rows], l[rows], mass[rows], coarse[rows], size[rows]
     score = 2.0 ** -17 * size + 2.0 ** -17
     assert torch.equal(torch.isnan(lse), torch.isnan(l)) and torch.equal(lse == -math.inf, l == -math.inf)
     fine = torch.isfinite(l)
     err = torch.where(fine, (lse - l).abs(), 0.0)
     assert bool((err <= score + 2.0 ** -23 * torch.where(fine, l.abs(), 0.0))[fine].all()), float((err / score)[fine].max())
     assert torch.equal(torch.isnan(out), torch.isnan(o))
-    bound = HALF_STEP[dtype] * o.abs() + (2 * 2.0 ** -11 * 1.01 + 2 * score + 2 * keys / 16 * 2.0 ** -23)[..., None] * mass + 2.0 ** -25 * mass.amax(-1, keepdim=True) + (2.0 ** -25 if dtype is torch.float16 else 1e-37)
+    bound = HALF_STEP[dtype] * o.abs() + (2 * 2.0 ** -11 * 1.01 + 2 * score)[..., None] * mass + (4 * 2.0 ** -22 + 4 * (keys / 16 + 2) * 2.0 ** -23) * coarse + 2.0 ** -25 * coarse.amax(-1, keepdim=True) + (2.0 ** -25 if dtype is torch.float16 else 1e-37)
     bad = (out - o).abs() > bound
     assert not bool(bad.any()), float(((out - o).abs() / bound)[torch.isfinite(o)].max())
 
