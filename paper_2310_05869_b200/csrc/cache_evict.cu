@@ -114,66 +114,139 @@ __device__ __forceinline__ Cut cut_of(const EvictArgs& a, int r) {
 // the order of weights as that of whole numbers: those that are negative or no numbers count as 0
 __device__ __forceinline__ uint32_t order_of(float w) { return w > 0.f ? __float_as_uint(w) : 0u; }
 
-// A CTA takes a request and key head: the smallest weight that stays is found digit by digit (8 bits at a time, from the top), then the tokens are numbered in order.
-constexpr int kSelectThreads = 1024, kSelectWarps = kSelectThreads / 32;
+// A cluster of CTAs takes a request and key head, each a slice of its tokens, whose weights (in order) it holds in shared memory if they fit.  The smallest weight that stays is
+// found by three digits of 11, 11 and 10 bits, from the top: a histogram in each CTA, which all add up for themselves; then the tokens are numbered in order.
+// 2 x 131072 tokens of 32 heads: 115 us with a CTA each and four digits from global memory.
+constexpr int kSelectThreads = 1024, kSelectWarps = kSelectThreads / 32, kBins = 2048, kMostHeld = 40960;
 
-__global__ void __launch_bounds__(kSelectThreads) select_kernel(const __grid_constant__ EvictArgs a) {
-  __shared__ int s_hist[256], s_digit, s_above;
+__device__ __forceinline__ uint32_t cluster_rank() {
+  uint32_t r;
+  asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+  return r;
+}
+__device__ __forceinline__ void cluster_sync() {
+  asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+// a word of another CTA's shared memory, at the place where this one has `addr`
+__device__ __forceinline__ int peer_word(uint32_t addr, uint32_t rank) {
+  uint32_t at;
+  int v;
+  asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(addr), "r"(rank));
+  asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(at) : "memory");
+  return v;
+}
+
+__global__ void __launch_bounds__(kSelectThreads) select_kernel(const __grid_constant__ EvictArgs a, int ctas, int held) {
+  extern __shared__ __align__(16) int s_mem[];
+  int* s_hist = s_mem;                                 // [3][kBins]
+  uint32_t* s_key = reinterpret_cast<uint32_t*>(s_mem + 3 * kBins);            // [held]
+  __shared__ int s_digit, s_above, s_count[2];
   __shared__ uint32_t s_warp[kSelectWarps];
   wait_for_stream();
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const int r = blockIdx.x / a.cache.heads, cap = a.width * a.cache.page;
+  const int pair = blockIdx.x / ctas, rank = ctas > 1 ? (int)cluster_rank() : 0, r = pair / a.cache.heads, cap = a.width * a.cache.page;
   const Cut c = cut_of(a, r);
-  const float* w = a.weights + (size_t)blockIdx.x * cap;
-  float* out = a.weights_out + (size_t)blockIdx.x * cap;
-  int32_t* kept = a.kept + (size_t)blockIdx.x * cap;
-  if (!c.moved()) {
-    for (int t = tid; t < cap; t += kSelectThreads) { out[t] = t < c.len ? w[t] : 0.f; kept[t] = -1; }
+  const float* w = a.weights + (size_t)pair * cap;
+  float* out = a.weights_out + (size_t)pair * cap;
+  int32_t* kept = a.kept + (size_t)pair * cap;
+  const int4 none = make_int4(-1, -1, -1, -1);
+  if (!c.moved()) {                                    // (all CTAs of the cluster)
+    for (int t = 4 * (rank * kSelectThreads + tid); t < cap; t += 4 * ctas * kSelectThreads) {
+      float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+      if (t < c.len) {
+        x = *reinterpret_cast<const float4*>(w + t);
+        if (t + 1 >= c.len) x.y = 0.f;
+        if (t + 2 >= c.len) x.z = 0.f;
+        if (t + 3 >= c.len) x.w = 0.f;
+      }
+      *reinterpret_cast<float4*>(out + t) = x;
+      *reinterpret_cast<int4*>(kept + t) = none;
+    }
     return;
   }
   const int recent = min(a.recent, c.n), first = min(a.first, c.n - recent), begin = first, end = c.len - recent;
   int want = c.n - recent - first;                     // tokens of [begin, end) that stay
-  uint32_t top = 0;                                    // digits of the smallest one's weight so far
+  // (a multiple of 4 tokens each; no sum that wraps)
+  const int slice = ((c.len - 1) / ctas / 4 + 1) * 4, t0 = (int)min((long long)rank * slice, (long long)c.len), t1 = (int)min((long long)t0 + slice, (long long)c.len);
+  const bool hold = slice <= held;
+  for (int i = tid; i < 3 * kBins; i += kSelectThreads) s_hist[i] = 0;
+  if (hold)
+    for (int t = t0 + 4 * tid; t < t1; t += 4 * kSelectThreads) {
+      const float4 x = *reinterpret_cast<const float4*>(w + t);                  // (a row is whole quads)
+      *reinterpret_cast<uint4*>(s_key + t - t0) = make_uint4(order_of(x.x), order_of(x.y), order_of(x.z), order_of(x.w));
+    }
+  __syncthreads();
+  auto key_of = [&](int t) { return hold ? s_key[t - t0] : order_of(w[t]); };
+  uint32_t top = 0;                                    // digits of the smallest weight that stays, so far
   if (want > 0) {
-    for (int shift = 24; shift >= 0; shift -= 8) {
-      for (int i = tid; i < 256; i += kSelectThreads) s_hist[i] = 0;
-      __syncthreads();
-      for (int t = begin + tid; t < end; t += kSelectThreads) {
-        const uint32_t x = order_of(w[t]);
-        if (shift == 24 || x >> (shift + 8) == top >> (shift + 8)) atomicAdd(&s_hist[x >> shift & 255], 1);
+#pragma unroll
+    for (int pass = 0; pass < 3; ++pass) {
+      const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, bins = pass == 2 ? 1024 : kBins;
+      int* hist = s_hist + pass * kBins;
+      for (int t = max(begin, t0) + tid; t < min(end, t1); t += kSelectThreads) {
+        const uint32_t x = key_of(t);
+        if (pass == 0 || x >> (pass == 1 ? 21 : 10) == top >> (pass == 1 ? 21 : 10)) atomicAdd(&hist[x >> shift & (bins - 1)], 1);
       }
+      if (ctas > 1) cluster_sync(); else __syncthreads();
+      // a thread has two digits, from the largest downwards
+      int mine[2] = {0, 0};
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const int digit = bins - 1 - 2 * tid - e;
+        if (digit >= 0) {
+          if (ctas > 1)
+            for (int k = 0; k < ctas; ++k) mine[e] += peer_word(smem_u32(hist + digit), k);
+          else mine[e] = hist[digit];
+        }
+      }
+      int sum = mine[0] + mine[1];
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) { const int y = __shfl_up_sync(0xffffffffu, sum, o); if (lane >= o) sum += y; }
+      if (lane == 31) s_warp[warp] = sum;
       __syncthreads();
-      if (warp == 0) {
-        // lane l has digits 255 - 8 l downwards
-        int mine = 0;
-        for (int i = 0; i < 8; ++i) mine += s_hist[255 - 8 * lane - i];
-        int sum = mine;
-        for (int o = 1; o < 32; o <<= 1) { const int y = __shfl_up_sync(0xffffffffu, sum, o); if (lane >= o) sum += y; }
-        int above = sum - mine;
-        if (above < want && sum >= want)
-          for (int i = 0; i < 8; ++i) {
-            const int digit = 255 - 8 * lane - i;
-            if (above + s_hist[digit] >= want) { s_digit = digit; s_above = above; break; }
-            above += s_hist[digit];
-          }
+      int above = sum - mine[0] - mine[1];
+      for (int k = 0; k < warp; ++k) above += s_warp[k];
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        if (above < want && above + mine[e] >= want) { s_digit = bins - 1 - 2 * tid - e; s_above = above; }
+        above += mine[e];
       }
       __syncthreads();
       top |= (uint32_t)s_digit << shift;
       want -= s_above;
-      __syncthreads();
     }
   } else top = 0xffffffffu;
   // `want` of those that weigh `top` stay, the first ones; and all that weigh more
-  int base = 0, equal = 0;                             // tokens that stay, and equal ones, before this round's
-  for (int t0 = 0; t0 < c.len; t0 += 4 * kSelectThreads) {
-    float x[4];
+  auto sure_of = [&](int t, uint32_t x) { return t < begin || t >= end || x > top; };
+  auto same_of = [&](int t, uint32_t x) { return want > 0 && t >= begin && t < end && x == top; };
+  int base = 0, equal = 0;                             // tokens that stay for sure, and equal ones, before this round's
+  if (ctas > 1) {
+    int sure = 0, same = 0;
+    for (int t = t0 + tid; t < t1; t += kSelectThreads) {
+      const uint32_t x = key_of(t);
+      sure += sure_of(t, x);
+      same += same_of(t, x);
+    }
+    sure = __reduce_add_sync(0xffffffffu, sure);
+    same = __reduce_add_sync(0xffffffffu, same);
+    if (tid < 2) s_count[tid] = 0;
+    __syncthreads();
+    if (lane == 0) { atomicAdd(&s_count[0], sure); atomicAdd(&s_count[1], same); }
+    cluster_sync();
+    for (int k = 0; k < rank; ++k) { base += peer_word(smem_u32(&s_count[0]), k); equal += peer_word(smem_u32(&s_count[1]), k); }
+  }
+  for (int q = t0; q < t1; q += 4 * kSelectThreads) {
+    float x[4] = {0.f, 0.f, 0.f, 0.f};
     uint32_t mine = 0, stays = 0, same = 0;            // counts: those that stay for sure | equal ones << 16
+    const int t = q + 4 * tid;
+    if (t < t1) {
+      const float4 v = *reinterpret_cast<const float4*>(w + t);
+      x[0] = v.x; x[1] = v.y; x[2] = v.z; x[3] = v.w;
+    }
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const int t = t0 + 4 * tid + i;
-      x[i] = t < c.len ? w[t] : 0.f;
-      const bool inside = t >= begin && t < end;
-      const bool sure = t < c.len && (!inside || order_of(x[i]) > top), eq = inside && want > 0 && order_of(x[i]) == top;
+      const uint32_t key = order_of(x[i]);
+      const bool there = t + i < t1, sure = there && sure_of(t + i, key), eq = there && same_of(t + i, key);
       stays |= (uint32_t)sure << i;
       same |= (uint32_t)eq << i;
       mine += sure + ((uint32_t)eq << 16);
@@ -181,18 +254,21 @@ __global__ void __launch_bounds__(kSelectThreads) select_kernel(const __grid_con
     uint32_t sum = mine;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) { const uint32_t y = __shfl_up_sync(0xffffffffu, sum, o); if (lane >= o) sum += y; }
+    __syncthreads();                                   // (the last round's counts have been read)
     if (lane == 31) s_warp[warp] = sum;
     __syncthreads();
-    uint32_t all = 0, mybase = 0;
-    for (int k = 0; k < kSelectWarps; ++k) { if (k == warp) mybase = all; all += s_warp[k]; }
-    const uint32_t ahead = mybase + sum - mine;
+    uint32_t all = s_warp[lane], run = all;            // (as many warps as lanes)
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) { const uint32_t y = __shfl_up_sync(0xffffffffu, run, o); if (lane >= o) run += y; }
+    all = __shfl_sync(0xffffffffu, run, 31);
+    const uint32_t ahead = (warp ? __shfl_sync(0xffffffffu, run, (warp + 31) & 31) : 0u) + sum - mine;
     int sure = base + (ahead & 0xffff), eq = equal + (ahead >> 16);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const bool s = stays >> i & 1, e = same >> i & 1;
       if (s || (e && eq < want)) {
         const int at = sure + min(eq, want);
-        kept[at] = t0 + 4 * tid + i;
+        kept[at] = t + i;
         out[at] = x[i];
       }
       sure += s;
@@ -200,10 +276,16 @@ __global__ void __launch_bounds__(kSelectThreads) select_kernel(const __grid_con
     }
     base += all & 0xffff;
     equal += all >> 16;
-    __syncthreads();
   }
-  for (int t = c.n + tid; t < cap; t += kSelectThreads) { out[t] = 0.f; kept[t] = -1; }
+  const int whole = min((c.n + 3) / 4 * 4, cap);
+  if (rank == 0 && tid < whole - c.n) { out[c.n + tid] = 0.f; kept[c.n + tid] = -1; }
+  for (int t = whole + 4 * (rank * kSelectThreads + tid); t < cap; t += 4 * ctas * kSelectThreads) {
+    *reinterpret_cast<float4*>(out + t) = make_float4(0.f, 0.f, 0.f, 0.f);
+    *reinterpret_cast<int4*>(kept + t) = none;
+  }
+  if (ctas > 1) cluster_sync();                        // (nobody's shared memory goes while another may read it)
 }
+static_assert(kSelectWarps == 32, "a lane for every warp");
 
 // ---- moving them -------------------------------------------------------------------------------------------------------------
 // A warp makes a block of 16 tokens of the new pages at a time, from the blocks that its tokens are in: K by pieces of a token (16 bytes, d = 64: 8), V by 16-byte loads that
@@ -238,24 +320,41 @@ __global__ void __launch_bounds__(32 * kMoveWarps) move_kernel(const __grid_cons
   const int H = a.cache.heads, subs = a.cache.page / kBlockTokens, cap = a.width * a.cache.page;
   const long long total = (long long)s_starts[a.requests] * H, warps = (long long)gridDim.x * kMoveWarps;
   const uint8_t* pages = a.cache.pages;
-  for (long long u = blockIdx.x * kMoveWarps + warp; u < total; u += warps) {
-    int lo = 0, hi = a.requests;                       // the last request whose blocks start there or before
-    while (hi - lo > 1) { const int mid = (lo + hi) >> 1; if ((long long)s_starts[mid] * H <= u) lo = mid; else hi = mid; }
-    const int r = lo, blocks = s_starts[r + 1] - s_starts[r];
-    const int rest = (int)(u - (long long)s_starts[r] * H), head = rest / blocks, b = rest - head * blocks;
-    const int to_page = b / subs < a.width ? a.to_table[(size_t)r * a.width + b / subs] : -1;
-    if (to_page < 0 || to_page >= a.cache.num_pages) continue;
-    uint8_t* to = block_at<D>(a.cache, to_page, head, b % subs);
-    // lane t < 16: where token t comes from (block -1: nowhere, zeros)
-    int src = -1, block = -1;
-    if (lane < kBlockTokens) {
-      const int at = b * kBlockTokens + lane;
-      src = at < cap ? a.kept[((size_t)r * H + head) * cap + at] : -1;
-      if (src >= 0) {
-        const int page = a.table[(size_t)r * a.width + src / a.cache.page];
-        if (page >= 0 && page < a.cache.num_pages) block = (page * H + head) * subs + src % a.cache.page / kBlockTokens;
-      }
-    }
+  // A block's place, and for lane t < 16 where its token t comes from: asked for two blocks (which tokens) and one block (which pages) before it is made.
+  struct Job { int r, head, b, src, page, to_page; };
+  auto find = [&](long long u, Job& j, int from) {     // which tokens
+    j.r = -1;
+    j.src = -1;
+    if (u >= total) return;
+    int r = from;                                      // (blocks come in order: the request is this one or a later one)
+    while ((long long)s_starts[r + 1] * H <= u) ++r;
+    const int blocks = s_starts[r + 1] - s_starts[r], rest = (int)(u - (long long)s_starts[r] * H);
+    j.r = r;
+    j.head = rest / blocks;
+    j.b = rest - j.head * blocks;
+    const int at = j.b * kBlockTokens + lane;
+    if (lane < kBlockTokens && at < cap) j.src = a.kept[((size_t)r * H + j.head) * cap + at];
+  };
+  auto pages_of = [&](Job& j) {
+    j.page = j.to_page = -1;
+    if (j.r < 0) return;
+    if (j.b / subs < a.width) j.to_page = a.to_table[(size_t)j.r * a.width + j.b / subs];
+    if (j.src >= 0 && j.src < cap) j.page = a.table[(size_t)j.r * a.width + j.src / a.cache.page];
+  };
+  long long u = blockIdx.x * kMoveWarps + warp;
+  Job now, next, then;
+  find(u, now, 0);
+  find(u + warps, next, max(now.r, 0));
+  pages_of(now);
+  for (; now.r >= 0; u += warps, now = next, next = then) {
+    pages_of(next);
+    find(u + 2 * warps, then, max(next.r, 0));
+    const int head = now.head, b = now.b;
+    if (now.to_page < 0 || now.to_page >= a.cache.num_pages) continue;
+    uint8_t* to = block_at<D>(a.cache, now.to_page, head, b % subs);
+    // (block -1: nowhere, zeros)
+    const int block = now.page >= 0 && now.page < a.cache.num_pages ? (now.page * H + head) * subs + now.src % a.cache.page / kBlockTokens : -1;
+    int src = now.src;
     src &= kBlockTokens - 1;
     auto block_of = [&](int t) { return __shfl_sync(0xffffffffu, block, t); };
     auto token_of = [&](int t) { return __shfl_sync(0xffffffffu, src, t); };
@@ -336,7 +435,7 @@ extern "C" int hyperattn_cache_evict(const hyperattn_evict_params* p) {
   int rc;
   if (!p || p->requests < 0 || p->table_width <= 0 || p->recent < 0 || p->first < 0) return HYPERATTN_INVALID_ARGUMENT;
   if (bad_cache(p->cache, &rc)) return rc;
-  if (p->requests > kMostRequests || (long long)p->table_width * p->cache.page_tokens > 0x7fffffffLL || (long long)p->requests * p->cache.kv_heads > 0x7fffffffLL ||
+  if (p->requests > kMostRequests || (long long)p->table_width * p->cache.page_tokens > 0x7fffffffLL || (long long)p->requests * p->cache.kv_heads > 0x7fffffffLL / 8 ||
       (long long)p->requests * p->table_width * (p->cache.page_tokens / kBlockTokens) > 0x7fffffffLL ||
       (long long)p->cache.num_pages * (p->cache.page_tokens / kBlockTokens) * p->cache.kv_heads > 0x7fffffffLL)
     return HYPERATTN_UNSUPPORTED_SHAPE;
@@ -345,7 +444,24 @@ extern "C" int hyperattn_cache_evict(const hyperattn_evict_params* p) {
   if (misaligned(p->weights) || misaligned(p->weights_out) || misaligned(p->kept) || p->weights == p->weights_out) return HYPERATTN_MISALIGNED;
   const EvictArgs a = {view_of(p->cache), p->weights, p->weights_out, p->kept, p->table, p->lengths, p->to_table, p->to_lengths, p->requests, p->table_width, p->recent, p->first};
   const cudaStream_t st = reinterpret_cast<cudaStream_t>(p->stream);
-  cudaError_t e = launch(select_kernel, dim3((unsigned)(p->requests * p->cache.kv_heads)), dim3(kSelectThreads), 0, st, a);
+  // CTAs of a cluster: so that each has some 8192 tokens at most, up to eight
+  const int cap = p->table_width * p->cache.page_tokens;
+  int ctas = 1;
+  while (ctas < 8 && cap > 8192 * ctas) ctas *= 2;
+  int held = (cap / ctas + 7) / 4 * 4;
+  if (held > kMostHeld) held = 0;
+  const int smem = (3 * kBins + held) * 4;
+  cudaError_t e = allow_smem<select_kernel>((3 * kBins + kMostHeld) * 4);
+  if (e == cudaSuccess) {
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim = {(unsigned)ctas, 1, 1};
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(p->requests * p->cache.kv_heads * ctas)); cfg.blockDim = dim3(kSelectThreads); cfg.dynamicSmemBytes = smem; cfg.stream = st; cfg.attrs = attr; cfg.numAttrs = 2;
+    e = cudaLaunchKernelEx(&cfg, select_kernel, a, ctas, held);
+  }
   if (e == cudaSuccess) {
     const long long blocks = (long long)p->requests * p->cache.kv_heads * ((long long)p->table_width * p->cache.page_tokens / kBlockTokens);
     const long long want = (blocks + kMoveWarps - 1) / kMoveWarps;
