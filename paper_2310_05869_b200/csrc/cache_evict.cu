@@ -115,8 +115,7 @@ __device__ __forceinline__ Cut cut_of(const EvictArgs& a, int r) {
 __device__ __forceinline__ uint32_t order_of(float w) { return w > 0.f ? __float_as_uint(w) : 0u; }
 
 // A cluster of CTAs takes a request and key head, each a slice of its tokens, whose weights (in order) it holds in shared memory if they fit.  The smallest weight that stays is
-// found by three digits of 11, 11 and 10 bits, from the top: a histogram in each CTA, which all add up for themselves; then the tokens are numbered in order.
-// 2 x 131072 tokens of 32 heads: 115 us with a CTA each and four digits from global memory.
+// found by three digits of 10, 11 and 10 bits, from the top: a histogram in each CTA, which all add up for themselves.  Then every warp counts a part of the slice, and numbers it.
 constexpr int kSelectThreads = 1024, kSelectWarps = kSelectThreads / 32, kBins = 2048, kMostHeld = 40960;
 
 __device__ __forceinline__ uint32_t cluster_rank() {
@@ -170,112 +169,93 @@ __global__ void __launch_bounds__(kSelectThreads) select_kernel(const __grid_con
   const int slice = ((c.len - 1) / ctas / 4 + 1) * 4, t0 = (int)min((long long)rank * slice, (long long)c.len), t1 = (int)min((long long)t0 + slice, (long long)c.len);
   const bool hold = slice <= held;
   for (int i = tid; i < 3 * kBins; i += kSelectThreads) s_hist[i] = 0;
-  if (hold)
-    for (int t = t0 + 4 * tid; t < t1; t += 4 * kSelectThreads) {
-      const float4 x = *reinterpret_cast<const float4*>(w + t);                  // (a row is whole quads)
-      *reinterpret_cast<uint4*>(s_key + t - t0) = make_uint4(order_of(x.x), order_of(x.y), order_of(x.z), order_of(x.w));
-    }
   __syncthreads();
   auto key_of = [&](int t) { return hold ? s_key[t - t0] : order_of(w[t]); };
+  auto inside = [&](int t) { return t >= begin && t < end; };
   uint32_t top = 0;                                    // digits of the smallest weight that stays, so far
-  if (want > 0) {
 #pragma unroll
-    for (int pass = 0; pass < 3; ++pass) {
-      const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, bins = pass == 2 ? 1024 : kBins;
-      int* hist = s_hist + pass * kBins;
+  for (int pass = 0; pass < 3; ++pass) {
+    const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, bins = pass == 1 ? 2048 : 1024;
+    int* hist = s_hist + pass * kBins;
+    if (pass == 0) {
+      for (int t = t0 + 4 * tid; t < t1; t += 4 * kSelectThreads) {
+        const float4 x = *reinterpret_cast<const float4*>(w + t);                // (a row is whole quads)
+        const uint4 k = make_uint4(order_of(x.x), order_of(x.y), order_of(x.z), order_of(x.w));
+        if (hold) *reinterpret_cast<uint4*>(s_key + t - t0) = k;
+        if (inside(t)) atomicAdd(&hist[k.x >> 21], 1);
+        if (inside(t + 1) && t + 1 < t1) atomicAdd(&hist[k.y >> 21], 1);
+        if (inside(t + 2) && t + 2 < t1) atomicAdd(&hist[k.z >> 21], 1);
+        if (inside(t + 3) && t + 3 < t1) atomicAdd(&hist[k.w >> 21], 1);
+      }
+    } else {
+      const int done = pass == 1 ? 21 : 10;
       for (int t = max(begin, t0) + tid; t < min(end, t1); t += kSelectThreads) {
         const uint32_t x = key_of(t);
-        if (pass == 0 || x >> (pass == 1 ? 21 : 10) == top >> (pass == 1 ? 21 : 10)) atomicAdd(&hist[x >> shift & (bins - 1)], 1);
+        if (x >> done == top >> done) atomicAdd(&hist[x >> shift & (bins - 1)], 1);
       }
-      if (ctas > 1) cluster_sync(); else __syncthreads();
-      // a thread has two digits, from the largest downwards
-      int mine[2] = {0, 0};
+    }
+    if (ctas > 1) cluster_sync(); else __syncthreads();
+    // a thread has one digit or two, from the largest downwards
+    const int each = bins / kSelectThreads;
+    int mine[2] = {0, 0};
 #pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        const int digit = bins - 1 - 2 * tid - e;
-        if (digit >= 0) {
-          if (ctas > 1)
-            for (int k = 0; k < ctas; ++k) mine[e] += peer_word(smem_u32(hist + digit), k);
-          else mine[e] = hist[digit];
-        }
-      }
-      int sum = mine[0] + mine[1];
+    for (int e = 0; e < each; ++e) {
+      const int digit = bins - 1 - each * tid - e;
+      if (ctas > 1) {
+#pragma unroll 8
+        for (int k = 0; k < ctas; ++k) mine[e] += peer_word(smem_u32(hist + digit), k);
+      } else mine[e] = hist[digit];
+    }
+    int sum = mine[0] + mine[1];
 #pragma unroll
-      for (int o = 1; o < 32; o <<= 1) { const int y = __shfl_up_sync(0xffffffffu, sum, o); if (lane >= o) sum += y; }
-      if (lane == 31) s_warp[warp] = sum;
-      __syncthreads();
-      int above = sum - mine[0] - mine[1];
-      for (int k = 0; k < warp; ++k) above += s_warp[k];
+    for (int o = 1; o < 32; o <<= 1) { const int y = __shfl_up_sync(0xffffffffu, sum, o); if (lane >= o) sum += y; }
+    if (lane == 31) s_warp[warp] = sum;
+    __syncthreads();
+    const int before = lane < warp ? (int)s_warp[lane] : 0;
+    int above = __reduce_add_sync(0xffffffffu, before) + sum - mine[0] - mine[1];
 #pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        if (above < want && above + mine[e] >= want) { s_digit = bins - 1 - 2 * tid - e; s_above = above; }
-        above += mine[e];
-      }
-      __syncthreads();
+    for (int e = 0; e < each; ++e) {
+      if (above < want && above + mine[e] >= want) { s_digit = bins - 1 - each * tid - e; s_above = above; }
+      above += mine[e];
+    }
+    __syncthreads();
+    if (want > 0) {                                    // (0: none of these stays)
       top |= (uint32_t)s_digit << shift;
       want -= s_above;
     }
-  } else top = 0xffffffffu;
-  // `want` of those that weigh `top` stay, the first ones; and all that weigh more
-  auto sure_of = [&](int t, uint32_t x) { return t < begin || t >= end || x > top; };
-  auto same_of = [&](int t, uint32_t x) { return want > 0 && t >= begin && t < end && x == top; };
-  int base = 0, equal = 0;                             // tokens that stay for sure, and equal ones, before this round's
-  if (ctas > 1) {
-    int sure = 0, same = 0;
-    for (int t = t0 + tid; t < t1; t += kSelectThreads) {
-      const uint32_t x = key_of(t);
-      sure += sure_of(t, x);
-      same += same_of(t, x);
-    }
-    sure = __reduce_add_sync(0xffffffffu, sure);
-    same = __reduce_add_sync(0xffffffffu, same);
-    if (tid < 2) s_count[tid] = 0;
-    __syncthreads();
-    if (lane == 0) { atomicAdd(&s_count[0], sure); atomicAdd(&s_count[1], same); }
-    cluster_sync();
-    for (int k = 0; k < rank; ++k) { base += peer_word(smem_u32(&s_count[0]), k); equal += peer_word(smem_u32(&s_count[1]), k); }
   }
-  for (int q = t0; q < t1; q += 4 * kSelectThreads) {
-    float x[4] = {0.f, 0.f, 0.f, 0.f};
-    uint32_t mine = 0, stays = 0, same = 0;            // counts: those that stay for sure | equal ones << 16
-    const int t = q + 4 * tid;
-    if (t < t1) {
-      const float4 v = *reinterpret_cast<const float4*>(w + t);
-      x[0] = v.x; x[1] = v.y; x[2] = v.z; x[3] = v.w;
+  if (want == 0) top = 0xffffffffu;
+  // `want` of those that weigh `top` stay, the first ones; and all that weigh more.  A warp has consecutive tokens
+  const int part = ((t1 - t0 + kSelectWarps - 1) / kSelectWarps + 31) / 32 * 32, p0 = min(t0 + warp * part, t1), p1 = min(p0 + part, t1);
+  int sure = 0, same = 0;                              // tokens that stay for sure, and equal ones: of the warp, then before it
+  for (int t = p0 + lane; t < p1 + lane; t += 32) {
+    const uint32_t x = t < p1 ? key_of(t) : 0u;
+    sure += __popc(__ballot_sync(0xffffffffu, t < p1 && (!inside(t) || x > top)));
+    same += __popc(__ballot_sync(0xffffffffu, t < p1 && inside(t) && x == top));
+  }
+  uint2* s_part = reinterpret_cast<uint2*>(s_hist);    // [kSelectWarps] (the first digit's histogram has been read by all: two rounds ago)
+  if (lane == 0) s_part[warp] = make_uint2(sure, same);
+  __syncthreads();
+  uint2 counts = s_part[lane];
+  int ahead_sure = __reduce_add_sync(0xffffffffu, lane < warp ? counts.x : 0u), ahead_same = __reduce_add_sync(0xffffffffu, lane < warp ? counts.y : 0u);
+  if (ctas > 1) {
+    const int all_sure = __reduce_add_sync(0xffffffffu, counts.x), all_same = __reduce_add_sync(0xffffffffu, counts.y);
+    if (tid == 0) { s_count[0] = all_sure; s_count[1] = all_same; }
+    cluster_sync();
+    for (int k = 0; k < rank; ++k) { ahead_sure += peer_word(smem_u32(&s_count[0]), k); ahead_same += peer_word(smem_u32(&s_count[1]), k); }
+  }
+  for (int t = p0 + lane; t < p1 + lane; t += 32) {
+    const uint32_t x = t < p1 ? key_of(t) : 0u;
+    const bool s = t < p1 && (!inside(t) || x > top), e = t < p1 && inside(t) && x == top;
+    const unsigned ms = __ballot_sync(0xffffffffu, s), me = __ballot_sync(0xffffffffu, e), below = (1u << lane) - 1;
+    const int eq = ahead_same + __popc(me & below);
+    if (s || (e && eq < want)) {
+      const int at = ahead_sure + __popc(ms & below) + min(eq, want);
+      kept[at] = t;
+      out[at] = w[t];
     }
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const uint32_t key = order_of(x[i]);
-      const bool there = t + i < t1, sure = there && sure_of(t + i, key), eq = there && same_of(t + i, key);
-      stays |= (uint32_t)sure << i;
-      same |= (uint32_t)eq << i;
-      mine += sure + ((uint32_t)eq << 16);
-    }
-    uint32_t sum = mine;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) { const uint32_t y = __shfl_up_sync(0xffffffffu, sum, o); if (lane >= o) sum += y; }
-    __syncthreads();                                   // (the last round's counts have been read)
-    if (lane == 31) s_warp[warp] = sum;
-    __syncthreads();
-    uint32_t all = s_warp[lane], run = all;            // (as many warps as lanes)
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) { const uint32_t y = __shfl_up_sync(0xffffffffu, run, o); if (lane >= o) run += y; }
-    all = __shfl_sync(0xffffffffu, run, 31);
-    const uint32_t ahead = (warp ? __shfl_sync(0xffffffffu, run, (warp + 31) & 31) : 0u) + sum - mine;
-    int sure = base + (ahead & 0xffff), eq = equal + (ahead >> 16);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const bool s = stays >> i & 1, e = same >> i & 1;
-      if (s || (e && eq < want)) {
-        const int at = sure + min(eq, want);
-        kept[at] = t + i;
-        out[at] = x[i];
-      }
-      sure += s;
-      eq += e;
-    }
-    base += all & 0xffff;
-    equal += all >> 16;
+    ahead_sure += __popc(ms);
+    ahead_same += __popc(me);
   }
   const int whole = min((c.n + 3) / 4 * 4, cap);
   if (rank == 0 && tid < whole - c.n) { out[c.n + tid] = 0.f; kept[c.n + tid] = -1; }
