@@ -118,7 +118,6 @@ struct CCfg {
   // TMEM columns: O_0, O_1, Q_0, Q_1, S_0, S_1; at d = 64 P_i beside S_i, so that the next scores do not wait for this tile's weights
   static constexpr bool kOwnP = D == 64;
   static constexpr uint32_t kColQ = 2 * D, kColS = 3 * D;
-  static constexpr int kArithmetic = 8;
   __host__ __device__ static constexpr uint32_t col_p(int i) { return kOwnP ? kColS + 2 * kKeys + (kKeys / 2) * i : kColS + kKeys * i; }
 };
 
@@ -341,32 +340,25 @@ __global__ void __launch_bounds__(kCThreads, 1) chunk_kernel(const __grid_consta
             const float off = (ref == -INFINITY ? 0.f : -ref) - less;
             const uint64_t off2 = pack_f2(off, off);
             uint64_t tile2 = 0;
-            float most = -INFINITY;
 #pragma unroll
             for (int c = 0; c < 2; ++c) {
               uint32_t p[16];
 #pragma unroll
               for (int e = 0; e < 16; ++e) {
                 const uint64_t x2 = ffma2(pack_u2(r[c][2 * e], r[c][2 * e + 1]), sc2, off2);
-                uint64_t w2;
-                if (e % C::kArithmetic == C::kArithmetic - 1) w2 = exp2_pair<false>(x2, most);
-                else {
-                  float x, y;
-                  unpack_f2(x2, x, y);
-                  w2 = pack_f2(ex2(x), ex2(y));
-                }
-                tile2 = fadd2(tile2, w2);
                 float x, y;
-                unpack_f2(w2, x, y);
+                unpack_f2(x2, x, y);
+                x = ex2(x);
+                y = ex2(y);
+                tile2 = fadd2(tile2, pack_f2(x, y));
                 p[e] = from_float2<__half>(x, y);
               }
               tmem_st16(pcol + 16 * c, p);
             }
             float t0, t1;
             unpack_f2(tile2, t0, t1);
-            const bool over = there && !(t0 + t1 <= kSumLimit && most <= kMostByArithmetic);
+            const bool over = there && !(t0 + t1 <= kSumLimit);
             if (attempt > 0 || !__any_sync(0xffffffffu, over)) {
-              if (attempt > 0 && !(most <= kMostByArithmetic)) tile2 = pack_f2(NAN, NAN);
               const float back = exp2f(less);
               sum2 = ffma2(tile2, pack_f2(back, back), sum2);
               break;
@@ -743,7 +735,7 @@ __global__ void __launch_bounds__(kCThreads, 1) chunk_kernel(const __grid_consta
         const long long first = x - (rest - d.kv * whole), last = first + whole;               // the segment's
         d.tile0 = (int)((x - first) / k.cost);
         d.tile1 = (int)((min(last, end) - first) / k.cost);
-        d.place = x == first && last <= end ? -1 : 2 * blockIdx.x + (x > begin ? 1 : 0);
+        d.place = x == first && last <= end ? -1 : 2 * (int)blockIdx.x + (x > begin ? 1 : 0);
         x = min(last, end);
       }
       if (it >= 2) ok = warp_wait<17>(bar_piecefree(it & 1), ((it >> 1) - 1) & 1, s_abort, status);

@@ -6,6 +6,7 @@
 // queries is three.  Queries are fp16 numbers after a power of two for their row, scales and minima after one for their token (or tile), so the fp32 sums of the tensor cores are all
 // that is rounded.  (Keys rounded to 16 bits would be half the products, and scores off by 2e-4: weights and log-sum-exps are fp32 results, which show it.)
 #pragma once
+#include <climits>
 #include "serving.cuh"
 #include "tc_util.cuh"
 
@@ -34,12 +35,13 @@ __device__ __forceinline__ Span span_of(const ChunkArgs& a, int r) {
 
 // ---- queries ---------------------------------------------------------------------------------------------------------------
 // A request's rows of a key head are its tokens times the head's query heads.  NR of them, as shared memory holds them: fp16 [NR x d] with the 128-byte swizzle in slabs of 64
-// columns; sums of the groups [2][NR][8] (high parts, what those lack, what is still missing, zeros); for every two rows their factors to base-2 scores and minus
-// their log-sum-exps (weights; to base 2).  Rows that do not exist are zeros (minus infinity).
+// columns; sums of the groups [2][NR][8] (high parts, what those lack, what is still missing, zeros); minus the rows' log-sum-exps (to base 2); their factors to base-2 scores;
+// and the factor of all rows, if they have one (0: they do not).  Rows that do not exist are zeros (minus infinity).
 template <int D, int NR>
 struct Image {
-  static constexpr uint32_t kSlab = NR * 128, kSums = NR * 2 * D, kFactors = kSums + NR * 32, kBytes = (kFactors + NR * 8 + 1023) / 1024 * 1024;
+  static constexpr uint32_t kSlab = NR * 128, kSums = NR * 2 * D, kMinus = kSums + NR * 32, kFactors = kMinus + NR * 4, kFactor = kFactors + NR * 4, kBytes = (kFactor + 4 + 1023) / 1024 * 1024;
 };
+constexpr int kSpread = 12;              // octaves that a row may be smaller than the image's largest and have its factor: 2^-21 of its largest entry are still whole steps
 // The images of a request come after those of the ones before it, wherever those end: r chunks are room for what the earlier requests' last ones do not fill.
 __host__ __device__ __forceinline__ long long image_slots(long long rows_before, int requests_before, int group, int nr) { return rows_before * group / nr + requests_before; }
 
@@ -59,21 +61,42 @@ __global__ void __launch_bounds__(128) image_kernel(const __grid_constant__ Chun
   const long long row0 = (slot - image_slots(s.first, lo, group, NR)) * NR, rows = (long long)s.rows * group;
   if (row0 < 0 || row0 >= rows) return;
   uint8_t* to = a.images + (size_t)blockIdx.x * I::kBytes;
+  __shared__ int s_exp[NR], s_most, s_apart;
+  if (threadIdx.x == 0) { s_most = INT_MIN; s_apart = 0; }
   const int c = threadIdx.x % LANES;
-  for (int i = threadIdx.x / LANES; i < NR; i += AT_ONCE) {
-    const bool there = row0 + i < rows;
+  auto query = [&](int i) {
+    if (row0 + i >= rows) return make_uint4(0, 0, 0, 0);
     const int row = s.first + (int)((row0 + i) / group), head = kv * group + (int)((row0 + i) % group);
-    uint4 raw = make_uint4(0, 0, 0, 0);
-    if (there) raw = *reinterpret_cast<const uint4*>(reinterpret_cast<const T*>(a.q) + (long long)row * a.q_row + (long long)head * a.q_head + 8 * c);
+    return *reinterpret_cast<const uint4*>(reinterpret_cast<const T*>(a.q) + (long long)row * a.q_row + (long long)head * a.q_head + 8 * c);
+  };
+  // The rows' exponents.  A row is multiplied by 2^(9 - e), e the exponent of its largest entry (then a group's sum is an fp16 number, and entries 2^-33 of the largest are whole
+  // steps) - or of the image's largest, if it is not much smaller, so that all have one factor.
+  __syncthreads();
+#pragma unroll 4
+  for (int i = threadIdx.x / LANES; i < NR; i += AT_ONCE) {
+    const uint4 raw = query(i);
     const uint32_t v[4] = {raw.x, raw.y, raw.z, raw.w};
     float top = 0.f;
 #pragma unroll
     for (int k = 0; k < 4; ++k) { const float2 f = to_float2<T>(v[k]); top = fmaxf(top, fmaxf(fabsf(f.x), fabsf(f.y))); }
 #pragma unroll
     for (int o = 1; o < LANES; o <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-    // times 2^(9 - e), e the exponent of the largest entry (0 and what is not finite: as it is): a group's sum is an fp16 number, and entries 2^-33 of the largest are whole steps
-    int e = (int)(__float_as_uint(top) >> 23) - 127 - 9;
-    e = top == 0.f || !(top < INFINITY) ? 0 : min(max(e, -126), 126);
+    const int e = top == 0.f || !(top < INFINITY) ? INT_MIN : min(max((int)(__float_as_uint(top) >> 23) - 127 - 9, -126), 126);      // (0, and what is not finite: any will do)
+    if (c == 0) {
+      s_exp[i] = e;
+      if (e != INT_MIN) atomicMax(&s_most, e);
+    }
+  }
+  __syncthreads();
+  const int most = s_most == INT_MIN ? 0 : s_most;
+#pragma unroll 2
+  for (int i = threadIdx.x / LANES; i < NR; i += AT_ONCE) {
+    const bool there = row0 + i < rows;
+    const int row = s.first + (int)((row0 + i) / group), head = kv * group + (int)((row0 + i) % group);
+    const uint4 raw = query(i);
+    const uint32_t v[4] = {raw.x, raw.y, raw.z, raw.w};
+    const int own = s_exp[i], e = own == INT_MIN || most - own <= kSpread ? most : own;
+    if (c == 0 && e != most) s_apart = 1;
     const float down = __uint_as_float((uint32_t)(127 - e) << 23);
     uint32_t w[4];
     float sum = 0.f;
@@ -105,12 +128,13 @@ __global__ void __launch_bounds__(128) image_kernel(const __grid_constant__ Chun
     if (c == 0) {
       *reinterpret_cast<uint4*>(to + I::kSums + i * 16) = make_uint4(sums[0], sums[1], sums[2], sums[3]);
       *reinterpret_cast<uint4*>(to + I::kSums + (NR + i) * 16) = make_uint4(sums[4], sums[5], sums[6], sums[7]);
-      float* f = reinterpret_cast<float*>(to + I::kFactors) + i / 2 * 4 + i % 2;
-      f[0] = there ? __uint_as_float((uint32_t)(127 + e) << 23) * a.scale_log2 : 0.f;
-      const float l = there && lse ? lse[(size_t)row * a.q_heads + head] : -INFINITY;
-      f[2] = l == -INFINITY ? l : -l * 1.4426950408889634f;                // (a row that saw nothing gives nothing)
+      const float l = there ? lse[(size_t)row * a.q_heads + head] : -INFINITY;
+      reinterpret_cast<float*>(to + I::kMinus)[i] = l == -INFINITY ? l : -l * 1.4426950408889634f;           // (a row that saw nothing gives nothing)
+      reinterpret_cast<float*>(to + I::kFactors)[i] = __uint_as_float((uint32_t)(127 + e) << 23) * a.scale_log2;
     }
   }
+  __syncthreads();
+  if (threadIdx.x == 0) *reinterpret_cast<float*>(to + I::kFactor) = s_apart ? 0.f : __uint_as_float((uint32_t)(127 + most) << 23) * a.scale_log2;
 }
 
 // ---- keys ------------------------------------------------------------------------------------------------------------------

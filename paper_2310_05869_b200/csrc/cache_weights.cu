@@ -34,7 +34,7 @@ template <int D, int NR>
 struct WCfg {
   using I = Image<D, NR>;
   static constexpr uint32_t kRawBlock = 10 * D, kRaw = 8 * kRawBlock, kScales = 64 * D;           // K's half of 8 blocks: their codes, then their scales
-  static constexpr int kRawStages = D == 128 ? 6 : 8, kQStages = NR == 16 ? 6 : 4;
+  static constexpr int kRawStages = D == 128 ? 6 : 8, kQStages = 4;
   static constexpr uint32_t kOffQ = 0, kOffRaw = kQStages * I::kBytes, kOffMisc = kOffRaw + kRawStages * kRaw;
   static constexpr uint32_t kSmem = kOffMisc + 4096 + 1024;                      // (the images begin at multiples of 1024)
   static constexpr uint32_t kImage = I::kBytes;
@@ -150,6 +150,11 @@ __global__ void __launch_bounds__(kWThreads, 1) weights_kernel(const __grid_cons
     // ================= sums: a thread a token ==============================================================
     const int g = warp >> 2, t = tid & 127;
     const uint32_t lane_addr = tmem + ((uint32_t)((warp & 3) * 32) << 16);
+    auto sum_of = [](const uint64_t (&x)[2]) {
+      float s0, s1;
+      unpack_f2(fadd2(x[0], x[1]), s0, s1);
+      return s0 + s1;
+    };
     int images = 0, keyed = 0, plain = 0, shared = 0;      // images, tiles with rows, without, and with several images so far
     auto had = [&](const Walk& w, bool mine) {             // what the token had, asked for ahead
       const int token = w.j * kTileTokens + t;
@@ -163,7 +168,7 @@ __global__ void __launch_bounds__(kWThreads, 1) weights_kernel(const __grid_cons
       const bool mine = lead == g;
       if (!mine && count < 2) { images += count; keyed += count; continue; }
       const float old = had(w, mine);
-      uint64_t sum2 = 0;
+      uint64_t sum2[2] = {0, 0};
       bool there = token < w.s.len;
       if (count) {
         const int b = keyed & 1;
@@ -174,7 +179,6 @@ __global__ void __launch_bounds__(kWThreads, 1) weights_kernel(const __grid_cons
         if (count == 1 && lane == 0) mbar_arrive(bar_keyfree(b));
         ++keyed;
         there = there && f > 0.f;
-        const uint64_t f2 = pack_f2(f, f);
         // columns of all images that see the token: from `sees` on, up to the rows that there are
         const long long sees = a.causal ? (long long)(token - (w.s.len - w.s.rows)) * group : 0, rows = (long long)w.s.rows * group;
         const long long partly = a.causal ? (long long)(w.j * kTileTokens + kTileTokens - 1 - (w.s.len - w.s.rows)) * group : 0;       // (of the tile's last token)
@@ -185,31 +189,45 @@ __global__ void __launch_bounds__(kWThreads, 1) weights_kernel(const __grid_cons
           if (ok) ok = warp_wait<22>(bar_q(qs), (images / NQ) & 1, s_abort, status);                    // (it has landed: the factors beside it are visible to this thread too)
           if (!ok) break;
           tc_fence_after();
-          const float4* factors = reinterpret_cast<const float4*>(smem + C::kOffQ + qs * I::kBytes + I::kFactors);
+          const uint8_t* image = smem + C::kOffQ + qs * I::kBytes;
           const long long c0 = (long long)i * NR;
-          const bool masked = c0 < partly || c0 + NR > rows;
-          const int lo = (int)min(max(sees - c0, 0ll), (long long)NR), hi = (int)min(rows - c0, (long long)NR);
-          constexpr int STEP = NR < 32 ? NR : 32;
+          const float factor = *reinterpret_cast<const float*>(image + I::kFactor);
+          // (masks, and rows with factors of their own: a path apart)
+          auto add = [&](auto plain) {
+            constexpr bool PLAIN = decltype(plain)::value;
+            const int lo = PLAIN ? 0 : (int)min(max(sees - c0, 0ll), (long long)NR), hi = PLAIN ? NR : (int)min(rows - c0, (long long)NR);
+            const uint64_t times = pack_f2(factor * f, factor * f);
+            constexpr int STEP = 32;
 #pragma unroll
-          for (int c = 0; c < NR; c += STEP) {
-            uint32_t r[STEP];
-            if constexpr (STEP == 32) { tmem_ld32_issue(lane_addr + C::kColS + st * NR + c, r); tmem_ld32_wait(r); }
-            else { tmem_ld16_issue(lane_addr + C::kColS + st * NR + c, r); tmem_ld16_wait(r); }
-            if (c + STEP == NR) { tc_fence_before(); mbar_arrive(bar_sfree(st)); }
+            for (int c = 0; c < NR; c += STEP) {
+              uint32_t r[STEP];
+              tmem_ld32_issue(lane_addr + C::kColS + st * NR + c, r);
+              tmem_ld32_wait(r);
+              if (c + STEP == NR) { tc_fence_before(); mbar_arrive(bar_sfree(st)); }
 #pragma unroll
-            for (int e = 0; e < STEP; e += 2) {
-              const float4 q = factors[(c + e) / 2];
-              float x, y;
-              unpack_f2(ffma2(fmul2(pack_u2(r[e], r[e + 1]), f2), pack_f2(q.x, q.y), pack_f2(q.z, q.w)), x, y);
-              x = ex2(x);
-              y = ex2(y);
-              if (masked) {
-                x = c + e >= lo && c + e < hi ? x : 0.f;
-                y = c + e + 1 >= lo && c + e + 1 < hi ? y : 0.f;
+              for (int e = 0; e < STEP; e += 4) {
+                const float4 minus = reinterpret_cast<const float4*>(image + I::kMinus)[(c + e) / 4];
+                uint64_t times0 = times, times1 = times;
+                if constexpr (!PLAIN) {
+                  const float4 g = reinterpret_cast<const float4*>(image + I::kFactors)[(c + e) / 4];
+                  times0 = pack_f2(g.x * f, g.y * f);
+                  times1 = pack_f2(g.z * f, g.w * f);
+                }
+                float x[4];
+                unpack_f2(ffma2(pack_u2(r[e], r[e + 1]), times0, pack_f2(minus.x, minus.y)), x[0], x[1]);
+                unpack_f2(ffma2(pack_u2(r[e + 2], r[e + 3]), times1, pack_f2(minus.z, minus.w)), x[2], x[3]);
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                  x[k] = ex2(x[k]);
+                  if constexpr (!PLAIN) x[k] = c + e + k >= lo && c + e + k < hi ? x[k] : 0.f;
+                }
+                sum2[0] = fadd2(sum2[0], pack_f2(x[0], x[1]));
+                sum2[1] = fadd2(sum2[1], pack_f2(x[2], x[3]));
               }
-              sum2 = fadd2(sum2, pack_f2(x, y));
             }
-          }
+          };
+          if (c0 < partly || c0 + NR > rows || factor == 0.f) add(std::false_type());
+          else add(std::true_type());
           __syncwarp();
           if (lane == 0) mbar_arrive(bar_qfree(qs));
         }
@@ -220,24 +238,19 @@ __global__ void __launch_bounds__(kWThreads, 1) weights_kernel(const __grid_cons
           if (!mine) {
             if (turn > 0) ok = warp_wait<18>(bar_partfree(half), (turn - 1) & 1, s_abort, status);
             if (!ok) break;
-            float s0, s1;
-            unpack_f2(sum2, s0, s1);
-            s_part[half * 128 + t] = s0 + s1;
+            s_part[half * 128 + t] = sum_of(sum2);
             mbar_arrive(bar_part(half));
             continue;
           }
           ok = warp_wait<19>(bar_part(half), turn & 1, s_abort, status);
           if (!ok) break;
           if (lane == 0) mbar_arrive(bar_keyfree(b));
-          float s0, s1;
-          unpack_f2(sum2, s0, s1);
-          sum2 = pack_f2(s0 + s1, s_part[half * 128 + t]);
+          sum2[0] = pack_f2(sum_of(sum2), s_part[half * 128 + t]);
+          sum2[1] = 0;
           mbar_arrive(bar_partfree(half));
         }
       }
-      float s0, s1;
-      unpack_f2(sum2, s0, s1);
-      if (token < cap) p.out[at] = token < w.s.len ? (token < w.s.len - w.s.rows ? p.decay * old : 0.f) + (there ? s0 + s1 : 0.f) : 0.f;
+      if (token < cap) p.out[at] = token < w.s.len ? (token < w.s.len - w.s.rows ? p.decay * old : 0.f) + (there ? sum_of(sum2) : 0.f) : 0.f;
     }
   } else if (warp < 16) {
     // ================= keys: a thread a token ==============================================================
@@ -379,8 +392,11 @@ __global__ void __launch_bounds__(256) blank_kernel(const __grid_constant__ Weig
   for (int i = from / 4 + blockIdx.y * 256 + threadIdx.x; i < cap / 4; i += 256 * gridDim.y) to[i] = make_float4(0.f, 0.f, 0.f, 0.f);
 }
 
-constexpr int kImageRows = 64;
-long long slots_of(const hyperattn_weights_params& p) { return image_slots(p.rows, p.requests, p.q_heads / p.cache.kv_heads, kImageRows) + 1; }
+// rows of an image: a product of 64 rows takes 48 clocks, of 128 rows 64; beside two tiles' keys of d = 128 TMEM has room for the scores of two images of 96
+template <int D> constexpr int kImageRows = D == 64 ? 128 : 96;
+long long slots_of(const hyperattn_weights_params& p) {
+  return image_slots(p.rows, p.requests, p.q_heads / p.cache.kv_heads, p.cache.d == 64 ? kImageRows<64> : kImageRows<128>) + 1;
+}
 
 }  // namespace
 }  // namespace hyperattn
@@ -393,7 +409,7 @@ extern "C" int hyperattn_cache_weights_workspace_bytes(const hyperattn_weights_p
   *bytes = 0;
   if (p->requests == 0 || few_rows_weights(*p)) return HYPERATTN_OK;
   if (slots_of(*p) * p->cache.kv_heads > 0x7fffffffLL) return HYPERATTN_UNSUPPORTED_SHAPE;
-  *bytes = (size_t)(slots_of(*p) * p->cache.kv_heads) * (p->cache.d == 64 ? Image<64, kImageRows>::kBytes : Image<128, kImageRows>::kBytes);
+  *bytes = (size_t)(slots_of(*p) * p->cache.kv_heads) * (p->cache.d == 64 ? Image<64, kImageRows<64>>::kBytes : Image<128, kImageRows<128>>::kBytes);
   return HYPERATTN_OK;
 }
 
@@ -423,7 +439,7 @@ extern "C" int hyperattn_cache_weights(const hyperattn_weights_params* p) {
   if (e != cudaSuccess) return status_of(e, "cache weights");
   if (few) return launch_few_rows_weights(*p, status);
   auto go = [&](auto dim) {
-    constexpr int D = decltype(dim)::value, NR = kImageRows;
+    constexpr int D = decltype(dim)::value, NR = kImageRows<D>;
     using C = WCfg<D, NR>;
     cudaError_t e = allow_smem<weights_kernel<D, NR>>(C::kSmem);
     const dim3 slots((unsigned)(slots_of(*p) * p->cache.kv_heads));
