@@ -37,7 +37,6 @@ struct WCfg {
   static constexpr int kRawStages = D == 128 ? 6 : 8, kQStages = 4;
   static constexpr uint32_t kOffQ = 0, kOffRaw = kQStages * I::kBytes, kOffMisc = kOffRaw + kRawStages * kRaw;
   static constexpr uint32_t kSmem = kOffMisc + 4096 + 1024;                      // (the images begin at multiples of 1024)
-  static constexpr uint32_t kImage = I::kBytes;
   // TMEM columns: keys of two tiles, scores of several images
   static constexpr uint32_t kColS = 2 * KeyCols<D>::kAll;
   static constexpr int kStages = (512 - kColS) / NR < 4 ? (512 - kColS) / NR : 4;
@@ -192,30 +191,37 @@ __global__ void __launch_bounds__(kWThreads, 1) weights_kernel(const __grid_cons
           const uint8_t* image = smem + C::kOffQ + qs * I::kBytes;
           const long long c0 = (long long)i * NR;
           const float factor = *reinterpret_cast<const float*>(image + I::kFactor);
-          // (masks, and rows with factors of their own: a path apart)
-          auto add = [&](auto plain) {
-            constexpr bool PLAIN = decltype(plain)::value;
-            const int lo = PLAIN ? 0 : (int)min(max(sees - c0, 0ll), (long long)NR), hi = PLAIN ? NR : (int)min(rows - c0, (long long)NR);
-            const uint64_t times = pack_f2(factor * f, factor * f);
-            constexpr int STEP = 32;
-#pragma unroll
-            for (int c = 0; c < NR; c += STEP) {
-              uint32_t r[STEP];
-              tmem_ld32_issue(lane_addr + C::kColS + st * NR + c, r);
-              tmem_ld32_wait(r);
-              if (c + STEP == NR) { tc_fence_before(); mbar_arrive(bar_sfree(st)); }
+          // Rows that all tokens of the tile see, in steps of 32; masks, and rows with factors of their own, are a path apart; what no token sees is left out
+          const int hi = (int)min(rows - c0, (long long)NR), all = (int)min(max(partly - c0, 0ll), (long long)NR), lo = (int)min(max(sees - c0, 0ll), (long long)NR);
+          const int some = max(all - kTileTokens * group, 0);              // (the tile's first token sees rows from here on, or from further)
+          const float times = factor * f;
+          constexpr int STEP = 32;
+          const int begin_c = some / STEP * STEP;
+          if (begin_c >= hi) mbar_arrive(bar_sfree(st));
+#pragma unroll 1
+          for (int c = begin_c; c < hi; c += STEP) {
+            uint32_t r[STEP];
+            tmem_ld32_issue(lane_addr + C::kColS + st * NR + c, r);
+            const float4* minus = reinterpret_cast<const float4*>(image + I::kMinus) + c / 4;
+            tmem_ld32_wait(r);
+            if (c + STEP >= hi) {
+              tc_fence_before();
+              mbar_arrive(bar_sfree(st));
+            }
+            auto add = [&](auto plain) {
+              constexpr bool PLAIN = decltype(plain)::value;
+              uint64_t times0 = pack_f2(times, times), times1 = times0;
 #pragma unroll
               for (int e = 0; e < STEP; e += 4) {
-                const float4 minus = reinterpret_cast<const float4*>(image + I::kMinus)[(c + e) / 4];
-                uint64_t times0 = times, times1 = times;
+                const float4 m = minus[e / 4];
                 if constexpr (!PLAIN) {
                   const float4 g = reinterpret_cast<const float4*>(image + I::kFactors)[(c + e) / 4];
                   times0 = pack_f2(g.x * f, g.y * f);
                   times1 = pack_f2(g.z * f, g.w * f);
                 }
                 float x[4];
-                unpack_f2(ffma2(pack_u2(r[e], r[e + 1]), times0, pack_f2(minus.x, minus.y)), x[0], x[1]);
-                unpack_f2(ffma2(pack_u2(r[e + 2], r[e + 3]), times1, pack_f2(minus.z, minus.w)), x[2], x[3]);
+                unpack_f2(ffma2(pack_u2(r[e], r[e + 1]), times0, pack_f2(m.x, m.y)), x[0], x[1]);
+                unpack_f2(ffma2(pack_u2(r[e + 2], r[e + 3]), times1, pack_f2(m.z, m.w)), x[2], x[3]);
 #pragma unroll
                 for (int k = 0; k < 4; ++k) {
                   x[k] = ex2(x[k]);
@@ -224,10 +230,10 @@ __global__ void __launch_bounds__(kWThreads, 1) weights_kernel(const __grid_cons
                 sum2[0] = fadd2(sum2[0], pack_f2(x[0], x[1]));
                 sum2[1] = fadd2(sum2[1], pack_f2(x[2], x[3]));
               }
-            }
-          };
-          if (c0 < partly || c0 + NR > rows || factor == 0.f) add(std::false_type());
-          else add(std::true_type());
+            };
+            if (c >= all && c + STEP <= hi && factor != 0.f) add(std::true_type());
+            else add(std::false_type());
+          }
           __syncwarp();
           if (lane == 0) mbar_arrive(bar_qfree(qs));
         }
