@@ -640,6 +640,7 @@ __global__ void __launch_bounds__(32 * kWarps, ctas_by_registers(NT)) cache_attn
   for (int r = r0; r < r1; ++r) s_starts[r] += run;
   if (tid == 32 * kWarps - 1) s_starts[a.requests] = run + mine;
   __syncthreads();
+  if constexpr (MODE == kWeights) blank(a.weights, a.lengths, a.requests, a.cache.heads, a.width * a.cache.page, R::kUnitTokens, blockIdx.x, gridDim.x);
   const int segs = a.cache.heads * (MODE == kOneQuery ? a.chunks : 1);   // of a request (some rows: key heads, of which each has the request's chunks)
   const int total = s_starts[a.requests] * segs, warps = gridDim.x * kWarps, part = max(1, total / warps + (total % warps != 0));
   if (MODE != kWeights && blockIdx.x == 0) {

@@ -826,9 +826,11 @@ ChunkShape chunk_shape(const hyperattn_chunk_params& p) {
   s.bytes = s.part_o + (size_t)s.parts * 2 * kBlockRows * p.cache.d * 4;
   return s;
 }
-// few rows: the warp-level kernels
+// Few rows on average: the warp-level kernels.  us there / here: 32 rows over 4000 tokens, 8 heads of 128, 8 requests 65 / 88, 64 rows 111 / 88; 2 x 30000 tokens, 32 heads of 64, 32 rows
+// 288 / 371, 64 rows 423 / 312; tables of no more than 1024 tokens (here the first and the last launch take as long as the work): 64 rows 19 / 39.
 bool few_rows(const hyperattn_chunk_params& p, size_t* bytes) {
-  return (long long)p.rows * (p.q_heads / p.cache.kv_heads) <= 16ll * p.requests && few_rows_attention(p, bytes);
+  const long long most = (long long)p.table_width * p.cache.page_tokens <= 1024 ? 64 : 32;
+  return (long long)p.rows * (p.q_heads / p.cache.kv_heads) <= most * p.requests && few_rows_attention(p, bytes);
 }
 
 int check(const hyperattn_chunk_params* p) {

@@ -14,8 +14,10 @@ template <int D, Mode MODE>
 RowsShape rows_shape(int requests, int rows, int group, int kv_heads, long long tokens) {
   RowsShape s;
   const long long all = (long long)rows * group;
-  // as many rows in a tile as requests have on average: four (and what the rounding of their weights loses beside them), eight, or two tiles of eight
-  s.tiles = MODE == kSomeRows && all <= 4ll * requests ? 0 : all <= 8ll * requests ? 1 : 2;
+  // Rows in a tile: attention four (and what the rounding of their weights loses beside them) where requests have that many on average, two tiles of eight where they have more than eight
+  // and d = 64, else eight.  us for four / eight / sixteen: 16 rows over 4000 tokens, 8 heads of 128, 8 requests 51 / 43 / 47, 32 rows 91 / 65 / 72; 2 x 30000 tokens, 32 heads of 64,
+  // 16 rows 309 / 190 / 184, 32 rows 556 / 316 / 288; weights of 16 rows over 300 tokens - / 10.8 / 9.4.
+  s.tiles = MODE == kSomeRows && all <= 4ll * requests ? 0 : all <= 8ll * requests || (MODE == kSomeRows && D == 128) ? 1 : 2;
   s.per_chunk = s.tiles == 0 ? 4 : 8 * s.tiles;
   s.slots = chunk_slots(rows, requests, group, s.per_chunk) + 1;
   constexpr int unit = Ring<D, MODE>::kUnitTokens;
@@ -112,7 +114,5 @@ int launch_few_rows_weights(const hyperattn_weights_params& p, int* status) {
     return s.tiles == 1 ? of_type(std::integral_constant<int, 1>{}) : of_type(std::integral_constant<int, 2>{});
   });
 }
-
-int few_rows_unit(int d) { return d == 64 ? Ring<64, kWeights>::kUnitTokens : Ring<128, kWeights>::kUnitTokens; }
 
 }  // namespace hyperattn

@@ -46,10 +46,14 @@ constexpr int kSpread = 12;              // octaves that a row may be smaller th
 __host__ __device__ __forceinline__ long long image_slots(long long rows_before, int requests_before, int group, int nr) { return rows_before * group / nr + requests_before; }
 
 template <int D, int NR, class T>
-__global__ void __launch_bounds__(128) image_kernel(const __grid_constant__ ChunkArgs a, const float* lse) {
+__global__ void __launch_bounds__(128) image_kernel(const __grid_constant__ ChunkArgs a, const float* lse, int images, float* out, int unit) {
   constexpr int LANES = D / 8, AT_ONCE = 128 / LANES, G = D / kGroup;
   using I = Image<D, NR>;
   wait_for_stream();
+  if ((int)blockIdx.x >= images) {                     // the others: zeros beyond the requests' tokens
+    blank(out, a.lengths, a.requests, a.cache.heads, a.width * a.cache.page, unit, blockIdx.x - images, gridDim.x - images);
+    return;
+  }
   const int kv = blockIdx.x % a.cache.heads, group = a.q_heads / a.cache.heads;
   const long long slot = blockIdx.x / a.cache.heads;
   int lo = 0, hi = a.requests;                         // the last request whose images start there or before

@@ -387,17 +387,6 @@ __global__ void __launch_bounds__(kWThreads, 1) weights_kernel(const __grid_cons
   }
 }
 
-// zeros beyond the requests' tokens (and beyond those that the kernels take with them, `unit` at a time)
-__global__ void __launch_bounds__(256) blank_kernel(const __grid_constant__ WeightArgs p, int unit) {
-  wait_for_stream();
-  const ChunkArgs& a = p.c;
-  const int cap = a.width * a.cache.page, r = blockIdx.x / a.cache.heads;
-  const Span s = span_of(a, r);
-  const int from = (int)min(((long long)s.len + unit - 1) / unit * unit, (long long)cap);
-  float4* to = reinterpret_cast<float4*>(p.out + (size_t)blockIdx.x * cap);                // (a page is a multiple of 16 tokens)
-  for (int i = from / 4 + blockIdx.y * 256 + threadIdx.x; i < cap / 4; i += 256 * gridDim.y) to[i] = make_float4(0.f, 0.f, 0.f, 0.f);
-}
-
 // rows of an image: a product of 64 rows takes 48 clocks, of 128 rows 64; beside two tiles' keys of d = 128 TMEM has room for the scores of two images of 96
 template <int D> constexpr int kImageRows = D == 64 ? 128 : 96;
 long long slots_of(const hyperattn_weights_params& p) {
@@ -414,7 +403,7 @@ extern "C" int hyperattn_cache_weights_workspace_bytes(const hyperattn_weights_p
   if (int rc = check_chunk(p)) return rc;
   *bytes = 0;
   if (p->requests == 0 || few_rows_weights(*p)) return HYPERATTN_OK;
-  if (slots_of(*p) * p->cache.kv_heads > 0x7fffffffLL) return HYPERATTN_UNSUPPORTED_SHAPE;
+  if (slots_of(*p) * p->cache.kv_heads > 0x7fffffffLL - 2 * kSms) return HYPERATTN_UNSUPPORTED_SHAPE;
   *bytes = (size_t)(slots_of(*p) * p->cache.kv_heads) * (p->cache.d == 64 ? Image<64, kImageRows<64>>::kBytes : Image<128, kImageRows<128>>::kBytes);
   return HYPERATTN_OK;
 }
@@ -438,19 +427,16 @@ extern "C" int hyperattn_cache_weights(const hyperattn_weights_params* p) {
   if (int rc = device_status_word(st, &status)) return rc;
   int sms = 0;
   cudaError_t e = sm_count(&sms);
-  const int heads = p->requests * p->cache.kv_heads, cap = p->table_width * p->cache.page_tokens;
-  int y = (4 * kSms + heads - 1) / heads;
-  if (y > (cap + 4095) / 4096) y = (cap + 4095) / 4096;
-  if (e == cudaSuccess) e = launch(blank_kernel, dim3((unsigned)heads, (unsigned)y), dim3(256), 0, st, w, few ? few_rows_unit(d) : kTileTokens);
   if (e != cudaSuccess) return status_of(e, "cache weights");
   if (few) return launch_few_rows_weights(*p, status);
   auto go = [&](auto dim) {
     constexpr int D = decltype(dim)::value, NR = kImageRows<D>;
     using C = WCfg<D, NR>;
     cudaError_t e = allow_smem<weights_kernel<D, NR>>(C::kSmem);
-    const dim3 slots((unsigned)(slots_of(*p) * p->cache.kv_heads));
-    if (e == cudaSuccess) e = p->dtype == HYPERATTN_BF16 ? launch(image_kernel<D, NR, __nv_bfloat16>, slots, dim3(128), 0, st, w.c, p->lse) : launch(image_kernel<D, NR, __half>, slots, dim3(128), 0, st, w.c, p->lse);
-    const long long tiles = (long long)heads * ((cap + kTileTokens - 1) / kTileTokens);
+    const int images = (int)(slots_of(*p) * p->cache.kv_heads);
+    auto make = [&](auto kernel) { return launch(kernel, dim3((unsigned)images + 2 * kSms), dim3(128), 0, st, w.c, p->lse, images, p->weights_out, kTileTokens); };
+    if (e == cudaSuccess) e = p->dtype == HYPERATTN_BF16 ? make(image_kernel<D, NR, __nv_bfloat16>) : make(image_kernel<D, NR, __half>);
+    const long long tiles = (long long)p->requests * p->cache.kv_heads * (((long long)p->table_width * p->cache.page_tokens + kTileTokens - 1) / kTileTokens);
     if (e == cudaSuccess) e = launch(weights_kernel<D, NR>, dim3((unsigned)(tiles < sms ? tiles : sms)), dim3(kWThreads), C::kSmem, st, w, maps, status);
     return status_of(e, "cache weights");
   };

@@ -89,6 +89,21 @@ __device__ __forceinline__ void sums_before(int (&x)[N], int (*s_warp)[kPlanWarp
     for (int w = 0; w < warp; ++w) x[q] = plus(x[q], s_warp[q][w]);
 }
 
+// Zeros in [requests, heads, cap] (fp32, cap a multiple of 4) beyond the requests' tokens, and beyond those that others write with them, `unit` at a time.  Pieces of the array over
+// `ctas` CTAs, of which this is number `cta`; all threads.
+__device__ __forceinline__ void blank(float* out, const int32_t* lengths, int requests, int heads, int cap, int unit, int cta, int ctas) {
+  constexpr int kPiece = 4096;
+  const int pieces = cap / kPiece + (cap % kPiece != 0);
+  const long long total = (long long)requests * heads * pieces;
+  for (long long p = cta; p < total; p += ctas) {
+    const long long row = p / pieces;
+    const int begin = (int)(p - row * pieces) * kPiece, len = min(max(lengths[row / heads], 0), cap);
+    const int from = max(begin, (int)min(((long long)len + unit - 1) / unit * unit, (long long)cap)), end = cap - begin < kPiece ? cap : begin + kPiece;
+    float4* to = reinterpret_cast<float4*>(out + row * cap);
+    for (int i = from / 4 + threadIdx.x; i < end / 4; i += blockDim.x) to[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+  }
+}
+
 inline CacheView view_of(const hyperattn_cache& c) { return {reinterpret_cast<uint8_t*>(c.pages), c.num_pages, c.page_tokens, c.kv_heads}; }
 inline int status_of(cudaError_t e, const char* what) {
   if (e == cudaSuccess) return HYPERATTN_OK;
