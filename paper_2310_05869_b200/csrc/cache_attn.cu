@@ -58,7 +58,7 @@ extern "C" int hyperattn_cache_attention(const hyperattn_cache_attention_params*
   if (misaligned(p->q) || misaligned(p->out) || misaligned(p->workspace)) return HYPERATTN_MISALIGNED;
   const Shape s = shape_of(*p);
   if (p->workspace_bytes < s.bytes) return HYPERATTN_WORKSPACE_TOO_SMALL;
-  CacheAttnArgs a = {};
+  KernelArgs<kOneQuery> a = {};
   a.cache = {reinterpret_cast<uint8_t*>(p->cache.pages), p->cache.num_pages, p->cache.page_tokens, p->cache.kv_heads};
   a.q = p->q; a.q_row = p->q_row_stride; a.q_head = p->q_head_stride;
   a.out = p->out; a.lse = p->lse; a.table = p->table; a.lengths = p->lengths;

@@ -53,8 +53,19 @@ struct CacheAttnArgs {
   float decay;
 };
 
+// K's codes, scales and minima of `run` blocks that follow each other, as boxes of the cache
+struct alignas(64) KeyMaps {
+  CUtensorMap codes, scales;
+};
+
 // What a build is for: one query a request; some rows a request; the weight that tokens get from some rows
 enum Mode { kOneQuery, kSomeRows, kWeights };
+
+template <Mode MODE> struct KernelArgs : CacheAttnArgs {};
+template <> struct KernelArgs<kWeights> : CacheAttnArgs {
+  KeyMaps maps;
+  int run;                                     // blocks of a copy: the largest power of two, up to a unit, that divides a page's
+};
 
 // a request's tokens of queries (first row, how many)
 __device__ __forceinline__ int2 queries_of(const CacheAttnArgs& a, int r) {
@@ -116,6 +127,16 @@ template <int D, int NT, bool PAIR, class T, Mode MODE>
 __device__ __forceinline__ void load_heads(Heads<D, NT>& h, const CacheAttnArgs& a, int request, int first_head, int heads, int kv, int2 queries) {
   constexpr int G = Heads<D, NT>::kGroups;
   const int lane = threadIdx.x & 31, c = lane & 3;
+  float lse[NT][2];                                      // weights: of the rows of the lane's results (asked for beside the queries)
+  if constexpr (MODE == kWeights) {
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const int g = group_of(a), mine = 8 * t + 2 * c + i, row = first_head + mine, token = row / g;
+        lse[t][i] = mine < heads ? a.lse_in[(size_t)(queries.x + token) * a.q_heads + kv * g + row - token * g] : -INFINITY;
+      }
+  }
 #pragma unroll
   for (int t = 0; t < NT; ++t) {
     const int head = PAIR ? lane / 4 % 4 : lane / 4 + 8 * t;
@@ -175,10 +196,7 @@ __device__ __forceinline__ void load_heads(Heads<D, NT>& h, const CacheAttnArgs&
       if constexpr (MODE != kOneQuery) {
         const int g = group_of(a), mine = PAIR ? (2 * c + i) % 4 : 8 * t + 2 * c + i, row = first_head + mine, token = row / g;
         h.back[t][i] = mine >= heads ? kNeverSeen : a.causal ? queries.y - token : 1;
-        if constexpr (MODE == kWeights) {
-          const float l = mine < heads ? a.lse_in[(size_t)(queries.x + token) * a.q_heads + kv * g + row - token * g] : -INFINITY;
-          h.minus[t][i] = l == -INFINITY ? l : -l * 1.4426950408889634f;           // (a row that saw nothing gives nothing)
-        }
+        if constexpr (MODE == kWeights) h.minus[t][i] = lse[t][i] == -INFINITY ? -INFINITY : -lse[t][i] * 1.4426950408889634f;           // (a row that saw nothing gives nothing)
       }
     }
 #pragma unroll
@@ -189,9 +207,9 @@ __device__ __forceinline__ void load_heads(Heads<D, NT>& h, const CacheAttnArgs&
   if constexpr (MODE != kOneQuery) h.most_back = a.causal ? queries.y - first_head / group_of(a) : 1;
 }
 
-// Scores of one block of 16 tokens at `block`, the first `valid` of which exist: S^T of tokens lane / 4 (+ 8) and heads 2 c, 2 c + 1.  (Weights: K's scales follow its codes.)
+// Scores of one block of 16 tokens at `block`, the first `valid` of which exist: S^T of tokens lane / 4 (+ 8) and heads 2 c, 2 c + 1.  scales: K's.
 template <int D, int NT, Mode MODE>
-__device__ __forceinline__ void scores_of(const Heads<D, NT>& h, const uint8_t* block, int valid, float (&s)[NT][4]) {
+__device__ __forceinline__ void scores_of(const Heads<D, NT>& h, const uint8_t* block, const uint8_t* scales, int valid, float (&s)[NT][4]) {
   constexpr int G = D / kGroup;
   const int lane = threadIdx.x & 31, c = lane & 3;
   uint32_t kw[2][G], sc[2][G / 2], mn[2];                // codes, scales of group pairs, minima of the lane's pair (see load_heads)
@@ -208,7 +226,7 @@ __device__ __forceinline__ void scores_of(const Heads<D, NT>& h, const uint8_t* 
   const uint32_t pick = lane & 4 ? 0x7632u : 0x5410u;    // of two halves with tokens (2 i, 2 i + 1): the lane's token
 #pragma unroll
   for (int half = 0; half < 2; ++half) {
-    const uint8_t* at = block + (MODE == kWeights ? 8 * D : Block<D>::kScaleK) + (half * 4 + lane / 8) * G * 8;
+    const uint8_t* at = scales + (half * 4 + lane / 8) * G * 8;
     const uint4 v = *reinterpret_cast<const uint4*>(at);
     sc[half][0] = __byte_perm(v.x, v.z, pick);
     if constexpr (G == 2) mn[half] = __byte_perm(v.y, v.w, pick);
@@ -451,7 +469,7 @@ template <int D, int NT, bool PAIR, int NB, bool FINE, Mode MODE>
 __device__ __forceinline__ void attend_blocks(Heads<D, NT>& h, const uint8_t* block, const int (&valid)[NB]) {
   float s[NB][NT][4], y[NB][NT][4], most = -INFINITY;
 #pragma unroll
-  for (int b = 0; b < NB; ++b) scores_of<D, NT, MODE>(h, block + b * Block<D>::kBytes, valid[b], s[b]);
+  for (int b = 0; b < NB; ++b) scores_of<D, NT, MODE>(h, block + b * Block<D>::kBytes, block + b * Block<D>::kBytes + Block<D>::kScaleK, valid[b], s[b]);
 #pragma unroll
   for (int b = 0; b < NB; ++b)
 #pragma unroll
@@ -536,25 +554,28 @@ struct Ring {
   static constexpr int kStages = 2;                                      // units on their way, a warp
   static constexpr int kWarpBytes = kStages * kUnitBytes;                // (>= 16 x D floats: a warp's outputs, when the parts are put together)
   static constexpr int kKnown = MODE == kOneQuery ? 1280 : 1536;         // what a warp knows of its next units
-  static constexpr int bytes(int requests) { return kWarps * (kWarpBytes + kKnown + kStages * 8 + 4 + 16 * 12) + 16 + (requests + 1) * 4 + (MODE == kOneQuery ? 0 : requests * 4); }
+  static constexpr int bytes(int requests) { return kWarps * (kWarpBytes + kKnown + kStages * 8 + 4 + 16 * 12) + 16 + (requests + 1) * 4 + (MODE == kOneQuery ? 0 : (requests + 1) * 8); }
 };
 template <int D, Mode MODE> int ctas_by_memory(int requests) { return 227 * 1024 / (Ring<D, MODE>::bytes(requests) + 1024); }
 
 __device__ __forceinline__ void bulk_copy(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
   asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
 }
+// Weights: empty units at a segment's end, for what its beginning costs (queries and log-sum-exps, 2.5 to 4 us beside 1 us a unit; without them a warp that had
+// requests of a token each was what 64 requests waited for: 64 us).
+constexpr int kBegin = 2;
 template <int D, Mode MODE> __device__ __forceinline__ int units_of(const CacheAttnArgs& a, int r) {
   const int tokens = min(max(a.lengths[r], 0), a.width * a.cache.page);        // (up to 2^31 - 1)
-  return tokens / Ring<D, MODE>::kUnitTokens + (tokens % Ring<D, MODE>::kUnitTokens != 0);
+  const int units = tokens / Ring<D, MODE>::kUnitTokens + (tokens % Ring<D, MODE>::kUnitTokens != 0);
+  return MODE == kWeights && units ? units + kBegin : units;
 }
 // A unit's tokens: what they had, times the decay, and what the request's rows of key head kv give them (in chunks; nearly always one).  A lane ends up with the two tokens
 // lane / 4 (+ 8) of blocks c, c + 4, ...; wait(): until the unit's keys are there.
 template <int D, int NT, class T, class W>
-__device__ __forceinline__ void weigh_unit(Heads<D, NT>& h, const CacheAttnArgs& a, const uint8_t* unit, int request, int kv, int chunks, int left, int there, int2 queries, W wait) {
-  using R = Ring<D, kWeights>;
-  constexpr int U = R::kUnit, MINE = U / 4;
+__device__ __forceinline__ void weigh_unit(Heads<D, NT>& h, const CacheAttnArgs& a, const uint8_t* unit, int request, int kv, int chunks, int first, int left, int there, int2 queries, bool fresh, W wait) {
+  constexpr int U = Ring<D, kWeights>::kUnit, MINE = U / 4;
   const int lane = threadIdx.x & 31, c = lane & 3, cap = a.width * a.cache.page;
-  const int len = min(max(a.lengths[request], 0), cap), first = len - left, old = len - queries.y;       // tokens from `old` on are the rows' own
+  const int len = first + left, old = len - queries.y;                   // tokens from `old` on are the rows' own
   const size_t at = ((size_t)request * a.cache.heads + kv) * cap;
   float had[MINE][2], got[MINE][2];
 #pragma unroll
@@ -565,23 +586,43 @@ __device__ __forceinline__ void weigh_unit(Heads<D, NT>& h, const CacheAttnArgs&
       had[k][e] = a.before && token < old ? a.before[at + token] : 0.f;
       got[k][e] = 0.f;
     }
+  // (a segment's first unit: its queries, beside what the tokens had)
+  if (fresh) load_heads<D, NT, false, T, kWeights>(h, a, request, 0, min(queries.y * group_of(a), 8 * NT), kv, queries);
   if (!wait()) return;
   for (int chunk = 0; chunk < chunks; ++chunk) {
-    if (chunks > 1) load_heads<D, NT, false, T, kWeights>(h, a, request, chunk * 8 * NT, min(queries.y * group_of(a) - chunk * 8 * NT, 8 * NT), kv, queries);
+    if (chunks > 1 && !(chunk == 0 && fresh)) load_heads<D, NT, false, T, kWeights>(h, a, request, chunk * 8 * NT, min(queries.y * group_of(a) - chunk * 8 * NT, 8 * NT), kv, queries);
 #pragma unroll
-    for (int b = 0; b < U; ++b) {
-      if (!(there >> b & 1)) continue;
-      float s[NT][4], sum[2] = {0.f, 0.f};
-      scores_of<D, NT, kWeights>(h, unit + b * R::kBlockBytes, left - b * kBlockTokens, s);
+    for (int b4 = 0; b4 < U; b4 += 4) {
+      // four blocks; two at a time where they are there, so that one's products cover the other's latencies
+      float sum[4][2];
+      auto block = [&](int i) {
+        float s[NT][4];
+        scores_of<D, NT, kWeights>(h, unit + (b4 + i) * 8 * D, unit + U * 8 * D + (b4 + i) * 2 * D, left - (b4 + i) * kBlockTokens, s);
+        sum[i][0] = sum[i][1] = 0.f;
 #pragma unroll
-      for (int t = 0; t < NT; ++t)
+        for (int t = 0; t < NT; ++t)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) sum[i >> 1] += ex2(fmaf(s[t][i], h.scale[t][i & 1], h.minus[t][i & 1]));
+          for (int k = 0; k < 4; ++k) sum[i][k >> 1] += ex2(fmaf(s[t][k], h.scale[t][k & 1], h.minus[t][k & 1]));
+      };
+#pragma unroll
+      for (int i = 0; i < 4; i += 2) {
+        const int two = there >> (b4 + i) & 3;
+        if (two == 3) { block(i); block(i + 1); }
+        else {
+#pragma unroll
+          for (int k = i; k < i + 2; ++k) {
+            if (there >> (b4 + k) & 1) block(k);
+            else sum[k][0] = sum[k][1] = 0.f;
+          }
+        }
+      }
+      // over the four lanes of a token: each ends up with one block's
+      const bool b0 = c & 1, b1 = c & 2;
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
-        sum[e] += __shfl_xor_sync(0xffffffffu, sum[e], 1);
-        sum[e] += __shfl_xor_sync(0xffffffffu, sum[e], 2);
-        if (c == b % 4) got[b / 4][e] += sum[e];
+        const float x = (b0 ? sum[1][e] : sum[0][e]) + __shfl_xor_sync(0xffffffffu, b0 ? sum[0][e] : sum[1][e], 1);
+        const float y = (b0 ? sum[3][e] : sum[2][e]) + __shfl_xor_sync(0xffffffffu, b0 ? sum[2][e] : sum[3][e], 1);
+        got[b4 / 4][e] += (b1 ? y : x) + __shfl_xor_sync(0xffffffffu, b1 ? x : y, 2);
       }
     }
   }
@@ -597,7 +638,7 @@ __device__ __forceinline__ void weigh_unit(Heads<D, NT>& h, const CacheAttnArgs&
 __device__ __forceinline__ float* piece_at(const CacheAttnArgs& a, long long slot, int head, int d) { return a.part + (slot * a.part_heads + head) * (d + 2); }
 
 template <int D, int NT, bool PAIR, class T, Mode MODE>
-__global__ void __launch_bounds__(32 * kWarps, ctas_by_registers(NT)) cache_attn_kernel(const __grid_constant__ CacheAttnArgs a, int* status) {
+__global__ void __launch_bounds__(32 * kWarps, ctas_by_registers(NT)) cache_attn_kernel(const __grid_constant__ KernelArgs<MODE> a, int* status) {
   using R = Ring<D, MODE>;
   constexpr int kPerChunk = PAIR ? 4 : 8 * NT;                           // rows (heads) of a chunk
   constexpr bool FINE = std::is_same<T, __half>::value;
@@ -608,7 +649,8 @@ __global__ void __launch_bounds__(32 * kWarps, ctas_by_registers(NT)) cache_attn
   float* s_stat = reinterpret_cast<float*>(s_sums + kWarps);             // [kWarps][16][2] references, sums
   float* s_factor = s_stat + kWarps * 32;                                // [kWarps][16]
   int* s_starts = reinterpret_cast<int*>(s_factor + kWarps * 16);        // [requests + 1] units (of one segment each; some rows: of one key head) before a request
-  int* s_chunks = s_starts + a.requests + 1;                             // some rows, weights: [requests] chunks of a request's rows
+  int2* s_queries = reinterpret_cast<int2*>(s_starts + (a.requests + 2) / 2 * 2);               // some rows, weights: [requests] a request's queries: first row, how many
+  auto chunks_of = [&](int r) { return (s_queries[r].y * group_of(a) + kPerChunk - 1) / kPerChunk; };
   const int tid = threadIdx.x, lane = tid & 31, c = lane & 3;
   const int warp = __shfl_sync(0xffffffffu, tid >> 5, 0);
   const uint32_t ring = smem_u32(smem) + warp * R::kWarpBytes, bars = smem_u32(smem) + kWarps * (R::kWarpBytes + R::kKnown) + warp * R::kStages * 8;
@@ -625,8 +667,8 @@ __global__ void __launch_bounds__(32 * kWarps, ctas_by_registers(NT)) cache_attn
     s_starts[r] = mine;
     int units = units_of<D, MODE>(a, r);
     if constexpr (MODE != kOneQuery) {
-      s_chunks[r] = (queries_of(a, r).y * group_of(a) + kPerChunk - 1) / kPerChunk;
-      if (MODE == kSomeRows) units *= s_chunks[r];
+      s_queries[r] = queries_of(a, r);
+      if (MODE == kSomeRows) units *= chunks_of(r);
     }
     mine += units;
   }
@@ -672,12 +714,12 @@ __global__ void __launch_bounds__(32 * kWarps, ctas_by_registers(NT)) cache_attn
     const int t = n / segs;
     while (hi - lo > 1) { const int mid = (lo + hi) >> 1; if (s_starts[mid] <= t) lo = mid; else hi = mid; }
     int units = s_starts[lo + 1] - s_starts[lo];
-    if constexpr (MODE == kSomeRows) units /= s_chunks[lo];
+    const int chunks = MODE == kOneQuery ? a.chunks : MODE == kSomeRows ? chunks_of(lo) : 1;
+    if constexpr (MODE == kSomeRows) units /= chunks;
     const int rest = n - s_starts[lo] * segs, seg = rest / units, b = (rest - seg * units) * U + lane % U;
     const int column = shift >= 0 ? b >> shift : b / subs;
     *reinterpret_cast<int2*>(&s_known[slot]) = make_int2(MODE == kOneQuery ? lo * segs + seg : seg, b);
     if constexpr (MODE != kOneQuery) s_request[slot] = lo;
-    const int chunks = MODE == kOneQuery ? a.chunks : MODE == kSomeRows ? s_chunks[lo] : 1;
     s_place[slot] = (chunks == 1 ? seg : seg / chunks) * subs + b - column * subs;
     const uint32_t to = smem_u32(&s_known[slot]);
     asm volatile("cp.async.ca.shared.global [%0], [%1], 4;\n\tcp.async.ca.shared.global [%2], [%3], 4;" ::"r"(to + 8), "l"(a.table + (size_t)lo * a.width + min(column, a.width - 1)), "r"(to + 12),
@@ -691,23 +733,24 @@ __global__ void __launch_bounds__(32 * kWarps, ctas_by_registers(NT)) cache_attn
     const int left = min(k.w, a.width * a.cache.page) - (k.y - in_unit) * kBlockTokens;
     const bool there = in_unit * kBlockTokens < left && k.z >= 0 && k.z < a.cache.num_pages;
     const unsigned all = __ballot_sync(0xffffffffu, there) >> (lane - in_unit) & ((1u << U) - 1);
-    const int bytes = MODE == kWeights ? there : whole ? (in_unit == 0 ? __popc(all) : 0) : there;
+    const int bytes = whole ? (in_unit == 0 ? __popc(all) : 0) : there;
     s_known[slot] = make_int4(k.x, left, k.z * a.cache.heads * subs + s_place[slot], bytes * Block<D>::kBytes | all << 16);
+    if constexpr (MODE == kWeights) s_place[slot] = k.y * kBlockTokens;   // (weights: from here on the block's first token)
     __syncwarp();
   };
   int asked = 0;                                                         // units whose copies have been asked for
   auto ask = [&] {
-    if constexpr (MODE == kWeights) {                                    // K's codes, and its scales
-      if (lane < 2 * U) {
+    if constexpr (MODE == kWeights) {                                    // the unit's codes, then its scales; a run of blocks is in one page and comes as a whole
+      if (lane < U) {
         const int st = asked % R::kStages;
         const uint32_t bar = bars + 8 * st;
-        const int4 k = s_known[asked % (2 * kBatch) * U + lane / 2];
-        if (lane == 0) asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(__popc(k.w >> 16) * R::kBlockBytes) : "memory");
-        const uint8_t* from = a.cache.pages + (size_t)k.z * Block<D>::kBytes;
-        const uint32_t to = ring + st * R::kUnitBytes + lane / 2 * R::kBlockBytes;
-        if (k.w & 0xffff) {
-          if (lane & 1) bulk_copy(to + 8 * D, from + Block<D>::kScaleK, 2 * D, bar);
-          else bulk_copy(to, from, 8 * D, bar);
+        const int4 k = s_known[asked % (2 * kBatch) * U + lane];
+        const uint32_t leaders = a.run == 1 ? 0xffu : a.run == 2 ? 0x55u : a.run == 4 ? 0x11u : 0x01u;
+        if (lane == 0) asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(__popc(k.w >> 16 & leaders) * a.run * R::kBlockBytes) : "memory");
+        if ((leaders >> lane & 1) && (k.w >> 16 >> lane & 1)) {
+          const uint32_t to = ring + st * R::kUnitBytes;
+          tma_tile(to + lane * 8 * D, &a.maps.codes, 0, k.z, bar);
+          tma_tile(to + U * 8 * D + lane * 2 * D, &a.maps.scales, 4 * D, k.z, bar);
         }
       }
     } else if (lane < U) {
@@ -731,8 +774,8 @@ __global__ void __launch_bounds__(32 * kWarps, ctas_by_registers(NT)) cache_attn
       load_heads<D, NT, PAIR, T, MODE>(h, a, request, kv * per_kv + chunk * 8 * NT, min(per_kv - chunk * 8 * NT, 8 * NT), kv, queries);
     } else {
       request = rq; seg = sg;
-      queries = queries_of(a, request);
-      chunks = MODE == kSomeRows ? s_chunks[request] : 1;
+      queries = s_queries[request];
+      chunks = MODE == kSomeRows ? chunks_of(request) : 1;
       const int kv = seg / chunks, chunk = seg - kv * chunks;
       load_heads<D, NT, PAIR, T, MODE>(h, a, request, chunk * kPerChunk, min(queries.y * per_kv - chunk * kPerChunk, kPerChunk), kv, queries);
     }
@@ -790,10 +833,18 @@ __global__ void __launch_bounds__(32 * kWarps, ctas_by_registers(NT)) cache_attn
     const int4 unit = s_known[n % (2 * kBatch) * U];
     const int sg = unit.x, left = unit.y, there = unit.w >> 16;
     const int rq = MODE == kOneQuery ? 0 : s_request[n % (2 * kBatch) * U];
-    if (sg != segment || (MODE != kOneQuery && rq != request)) take_segment(sg, rq);
+    if (MODE == kWeights && left <= 0) {                                  // (an empty unit: no copy was asked for)
+      if (asked < count) ask();
+      continue;
+    }
+    const bool fresh = sg != segment || (MODE != kOneQuery && rq != request);
+    if (MODE != kWeights && fresh) take_segment(sg, rq);
     const int st = n % R::kStages;
     if constexpr (MODE == kWeights) {
-      weigh_unit<D, NT, T>(h, a, smem + warp * R::kWarpBytes + st * R::kUnitBytes, request, seg, s_chunks[request], left, there, queries, [&] {
+      segment = seg = sg;
+      request = rq;
+      queries = s_queries[rq];
+      weigh_unit<D, NT, T>(h, a, smem + warp * R::kWarpBytes + st * R::kUnitBytes, request, seg, chunks_of(request), s_place[n % (2 * kBatch) * U], left, there, queries, fresh, [&] {
         ok = warp_wait<12>(bars + 8 * st, (uint32_t)(n / R::kStages) & 1, s_abort, status);
         return ok;
       });

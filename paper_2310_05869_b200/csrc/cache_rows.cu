@@ -32,10 +32,11 @@ RowsShape rows_shape(int requests, int rows, int group, int kv_heads, long long 
 // units are counted in ints
 template <int D, Mode MODE>
 bool countable(const RowsShape& s, int requests, int kv_heads, long long tokens) {
-  return (MODE == kWeights ? (long long)requests : s.slots) * kv_heads <= 0x7fffffffLL / (tokens / Ring<D, MODE>::kUnitTokens + 2) && s.slots * kv_heads <= 0x7fffffffLL;
+  return (MODE == kWeights ? (long long)requests : s.slots) * kv_heads <= 0x7fffffffLL / (tokens / Ring<D, MODE>::kUnitTokens + 2 + kBegin) && s.slots * kv_heads <= 0x7fffffffLL;
 }
-CacheAttnArgs rows_args(const ChunkArgs& c) {
-  CacheAttnArgs a = {};
+template <Mode MODE>
+KernelArgs<MODE> rows_args(const ChunkArgs& c) {
+  KernelArgs<MODE> a = {};
   a.cache = c.cache; a.q = c.q; a.q_row = c.q_row; a.q_head = c.q_head; a.table = c.table; a.lengths = c.lengths; a.cu_q = c.cu_q;
   a.requests = c.requests; a.width = c.width; a.q_heads = c.q_heads; a.rows = c.rows; a.causal = c.causal; a.scale_log2 = c.scale_log2; a.chunks = 1;
   return a;
@@ -59,7 +60,7 @@ bool few_rows_attention(const hyperattn_chunk_params& p, size_t* bytes) {
 int launch_few_rows_attention(const hyperattn_chunk_params& p, int* status) {
   const int group = p.q_heads / p.cache.kv_heads;
   const cudaStream_t st = reinterpret_cast<cudaStream_t>(p.stream);
-  CacheAttnArgs a = rows_args(chunk_args(p));
+  KernelArgs<kSomeRows> a = rows_args<kSomeRows>(chunk_args(p));
   a.out = p.out; a.lse = p.lse; a.out_kind = p.out_dtype;
   return of_dim(p.cache.d, [&](auto dim) {
     constexpr int D = decltype(dim)::value;
@@ -75,7 +76,8 @@ int launch_few_rows_attention(const hyperattn_chunk_params& p, int* status) {
       cudaError_t e = allow_smem<kernel>(R::bytes(kMaxRequests));
       if (e == cudaSuccess) e = launch(kernel, dim3((unsigned)s.ctas), dim3(32 * kWarps), R::bytes(p.requests), st, a, status);
       const long long segments = s.slots * p.cache.kv_heads;
-      int split = (int)((4 * kSms + segments - 1) / segments);
+      // few segments: a CTA for a row or some (8 requests of 16 rows, 8 heads: 13 us with two, of 25 in all)
+      int split = (int)((16 * kSms + segments - 1) / segments);
       if (split > s.per_chunk) split = s.per_chunk;
       const int heads = (s.per_chunk + split - 1) / split;
       if (e == cudaSuccess) e = launch(join_kernel<D, kSomeRows>, dim3((unsigned)segments, (unsigned)((s.per_chunk + heads - 1) / heads)), dim3(kJoinThreads), 0, st, a, heads);
@@ -98,11 +100,15 @@ bool few_rows_weights(const hyperattn_weights_params& p) {
 
 int launch_few_rows_weights(const hyperattn_weights_params& p, int* status) {
   const cudaStream_t st = reinterpret_cast<cudaStream_t>(p.stream);
-  CacheAttnArgs a = rows_args(chunk_args(p));
+  KernelArgs<kWeights> a = rows_args<kWeights>(chunk_args(p));
   a.lse_in = p.lse; a.before = p.weights; a.weights = p.weights_out; a.decay = p.decay;
   return of_dim(p.cache.d, [&](auto dim) {
     constexpr int D = decltype(dim)::value;
     using R = Ring<D, kWeights>;
+    const int subs = p.cache.page_tokens / kBlockTokens;
+    a.run = subs % R::kUnit == 0 ? R::kUnit : subs & -subs;
+    const long long blocks = (long long)p.cache.num_pages * p.cache.kv_heads * subs;
+    if (!encode_words_map(&a.maps.codes, p.cache.pages, blocks, 5 * D, 2 * D, a.run) || !encode_words_map(&a.maps.scales, p.cache.pages, blocks, 5 * D, D / 2, a.run)) return (int)HYPERATTN_UNSUPPORTED_SHAPE;
     const RowsShape s = rows_shape<D, kWeights>(p.requests, p.rows, p.q_heads / p.cache.kv_heads, p.cache.kv_heads, (long long)p.table_width * p.cache.page_tokens);
     auto go = [&](auto tiles, auto type) {
       constexpr auto kernel = cache_attn_kernel<D, decltype(tiles)::value, false, decltype(type), kWeights>;
