@@ -1,12 +1,18 @@
 """A small server of a decoder: prompts of different lengths come and go, their keys and values are kept in a paged 4-bit cache.
 
     python examples/serve.py                 # random weights; prints what it generated and how long a step took
+    python examples/serve.py --keep 512      # the same with contexts that are cut to 512 tokens
 
 Every step schedules the cache's pages (cache_plan), runs the new tokens of all requests as one packed batch - whole prompts for
 requests that have just come, one token for the others - and, layer by layer, stores their keys and values (cache_store) and attends:
 prompts to themselves (prompt_attention), or, from `long_prompt` tokens on, with HyperAttention in the layers that are to be
 approximated; single tokens to everything that is cached of their request (cache_attention).  A prompt that comes in parts attends
-to its cached part, read back (cache_read), and to itself.  This is a loop to read, not a server: everything outside the library's
+to its cached part, read back (cache_read), and to itself.
+
+With `keep`, no request has more than that many tokens for long: all rows of a step attend to what is cached of their requests, their
+own tokens included (cache_chunk_attention), the weight that every cached token gets is added up (cache_weights), and requests that
+have grown too long are cut to the first and the last tokens and those of most weight (cache_evict_plan, and cache_evict for every
+layer).  This is a loop to read, not a server: everything outside the library's
 calls is plain torch."""
 from __future__ import annotations
 
@@ -60,8 +66,8 @@ class Decoder:
 
 
 class Server:
-    def __init__(self, model, requests=8, pages=64, page_tokens=64, longest=2048, long_prompt=1 << 30):
-        self.model, self.page, self.long_prompt = model, page_tokens, long_prompt
+    def __init__(self, model, requests=8, pages=64, page_tokens=64, longest=2048, long_prompt=1 << 30, keep=0, recent=32, first=4):
+        self.model, self.page, self.long_prompt, self.keep, self.recent, self.first = model, page_tokens, long_prompt, keep, recent, first
         self.caches = [ha.cache_pages(pages, model.kv_heads, model.d, page_tokens) for _ in model.layers]
 
         def ints(*shape, fill=0):
@@ -69,6 +75,9 @@ class Server:
 
         self.lengths, self.table = ints(requests), ints(requests, -(-longest // page_tokens), fill=-1)
         self.free, self.n_free = torch.arange(pages, dtype=torch.int32, device="cuda"), ints(1, fill=pages)
+        if keep:                                                   # what every cached token has got, and how many tokens of a request are gone
+            self.weights = [torch.zeros(requests, model.kv_heads, self.table.shape[1] * page_tokens, device="cuda") for _ in model.layers]
+            self.gone, self.most = ints(requests), ints(requests, fill=keep)
 
     def step(self, new):
         """new: for every request None (nothing), False (it has ended) or its new tokens (a list); returns the logits of every request's last
@@ -79,6 +88,8 @@ class Server:
         before = self.lengths
         plan = ha.cache_plan(before, torch.tensor(count, dtype=torch.int32, device="cuda"), self.table, self.free, self.n_free, self.page, rows)
         self.lengths, self.table, self.free, self.n_free = plan.lengths, plan.table, plan.free, plan.n_free
+        if self.keep:
+            self.gone.masked_fill_(plan.lengths == 0, 0)
         if rows == 0:
             return {}
         tokens = torch.tensor([t for request in new if request for t in request], device="cuda")
@@ -90,6 +101,26 @@ class Server:
         rows_of_single = torch.tensor([first[r] for r in single], device="cuda", dtype=torch.long)
         at = torch.tensor(single, device="cuda", dtype=torch.long)
         table1, lengths1 = plan.table[at].contiguous(), plan.lengths[at].contiguous()
+
+        if self.keep:
+            # rows of the requests that were admitted, one after the other (all of them, nearly always)
+            mine = sorted(admitted)
+            if not mine:
+                return {}
+            pick = torch.cat([torch.arange(first[r], first[r + 1]) for r in mine]).cuda()
+            cu = torch.tensor([0] + [count[r] if r in admitted else 0 for r in range(len(new))]).cumsum(0).int().cuda()
+            moved = torch.repeat_interleave(self.gone, plan.cu_new.diff(), output_size=rows)
+
+            def attend_cached(layer, q, k, v):
+                cache = self.caches[layer]
+                ha.cache_store(cache, k, v, plan.slots)
+                q1 = q if pick.shape[0] == rows else q[pick]
+                got, lse = ha.cache_chunk_attention(q1, cache, plan.table, plan.lengths, cu)
+                ha.cache_weights(q1, cache, plan.table, plan.lengths, lse, cu, weights=self.weights[layer], out=self.weights[layer])
+                return got if pick.shape[0] == rows else torch.zeros_like(q).index_copy_(0, pick, got)
+
+            logits = model.run(tokens, plan.positions.clamp(min=0) + moved, attend_cached)
+            return {r: logits[first[r + 1] - 1] for r in mine}
 
         def attend(layer, q, k, v):
             out = torch.zeros_like(q)
@@ -119,9 +150,20 @@ class Server:
         logits = model.run(tokens, plan.positions.clamp(min=0), attend)
         return {r: logits[first[r + 1] - 1] for r in single + prompts}
 
+    def cut(self):
+        """Requests of more than `keep` tokens are cut to that; returns the tokens (before) that stay, a tensor for every layer."""
+        plan = ha.cache_evict_plan(self.lengths, self.most, self.table, self.free, self.n_free, self.page)
+        kept = []
+        for layer, cache in enumerate(self.caches):
+            self.weights[layer], stay = ha.cache_evict(cache, self.weights[layer], self.table, self.lengths, plan.table, plan.lengths, recent=self.recent, first=self.first)
+            kept.append(stay)
+        self.gone += self.lengths - plan.lengths
+        self.lengths, self.table, self.free, self.n_free = plan
+        return kept
 
-def main():
-    server = Server(Decoder(layers=4, approximated={3}), requests=4, pages=200, longest=8192, long_prompt=4096)
+
+def main(keep=0):
+    server = Server(Decoder(layers=4, approximated={3}), requests=4, pages=200, longest=8192, long_prompt=4096, keep=keep)
     gen = torch.Generator().manual_seed(1)
     waiting = [torch.randint(0, 512, (n,), generator=gen).tolist() for n in (5, 700, 5000, 64, 1, 300)]
     said = {r: [] for r in range(len(waiting))}
@@ -132,6 +174,8 @@ def main():
             if running[s] is None and new[s] is None and todo:
                 running[s], new[s] = todo.pop(0)
         got = server.step(new)
+        if keep:
+            server.cut()
         new = [None] * 4
         for s, logits in got.items():
             said[running[s]].append(int(logits.argmax()))
@@ -147,4 +191,4 @@ def main():
 
 
 if __name__ == "__main__":
-    main()
+    main(int(sys.argv[sys.argv.index("--keep") + 1]) if "--keep" in sys.argv else 0)
