@@ -2,11 +2,12 @@
 //
 // A segment is a request, a key head and 256 of its rows (tokens times the query heads that read the key head), in two units of 128.  A CTA walks over tiles of 64
 // tokens, from the first one up:
-//     K = (scale * code, what its rounding has lost, minimum), V = minimum + scale * code      from the cache's bytes to shared memory, by four warps, for both units
+//     K = (scale * code, what its rounding has lost, minimum), V = minimum + scale * code      from the cache's bytes to shared memory, by four warps for every other tile
 //     S_i = Q_i K^T           tcgen05.mma, queries from TMEM; exact products (cache_tiles.cuh)
 //     P_i = exp2(c S_i - m)   four warps a unit, a thread a row; P_i in TMEM, fp16
 //     O_i += P_i V            tcgen05.mma
-// The tensor pipe works for one unit while the other one's weights are made.  References move as in the attention of prompts (softmax.cuh); weights' references are 2^7 below
+// The tensor pipe works for one unit while the other one's weights are made.  A segment of up to 128 rows has both units work for them, on every other tile each; unit 0's
+// warps put the two results together (a lane of TMEM is the same row in both).  References move as in the attention of prompts (softmax.cuh); weights' references are 2^7 below
 // the largest score.  K's scales and minima are multiplied by a power of two for their tile, V's by one that is a multiple of four octaves; a tile with larger values than O's has O multiplied, one with
 // smaller ones its weights, so values of any size are as exact as any others.
 //
@@ -18,7 +19,8 @@
 //
 // Roundings: weights and values enter the second product as fp16 (2^-11 of each), sums of weights before that; O is one chain of products over a part's tokens.
 //
-// Warp roles (480 threads): 0-3 and 4-7 softmax and results of unit 0 and 1, 8-11 keys and values, 12 products (and TMEM), 13 copies, 14 segments.
+// Warp roles (640 threads): 0-3 and 4-7 softmax and results of unit 0 and 1, 8-11 and 12-15 keys and values of even and odd tiles, 16 products (and TMEM), 17 copies, 18 segments, 19
+// nothing (four warps give registers up together).
 // Every wait is bounded: a CTA that gives up raises the device status word, drains its copies, frees its TMEM and returns.
 #include <climits>
 #include <type_traits>
@@ -29,7 +31,7 @@
 namespace hyperattn {
 namespace {
 
-constexpr int kUnitRows = 128, kBlockRows = 256, kKeys = 64, kCThreads = 480;
+constexpr int kUnitRows = 128, kBlockRows = 256, kKeys = 64, kCThreads = 640;
 
 struct ChunkOut {
   void* out;
@@ -111,10 +113,10 @@ template <int D>
 struct CCfg {
   static constexpr uint32_t kKeySlab = kKeys * 128, kP = (D / 64) * kKeySlab;                       // 64 columns of 64 tokens; scale * code of a tile
   static constexpr uint32_t kOffRest = kP, kOffV = 2 * kP, kOffMinima = kOffV + D * 128, kStage = kOffMinima + kKeys * 32;
-  static constexpr int kStages = D == 128 ? 3 : 5, kRawStages = D == 128 ? 5 : 8;
+  static constexpr int kStages = D == 128 ? 3 : 5, kRawStages = D == 128 ? 6 : 8;        // (even: a slot is the same group's every time)
   static constexpr uint32_t kRaw = 4 * Block<D>::kBytes, kSums = kUnitRows * 32;
   static constexpr uint32_t kOffRaw = kStages * kStage, kOffSums = kOffRaw + kRawStages * kRaw, kOffMisc = kOffSums + 2 * kSums;
-  static constexpr uint32_t kSmem = kOffMisc + 1024 + 1024;
+  static constexpr uint32_t kSmem = kOffMisc + 1024 + 2048 + 1024;
   // TMEM columns: O_0, O_1, Q_0, Q_1, S_0, S_1; at d = 64 P_i beside S_i, so that the next scores do not wait for this tile's weights
   static constexpr bool kOwnP = D == 64;
   static constexpr uint32_t kColQ = 2 * D, kColS = 3 * D;
@@ -126,6 +128,7 @@ struct Piece {                           // of a segment, in a CTA's part
   int request, kv, row0, units[2];       // rows of either unit
   Span s;
   int tile0, tile1;
+  int split;                             // both units have the same rows, and every other tile
   int place;                             // in the workspace; -1: the segment is finished here
   __device__ __forceinline__ int last_seen(const ChunkArgs& a, int row) const {       // last token that a row of the segment sees
     const int token = (row0 + row) / (a.q_heads / a.cache.heads);
@@ -144,12 +147,13 @@ __global__ void __launch_bounds__(kCThreads, 1) chunk_kernel(const __grid_consta
   uint8_t* misc = smem + C::kOffMisc;
   Piece* s_piece = reinterpret_cast<Piece*>(misc);                               // [2]
   int* s_nan = reinterpret_cast<int*>(misc + 192);                               // [2][4] first token with a NaN among the values of a group
-  int* s_exp = reinterpret_cast<int*>(misc + 224);                               // [2][4] the blocks' exponents
-  uint32_t* s_there = reinterpret_cast<uint32_t*>(misc + 256);                   // [kRawStages] which of a tile's blocks are in the cache
-  float4* s_tile = reinterpret_cast<float4*>(misc + 288);                        // [kStages] factor of the scores, octaves that V is multiplied by, blocks
-  uint32_t* s_tmem = reinterpret_cast<uint32_t*>(misc + 384);
-  volatile int* s_abort = reinterpret_cast<volatile int*>(misc + 388);
-  const uint32_t bar0 = ubase + C::kOffMisc + 400;
+  int* s_exp = reinterpret_cast<int*>(misc + 224);                               // [2][2][4] the blocks' exponents, of even and odd tiles
+  uint32_t* s_there = reinterpret_cast<uint32_t*>(misc + 288);                   // [kRawStages] which of a tile's blocks are in the cache
+  float4* s_tile = reinterpret_cast<float4*>(misc + 320);                        // [kStages] factor of the scores, octaves that V is multiplied by, blocks
+  float4* s_merge = reinterpret_cast<float4*>(misc + 1024);                      // [128] split: reference, sum and octaves of unit 1's rows
+  uint32_t* s_tmem = reinterpret_cast<uint32_t*>(misc + 400);
+  volatile int* s_abort = reinterpret_cast<volatile int*>(misc + 404);
+  const uint32_t bar0 = ubase + C::kOffMisc + 408;
   auto bar_piece = [&](int set) { return bar0 + 8 * set; };
   auto bar_piecefree = [&](int set) { return bar0 + 16 + 8 * set; };
   auto bar_q = [&](int i) { return bar0 + 32 + 8 * i; };                         // Q_i is in TMEM
@@ -164,7 +168,8 @@ __global__ void __launch_bounds__(kCThreads, 1) chunk_kernel(const __grid_consta
   auto bar_opfree = [&](int s) { return bar0 + 160 + 8 * (NS + s); };
   auto bar_raw = [&](int s) { return bar0 + 160 + 8 * (2 * NS + s); };
   auto bar_rawfree = [&](int s) { return bar0 + 160 + 8 * (2 * NS + NRAW + s); };
-  static_assert(400 + 160 + 8 * (2 * NS + 2 * NRAW) <= 1024, "room for the barriers");
+  const uint32_t bar_merge = bar0 + 160 + 8 * (2 * NS + 2 * NRAW);               // split: unit 1's references and sums are there
+  static_assert(408 + 160 + 8 * (2 * NS + 2 * NRAW + 1) <= 1024 && sizeof(Piece) <= 96, "room for the barriers");
   const int tid = threadIdx.x, lane = tid & 31;
   const int warp = __shfl_sync(0xffffffffu, tid >> 5, 0);
   if (tid == 0) *s_abort = *reinterpret_cast<volatile int*>(status);
@@ -174,27 +179,33 @@ __global__ void __launch_bounds__(kCThreads, 1) chunk_kernel(const __grid_consta
   if (tid == 0) {
     for (int i = 0; i < 2; ++i) {
       mbar_init(bar_piece(i), 1);
-      mbar_init(bar_piecefree(i), 256 + 4 + 2);
+      mbar_init(bar_piecefree(i), 256 + 8 + 2);
       mbar_init(bar_q(i), 128); mbar_init(bar_qfree(i), 1);
       mbar_init(bar_s(i), 1); mbar_init(bar_p(i), 128);
       mbar_init(bar_o(i), 1); mbar_init(bar_ofree(i), 128);
       mbar_init(bar_sfree(i), 128); mbar_init(bar_pfree(i), 1);
     }
+    mbar_init(bar_merge, 128);
     for (int s = 0; s < NS; ++s) { mbar_init(bar_op(s), 128); mbar_init(bar_opfree(s), 1); }
     for (int s = 0; s < NRAW; ++s) { mbar_init(bar_raw(s), 1); mbar_init(bar_rawfree(s), 4); }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
-  if (warp == 12) {
+  if (warp == 16) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(s_tmem)) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  const uint32_t tmem = __shfl_sync(0xffffffffu, *s_tmem, 0);
+  const uint32_t tmem = __reduce_max_sync(0xffffffffu, *s_tmem);      // (in a uniform register, as the products want their operands)
   wait_for_stream();
   const int group = a.q_heads / a.cache.heads, subs = a.cache.page / kBlockTokens;
   auto piece_wait = [&](int it, auto site) { return warp_wait<decltype(site)::value>(bar_piece(it & 1), (it >> 1) & 1, s_abort, status); };
+
+  // Registers: 96 a thread at launch; 136 for the softmax, 80 for keys and values, 48 for the others (together as many).
+  if (warp < 8) asm volatile("setmaxnreg.inc.sync.aligned.u32 136;");
+  else if (warp < 16) asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
+  else asm volatile("setmaxnreg.dec.sync.aligned.u32 48;");
 
   if (warp < 8) {
     // ================= softmax and results of unit i: a thread a row =======================================
@@ -202,18 +213,20 @@ __global__ void __launch_bounds__(kCThreads, 1) chunk_kernel(const __grid_consta
     const uint32_t lane_addr = tmem + ((uint32_t)((warp & 3) * 32) << 16);
     const uint32_t scol = lane_addr + C::kColS + kKeys * i, pcol = lane_addr + C::col_p(i), ocol = lane_addr + D * i, qcol = lane_addr + C::kColQ + (D / 2) * i;
     int done = 0, pieces = 0, tiles = 0;       // tiles of this unit, pieces with rows of it, tiles of the CTA so far
+    int others = 0, splits = 0;                // pieces with rows of unit 1, that were split
     bool ok = true;
     for (int it = 0; ok; ++it) {
       ok = piece_wait(it, std::integral_constant<int, 0>{});
       if (!ok) break;
       const Piece d = s_piece[it & 1];
       if (d.end) break;
-      const int count = d.tile1 - d.tile0, rows = i ? d.units[1] : d.units[0];
+      const int all = d.tile1 - d.tile0, rows = i && !d.split ? d.units[1] : d.units[0];
+      const int from = d.split ? i : 0, step = d.split ? 2 : 1, count = (all - from + step - 1) / step, base = d.split ? 0 : i * kUnitRows;       // its tiles; its first row
       if (rows > 0) {
         const bool there = row < rows;
-        const int in_block = i * kUnitRows + row, token = (d.row0 + in_block) / group, head = d.row0 + in_block - token * group;
+        const int in_block = base + row, token = (d.row0 + in_block) / group, head = d.row0 + in_block - token * group;
         const int limit = there ? d.last_seen(a, in_block) : -1;               // last token that the row sees
-        const int least = d.last_seen(a, i * kUnitRows);                       // the unit's first row
+        const int least = d.last_seen(a, base);                                // the unit's first row
         const size_t at = (size_t)(d.s.first + token) * a.q_heads + d.kv * group + head;
         // ---- the row's query ----
         float scale;
@@ -275,10 +288,10 @@ __global__ void __launch_bounds__(kCThreads, 1) chunk_kernel(const __grid_consta
         uint64_t sum2 = 0;
         int lift = 127;                                                        // octaves that O's values are multiplied by (none yet)
         for (int n = 0; n < count && ok; ++n) {
-          const int key0 = (d.tile0 + n) * kKeys, st = (tiles + n) % NS;
+          const int tile_n = from + n * step, key0 = (d.tile0 + tile_n) * kKeys, st = (tiles + tile_n) % NS;
           ok = warp_wait<3>(bar_s(i), (done + n) & 1, s_abort, status);
           // (the tile's operands were there for its scores; this thread sees what was written beside them.  Not before: a unit that has had no rows may be phases behind)
-          if (ok) ok = warp_wait<2>(bar_op(st), ((tiles + n) / NS) & 1, s_abort, status);
+          if (ok) ok = warp_wait<2>(bar_op(st), ((tiles + tile_n) / NS) & 1, s_abort, status);
           if (!ok) break;
           const float4 tile = s_tile[st];
           tc_fence_after();
@@ -374,13 +387,38 @@ __global__ void __launch_bounds__(kCThreads, 1) chunk_kernel(const __grid_consta
         // ---- results ----
         float s0, s1;
         unpack_f2(sum2, s0, s1);
-        const float sum = s0 + s1;
-        const bool none = ref == -INFINITY && sum == sum;
+        float sum = s0 + s1;
+        if (d.split && i == 1) {                                               // unit 0 does the rest
+          s_merge[row] = make_float4(ref, sum, (float)lift, 0.f);
+          mbar_arrive(bar_merge);
+          ++pieces;
+          tiles += all;
+          mbar_arrive(bar_piecefree(it & 1));
+          continue;
+        }
+        bool none = ref == -INFINITY && sum == sum;
         ok = warp_wait<5>(bar_o(i), pieces & 1, s_abort, status);
         if (!ok) break;
-        tc_fence_after();
         const bool piece = d.place >= 0;
-        const float times = exp2f((float)-lift) * (piece ? 1.f : 1.f / sum);
+        float times = exp2f((float)-lift), times1 = 0.f;                       // of O; of unit 1's
+        if (d.split) {
+          ok = warp_wait<18>(bar_o(1), others & 1, s_abort, status);
+          if (ok) ok = warp_wait<19>(bar_merge, splits & 1, s_abort, status);
+          if (!ok) break;
+          ++splits;
+          const float4 x = s_merge[row];
+          const bool none1 = x.x == -INFINITY && x.y == x.y;
+          const float top = fmaxf(ref, x.x);
+          // (a sum without a reference: NaN)
+          const float f0 = ref == -INFINITY ? (none ? 0.f : 1.f) : ex2(ref - top), f1 = x.x == -INFINITY ? (none1 ? 0.f : 1.f) : ex2(x.x - top);
+          sum = sum * f0 + x.y * f1;
+          times *= f0;
+          times1 = exp2f(-x.z) * f1;
+          ref = top;
+          none = none && none1;
+        }
+        tc_fence_after();
+        if (!piece) { times *= 1.f / sum; times1 *= 1.f / sum; }
         const size_t place = (size_t)max(d.place, 0) * kBlockRows + in_block;
         uint32_t nan = 0;                                                      // groups with a NaN that the row sees
 #pragma unroll
@@ -391,7 +429,16 @@ __global__ void __launch_bounds__(kCThreads, 1) chunk_kernel(const __grid_consta
           tmem_ld32_issue(ocol + 32 * c, v);
           tmem_ld32_wait(v);
 #pragma unroll
-          for (int e = 0; e < 32; ++e) v[e] = none ? 0u : nan >> c & 1 ? 0x7fffffffu : __float_as_uint(__uint_as_float(v[e]) * times);
+          for (int e = 0; e < 32; ++e) v[e] = __float_as_uint(__uint_as_float(v[e]) * times);
+          if (d.split) {
+            uint32_t v1[32];
+            tmem_ld32_issue(ocol + D + 32 * c, v1);
+            tmem_ld32_wait(v1);
+#pragma unroll
+            for (int e = 0; e < 32; ++e) v[e] = __float_as_uint(fmaf(__uint_as_float(v1[e]), times1, __uint_as_float(v[e])));
+          }
+#pragma unroll
+          for (int e = 0; e < 32; ++e) v[e] = none ? 0u : nan >> c & 1 ? 0x7fffffffu : v[e];
           if (there) {
             if (piece || o.out_kind == HYPERATTN_FP32) {
               float4* to = reinterpret_cast<float4*>((piece ? o.part_o + place * D : reinterpret_cast<float*>(o.out) + at * D) + 32 * c);
@@ -412,22 +459,24 @@ __global__ void __launch_bounds__(kCThreads, 1) chunk_kernel(const __grid_consta
         }
         tc_fence_before();
         mbar_arrive(bar_ofree(i));
+        if (d.split) mbar_arrive(bar_ofree(1));
         ++pieces;
         if (there) {
           if (piece) o.part_s[place] = make_float2(none ? -INFINITY : ref, none ? 0.f : sum);
           else o.lse[at] = none ? -INFINITY : (ref + log2f(sum)) * 0.6931471805599453f;
         }
       }
-      tiles += count;
+      others += d.split || d.units[1] > 0;
+      tiles += all;
       mbar_arrive(bar_piecefree(it & 1));
     }
-  } else if (warp < 12) {
+  } else if (warp < 16) {
     // ================= keys and values: a warp a block of 16 tokens ========================================
-    const int sub = warp & 3, c4 = lane & 3, r8 = lane >> 2;
+    const int group_kv = (warp >> 2) & 1, sub = warp & 3, c4 = lane & 3, r8 = lane >> 2;
     // (what one of the four gives up on, all do: they meet at a barrier that has no limit)
     auto all_ok = [&](bool mine) {
       uint32_t all;
-      asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\tbarrier.cta.red.and.pred q, 1, 128, p;\n\tselp.u32 %0, 1, 0, q;\n\t}" : "=r"(all) : "r"((uint32_t)mine) : "memory");
+      asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\tbarrier.cta.red.and.pred q, %2, 128, p;\n\tselp.u32 %0, 1, 0, q;\n\t}" : "=r"(all) : "r"((uint32_t)mine), "r"(1 + group_kv) : "memory");
       return all != 0;
     };
     int tiles = 0;
@@ -438,7 +487,9 @@ __global__ void __launch_bounds__(kCThreads, 1) chunk_kernel(const __grid_consta
       const Piece d = s_piece[it & 1];
       if (d.end) break;
       for (int n = d.tile0; n < d.tile1; ++n, ++tiles) {
+        if ((tiles & 1) != group_kv) continue;
         const int st = tiles % NS, rs = tiles % NRAW;
+        int* exponents = s_exp + (2 * group_kv + (tiles >> 1 & 1)) * 4;
         bool mine = tiles < NS || warp_wait<7>(bar_opfree(st), (tiles / NS - 1) & 1, s_abort, status);
         if (mine) mine = warp_wait<8>(bar_raw(rs), (tiles / NRAW) & 1, s_abort, status);
         const uint32_t blocks = s_there[rs];
@@ -493,12 +544,12 @@ __global__ void __launch_bounds__(kCThreads, 1) chunk_kernel(const __grid_consta
             vtop_s = __hmax2(vtop_s, as_half2(sv[half][g])); vtop_m = __hmax2(vtop_m, __habs2(as_half2(mv[half][g])));
           }
         const int ek = __reduce_max_sync(0xffffffffu, exponent_of(as_u32(top_s), as_u32(top_m))), ev = __reduce_max_sync(0xffffffffu, exponent_of(as_u32(vtop_s), as_u32(vtop_m)));
-        if (lane == 0) s_exp[(tiles & 1) * 4 + sub] = ek | ev << 8;
+        if (lane == 0) exponents[sub] = ek | ev << 8;
         ok = all_ok(mine);
         if (!ok) break;
         int tile_k = 0, tile_v = 0;
 #pragma unroll
-        for (int w = 0; w < 4; ++w) { const int e = s_exp[(tiles & 1) * 4 + w]; tile_k = max(tile_k, e & 255); tile_v = max(tile_v, e >> 8); }
+        for (int w = 0; w < 4; ++w) { const int e = exponents[w]; tile_k = max(tile_k, e & 255); tile_v = max(tile_v, e >> 8); }
         const int lift_k = lift_of(tile_k), lift_v = lift_of(tile_v) & ~3;
         const __half2 up_k = lift2(lift_k), up_v = lift2(lift_v);
         uint8_t* to = smem + st * C::kStage;
@@ -576,7 +627,7 @@ __global__ void __launch_bounds__(kCThreads, 1) chunk_kernel(const __grid_consta
       __syncwarp();
       if (lane == 0) mbar_arrive(bar_piecefree(it & 1));
     }
-  } else if (warp == 12) {
+  } else if (warp == 16) {
     // ================= products ============================================================================
     const bool el = elect_one();
     constexpr uint32_t idesc_s = (1u << 4) | ((uint32_t)(kKeys >> 3) << 17) | ((128u >> 4) << 24);
@@ -587,9 +638,9 @@ __global__ void __launch_bounds__(kCThreads, 1) chunk_kernel(const __grid_consta
       ok = piece_wait(it, std::integral_constant<int, 9>{});
       if (!ok) break;
       const Piece& d = s_piece[it & 1];
-      auto uni = [&](int x) { return __shfl_sync(0xffffffffu, x, 0); };
-      const bool end = uni(d.end) != 0, has[2] = {uni(d.units[0]) > 0, uni(d.units[1]) > 0};
-      const int count = uni(d.tile1 - d.tile0);
+      auto uni = [&](int x) { return __reduce_max_sync(0xffffffffu, x); };
+      const bool end = uni(d.end) != 0, split = uni(d.split) != 0, has[2] = {uni(d.units[0]) > 0, split || uni(d.units[1]) > 0};
+      const int count = uni(d.tile1 - d.tile0), step = split ? 2 : 1;
       __syncwarp();
       if (el) mbar_arrive(bar_piecefree(it & 1));
       if (end) break;
@@ -598,38 +649,76 @@ __global__ void __launch_bounds__(kCThreads, 1) chunk_kernel(const __grid_consta
         if (ok && has[i]) ok = warp_wait<10>(bar_q(i), pieces[i] & 1, s_abort, status);
       if (!ok) break;
       auto wait_tile = [&](int n) { if (ok) ok = warp_wait<11>(bar_op((tiles + n) % NS), ((tiles + n) / NS) & 1, s_abort, status); };
+      // tile n, the unit's last one if there is none `step` further
       auto scores = [&](int i, int n) {
-        const uint32_t stage = ubase + (uint32_t)((tiles + n) % NS) * C::kStage, to = tmem + C::kColS + kKeys * i;
+        const uint32_t stage = (ubase + (uint32_t)((tiles + n) % NS) * C::kStage) >> 4, to = tmem + C::kColS + kKeys * i;
         if (el) {
 #pragma unroll
           for (int part = 0; part < 2; ++part)
 #pragma unroll
             for (int ks = 0; ks < D / 16; ++ks)
-              mma_ts2(to, tmem + C::kColQ + (D / 2) * i + 8 * ks, ((stage + part * C::kOffRest + (ks >> 2) * C::kKeySlab + (ks & 3) * 32) >> 4) | (1u << 16), kDescSwizzled, idesc_s, part + ks > 0);
-          mma_ss2(to, ((ubase + C::kOffSums + i * C::kSums) >> 4) | (((kUnitRows * 16u) >> 4) << 16), ((stage + C::kOffMinima) >> 4) | (((kKeys * 16u) >> 4) << 16), kDescPlain, idesc_s, 1);
+              mma_ts2(to, tmem + C::kColQ + (D / 2) * i + 8 * ks, (stage | (1u << 16)) + ((part * C::kOffRest + (ks >> 2) * C::kKeySlab + (ks & 3) * 32) >> 4), kDescSwizzled, idesc_s, part + ks > 0);
+          mma_ss2(to, ((ubase + C::kOffSums + i * C::kSums) >> 4) | (((kUnitRows * 16u) >> 4) << 16), (stage + (C::kOffMinima >> 4)) | (((kKeys * 16u) >> 4) << 16), kDescPlain, idesc_s, 1);
           umma_commit(bar_s(i));
-          if (n + 1 == count) umma_commit(bar_qfree(i));
+          if (n + step >= count) umma_commit(bar_qfree(i));
         }
       };
-      auto outputs = [&](int i, int n) {
-        if (n == 0 && pieces[i] > 0) ok = warp_wait<12>(bar_ofree(i), (pieces[i] - 1) & 1, s_abort, status);
-        if (ok) ok = warp_wait<13>(bar_p(i), (done[i] + n) & 1, s_abort, status);
+      // (k: tiles of the unit before it)
+      auto outputs = [&](int i, int n, int k) {
+        if (k == 0 && pieces[i] > 0) ok = warp_wait<12>(bar_ofree(i), (pieces[i] - 1) & 1, s_abort, status);
+        if (ok) ok = warp_wait<13>(bar_p(i), (done[i] + k) & 1, s_abort, status);
         if (!ok) return;
         tc_fence_after();
         const uint32_t v_lo = ((ubase + (uint32_t)((tiles + n) % NS) * C::kStage + C::kOffV) >> 4) | (1u << 16);
         if (el) {
 #pragma unroll
-          for (int kk = 0; kk < kKeys / 16; ++kk) mma_ts2(tmem + D * i, tmem + C::col_p(i) + kk * 8, v_lo + kk * (32 >> 4), kDescSwizzled, idesc_o, kk > 0 || n > 0);
+          for (int kk = 0; kk < kKeys / 16; ++kk) mma_ts2(tmem + D * i, tmem + C::col_p(i) + kk * 8, v_lo + kk * (32 >> 4), kDescSwizzled, idesc_o, kk > 0 || k > 0);
           if (C::kOwnP) umma_commit(bar_pfree(i));
-          if (n + 1 == count) umma_commit(bar_o(i));
+          if (n + step >= count) umma_commit(bar_o(i));
         }
       };
+      auto next_scores = [&](int i, int n, int k) {                              // of tile n, k tiles of the unit before it
+        if constexpr (C::kOwnP) {
+          ok = warp_wait<14>(bar_sfree(i), (done[i] + k - 1) & 1, s_abort, status);
+          if (!ok) return;
+          tc_fence_after();
+        }
+        scores(i, n);
+      };
       wait_tile(0);
+      if (split && count > 1) wait_tile(1);
       if (!ok) break;
       tc_fence_after();
 #pragma unroll
       for (int i = 0; i < 2; ++i)
-        if (has[i]) scores(i, 0);
+        if (has[i]) scores(i, split ? i : 0);
+      if (split) {
+        for (int n0 = 0; n0 < count && ok; n0 += 2) {
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            const int n = n0 + i, k = n0 / 2;
+            if (!ok || n >= count) break;
+            auto next = [&] {
+              if (n + 2 >= count) return;
+              wait_tile(n + 2);
+              if (!ok) return;
+              tc_fence_after();
+              next_scores(i, n + 2, k + 1);
+            };
+            // (P in the place of S; and of three stages, tile n + 2 gets that of tile n - 1: its keys come while this tile's weights are multiplied)
+            if (C::kOwnP) next();
+            if (ok) outputs(i, n, k);
+            if (ok && el) umma_commit(bar_opfree((tiles + n) % NS));
+            if (ok && !C::kOwnP) next();
+          }
+        }
+        tiles += count;
+        done[0] += (count + 1) / 2;
+        done[1] += count / 2;
+        ++pieces[0];
+        ++pieces[1];
+        continue;
+      }
       for (int n = 0; n < count && ok; ++n) {
         if (n + 1 < count) wait_tile(n + 1);
         if (!ok) break;
@@ -638,21 +727,16 @@ __global__ void __launch_bounds__(kCThreads, 1) chunk_kernel(const __grid_consta
           // the next scores as soon as these have been read, then the products with V
 #pragma unroll
           for (int i = 0; i < 2; ++i)
-            if (ok && n + 1 < count && has[i]) {
-              ok = warp_wait<14>(bar_sfree(i), (done[i] + n) & 1, s_abort, status);
-              if (!ok) break;
-              tc_fence_after();
-              scores(i, n + 1);
-            }
+            if (ok && n + 1 < count && has[i]) next_scores(i, n + 1, n + 1);
 #pragma unroll
           for (int i = 0; i < 2; ++i)
-            if (ok && has[i]) outputs(i, n);
+            if (ok && has[i]) outputs(i, n, n);
         } else {
 #pragma unroll
           for (int i = 0; i < 2; ++i)
             if (ok && has[i]) {
-              outputs(i, n);
-              if (ok && n + 1 < count) scores(i, n + 1);
+              outputs(i, n, n);
+              if (ok && n + 1 < count) next_scores(i, n + 1, n + 1);
             }
         }
         if (ok && el) umma_commit(bar_opfree((tiles + n) % NS));
@@ -663,7 +747,7 @@ __global__ void __launch_bounds__(kCThreads, 1) chunk_kernel(const __grid_consta
         if (has[i]) { done[i] += count; ++pieces[i]; }
     }
     __syncwarp();
-  } else if (warp == 13) {
+  } else if (warp == 17) {
     // ================= copies ==============================================================================
     // A lane has a block of the next eight tiles: its page is looked up before their turn comes.
     int tiles = 0;
@@ -708,7 +792,7 @@ __global__ void __launch_bounds__(kCThreads, 1) chunk_kernel(const __grid_consta
     }
     // nothing may be on its way into shared memory when the CTA ends
     for (int s = 0; s < NRAW && s < tiles; ++s) mbar_drain(bar_raw(s), ((tiles - 1 - s) / NRAW) & 1);
-  } else {
+  } else if (warp == 18) {
     // ================= segments ============================================================================
     const long long begin = o.start[blockIdx.x], end = o.start[blockIdx.x + 1];
     int slot = 0;
@@ -735,6 +819,7 @@ __global__ void __launch_bounds__(kCThreads, 1) chunk_kernel(const __grid_consta
         const long long first = x - (rest - d.kv * whole), last = first + whole;               // the segment's
         d.tile0 = (int)((x - first) / k.cost);
         d.tile1 = (int)((min(last, end) - first) / k.cost);
+        d.split = d.units[1] == 0 && d.tile1 - d.tile0 > 1;
         d.place = x == first && last <= end ? -1 : 2 * (int)blockIdx.x + (x > begin ? 1 : 0);
         x = min(last, end);
       }
@@ -753,7 +838,7 @@ __global__ void __launch_bounds__(kCThreads, 1) chunk_kernel(const __grid_consta
   // ---- teardown ----
   tc_fence_before();
   __syncthreads();
-  if (warp == 12) {
+  if (warp == 16) {
     tc_fence_after();
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
   }
