@@ -845,7 +845,8 @@ __global__ void __launch_bounds__(kCThreads, 1) chunk_kernel(const __grid_consta
 }
 
 // Puts the pieces of segments together that lie in several parts; rows without any tile get their zeros.
-constexpr int kPutThreads = 256, kPutRows = 32;
+constexpr int kPutThreads = 256;
+template <int D> constexpr int kPutRows = kPutThreads / (D / 4);        // (a row for every 32 or 16 threads: with 32 rows a CTA it took 20 us)
 
 template <int D, class T>
 __global__ void __launch_bounds__(kPutThreads) put_kernel(const __grid_constant__ ChunkArgs a, const __grid_constant__ ChunkOut o) {
@@ -855,7 +856,7 @@ __global__ void __launch_bounds__(kPutThreads) put_kernel(const __grid_constant_
   if (b.x < 0) return;
   const Span s = span_of(a, b.x);
   const RowBlock k = row_block(a, s, b.y);
-  const int row0 = blockIdx.y * kPutRows;
+  const int row0 = blockIdx.y * kPutRows<D>;
   if (row0 >= k.rows) return;
   const long long whole = (long long)k.tiles * k.cost, first = o.before[slot] + kv * whole, last = first + whole;
   int p0 = 0, p1 = 0;                                  // its first and last part
@@ -869,12 +870,13 @@ __global__ void __launch_bounds__(kPutThreads) put_kernel(const __grid_constant_
     --p1;
     if (p0 == p1) return;                              // finished there
   }
-  constexpr int LANES = D / 4, ROWS = kPutThreads / LANES;
-  const int lane = tid % LANES;
-  for (int row = row0 + tid / LANES; row < min(row0 + kPutRows, k.rows); row += ROWS) {
+  constexpr int LANES = D / 4;
+  const int lane = tid % LANES, row = row0 + tid / LANES;
+  if (row < k.rows) {
     float ref = -INFINITY, sum = 0.f;
     float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
     if (k.tiles > 0)
+#pragma unroll 4
       for (int c = p0; c <= p1; ++c) {
         if (o.start[c] == o.start[c + 1]) continue;
         const size_t at = (size_t)(2 * c + (c == p0 && o.start[c] < first ? 1 : 0)) * kBlockRows + row;
@@ -911,8 +913,8 @@ ChunkShape chunk_shape(const hyperattn_chunk_params& p) {
   s.bytes = s.part_o + (size_t)s.parts * 2 * kBlockRows * p.cache.d * 4;
   return s;
 }
-// Few rows on average: the warp-level kernels.  us there / here: 32 rows over 4000 tokens, 8 heads of 128, 8 requests 65 / 88, 64 rows 111 / 88; 2 x 30000 tokens, 32 heads of 64, 32 rows
-// 288 / 371, 64 rows 423 / 312; tables of no more than 1024 tokens (here the first and the last launch take as long as the work): 64 rows 19 / 39.
+// Few rows on average: the warp-level kernels.  us there / here, up to 8000 tokens, 8 requests: 8 heads of 128, 32 rows 60 / 79, 48 rows 94 / 91, 64 rows 106 / 74; 32 heads of 64,
+// 32 rows 129 / 161, 48 rows 157 / 157, 64 rows 173 / 143.  Tables of no more than 1024 tokens (here the first and the last launch take as long as the work), 64 rows: 21 / 25.
 bool few_rows(const hyperattn_chunk_params& p, size_t* bytes) {
   const long long most = (long long)p.table_width * p.cache.page_tokens <= 1024 ? 64 : 32;
   return (long long)p.rows * (p.q_heads / p.cache.kv_heads) <= most * p.requests && few_rows_attention(p, bytes);
@@ -964,7 +966,7 @@ extern "C" int hyperattn_cache_chunk_attention(const hyperattn_chunk_params* p) 
     cudaError_t e = allow_smem<chunk_kernel<D, T>>(CCfg<D>::kSmem);
     if (e == cudaSuccess) e = launch(share_kernel, dim3(1), dim3(kShareThreads), 0, st, a, o);
     if (e == cudaSuccess) e = launch(chunk_kernel<D, T>, dim3((unsigned)s.parts), dim3(kCThreads), CCfg<D>::kSmem, st, a, o, run, status);
-    if (e == cudaSuccess) e = launch(put_kernel<D, T>, dim3((unsigned)(s.slots * p->cache.kv_heads), kBlockRows / kPutRows), dim3(kPutThreads), 0, st, a, o);
+    if (e == cudaSuccess) e = launch(put_kernel<D, T>, dim3((unsigned)(s.slots * p->cache.kv_heads), kBlockRows / kPutRows<D>), dim3(kPutThreads), 0, st, a, o);
     return status_of(e, "chunk attention");
   };
   auto of_type = [&](auto dim) { return p->dtype == HYPERATTN_BF16 ? go(dim, __nv_bfloat16()) : go(dim, __half()); };
