@@ -323,8 +323,9 @@ int hyperattn_alpha_workspace_bytes(int B, int H, int n, int n_k, size_t* bytes)
  * grouped: q_heads is a multiple of kv_heads, query head h reads key head h / (q_heads / kv_heads).  d in {64, 128}.
  * dtype is HYPERATTN_BF16 or HYPERATTN_FP16 (queries, keys, values), out_dtype the same or HYPERATTN_FP32.  Lengths,
  * offsets, tables and slots are device arrays of int32, read by the kernels: no entry point looks at them on the host,
- * synchronises or allocates, so every call can be captured in a graph (the two attentions after one call outside a capture, or
- * any other call of the library: the first one on a device makes the status word, HYPERATTN_WORKSPACE_TOO_SMALL in a capture).
+ * synchronises or allocates, so every call can be captured in a graph (the three attentions and the
+ * weights after one call outside a capture, or any other call of the library: the first one on a device makes the status word,
+ * HYPERATTN_WORKSPACE_TOO_SMALL in a capture).
  * Their waits on the device are bounded like those of hyperattn_forward: hyperattn_last_device_status.  Calls without rows
  * return at once (and write nothing).
  *
@@ -431,8 +432,13 @@ int hyperattn_prompt_attention(const hyperattn_prompt_params* p);
  * cu_q[r + 1] - 1 of q are request r's queries (cu_q = NULL: row r alone, and rows = requests), its keys and values tokens 0 .. lengths[r] - 1 of
  * the cache.  causal: the last query sees all of them, every earlier one a token less (so with fewer tokens than queries the first queries see none).
  * out and lse as in hyperattn_cache_attention; a query that sees no token gets out = 0, lse = -infinity; rows beyond cu_q[requests] are not
- * written.  A group of K or V whose scale or minimum is not finite counts as NaN: a query that sees it gets NaN (K) or NaN in those 32
- * coordinates (V), other queries do not notice.  requests <= 4096; rows * q_heads < 2^31. */
+ * written.  A group of 32 whose scale or minimum is not finite is the matter of the queries that see it: they get NaN or what an infinite number gives (V: in those
+ * 32 coordinates), other queries do not notice.  Offsets that do not ascend leave the results of the rows concerned undefined, nothing else.
+ * Queries enter the products as fp16 (after a power of two that brings a row's largest entry near one, or near 2^9), keys as they are stored, so scores are sums in fp32 of exact products.
+ * Weights enter the second product as fp16 (2^-11; requests of few rows, with fp16 queries or four rows and fewer: what that loses too), values of requests of many
+ * rows as fp16 as well (2^-11 more).  Sums of weights, outputs and the log-sum-exp are fp32.  A result depends on what the call is made of: requests' rows are split over the GPU by
+ * their number; the same call gives the same bits.
+ * requests <= 4096; rows * q_heads < 2^31; table_width * page_tokens < 2^31 - 2^16. */
 typedef struct hyperattn_chunk_params {
   hyperattn_cache cache;
   const void* q;           /* [rows, q_heads, d], strides in elements (multiples of 8) */
@@ -454,7 +460,9 @@ int hyperattn_cache_chunk_attention_workspace_bytes(const hyperattn_chunk_params
  *   weights_out[r, g, t] = decay weights[r, g, t] [t < lengths[r] - n] + sum exp(softmax_scale <q[i, h], k_t> - lse[i, h])
  * over the request's rows i that see token t and the query heads h that read key head g; 0 for t >= lengths[r].  (Tokens of the rows themselves start
  * from nothing, whatever their places held.)  weights, weights_out: fp32 [requests, kv_heads, table_width * page_tokens] contiguous,
- * weights = NULL: nothing so far; they may be the same array.  Tokens in table entries that are no page get no weight. */
+ * weights = NULL: nothing so far; they may be the same array.  Tokens in table entries that are no page get no weight.  Scores as in hyperattn_cache_chunk_attention (exact
+ * products, sums in fp32; rows whose largest entry is up to 2^12 smaller than that of others beside them share their power of two: entries below 2^-21 of their row's
+ * largest are then rounded), exponentials (2^-22) and sums over rows in fp32, in an order that does not depend on timing.  A row whose lse is -infinity gives nothing.  Limits as there. */
 typedef struct hyperattn_weights_params {
   hyperattn_cache cache;
   const void* q;
@@ -478,7 +486,8 @@ int hyperattn_cache_weights_workspace_bytes(const hyperattn_weights_params* p, s
  *   lengths_out [requests]  keep[r] if request r is cut, else lengths[r]
  *   table_out   [requests, table_width]: the new pages of a request that is cut, else its old ones; unused entries -1
  *   free_out, n_free_out    the stack after the step, [num_free], unused entries -1
- * Limits as for hyperattn_cache_plan. */
+ * (A page in several requests' tables would be given back while others still have it: such requests are not for this plan.)  Limits as for hyperattn_cache_plan, but
+ * requests * table_width + num_free < 2^31 - 2^20. */
 typedef struct hyperattn_evict_plan {
   const int32_t *lengths, *keep, *table, *free_pages, *n_free;
   int requests, table_width, num_free, page_tokens;
@@ -493,7 +502,7 @@ int hyperattn_cache_evict_plan(const hyperattn_evict_plan* p);
  * page that the call reads (hyperattn_cache_evict_plan makes such a table).  Nothing of other requests moves.
  *   weights, weights_out  fp32 [requests, kv_heads, table_width * page_tokens]: what every token has, in its new order; 0 beyond the tokens
  *   kept                  int32, of that shape: the tokens (before) that the new ones are; -1 beyond them, and for requests that are not cut
- * weights_out must not be weights. */
+ * weights_out must not be weights.  table_width * page_tokens < 2^31 - 2^20; requests * table_width * page_tokens / 16 < 2^31. */
 typedef struct hyperattn_evict_params {
   hyperattn_cache cache;
   const float* weights;

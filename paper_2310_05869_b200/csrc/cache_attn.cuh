@@ -670,20 +670,28 @@ __global__ void __launch_bounds__(32 * kWarps, ctas_by_registers(NT)) cache_attn
       s_queries[r] = queries_of(a, r);
       if (MODE == kSomeRows) units *= chunks_of(r);
     }
-    mine += units;
+    if constexpr (MODE == kSomeRows) mine = plus(mine, units);
+    else mine += units;
   }
   int run = mine;
 #pragma unroll
-  for (int o = 1; o < 32; o <<= 1) { const int y = __shfl_up_sync(0xffffffffu, run, o); if (lane >= o) run += y; }
+  for (int o = 1; o < 32; o <<= 1) { const int y = __shfl_up_sync(0xffffffffu, run, o); if (lane >= o) run = MODE == kSomeRows ? plus(run, y) : run + y; }
   if (lane == 31) s_sums[warp] = run;
   __syncthreads();
   run -= mine;
-  for (int w = 0; w < warp; ++w) run += s_sums[w];
-  for (int r = r0; r < r1; ++r) s_starts[r] += run;
-  if (tid == 32 * kWarps - 1) s_starts[a.requests] = run + mine;
+  for (int w = 0; w < warp; ++w) run = MODE == kSomeRows ? plus(run, s_sums[w]) : run + s_sums[w];
+  for (int r = r0; r < r1; ++r) s_starts[r] = MODE == kSomeRows ? plus(s_starts[r], run) : s_starts[r] + run;
+  if (tid == 32 * kWarps - 1) s_starts[a.requests] = MODE == kSomeRows ? plus(run, mine) : run + mine;
   __syncthreads();
   if constexpr (MODE == kWeights) blank(a.weights, a.lengths, a.requests, a.cache.heads, a.width * a.cache.page, R::kUnitTokens, blockIdx.x, gridDim.x);
   const int segs = a.cache.heads * (MODE == kOneQuery ? a.chunks : 1);   // of a request (some rows: key heads, of which each has the request's chunks)
+  if constexpr (MODE == kSomeRows) {                                     // (offsets that do not ascend may ask for more units than a number holds: none then)
+    const bool many = s_starts[a.requests] > 0x7fffffff / segs;
+    __syncthreads();
+    if (many)
+      for (int r = tid; r <= a.requests; r += 32 * kWarps) s_starts[r] = 0;
+    __syncthreads();
+  }
   const int total = s_starts[a.requests] * segs, warps = gridDim.x * kWarps, part = max(1, total / warps + (total % warps != 0));
   if (MODE != kWeights && blockIdx.x == 0) {
     for (int r = tid; r <= a.requests; r += 32 * kWarps) a.starts[r] = s_starts[r];
@@ -953,26 +961,28 @@ __global__ void __launch_bounds__(kJoinThreads) join_kernel(const __grid_constan
     first_head = kv * per_kv + chunk * a.part_heads; heads = min(per_kv - chunk * a.part_heads, a.part_heads);
   } else {
     // which request has the chunk (of all) that this CTA is for
-    __shared__ int s_found[4];
+    __shared__ int s_found;
     segs = a.cache.heads;
     const int slot = blockIdx.x / segs;
     kv = blockIdx.x - slot * segs;
-    if (threadIdx.x == 0) s_found[0] = -1;
+    if (threadIdx.x == 0) s_found = -1;
     __syncthreads();
     for (int i = threadIdx.x; i < a.requests; i += kJoinThreads) {
       const int2 q = queries_of(a, i);
       const long long first = chunk_slots(q.x, i, per_kv, a.part_heads);
       const int n = (q.y * per_kv + a.part_heads - 1) / a.part_heads;
-      if (slot >= first && slot < first + n) { s_found[0] = i; s_found[1] = (int)(slot - first); s_found[2] = q.x; s_found[3] = q.y; }
+      if (slot >= first && slot < first + n) atomicMax(&s_found, i);      // (one of them, if offsets that do not ascend give a chunk to several)
     }
     __syncthreads();
-    r = s_found[0];
+    r = s_found;
     if (r < 0) return;
-    first_query = s_found[2];
-    first_head = s_found[1] * a.part_heads;
-    heads = min(s_found[3] * per_kv - first_head, a.part_heads);
-    chunks = (s_found[3] * per_kv + a.part_heads - 1) / a.part_heads;
-    seg = kv * chunks + s_found[1];
+    const int2 q = queries_of(a, r);
+    const int chunk = (int)(slot - chunk_slots(q.x, r, per_kv, a.part_heads));
+    first_query = q.x;
+    first_head = chunk * a.part_heads;
+    heads = min(q.y * per_kv - first_head, a.part_heads);
+    chunks = (q.y * per_kv + a.part_heads - 1) / a.part_heads;
+    seg = kv * chunks + chunk;
   }
   auto row_of = [&](int head) {
     if constexpr (MODE == kOneQuery) return (size_t)r * a.q_heads + first_head + head;

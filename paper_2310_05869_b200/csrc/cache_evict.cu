@@ -9,6 +9,7 @@ namespace {
 // As the cache's plan (cache.cu): every CTA makes the running sums for itself, then some write the tables, some the stack, one the requests' lengths.
 constexpr int kColumns = 512;            // table entries of a warp at a time
 struct EvictParts { int tables, stack; };
+constexpr int kBeyond = 1 << 20;        // what the step of a loop may add to the last index that there is
 
 __global__ void __launch_bounds__(kPlanThreads) evict_plan_kernel(const __grid_constant__ hyperattn_evict_plan p, EvictParts parts) {
   extern __shared__ int smem[];
@@ -396,7 +397,7 @@ using namespace hyperattn;
 extern "C" int hyperattn_cache_evict_plan(const hyperattn_evict_plan* p) {
   if (!p || p->requests < 0 || p->table_width <= 0 || p->num_free < 0 || p->page_tokens <= 0) return HYPERATTN_INVALID_ARGUMENT;
   if (p->requests > HYPERATTN_PLAN_MAX_REQUESTS || (long long)p->table_width * p->page_tokens > 0x7fffffffLL || p->table_width >= 1 << 28 ||
-      (long long)p->requests * p->table_width + p->num_free > 0x7fffffffLL)
+      (long long)p->requests * p->table_width + p->num_free > 0x7fffffffLL - kBeyond)
     return HYPERATTN_UNSUPPORTED_SHAPE;
   if (p->requests == 0) return HYPERATTN_OK;
   if (!p->lengths || !p->keep || !p->table || (p->num_free && (!p->free_pages || !p->free_out)) || !p->n_free || !p->lengths_out || !p->table_out || !p->n_free_out)
@@ -415,7 +416,7 @@ extern "C" int hyperattn_cache_evict(const hyperattn_evict_params* p) {
   int rc;
   if (!p || p->requests < 0 || p->table_width <= 0 || p->recent < 0 || p->first < 0) return HYPERATTN_INVALID_ARGUMENT;
   if (bad_cache(p->cache, &rc)) return rc;
-  if (p->requests > kMostRequests || (long long)p->table_width * p->cache.page_tokens > 0x7fffffffLL || (long long)p->requests * p->cache.kv_heads > 0x7fffffffLL / 8 ||
+  if (p->requests > kMostRequests || (long long)p->table_width * p->cache.page_tokens > 0x7fffffffLL - kBeyond || (long long)p->requests * p->cache.kv_heads > 0x7fffffffLL / 8 ||
       (long long)p->requests * p->table_width * (p->cache.page_tokens / kBlockTokens) > 0x7fffffffLL ||
       (long long)p->cache.num_pages * (p->cache.page_tokens / kBlockTokens) * p->cache.kv_heads > 0x7fffffffLL)
     return HYPERATTN_UNSUPPORTED_SHAPE;

@@ -283,6 +283,9 @@ __device__ __forceinline__ void places_of(int requests, int part, int parts, F w
   __syncthreads();
 }
 
+// Places of a table row: so far below 2^31 that what a loop over them, or a last unit of tokens, adds does not pass it
+constexpr long long kMostPlaces = 0x7fffffffLL - (1 << 16);
+
 template <class P>
 int check_chunk(const P* p) {
   int rc;
@@ -290,7 +293,7 @@ int check_chunk(const P* p) {
   if (bad_cache(p->cache, &rc)) return rc;
   if (p->dtype != HYPERATTN_BF16 && p->dtype != HYPERATTN_FP16) return p->dtype == HYPERATTN_FP32 ? HYPERATTN_UNSUPPORTED_SHAPE : HYPERATTN_INVALID_ARGUMENT;
   if (p->q_heads % p->cache.kv_heads || bad_stride(p->q_row_stride) || bad_stride(p->q_head_stride) || p->requests > HYPERATTN_PLAN_MAX_REQUESTS) return HYPERATTN_UNSUPPORTED_SHAPE;
-  if ((long long)p->table_width * p->cache.page_tokens > 0x7fffffffLL - 256 || (long long)p->rows * p->q_heads > 0x7fffffffLL ||
+  if ((long long)p->table_width * p->cache.page_tokens > kMostPlaces || (long long)p->rows * p->q_heads > 0x7fffffffLL ||
       (long long)p->cache.num_pages * (p->cache.page_tokens / kBlockTokens) * p->cache.kv_heads > 0x7fffffffLL ||
       ((long long)p->table_width * p->cache.page_tokens / 64 + 1) * p->cache.kv_heads > 0x7fffffffLL)
     return HYPERATTN_UNSUPPORTED_SHAPE;
