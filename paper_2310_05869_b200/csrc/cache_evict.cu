@@ -6,7 +6,7 @@ namespace hyperattn {
 namespace {
 
 // ---- plan ------------------------------------------------------------------------------------------------------------------
-// As the cache's plan (cache.cu): every CTA makes the running sums for itself, then some write the tables, some the stack, one the requests' lengths.
+// As the cache's plan (cache.cu): every CTA makes the running sums for itself, then some write the tables, some the stack, one the requests' lengths.  256 requests 6.5 us, 1024 x 2048 pages 16.6.
 constexpr int kColumns = 512;            // table entries of a warp at a time
 struct EvictParts { int tables, stack; };
 constexpr int kBeyond = 1 << 20;        // what the step of a loop may add to the last index that there is
@@ -117,6 +117,8 @@ __device__ __forceinline__ uint32_t order_of(float w) { return w > 0.f ? __float
 
 // A cluster of CTAs takes a request and key head, each a slice of its tokens, whose weights (in order) it holds in shared memory if they fit.  The smallest weight that stays is
 // found by three digits of 10, 11 and 10 bits, from the top: a histogram in each CTA, which all add up for themselves.  Then every warp counts a part of the slice, and numbers it.
+// 2 x 131072 tokens, 32 heads, to 8192 each: 57 us (115 with four digits of 8 bits), of 15 for its bytes: two waves of clusters, instructions and latencies between the digits.  32 requests up to 8192
+// tokens, 8 heads: 19 us.
 constexpr int kSelectThreads = 1024, kSelectWarps = kSelectThreads / 32, kBins = 2048, kMostHeld = 40960;
 
 __device__ __forceinline__ uint32_t cluster_rank() {
@@ -271,6 +273,7 @@ static_assert(kSelectWarps == 32, "a lane for every warp");
 // ---- moving them -------------------------------------------------------------------------------------------------------------
 // A warp makes a block of 16 tokens of the new pages at a time, from the blocks that its tokens are in: K by pieces of a token (16 bytes, d = 64: 8), V by 16-byte loads that
 // hold a token's byte of four words, scales and minima one by one.  The blocks of all requests that are cut are one sequence, in equal parts for the warps.
+// 32 requests to 2048 tokens, 8 heads of 128: 45 us (115 MB read where tokens that stay have about 40: sectors are used in part; stalls are those of gathers).
 constexpr int kMoveWarps = 4, kMostRequests = HYPERATTN_PLAN_MAX_REQUESTS;
 
 template <int D>

@@ -5,6 +5,10 @@
 //     w_t += sum_i exp2(s_ti c_i - lse_i)          a thread a token, so that sums over rows stay in it
 // Every token's sum is one thread's (two: a tile's first, third ... images and its second, fourth ...), so nothing is atomic and results do not depend on timing.
 //
+// What bounds it: exponentials, 16 a clock and SM (60 % of the cycles), and what stands around them: 2 requests, 1025 rows over up to 32000 tokens, 32 heads of 64: 299 us (251 without the
+// exponentials, 273 without the products, 167 without the sums, 293 without the keys' conversion); bytes alone 50.  16 warps for the sums instead of 8: 310; one pair of exponentials in eight by
+// arithmetic: 347; the next scores on their way while 16 are used: 355.
+//
 // Warp roles: 0-7 sums (two groups of four, for every other image), 8-15 keys (two groups, for every other tile), 16 products (and TMEM), 17 copies of keys, 18 of images.
 // Every wait is bounded: a CTA that gives up raises the device status word, drains its copies, frees its TMEM and returns.
 #include <type_traits>

@@ -10,6 +10,13 @@ its bytes).  A decode step of a server:
     plan = cache_plan(lengths, new, table, free, n_free, page_tokens, rows)       # pages, slots and positions of the step's tokens
     cache_store(cache, k, v, plan.slots)                                          # for every layer: the new keys and values,
     out, lse = cache_attention(q, cache, plan.table, plan.lengths)                # attention over all that is cached
+
+With several new tokens a request (`plan.cu_new` has their offsets), and contexts that are cut to the tokens of most weight:
+
+    out, lse = cache_chunk_attention(q, cache, plan.table, plan.lengths, plan.cu_new)
+    w = cache_weights(q, cache, plan.table, plan.lengths, lse, plan.cu_new, weights=w)             # what cached tokens have got so far, for every layer
+    less = cache_evict_plan(plan.lengths, keep, plan.table, plan.free, plan.n_free, page_tokens)   # new pages for keep[r] tokens of requests that have more
+    w, kept = cache_evict(cache, w, plan.table, plan.lengths, less.table, less.lengths, recent=32) # and those tokens moved there
 """
 from __future__ import annotations
 
