@@ -273,7 +273,8 @@ static_assert(kSelectWarps == 32, "a lane for every warp");
 // ---- moving them -------------------------------------------------------------------------------------------------------------
 // A warp makes a block of 16 tokens of the new pages at a time, from the blocks that its tokens are in: K by pieces of a token (16 bytes, d = 64: 8), V by 16-byte loads that
 // hold a token's byte of four words, scales and minima one by one.  The blocks of all requests that are cut are one sequence, in equal parts for the warps.
-// 32 requests to 2048 tokens, 8 heads of 128: 45 us (115 MB read where tokens that stay have about 40: sectors are used in part; stalls are those of gathers).
+// 32 requests to 2048 tokens, 8 heads of 128: 41 us (115 MB read where tokens that stay have about 40: sectors are used in part; stalls are those of gathers).
+// With 12 CTAs an SM, of which 9 are there at a time, 127.8 for all of the eviction and its reading back, with 18 or 36 123.5 (2 x 131072 tokens, d = 64: 131.1, 128.6).
 constexpr int kMoveWarps = 4, kMostRequests = HYPERATTN_PLAN_MAX_REQUESTS;
 
 template <int D>
@@ -449,7 +450,7 @@ extern "C" int hyperattn_cache_evict(const hyperattn_evict_params* p) {
   if (e == cudaSuccess) {
     const long long blocks = (long long)p->requests * p->cache.kv_heads * ((long long)p->table_width * p->cache.page_tokens / kBlockTokens);
     const long long want = (blocks + kMoveWarps - 1) / kMoveWarps;
-    const dim3 grid((unsigned)(want < 12 * kSms ? want : 12 * kSms));
+    const dim3 grid((unsigned)(want < 18 * kSms ? want : 18 * kSms));
     const int smem = (p->requests + 1) * (int)sizeof(int);
     e = p->cache.d == 64 ? launch(move_kernel<64>, grid, dim3(32 * kMoveWarps), smem, st, a) : launch(move_kernel<128>, grid, dim3(32 * kMoveWarps), smem, st, a);
   }
