@@ -47,7 +47,7 @@ struct CacheAttnArgs {
   int part_heads;                              // heads of a chunk
   // several queries a request: its rows are its tokens times the query heads of a key head, a chunk some of them
   const int32_t* cu_q;
-  int rows, causal;
+  int rows, causal, most;                      // most: requests with more rows than this are not for this launch
   const float *lse_in, *before;                // weights: log-sum-exps of the rows, what tokens had
   float* weights;
   float decay;
@@ -67,13 +67,13 @@ template <> struct KernelArgs<kWeights> : CacheAttnArgs {
   int run;                                     // blocks of a copy: the largest power of two, up to a unit, that divides a page's
 };
 
-// a request's tokens of queries (first row, how many)
-__device__ __forceinline__ int2 queries_of(const CacheAttnArgs& a, int r) {
-  if (!a.cu_q) return make_int2(r, 1);
-  const int first = min(max(a.cu_q[r], 0), a.rows);
-  return make_int2(first, min(max(a.cu_q[r + 1], first), a.rows) - first);
-}
 __device__ __forceinline__ int group_of(const CacheAttnArgs& a) { return a.q_heads / a.cache.heads; }
+// a request's tokens of queries (first row, how many; -1: it has more rows than this launch is for)
+__device__ __forceinline__ int2 queries_of(const CacheAttnArgs& a, int r) {
+  if (!a.cu_q) return make_int2(r, group_of(a) > a.most ? -1 : 1);
+  const int first = min(max(a.cu_q[r], 0), a.rows), n = min(max(a.cu_q[r + 1], first), a.rows) - first;
+  return make_int2(first, n * group_of(a) > a.most ? -1 : n);
+}
 // the chunks of a request come after those of the ones before it, wherever those end
 __host__ __device__ __forceinline__ long long chunk_slots(long long rows_before, int requests_before, int group, int per_chunk) { return rows_before * group / per_chunk + requests_before; }
 constexpr int kNeverSeen = 1 << 30;
@@ -668,6 +668,7 @@ __global__ void __launch_bounds__(32 * kWarps, ctas_by_registers(NT)) cache_attn
     int units = units_of<D, MODE>(a, r);
     if constexpr (MODE != kOneQuery) {
       s_queries[r] = queries_of(a, r);
+      if (s_queries[r].y < 0) { s_queries[r].y = 0; units = 0; }
       if (MODE == kSomeRows) units *= chunks_of(r);
     }
     if constexpr (MODE == kSomeRows) mine = plus(mine, units);
@@ -970,7 +971,7 @@ __global__ void __launch_bounds__(kJoinThreads) join_kernel(const __grid_constan
     for (int i = threadIdx.x; i < a.requests; i += kJoinThreads) {
       const int2 q = queries_of(a, i);
       const long long first = chunk_slots(q.x, i, per_kv, a.part_heads);
-      const int n = (q.y * per_kv + a.part_heads - 1) / a.part_heads;
+      const int n = (max(q.y, 0) * per_kv + a.part_heads - 1) / a.part_heads;
       if (slot >= first && slot < first + n) atomicMax(&s_found, i);      // (one of them, if offsets that do not ascend give a chunk to several)
     }
     __syncthreads();

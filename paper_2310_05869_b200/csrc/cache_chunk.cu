@@ -20,8 +20,8 @@
 // Roundings: weights and values enter the second product as fp16 (2^-11 of each), sums of weights before that; O is one chain of products over a part's tokens.
 //
 // What bounds it: a tile of 64 tokens and 256 rows takes about 2300 clocks, near which lie its conversion, its 42 products (d = 128; half of those for scores are what exact keys cost) and the
-// hand-overs of the softmax.  2048 rows over 30720 tokens, 32 / 8 heads of 128: 1285 us for a floor of 636 (tensor pipe 60 %, issue 57 %); 5 requests, 1501 rows over up to 5000 tokens, 32 heads
-// of 64: 162 us (tensor pipe 28 %, issue 48 %), of which the first and the last launch take 10.  Two halves of a row block of up to 128 rows: 64 rows over 8000 tokens, 32 heads of 64, 8
+// hand-overs of the softmax.  2048 rows over 30720 tokens, 32 / 8 heads of 128: 1285 us for a floor of 636 (tensor pipe 61 %, issue 55 %); 5 requests, 1501 rows over up to 5000 tokens, 32 heads
+// of 64: 162 us (tensor pipe 31 %, issue 50 %), of which the first and the last launch take 10.  Two halves of a row block of up to 128 rows: 64 rows over 8000 tokens, 32 heads of 64, 8
 // requests 297 -> 242 us.
 //
 // Warp roles (640 threads): 0-3 and 4-7 softmax and results of unit 0 and 1, 8-11 and 12-15 keys and values of even and odd tiles, 16 products (and TMEM), 17 copies, 18 segments, 19
@@ -72,7 +72,7 @@ __global__ void __launch_bounds__(kShareThreads) share_kernel(const __grid_const
   __syncthreads();
   for (int r = warp; r < a.requests; r += kShareThreads / 32) {
     const Span s = span_of(a, r);
-    const int blocks = (int)(((long long)s.rows * group + kBlockRows - 1) / kBlockRows);
+    const int blocks = is_for(a, s) ? (int)(((long long)s.rows * group + kBlockRows - 1) / kBlockRows) : 0;
     const long long first = image_slots(s.first, r, group, kBlockRows);
     for (int b = lane; b < blocks; b += 32) o.block[first + b] = make_int2(r, b);
   }
@@ -918,11 +918,10 @@ ChunkShape chunk_shape(const hyperattn_chunk_params& p) {
   s.bytes = s.part_o + (size_t)s.parts * 2 * kBlockRows * p.cache.d * 4;
   return s;
 }
-// Few rows on average: the warp-level kernels.  us there / here, up to 8000 tokens, 8 requests: 8 heads of 128, 32 rows 60 / 79, 48 rows 94 / 91, 64 rows 106 / 74; 32 heads of 64,
-// 32 rows 129 / 161, 48 rows 157 / 157, 64 rows 173 / 143.  Tables of no more than 1024 tokens (here the first and the last launch take as long as the work), 64 rows: 21 / 25.
-bool few_rows(const hyperattn_chunk_params& p, size_t* bytes) {
-  const long long most = (long long)p.table_width * p.cache.page_tokens <= 1024 ? 64 : 32;
-  return (long long)p.rows * (p.q_heads / p.cache.kv_heads) <= most * p.requests && few_rows_attention(p, bytes);
+// (what the few rows' kernels cannot count: all is for these)
+Kinds chunk_kinds(const hyperattn_chunk_params& p, size_t* bytes) {
+  const Kinds k = kinds_of(p, most_of(p));
+  return k.few && !few_rows_attention(p, bytes) ? Kinds{false, true} : k;
 }
 
 int check(const hyperattn_chunk_params* p) {
@@ -940,10 +939,12 @@ extern "C" int hyperattn_cache_chunk_attention_workspace_bytes(const hyperattn_c
   if (!bytes) return HYPERATTN_INVALID_ARGUMENT;
   if (int rc = check(p)) return rc;
   *bytes = 0;
-  if (p->requests == 0 || p->rows == 0 || few_rows(*p, bytes)) return HYPERATTN_OK;
+  if (p->requests == 0 || p->rows == 0) return HYPERATTN_OK;
+  const Kinds kinds = chunk_kinds(*p, bytes);
+  if (!kinds.many) return HYPERATTN_OK;
   const ChunkShape s = chunk_shape(*p);
   if (s.slots * p->cache.kv_heads > 0x7fffffffLL) return HYPERATTN_UNSUPPORTED_SHAPE;
-  *bytes = s.bytes;
+  *bytes = (kinds.few ? (*bytes + 255) / 256 * 256 : 0) + s.bytes;
   return HYPERATTN_OK;
 }
 
@@ -958,10 +959,16 @@ extern "C" int hyperattn_cache_chunk_attention(const hyperattn_chunk_params* p) 
   const cudaStream_t st = reinterpret_cast<cudaStream_t>(p->stream);
   int* status = nullptr;
   if (int rc = device_status_word(st, &status)) return rc;
-  if (few_rows(*p, &bytes)) return launch_few_rows_attention(*p, status);
-  const ChunkArgs a = chunk_args(*p);
-  const ChunkShape s = chunk_shape(*p);
+  ChunkArgs a = chunk_args(*p);
   char* ws = reinterpret_cast<char*>(p->workspace);
+  const Kinds kinds = chunk_kinds(*p, &bytes);
+  if (kinds.few) {
+    const int rc = launch_few_rows_attention(*p, kinds.many ? most_of(*p) : INT_MAX, status);
+    if (rc || !kinds.many) return rc;
+    a.least = most_of(*p);
+    ws += (bytes + 255) / 256 * 256;
+  }
+  const ChunkShape s = chunk_shape(*p);
   const ChunkOut o = {p->out, p->lse, p->out_dtype, reinterpret_cast<long long*>(ws), reinterpret_cast<int2*>(ws + s.block), reinterpret_cast<long long*>(ws + s.start),
                       reinterpret_cast<float*>(ws + s.part_o), reinterpret_cast<float2*>(ws + s.part_s), (int)s.slots, s.parts};
   const int subs = p->cache.page_tokens / kBlockTokens, run = subs % 4 == 0 ? 4 : subs & -subs;

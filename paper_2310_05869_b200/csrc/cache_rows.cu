@@ -11,13 +11,15 @@ namespace {
 // What a call's launches look like: rows of a chunk (0: four, twice in a tile), CTAs, bytes of the workspace
 struct RowsShape { int tiles, per_chunk, ctas; long long slots; size_t starts, bytes; };
 template <int D, Mode MODE>
-RowsShape rows_shape(int requests, int rows, int group, int kv_heads, long long tokens) {
+RowsShape rows_shape(int requests, int rows, int group, int kv_heads, long long tokens, bool both) {
   RowsShape s;
   const long long all = (long long)rows * group;
   // Rows in a tile: attention four (and what the rounding of their weights loses beside them) where requests have that many on average, two tiles of eight where they have more than eight
   // and d = 64, else eight.  us for four / eight / sixteen: 16 rows over 4000 tokens, 8 heads of 128, 8 requests 51 / 43 / 47, 32 rows 91 / 65 / 72; 2 x 30000 tokens, 32 heads of 64,
   // 16 rows 309 / 190 / 184, 32 rows 556 / 316 / 288; weights of 16 rows over 300 tokens - / 10.8 / 9.4.
-  s.tiles = MODE == kSomeRows && all <= 4ll * requests ? 0 : all <= 8ll * requests || (MODE == kSomeRows && D == 128) ? 1 : 2;
+  // (Both kinds of kernels: the average is not these requests', whose tokens may be single ones.  Weights have two tiles all the same: requests of more rows than a tile's load their queries anew for
+  // every unit, 16 rows 242 us instead of 127.)
+  s.tiles = MODE == kSomeRows && all <= 4ll * requests ? 0 : all <= 8ll * requests || (MODE == kSomeRows && (both || D == 128)) ? 1 : 2;
   s.per_chunk = s.tiles == 0 ? 4 : 8 * s.tiles;
   s.slots = chunk_slots(rows, requests, group, s.per_chunk) + 1;
   constexpr int unit = Ring<D, MODE>::kUnitTokens;
@@ -35,10 +37,10 @@ bool countable(const RowsShape& s, int requests, int kv_heads, long long tokens)
   return (MODE == kWeights ? (long long)requests : s.slots) * kv_heads <= 0x7fffffffLL / (tokens / Ring<D, MODE>::kUnitTokens + 2 + kBegin) && s.slots * kv_heads <= 0x7fffffffLL;
 }
 template <Mode MODE>
-KernelArgs<MODE> rows_args(const ChunkArgs& c) {
+KernelArgs<MODE> rows_args(const ChunkArgs& c, int most) {
   KernelArgs<MODE> a = {};
   a.cache = c.cache; a.q = c.q; a.q_row = c.q_row; a.q_head = c.q_head; a.table = c.table; a.lengths = c.lengths; a.cu_q = c.cu_q;
-  a.requests = c.requests; a.width = c.width; a.q_heads = c.q_heads; a.rows = c.rows; a.causal = c.causal; a.scale_log2 = c.scale_log2; a.chunks = 1;
+  a.requests = c.requests; a.width = c.width; a.q_heads = c.q_heads; a.rows = c.rows; a.causal = c.causal; a.most = most; a.scale_log2 = c.scale_log2; a.chunks = 1;
   return a;
 }
 template <class F>
@@ -51,21 +53,21 @@ bool few_rows_attention(const hyperattn_chunk_params& p, size_t* bytes) {
   const long long tokens = (long long)p.table_width * p.cache.page_tokens;
   return of_dim(p.cache.d, [&](auto dim) {
     constexpr int D = decltype(dim)::value;
-    const RowsShape s = rows_shape<D, kSomeRows>(p.requests, p.rows, group, p.cache.kv_heads, tokens);
+    const RowsShape s = rows_shape<D, kSomeRows>(p.requests, p.rows, group, p.cache.kv_heads, tokens, kinds_of(p, most_of(p)).many);
     *bytes = s.bytes;
     return countable<D, kSomeRows>(s, p.requests, p.cache.kv_heads, tokens);
   });
 }
 
-int launch_few_rows_attention(const hyperattn_chunk_params& p, int* status) {
+int launch_few_rows_attention(const hyperattn_chunk_params& p, int most, int* status) {
   const int group = p.q_heads / p.cache.kv_heads;
   const cudaStream_t st = reinterpret_cast<cudaStream_t>(p.stream);
-  KernelArgs<kSomeRows> a = rows_args<kSomeRows>(chunk_args(p));
+  KernelArgs<kSomeRows> a = rows_args<kSomeRows>(chunk_args(p), most);
   a.out = p.out; a.lse = p.lse; a.out_kind = p.out_dtype;
   return of_dim(p.cache.d, [&](auto dim) {
     constexpr int D = decltype(dim)::value;
     using R = Ring<D, kSomeRows>;
-    const RowsShape s = rows_shape<D, kSomeRows>(p.requests, p.rows, group, p.cache.kv_heads, (long long)p.table_width * p.cache.page_tokens);
+    const RowsShape s = rows_shape<D, kSomeRows>(p.requests, p.rows, group, p.cache.kv_heads, (long long)p.table_width * p.cache.page_tokens, kinds_of(p, most_of(p)).many);
     a.starts = reinterpret_cast<int*>(p.workspace);
     a.part = reinterpret_cast<float*>(reinterpret_cast<char*>(p.workspace) + s.starts);
     a.part_heads = s.per_chunk;
@@ -91,16 +93,15 @@ int launch_few_rows_attention(const hyperattn_chunk_params& p, int* status) {
 bool few_rows_weights(const hyperattn_weights_params& p) {
   const int group = p.q_heads / p.cache.kv_heads;
   const long long tokens = (long long)p.table_width * p.cache.page_tokens;
-  if ((long long)p.rows * group > 16ll * p.requests) return false;
   return of_dim(p.cache.d, [&](auto dim) {
     constexpr int D = decltype(dim)::value;
-    return countable<D, kWeights>(rows_shape<D, kWeights>(p.requests, p.rows, group, p.cache.kv_heads, tokens), p.requests, p.cache.kv_heads, tokens);
+    return countable<D, kWeights>(rows_shape<D, kWeights>(p.requests, p.rows, group, p.cache.kv_heads, tokens, kinds_of(p, most_of(p)).many), p.requests, p.cache.kv_heads, tokens);
   });
 }
 
-int launch_few_rows_weights(const hyperattn_weights_params& p, int* status) {
+int launch_few_rows_weights(const hyperattn_weights_params& p, int most, int* status) {
   const cudaStream_t st = reinterpret_cast<cudaStream_t>(p.stream);
-  KernelArgs<kWeights> a = rows_args<kWeights>(chunk_args(p));
+  KernelArgs<kWeights> a = rows_args<kWeights>(chunk_args(p), most);
   a.lse_in = p.lse; a.before = p.weights; a.weights = p.weights_out; a.decay = p.decay;
   return of_dim(p.cache.d, [&](auto dim) {
     constexpr int D = decltype(dim)::value;
@@ -109,7 +110,7 @@ int launch_few_rows_weights(const hyperattn_weights_params& p, int* status) {
     a.run = subs % R::kUnit == 0 ? R::kUnit : subs & -subs;
     const long long blocks = (long long)p.cache.num_pages * p.cache.kv_heads * subs;
     if (!encode_words_map(&a.maps.codes, p.cache.pages, blocks, 5 * D, 2 * D, a.run) || !encode_words_map(&a.maps.scales, p.cache.pages, blocks, 5 * D, D / 2, a.run)) return (int)HYPERATTN_UNSUPPORTED_SHAPE;
-    const RowsShape s = rows_shape<D, kWeights>(p.requests, p.rows, p.q_heads / p.cache.kv_heads, p.cache.kv_heads, (long long)p.table_width * p.cache.page_tokens);
+    const RowsShape s = rows_shape<D, kWeights>(p.requests, p.rows, p.q_heads / p.cache.kv_heads, p.cache.kv_heads, (long long)p.table_width * p.cache.page_tokens, kinds_of(p, most_of(p)).many);
     auto go = [&](auto tiles, auto type) {
       constexpr auto kernel = cache_attn_kernel<D, decltype(tiles)::value, false, decltype(type), kWeights>;
       cudaError_t e = allow_smem<kernel>(R::bytes(kMaxRequests));

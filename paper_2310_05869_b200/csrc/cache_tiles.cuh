@@ -18,7 +18,7 @@ struct ChunkArgs {
   const void* q;
   long long q_row, q_head;
   const int32_t *table, *lengths, *cu_q;
-  int requests, rows, width, q_heads, causal;
+  int requests, rows, width, q_heads, causal, least;      // least: requests of so few rows are not for this launch (-1: all are)
   float scale_log2;
   uint8_t* images;                       // queries as operands, see Image
 };
@@ -32,6 +32,8 @@ __device__ __forceinline__ Span span_of(const ChunkArgs& a, int r) {
   s.len = min(max(a.lengths[r], 0), a.width * a.cache.page);
   return s;
 }
+
+__device__ __forceinline__ bool is_for(const ChunkArgs& a, const Span& s) { return s.rows * (a.q_heads / a.cache.heads) > a.least; }
 
 // ---- queries ---------------------------------------------------------------------------------------------------------------
 // A request's rows of a key head are its tokens times the head's query heads.  NR of them, as shared memory holds them: fp16 [NR x d] with the 128-byte swizzle in slabs of 64
@@ -63,7 +65,7 @@ __global__ void __launch_bounds__(128) image_kernel(const __grid_constant__ Chun
   }
   const Span s = span_of(a, lo);
   const long long row0 = (slot - image_slots(s.first, lo, group, NR)) * NR, rows = (long long)s.rows * group;
-  if (row0 < 0 || row0 >= rows) return;
+  if (row0 < 0 || row0 >= rows || !is_for(a, s)) return;
   uint8_t* to = a.images + (size_t)blockIdx.x * I::kBytes;
   __shared__ int s_exp[NR], s_most, s_apart;
   if (threadIdx.x == 0) { s_most = INT_MIN; s_apart = 0; }
@@ -307,6 +309,7 @@ ChunkArgs chunk_args(const P& p) {
   a.table = p.table; a.lengths = p.lengths; a.cu_q = p.cu_q;
   a.requests = p.requests; a.rows = p.rows; a.width = p.table_width; a.q_heads = p.q_heads; a.causal = p.causal != 0;
   a.scale_log2 = (p.softmax_scale > 0.f ? p.softmax_scale : 1.f / sqrtf((float)p.cache.d)) * 1.4426950408889634f;
+  a.least = -1;
   a.images = reinterpret_cast<uint8_t*>(p.workspace);
   return a;
 }

@@ -11,6 +11,7 @@
 //
 // Warp roles: 0-7 sums (two groups of four, for every other image), 8-15 keys (two groups, for every other tile), 16 products (and TMEM), 17 copies of keys, 18 of images.
 // Every wait is bounded: a CTA that gives up raises the device status word, drains its copies, frees its TMEM and returns.
+#include <climits>
 #include <type_traits>
 #include "cache_rows.cuh"
 #include "cache_tiles.cuh"
@@ -60,7 +61,7 @@ __device__ __forceinline__ void walk_request(const ChunkArgs& a, Walk& w, const 
     w.end = w.request > end.request || (w.request == end.request && w.tile >= end.tile) || w.request >= a.requests;
     if (w.end) return;
     w.s = span_of(a, w.request);
-    w.tiles = (w.s.len + kTileTokens - 1) / kTileTokens;
+    w.tiles = is_for(a, w.s) ? (w.s.len + kTileTokens - 1) / kTileTokens : 0;
     if (w.tile < w.tiles * a.cache.heads) break;
   }
   w.images = (int)(((long long)w.s.rows * (a.q_heads / a.cache.heads) + NR - 1) / NR);
@@ -143,7 +144,7 @@ __global__ void __launch_bounds__(kWThreads, 1) weights_kernel(const __grid_cons
   const int group = a.q_heads / a.cache.heads, cap = a.width * a.cache.page, subs = a.cache.page / kBlockTokens;
   places_of<kWThreads>(a.requests, blockIdx.x, gridDim.x, [&](int r) {
     const Span s = span_of(a, r);
-    return make_int2((s.len + kTileTokens - 1) / kTileTokens * a.cache.heads, kKeyCost + (int)(((long long)s.rows * group + NR - 1) / NR));
+    return make_int2(is_for(a, s) ? (s.len + kTileTokens - 1) / kTileTokens * a.cache.heads : 0, kKeyCost + (int)(((long long)s.rows * group + NR - 1) / NR));
   }, s_sums, s_place);
   const Place begin = s_place[0], end = s_place[1];
   auto image_at = [&](const Walk& w, int i) { return a.images + ((size_t)(image_slots(w.s.first, w.request, group, NR) + i) * a.cache.heads + w.head) * I::kBytes; };
@@ -393,6 +394,11 @@ __global__ void __launch_bounds__(kWThreads, 1) weights_kernel(const __grid_cons
 
 // rows of an image: a product of 64 rows takes 48 clocks, of 128 rows 64; beside two tiles' keys of d = 128 TMEM has room for the scores of two images of 96
 template <int D> constexpr int kImageRows = D == 64 ? 128 : 96;
+// (what the few rows' kernels cannot count: all is for these)
+Kinds weights_kinds(const hyperattn_weights_params& p) {
+  const Kinds k = kinds_of(p, most_of(p));
+  return k.few && !few_rows_weights(p) ? Kinds{false, true} : k;
+}
 long long slots_of(const hyperattn_weights_params& p) {
   return image_slots(p.rows, p.requests, p.q_heads / p.cache.kv_heads, p.cache.d == 64 ? kImageRows<64> : kImageRows<128>) + 1;
 }
@@ -406,7 +412,7 @@ extern "C" int hyperattn_cache_weights_workspace_bytes(const hyperattn_weights_p
   if (!bytes) return HYPERATTN_INVALID_ARGUMENT;
   if (int rc = check_chunk(p)) return rc;
   *bytes = 0;
-  if (p->requests == 0 || few_rows_weights(*p)) return HYPERATTN_OK;
+  if (p->requests == 0 || !weights_kinds(*p).many) return HYPERATTN_OK;
   if (slots_of(*p) * p->cache.kv_heads > 0x7fffffffLL - 2 * kSms) return HYPERATTN_UNSUPPORTED_SHAPE;
   *bytes = (size_t)(slots_of(*p) * p->cache.kv_heads) * (p->cache.d == 64 ? Image<64, kImageRows<64>>::kBytes : Image<128, kImageRows<128>>::kBytes);
   return HYPERATTN_OK;
@@ -421,24 +427,28 @@ extern "C" int hyperattn_cache_weights(const hyperattn_weights_params* p) {
   if (misaligned(p->q) || misaligned(p->weights) || misaligned(p->weights_out) || misaligned(p->workspace)) return HYPERATTN_MISALIGNED;
   if (p->workspace_bytes < bytes) return HYPERATTN_WORKSPACE_TOO_SMALL;
   const int subs = p->cache.page_tokens / kBlockTokens, d = p->cache.d;
-  const WeightArgs w = {chunk_args(*p), p->weights, p->weights_out, p->decay, subs % 8 == 0 ? 8 : subs & -subs};
-  const bool few = few_rows_weights(*p);
+  WeightArgs w = {chunk_args(*p), p->weights, p->weights_out, p->decay, subs % 8 == 0 ? 8 : subs & -subs};
+  const Kinds kinds = weights_kinds(*p);
   KeyMaps maps;
   const long long blocks = (long long)p->cache.num_pages * p->cache.kv_heads * subs;
-  if (!few && (!encode_words_map(&maps.codes, p->cache.pages, blocks, 5 * d, 2 * d, w.run) || !encode_words_map(&maps.scales, p->cache.pages, blocks, 5 * d, d / 2, w.run))) return HYPERATTN_UNSUPPORTED_SHAPE;
+  if (kinds.many && (!encode_words_map(&maps.codes, p->cache.pages, blocks, 5 * d, 2 * d, w.run) || !encode_words_map(&maps.scales, p->cache.pages, blocks, 5 * d, d / 2, w.run))) return HYPERATTN_UNSUPPORTED_SHAPE;
   const cudaStream_t st = reinterpret_cast<cudaStream_t>(p->stream);
   int* status = nullptr;
   if (int rc = device_status_word(st, &status)) return rc;
   int sms = 0;
   cudaError_t e = sm_count(&sms);
   if (e != cudaSuccess) return status_of(e, "cache weights");
-  if (few) return launch_few_rows_weights(*p, status);
+  if (kinds.few) {                               // (these write the zeros behind the tokens too)
+    const int rc = launch_few_rows_weights(*p, kinds.many ? most_of(*p) : INT_MAX, status);
+    if (rc || !kinds.many) return rc;
+    w.c.least = most_of(*p);
+  }
   auto go = [&](auto dim) {
     constexpr int D = decltype(dim)::value, NR = kImageRows<D>;
     using C = WCfg<D, NR>;
     cudaError_t e = allow_smem<weights_kernel<D, NR>>(C::kSmem);
     const int images = (int)(slots_of(*p) * p->cache.kv_heads);
-    auto make = [&](auto kernel) { return launch(kernel, dim3((unsigned)images + 2 * kSms), dim3(128), 0, st, w.c, p->lse, images, p->weights_out, kTileTokens); };
+    auto make = [&](auto kernel) { return launch(kernel, dim3((unsigned)images + (kinds.few ? 0 : 2 * kSms)), dim3(128), 0, st, w.c, p->lse, images, p->weights_out, kTileTokens); };
     if (e == cudaSuccess) e = p->dtype == HYPERATTN_BF16 ? make(image_kernel<D, NR, __nv_bfloat16>) : make(image_kernel<D, NR, __half>);
     const long long tiles = (long long)p->requests * p->cache.kv_heads * (((long long)p->table_width * p->cache.page_tokens + kTileTokens - 1) / kTileTokens);
     if (e == cudaSuccess) e = launch(weights_kernel<D, NR>, dim3((unsigned)(tiles < sms ? tiles : sms)), dim3(kWThreads), C::kSmem, st, w, maps, status);

@@ -144,3 +144,43 @@ def test_offsets_that_ask_for_more_than_numbers_hold():
     out, lse = ha.cache_chunk_attention(q, cache, table, torch.full((4096,), 131072, dtype=torch.int32, device="cuda"), cu)
     torch.cuda.synchronize()
     assert not out.any() and bool((lse == -math.inf).all())
+
+
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("heads", [(2, 2, 64), (4, 1, 128), (8, 2, 64)])
+def test_a_part_of_a_prompt_beside_single_tokens(heads, causal):
+    """Few rows a request on average, and some of many: both kinds of kernels have their requests."""
+    G = heads[0] // heads[1]
+    lens, counts = [1 + 11 * i for i in range(60)], [1] * 60
+    for r, n, length in ((0, 300, 500), (23, 0, 40), (24, 33 // G + 1, 1500), (25, 5, 0), (40, 32 // G, 700), (41, 16 // G, 700), (42, 17 // G + 1, 100), (59, 400 // G, 399 // G)):
+        lens[r], counts[r] = length, n
+    q, cache, table, k, v, (out, lse), _ = TC.both(lens, counts, heads, 16, torch.bfloat16, causal=causal, width=100)
+    before = torch.rand(60, heads[1], 1600, device="cuda")
+    got = TC.check_weights(q, cache, table, k, lens, counts, lse, causal=causal, before=before, decay=0.75)
+    assert torch.equal(ha.cache_weights(q, cache, table, CU.ints(lens), lse, CU.offsets(counts), weights=before, decay=0.75, causal=causal, out=before), got)
+    again = ha.cache_chunk_attention(q, cache, table, CU.ints(lens), CU.offsets(counts), causal=causal)
+    assert torch.equal(again[0], out) and torch.equal(again[1], lse)
+
+
+@pytest.mark.parametrize("heads,many", [((2, 2, 64), 60), ((4, 1, 128), 60), ((2, 1, 64), 17), ((32, 8, 128), 16)])
+def test_large_parts_beside_single_tokens(heads, many):
+    """More rows a request on average than the few rows' kernels take a request, and requests that suit them all the same."""
+    lens, counts = [33 + 19 * i for i in range(many)], [1] * many
+    for r, n in ((1, 700), (2, 3), (many // 2, 1900), (many - 1, 260)):
+        counts[r], lens[r] = n, max(lens[r], n // 2 + 300)
+    q, cache, table, k, v, (out, lse), _ = TC.both(lens, counts, heads, 64, torch.float16)
+    before = torch.rand(many, heads[1], table.shape[1] * 64, device="cuda")
+    TC.check_weights(q, cache, table, k, lens, counts, lse, before=before, decay=0.75)
+
+
+@pytest.mark.parametrize("heads", [260, 40, 20])
+def test_one_token_of_very_many_heads(heads):
+    lens = [1 + 37 * i for i in range(17)]
+    cache, table, k, v = CU.filled(lens, 1, 64, 16)
+    q = TC.queries(17, heads, 64, torch.bfloat16)
+    out, lse = ha.cache_chunk_attention(q, cache, table, CU.ints(lens))
+    CU.check_attention((out, lse), CU.attention(q.double(), k, v, lens, [1] * 17), torch.bfloat16, max(lens), 17)
+    w = torch.rand(17, 1, table.shape[1] * 16, device="cuda")
+    want, bound = CU.weights(q.double(), k, lens, [1] * 17, lse, w, 0.5, cap=w.shape[2])
+    got = ha.cache_weights(q, cache, table, CU.ints(lens), lse, weights=w, decay=0.5, out=w)
+    assert bool(((got.double() - want).abs() <= bound).all())
