@@ -861,8 +861,7 @@ __global__ void __launch_bounds__(kPutThreads) put_kernel(const __grid_constant_
   if (b.x < 0) return;
   const Span s = span_of(a, b.x);
   const RowBlock k = row_block(a, s, b.y);
-  const int row0 = blockIdx.y * kPutRows<D>;
-  if (row0 >= k.rows) return;
+  if ((int)blockIdx.y * kPutRows<D> >= k.rows) return;
   const long long whole = (long long)k.tiles * k.cost, first = o.before[slot] + kv * whole, last = first + whole;
   int p0 = 0, p1 = 0;                                  // its first and last part
   if (k.tiles > 0) {
@@ -876,8 +875,8 @@ __global__ void __launch_bounds__(kPutThreads) put_kernel(const __grid_constant_
     if (p0 == p1) return;                              // finished there
   }
   constexpr int LANES = D / 4;
-  const int lane = tid % LANES, row = row0 + tid / LANES;
-  if (row < k.rows) {
+  const int lane = tid % LANES;
+  for (int row = blockIdx.y * kPutRows<D> + tid / LANES; row < k.rows; row += gridDim.y * kPutRows<D>) {
     float ref = -INFINITY, sum = 0.f;
     float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
     if (k.tiles > 0)
@@ -978,7 +977,9 @@ extern "C" int hyperattn_cache_chunk_attention(const hyperattn_chunk_params* p) 
     cudaError_t e = allow_smem<chunk_kernel<D, T>>(CCfg<D>::kSmem);
     if (e == cudaSuccess) e = launch(share_kernel, dim3(1), dim3(kShareThreads), 0, st, a, o);
     if (e == cudaSuccess) e = launch(chunk_kernel<D, T>, dim3((unsigned)s.parts), dim3(kCThreads), CCfg<D>::kSmem, st, a, o, run, status);
-    if (e == cudaSuccess) e = launch(put_kernel<D, T>, dim3((unsigned)(s.slots * p->cache.kv_heads), kBlockRows / kPutRows<D>), dim3(kPutThreads), 0, st, a, o);
+    // (as many CTAs as the GPU holds several times over, at most: 64 requests of few rows, 8 heads, had 17 664, most with nothing to do)
+    const long long blocks = s.slots * p->cache.kv_heads, most = kBlockRows / kPutRows<D>, want = (32 * kSms + blocks - 1) / blocks;
+    if (e == cudaSuccess) e = launch(put_kernel<D, T>, dim3((unsigned)blocks, (unsigned)(want < most ? want : most)), dim3(kPutThreads), 0, st, a, o);
     return status_of(e, "chunk attention");
   };
   auto of_type = [&](auto dim) { return p->dtype == HYPERATTN_BF16 ? go(dim, __nv_bfloat16()) : go(dim, __half()); };
