@@ -17,11 +17,13 @@
 // The tiles of all segments are one sequence, cut into equal parts, one for each CTA (a first launch of one CTA finds the cuts); pieces of segments that lie in several parts
 // go to the workspace, and a last launch puts them together, in order.
 //
-// Roundings: weights and values enter the second product as fp16 (2^-11 of each), sums of weights before that; O is one chain of products over a part's tokens.
+// Roundings: weights and values enter the second product as fp16 (2^-11 of each), sums of weights before that; O is one chain of products over a part's tokens.  With fp16 queries what the weights'
+// rounding has lost goes through the product too (results off by 2.8e-4 instead of 3.5e-4 of their size, where rounding them alone is 2.1e-4; 5 requests, 1501 rows 161 -> 200 us; bf16 results,
+// 1.7e-3, do not show it).
 //
 // What bounds it: a tile of 64 tokens and 256 rows takes about 2300 clocks, near which lie its conversion, its 42 products (d = 128; half of those for scores are what exact keys cost) and the
 // hand-overs of the softmax.  2048 rows over 30720 tokens, 32 / 8 heads of 128: 1285 us for a floor of 636 (tensor pipe 61 %, issue 55 %); 5 requests, 1501 rows over up to 5000 tokens, 32 heads
-// of 64: 162 us (tensor pipe 31 %, issue 50 %), of which the first and the last launch take 10.  Two halves of a row block of up to 128 rows: 64 rows over 8000 tokens, 32 heads of 64, 8
+// of 64, fp16: 200 us (with single weights 162: tensor pipe 31 %, issue 50 %), of which the first and the last launch take 10.  Two halves of a row block of up to 128 rows: 64 rows over 8000 tokens, 32 heads of 64, 8
 // requests 297 -> 242 us.
 //
 // Warp roles (640 threads): 0-3 and 4-7 softmax and results of unit 0 and 1, 8-11 and 12-15 keys and values of even and odd tiles, 16 products (and TMEM), 17 copies, 18 segments, 19
@@ -125,7 +127,8 @@ struct CCfg {
   // TMEM columns: O_0, O_1, Q_0, Q_1, S_0, S_1; at d = 64 P_i beside S_i, so that the next scores do not wait for this tile's weights
   static constexpr bool kOwnP = D == 64;
   static constexpr uint32_t kColQ = 2 * D, kColS = 3 * D;
-  __host__ __device__ static constexpr uint32_t col_p(int i) { return kOwnP ? kColS + 2 * kKeys + (kKeys / 2) * i : kColS + kKeys * i; }
+  __host__ __device__ static constexpr uint32_t col_p(int i) { return kColS + (kOwnP ? 2 * kKeys : 0) + kKeys * i; }
+  static constexpr uint32_t kRest = kKeys / 2;                                   // (from P on: what its rounding has lost)
 };
 
 struct Piece {                           // of a segment, in a CTA's part
@@ -146,6 +149,8 @@ __global__ void __launch_bounds__(kCThreads, 1) chunk_kernel(const __grid_consta
   using C = CCfg<D>;
   using B = Block<D>;
   constexpr int G = D / kGroup, NS = C::kStages, NRAW = C::kRawStages;
+  constexpr bool FINE = std::is_same<T, __half>::value;
+  constexpr int kAtOnce = FINE ? 16 : 32;        // weights that go to TMEM at a time (their number and the scores, which may be needed once more, are what registers hold)
   extern __shared__ uint8_t smem_[];
   uint8_t* smem = smem_ + (1024 - (smem_u32(smem_) & 1023)) % 1024;
   const uint32_t ubase = smem_u32(smem);
@@ -359,19 +364,27 @@ __global__ void __launch_bounds__(kCThreads, 1) chunk_kernel(const __grid_consta
             const uint64_t off2 = pack_f2(off, off);
             uint64_t tile2 = 0;
 #pragma unroll
-            for (int c = 0; c < 2; ++c) {
-              uint32_t p[16];
+            for (int c = 0; c < 64 / kAtOnce; ++c) {
+              uint32_t p[kAtOnce / 2], rest[kAtOnce / 2];
 #pragma unroll
-              for (int e = 0; e < 16; ++e) {
-                const uint64_t x2 = ffma2(pack_u2(r[c][2 * e], r[c][2 * e + 1]), sc2, off2);
+              for (int e = 0; e < kAtOnce / 2; ++e) {
+                const int at = kAtOnce * c + 2 * e;
+                const uint64_t x2 = ffma2(pack_u2(r[at / 32][at % 32], r[at / 32][at % 32 + 1]), sc2, off2);
                 float x, y;
                 unpack_f2(x2, x, y);
                 x = ex2(x);
                 y = ex2(y);
                 tile2 = fadd2(tile2, pack_f2(x, y));
                 p[e] = from_float2<__half>(x, y);
+                if constexpr (FINE) {
+                  const float2 r2 = to_float2<__half>(p[e]);
+                  rest[e] = from_float2<__half>(x - r2.x, y - r2.y);
+                }
               }
-              tmem_st16(pcol + 16 * c, p);
+              if constexpr (FINE) {
+                tmem_st8(pcol + kAtOnce / 2 * c, p);
+                tmem_st8(pcol + C::kRest + kAtOnce / 2 * c, rest);
+              } else tmem_st16(pcol + kAtOnce / 2 * c, p);
             }
             float t0, t1;
             unpack_f2(tile2, t0, t1);
@@ -678,6 +691,10 @@ __global__ void __launch_bounds__(kCThreads, 1) chunk_kernel(const __grid_consta
         if (el) {
 #pragma unroll
           for (int kk = 0; kk < kKeys / 16; ++kk) mma_ts2(tmem + D * i, tmem + C::col_p(i) + kk * 8, v_lo + kk * (32 >> 4), kDescSwizzled, idesc_o, kk > 0 || k > 0);
+          if constexpr (FINE) {
+#pragma unroll
+            for (int kk = 0; kk < kKeys / 16; ++kk) mma_ts2(tmem + D * i, tmem + C::col_p(i) + C::kRest + kk * 8, v_lo + kk * (32 >> 4), kDescSwizzled, idesc_o, 1);
+          }
           if (C::kOwnP) umma_commit(bar_pfree(i));
           if (n + step >= count) umma_commit(bar_o(i));
         }
