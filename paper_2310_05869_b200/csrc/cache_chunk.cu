@@ -533,10 +533,10 @@ __global__ void __launch_bounds__(kCThreads, 1) chunk_kernel(const __grid_consta
             for (int g = 0; g < G; ++g) { sk[half][g] &= keep_k; mk[half][g] &= keep_k; sv[half][g] &= keep_v; mv[half][g] &= keep_v; }
           }
         }
+        auto bad_of = [](uint32_t x) { return ((x & 0x7fff7fffu) + 0x04000400u) & 0x80008000u; };          // an exponent of ones carries into the sign's place
         // values that are no numbers
         {
           uint32_t any = 0;
-          auto bad_of = [](uint32_t x) { return ((x & 0x7fff7fffu) + 0x04000400u) & 0x80008000u; };        // an exponent of ones carries into the sign's place
 #pragma unroll
           for (int half = 0; half < 2; ++half)
 #pragma unroll
@@ -561,7 +561,16 @@ __global__ void __launch_bounds__(kCThreads, 1) chunk_kernel(const __grid_consta
             top_s = __hmax2(top_s, as_half2(sk[half][g])); top_m = __hmax2(top_m, __habs2(as_half2(mk[half][g])));
             vtop_s = __hmax2(vtop_s, as_half2(sv[half][g])); vtop_m = __hmax2(vtop_m, __habs2(as_half2(mv[half][g])));
           }
-        const int ek = __reduce_max_sync(0xffffffffu, exponent_of(as_u32(top_s), as_u32(top_m))), ev = __reduce_max_sync(0xffffffffu, exponent_of(as_u32(vtop_s), as_u32(vtop_m)));
+        int mine_k = exponent_of(as_u32(top_s), as_u32(top_m));
+        // (K's infinities are still there, and one would hide the other tokens' numbers: then one by one.  V's are gone)
+        if (__any_sync(0xffffffffu, bad_of(as_u32(top_s)) | bad_of(as_u32(top_m)))) {
+          mine_k = 0;
+#pragma unroll
+          for (int half = 0; half < 2; ++half)
+#pragma unroll
+            for (int g = 0; g < G; ++g) mine_k = max(mine_k, exponent_of(sk[half][g], mk[half][g]));
+        }
+        const int ek = __reduce_max_sync(0xffffffffu, mine_k), ev = __reduce_max_sync(0xffffffffu, exponent_of(as_u32(vtop_s), as_u32(vtop_m)));
         if (lane == 0) exponents[sub] = ek | ev << 8;
         ok = all_ok(mine);
         if (!ok) break;
