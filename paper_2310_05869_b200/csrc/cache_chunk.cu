@@ -17,7 +17,7 @@
 // The tiles of all segments are one sequence, cut into equal parts, one for each CTA (a first launch of one CTA finds the cuts); pieces of segments that lie in several parts
 // go to the workspace, and a last launch puts them together, in order.
 //
-// Roundings: weights and values enter the second product as fp16 (2^-11 of each), sums of weights before that; O is one chain of products over a part's tokens.  With fp16 queries what the weights'
+// Roundings: weights and values enter the second product as fp16 (2^-11 of each), sums of weights before that; O is a chain of products over 96 tiles at most (kChain).  With fp16 queries what the weights'
 // rounding has lost goes through the product too (results off by 2.8e-4 instead of 3.5e-4 of their size, where rounding them alone is 2.1e-4; 5 requests, 1501 rows 161 -> 200 us; bf16 results,
 // 1.7e-3, do not show it).
 //
@@ -39,6 +39,12 @@ namespace hyperattn {
 namespace {
 
 constexpr int kUnitRows = 128, kBlockRows = 256, kKeys = 64, kCThreads = 640;
+// Tiles of a unit's chain of products, at most.  The tensor cores cut their sums, always downwards, by 1.2 2^-23 of the partial sum for every 16 products on average: values of one sign came out 6e-4 too
+// small after one chain over 131072 tokens, three times what rounding to fp16 does; after chains of 96 tiles (6144 tokens) whose results are added in fp32, 3.6e-5 (fp16
+// queries: 4.3e-5).  A longer segment is several
+// pieces in a row; what they give is added up at the segment's place in the workspace, a thread its row.  us of 2048 rows over 30720 tokens, 32 / 8 heads of 128: without a limit 1267, 128 tiles 1314, 96
+// 1348, 64 1396 (some 20 000 clocks a piece, in which nothing is multiplied).
+constexpr int kChain = 96;
 
 struct ChunkOut {
   void* out;
@@ -48,7 +54,7 @@ struct ChunkOut {
   long long* before;                     // [slots + 1] cost of the row blocks (of all key heads) before each
   int2* block;                           // [slots] request and row block, -1: none
   long long* start;                      // [parts + 1] where a part starts
-  float* part_o;                         // [2 parts][256][d] pieces of outputs, by place
+  float4* part_o;                        // [2 parts][d / 4][256] pieces of outputs, by place
   float2* part_s;                        // [2 parts][256] their references and sums
   int slots, parts;
 };
@@ -137,7 +143,8 @@ struct Piece {                           // of a segment, in a CTA's part
   Span s;
   int tile0, tile1;
   int split;                             // both units have the same rows, and every other tile
-  int place;                             // in the workspace; -1: the segment is finished here
+  int place;                             // in the workspace
+  int begun, more, last;                 // the CTA had the segment's piece before this one, whose results are at that place; it has the next one; the segment is finished here
   __device__ __forceinline__ int last_seen(const ChunkArgs& a, int row) const {       // last token that a row of the segment sees
     const int token = (row0 + row) / (a.q_heads / a.cache.heads);
     return a.causal ? min(s.len - s.rows + token, s.len - 1) : s.len - 1;
@@ -223,7 +230,8 @@ __global__ void __launch_bounds__(kCThreads, 1) chunk_kernel(const __grid_consta
     const uint32_t lane_addr = tmem + ((uint32_t)((warp & 3) * 32) << 16);
     const uint32_t scol = lane_addr + C::kColS + kKeys * i, pcol = lane_addr + C::col_p(i), ocol = lane_addr + D * i, qcol = lane_addr + C::kColQ + (D / 2) * i;
     int done = 0, pieces = 0, tiles = 0;       // tiles of this unit, pieces with rows of it, tiles of the CTA so far
-    int others = 0, splits = 0;                // pieces with rows of unit 1, that were split
+    int others = 0, splits = 0, loaded = 0;    // pieces with rows of unit 1, that were split; queries that this unit has had
+    float scale = 0.f;
     bool ok = true;
     for (int it = 0; ok; ++it) {
       ok = piece_wait(it, std::integral_constant<int, 0>{});
@@ -238,9 +246,8 @@ __global__ void __launch_bounds__(kCThreads, 1) chunk_kernel(const __grid_consta
         const int limit = there ? d.last_seen(a, in_block) : -1;               // last token that the row sees
         const int least = d.last_seen(a, base);                                // the unit's first row
         const size_t at = (size_t)(d.s.first + token) * a.q_heads + d.kv * group + head;
-        // ---- the row's query ----
-        float scale;
-        {
+        // ---- the row's query (that of the piece before is there still) ----
+        if (!d.begun) {
           uint32_t raw[D / 2];
           const T* from = reinterpret_cast<const T*>(a.q) + (long long)(d.s.first + token) * a.q_row + (long long)(d.kv * group + head) * a.q_head;
 #pragma unroll
@@ -276,7 +283,7 @@ __global__ void __launch_bounds__(kCThreads, 1) chunk_kernel(const __grid_consta
           for (int p = 0; p < 3; ++p)
 #pragma unroll
             for (int g = 0; g < G; g += 2) sums[(p * G + g) / 2] = from_float2<__half>(parts[p][g], parts[p][g + 1]);
-          if (pieces > 0) ok = warp_wait<1>(bar_qfree(i), (pieces - 1) & 1, s_abort, status);
+          if (loaded > 0) ok = warp_wait<1>(bar_qfree(i), (loaded - 1) & 1, s_abort, status);
           if (!ok) break;
           tc_fence_after();
 #pragma unroll
@@ -293,6 +300,7 @@ __global__ void __launch_bounds__(kCThreads, 1) chunk_kernel(const __grid_consta
           fence_async_smem();
           tc_fence_before();
           mbar_arrive(bar_q(i));
+          ++loaded;
         }
         float ref = -INFINITY;
         uint64_t sum2 = 0;
@@ -417,7 +425,6 @@ __global__ void __launch_bounds__(kCThreads, 1) chunk_kernel(const __grid_consta
         bool none = ref == -INFINITY && sum == sum;
         ok = warp_wait<5>(bar_o(i), pieces & 1, s_abort, status);
         if (!ok) break;
-        const bool piece = d.place >= 0;
         float times = exp2f((float)-lift), times1 = 0.f;                       // of O; of unit 1's
         if (d.split) {
           ok = warp_wait<18>(bar_o(1), others & 1, s_abort, status);
@@ -436,11 +443,25 @@ __global__ void __launch_bounds__(kCThreads, 1) chunk_kernel(const __grid_consta
           none = none && none1;
         }
         tc_fence_after();
-        if (!piece) { times *= 1.f / sum; times1 *= 1.f / sum; }
-        const size_t place = (size_t)max(d.place, 0) * kBlockRows + in_block;
+        const size_t place = (size_t)d.place * kBlockRows + in_block;
         uint32_t nan = 0;                                                      // groups with a NaN that the row sees
 #pragma unroll
         for (int g = 0; g < G; ++g) nan |= (uint32_t)(s_nan[(it & 1) * 4 + g] <= limit && !none) << g;
+        // the pieces of the segment before this one, which this thread has put at the place
+        const bool begun = d.begun && there;
+        float past = 0.f;                                                      // of what is there
+        if (begun) {
+          const float2 x = o.part_s[place];
+          const bool none1 = x.x == -INFINITY && x.y == 0.f;
+          const float top = fmaxf(ref, x.x), f = ref == -INFINITY ? (none ? 0.f : 1.f) : ex2(ref - top);
+          past = x.x == -INFINITY ? (none1 ? 0.f : 1.f) : ex2(x.x - top);
+          sum = (none ? 0.f : sum * f) + x.y * past;
+          times *= f;
+          times1 *= f;
+          ref = top;
+          none = none && none1;
+        }
+        if (d.last) { const float inv = none ? 0.f : 1.f / sum; times *= inv; times1 *= inv; past *= inv; }
 #pragma unroll
         for (int c = 0; c < D / 32; ++c) {
           uint32_t v[32];
@@ -457,12 +478,24 @@ __global__ void __launch_bounds__(kCThreads, 1) chunk_kernel(const __grid_consta
           }
 #pragma unroll
           for (int e = 0; e < 32; ++e) v[e] = none ? 0u : nan >> c & 1 ? 0x7fffffffu : v[e];
+          if (begun) {
+            const float4* x = o.part_o + ((size_t)d.place * (D / 4) + 8 * c) * kBlockRows + in_block;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+              const float4 y = x[e * kBlockRows];
+              v[4 * e] = __float_as_uint(fmaf(y.x, past, __uint_as_float(v[4 * e])));
+              v[4 * e + 1] = __float_as_uint(fmaf(y.y, past, __uint_as_float(v[4 * e + 1])));
+              v[4 * e + 2] = __float_as_uint(fmaf(y.z, past, __uint_as_float(v[4 * e + 2])));
+              v[4 * e + 3] = __float_as_uint(fmaf(y.w, past, __uint_as_float(v[4 * e + 3])));
+            }
+          }
           if (there) {
-            if (piece || o.out_kind == HYPERATTN_FP32) {
-              float4* to = reinterpret_cast<float4*>((piece ? o.part_o + place * D : reinterpret_cast<float*>(o.out) + at * D) + 32 * c);
+            if (!d.last || o.out_kind == HYPERATTN_FP32) {
+              float4* to = d.last ? reinterpret_cast<float4*>(o.out) + at * (D / 4) + 8 * c : o.part_o + ((size_t)d.place * (D / 4) + 8 * c) * kBlockRows + in_block;
+              const int step = d.last ? 1 : kBlockRows;
 #pragma unroll
               for (int e = 0; e < 8; ++e)
-                to[e] = make_float4(__uint_as_float(v[4 * e]), __uint_as_float(v[4 * e + 1]), __uint_as_float(v[4 * e + 2]), __uint_as_float(v[4 * e + 3]));
+                to[e * step] = make_float4(__uint_as_float(v[4 * e]), __uint_as_float(v[4 * e + 1]), __uint_as_float(v[4 * e + 2]), __uint_as_float(v[4 * e + 3]));
             } else {
               uint4* to = reinterpret_cast<uint4*>(reinterpret_cast<T*>(o.out) + at * D + 32 * c);
 #pragma unroll
@@ -480,7 +513,7 @@ __global__ void __launch_bounds__(kCThreads, 1) chunk_kernel(const __grid_consta
         if (d.split) mbar_arrive(bar_ofree(1));
         ++pieces;
         if (there) {
-          if (piece) o.part_s[place] = make_float2(none ? -INFINITY : ref, none ? 0.f : sum);
+          if (!d.last) o.part_s[place] = make_float2(none ? -INFINITY : ref, none ? 0.f : sum);
           else o.lse[at] = none ? -INFINITY : (ref + log2f(sum)) * 0.6931471805599453f;
         }
       }
@@ -659,7 +692,7 @@ __global__ void __launch_bounds__(kCThreads, 1) chunk_kernel(const __grid_consta
     const bool el = elect_one();
     constexpr uint32_t idesc_s = (1u << 4) | ((uint32_t)(kKeys >> 3) << 17) | ((128u >> 4) << 24);
     constexpr uint32_t idesc_o = (1u << 4) | ((uint32_t)(D >> 3) << 17) | ((128u >> 4) << 24);
-    int tiles = 0, done[2] = {0, 0}, pieces[2] = {0, 0};
+    int tiles = 0, done[2] = {0, 0}, pieces[2] = {0, 0}, queries[2] = {0, 0};
     bool ok = true;
     for (int it = 0; ok; ++it) {
       ok = piece_wait(it, std::integral_constant<int, 9>{});
@@ -667,13 +700,19 @@ __global__ void __launch_bounds__(kCThreads, 1) chunk_kernel(const __grid_consta
       const Piece& d = s_piece[it & 1];
       auto uni = [&](int x) { return __reduce_max_sync(0xffffffffu, x); };
       const bool end = uni(d.end) != 0, split = uni(d.split) != 0, has[2] = {uni(d.units[0]) > 0, split || uni(d.units[1]) > 0};
+      const bool begun = uni(d.begun) != 0, more = uni(d.more) != 0;
       const int count = uni(d.tile1 - d.tile0), step = split ? 2 : 1;
       __syncwarp();
       if (el) mbar_arrive(bar_piecefree(it & 1));
       if (end) break;
+      // (Queries of the piece before: the first scores come as soon as the last ones have been read.  Unit 1 cannot be at its piece's end before unit 0 has put the last piece's results together: both have
+      // tens of tiles then, and the second one's scores come after O has been read.)
 #pragma unroll
       for (int i = 0; i < 2; ++i)
-        if (ok && has[i]) ok = warp_wait<10>(bar_q(i), pieces[i] & 1, s_abort, status);
+        if (ok && has[i]) {
+          if (!begun) ok = warp_wait<10>(bar_q(i), queries[i]++ & 1, s_abort, status);
+          else if constexpr (C::kOwnP) ok = warp_wait<14>(bar_sfree(i), (done[i] - 1) & 1, s_abort, status);
+        }
       if (!ok) break;
       auto wait_tile = [&](int n) { if (ok) ok = warp_wait<11>(bar_op((tiles + n) % NS), ((tiles + n) / NS) & 1, s_abort, status); };
       // tile n, the unit's last one if there is none `step` further
@@ -687,7 +726,7 @@ __global__ void __launch_bounds__(kCThreads, 1) chunk_kernel(const __grid_consta
               mma_ts2(to, tmem + C::kColQ + (D / 2) * i + 8 * ks, (stage | (1u << 16)) + ((part * C::kOffRest + (ks >> 2) * C::kKeySlab + (ks & 3) * 32) >> 4), kDescSwizzled, idesc_s, part + ks > 0);
           mma_ss2(to, ((ubase + C::kOffSums + i * C::kSums) >> 4) | (((kUnitRows * 16u) >> 4) << 16), (stage + (C::kOffMinima >> 4)) | (((kKeys * 16u) >> 4) << 16), kDescPlain, idesc_s, 1);
           umma_commit(bar_s(i));
-          if (n + step >= count) umma_commit(bar_qfree(i));
+          if (n + step >= count && !more) umma_commit(bar_qfree(i));
         }
       };
       // (k: tiles of the unit before it)
@@ -849,10 +888,16 @@ __global__ void __launch_bounds__(kCThreads, 1) chunk_kernel(const __grid_consta
         d.units[1] = k.rows - d.units[0];
         const long long first = x - (rest - d.kv * whole), last = first + whole;               // the segment's
         d.tile0 = (int)((x - first) / k.cost);
-        d.tile1 = (int)((min(last, end) - first) / k.cost);
+        const int tiles = (int)((min(last, end) - first) / k.cost) - d.tile0, most = d.units[1] ? kChain : 2 * kChain, pieces = (tiles + most - 1) / most;        // (that are left here)
+        d.tile1 = d.tile0 + (tiles + pieces - 1) / pieces;
         d.split = d.units[1] == 0 && d.tile1 - d.tile0 > 1;
-        d.place = x == first && last <= end ? -1 : 2 * (int)blockIdx.x + (x > begin ? 1 : 0);
-        x = min(last, end);
+        // (a segment that is finished here as a whole has the place of the part's end for that long)
+        const bool inside = first >= begin && last <= end;
+        d.begun = x > first && x > begin;
+        d.more = pieces > 1;
+        d.last = inside && pieces == 1;
+        d.place = 2 * (int)blockIdx.x + (inside || first > begin ? 1 : 0);
+        x = first + (long long)d.tile1 * k.cost;
       }
       if (it >= 2) ok = warp_wait<17>(bar_piecefree(it & 1), ((it >> 1) - 1) & 1, s_abort, status);
       if (!ok) break;
@@ -900,18 +945,17 @@ __global__ void __launch_bounds__(kPutThreads) put_kernel(const __grid_constant_
     --p1;
     if (p0 == p1) return;                              // finished there
   }
-  constexpr int LANES = D / 4;
-  const int lane = tid % LANES;
-  for (int row = blockIdx.y * kPutRows<D> + tid / LANES; row < k.rows; row += gridDim.y * kPutRows<D>) {
+  const int lane = tid / kPutRows<D>;
+  for (int row = blockIdx.y * kPutRows<D> + tid % kPutRows<D>; row < k.rows; row += gridDim.y * kPutRows<D>) {
     float ref = -INFINITY, sum = 0.f;
     float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
     if (k.tiles > 0)
 #pragma unroll 4
       for (int c = p0; c <= p1; ++c) {
         if (o.start[c] == o.start[c + 1]) continue;
-        const size_t at = (size_t)(2 * c + (c == p0 && o.start[c] < first ? 1 : 0)) * kBlockRows + row;
-        const float2 x = o.part_s[at];
-        const float4 y = *reinterpret_cast<const float4*>(o.part_o + at * D + 4 * lane);
+        const size_t place = 2 * c + (c == p0 && o.start[c] < first ? 1 : 0);
+        const float2 x = o.part_s[place * kBlockRows + row];
+        const float4 y = o.part_o[(place * (D / 4) + lane) * kBlockRows + row];
         const float m = fmaxf(ref, x.x);
         const float f = x.x == -INFINITY ? (x.y == 0.f ? 0.f : 1.f) : ex2(x.x - m), g = ref == -INFINITY ? (sum == 0.f ? 0.f : 1.f) : ex2(ref - m);
         ref = m;
@@ -995,7 +1039,7 @@ extern "C" int hyperattn_cache_chunk_attention(const hyperattn_chunk_params* p) 
   }
   const ChunkShape s = chunk_shape(*p);
   const ChunkOut o = {p->out, p->lse, p->out_dtype, reinterpret_cast<long long*>(ws), reinterpret_cast<int2*>(ws + s.block), reinterpret_cast<long long*>(ws + s.start),
-                      reinterpret_cast<float*>(ws + s.part_o), reinterpret_cast<float2*>(ws + s.part_s), (int)s.slots, s.parts};
+                      reinterpret_cast<float4*>(ws + s.part_o), reinterpret_cast<float2*>(ws + s.part_s), (int)s.slots, s.parts};
   const int subs = p->cache.page_tokens / kBlockTokens, run = subs % 4 == 0 ? 4 : subs & -subs;
   auto go = [&](auto dim, auto type) {
     constexpr int D = decltype(dim)::value;

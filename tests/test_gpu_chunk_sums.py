@@ -1,0 +1,76 @@
+"""Sums over long contexts: chunks of many rows whose segments have a CTA each, so that nothing but the kernels' own limit ends a chain of products."""
+import math
+
+import pytest
+import torch
+
+import paper_2310_05869_b200 as ha
+import chunk_util as CU
+import test_gpu_cache_chunk as TC
+
+pytestmark = pytest.mark.gpu
+
+
+def context(length, heads, d, dtype, change, page=64):
+    """A cache of one request, its table, and K and V in 64 bits as it holds them.  change(k, v, first token): what is stored."""
+    gen = torch.Generator("cuda").manual_seed(7)
+    pages = -(-length // page)
+    cache = ha.cache_pages(pages, heads, d, page)
+    table = torch.randperm(pages, generator=gen, device="cuda").int()[None].contiguous()
+    for a in range(0, length, 8192):
+        n = min(8192, length - a)
+        k, v = (torch.randn(n, heads, d, generator=gen, device="cuda") for _ in range(2))
+        k, v = change(k, v, a)
+        token = torch.arange(a, a + n, device="cuda")
+        ha.cache_store(cache, k.to(dtype), v.to(dtype), (table[0, token // page] * page + token % page).int())
+    k, v = ha.cache_read(cache, table, CU.ints([0, length]), length, dtype=torch.float32)
+    return cache, table, k.double(), v.double()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("heads,rows,length", [((16, 16, 64), 2560, 65536), ((8, 8, 128), 5120, 40000), ((160, 160, 64), 100, 30001)])
+def test_values_of_one_sign_do_not_drift(heads, rows, length, dtype):
+    """The tensor cores cut some 1.2 2^-23 of the partial sum from every sum of 16 products, always downwards; values of one sign show what that comes to.  No chain is longer than 384 sums (fp16
+    queries: 768, the weights' second part among them), so 512 (1024) times 2^-23, and the partial sum is half of the last one on average; roundings of weights, of values and of their sums differ in
+    sign: 2^-11 over the root of the tokens that have weight (thousands) leave less than 1e-5.  (One chain over 65536 tokens: 3e-4.)"""
+    cache, table, k, v = context(length, heads[1], heads[2], CU.TYPES[dtype], lambda k, v, a: (k, 1 + 0.2 * v))
+    q = TC.queries(rows, heads[0], heads[2], CU.TYPES[dtype], scale=0.3)
+    out, lse = ha.cache_chunk_attention(q, cache, table, CU.ints([length]), CU.offsets([rows]), out_dtype=torch.float32)
+    pick = [0, 1, rows // 2, rows - 1]                             # (rows, of which every fourth head or so is looked at)
+    hs = list(range(0, heads[0], max(1, heads[0] // 4)))
+    seen = torch.arange(length, device="cuda") <= torch.tensor(pick, device="cuda")[:, None] + length - rows
+    off = []
+    for h in hs:
+        z = (q[pick, h].double() @ k[:, h].T / math.sqrt(heads[2])).masked_fill(~seen, -math.inf)
+        want = z.softmax(-1) @ v[:, h]
+        off.append(((out[pick, h].double() - want) / want).mean())
+        assert bool((torch.logsumexp(z, -1) - lse[pick, h]).abs().max() <= 2.0 ** -17 * (z.abs() * seen).nan_to_num(0).amax() + 2.0 ** -17)
+    sums = 1024 if dtype == "fp16" else 512
+    drift = float(torch.stack(off).mean().abs())
+    assert drift <= sums / 2 * 2.0 ** -23 + 1e-5, drift
+
+
+@pytest.mark.parametrize("missing", [(0, 9500), (9000, 20000), (100, 23000), (0, 0)])
+@pytest.mark.parametrize("heads,rows", [((16, 16, 64), 2500), ((4, 4, 128), 5000), ((150, 150, 64), 70)])
+def test_pieces_in_a_row(heads, rows, missing):
+    """Stretches without pages, so that rows see nothing in some pieces of their segment; a NaN early and late; values whose size changes."""
+    length, page = 24000, 64
+
+    def change(k, v, a):
+        t = torch.arange(a, a + k.shape[0], device="cuda")[:, None, None]
+        v = torch.where(t < 12000, v * 2.0 ** -12, v)
+        v[((t == 3000) | (t == length - 40)).expand_as(v) & (torch.arange(v.shape[2], device="cuda") == 33)] = math.nan
+        return torch.where(t % 5000 == 77, k * 3, k), v
+
+    cache, table, k, v = context(length, heads[1], heads[2], torch.bfloat16, change, page)
+    first, end = missing[0] // page, missing[1] // page
+    table[0, first:end] = -1
+    there = torch.ones(length, dtype=torch.bool, device="cuda")
+    there[first * page:end * page] = False
+    q = TC.queries(rows, heads[0], heads[2], torch.bfloat16)
+    hs = [0, heads[0] - 1]
+    got = ha.cache_chunk_attention(q, cache, table, CU.ints([length]), CU.offsets([rows]), out_dtype=torch.float32)
+    want = CU.attention(q[:, hs].double(), k[:, hs], v[:, hs], [length], [rows], there=there)
+    CU.check_attention((got[0][:, hs], got[1][:, hs]), want, torch.float32, length, rows)
+    again = ha.cache_chunk_attention(q, cache, table, CU.ints([length]), CU.offsets([rows]), out_dtype=torch.float32)
+    assert torch.equal(again[0].view(torch.int32), got[0].view(torch.int32)) and torch.equal(again[1], got[1])
