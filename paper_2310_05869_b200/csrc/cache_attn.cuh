@@ -637,11 +637,11 @@ __device__ __forceinline__ void weigh_unit(Heads<D, NT>& h, const CacheAttnArgs&
 // where the pieces of a segment lie: see combine
 __device__ __forceinline__ float* piece_at(const CacheAttnArgs& a, long long slot, int head, int d) { return a.part + (slot * a.part_heads + head) * (d + 2); }
 
-template <int D, int NT, bool PAIR, class T, Mode MODE>
+// FINE: what rounding the weights to fp16 has lost enters too (fp16 queries; some rows: also fp32 results, which would show it)
+template <int D, int NT, bool PAIR, class T, Mode MODE, bool FINE = std::is_same<T, __half>::value>
 __global__ void __launch_bounds__(32 * kWarps, ctas_by_registers(NT)) cache_attn_kernel(const __grid_constant__ KernelArgs<MODE> a, int* status) {
   using R = Ring<D, MODE>;
   constexpr int kPerChunk = PAIR ? 4 : 8 * NT;                           // rows (heads) of a chunk
-  constexpr bool FINE = std::is_same<T, __half>::value;
   extern __shared__ __align__(128) uint8_t smem[];
   uint8_t* misc = smem + kWarps * (R::kWarpBytes + R::kKnown + R::kStages * 8);
   volatile int* s_abort = reinterpret_cast<volatile int*>(misc);

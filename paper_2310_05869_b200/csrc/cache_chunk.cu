@@ -17,7 +17,7 @@
 // The tiles of all segments are one sequence, cut into equal parts, one for each CTA (a first launch of one CTA finds the cuts); pieces of segments that lie in several parts
 // go to the workspace, and a last launch puts them together, in order.
 //
-// Roundings: weights and values enter the second product as fp16 (2^-11 of each), sums of weights before that; O is a chain of products over 96 tiles at most (kChain).  With fp16 queries what the weights'
+// Roundings: weights and values enter the second product as fp16 (2^-11 of each), sums of weights before that; O is a chain of products over 96 tiles at most (kChain).  With fp16 queries, or fp32 results, what the weights'
 // rounding has lost goes through the product too (results off by 2.8e-4 instead of 3.5e-4 of their size, where rounding them alone is 2.1e-4; 5 requests, 1501 rows 161 -> 200 us; bf16 results,
 // 1.7e-3, do not show it).
 //
@@ -151,12 +151,12 @@ struct Piece {                           // of a segment, in a CTA's part
   }
 };
 
-template <int D, class T>
+// FINE: what rounding the weights to fp16 has lost goes through the product too
+template <int D, class T, bool FINE>
 __global__ void __launch_bounds__(kCThreads, 1) chunk_kernel(const __grid_constant__ ChunkArgs a, const __grid_constant__ ChunkOut o, int run, int* status) {
   using C = CCfg<D>;
   using B = Block<D>;
   constexpr int G = D / kGroup, NS = C::kStages, NRAW = C::kRawStages;
-  constexpr bool FINE = std::is_same<T, __half>::value;
   constexpr int kAtOnce = FINE ? 16 : 32;        // weights that go to TMEM at a time (their number and the scores, which may be needed once more, are what registers hold)
   extern __shared__ uint8_t smem_[];
   uint8_t* smem = smem_ + (1024 - (smem_u32(smem_) & 1023)) % 1024;
@@ -1041,17 +1041,20 @@ extern "C" int hyperattn_cache_chunk_attention(const hyperattn_chunk_params* p) 
   const ChunkOut o = {p->out, p->lse, p->out_dtype, reinterpret_cast<long long*>(ws), reinterpret_cast<int2*>(ws + s.block), reinterpret_cast<long long*>(ws + s.start),
                       reinterpret_cast<float4*>(ws + s.part_o), reinterpret_cast<float2*>(ws + s.part_s), (int)s.slots, s.parts};
   const int subs = p->cache.page_tokens / kBlockTokens, run = subs % 4 == 0 ? 4 : subs & -subs;
-  auto go = [&](auto dim, auto type) {
+  auto go = [&](auto dim, auto type, auto fine) {
     constexpr int D = decltype(dim)::value;
     using T = decltype(type);
-    cudaError_t e = allow_smem<chunk_kernel<D, T>>(CCfg<D>::kSmem);
+    constexpr auto kernel = chunk_kernel<D, T, decltype(fine)::value>;
+    cudaError_t e = allow_smem<kernel>(CCfg<D>::kSmem);
     if (e == cudaSuccess) e = launch(share_kernel, dim3(1), dim3(kShareThreads), 0, st, a, o);
-    if (e == cudaSuccess) e = launch(chunk_kernel<D, T>, dim3((unsigned)s.parts), dim3(kCThreads), CCfg<D>::kSmem, st, a, o, run, status);
+    if (e == cudaSuccess) e = launch(kernel, dim3((unsigned)s.parts), dim3(kCThreads), CCfg<D>::kSmem, st, a, o, run, status);
     // (as many CTAs as the GPU holds several times over, at most: 64 requests of few rows, 8 heads, had 17 664, most with nothing to do)
     const long long blocks = s.slots * p->cache.kv_heads, most = kBlockRows / kPutRows<D>, want = (32 * kSms + blocks - 1) / blocks;
     if (e == cudaSuccess) e = launch(put_kernel<D, T>, dim3((unsigned)blocks, (unsigned)(want < most ? want : most)), dim3(kPutThreads), 0, st, a, o);
     return status_of(e, "chunk attention");
   };
-  auto of_type = [&](auto dim) { return p->dtype == HYPERATTN_BF16 ? go(dim, __nv_bfloat16()) : go(dim, __half()); };
+  auto of_type = [&](auto dim) {
+    return p->dtype != HYPERATTN_BF16 ? go(dim, __half(), std::true_type()) : p->out_dtype == HYPERATTN_FP32 ? go(dim, __nv_bfloat16(), std::true_type()) : go(dim, __nv_bfloat16(), std::false_type());
+  };
   return p->cache.d == 64 ? of_type(std::integral_constant<int, 64>()) : of_type(std::integral_constant<int, 128>());
 }

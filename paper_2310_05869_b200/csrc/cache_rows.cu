@@ -71,10 +71,10 @@ int launch_few_rows_attention(const hyperattn_chunk_params& p, int most, int* st
     a.starts = reinterpret_cast<int*>(p.workspace);
     a.part = reinterpret_cast<float*>(reinterpret_cast<char*>(p.workspace) + s.starts);
     a.part_heads = s.per_chunk;
-    auto go = [&](auto tiles, auto type) {
+    auto go = [&](auto tiles, auto type, auto fine) {
       constexpr int NT = decltype(tiles)::value > 1 ? 2 : 1;
       constexpr bool PAIR = decltype(tiles)::value == 0;
-      constexpr auto kernel = cache_attn_kernel<D, NT, PAIR, decltype(type), kSomeRows>;
+      constexpr auto kernel = cache_attn_kernel<D, NT, PAIR, decltype(type), kSomeRows, decltype(fine)::value>;
       cudaError_t e = allow_smem<kernel>(R::bytes(kMaxRequests));
       if (e == cudaSuccess) e = launch(kernel, dim3((unsigned)s.ctas), dim3(32 * kWarps), R::bytes(p.requests), st, a, status);
       const long long segments = s.slots * p.cache.kv_heads;
@@ -85,7 +85,9 @@ int launch_few_rows_attention(const hyperattn_chunk_params& p, int most, int* st
       if (e == cudaSuccess) e = launch(join_kernel<D, kSomeRows>, dim3((unsigned)segments, (unsigned)((s.per_chunk + heads - 1) / heads)), dim3(kJoinThreads), 0, st, a, heads);
       return status_of(e, "chunk attention");
     };
-    auto of_type = [&](auto tiles) { return p.dtype == HYPERATTN_BF16 ? go(tiles, __nv_bfloat16()) : go(tiles, __half()); };
+    auto of_type = [&](auto tiles) {
+      return p.dtype != HYPERATTN_BF16 ? go(tiles, __half(), std::true_type()) : p.out_dtype == HYPERATTN_FP32 ? go(tiles, __nv_bfloat16(), std::true_type()) : go(tiles, __nv_bfloat16(), std::false_type());
+    };
     return s.tiles == 0 ? of_type(std::integral_constant<int, 0>{}) : s.tiles == 1 ? of_type(std::integral_constant<int, 1>{}) : of_type(std::integral_constant<int, 2>{});
   });
 }

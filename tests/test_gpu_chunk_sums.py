@@ -74,3 +74,26 @@ def test_pieces_in_a_row(heads, rows, missing):
     CU.check_attention((got[0][:, hs], got[1][:, hs]), want, torch.float32, length, rows)
     again = ha.cache_chunk_attention(q, cache, table, CU.ints([length]), CU.offsets([rows]), out_dtype=torch.float32)
     assert torch.equal(again[0].view(torch.int32), got[0].view(torch.int32)) and torch.equal(again[1], got[1])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("heads,rows", [((4, 4, 64), 3), ((8, 2, 64), 2), ((6, 2, 64), 5), ((4, 1, 128), 1), ((8, 1, 128), 3), ((4, 4, 64), 90), ((2, 1, 128), 70), ((8, 2, 128), 150)])
+def test_fp32_results_show_what_rounding_weights_loses(heads, rows, dtype):
+    """Values that are fp16 numbers and that the cache holds as they are (steps of 1/8 from -1 on), so that nothing but weights is rounded on the way to an fp32 result.  Weights rounded to fp16 alone
+    would leave 2e-4 of it (the root mean square of a rounding to fp16, as many signs as tokens).  In two parts they are 2^-22 off; what is left are the sums: up to 128 of products with values and 33 of
+    scores, 1.2 2^-23 of partial sums each: 2e-5 of the result and 5e-6 in scores of size one.  Twice that is the bound."""
+    length = 1000
+
+    def change(k, v, a):
+        v = (v.mul(4).round().clamp(-8, 7)) / 8
+        groups = v.view(*v.shape[:2], -1, 32)
+        groups[..., 0], groups[..., 1] = -1, 0.875
+        return k, v
+
+    cache, table, k, v = context(length, heads[1], heads[2], CU.TYPES[dtype], change)
+    assert torch.equal(v.half().double(), v) and torch.equal((v * 8).round(), v * 8)
+    q = TC.queries(rows, heads[0], heads[2], CU.TYPES[dtype], scale=0.5)
+    out, lse = ha.cache_chunk_attention(q, cache, table, CU.ints([length]), CU.offsets([rows]), out_dtype=torch.float32)
+    want = CU.attention(q.double(), k, v, [length], [rows])[0]
+    off, want = ((x.unflatten(-1, (-1, 32))[..., 2:]) for x in (out.double() - want, want))        # (not the two that make the steps, whose results are sums of one sign)
+    assert float(off.norm() / want.norm()) <= 5e-5, float(off.norm() / want.norm())
