@@ -41,7 +41,8 @@ struct WCfg {
   static constexpr uint32_t kRawBlock = 10 * D, kRaw = 8 * kRawBlock, kScales = 64 * D;           // K's half of 8 blocks: their codes, then their scales
   static constexpr int kRawStages = D == 128 ? 6 : 8, kQStages = 4;
   static constexpr uint32_t kOffQ = 0, kOffRaw = kQStages * I::kBytes, kOffMisc = kOffRaw + kRawStages * kRaw;
-  static constexpr uint32_t kSmem = kOffMisc + 4096 + 1024;                      // (the images begin at multiples of 1024)
+  static constexpr uint32_t kOffNext = kOffMisc + 4096, kMostRequests = HYPERATTN_PLAN_MAX_REQUESTS;
+  static constexpr uint32_t kSmem = kOffNext + kMostRequests * 2 + 1024;         // (the images begin at multiples of 1024)
   // TMEM columns: keys of two tiles, scores of several images
   static constexpr uint32_t kColS = 2 * KeyCols<D>::kAll;
   static constexpr int kStages = (512 - kColS) / NR < 4 ? (512 - kColS) / NR : 4;
@@ -54,10 +55,11 @@ struct Walk {
   int images, first;                     // of the request; first one with a row that sees one of the tile's tokens
   bool end;
 };
-// the request that tile `tile` of w.request is in, if any
+// The request that tile `tile` of w.request is in, if any.  next: of each request, the next one with tiles (most of a server's places may be without a request; asked one after the other, 1023 of them
+// took 230 us).
 template <int NR>
-__device__ __forceinline__ void walk_request(const ChunkArgs& a, Walk& w, const Place& end) {
-  for (;; ++w.request, w.tile = 0) {
+__device__ __forceinline__ void walk_request(const ChunkArgs& a, Walk& w, const Place& end, const uint16_t* next) {
+  for (;; w.request = next[w.request], w.tile = 0) {
     w.end = w.request > end.request || (w.request == end.request && w.tile >= end.tile) || w.request >= a.requests;
     if (w.end) return;
     w.s = span_of(a, w.request);
@@ -73,20 +75,21 @@ __device__ __forceinline__ void walk_first(const ChunkArgs& a, Walk& w) {
   const int from = w.j * kTileTokens - (w.s.len - w.s.rows);               // first row (token) that sees the tile's first token
   w.first = a.causal && from > 0 ? (int)min((long long)from * (a.q_heads / a.cache.heads) / NR, (long long)w.images) : 0;
 }
+// (out of line: as a part of each role it made all of them slower, 2 requests of 1025 rows 298 -> 340 us)
 template <int NR>
-__device__ __forceinline__ Walk walk_from(const ChunkArgs& a, const Place& begin, const Place& end) {
+__device__ __noinline__ Walk walk_from(const ChunkArgs& a, const Place& begin, const Place& end, const uint16_t* next) {
   Walk w = {};
   w.request = begin.request;
   w.tile = begin.tile;
-  walk_request<NR>(a, w, end);
+  walk_request<NR>(a, w, end, next);
   walk_first<NR>(a, w);
   return w;
 }
 template <int NR>
-__device__ __forceinline__ void walk_on(const ChunkArgs& a, Walk& w, const Place& end) {
+__device__ __forceinline__ void walk_on(const ChunkArgs& a, Walk& w, const Place& end, const uint16_t* next) {
   ++w.tile;
   if (++w.j == w.tiles) { w.j = 0; ++w.head; }
-  if (w.head == a.cache.heads) { ++w.request; w.tile = 0; walk_request<NR>(a, w, end); }
+  if (w.head == a.cache.heads) { w.request = next[w.request]; w.tile = 0; walk_request<NR>(a, w, end, next); }
   else w.end = w.request == end.request && w.tile >= end.tile;
   walk_first<NR>(a, w);
 }
@@ -108,7 +111,10 @@ __global__ void __launch_bounds__(kWThreads, 1) weights_kernel(const __grid_cons
   uint32_t* s_tmem = reinterpret_cast<uint32_t*>(misc + 2048 + 176);
   volatile int* s_abort = reinterpret_cast<volatile int*>(misc + 2048 + 180);
   uint32_t* s_there = reinterpret_cast<uint32_t*>(misc + 2048 + 184);          // [kRawStages] which of a tile's blocks are in the cache
+  uint32_t* s_with = reinterpret_cast<uint32_t*>(misc + 3072);                 // [kMostRequests / 32] a bit a request: it has tiles
+  uint16_t* s_next = reinterpret_cast<uint16_t*>(smem + C::kOffNext);          // [kMostRequests] the next request that has
   const uint32_t bar0 = ubase + C::kOffMisc + 2048 + 232;
+  static_assert(232 + 64 + 8 * (2 * NS + 2 * NQ + 2 * NRAW) <= 1024 && C::kMostRequests / 8 <= 1024, "room for barriers and bits");
   auto bar_key = [&](int b) { return bar0 + 8 * b; };                          // keys of a tile are in TMEM
   auto bar_keyfree = [&](int b) { return bar0 + 16 + 8 * b; };                 // multiplied, factors read
   auto bar_s = [&](int s) { return bar0 + 32 + 8 * s; };                       // scores of an image
@@ -132,6 +138,7 @@ __global__ void __launch_bounds__(kWThreads, 1) weights_kernel(const __grid_cons
     for (int i = 0; i < NRAW; ++i) { mbar_init(bar_raw(i), 1); mbar_init(bar_rawfree(i), 4); }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
+  for (int i = tid; i < (int)C::kMostRequests / 32; i += kWThreads) s_with[i] = 0;
   if (warp == 16) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(s_tmem)) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
@@ -144,9 +151,18 @@ __global__ void __launch_bounds__(kWThreads, 1) weights_kernel(const __grid_cons
   const int group = a.q_heads / a.cache.heads, cap = a.width * a.cache.page, subs = a.cache.page / kBlockTokens;
   places_of<kWThreads>(a.requests, blockIdx.x, gridDim.x, [&](int r) {
     const Span s = span_of(a, r);
-    return make_int2(is_for(a, s) ? (s.len + kTileTokens - 1) / kTileTokens * a.cache.heads : 0, kKeyCost + (int)(((long long)s.rows * group + NR - 1) / NR));
+    const int tiles = is_for(a, s) ? (s.len + kTileTokens - 1) / kTileTokens : 0;
+    if (tiles > 0) atomicOr(&s_with[r >> 5], 1u << (r & 31));
+    return make_int2(tiles * a.cache.heads, kKeyCost + (int)(((long long)s.rows * group + NR - 1) / NR));
   }, s_sums, s_place);
   const Place begin = s_place[0], end = s_place[1];
+  for (int r = tid; r < a.requests; r += kWThreads) {
+    int word = (r + 1) >> 5;
+    uint32_t bits = r + 1 < a.requests ? s_with[word] >> ((r + 1) & 31) << ((r + 1) & 31) : 0u;
+    while (!bits && ++word * 32 < a.requests) bits = s_with[word];
+    s_next[r] = (uint16_t)(bits ? word * 32 + __ffs(bits) - 1 : a.requests);
+  }
+  __syncthreads();
   auto image_at = [&](const Walk& w, int i) { return a.images + ((size_t)(image_slots(w.s.first, w.request, group, NR) + i) * a.cache.heads + w.head) * I::kBytes; };
   bool ok = true;
 
@@ -164,7 +180,7 @@ __global__ void __launch_bounds__(kWThreads, 1) weights_kernel(const __grid_cons
       const int token = w.j * kTileTokens + t;
       return mine && p.before && token < w.s.len - w.s.rows ? p.before[((size_t)w.request * a.cache.heads + w.head) * cap + token] : 0.f;
     };
-    for (Walk w = walk_from<NR>(a, begin, end); !w.end && ok; walk_on<NR>(a, w, end)) {
+    for (Walk w = walk_from<NR>(a, begin, end, s_next); !w.end && ok; walk_on<NR>(a, w, end, s_next)) {
       const int token = w.j * kTileTokens + t, count = w.images - w.first;
       const size_t at = ((size_t)w.request * a.cache.heads + w.head) * cap + token;
       // the group that has the tile's first image puts its results together; the other one has nothing to do with a tile of one image
@@ -268,7 +284,7 @@ __global__ void __launch_bounds__(kWThreads, 1) weights_kernel(const __grid_cons
     const int g = (warp >> 2) & 1, t = tid & 127;
     const uint32_t lane_addr = tmem + ((uint32_t)((warp & 3) * 32) << 16);
     int keyed = 0;
-    for (Walk w = walk_from<NR>(a, begin, end); !w.end && ok; walk_on<NR>(a, w, end)) {
+    for (Walk w = walk_from<NR>(a, begin, end, s_next); !w.end && ok; walk_on<NR>(a, w, end, s_next)) {
       if (w.first >= w.images) continue;
       const int k = keyed++;
       if ((k & 1) != g) continue;
@@ -292,7 +308,7 @@ __global__ void __launch_bounds__(kWThreads, 1) weights_kernel(const __grid_cons
     // ================= products ============================================================================
     const bool el = elect_one();
     int images = 0, keyed = 0;
-    for (Walk w = walk_from<NR>(a, begin, end); !w.end && ok; walk_on<NR>(a, w, end)) {
+    for (Walk w = walk_from<NR>(a, begin, end, s_next); !w.end && ok; walk_on<NR>(a, w, end, s_next)) {
       if (w.first >= w.images) continue;
       const int b = keyed & 1;
       ok = warp_wait<25>(bar_key(b), (keyed >> 1) & 1, s_abort, status);
@@ -316,14 +332,14 @@ __global__ void __launch_bounds__(kWThreads, 1) weights_kernel(const __grid_cons
     // ================= copies of keys ======================================================================
     // A lane has a block of the next four tiles: its page is looked up before their turn comes.
     int keyed = 0;                                         // tiles that have been asked for
-    Walk ahead = walk_from<NR>(a, begin, end);             // the first tile whose pages have not been looked up
+    Walk ahead = walk_from<NR>(a, begin, end, s_next);             // the first tile whose pages have not been looked up
     int left = 0, left1 = 0;                               // tiles that have been, of these four and the next
     struct Asked { int page, place; };                     // (the page's number is looked at when it is needed)
     auto look = [&](int& n) {
       Asked got = {-1, 0};
       n = 0;
 #pragma unroll 1
-      for (; n < 4 && !ahead.end; walk_on<NR>(a, ahead, end)) {
+      for (; n < 4 && !ahead.end; walk_on<NR>(a, ahead, end, s_next)) {
         if (ahead.first >= ahead.images) continue;
         if (lane / 8 == n) {
           const int token = ahead.j * kTileTokens + lane % 8 * kBlockTokens;
@@ -369,7 +385,7 @@ __global__ void __launch_bounds__(kWThreads, 1) weights_kernel(const __grid_cons
   } else {
     // ================= copies of images ====================================================================
     int images = 0;                                        // asked for
-    for (Walk w = walk_from<NR>(a, begin, end); !w.end && ok; walk_on<NR>(a, w, end))
+    for (Walk w = walk_from<NR>(a, begin, end, s_next); !w.end && ok; walk_on<NR>(a, w, end, s_next))
       for (int i = w.first; i < w.images && ok; ++i) {
         const int qs = images % NQ;
         if (images >= NQ) ok = warp_wait<29>(bar_qfree(qs), (images / NQ - 1) & 1, s_abort, status);
