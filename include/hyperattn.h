@@ -453,6 +453,9 @@ typedef struct hyperattn_chunk_params {
   void* stream;
 } hyperattn_chunk_params;
 int hyperattn_cache_chunk_attention(const hyperattn_chunk_params* p);
+/* The same for a caller that knows on the host how many new tokens a request has at most (most_new; 0: it does not).  It says which kernels are launched, no more: without it a call of many single tokens
+ * also launches those for requests of many rows, which costs some 10 us; requests that have more than it says are right all the same, but slow.  The workspace is the same one. */
+int hyperattn_cache_chunk_attention_ex(const hyperattn_chunk_params* p, int most_new);
 int hyperattn_cache_chunk_attention_workspace_bytes(const hyperattn_chunk_params* p, size_t* bytes);
 
 /* Attention weight that every cached token has got so far, for each key head: with q, cu_q, causal as above, n = request r's queries and lse the
@@ -477,6 +480,7 @@ typedef struct hyperattn_weights_params {
   void* stream;
 } hyperattn_weights_params;
 int hyperattn_cache_weights(const hyperattn_weights_params* p);
+int hyperattn_cache_weights_ex(const hyperattn_weights_params* p, int most_new);        /* most_new: as for hyperattn_cache_chunk_attention_ex */
 int hyperattn_cache_weights_workspace_bytes(const hyperattn_weights_params* p, size_t* bytes);
 
 /* Pages for what stays of requests that have grown too long.  Request r is to be cut to keep[r] tokens if 0 <= keep[r] < lengths[r].  Such requests are

@@ -23,7 +23,7 @@ EXPORTS = ["hyperattn_forward", "hyperattn_forward_ex", "hyperattn_forward_host"
            "hyperattn_alpha", "hyperattn_alpha_workspace_bytes", "hyperattn_get_node_projections",
            "hyperattn_cache_plan", "hyperattn_cache_store", "hyperattn_cache_read", "hyperattn_cache_attention",
            "hyperattn_cache_attention_workspace_bytes", "hyperattn_prompt_attention",
-           "hyperattn_cache_chunk_attention", "hyperattn_cache_chunk_attention_workspace_bytes", "hyperattn_cache_weights",
+           "hyperattn_cache_chunk_attention", "hyperattn_cache_chunk_attention_ex", "hyperattn_cache_chunk_attention_workspace_bytes", "hyperattn_cache_weights", "hyperattn_cache_weights_ex",
            "hyperattn_cache_weights_workspace_bytes", "hyperattn_cache_evict_plan", "hyperattn_cache_evict"]
 
 

@@ -81,7 +81,7 @@ __global__ void __launch_bounds__(kShareThreads) share_kernel(const __grid_const
   for (int r = warp; r < a.requests; r += kShareThreads / 32) {
     const Span s = span_of(a, r);
     const int blocks = is_for(a, s) ? (int)(((long long)s.rows * group + kBlockRows - 1) / kBlockRows) : 0;
-    const long long first = image_slots(s.first, r, group, kBlockRows);
+    const long long first = image_slots(s.first, r, group, kBlockRows, a.least);
     for (int b = lane; b < blocks; b += 32) o.block[first + b] = make_int2(r, b);
   }
   __syncthreads();
@@ -974,9 +974,9 @@ __global__ void __launch_bounds__(kPutThreads) put_kernel(const __grid_constant_
 
 // What a call's launches look like, and where its workspace has what
 struct ChunkShape { long long slots; int parts; size_t block, start, part_s, part_o, bytes; };
-ChunkShape chunk_shape(const hyperattn_chunk_params& p) {
+ChunkShape chunk_shape(const hyperattn_chunk_params& p, int least) {
   ChunkShape s;
-  s.slots = image_slots(p.rows, p.requests, p.q_heads / p.cache.kv_heads, kBlockRows) + 1;
+  s.slots = image_slots(p.rows, p.requests, p.q_heads / p.cache.kv_heads, kBlockRows, least) + 1;
   const long long tiles = s.slots * p.cache.kv_heads * (((long long)p.table_width * p.cache.page_tokens + kKeys - 1) / kKeys);
   s.parts = (int)(tiles < kSms ? tiles : kSms);
   auto up = [](size_t x) { return (x + 255) / 256 * 256; };
@@ -987,10 +987,12 @@ ChunkShape chunk_shape(const hyperattn_chunk_params& p) {
   s.bytes = s.part_o + (size_t)s.parts * 2 * kBlockRows * p.cache.d * 4;
   return s;
 }
-// (what the few rows' kernels cannot count: all is for these)
-Kinds chunk_kinds(const hyperattn_chunk_params& p, size_t* bytes) {
-  const Kinds k = kinds_of(p, most_of(p));
-  return k.few && !few_rows_attention(p, bytes) ? Kinds{false, true} : k;
+// The kernels of a call, and what its workspace has for those of few rows (what they cannot count: all is for these)
+Kinds chunk_kinds(const hyperattn_chunk_params& p, Kinds k, size_t* few) {
+  *few = 0;
+  if (k.few && !few_rows_attention(p, k.many, few)) { *few = 0; return {false, true}; }
+  *few = (*few + 255) / 256 * 256;
+  return k;
 }
 
 int check(const hyperattn_chunk_params* p) {
@@ -1009,16 +1011,23 @@ extern "C" int hyperattn_cache_chunk_attention_workspace_bytes(const hyperattn_c
   if (int rc = check(p)) return rc;
   *bytes = 0;
   if (p->requests == 0 || p->rows == 0) return HYPERATTN_OK;
-  const Kinds kinds = chunk_kinds(*p, bytes);
-  if (!kinds.many) return HYPERATTN_OK;
-  const ChunkShape s = chunk_shape(*p);
+  // (whatever a caller says about the most new tokens: without any word there are both kinds if there can be)
+  size_t few, alone = 0;
+  const Kinds any = chunk_kinds(*p, kinds_of(*p, 0), &few);
+  if (any.many) chunk_kinds(*p, {true, false}, &alone);
+  *bytes = few > alone ? few : alone;
+  if (!any.many) return HYPERATTN_OK;
+  const ChunkShape s = chunk_shape(*p, any.few ? most_of(*p) : -1);
   if (s.slots * p->cache.kv_heads > 0x7fffffffLL) return HYPERATTN_UNSUPPORTED_SHAPE;
-  *bytes = (kinds.few ? (*bytes + 255) / 256 * 256 : 0) + s.bytes;
+  *bytes += s.bytes;
   return HYPERATTN_OK;
 }
 
-extern "C" int hyperattn_cache_chunk_attention(const hyperattn_chunk_params* p) {
+extern "C" int hyperattn_cache_chunk_attention(const hyperattn_chunk_params* p) { return hyperattn_cache_chunk_attention_ex(p, 0); }
+
+extern "C" int hyperattn_cache_chunk_attention_ex(const hyperattn_chunk_params* p, int most_new) {
   size_t bytes = 0;
+  if (most_new < 0) return HYPERATTN_INVALID_ARGUMENT;
   if (int rc = hyperattn_cache_chunk_attention_workspace_bytes(p, &bytes)) return rc;
   if (!p->cu_q && p->rows != p->requests) return HYPERATTN_INVALID_ARGUMENT;
   if (p->requests == 0 || p->rows == 0) return HYPERATTN_OK;
@@ -1030,14 +1039,15 @@ extern "C" int hyperattn_cache_chunk_attention(const hyperattn_chunk_params* p) 
   if (int rc = device_status_word(st, &status)) return rc;
   ChunkArgs a = chunk_args(*p);
   char* ws = reinterpret_cast<char*>(p->workspace);
-  const Kinds kinds = chunk_kinds(*p, &bytes);
+  size_t few;
+  const Kinds kinds = chunk_kinds(*p, kinds_of(*p, p->cu_q ? most_new : 1), &few);
   if (kinds.few) {
-    const int rc = launch_few_rows_attention(*p, kinds.many ? most_of(*p) : INT_MAX, status);
+    const int rc = launch_few_rows_attention(*p, kinds.many, status);
     if (rc || !kinds.many) return rc;
     a.least = most_of(*p);
-    ws += (bytes + 255) / 256 * 256;
+    ws += few;
   }
-  const ChunkShape s = chunk_shape(*p);
+  const ChunkShape s = chunk_shape(*p, a.least);
   const ChunkOut o = {p->out, p->lse, p->out_dtype, reinterpret_cast<long long*>(ws), reinterpret_cast<int2*>(ws + s.block), reinterpret_cast<long long*>(ws + s.start),
                       reinterpret_cast<float4*>(ws + s.part_o), reinterpret_cast<float2*>(ws + s.part_s), (int)s.slots, s.parts};
   const int subs = p->cache.page_tokens / kBlockTokens, run = subs % 4 == 0 ? 4 : subs & -subs;

@@ -48,26 +48,26 @@ auto of_dim(int d, F f) { return d == 64 ? f(std::integral_constant<int, 64>{}) 
 
 }  // namespace
 
-bool few_rows_attention(const hyperattn_chunk_params& p, size_t* bytes) {
+bool few_rows_attention(const hyperattn_chunk_params& p, bool both, size_t* bytes) {
   const int group = p.q_heads / p.cache.kv_heads;
   const long long tokens = (long long)p.table_width * p.cache.page_tokens;
   return of_dim(p.cache.d, [&](auto dim) {
     constexpr int D = decltype(dim)::value;
-    const RowsShape s = rows_shape<D, kSomeRows>(p.requests, p.rows, group, p.cache.kv_heads, tokens, kinds_of(p, most_of(p)).many);
+    const RowsShape s = rows_shape<D, kSomeRows>(p.requests, p.rows, group, p.cache.kv_heads, tokens, both);
     *bytes = s.bytes;
     return countable<D, kSomeRows>(s, p.requests, p.cache.kv_heads, tokens);
   });
 }
 
-int launch_few_rows_attention(const hyperattn_chunk_params& p, int most, int* status) {
+int launch_few_rows_attention(const hyperattn_chunk_params& p, bool both, int* status) {
   const int group = p.q_heads / p.cache.kv_heads;
   const cudaStream_t st = reinterpret_cast<cudaStream_t>(p.stream);
-  KernelArgs<kSomeRows> a = rows_args<kSomeRows>(chunk_args(p), most);
+  KernelArgs<kSomeRows> a = rows_args<kSomeRows>(chunk_args(p), both ? most_of(p) : INT_MAX);
   a.out = p.out; a.lse = p.lse; a.out_kind = p.out_dtype;
   return of_dim(p.cache.d, [&](auto dim) {
     constexpr int D = decltype(dim)::value;
     using R = Ring<D, kSomeRows>;
-    const RowsShape s = rows_shape<D, kSomeRows>(p.requests, p.rows, group, p.cache.kv_heads, (long long)p.table_width * p.cache.page_tokens, kinds_of(p, most_of(p)).many);
+    const RowsShape s = rows_shape<D, kSomeRows>(p.requests, p.rows, group, p.cache.kv_heads, (long long)p.table_width * p.cache.page_tokens, both);
     a.starts = reinterpret_cast<int*>(p.workspace);
     a.part = reinterpret_cast<float*>(reinterpret_cast<char*>(p.workspace) + s.starts);
     a.part_heads = s.per_chunk;
@@ -92,18 +92,18 @@ int launch_few_rows_attention(const hyperattn_chunk_params& p, int most, int* st
   });
 }
 
-bool few_rows_weights(const hyperattn_weights_params& p) {
+bool few_rows_weights(const hyperattn_weights_params& p, bool both) {
   const int group = p.q_heads / p.cache.kv_heads;
   const long long tokens = (long long)p.table_width * p.cache.page_tokens;
   return of_dim(p.cache.d, [&](auto dim) {
     constexpr int D = decltype(dim)::value;
-    return countable<D, kWeights>(rows_shape<D, kWeights>(p.requests, p.rows, group, p.cache.kv_heads, tokens, kinds_of(p, most_of(p)).many), p.requests, p.cache.kv_heads, tokens);
+    return countable<D, kWeights>(rows_shape<D, kWeights>(p.requests, p.rows, group, p.cache.kv_heads, tokens, both), p.requests, p.cache.kv_heads, tokens);
   });
 }
 
-int launch_few_rows_weights(const hyperattn_weights_params& p, int most, int* status) {
+int launch_few_rows_weights(const hyperattn_weights_params& p, bool both, int* status) {
   const cudaStream_t st = reinterpret_cast<cudaStream_t>(p.stream);
-  KernelArgs<kWeights> a = rows_args<kWeights>(chunk_args(p), most);
+  KernelArgs<kWeights> a = rows_args<kWeights>(chunk_args(p), both ? most_of(p) : INT_MAX);
   a.lse_in = p.lse; a.before = p.weights; a.weights = p.weights_out; a.decay = p.decay;
   return of_dim(p.cache.d, [&](auto dim) {
     constexpr int D = decltype(dim)::value;
@@ -112,7 +112,7 @@ int launch_few_rows_weights(const hyperattn_weights_params& p, int most, int* st
     a.run = subs % R::kUnit == 0 ? R::kUnit : subs & -subs;
     const long long blocks = (long long)p.cache.num_pages * p.cache.kv_heads * subs;
     if (!encode_words_map(&a.maps.codes, p.cache.pages, blocks, 5 * D, 2 * D, a.run) || !encode_words_map(&a.maps.scales, p.cache.pages, blocks, 5 * D, D / 2, a.run)) return (int)HYPERATTN_UNSUPPORTED_SHAPE;
-    const RowsShape s = rows_shape<D, kWeights>(p.requests, p.rows, p.q_heads / p.cache.kv_heads, p.cache.kv_heads, (long long)p.table_width * p.cache.page_tokens, kinds_of(p, most_of(p)).many);
+    const RowsShape s = rows_shape<D, kWeights>(p.requests, p.rows, p.q_heads / p.cache.kv_heads, p.cache.kv_heads, (long long)p.table_width * p.cache.page_tokens, both);
     auto go = [&](auto tiles, auto type) {
       constexpr auto kernel = cache_attn_kernel<D, decltype(tiles)::value, false, decltype(type), kWeights>;
       cudaError_t e = allow_smem<kernel>(R::bytes(kMaxRequests));

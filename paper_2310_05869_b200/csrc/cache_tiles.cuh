@@ -44,8 +44,12 @@ struct Image {
   static constexpr uint32_t kSlab = NR * 128, kSums = NR * 2 * D, kMinus = kSums + NR * 32, kFactors = kMinus + NR * 4, kFactor = kFactors + NR * 4, kBytes = (kFactor + 4 + 1023) / 1024 * 1024;
 };
 constexpr int kSpread = 12;              // octaves that a row may be smaller than the image's largest and have its factor: 2^-21 of its largest entry are still whole steps
-// The images of a request come after those of the ones before it, wherever those end: r chunks are room for what the earlier requests' last ones do not fill.
-__host__ __device__ __forceinline__ long long image_slots(long long rows_before, int requests_before, int group, int nr) { return rows_before * group / nr + requests_before; }
+// The images of a request come after those of the ones before it, wherever those end: one for each request before is room for what its last one does not fill.  Requests of up to `least` rows have
+// none; so no more than a request for every least + 1 rows needs that room (1024 places of a server with a part of a prompt or two: some tens of megabytes instead of 745).
+__host__ __device__ __forceinline__ long long image_slots(long long rows_before, int requests_before, int group, int nr, int least) {
+  const long long rows = rows_before * group, most = least < 0 ? requests_before : rows / (least + 1);
+  return rows / nr + (most < requests_before ? most : requests_before);
+}
 
 template <int D, int NR, class T>
 __global__ void __launch_bounds__(128) image_kernel(const __grid_constant__ ChunkArgs a, const float* lse, int images, float* out, int unit) {
@@ -61,10 +65,10 @@ __global__ void __launch_bounds__(128) image_kernel(const __grid_constant__ Chun
   int lo = 0, hi = a.requests;                         // the last request whose images start there or before
   while (hi - lo > 1) {
     const int mid = (lo + hi) >> 1;
-    if (image_slots(span_of(a, mid).first, mid, group, NR) <= slot) lo = mid; else hi = mid;
+    if (image_slots(span_of(a, mid).first, mid, group, NR, a.least) <= slot) lo = mid; else hi = mid;
   }
   const Span s = span_of(a, lo);
-  const long long row0 = (slot - image_slots(s.first, lo, group, NR)) * NR, rows = (long long)s.rows * group;
+  const long long row0 = (slot - image_slots(s.first, lo, group, NR, a.least)) * NR, rows = (long long)s.rows * group;
   if (row0 < 0 || row0 >= rows || !is_for(a, s)) return;
   uint8_t* to = a.images + (size_t)blockIdx.x * I::kBytes;
   __shared__ int s_exp[NR], s_most, s_apart;

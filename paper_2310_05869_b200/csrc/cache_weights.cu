@@ -163,7 +163,7 @@ __global__ void __launch_bounds__(kWThreads, 1) weights_kernel(const __grid_cons
     s_next[r] = (uint16_t)(bits ? word * 32 + __ffs(bits) - 1 : a.requests);
   }
   __syncthreads();
-  auto image_at = [&](const Walk& w, int i) { return a.images + ((size_t)(image_slots(w.s.first, w.request, group, NR) + i) * a.cache.heads + w.head) * I::kBytes; };
+  auto image_at = [&](const Walk& w, int i) { return a.images + ((size_t)(image_slots(w.s.first, w.request, group, NR, a.least) + i) * a.cache.heads + w.head) * I::kBytes; };
   bool ok = true;
 
   if (warp < 8) {
@@ -411,12 +411,9 @@ __global__ void __launch_bounds__(kWThreads, 1) weights_kernel(const __grid_cons
 // rows of an image: a product of 64 rows takes 48 clocks, of 128 rows 64; beside two tiles' keys of d = 128 TMEM has room for the scores of two images of 96
 template <int D> constexpr int kImageRows = D == 64 ? 128 : 96;
 // (what the few rows' kernels cannot count: all is for these)
-Kinds weights_kinds(const hyperattn_weights_params& p) {
-  const Kinds k = kinds_of(p, most_of(p));
-  return k.few && !few_rows_weights(p) ? Kinds{false, true} : k;
-}
-long long slots_of(const hyperattn_weights_params& p) {
-  return image_slots(p.rows, p.requests, p.q_heads / p.cache.kv_heads, p.cache.d == 64 ? kImageRows<64> : kImageRows<128>) + 1;
+Kinds weights_kinds(const hyperattn_weights_params& p, Kinds k) { return k.few && !few_rows_weights(p, k.many) ? Kinds{false, true} : k; }
+long long slots_of(const hyperattn_weights_params& p, int least) {
+  return image_slots(p.rows, p.requests, p.q_heads / p.cache.kv_heads, p.cache.d == 64 ? kImageRows<64> : kImageRows<128>, least) + 1;
 }
 
 }  // namespace
@@ -428,14 +425,21 @@ extern "C" int hyperattn_cache_weights_workspace_bytes(const hyperattn_weights_p
   if (!bytes) return HYPERATTN_INVALID_ARGUMENT;
   if (int rc = check_chunk(p)) return rc;
   *bytes = 0;
-  if (p->requests == 0 || !weights_kinds(*p).many) return HYPERATTN_OK;
-  if (slots_of(*p) * p->cache.kv_heads > 0x7fffffffLL - 2 * kSms) return HYPERATTN_UNSUPPORTED_SHAPE;
-  *bytes = (size_t)(slots_of(*p) * p->cache.kv_heads) * (p->cache.d == 64 ? Image<64, kImageRows<64>>::kBytes : Image<128, kImageRows<128>>::kBytes);
+  if (p->requests == 0) return HYPERATTN_OK;
+  // (whatever a caller says about the most new tokens: without any word there are both kinds if there can be)
+  const Kinds any = weights_kinds(*p, kinds_of(*p, 0));
+  if (!any.many) return HYPERATTN_OK;
+  const long long images = slots_of(*p, any.few ? most_of(*p) : -1) * p->cache.kv_heads;
+  if (images > 0x7fffffffLL - 2 * kSms) return HYPERATTN_UNSUPPORTED_SHAPE;
+  *bytes = (size_t)images * (p->cache.d == 64 ? Image<64, kImageRows<64>>::kBytes : Image<128, kImageRows<128>>::kBytes);
   return HYPERATTN_OK;
 }
 
-extern "C" int hyperattn_cache_weights(const hyperattn_weights_params* p) {
+extern "C" int hyperattn_cache_weights(const hyperattn_weights_params* p) { return hyperattn_cache_weights_ex(p, 0); }
+
+extern "C" int hyperattn_cache_weights_ex(const hyperattn_weights_params* p, int most_new) {
   size_t bytes = 0;
+  if (most_new < 0) return HYPERATTN_INVALID_ARGUMENT;
   if (int rc = hyperattn_cache_weights_workspace_bytes(p, &bytes)) return rc;
   if (!p->cu_q && p->rows != p->requests) return HYPERATTN_INVALID_ARGUMENT;
   if (p->requests == 0) return HYPERATTN_OK;
@@ -444,7 +448,7 @@ extern "C" int hyperattn_cache_weights(const hyperattn_weights_params* p) {
   if (p->workspace_bytes < bytes) return HYPERATTN_WORKSPACE_TOO_SMALL;
   const int subs = p->cache.page_tokens / kBlockTokens, d = p->cache.d;
   WeightArgs w = {chunk_args(*p), p->weights, p->weights_out, p->decay, subs % 8 == 0 ? 8 : subs & -subs};
-  const Kinds kinds = weights_kinds(*p);
+  const Kinds kinds = weights_kinds(*p, kinds_of(*p, p->cu_q ? most_new : 1));
   KeyMaps maps;
   const long long blocks = (long long)p->cache.num_pages * p->cache.kv_heads * subs;
   if (kinds.many && (!encode_words_map(&maps.codes, p->cache.pages, blocks, 5 * d, 2 * d, w.run) || !encode_words_map(&maps.scales, p->cache.pages, blocks, 5 * d, d / 2, w.run))) return HYPERATTN_UNSUPPORTED_SHAPE;
@@ -455,7 +459,7 @@ extern "C" int hyperattn_cache_weights(const hyperattn_weights_params* p) {
   cudaError_t e = sm_count(&sms);
   if (e != cudaSuccess) return status_of(e, "cache weights");
   if (kinds.few) {                               // (these write the zeros behind the tokens too)
-    const int rc = launch_few_rows_weights(*p, kinds.many ? most_of(*p) : INT_MAX, status);
+    const int rc = launch_few_rows_weights(*p, kinds.many, status);
     if (rc || !kinds.many) return rc;
     w.c.least = most_of(*p);
   }
@@ -463,7 +467,7 @@ extern "C" int hyperattn_cache_weights(const hyperattn_weights_params* p) {
     constexpr int D = decltype(dim)::value, NR = kImageRows<D>;
     using C = WCfg<D, NR>;
     cudaError_t e = allow_smem<weights_kernel<D, NR>>(C::kSmem);
-    const int images = (int)(slots_of(*p) * p->cache.kv_heads);
+    const int images = (int)(slots_of(*p, w.c.least) * p->cache.kv_heads);
     auto make = [&](auto kernel) { return launch(kernel, dim3((unsigned)images + (kinds.few ? 0 : 2 * kSms)), dim3(128), 0, st, w.c, p->lse, images, p->weights_out, kTileTokens); };
     if (e == cudaSuccess) e = p->dtype == HYPERATTN_BF16 ? make(image_kernel<D, NR, __nv_bfloat16>) : make(image_kernel<D, NR, __half>);
     const long long tiles = (long long)p->requests * p->cache.kv_heads * (((long long)p->table_width * p->cache.page_tokens + kTileTokens - 1) / kTileTokens);

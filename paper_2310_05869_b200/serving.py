@@ -106,8 +106,8 @@ def _lib():
     for name, args in (("hyperattn_cache_plan", [p]), ("hyperattn_cache_store", [p, p, p, i, i, ll, ll, ll, ll, p, p]),
                        ("hyperattn_cache_read", [p, p, i, i, p, p, i, p, p, i, p]), ("hyperattn_cache_attention", [p]),
                        ("hyperattn_cache_attention_workspace_bytes", [p, C.POINTER(C.c_size_t)]), ("hyperattn_prompt_attention", [p]),
-                       ("hyperattn_cache_chunk_attention", [p]), ("hyperattn_cache_chunk_attention_workspace_bytes", [p, C.POINTER(C.c_size_t)]),
-                       ("hyperattn_cache_weights", [p]), ("hyperattn_cache_weights_workspace_bytes", [p, C.POINTER(C.c_size_t)]),
+                       ("hyperattn_cache_chunk_attention_ex", [p, i]), ("hyperattn_cache_chunk_attention", [p]), ("hyperattn_cache_chunk_attention_workspace_bytes", [p, C.POINTER(C.c_size_t)]),
+                       ("hyperattn_cache_weights_ex", [p, i]), ("hyperattn_cache_weights", [p]), ("hyperattn_cache_weights_workspace_bytes", [p, C.POINTER(C.c_size_t)]),
                        ("hyperattn_cache_evict_plan", [p]), ("hyperattn_cache_evict", [p])):
         getattr(L, name).restype = i
         getattr(L, name).argtypes = args
@@ -349,6 +349,15 @@ def _queries(q, cache, table, lengths, cu_q):
     return c, index, *_rows(q)
 
 
+def _most(most_new):
+    """most_new as the library takes it, 0 for what is not known."""
+    if most_new is None:
+        return 0
+    if most_new < 0:
+        raise HyperAttnError("most_new must not be negative")
+    return max(min(most_new, 0x7fffffff), 1)
+
+
 @functools.lru_cache(4096)
 def _chunk_workspace(*shape):
     """Workspace of hyperattn_cache_chunk_attention: (pages, page_tokens, kv_heads, d, requests, rows, width, q_heads, causal, dtype, out_dtype)."""
@@ -360,13 +369,15 @@ def _chunk_workspace(*shape):
     return size.value
 
 
-def cache_chunk_attention(q, cache, table, lengths, cu_q=None, causal=True, scale=0.0, out_dtype=None, stream=None):
+def cache_chunk_attention(q, cache, table, lengths, cu_q=None, causal=True, scale=0.0, out_dtype=None, stream=None, most_new=None):
     """Attention of several new tokens a request, q [rows, q_heads, d] (bf16 or fp16, any strides), over its cached tokens 0 .. lengths[r] - 1, which
     are theirs too: request r's queries are rows cu_q[r] .. cu_q[r + 1] - 1 (default: one row a request).  causal: a request's last query sees
     all its tokens, every earlier one a token less.  table [requests, width], lengths [requests], cu_q [requests + 1]: int32.  Returns (out
-    [rows, q_heads, d], lse [rows, q_heads]); a query that sees no token gets zeros and -inf, rows beyond cu_q[-1] are not written."""
+    [rows, q_heads, d], lse [rows, q_heads]); a query that sees no token gets zeros and -inf, rows beyond cu_q[-1] are not written.  most_new: how many new tokens a request has at most,
+    if the host knows that (a number); a step of many single tokens is some 10 us faster for it, results are right whatever it is."""
     if stream is not None:
-        return _on_stream(stream, cache_chunk_attention, q, cache, table, lengths, cu_q, causal, scale, out_dtype)
+        return _on_stream(stream, cache_chunk_attention, q, cache, table, lengths, cu_q, causal, scale, out_dtype, most_new=most_new)
+    most = _most(most_new)
     c, index, q, row, head = _queries(q, cache, table, lengths, cu_q)
     T, H, d = q.shape
     R, W = table.shape
@@ -378,9 +389,9 @@ def cache_chunk_attention(q, cache, table, lengths, cu_q=None, causal=True, scal
     causal = 1 if causal else 0
     size = _chunk_workspace(*c[1:], R, T, W, H, causal, dtype, out_code)
     work = _new((size,), torch.uint8, device)
-    _call("hyperattn_cache_chunk_attention", index, _chunk_bytes(
+    _call("hyperattn_cache_chunk_attention_ex", index, _chunk_bytes(
         *c, q.data_ptr(), row, head, out.data_ptr(), lse.data_ptr(), table.data_ptr(), lengths.data_ptr(), 0 if cu_q is None else cu_q.data_ptr(), R, T, W, H, causal, dtype, out_code,
-        scale, work.data_ptr(), size, _stream(index)))
+        scale, work.data_ptr(), size, _stream(index)), most)
     return out, lse
 
 
@@ -402,13 +413,14 @@ def _weights_of(x, name, requests, c, width, index):
     return x.data_ptr()
 
 
-def cache_weights(q, cache, table, lengths, lse, cu_q=None, weights=None, decay=1.0, causal=True, scale=0.0, out=None, stream=None):
+def cache_weights(q, cache, table, lengths, lse, cu_q=None, weights=None, decay=1.0, causal=True, scale=0.0, out=None, stream=None, most_new=None):
     """The attention weight that every cached token has got, summed over queries and the query heads of its key head: decay times what it had (weights; None: nothing)
     plus what these rows give it.  q, cu_q, causal as for cache_chunk_attention, lse [rows, q_heads] (float32) as it or cache_attention returned it.  Tokens of the rows
     themselves - a request's last ones, as many as it has rows - start from nothing.  Returns fp32 [requests, kv_heads, width * page_tokens], zeros beyond a request's tokens; out: the
-    tensor to write it to (it may be `weights`)."""
+    tensor to write it to (it may be `weights`).  most_new: as for cache_chunk_attention."""
     if stream is not None:
-        return _on_stream(stream, cache_weights, q, cache, table, lengths, lse, cu_q, weights, decay, causal, scale, out)
+        return _on_stream(stream, cache_weights, q, cache, table, lengths, lse, cu_q, weights, decay, causal, scale, out, most_new=most_new)
+    most = _most(most_new)
     c, index, q, row, head = _queries(q, cache, table, lengths, cu_q)
     T, H, d = q.shape
     R, W = table.shape
@@ -422,9 +434,9 @@ def cache_weights(q, cache, table, lengths, lse, cu_q=None, weights=None, decay=
     dtype, causal = _code(q.dtype, "q"), 1 if causal else 0
     size = _weights_workspace(*c[1:], R, T, W, H, causal, dtype)
     work = _new((size,), torch.uint8, q.device)
-    _call("hyperattn_cache_weights", index, _weights_bytes(
+    _call("hyperattn_cache_weights_ex", index, _weights_bytes(
         *c, q.data_ptr(), row, head, lse.data_ptr(), before, to, table.data_ptr(), lengths.data_ptr(), 0 if cu_q is None else cu_q.data_ptr(), R, T, W, H, causal, dtype,
-        scale, decay, work.data_ptr(), size, _stream(index)))
+        scale, decay, work.data_ptr(), size, _stream(index)), most)
     return out
 
 
