@@ -436,7 +436,7 @@ int hyperattn_prompt_attention(const hyperattn_prompt_params* p);
  * 32 coordinates), other queries do not notice.  Offsets that do not ascend leave the results of the rows concerned undefined, nothing else.
  * Queries enter the products as fp16 (after a power of two that brings a row's largest entry near one, or near 2^9), keys as they are stored, so scores are sums in fp32 of exact products.
  * Weights enter the second product as fp16 (2^-11; with fp16 queries, and for fp32 results, what that loses too), values of requests of many rows as fp16 as well (2^-11).  Sums of weights, outputs and the log-sum-exp are fp32;
- * outputs of requests of many rows are fp32 sums of chains of at most 384 products of 16 tokens (where weights come in two parts: 768), from each of whose sums some 1.2 2^-23 of the partial sum is cut: up to 5e-5 for values of one sign.  Which kernels a request's rows meet depends on what else the
+ * outputs of requests of many rows are fp32 sums of chains over at most 6144 tokens (bf16 results: 32768), in which 1.2 2^-23 of the partial sum is cut for every 16: values of one sign come out up to 5e-5 (1.5e-4) too small.  Which kernels a request's rows meet depends on what else the
  * call is made of, so results may differ by such a rounding with it; the same call gives the same bits.
  * requests <= 4096; rows * q_heads < 2^31; table_width * page_tokens < 2^31 - 2^16. */
 typedef struct hyperattn_chunk_params {

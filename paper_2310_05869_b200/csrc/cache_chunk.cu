@@ -17,7 +17,7 @@
 // The tiles of all segments are one sequence, cut into equal parts, one for each CTA (a first launch of one CTA finds the cuts); pieces of segments that lie in several parts
 // go to the workspace, and a last launch puts them together, in order.
 //
-// Roundings: weights and values enter the second product as fp16 (2^-11 of each), sums of weights before that; O is a chain of products over 96 tiles at most (kChain).  With fp16 queries, or fp32 results, what the weights'
+// Roundings: weights and values enter the second product as fp16 (2^-11 of each), sums of weights before that; O is a chain of products over 96 or 512 tiles at most (kChain).  With fp16 queries, or fp32 results, what the weights'
 // rounding has lost goes through the product too (results off by 2.8e-4 instead of 3.5e-4 of their size, where rounding them alone is 2.1e-4; 5 requests, 1501 rows 161 -> 200 us; bf16 results,
 // 1.7e-3, do not show it).
 //
@@ -40,11 +40,11 @@ namespace {
 
 constexpr int kUnitRows = 128, kBlockRows = 256, kKeys = 64, kCThreads = 640;
 // Tiles of a unit's chain of products, at most.  The tensor cores cut their sums, always downwards, by 1.2 2^-23 of the partial sum for every 16 products on average: values of one sign came out 6e-4 too
-// small after one chain over 131072 tokens, three times what rounding to fp16 does; after chains of 96 tiles (6144 tokens) whose results are added in fp32, 3.6e-5 (fp16
-// queries: 4.3e-5).  A longer segment is several
-// pieces in a row; what they give is added up at the segment's place in the workspace, a thread its row.  us of 2048 rows over 30720 tokens, 32 / 8 heads of 128: without a limit 1267, 128 tiles 1314, 96
-// 1348, 64 1396 (some 20 000 clocks a piece, in which nothing is multiplied).
-constexpr int kChain = 96;
+// small after one chain over 131072 tokens, three times what rounding to fp16 does.  After chains of 96 tiles (6144 tokens) whose results are added in fp32 they are 4.3e-5 too small, after 512 tiles
+// 1.4e-4, a twelfth of what rounding to bf16 does: that for bf16 results, which so hardly ever pay for it.  A longer segment is several pieces in a row; what they give is added up at the segment's place in
+// the workspace, a thread its row.  us of 2048 rows over 30720 tokens, 32 / 8 heads of 128: without a limit 1267, 128 tiles 1314, 96 1348, 64 1396 (some 20 000 clocks a piece, in which
+// nothing is multiplied).
+template <bool FINE> constexpr int kChain = FINE ? 96 : 512;
 
 struct ChunkOut {
   void* out;
@@ -888,7 +888,7 @@ __global__ void __launch_bounds__(kCThreads, 1) chunk_kernel(const __grid_consta
         d.units[1] = k.rows - d.units[0];
         const long long first = x - (rest - d.kv * whole), last = first + whole;               // the segment's
         d.tile0 = (int)((x - first) / k.cost);
-        const int tiles = (int)((min(last, end) - first) / k.cost) - d.tile0, most = d.units[1] ? kChain : 2 * kChain, pieces = (tiles + most - 1) / most;        // (that are left here)
+        const int tiles = (int)((min(last, end) - first) / k.cost) - d.tile0, most = d.units[1] ? kChain<FINE> : 2 * kChain<FINE>, pieces = (tiles + most - 1) / most;        // (that are left here)
         d.tile1 = d.tile0 + (tiles + pieces - 1) / pieces;
         d.split = d.units[1] == 0 && d.tile1 - d.tile0 > 1;
         // (a segment that is finished here as a whole has the place of the part's end for that long)

@@ -50,6 +50,25 @@ def test_values_of_one_sign_do_not_drift(heads, rows, length, dtype):
     assert drift <= sums / 2 * 2.0 ** -23 + 1e-5, drift
 
 
+def test_bf16_results_do_not_drift_either():
+    """Chains of 2048 sums at most (32768 tokens): 1.5e-4 by the rule above, beside what rounding to bf16 leaves.  Rows of one coordinate do not count as different samples of that: over 131072 tokens
+    their results differ by 0.2 / 2^8.5 = 5e-4 of their size, less than half a step of 2^-8, and are mostly rounded to the same number.  So the mean is that of 16 heads x 64 coordinates, 1.7e-3 / 32 = 5.3e-5
+    off; four times that are allowed.  (One chain over all tokens: 6e-4.)  Values are spread from one to two, as results near one number would all be rounded to it."""
+    length, rows, heads, d = 131072, 2560, 16, 64
+    size = 1 + torch.arange(heads * d, device="cuda").view(heads, d) * 0.6180339887 % 1
+    cache, table, k, v = context(length, heads, d, torch.bfloat16, lambda k, v, a: (k, size * (1 + 0.2 * v)))
+    q = TC.queries(rows, heads, d, torch.bfloat16, scale=0.3)
+    out, lse = ha.cache_chunk_attention(q, cache, table, CU.ints([length]), CU.offsets([rows]))
+    pick = torch.arange(0, rows, rows // 16, device="cuda")
+    seen = torch.arange(length, device="cuda") <= pick[:, None] + length - rows
+    off = []
+    for h in range(heads):
+        want = (q[pick, h].double() @ k[:, h].T / math.sqrt(d)).masked_fill(~seen, -math.inf).softmax(-1) @ v[:, h]
+        off.append(((out[pick, h].double() - want) / want).mean())
+    drift = float(torch.stack(off).mean().abs())
+    assert drift <= 1.5e-4 + 4 * 1.7e-3 / 32, drift
+
+
 @pytest.mark.parametrize("missing", [(0, 9500), (9000, 20000), (100, 23000), (0, 0)])
 @pytest.mark.parametrize("heads,rows", [((16, 16, 64), 2500), ((4, 4, 128), 5000), ((150, 150, 64), 70)])
 def test_pieces_in_a_row(heads, rows, missing):
