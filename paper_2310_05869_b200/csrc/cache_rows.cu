@@ -88,7 +88,10 @@ int launch_few_rows_attention(const hyperattn_chunk_params& p, bool both, int* s
     auto of_type = [&](auto tiles) {
       return p.dtype != HYPERATTN_BF16 ? go(tiles, __half(), std::true_type()) : p.out_dtype == HYPERATTN_FP32 ? go(tiles, __nv_bfloat16(), std::true_type()) : go(tiles, __nv_bfloat16(), std::false_type());
     };
-    return s.tiles == 0 ? of_type(std::integral_constant<int, 0>{}) : s.tiles == 1 ? of_type(std::integral_constant<int, 1>{}) : of_type(std::integral_constant<int, 2>{});
+    // (d = 128: never two tiles, see rows_shape)
+    if constexpr (D == 64)
+      if (s.tiles == 2) return of_type(std::integral_constant<int, 2>{});
+    return s.tiles == 0 ? of_type(std::integral_constant<int, 0>{}) : of_type(std::integral_constant<int, 1>{});
   });
 }
 
