@@ -191,7 +191,10 @@ __global__ void __launch_bounds__(kCThreads, 1) chunk_kernel(const __grid_consta
   const int warp = __shfl_sync(0xffffffffu, tid >> 5, 0);
   if (tid == 0) *s_abort = *reinterpret_cast<volatile int*>(status);
   __syncthreads();
-  if (*s_abort) return;
+  if (*s_abort) {
+    wait_for_stream();                                 // (the last launch reads what the first one wrote: this one may not be over before it)
+    return;
+  }
   __syncthreads();
   if (tid == 0) {
     for (int i = 0; i < 2; ++i) {
