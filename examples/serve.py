@@ -1,7 +1,7 @@
 """A small server of a decoder: prompts of different lengths come and go, their keys and values are kept in a paged 4-bit cache.
 
     python examples/serve.py                 # random weights; prints what it generated and how long a step took
-    python examples/serve.py --keep 512      # the same with contexts that are cut to 512 tokens
+    python examples/serve.py --keep 512      # the same prompts with contexts that are cut to 512 tokens; no layer is approximated then
 
 Every step schedules the cache's pages (cache_plan), runs the new tokens of all requests as one packed batch - whole prompts for
 requests that have just come, one token for the others - and, layer by layer, stores their keys and values (cache_store) and attends:
@@ -12,8 +12,8 @@ to its cached part, read back (cache_read), and to itself.
 With `keep`, no request has more than that many tokens for long: all rows of a step attend to what is cached of their requests, their
 own tokens included (cache_chunk_attention), the weight that every cached token gets is added up (cache_weights), and requests that
 have grown too long are cut to the first and the last tokens and those of most weight (cache_evict_plan, and cache_evict for every
-layer).  This is a loop to read, not a server: everything outside the library's
-calls is plain torch."""
+layer).  The weights are those of exact attention, so a model with approximated layers is refused.  This is a loop to read, not a
+server: everything outside the library's calls is plain torch."""
 from __future__ import annotations
 
 import math
@@ -67,6 +67,8 @@ class Decoder:
 
 class Server:
     def __init__(self, model, requests=8, pages=64, page_tokens=64, longest=2048, long_prompt=1 << 30, keep=0, recent=32, first=4):
+        if keep and model.approximated:
+            raise ValueError("keep needs a model without approximated layers")
         self.model, self.page, self.long_prompt, self.keep, self.recent, self.first = model, page_tokens, long_prompt, keep, recent, first
         self.caches = [ha.cache_pages(pages, model.kv_heads, model.d, page_tokens) for _ in model.layers]
 
@@ -93,15 +95,8 @@ class Server:
         if rows == 0:
             return {}
         tokens = torch.tensor([t for request in new if request for t in request], device="cuda")
-        held = before.tolist()                                     # (a real server knows the lengths it has sent)
         admitted = {r for r, ok in enumerate((plan.lengths > before).tolist()) if ok}
-        single = [r for r, n in enumerate(count) if n == 1 and r in admitted]
-        prompts = [r for r, n in enumerate(count) if n > 1 and r in admitted]
         first = plan.cu_new.tolist()
-        rows_of_single = torch.tensor([first[r] for r in single], device="cuda", dtype=torch.long)
-        at = torch.tensor(single, device="cuda", dtype=torch.long)
-        table1, lengths1 = plan.table[at].contiguous(), plan.lengths[at].contiguous()
-
         if self.keep:
             # rows of the requests that were admitted, one after the other (all of them, nearly always)
             mine = sorted(admitted)
@@ -110,17 +105,25 @@ class Server:
             pick = torch.cat([torch.arange(first[r], first[r + 1]) for r in mine]).cuda()
             cu = torch.tensor([0] + [count[r] if r in admitted else 0 for r in range(len(new))]).cumsum(0).int().cuda()
             moved = torch.repeat_interleave(self.gone, plan.cu_new.diff(), output_size=rows)
+            most = max(count)
 
             def attend_cached(layer, q, k, v):
                 cache = self.caches[layer]
                 ha.cache_store(cache, k, v, plan.slots)
                 q1 = q if pick.shape[0] == rows else q[pick]
-                got, lse = ha.cache_chunk_attention(q1, cache, plan.table, plan.lengths, cu)
-                ha.cache_weights(q1, cache, plan.table, plan.lengths, lse, cu, weights=self.weights[layer], out=self.weights[layer])
+                got, lse = ha.cache_chunk_attention(q1, cache, plan.table, plan.lengths, cu, most_new=most)
+                ha.cache_weights(q1, cache, plan.table, plan.lengths, lse, cu, weights=self.weights[layer], out=self.weights[layer], most_new=most)
                 return got if pick.shape[0] == rows else torch.zeros_like(q).index_copy_(0, pick, got)
 
             logits = model.run(tokens, plan.positions.clamp(min=0) + moved, attend_cached)
             return {r: logits[first[r + 1] - 1] for r in mine}
+
+        held = before.tolist()                                     # (a real server knows the lengths it has sent)
+        single = [r for r, n in enumerate(count) if n == 1 and r in admitted]
+        prompts = [r for r, n in enumerate(count) if n > 1 and r in admitted]
+        rows_of_single = torch.tensor([first[r] for r in single], device="cuda", dtype=torch.long)
+        at = torch.tensor(single, device="cuda", dtype=torch.long)
+        table1, lengths1 = plan.table[at].contiguous(), plan.lengths[at].contiguous()
 
         def attend(layer, q, k, v):
             out = torch.zeros_like(q)
@@ -163,7 +166,7 @@ class Server:
 
 
 def main(keep=0):
-    server = Server(Decoder(layers=4, approximated={3}), requests=4, pages=200, longest=8192, long_prompt=4096, keep=keep)
+    server = Server(Decoder(layers=4, approximated=() if keep else {3}), requests=4, pages=200, longest=8192, long_prompt=4096, keep=keep)
     gen = torch.Generator().manual_seed(1)
     waiting = [torch.randint(0, 512, (n,), generator=gen).tolist() for n in (5, 700, 5000, 64, 1, 300)]
     said = {r: [] for r in range(len(waiting))}
