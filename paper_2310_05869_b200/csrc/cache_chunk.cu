@@ -18,12 +18,12 @@
 // go to the workspace, and a last launch puts them together, in order.
 //
 // Roundings: weights and values enter the second product as fp16 (2^-11 of each), sums of weights before that; O is a chain of products over 96 or 512 tiles at most (kChain).  With fp16 queries, or fp32 results, what the weights'
-// rounding has lost goes through the product too (results off by 2.8e-4 instead of 3.5e-4 of their size, where rounding them alone is 2.1e-4; 5 requests, 1501 rows 161 -> 200 us; bf16 results,
-// 1.7e-3, do not show it).
+// rounding has lost goes through the product too (results off by 2.8e-4 instead of 3.5e-4 of their size, where rounding them alone is 2.1e-4; 5 requests, 1501 rows 161 -> 200 us when
+// that was added; bf16 results, 1.7e-3, do not show it).
 //
 // What bounds it: a tile of 64 tokens and 256 rows takes about 2300 clocks, near which lie its conversion, its 42 products (d = 128; half of those for scores are what exact keys cost) and the
-// hand-overs of the softmax.  2048 rows over 30720 tokens, 32 / 8 heads of 128: 1285 us for a floor of 636 (tensor pipe 61 %, issue 55 %); 5 requests, 1501 rows over up to 5000 tokens, 32 heads
-// of 64, fp16: 200 us (with single weights 162: tensor pipe 31 %, issue 50 %), of which the first and the last launch take 10.  Two halves of a row block of up to 128 rows: 64 rows over 8000 tokens, 32 heads of 64, 8
+// hand-overs of the softmax.  2048 rows over 30720 tokens, 32 / 8 heads of 128: 1261 us for a floor of 636 (tensor pipe 62 %, issue 56 %); 5 requests, 1501 rows over up to 5393 tokens, 32 heads
+// of 64, fp16: 181 us (tensor pipe 36 %, issue 57 %), of which the first and the last launch take 10.  Two halves of a row block of up to 128 rows: 64 rows over 8000 tokens, 32 heads of 64, 8
 // requests 297 -> 242 us.
 //
 // Warp roles (640 threads): 0-3 and 4-7 softmax and results of unit 0 and 1, 8-11 and 12-15 keys and values of even and odd tiles, 16 products (and TMEM), 17 copies, 18 segments, 19

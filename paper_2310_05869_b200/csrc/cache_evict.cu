@@ -117,7 +117,7 @@ __device__ __forceinline__ uint32_t order_of(float w) { return w > 0.f ? __float
 
 // A cluster of CTAs takes a request and key head, each a slice of its tokens, whose weights (in order) it holds in shared memory if they fit.  The smallest weight that stays is
 // found by three digits of 10, 11 and 10 bits, from the top: a histogram in each CTA, which all add up for themselves.  Then every warp counts a part of the slice, and numbers it.
-// 2 x 131072 tokens, 32 heads, to 8192 each: 57 us (115 with four digits of 8 bits), of 15 for its bytes: two waves of clusters, instructions and latencies between the digits.  32 requests up to 8192
+// 131072 tokens to 8192 beside a request of 7148 that stays, 32 heads: 57 us (115 with four digits of 8 bits), of 13 for its bytes: two waves of clusters, instructions and latencies between the digits.  32 requests up to 8192
 // tokens, 8 heads: 19 us.
 constexpr int kSelectThreads = 1024, kSelectWarps = kSelectThreads / 32, kBins = 2048, kMostHeld = 40960;
 
@@ -274,7 +274,7 @@ static_assert(kSelectWarps == 32, "a lane for every warp");
 // A warp makes a block of 16 tokens of the new pages at a time, from the blocks that its tokens are in: K by pieces of a token (16 bytes, d = 64: 8), V by 16-byte loads that
 // hold a token's byte of four words, scales and minima one by one.  The blocks of all requests that are cut are one sequence, in equal parts for the warps.
 // 32 requests to 2048 tokens, 8 heads of 128: 41 us (115 MB read where tokens that stay have about 40: sectors are used in part; stalls are those of gathers).
-// With 12 CTAs an SM, of which 9 are there at a time, 127.8 for all of the eviction and its reading back, with 18 or 36 123.5 (2 x 131072 tokens, d = 64: 131.1, 128.6).
+// With 12 CTAs an SM, of which 9 are there at a time, 127.8 for all of the eviction and its reading back, with 18 or 36 123.5 (131072 tokens to 8192, 32 heads of 64: 131.1, 128.6).
 constexpr int kMoveWarps = 4, kMostRequests = HYPERATTN_PLAN_MAX_REQUESTS;
 
 template <int D>
