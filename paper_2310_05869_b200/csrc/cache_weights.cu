@@ -111,7 +111,7 @@ __global__ void __launch_bounds__(kWThreads, 1) weights_kernel(const __grid_cons
   uint32_t* s_tmem = reinterpret_cast<uint32_t*>(misc + 2048 + 176);
   volatile int* s_abort = reinterpret_cast<volatile int*>(misc + 2048 + 180);
   uint32_t* s_there = reinterpret_cast<uint32_t*>(misc + 2048 + 184);          // [kRawStages] which of a tile's blocks are in the cache
-  uint32_t* s_with = reinterpret_cast<uint32_t*>(misc + 3072);                 // [kMostRequests / 32] a bit a request: it has tiles
+  uint32_t* s_with = reinterpret_cast<uint32_t*>(misc + 3 * 1024);                 // [kMostRequests / 32] a bit a request: it has tiles
   uint16_t* s_next = reinterpret_cast<uint16_t*>(smem + C::kOffNext);          // [kMostRequests] the next request that has
   const uint32_t bar0 = ubase + C::kOffMisc + 2048 + 232;
   static_assert(232 + 64 + 8 * (2 * NS + 2 * NQ + 2 * NRAW) <= 1024 && C::kMostRequests / 8 <= 1024, "room for barriers and bits");
